@@ -421,6 +421,133 @@ const char *pdb_strerror(int code);
 int pdb_sgd_epoch_ready_noalloc(const pdb_csr *X, const float *y, const uint32_t *gate, float *w, pdb_loss loss,
                                 float eta, int n_epochs, void *stream);
 
+/* ---------------------------------------------------------------- token models
+ *
+ * Operators of models over tokens: a chunk of the parameter database
+ * (Definition 2) is a row of a table, a token's id names the row it reads and
+ * updates (Definition 3), and an update sums an id's contributions in data
+ * order as Algorithm 2a's write half does (pdb_bsp_apply), with vectors for
+ * scalars.  The softmax losses take the place of pdb_loss.  The paper has no
+ * formulas for them; each declaration gives its own.
+ *
+ * Every call takes a pdb_tokens handle: the workspace of pdb_embed_grad, and
+ * the status word in which the kernels record an id out of range
+ * (pdb_tokens_status).  A recorded error stops no later call: a bad id gives the
+ * result its declaration states.  Calls that share a handle must be ordered on
+ * one stream.  Sums, softmax statistics and losses are held in fp32; a result
+ * in 16 bits is rounded once.  No atomics add floating values: the same inputs
+ * give the same bits.  No call allocates but pdb_tokens_create, and all but
+ * pdb_tokens_create and pdb_tokens_status can be recorded into a CUDA graph.
+ * PDB_LOG prints nothing for these calls. */
+
+/* Element types of a matrix: 32-bit, bfloat16, IEEE half. */
+typedef enum { PDB_TYPE_FLOAT = 0, PDB_TYPE_BFLOAT = 1, PDB_TYPE_HALF = 2 } pdb_type;
+
+/* rows x cols elements of one type in device memory; element (i, j) at
+ * data[i * stride + j], stride >= cols (elements; any alignment of the element
+ * type; stride is ignored for rows < 2).  Rows and columns may be 0. */
+typedef struct {
+    void *data;
+    int64_t rows, cols, stride;
+    int32_t type; /* a pdb_type value */
+} pdb_mat;
+
+/* n ids in device memory, 64 bits each when wide != 0, else 32: id i at
+ * data[i * stride], stride >= 1 (ids; ignored for n < 2) */
+typedef struct {
+    const void *data;
+    int64_t n, stride;
+    int32_t wide;
+} pdb_ids;
+
+typedef struct pdb_tokens pdb_tokens; /* opaque, library-owned device arrays */
+
+/* Handle for calls of at most max_tokens ids (below 2^31) and, in pdb_embed_grad, rows of at
+ * most max_dim elements; holds about (20 + max_dim / 4) bytes for each of
+ * max_tokens.  Allocates stream-ordered on `stream`.
+ * pdb_tokens_free waits for the work enqueued on the handle, then releases it.
+ * pdb_tokens_status SYNCHRONIZES `stream` and returns the first error that a
+ * kernel recorded in the handle (PDB_OK when none). */
+int pdb_tokens_create(int64_t max_tokens, int64_t max_dim, pdb_tokens **out, void *stream);
+void pdb_tokens_free(pdb_tokens *t);
+int pdb_tokens_status(const pdb_tokens *t, void *stream);
+
+/* out[i, :] = scale * table[ids[i], :]  (ids->n = out->rows, cols equal).
+ * Reads of the chunks that the ids name (Definition 3).  An id equal to `pad`
+ * gives a row of zeros, whatever its value; so does any other id outside [0, table->rows), which
+ * is recorded as PDB_ERANGE.  The product is formed in fp32 and rounded once to
+ * out's type.  out must not overlap the table. */
+int pdb_embed(pdb_tokens *t, const pdb_mat *table, const pdb_ids *ids, float scale, int64_t pad, const pdb_mat *out,
+              void *stream);
+
+/* dtable[v, :] = scale * sum of dout[i, :] over the i with ids[i] = v, i
+ * ascending (the ordered sums of Algorithm 2a's writes), 0 for an id that does not
+ * occur; with accumulate != 0 the sum is added to dtable[v, :] and the other
+ * rows are not touched, so that dtable = the table and scale = -eta * scale of
+ * pdb_embed make the SGD step in place.  Ids equal to `pad` are left out; so are
+ * other ids outside [0, dtable->rows), which are recorded as PDB_ERANGE.
+ * The ids are sorted with a stable sort; a run of equal ids is summed in fp32
+ * in pieces of 32 sorted positions, the pieces then in order; rounded once to
+ * dtable's type after the old value is added.  dout must not overlap dtable.
+ * PDB_ETOOBIG beyond the handle's max_tokens or max_dim. */
+int pdb_embed_grad(pdb_tokens *t, const pdb_ids *ids, const pdb_mat *dout, float scale, int64_t pad, int accumulate,
+                   const pdb_mat *dtable, void *stream);
+
+/* Per row of logits (z = scale * logits, scale > 0 the inverse temperature,
+ * p = softmax of z):
+ *   lse[r]      log sum_j exp z_j
+ *   logp[r]     z_t - lse, t = ids[r]
+ *   entropy[r]  - sum_j p_j log p_j   (terms with p_j = 0 are 0)
+ *   top_logp[r, 0..k), top_ids[r, 0..k)   the k largest logits, descending, ties
+ *               by the lower id, as log probabilities, and their ids
+ *               (row-major, k <= 64 and k <= cols; a NaN counts as largest)
+ * Any output may be NULL (ids too, when logp is).  Where ids[r] = `ignore`,
+ * logp[r] = 0; so also for any other id outside [0, cols), recorded as PDB_ERANGE.
+ * A logit of -inf is a token that the mask leaves out.  A row with nothing left
+ * has lse = logp = top_logp = -inf and entropy 0; a row that holds a NaN or
+ * +inf has NaN for lse, logp, entropy and top_logp. */
+int pdb_logprobs(pdb_tokens *t, const pdb_mat *logits, const pdb_ids *ids, float scale, int64_t ignore, float *logp,
+                 float *lse, float *entropy, int64_t k, float *top_logp, int32_t *top_ids, void *stream);
+
+/* Gradient of sum_r (dlogp[r] * logp[r] + dentropy[r] * entropy[r]) with
+ * respect to the logits, lse and entropy as pdb_logprobs gave them:
+ *   dlogits[r, j] = scale * (dlogp[r] * ([j = t] - p_j) - dentropy[r] * p_j * (log p_j + entropy[r]))
+ * dlogp or dentropy may be NULL (zero); entropy is read with dentropy only,
+ * ids with dlogp only.  A row whose two coefficients are 0 (dlogp counts as 0 where
+ * pdb_logprobs leaves ids[r] out) or that has nothing left gets zeros, whatever it
+ * holds.  dlogits may be the logits' own memory (same data, stride and type);
+ * it must not overlap them otherwise. */
+int pdb_logprobs_grad(pdb_tokens *t, const pdb_mat *logits, const pdb_ids *ids, float scale, int64_t ignore,
+                      const float *lse, const float *entropy, const float *dlogp, const float *dentropy,
+                      const pdb_mat *dlogits, void *stream);
+
+/* Distillation from a teacher's top logits: row r of the student's logits
+ * against K = top_logits->cols teacher logits (K <= 1024), slot k being token
+ * top_ids->data[r * top_ids->stride + k]: here n = rows * K and stride, at least K,
+ * is that of the rows.  With T = temperature > 0, p = softmax of logits[r] / T:
+ *   teacher_lse == NULL   q_k = softmax of top_logits[r] / T over the row's slots
+ *     loss[r] = T^2 * sum_k q_k (log q_k - log p_k)
+ *   else   teacher_lse[r] = log sum exp of ALL the teacher's logits / T,
+ *     q_k = exp(top_logits[r, k] / T - teacher_lse[r]), and what is left,
+ *     q_t = 1 - sum_k q_k, stands in one bucket against the student's
+ *     p_t = sum of p over the tokens in no slot: adds T^2 * q_t (log q_t - log p_t).
+ *     q_t <= 1e-6 counts as 0 (the rounding of teacher_lse).
+ * dlogits == NULL: the loss alone.  Else also the gradient of sum_r weight[r] * loss[r]
+ * (weight == NULL: every weight 1), for tokens j:
+ *   in a slot        weight * T * (p_j - sum of q_k over the slots of j)
+ *   in none          weight * T * p_j * (1 - q_t / p_t)  (weight * T * p_j without the bucket)
+ * loss may be NULL then.  A negative id is an empty slot; an id >= cols counts as one and is
+ * recorded as PDB_ERANGE.  Slots of one token add up in q (a teacher that lists a token
+ * twice).  A row without slots, or whose slots all hold -inf, has loss 0 and
+ * gradient 0; a row of weight 0 has gradient 0, whatever it holds; a row of logits with
+ * nothing but -inf has loss +inf and gradient 0.  A NaN in a row makes its loss and gradient NaN.
+ * dlogits may be the logits' own memory (same data, stride and type); it must not overlap
+ * them otherwise.  Reads the logits once from memory when the gradient is asked for
+ * in this call. */
+int pdb_distill(pdb_tokens *t, const pdb_mat *logits, const pdb_ids *top_ids, const pdb_mat *top_logits,
+                const float *teacher_lse, float temperature, float *loss, const float *weight, const pdb_mat *dlogits,
+                void *stream);
+
 /* ---------------------------------------------------------------- utilities */
 
 /* cudaMemcpyAsync with the kind inferred from the pointers (for bindings that

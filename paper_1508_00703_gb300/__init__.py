@@ -31,6 +31,7 @@ NOALLOC_MAX_COLS = 1 << 20
 PDB_LOSS_LOGISTIC, PDB_LOSS_SQUARED, PDB_LOSS_HINGE = 0, 1, 2
 PDB_SCHED_LEVELS, PDB_SCHED_READY, PDB_SCHED_CHAIN, PDB_SCHED_AUTO, PDB_SCHED_WINDOW = 0, 1, 2, 3, 4
 PDB_SSP_COUNT, PDB_SSP_PREFIX = 1, 2
+PDB_TYPE_FLOAT, PDB_TYPE_BFLOAT, PDB_TYPE_HALF = 0, 1, 2
 
 _lock = threading.Lock()
 _lib = None
@@ -106,12 +107,24 @@ class pdb_stats(ctypes.Structure):
         return {k: getattr(self, k) for k, _ in self._fields_}
 
 
+class pdb_mat(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("rows", ctypes.c_int64), ("cols", ctypes.c_int64),
+                ("stride", ctypes.c_int64), ("type", ctypes.c_int32)]
+
+
+class pdb_ids(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("n", ctypes.c_int64), ("stride", ctypes.c_int64),
+                ("wide", ctypes.c_int32)]
+
+
 EXPORTS = ["pdb_build_conflicts", "pdb_conflicts_arrays", "pdb_schedule_build", "pdb_schedule_levels",
            "pdb_schedule_ready",
            "pdb_sgd_epoch", "pdb_bsp_epoch", "pdb_status", "pdb_get_stats", "pdb_conflicts_free",
            "pdb_schedule_free", "pdb_strerror", "pdb_memcpy", "pdb_eval_expf", "pdb_eval_grad", "pdb_launch_count",
            "pdb_sgd_epoch_ready_noalloc", "pdb_ssp_epoch", "pdb_bsp_plan_build", "pdb_bsp_plan_batches",
-           "pdb_bsp_coef", "pdb_bsp_apply", "pdb_bsp_plan_free"]
+           "pdb_bsp_coef", "pdb_bsp_apply", "pdb_bsp_plan_free",
+           "pdb_tokens_create", "pdb_tokens_free", "pdb_tokens_status", "pdb_embed", "pdb_embed_grad", "pdb_logprobs",
+           "pdb_logprobs_grad", "pdb_distill"]
 
 
 def load(path: str | None = None):
@@ -151,6 +164,16 @@ def load(path: str | None = None):
         lib.pdb_bsp_apply.argtypes = [P, P, I64, P, P]
         lib.pdb_bsp_plan_free.argtypes = [P]
         lib.pdb_bsp_plan_free.restype = None
+        M, J, F32 = ctypes.POINTER(pdb_mat), ctypes.POINTER(pdb_ids), ctypes.c_float
+        lib.pdb_tokens_create.argtypes = [I64, I64, PP, P]
+        lib.pdb_tokens_free.argtypes = [P]
+        lib.pdb_tokens_free.restype = None
+        lib.pdb_tokens_status.argtypes = [P, P]
+        lib.pdb_embed.argtypes = [P, M, J, F32, I64, M, P]
+        lib.pdb_embed_grad.argtypes = [P, J, M, F32, I64, I32, M, P]
+        lib.pdb_logprobs.argtypes = [P, M, J, F32, I64, P, P, P, I64, P, P, P]
+        lib.pdb_logprobs_grad.argtypes = [P, M, J, F32, I64, P, P, P, P, M, P]
+        lib.pdb_distill.argtypes = [P, M, J, M, P, F32, P, P, M, P]
         lib.pdb_launch_count.argtypes = []
         lib.pdb_launch_count.restype = I64
         _lib = lib
@@ -448,6 +471,173 @@ def pdb_eval_grad(m, y, out, loss: int, stream=None):
 def pdb_eval_expf(x, out, stream=None):
     """out = the library's device exponential of x (float32 tensors), for tests."""
     _check(load().pdb_eval_expf(_ptr(x), _ptr(out), x.numel(), _stream(stream)), "pdb_eval_expf")
+
+
+class Tokens:
+    """Owns a pdb_tokens handle: workspace and status word of the token operators."""
+
+    def __init__(self, handle, device):
+        self.handle, self.device = handle, device
+
+    def __del__(self):
+        if getattr(self, "handle", None) and _lib is not None:
+            _lib.pdb_tokens_free(self.handle)
+            self.handle = None
+
+
+_types = None
+
+
+def _type_of(dtype):
+    global _types
+    if _types is None:
+        import torch
+        _types = {torch.float32: PDB_TYPE_FLOAT, torch.bfloat16: PDB_TYPE_BFLOAT, torch.float16: PDB_TYPE_HALF,
+                  torch.int32: "int32", torch.int64: "int64"}
+    return _types.get(dtype)
+
+
+def _refuse(what, why):
+    raise PdbError(PDB_EINVAL, f"{what}: {why}")
+
+
+def _mat(t, tok, what):
+    """A pdb_mat of a 2-D device tensor whose rows are contiguous."""
+    kind = _type_of(t.dtype)
+    if kind.__class__ is not int:
+        _refuse(what, f"float32, bfloat16 or float16 wanted, got {t.dtype}")
+    if t.dim() != 2 or t.get_device() != tok.device:
+        _refuse(what, f"a matrix on cuda:{tok.device} wanted, got {tuple(t.shape)} on {t.device}")
+    rows, cols = t.shape
+    stride, step = t.stride()
+    if (step != 1 and cols > 1) or (stride < cols and rows > 1):
+        _refuse(what, f"rows of neighbouring elements that do not overlap wanted, got strides {t.stride()}")
+    return pdb_mat(t.data_ptr(), rows, cols, stride, kind)
+
+
+def _ids(t, tok, what):
+    """A pdb_ids of a vector of ids."""
+    kind = _type_of(t.dtype)
+    if kind.__class__ is not str:
+        _refuse(what, f"int32 or int64 wanted, got {t.dtype}")
+    if t.dim() != 1 or t.get_device() != tok.device:
+        _refuse(what, f"a vector on cuda:{tok.device} wanted, got {tuple(t.shape)} on {t.device}")
+    return pdb_ids(t.data_ptr(), t.shape[0], t.stride(0), kind == "int64")
+
+
+def _rows_of_ids(t, tok, what):
+    """A pdb_ids of a matrix of ids whose rows are contiguous."""
+    kind = _type_of(t.dtype)
+    if kind.__class__ is not str:
+        _refuse(what, f"int32 or int64 wanted, got {t.dtype}")
+    if t.dim() != 2 or t.get_device() != tok.device:
+        _refuse(what, f"a matrix on cuda:{tok.device} wanted, got {tuple(t.shape)} on {t.device}")
+    rows, cols = t.shape
+    stride, step = t.stride()
+    if step != 1 and cols > 1:
+        _refuse(what, f"rows of neighbouring elements wanted, got strides {t.stride()}")
+    return pdb_ids(t.data_ptr(), rows * cols, stride, kind == "int64")
+
+
+def _vec(t, n, tok, what, kind=PDB_TYPE_FLOAT):
+    """The pointer of n contiguous device words (None stays None)."""
+    if t is None:
+        return None
+    if _type_of(t.dtype) != kind or t.get_device() != tok.device or t.numel() != n or not t.is_contiguous():
+        _refuse(what, f"{n} contiguous {'int32' if kind == 'int32' else 'float32'} on cuda:{tok.device} wanted, "
+                      f"got {t.dtype} {tuple(t.shape)} on {t.device}")
+    return t.data_ptr()
+
+
+def pdb_tokens_create(max_tokens: int = 0, max_dim: int = 0, stream=None) -> Tokens:
+    """Workspace and status word of the token operators, for pdb_embed_grad
+    calls of at most max_tokens ids and max_dim columns (the other calls need neither)."""
+    import torch
+    h = ctypes.c_void_p()
+    _check(load().pdb_tokens_create(int(max_tokens), int(max_dim), ctypes.byref(h), _stream(stream)),
+           "pdb_tokens_create")
+    return Tokens(h, torch.cuda.current_device())
+
+
+def pdb_tokens_status(tok: Tokens, stream=None) -> int:
+    """Synchronize the stream and return the first error a kernel recorded in tok
+    (PDB_ERANGE: an id out of range; PDB_OK when none)."""
+    return int(load().pdb_tokens_status(tok.handle, _stream(stream)))
+
+
+def pdb_embed(tok: Tokens, table, ids, out, scale: float = 1.0, pad: int = -1, stream=None):
+    """out[i] = scale * table[ids[i]] (Definition 3's reads); rows of zeros for ids equal to pad.
+    table (vocab, dim) and out (n, dim) in float32, bfloat16 or float16, each its own; ids n int32 or int64."""
+    _check(load().pdb_embed(tok.handle, _mat(table, tok, "pdb_embed table"), _ids(ids, tok, "pdb_embed ids"), scale,
+                            pad, _mat(out, tok, "pdb_embed out"), _stream(stream)), "pdb_embed")
+
+
+def pdb_embed_grad(tok: Tokens, ids, dout, dtable, scale: float = 1.0, pad: int = -1, accumulate: bool = False,
+                   stream=None):
+    """dtable[v] = scale * sum of dout[i] over ids[i] = v, in data order (Algorithm 2a's ordered sums); every
+    row is written.  accumulate=True adds to the rows that occur and leaves the others: with the table for
+    dtable and scale = -eta * scale, the SGD step in place."""
+    _check(load().pdb_embed_grad(tok.handle, _ids(ids, tok, "pdb_embed_grad ids"),
+                                 _mat(dout, tok, "pdb_embed_grad dout"), scale, pad, accumulate,
+                                 _mat(dtable, tok, "pdb_embed_grad dtable"), _stream(stream)), "pdb_embed_grad")
+
+
+def pdb_logprobs(tok: Tokens, logits, ids=None, logp=None, lse=None, entropy=None, top_logp=None, top_ids=None,
+                 scale: float = 1.0, ignore: int = -100, stream=None):
+    """Per row of logits (times scale, the inverse temperature): logp of the token ids[r], log-sum-exp, entropy,
+    and the top_logp.shape[1] most probable tokens, each where its output tensor (float32; top_ids int32) is given."""
+    z = _mat(logits, tok, "pdb_logprobs logits")
+    n, k = z.rows, 0
+    top = top_ids if top_logp is None else top_logp
+    if top is not None:
+        if top.dim() != 2:
+            _refuse("pdb_logprobs top", f"(rows, k) wanted, got {tuple(top.shape)}")
+        k = top.shape[1]
+    if (ids is None) != (logp is None):
+        _refuse("pdb_logprobs", "ids and logp go together")
+    _check(load().pdb_logprobs(
+        tok.handle, z, None if ids is None else _ids(ids, tok, "pdb_logprobs ids"), scale, ignore,
+        _vec(logp, n, tok, "pdb_logprobs logp"), _vec(lse, n, tok, "pdb_logprobs lse"),
+        _vec(entropy, n, tok, "pdb_logprobs entropy"), k, _vec(top_logp, n * k, tok, "pdb_logprobs top_logp"),
+        _vec(top_ids, n * k, tok, "pdb_logprobs top_ids", "int32"), _stream(stream)), "pdb_logprobs")
+
+
+def pdb_logprobs_grad(tok: Tokens, logits, ids, lse, entropy, dlogp, dentropy, dlogits, scale: float = 1.0,
+                      ignore: int = -100, stream=None):
+    """dlogits = the gradient of sum(dlogp * logp + dentropy * entropy), with lse and entropy as pdb_logprobs gave
+    them.  dlogp (with ids) or dentropy (with entropy) may be None; dlogits may be logits itself."""
+    z = _mat(logits, tok, "pdb_logprobs_grad logits")
+    n = z.rows
+    _check(load().pdb_logprobs_grad(
+        tok.handle, z, None if ids is None else _ids(ids, tok, "pdb_logprobs_grad ids"), scale, ignore,
+        _vec(lse, n, tok, "pdb_logprobs_grad lse"), _vec(entropy, n, tok, "pdb_logprobs_grad entropy"),
+        _vec(dlogp, n, tok, "pdb_logprobs_grad dlogp"), _vec(dentropy, n, tok, "pdb_logprobs_grad dentropy"),
+        _mat(dlogits, tok, "pdb_logprobs_grad dlogits"), _stream(stream)), "pdb_logprobs_grad")
+
+
+def pdb_distill(tok: Tokens, logits, top_ids, top_logits, loss=None, teacher_lse=None, weight=None, dlogits=None,
+                temperature: float = 1.0, stream=None):
+    """Loss per row of the student's logits against a teacher's top_logits (rows, K) at the tokens top_ids (a
+    negative id: an empty slot), and, where dlogits is given, the gradient of sum(weight * loss).  With
+    teacher_lse (log-sum-exp of all the teacher's logits / temperature) the rest of the teacher's
+    probability stands in one bucket; else its slots are renormalised.  dlogits may be logits itself."""
+    z = _mat(logits, tok, "pdb_distill logits")
+    n = z.rows
+    t = _mat(top_logits, tok, "pdb_distill top_logits")
+    if top_ids.shape != top_logits.shape:
+        _refuse("pdb_distill", f"top_ids {tuple(top_ids.shape)} and top_logits {tuple(top_logits.shape)} differ in shape")
+    _check(load().pdb_distill(
+        tok.handle, z, _rows_of_ids(top_ids, tok, "pdb_distill top_ids"), t,
+        _vec(teacher_lse, n, tok, "pdb_distill teacher_lse"), temperature, _vec(loss, n, tok, "pdb_distill loss"),
+        _vec(weight, n, tok, "pdb_distill weight"),
+        None if dlogits is None else _mat(dlogits, tok, "pdb_distill dlogits"), _stream(stream)), "pdb_distill")
+
+
+def check_tokens(tok: Tokens, stream=None):
+    """Synchronize and raise PdbError if a kernel recorded an error in tok."""
+    rc = pdb_tokens_status(tok, stream)
+    if rc != PDB_OK:
+        raise PdbError(rc, "device status")
 
 
 def pdb_launch_count() -> int:

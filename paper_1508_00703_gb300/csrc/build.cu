@@ -807,7 +807,7 @@ static int copy_words_to_host(int *pinned, const void *src, size_t bytes, cudaSt
     return cudaPeekAtLastError() == cudaSuccess ? PDB_OK : PDB_ECUDA;
 }
 
-static int read_words(void *dst, const void *src, size_t bytes, cudaStream_t s)
+int read_words(void *dst, const void *src, size_t bytes, cudaStream_t s)
 {
     if (bytes > sizeof(int) * INFO_WORDS) return PDB_EINVAL;
     int *stage = info_slot_take();          // a pinned, mapped slot of the info slab

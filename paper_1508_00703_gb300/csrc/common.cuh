@@ -456,6 +456,8 @@ struct UseMark {
 // fill bytes / 4 words at p with v on s by a kernel (a memset may run on a
 // copy engine and queue behind the caller's copies); bytes a multiple of 4
 int fill_words(void *p, uint32_t v, size_t bytes, cudaStream_t s);
+// waits for s and copies a few device words to the host (not through a copy engine)
+int read_words(void *dst, const void *src, size_t bytes, cudaStream_t s);
 int *info_slot_take();
 void info_slot_give(int *slot);
 

@@ -1,0 +1,140 @@
+// Shared by the token operators (embed.cu, logprobs.cu, distill.cu): element
+// types, argument checks, the handle.
+#pragma once
+
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include "common.cuh"
+
+struct pdb_tokens {
+    int device;
+    int64_t max_tokens, max_dim;
+    int *status;               // device: [0] first error recorded by a kernel; [1] always 0 (the sort's
+                               // kernels return at once when their status word is set)
+    uint32_t *key, *skey, *tkey;   // [max_tokens] ids as sort keys, sorted, scratch
+    int32_t *spos, *tpos;      // [max_tokens] positions in sorted order, scratch
+    float *part;               // pieces of runs that cross pieces (embed.cu)
+    cudaEvent_t ev_use;        // recorded after the last work any call enqueued on the handle
+};
+
+namespace pdb {
+
+// every call on a handle records ev_use when it returns
+struct TokensUse {
+    const pdb_tokens *t;
+    cudaStream_t s;
+    ~TokensUse()
+    {
+        if (t && t->ev_use) cudaEventRecord(t->ev_use, s);
+    }
+};
+
+inline int type_bytes(int type) { return type == PDB_TYPE_FLOAT ? 4 : 2; }
+
+// PDB_OK for a matrix that the calls accept
+inline int check_mat(const pdb_mat *m)
+{
+    if (!m || m->rows < 0 || m->cols < 0) return PDB_EINVAL;
+    if (m->type != PDB_TYPE_FLOAT && m->type != PDB_TYPE_BFLOAT && m->type != PDB_TYPE_HALF) return PDB_EINVAL;
+    if (m->rows > 1 && m->stride < m->cols) return PDB_EINVAL;
+    if (m->rows > 0 && m->cols > 0 && (!m->data || (uintptr_t)m->data % type_bytes(m->type) != 0)) return PDB_EINVAL;
+    if (m->cols > INT32_MAX / 2) return PDB_ETOOBIG;
+    return PDB_OK;
+}
+
+// ids of n rows of k each (pdb_ids.stride then is that of the rows)
+inline int check_ids(const pdb_ids *ids, int64_t n, int64_t k = 1)
+{
+    if (!ids || ids->n != n * k) return PDB_EINVAL;
+    if (n > 1 && ids->stride < k) return PDB_EINVAL;
+    if (n * k > 0 && (!ids->data || (uintptr_t)ids->data % (ids->wide ? 8 : 4) != 0)) return PDB_EINVAL;
+    return PDB_OK;
+}
+
+// the ids as the kernels take them
+struct Ids {
+    const void *data;
+    int64_t stride;
+    int wide;
+};
+inline Ids ids_of(const pdb_ids *ids, bool given = true)
+{
+    if (!given) return {nullptr, 0, 0};
+    return {ids->data, ids->n > 1 ? ids->stride : 0, ids->wide};
+}
+
+// stride of a matrix whose stride may be unset (fewer than two rows)
+inline int64_t stride_of(const pdb_mat *m) { return m->rows > 1 ? m->stride : m->cols; }
+
+// whether two matrices share memory
+inline bool overlap(const pdb_mat *a, const pdb_mat *b)
+{
+    if (a->rows == 0 || b->rows == 0 || a->cols == 0 || b->cols == 0) return false;
+    const char *a0 = (const char *)a->data, *b0 = (const char *)b->data;
+    const char *a1 = a0 + ((a->rows - 1) * stride_of(a) + a->cols) * type_bytes(a->type);
+    const char *b1 = b0 + ((b->rows - 1) * stride_of(b) + b->cols) * type_bytes(b->type);
+    return a0 < b1 && b0 < a1;
+}
+
+// a result that may be written over its input: the same matrix, or one apart
+inline bool same_or_apart(const pdb_mat *a, const pdb_mat *b)
+{
+    if (!overlap(a, b)) return true;
+    return a->data == b->data && a->type == b->type && stride_of(a) == stride_of(b);
+}
+
+// id k of row i
+__device__ __forceinline__ int64_t load_id(Ids ids, int64_t i, int k = 0)
+{
+    const int64_t at = i * ids.stride + k;
+    return ids.wide ? (int64_t)__ldg((const long long *)ids.data + at) : (int64_t)__ldg((const int *)ids.data + at);
+}
+
+__device__ __forceinline__ float to_float(float v) { return v; }
+__device__ __forceinline__ float to_float(__nv_bfloat16 v) { return __bfloat162float(v); }
+__device__ __forceinline__ float to_float(__half v) { return __half2float(v); }
+
+template <typename T>
+__device__ __forceinline__ T from_float(float v);
+template <>
+__device__ __forceinline__ float from_float<float>(float v) { return v; }
+template <>
+__device__ __forceinline__ __nv_bfloat16 from_float<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
+template <>
+__device__ __forceinline__ __half from_float<__half>(float v) { return __float2half_rn(v); }
+
+// f called with a null pointer of the element type
+template <typename F>
+inline auto with_type(int type, F f)
+{
+    if (type == PDB_TYPE_FLOAT) return f((float *)nullptr);
+    if (type == PDB_TYPE_BFLOAT) return f((__nv_bfloat16 *)nullptr);
+    return f((__half *)nullptr);
+}
+
+constexpr int ROW_THREADS = 256;
+
+// sum (or maximum) of v over the block, on every thread; `s` holds 32 words
+__device__ __forceinline__ float block_sum(float v, float *s)
+{
+    for (int off = 16; off >= 1; off >>= 1) v = __fadd_rn(v, __shfl_xor_sync(FULL, v, off));
+    __syncthreads();
+    if ((threadIdx.x & 31) == 0) s[threadIdx.x >> 5] = v;
+    __syncthreads();
+    v = 0.0f;
+    for (int w = 0; w < (int)(blockDim.x >> 5); ++w) v = __fadd_rn(v, s[w]);
+    return v;
+}
+__device__ __forceinline__ float block_max(float v, float *s)
+{
+    for (int off = 16; off >= 1; off >>= 1) v = fmaxf(v, __shfl_xor_sync(FULL, v, off));
+    __syncthreads();
+    if ((threadIdx.x & 31) == 0) s[threadIdx.x >> 5] = v;
+    __syncthreads();
+    v = s[0];
+    for (int w = 1; w < (int)(blockDim.x >> 5); ++w) v = fmaxf(v, s[w]);
+    return v;
+}
+
+}  // namespace pdb
