@@ -92,7 +92,9 @@ int pdb_tokens_create(int64_t max_tokens, int64_t max_dim, pdb_tokens **out, voi
     cudaStream_t s = (cudaStream_t)stream;
     pdb_tokens *t = new (std::nothrow) pdb_tokens();
     if (!t) return PDB_ENOMEM;
-    cudaGetDevice(&t->device);
+    const Launch l = launch_info();
+    t->device = l.device;
+    t->sms = l.sms;
     t->max_tokens = max_tokens;
     t->max_dim = max_dim;
     int rc = cudaEventCreateWithFlags(&t->ev_use, cudaEventDisableTiming) == cudaSuccess ? PDB_OK : PDB_ECUDA;

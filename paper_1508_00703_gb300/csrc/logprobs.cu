@@ -1,85 +1,284 @@
 // Log probabilities of given tokens with entropy and the most probable
 // alternatives, and their gradient (pdb_logprobs, pdb_logprobs_grad).
+//
+// Per row of logits z, c = scale * log2(e), in one pass over the row (rows.cuh):
+//   m = max z,  s = sum 2^((z - m) c),  w = sum 2^((z - m) c) (z - m) c
+//   log p_j = (z_j - m) scale - ln s,  lse = m scale + ln s,  entropy = ln s - ln2 w / s
+// The row's blocks hand (m, s, w) to the cluster's first one through its shared memory.
+//
+// Alternatives.  The pass keeps the maximum of each of 128 groups of threads
+// (1 to 4 neighbours).  The k-th largest of them, tau, is at most the k-th largest
+// logit, since k different logits reach it, and the groups that reach tau (k, and those
+// that tie) hold every logit that does.  Only those groups' vectors are read again (from L2), their logits
+// >= tau collected (a few more than k as a rule) and ranked by counting.  Where more
+// than the buffer reach tau (ties, masked rows) or a NaN hides from the maxima, a radix
+// selection over the block's share takes over: four counting passes, exact for
+// any order of the row.  The pass itself pays one maximum per thread and 64 bytes.
 #include <algorithm>
 #include <cmath>
 
-#include "tokens.cuh"
+#include "rows.cuh"
 
 using namespace pdb;
+namespace cg = cooperative_groups;
 
 namespace {
 
 constexpr int MAX_TOP = 64;
+constexpr int GROUPS = 128;
+constexpr int BUFFER = 1024;            // candidates of a block; also the lists of a cluster: MAX_CLUSTER * MAX_TOP
+static_assert(MAX_CLUSTER * MAX_TOP <= BUFFER, "the cluster's lists are ranked in one buffer");
 
-// a logit and its token as one word that orders like (logit descending, token ascending): NaN above all, -0 = +0
-__device__ __forceinline__ uint64_t top_key(float z, int j)
+// a logit as a word that orders like it: NaN above all, -0 = +0
+__device__ __forceinline__ uint32_t order_of(float z)
 {
-    uint32_t b = __float_as_uint(z);
-    b = z != z ? 0xfffffffeu : z == 0.0f ? 0x80000000u : (b & 0x80000000u) ? ~b : b | 0x80000000u;
-    return (uint64_t)b << 32 | (uint32_t)~j;
+    const uint32_t b = __float_as_uint(z);
+    return z != z ? 0xfffffffeu : z == 0.0f ? 0x80000000u : (b & 0x80000000u) ? ~b : b | 0x80000000u;
+}
+__device__ __forceinline__ float order_value(uint32_t o)
+{
+    return __uint_as_float((o & 0x80000000u) ? o ^ 0x80000000u : ~o);
+}
+// with its token: larger logits first, then lower tokens
+__device__ __forceinline__ uint64_t key_of(uint32_t order, int j) { return (uint64_t)order << 32 | (uint32_t)~j; }
+
+struct TopShared {
+    float group[GROUPS];
+    int list[GROUPS];                   // groups that reach tau
+    uint64_t key[BUFFER];               // candidates
+    uint64_t best[MAX_TOP];             // the block's best, in order
+    int hist[256];
+    int warp_count[16];
+    int n, n_list, need, digit;
+    float tau;
+};
+
+// best[0..min(k, n)) = the largest of key[0..n), in order (keys differ)
+template <int THREADS>
+__device__ __forceinline__ void rank_keys(TopShared &t, int n, int k)
+{
+    for (int i = threadIdx.x; i < n; i += THREADS) {
+        const uint64_t mine = t.key[i];
+        int above = 0;
+        for (int j = 0; j < n; ++j) above += t.key[j] > mine ? 1 : 0;
+        if (above < k) t.best[above] = mine;
+    }
+    __syncthreads();
 }
 
-template <typename T>
-__global__ __launch_bounds__(ROW_THREADS) void k_logprobs(const T *__restrict__ logits, int64_t rows, int cols,
-                                                          int64_t stride, Ids ids,
-                                                          float scale, int64_t ignore, float *logp, float *lse,
-                                                          float *entropy, int k, float *top_logp, int32_t *top_ids,
-                                                          int *status)
+// the k largest of row[j0..j1) into key[0..k) by radix selection, for any contents (j1 - j0 > k)
+template <typename T, int THREADS>
+__device__ __noinline__ void select_keys(TopShared &t, const T *row, int j0, int j1, int k)
 {
-    __shared__ float s_red[32];
-    __shared__ uint64_t s_key[32];
-    for (int64_t r = blockIdx.x; r < rows; r += gridDim.x) {
-        const T *z = logits + r * stride;
-        float m = -INFINITY;
-        for (int j = threadIdx.x; j < cols; j += blockDim.x) m = fmaxf(m, to_float(z[j]));
-        m = block_max(m, s_red);
-        const float ref = m == -INFINITY ? 0.0f : m;
-        float s = 0.0f, w = 0.0f;
-        for (int j = threadIdx.x; j < cols; j += blockDim.x) {
-            const float d = __fmul_rn(__fsub_rn(to_float(z[j]), ref), scale);
-            const float e = expf(d);
-            s = __fadd_rn(s, e);
-            w = __fadd_rn(w, e == 0.0f ? 0.0f : __fmul_rn(e, d));
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const uint32_t masked = order_of(-INFINITY);
+    uint32_t prefix = 0, fixed = 0;
+    int need = k;
+    for (int shift = 24; shift >= 0; shift -= 8) {
+        for (int i = threadIdx.x; i < 256; i += THREADS) t.hist[i] = 0;
+        __syncthreads();
+        int n_masked = 0;                // the one value that whole rows hold is counted apart
+        for (int j = j0 + threadIdx.x; j < j1; j += THREADS) {
+            const uint32_t o = order_of(to_float(row[j]));
+            if ((o & fixed) != prefix) continue;
+            if (o == masked) ++n_masked;
+            else atomicAdd(&t.hist[(o >> shift) & 255], 1);
         }
-        s = block_sum(s, s_red);
-        w = block_sum(w, s_red);
-        const float logs = logf(s);
-        const bool none = s == 0.0f;
+        if (n_masked) atomicAdd(&t.hist[(masked >> shift) & 255], n_masked);
+        __syncthreads();
         if (threadIdx.x == 0) {
-            if (lse) lse[r] = __fmaf_rn(ref, scale, logs);
-            if (entropy) entropy[r] = none ? 0.0f : __fsub_rn(logs, __fdiv_rn(w, s));
-            if (logp) {
-                const int64_t t = load_id(ids, r);
-                const bool there = t != ignore && t >= 0 && t < cols;
-                if (!there && t != ignore) set_status(status, PDB_ERANGE);
-                logp[r] = !there ? 0.0f
-                          : none ? -INFINITY
-                                 : __fsub_rn(__fmul_rn(__fsub_rn(to_float(z[t]), ref), scale), logs);
+            int d = 255;
+            while (d > 0 && t.hist[d] < need) need -= t.hist[d--];
+            t.digit = d;
+            t.need = need;
+            t.n = 0;
+        }
+        __syncthreads();
+        prefix |= (uint32_t)t.digit << shift;
+        fixed |= 255u << shift;
+        need = t.need;
+    }
+    // prefix is the k-th largest value: everything above it, and the first `need` that equal it
+    int taken = 0;
+    for (int base = j0; base < j1; base += THREADS) {
+        const int j = base + threadIdx.x;
+        const uint32_t o = j < j1 ? order_of(to_float(row[j])) : 0u;
+        if (j < j1 && o > prefix) t.key[atomicAdd(&t.n, 1)] = key_of(o, j);
+        const bool equal = j < j1 && o == prefix;
+        if (__syncthreads_or(equal && taken < need)) {
+            const unsigned b = __ballot_sync(FULL, equal);
+            if (lane == 0) t.warp_count[warp] = __popc(b);
+            __syncthreads();
+            int at = taken + __popc(b & lanemask_lt()), all = 0;
+            for (int w = 0; w < THREADS / 32; ++w) {
+                const int x = t.warp_count[w];
+                at += w < warp ? x : 0;
+                all += x;
+            }
+            if (equal && at < need) t.key[k - need + at] = key_of(o, j);   // behind the k - need above it
+            taken += all;
+            __syncthreads();
+        }
+    }
+    __syncthreads();
+}
+
+// best[0..k) = the block's share's k largest; returns how many there are
+template <typename T, int THREADS>
+__device__ __forceinline__ int top_of_share(TopShared &t, const T *row, const uint4 *body, const Share &sh, float top,
+                                            bool odd, int k)
+{
+    constexpr int PER = THREADS / GROUPS, E = Vec<T>::E;      // threads of a group
+    const int n_share = sh.j1 - sh.j0, have = min(k, n_share);
+    if (n_share <= k) {
+        for (int j = sh.j0 + threadIdx.x; j < sh.j1; j += THREADS) t.key[j - sh.j0] = key_of(order_of(to_float(row[j])), j);
+        __syncthreads();
+        rank_keys<THREADS>(t, n_share, k);
+        return have;
+    }
+    if (!odd) {
+#pragma unroll
+        for (int off = PER / 2; off >= 1; off >>= 1) top = fmaxf(top, __shfl_xor_sync(FULL, top, off));
+        if (threadIdx.x % PER == 0) t.group[threadIdx.x / PER] = top;
+        if (threadIdx.x == 0) t.n = t.n_list = 0;
+        __syncthreads();
+        if (threadIdx.x < GROUPS) {
+            const float mine = t.group[threadIdx.x];
+            int above = 0;
+#pragma unroll 8
+            for (int g = 0; g < GROUPS; ++g) {
+                const float o = t.group[g];
+                above += o > mine || (o == mine && g < (int)threadIdx.x) ? 1 : 0;
+            }
+            if (above == k - 1) t.tau = mine;
+        }
+        __syncthreads();
+        const float tau = t.tau;
+        if (threadIdx.x < GROUPS && t.group[threadIdx.x] >= tau) t.list[atomicAdd(&t.n_list, 1)] = threadIdx.x;
+        __syncthreads();
+        const int n_list = t.n_list;    // k, or more where groups tie
+        const int lane = threadIdx.x & 31, sub = lane % PER;
+        auto take = [&](float z, int j) {
+            if (z >= tau) {
+                const int at = atomicAdd(&t.n, 1);
+                if (at < BUFFER) t.key[at] = key_of(order_of(z), j);
+            }
+        };
+        for (int g = threadIdx.x >> 5; g < n_list; g += THREADS / 32) {
+            const int first = sh.v0 + t.list[g] * PER + sub;
+            for (int v = first + lane / PER * THREADS; v < sh.v1; v += 32 / PER * THREADS) {
+                float f[E];
+                Vec<T>::unpack(ld_keep(body + v), f);
+                float mx = f[0];
+#pragma unroll
+                for (int i = 1; i < E; ++i) mx = fmaxf(mx, f[i]);
+                if (mx >= tau)
+#pragma unroll
+                    for (int i = 0; i < E; ++i) take(f[i], sh.head + v * E + i);
             }
         }
-        uint64_t below = ~(uint64_t)0;
-        for (int i = 0; i < k; ++i) {
-            uint64_t best = 0;
-            for (int j = threadIdx.x; j < cols; j += blockDim.x) {
-                const uint64_t key = top_key(to_float(z[j]), j);
-                if (key < below && key > best) best = key;
-            }
-            for (int off = 16; off >= 1; off >>= 1) best = max(best, __shfl_xor_sync(FULL, best, off));
-            __syncthreads();
-            if ((threadIdx.x & 31) == 0) s_key[threadIdx.x >> 5] = best;
-            __syncthreads();
-            for (int q = 0; q < ROW_THREADS / 32; ++q) best = max(best, s_key[q]);
-            below = best;
-            if (threadIdx.x == 0) {
-                const int j = (int)~(uint32_t)best;
-                if (top_ids) top_ids[r * k + i] = j;
-                if (top_logp)
-                    top_logp[r * k + i] =
-                        none ? -INFINITY : __fsub_rn(__fmul_rn(__fsub_rn(to_float(z[j]), ref), scale), logs);
-            }
+        if ((int)threadIdx.x < sh.edges()) take(to_float(row[sh.edge(threadIdx.x)]), sh.edge(threadIdx.x));
+        __syncthreads();
+        const int n = t.n;
+        if (n <= BUFFER) {
+            rank_keys<THREADS>(t, n, k);
+            return have;
         }
         __syncthreads();
     }
+    select_keys<T, THREADS>(t, row, sh.j0, sh.j1, k);
+    rank_keys<THREADS>(t, k, k);
+    return have;
+}
+
+struct LogprobsOut {
+    float *logp, *lse, *entropy, *top_logp;
+    int32_t *top_ids;
+};
+
+template <typename T, bool ENT, bool TOP, int THREADS>
+__global__ __launch_bounds__(THREADS) void k_logprobs(const T *__restrict__ logits, int cols, int64_t stride, Ids ids,
+                                                      float scale, int64_t ignore, int k, LogprobsOut out, int *status)
+{
+    __shared__ float part[96];
+    __shared__ float own[4];            // this block's m, s, w, number of alternatives
+    __shared__ __align__(16) unsigned char top_raw[TOP ? sizeof(TopShared) : 16];
+    TopShared &t = *reinterpret_cast<TopShared *>(top_raw);
+    cg::cluster_group cluster = cg::this_cluster();
+    const int blocks = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
+    const int64_t r = blockIdx.x / blocks;
+    const T *row = logits + r * stride;
+    const Share sh = share_of(row, cols, rank, blocks);
+    const uint4 *body = reinterpret_cast<const uint4 *>(row + sh.head);
+    const float c = __fmul_rn(scale, LOG2E);
+
+    // the given token's logit, on its way while the row is read
+    int64_t given = -1;
+    float z_given = 0.0f;
+    bool there = false;
+    if (out.logp && rank == 0 && threadIdx.x == 0) {
+        given = load_id(ids, r);
+        there = given != ignore && given >= 0 && given < cols;
+        if (!there && given != ignore) set_status(status, PDB_ERANGE);
+        if (there) z_given = to_float(row[given]);
+    }
+    Stat<ENT> a;
+    float top = -INFINITY;
+    {
+        uint4 v[UNROLL];
+        load_vectors<T, THREADS>(v, body, sh.v0, sh.v1);
+        for (int base = sh.v0; base < sh.v1; base += THREADS * UNROLL) {
+            uint4 next[UNROLL];
+            load_vectors<T, THREADS>(next, body, base + THREADS * UNROLL, sh.v1);
+            add_vectors<T, ENT>(a, v, c, top);
+#pragma unroll
+            for (int u = 0; u < UNROLL; ++u) v[u] = next[u];
+        }
+    }
+    if ((int)threadIdx.x < sh.edges()) add_element(a, to_float(row[sh.edge(threadIdx.x)]), c);
+    block_join<THREADS>(a, c, part);
+    int have = 0;
+    if (TOP) have = top_of_share<T, THREADS>(t, row, body, sh, top, !(a.s < INFINITY), k);
+    if (blocks > 1) {
+        if (threadIdx.x == 0) own[0] = a.m, own[1] = a.s, own[2] = a.w, own[3] = (float)have;
+        cluster.sync();
+        if (rank == 0) {
+            for (int b = 1; b < blocks; ++b) {
+                const float *o = cluster.map_shared_rank(own, b);
+                a.join(o[0], o[1], ENT ? o[2] : 0.0f, c);
+            }
+            if (TOP) {
+                // the blocks' lists, one after the other, ranked together
+                if (threadIdx.x == 0) t.n = 0;
+                __syncthreads();
+                for (int i = threadIdx.x; i < blocks * k; i += THREADS) {
+                    const int b = i / k, at = i % k;
+                    if (at < (int)cluster.map_shared_rank(own, b)[3])
+                        t.key[atomicAdd(&t.n, 1)] = cluster.map_shared_rank(&t, b)->best[at];
+                }
+                __syncthreads();
+                rank_keys<THREADS>(t, t.n, k);
+            }
+        }
+        cluster.sync();                  // the others' shared memory has been read
+        if (rank != 0) return;
+    }
+    const bool none = a.s == 0.0f;
+    const float ref = none ? 0.0f : a.m, logs = logf(a.s);
+    if (threadIdx.x == 0) {
+        if (out.lse) out.lse[r] = none ? -INFINITY : __fmaf_rn(ref, scale, logs);
+        if (out.entropy) out.entropy[r] = none ? 0.0f : __fmaf_rn(-LN2, __fdiv_rn(a.w, a.s), logs);
+        if (out.logp)
+            out.logp[r] = !there ? 0.0f : none ? -INFINITY : __fmaf_rn(__fsub_rn(z_given, ref), scale, -logs);
+    }
+    if (TOP)
+        for (int i = threadIdx.x; i < k; i += THREADS) {
+            const uint64_t key = t.best[i];
+            if (out.top_ids) out.top_ids[r * k + i] = (int)~(uint32_t)key;
+            if (out.top_logp)
+                out.top_logp[r * k + i] =
+                    none ? -INFINITY : __fmaf_rn(__fsub_rn(order_value((uint32_t)(key >> 32)), ref), scale, -logs);
+        }
 }
 
 template <typename T>
@@ -136,14 +335,19 @@ int pdb_logprobs(pdb_tokens *t, const pdb_mat *logits, const pdb_ids *ids, float
     if (logits->rows == 0) return PDB_OK;
     cudaStream_t s = (cudaStream_t)stream;
     TokensUse use{t, s};
-    with_type(logits->type, [&](auto *a) {
+    const bool top = k > 0 && (top_logp || top_ids);
+    const LogprobsOut out{logp, lse, entropy, top_logp, top_ids};
+    return with_type(logits->type, [&](auto *a) {
         using T = std::remove_pointer_t<decltype(a)>;
-        k_logprobs<T><<<(unsigned)std::min<int64_t>(logits->rows, 1 << 20), ROW_THREADS, 0, s>>>(
-            (const T *)logits->data, logits->rows, (int)logits->cols, stride_of(logits), ids_of(ids, logp),
-             scale, ignore, logp, lse, entropy, (int)k, top_logp, top_ids, t->status);
-        note_launch();
+        const Shape shape = row_shape(logits->rows, logits->cols, Vec<T>::E, t->sms);
+        return with_threads(shape.threads, [&](auto n) {
+            constexpr int N = decltype(n)::value;
+            const auto kernel = entropy ? (top ? k_logprobs<T, true, true, N> : k_logprobs<T, true, false, N>)
+                                        : (top ? k_logprobs<T, false, true, N> : k_logprobs<T, false, false, N>);
+            return launch_rows(kernel, logits->rows, shape, 0, s, (const T *)logits->data, (int)logits->cols,
+                               stride_of(logits), ids_of(ids, logp), scale, ignore, (int)k, out, t->status);
+        });
     });
-    return cudaPeekAtLastError() == cudaSuccess ? PDB_OK : PDB_ECUDA;
 }
 
 int pdb_logprobs_grad(pdb_tokens *t, const pdb_mat *logits, const pdb_ids *ids, float scale, int64_t ignore,
@@ -168,7 +372,7 @@ int pdb_logprobs_grad(pdb_tokens *t, const pdb_mat *logits, const pdb_ids *ids, 
         using T = std::remove_pointer_t<decltype(a)>;
         k_logprobs_grad<T><<<(unsigned)std::min<int64_t>(logits->rows, 1 << 20), ROW_THREADS, 0, s>>>(
             (const T *)logits->data, logits->rows, (int)logits->cols, stride_of(logits), ids_of(ids, dlogp),
-             scale, ignore, lse, entropy, dlogp, dentropy, (T *)dlogits->data,
+            scale, ignore, lse, entropy, dlogp, dentropy, (T *)dlogits->data,
             stride_of(dlogits), t->status);
         note_launch();
     });

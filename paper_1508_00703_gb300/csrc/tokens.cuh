@@ -8,7 +8,7 @@
 #include "common.cuh"
 
 struct pdb_tokens {
-    int device;
+    int device, sms;
     int64_t max_tokens, max_dim;
     int *status;               // device: [0] first error recorded by a kernel; [1] always 0 (the sort's
                                // kernels return at once when their status word is set)
@@ -39,7 +39,7 @@ inline int check_mat(const pdb_mat *m)
     if (m->type != PDB_TYPE_FLOAT && m->type != PDB_TYPE_BFLOAT && m->type != PDB_TYPE_HALF) return PDB_EINVAL;
     if (m->rows > 1 && m->stride < m->cols) return PDB_EINVAL;
     if (m->rows > 0 && m->cols > 0 && (!m->data || (uintptr_t)m->data % type_bytes(m->type) != 0)) return PDB_EINVAL;
-    if (m->cols > INT32_MAX / 2) return PDB_ETOOBIG;
+    if (m->cols > INT32_MAX / 2 || m->rows > INT32_MAX) return PDB_ETOOBIG;
     return PDB_OK;
 }
 
