@@ -281,40 +281,80 @@ __global__ __launch_bounds__(THREADS) void k_logprobs(const T *__restrict__ logi
         }
 }
 
-template <typename T>
-__global__ __launch_bounds__(ROW_THREADS) void k_logprobs_grad(const T *logits, int64_t rows, int cols, int64_t stride,
-                                                               Ids ids, float scale,
-                                                               int64_t ignore, const float *__restrict__ lse,
-                                                               const float *__restrict__ entropy,
-                                                               const float *__restrict__ dlogp,
-                                                               const float *__restrict__ dentropy, T *dlogits,
-                                                               int64_t out_stride, int *status)
+// dlogits = -p (A + B x) (+ scale g at the given token), x = (z - lse / scale) c, p = 2^x,
+// A = scale (g + h entropy), B = scale h ln2.  One pass, every element read and written once: bound by
+// memory.  A block takes one piece of a row; pieces of a row need nothing from one another.
+template <typename T, int THREADS>
+__global__ __launch_bounds__(THREADS) void k_logprobs_grad(const T *logits, int cols, int64_t stride, int pieces, Ids ids,
+                                                           float scale, int64_t ignore, const float *__restrict__ lse,
+                                                           const float *__restrict__ entropy,
+                                                           const float *__restrict__ dlogp,
+                                                           const float *__restrict__ dentropy, T *dlogits,
+                                                           int64_t out_stride, int *status)
 {
-    for (int64_t r = blockIdx.x; r < rows; r += gridDim.x) {
-        const T *z = logits + r * stride;
-        T *d = dlogits + r * out_stride;
-        float g = dlogp ? dlogp[r] : 0.0f;
-        const float h = dentropy ? dentropy[r] : 0.0f;
-        int64_t t = -1;
-        if (dlogp) {
-            t = load_id(ids, r);
-            const bool there = t != ignore && t >= 0 && t < cols;
-            if (!there && t != ignore && threadIdx.x == 0) set_status(status, PDB_ERANGE);
-            if (!there) g = 0.0f, t = -1;
-        }
-        const float l = lse[r], H = h != 0.0f ? entropy[r] : 0.0f;
-        const bool zero = (g == 0.0f && h == 0.0f) || l == -INFINITY;
-        for (int j = threadIdx.x; j < cols; j += blockDim.x) {
-            float v = 0.0f;
-            if (!zero) {
-                const float x = __fsub_rn(__fmul_rn(to_float(z[j]), scale), l);
-                const float p = expf(x);
-                v = __fsub_rn(j == t ? g : 0.0f, __fmul_rn(p, g));
-                if (h != 0.0f && p != 0.0f) v = __fsub_rn(v, __fmul_rn(__fmul_rn(h, p), __fadd_rn(x, H)));
-                v = __fmul_rn(v, scale);
+    constexpr int E = Vec<T>::E;
+    const int64_t r = blockIdx.x / pieces;
+    const int piece = (int)(blockIdx.x - r * pieces);
+    const T *row = logits + r * stride;
+    T *drow = dlogits + r * out_stride;
+    const Share sh = share_of(row, cols, piece, pieces);
+    const uint4 *body = reinterpret_cast<const uint4 *>(row + sh.head);
+    uint4 v[UNROLL];
+    load_vectors<T, THREADS>(v, body, sh.v0, sh.v1);      // on their way while the row's numbers arrive
+
+    float g = dlogp ? dlogp[r] : 0.0f;
+    const float h = dentropy ? dentropy[r] : 0.0f;
+    int t = -1;
+    if (dlogp) {
+        const int64_t id = load_id(ids, r);
+        const bool there = id != ignore && id >= 0 && id < cols;
+        if (!there && id != ignore && threadIdx.x == 0 && piece == 0) set_status(status, PDB_ERANGE);
+        if (there) t = (int)id;
+        else g = 0.0f;
+    }
+    const float l = lse[r];
+    const bool zero = (g == 0.0f && h == 0.0f) || l == -INFINITY;
+    const float H = h != 0.0f ? entropy[r] : 0.0f;
+    const float ref = __fdiv_rn(l, scale), c = __fmul_rn(scale, LOG2E);
+    const float A = -__fmul_rn(scale, __fmaf_rn(h, H, g)), B = -__fmul_rn(__fmul_rn(scale, h), LN2);
+    const float at_t = __fmul_rn(scale, g);
+    auto slope = [&](float z) {
+        // x held above -200, where p = 0: B x p of a token masked by -inf is 0
+        const float x = max_nan(__fmul_rn(__fsub_rn(z, ref), c), -200.0f);
+        return __fmul_rn(ex2(x), __fmaf_rn(B, x, A));
+    };
+    const bool aligned = ((uintptr_t)(drow + sh.head) & 15) == 0;
+    for (int base = sh.v0; base < sh.v1; base += THREADS * UNROLL) {
+        uint4 next[UNROLL];
+        load_vectors<T, THREADS>(next, body, base + THREADS * UNROLL, sh.v1);
+#pragma unroll
+        for (int u = 0; u < UNROLL; ++u) {
+            const int i = base + (int)threadIdx.x + u * THREADS;
+            if (i < sh.v1) {
+                float f[E];
+                Vec<T>::unpack(v[u], f);
+                const int j = sh.head + i * E;
+#pragma unroll
+                for (int e = 0; e < E; ++e) f[e] = zero ? 0.0f : slope(f[e]);
+                if ((unsigned)(t - j) < (unsigned)E && !zero)
+#pragma unroll
+                    for (int e = 0; e < E; ++e)
+                        if (j + e == t) f[e] = __fadd_rn(f[e], at_t);
+                if (aligned) {
+                    __stcs(reinterpret_cast<uint4 *>(drow + j), Vec<T>::pack(f));
+                } else {
+#pragma unroll
+                    for (int e = 0; e < E; ++e) drow[j + e] = from_float<T>(f[e]);
+                }
             }
-            d[j] = from_float<T>(v);
         }
+#pragma unroll
+        for (int u = 0; u < UNROLL; ++u) v[u] = next[u];
+    }
+    if ((int)threadIdx.x < sh.edges()) {
+        const int j = sh.edge(threadIdx.x);
+        const float x = slope(to_float(row[j]));
+        drow[j] = from_float<T>(zero ? 0.0f : j == t ? __fadd_rn(x, at_t) : x);
     }
 }
 
@@ -368,15 +408,19 @@ int pdb_logprobs_grad(pdb_tokens *t, const pdb_mat *logits, const pdb_ids *ids, 
     if (!lse || (dentropy && !entropy)) return PDB_EINVAL;
     cudaStream_t s = (cudaStream_t)stream;
     TokensUse use{t, s};
-    with_type(logits->type, [&](auto *a) {
+    return with_type(logits->type, [&](auto *a) {
         using T = std::remove_pointer_t<decltype(a)>;
-        k_logprobs_grad<T><<<(unsigned)std::min<int64_t>(logits->rows, 1 << 20), ROW_THREADS, 0, s>>>(
-            (const T *)logits->data, logits->rows, (int)logits->cols, stride_of(logits), ids_of(ids, dlogp),
-            scale, ignore, lse, entropy, dlogp, dentropy, (T *)dlogits->data,
-            stride_of(dlogits), t->status);
-        note_launch();
+        Shape shape = row_shape(logits->rows, logits->cols, Vec<T>::E, t->sms);
+        const int pieces = shape.blocks;
+        return with_threads(shape.threads, [&](auto n) {
+            constexpr int N = decltype(n)::value;
+            k_logprobs_grad<T, N><<<(unsigned)(logits->rows * pieces), N, 0, s>>>(
+                (const T *)logits->data, (int)logits->cols, stride_of(logits), pieces, ids_of(ids, dlogp), scale, ignore,
+                lse, entropy, dlogp, dentropy, (T *)dlogits->data, stride_of(dlogits), t->status);
+            note_launch();
+            return cudaPeekAtLastError() == cudaSuccess ? PDB_OK : PDB_ECUDA;
+        });
     });
-    return cudaPeekAtLastError() == cudaSuccess ? PDB_OK : PDB_ECUDA;
 }
 
 }  // extern "C"

@@ -48,7 +48,7 @@ __device__ __forceinline__ uint4 ld_keep(const uint4 *p)
 __device__ __forceinline__ uint4 ld_last(const uint4 *p)
 {
     uint4 v;
-    asm volatile("ld.global.L1::no_allocate.L2::evict_first.v4.u32 {%0, %1, %2, %3}, [%4];"
+    asm volatile("ld.global.cs.v4.u32 {%0, %1, %2, %3}, [%4];"
                  : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p) : "memory");
     return v;
 }
