@@ -293,10 +293,6 @@ inline Shape row_shape(int64_t rows, int64_t cols, int vec, int sms)
 }
 
 // f called with the number of threads as a type
-template <int N>
-struct Num {
-    static constexpr int value = N;
-};
 template <typename F>
 inline auto with_threads(int threads, F f)
 {

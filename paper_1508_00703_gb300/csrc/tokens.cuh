@@ -104,6 +104,12 @@ __device__ __forceinline__ __nv_bfloat16 from_float<__nv_bfloat16>(float v) { re
 template <>
 __device__ __forceinline__ __half from_float<__half>(float v) { return __float2half_rn(v); }
 
+// a number as a type
+template <int N>
+struct Num {
+    static constexpr int value = N;
+};
+
 // f called with a null pointer of the element type
 template <typename F>
 inline auto with_type(int type, F f)
@@ -111,30 +117,6 @@ inline auto with_type(int type, F f)
     if (type == PDB_TYPE_FLOAT) return f((float *)nullptr);
     if (type == PDB_TYPE_BFLOAT) return f((__nv_bfloat16 *)nullptr);
     return f((__half *)nullptr);
-}
-
-constexpr int ROW_THREADS = 256;
-
-// sum (or maximum) of v over the block, on every thread; `s` holds 32 words
-__device__ __forceinline__ float block_sum(float v, float *s)
-{
-    for (int off = 16; off >= 1; off >>= 1) v = __fadd_rn(v, __shfl_xor_sync(FULL, v, off));
-    __syncthreads();
-    if ((threadIdx.x & 31) == 0) s[threadIdx.x >> 5] = v;
-    __syncthreads();
-    v = 0.0f;
-    for (int w = 0; w < (int)(blockDim.x >> 5); ++w) v = __fadd_rn(v, s[w]);
-    return v;
-}
-__device__ __forceinline__ float block_max(float v, float *s)
-{
-    for (int off = 16; off >= 1; off >>= 1) v = fmaxf(v, __shfl_xor_sync(FULL, v, off));
-    __syncthreads();
-    if ((threadIdx.x & 31) == 0) s[threadIdx.x >> 5] = v;
-    __syncthreads();
-    v = s[0];
-    for (int w = 1; w < (int)(blockDim.x >> 5); ++w) v = fmaxf(v, s[w]);
-    return v;
 }
 
 }  // namespace pdb
