@@ -437,7 +437,8 @@ int pdb_sgd_epoch_ready_noalloc(const pdb_csr *X, const float *y, const uint32_t
  * one stream.  Sums, softmax statistics and losses are held in fp32; a result
  * in 16 bits is rounded once.  No atomics add floating values: the same inputs
  * give the same bits.  No call allocates but pdb_tokens_create, and all but
- * pdb_tokens_create and pdb_tokens_status can be recorded into a CUDA graph.
+ * pdb_tokens_create and pdb_tokens_status can be recorded into a CUDA graph (keep the
+ * handle until the graph's last run has finished: pdb_tokens_free does not wait for it).
  * PDB_LOG prints nothing for these calls. */
 
 /* Element types of a matrix: 32-bit, bfloat16, IEEE half. */

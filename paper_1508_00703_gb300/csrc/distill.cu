@@ -85,7 +85,7 @@ __global__ __launch_bounds__(THREADS) void k_distill(const T *logits, int cols, 
 
     cg::cluster_group cluster = cg::this_cluster();
     const int blocks = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
-    const int64_t r = blockIdx.x / blocks;
+    const int64_t r = blockIdx.x / (unsigned)blocks;
     const T *row = logits + r * stride;
     const Share sh = share_of(row, cols, rank, blocks);
     const uint4 *body = reinterpret_cast<const uint4 *>(row + sh.head);

@@ -6,8 +6,8 @@
 //   log p_j = (z_j - m) scale - ln s,  lse = m scale + ln s,  entropy = ln s - ln2 w / s
 // The row's blocks hand (m, s, w) to the cluster's first one through its shared memory.
 //
-// Alternatives.  The pass keeps the maximum of each of 128 groups of threads
-// (1 to 4 neighbours).  The k-th largest of them, tau, is at most the k-th largest
+// Alternatives.  The pass keeps the maximum of each of 32 to 128 groups of
+// neighbouring threads.  The k-th largest of them, tau, is at most the k-th largest
 // logit, since k different logits reach it, and the groups that reach tau (k, and those
 // that tie) hold every logit that does.  Only those groups' vectors are read again (from L2), their logits
 // >= tau collected (a few more than k as a rule) and ranked by counting.  Where more
@@ -25,7 +25,7 @@ namespace cg = cooperative_groups;
 namespace {
 
 constexpr int MAX_TOP = 64;
-constexpr int GROUPS = 128;
+constexpr int GROUPS = 128;             // most groups of threads
 constexpr int BUFFER = 1024;            // candidates of a block; also the lists of a cluster: MAX_CLUSTER * MAX_TOP
 static_assert(MAX_CLUSTER * MAX_TOP <= BUFFER, "the cluster's lists are ranked in one buffer");
 
@@ -43,7 +43,7 @@ __device__ __forceinline__ float order_value(uint32_t o)
 __device__ __forceinline__ uint64_t key_of(uint32_t order, int j) { return (uint64_t)order << 32 | (uint32_t)~j; }
 
 struct TopShared {
-    float group[GROUPS];
+    alignas(16) float group[GROUPS];
     int list[GROUPS];                   // groups that reach tau
     uint64_t key[BUFFER];               // candidates
     uint64_t best[MAX_TOP];             // the block's best, in order
@@ -128,7 +128,7 @@ template <typename T, int THREADS>
 __device__ __forceinline__ int top_of_share(TopShared &t, const T *row, const uint4 *body, const Share &sh, float top,
                                             bool odd, int k)
 {
-    constexpr int PER = THREADS / GROUPS, E = Vec<T>::E;      // threads of a group
+    constexpr int E = Vec<T>::E;
     const int n_share = sh.j1 - sh.j0, have = min(k, n_share);
     if (n_share <= k) {
         for (int j = sh.j0 + threadIdx.x; j < sh.j1; j += THREADS) t.key[j - sh.j0] = key_of(order_of(to_float(row[j])), j);
@@ -137,27 +137,31 @@ __device__ __forceinline__ int top_of_share(TopShared &t, const T *row, const ui
         return have;
     }
     if (!odd) {
-#pragma unroll
-        for (int off = PER / 2; off >= 1; off >>= 1) top = fmaxf(top, __shfl_xor_sync(FULL, top, off));
-        if (threadIdx.x % PER == 0) t.group[threadIdx.x / PER] = top;
+        // At least twice as many groups as alternatives, so that few more than k logits reach tau: fewer groups are
+        // cheaper to rank, but longer to read again.
+        const int groups = k <= 16 ? 32 : k <= 32 ? 64 : GROUPS, per = THREADS / groups;
+        for (int off = per >> 1; off >= 1; off >>= 1) top = fmaxf(top, __shfl_xor_sync(FULL, top, off));
+        if (threadIdx.x % (unsigned)per == 0) t.group[threadIdx.x / (unsigned)per] = top;
         if (threadIdx.x == 0) t.n = t.n_list = 0;
         __syncthreads();
-        if (threadIdx.x < GROUPS) {
+        if ((int)threadIdx.x < groups) {
             const float mine = t.group[threadIdx.x];
             int above = 0;
-#pragma unroll 8
-            for (int g = 0; g < GROUPS; ++g) {
-                const float o = t.group[g];
-                above += o > mine || (o == mine && g < (int)threadIdx.x) ? 1 : 0;
+            for (int g = 0; g < groups; g += 4) {
+                const float4 o = *reinterpret_cast<const float4 *>(t.group + g);
+                const int me = (int)threadIdx.x - g;
+                above += (o.x > mine || (o.x == mine && 0 < me) ? 1 : 0) + (o.y > mine || (o.y == mine && 1 < me) ? 1 : 0) +
+                         (o.z > mine || (o.z == mine && 2 < me) ? 1 : 0) + (o.w > mine || (o.w == mine && 3 < me) ? 1 : 0);
             }
             if (above == k - 1) t.tau = mine;
         }
         __syncthreads();
         const float tau = t.tau;
-        if (threadIdx.x < GROUPS && t.group[threadIdx.x] >= tau) t.list[atomicAdd(&t.n_list, 1)] = threadIdx.x;
+        if ((int)threadIdx.x < groups && t.group[threadIdx.x] >= tau) t.list[atomicAdd(&t.n_list, 1)] = threadIdx.x;
         __syncthreads();
         const int n_list = t.n_list;    // k, or more where groups tie
-        const int lane = threadIdx.x & 31, sub = lane % PER;
+        // a warp reads one group's vectors: per at a time lie side by side
+        const int lane = threadIdx.x & 31, wide = min(per, 32), sub = lane % (unsigned)wide;
         auto take = [&](float z, int j) {
             if (z >= tau) {
                 const int at = atomicAdd(&t.n, 1);
@@ -165,8 +169,8 @@ __device__ __forceinline__ int top_of_share(TopShared &t, const T *row, const ui
             }
         };
         for (int g = threadIdx.x >> 5; g < n_list; g += THREADS / 32) {
-            const int first = sh.v0 + t.list[g] * PER + sub;
-            for (int v = first + lane / PER * THREADS; v < sh.v1; v += 32 / PER * THREADS) {
+            const int first = sh.v0 + t.list[g] * per + sub;
+            for (int v = first + lane / (unsigned)wide * THREADS; v < sh.v1; v += 32 / (unsigned)wide * THREADS) {
                 float f[E];
                 Vec<T>::unpack(ld_keep(body + v), f);
                 float mx = f[0];
@@ -206,7 +210,7 @@ __global__ __launch_bounds__(THREADS) void k_logprobs(const T *__restrict__ logi
     TopShared &t = *reinterpret_cast<TopShared *>(top_raw);
     cg::cluster_group cluster = cg::this_cluster();
     const int blocks = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
-    const int64_t r = blockIdx.x / blocks;
+    const int64_t r = blockIdx.x / (unsigned)blocks;
     const T *row = logits + r * stride;
     const Share sh = share_of(row, cols, rank, blocks);
     const uint4 *body = reinterpret_cast<const uint4 *>(row + sh.head);
@@ -293,7 +297,7 @@ __global__ __launch_bounds__(THREADS) void k_logprobs_grad(const T *logits, int 
                                                            int64_t out_stride, int *status)
 {
     constexpr int E = Vec<T>::E;
-    const int64_t r = blockIdx.x / pieces;
+    const int64_t r = blockIdx.x / (unsigned)pieces;
     const int piece = (int)(blockIdx.x - r * pieces);
     const T *row = logits + r * stride;
     T *drow = dlogits + r * out_stride;

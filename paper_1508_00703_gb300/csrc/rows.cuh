@@ -162,8 +162,9 @@ __device__ __forceinline__ Share share_of(const T *row, int cols, int rank, int 
     Share s;
     s.head = min(cols, (int)(((16 - ((uintptr_t)row & 15)) & 15) / sizeof(T)));
     const int nv = (cols - s.head) / E;
-    s.v0 = (int)((int64_t)nv * rank / blocks);
-    s.v1 = (int)((int64_t)nv * (rank + 1) / blocks);
+    const int log = __ffs(blocks) - 1;            // a power of two
+    s.v0 = (int)((int64_t)nv * rank >> log);
+    s.v1 = (int)((int64_t)nv * (rank + 1) >> log);
     s.b0 = s.head + s.v0 * E;
     s.b1 = s.head + s.v1 * E;
     s.j0 = rank == 0 ? 0 : s.b0;
@@ -194,11 +195,19 @@ struct Stat {
         s = __fadd_rn(s, o.s);
         if (ENT) w = __fadd_rn(w, o.w);
     }
+    // over groups of LANES lanes: all to the largest m, then plain sums
+    template <int LANES>
     __device__ __forceinline__ void warp_join(float c)
     {
+        float to = m;
 #pragma unroll
-        for (int off = 16; off >= 1; off >>= 1)
-            join(__shfl_xor_sync(FULL, m, off), __shfl_xor_sync(FULL, s, off), ENT ? __shfl_xor_sync(FULL, w, off) : 0.0f, c);
+        for (int off = LANES / 2; off >= 1; off >>= 1) to = fmaxf(to, __shfl_xor_sync(FULL, to, off));
+        rebase(to, c);
+#pragma unroll
+        for (int off = LANES / 2; off >= 1; off >>= 1) {
+            s = __fadd_rn(s, __shfl_xor_sync(FULL, s, off));
+            if (ENT) w = __fadd_rn(w, __shfl_xor_sync(FULL, w, off));
+        }
     }
 };
 
@@ -263,16 +272,15 @@ template <int THREADS, bool ENT>
 __device__ __forceinline__ void block_join(Stat<ENT> &a, float c, float *part)
 {
     constexpr int W = THREADS / 32;
-    a.warp_join(c);
+    a.template warp_join<32>(c);
     if ((threadIdx.x & 31) == 0) {
         const int w = threadIdx.x >> 5;
         part[w] = a.m, part[32 + w] = a.s, part[64 + w] = a.w;
     }
     __syncthreads();
-    const int lane = threadIdx.x & 31;
-    a = Stat<ENT>();
-    if (lane < W) a.m = part[lane], a.s = part[32 + lane], a.w = part[64 + lane];
-    a.warp_join(c);
+    const int lane = threadIdx.x & (W - 1);
+    a.m = part[lane], a.s = part[32 + lane], a.w = part[64 + lane];
+    a.template warp_join<W>(c);
 }
 
 // How many blocks share a row, and how many threads a block has.

@@ -20,13 +20,16 @@ struct pdb_tokens {
 
 namespace pdb {
 
-// every call on a handle records ev_use when it returns
+// every call on a handle records ev_use when it returns; not while a graph is
+// recorded, whose event could not be waited for (the graph's owner keeps the handle)
 struct TokensUse {
     const pdb_tokens *t;
     cudaStream_t s;
     ~TokensUse()
     {
-        if (t && t->ev_use) cudaEventRecord(t->ev_use, s);
+        cudaStreamCaptureStatus capturing = cudaStreamCaptureStatusNone;
+        if (cudaStreamIsCapturing(s, &capturing) != cudaSuccess || capturing != cudaStreamCaptureStatusNone) return;
+        if (t->ev_use) cudaEventRecord(t->ev_use, s);
     }
 };
 
