@@ -1,7 +1,10 @@
 // Rows of a table by token id, and the table's gradient by sorted ids
 // (pdb_embed, pdb_embed_grad), and the handle of the token operators.
 #include <algorithm>
+#include <mutex>
 #include <new>
+#include <set>
+#include <utility>
 
 #include "tokens.cuh"
 
@@ -323,6 +326,28 @@ __global__ __launch_bounds__(256) void k_embed_join(const uint32_t *__restrict__
 }
 
 }  // namespace
+
+namespace pdb {
+
+bool allow_smem(const void *kernel)
+{
+    static std::mutex lock;
+    static std::set<std::pair<const void *, int>> done;
+    int device = 0, most = 0;
+    cudaGetDevice(&device);
+    std::lock_guard<std::mutex> guard(lock);
+    if (done.count({kernel, device})) return true;
+    cudaFuncAttributes at;
+    const bool ok = cudaDeviceGetAttribute(&most, cudaDevAttrMaxSharedMemoryPerBlockOptin, device) == cudaSuccess &&
+                    cudaFuncGetAttributes(&at, kernel) == cudaSuccess &&
+                    cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                         most - (int)at.sharedSizeBytes) == cudaSuccess;
+    if (!ok) cudaGetLastError();
+    else done.insert({kernel, device});
+    return ok;
+}
+
+}  // namespace pdb
 
 extern "C" {
 

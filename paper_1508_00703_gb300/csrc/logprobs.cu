@@ -6,10 +6,10 @@
 //   log p_j = (z_j - m) scale - ln s,  lse = m scale + ln s,  entropy = ln s - ln2 w / s
 // The row's blocks hand (m, s, w) to the cluster's first one through its shared memory.
 //
-// Alternatives.  The pass keeps the maximum of each of 32 to 128 groups of
-// neighbouring threads.  The k-th largest of them, tau, is at most the k-th largest
-// logit, since k different logits reach it, and the groups that reach tau (k, and those
-// that tie) hold every logit that does.  Only those groups' vectors are read again (from L2), their logits
+// Alternatives.  The pass keeps the maximum of each of 64 or 128 groups of
+// neighbouring threads.  A value tau that k of them reach is at most the k-th largest
+// logit, since k different logits reach it, and the groups that reach tau hold every logit that
+// does.  Only those groups' vectors are read again (from L2), their logits
 // >= tau collected (a few more than k as a rule) and ranked by counting.  Where more
 // than the buffer reach tau (ties, masked rows) or a NaN hides from the maxima, a radix
 // selection over the block's share takes over: four counting passes, exact for
@@ -125,7 +125,7 @@ __device__ __noinline__ void select_keys(TopShared &t, const T *row, int j0, int
 
 // best[0..k) = the block's share's k largest; returns how many there are
 template <typename T, int THREADS>
-__device__ __forceinline__ int top_of_share(TopShared &t, const T *row, const uint4 *body, const Share &sh, float top,
+__device__ __forceinline__ int top_of_share(TopShared &t, const T *row, const uint4 *share, const Share &sh, float top,
                                             bool odd, int k)
 {
     constexpr int E = Vec<T>::E;
@@ -137,31 +137,40 @@ __device__ __forceinline__ int top_of_share(TopShared &t, const T *row, const ui
         return have;
     }
     if (!odd) {
-        // At least twice as many groups as alternatives, so that few more than k logits reach tau: fewer groups are
-        // cheaper to rank, but longer to read again.
-        const int groups = k <= 16 ? 32 : k <= 32 ? 64 : GROUPS, per = THREADS / groups;
+        // groups of `per` neighbouring threads: fewer for few alternatives
+        const int per = THREADS / (k <= 16 ? GROUPS / 2 : GROUPS), groups = THREADS / per;
         for (int off = per >> 1; off >= 1; off >>= 1) top = fmaxf(top, __shfl_xor_sync(FULL, top, off));
         if (threadIdx.x % (unsigned)per == 0) t.group[threadIdx.x / (unsigned)per] = top;
         if (threadIdx.x == 0) t.n = t.n_list = 0;
         __syncthreads();
-        if ((int)threadIdx.x < groups) {
-            const float mine = t.group[threadIdx.x];
-            int above = 0;
-            for (int g = 0; g < groups; g += 4) {
-                const float4 o = *reinterpret_cast<const float4 *>(t.group + g);
-                const int me = (int)threadIdx.x - g;
-                above += (o.x > mine || (o.x == mine && 0 < me) ? 1 : 0) + (o.y > mine || (o.y == mine && 1 < me) ? 1 : 0) +
-                         (o.z > mine || (o.z == mine && 2 < me) ? 1 : 0) + (o.w > mine || (o.w == mine && 3 < me) ? 1 : 0);
+        if (threadIdx.x < 32) {
+            // tau by bisection over the orders of the groups' maxima: any value that k groups reach will do, the higher
+            // the better; it stops when hardly more than k do
+            uint32_t o[GROUPS / 32], lo = 0, hi = 0;
+#pragma unroll
+            for (int i = 0; i < GROUPS / 32; ++i) {
+                o[i] = i * 32 < groups ? order_of(t.group[i * 32 + threadIdx.x]) : 0u;
+                hi = max(hi, o[i]);
             }
-            if (above == k - 1) t.tau = mine;
+            hi = __reduce_max_sync(FULL, hi) + 1;          // no group reaches hi; all reach lo
+            while (hi - lo > 1) {
+                const uint32_t mid = lo + (hi - lo) / 2;
+                int n = 0;
+#pragma unroll
+                for (int i = 0; i < GROUPS / 32; ++i) n += __popc(__ballot_sync(FULL, o[i] >= mid));
+                if (n >= k) lo = mid;
+                else hi = mid;
+                if (n >= k && n <= k + 1 + k / 8) break;
+            }
+            if (threadIdx.x == 0) t.tau = order_value(lo == 0 ? order_of(-INFINITY) : lo);
         }
         __syncthreads();
         const float tau = t.tau;
         if ((int)threadIdx.x < groups && t.group[threadIdx.x] >= tau) t.list[atomicAdd(&t.n_list, 1)] = threadIdx.x;
         __syncthreads();
-        const int n_list = t.n_list;    // k, or more where groups tie
-        // a warp reads one group's vectors: per at a time lie side by side
-        const int lane = threadIdx.x & 31, wide = min(per, 32), sub = lane % (unsigned)wide;
+        const int n_list = t.n_list;    // k, or somewhat more
+        // a warp reads one group's vectors, `per` of them side by side
+        const int lane = threadIdx.x & 31, sub = lane % (unsigned)per, n_vec = sh.v1 - sh.v0;
         auto take = [&](float z, int j) {
             if (z >= tau) {
                 const int at = atomicAdd(&t.n, 1);
@@ -169,16 +178,17 @@ __device__ __forceinline__ int top_of_share(TopShared &t, const T *row, const ui
             }
         };
         for (int g = threadIdx.x >> 5; g < n_list; g += THREADS / 32) {
-            const int first = sh.v0 + t.list[g] * per + sub;
-            for (int v = first + lane / (unsigned)wide * THREADS; v < sh.v1; v += 32 / (unsigned)wide * THREADS) {
+            const int member = t.list[g] * per + sub, start = (member & ~31) * UNROLL + (member & 31);
+            for (int i = lane / (unsigned)per;; i += 32 / (unsigned)per) {
+                const int v = start + i / UNROLL * (THREADS * UNROLL) + i % UNROLL * 32;
+                if (i / UNROLL * (THREADS * UNROLL) >= n_vec) break;
+                if (v >= n_vec) continue;
+                const uint4 x = ld_keep(share + v);
+                if (Vec<T>::max_float(Vec<T>::vmax(Vec<T>::max_init(), x)) < tau) continue;
                 float f[E];
-                Vec<T>::unpack(ld_keep(body + v), f);
-                float mx = f[0];
+                Vec<T>::unpack(x, f);
 #pragma unroll
-                for (int i = 1; i < E; ++i) mx = fmaxf(mx, f[i]);
-                if (mx >= tau)
-#pragma unroll
-                    for (int i = 0; i < E; ++i) take(f[i], sh.head + v * E + i);
+                for (int e = 0; e < E; ++e) take(f[e], sh.b0 + v * E + e);
             }
         }
         if ((int)threadIdx.x < sh.edges()) take(to_float(row[sh.edge(threadIdx.x)]), sh.edge(threadIdx.x));
@@ -201,7 +211,7 @@ struct LogprobsOut {
 };
 
 template <typename T, bool ENT, bool TOP, int THREADS>
-__global__ __launch_bounds__(THREADS) void k_logprobs(const T *__restrict__ logits, int cols, int64_t stride, Ids ids,
+__global__ __launch_bounds__(THREADS, 1024 / THREADS) void k_logprobs(const T *__restrict__ logits, int cols, int64_t stride, Ids ids,
                                                       float scale, int64_t ignore, int k, LogprobsOut out, int *status)
 {
     __shared__ float part[96];
@@ -213,33 +223,41 @@ __global__ __launch_bounds__(THREADS) void k_logprobs(const T *__restrict__ logi
     const int64_t r = blockIdx.x / (unsigned)blocks;
     const T *row = logits + r * stride;
     const Share sh = share_of(row, cols, rank, blocks);
-    const uint4 *body = reinterpret_cast<const uint4 *>(row + sh.head);
+    const uint4 *body = reinterpret_cast<const uint4 *>(row + sh.b0);
+    const int n_vec = sh.v1 - sh.v0;
     const float c = __fmul_rn(scale, LOG2E);
 
-    // the given token's logit, on its way while the row is read
-    int64_t given = -1;
-    float z_given = 0.0f;
+    // the given token, then its logit, on their way while the row is read
+    const bool asks = out.logp && rank == 0 && threadIdx.x == 0;
+    int2 raw = {0, 0};
+    if (asks) raw = fetch_id(ids, r);
+    T z_given = from_float<T>(0.0f);
     bool there = false;
-    if (out.logp && rank == 0 && threadIdx.x == 0) {
-        given = load_id(ids, r);
+    auto ask = [&]() {
+        const int64_t given = id_of(ids, raw);
         there = given != ignore && given >= 0 && given < cols;
         if (!there && given != ignore) set_status(status, PDB_ERANGE);
-        if (there) z_given = to_float(row[given]);
-    }
+        if (there) z_given = row[given];
+    };
+    const bool has_edge = (int)threadIdx.x < sh.edges();
+    T z_edge = from_float<T>(0.0f);
+    if (has_edge) z_edge = row[sh.edge(threadIdx.x)];
     Stat<ENT> a;
     float top = -INFINITY;
     {
         uint4 v[UNROLL];
-        load_vectors<T, THREADS>(v, body, sh.v0, sh.v1);
-        for (int base = sh.v0; base < sh.v1; base += THREADS * UNROLL) {
+        load_vectors<T, THREADS>(v, body, 0, n_vec);
+        for (int base = 0; base < n_vec; base += THREADS * UNROLL) {
             uint4 next[UNROLL];
-            load_vectors<T, THREADS>(next, body, base + THREADS * UNROLL, sh.v1);
+            load_vectors<T, THREADS>(next, body, base + THREADS * UNROLL, n_vec);
             add_vectors<T, ENT>(a, v, c, top);
 #pragma unroll
             for (int u = 0; u < UNROLL; ++u) v[u] = next[u];
+            if (base == 0 && asks) ask();
         }
+        if (n_vec == 0 && asks) ask();
     }
-    if ((int)threadIdx.x < sh.edges()) add_element(a, to_float(row[sh.edge(threadIdx.x)]), c);
+    if (has_edge) add_element(a, to_float(z_edge), c);
     block_join<THREADS>(a, c, part);
     int have = 0;
     if (TOP) have = top_of_share<T, THREADS>(t, row, body, sh, top, !(a.s < INFINITY), k);
@@ -273,7 +291,7 @@ __global__ __launch_bounds__(THREADS) void k_logprobs(const T *__restrict__ logi
         if (out.lse) out.lse[r] = none ? -INFINITY : __fmaf_rn(ref, scale, logs);
         if (out.entropy) out.entropy[r] = none ? 0.0f : __fmaf_rn(-LN2, __fdiv_rn(a.w, a.s), logs);
         if (out.logp)
-            out.logp[r] = !there ? 0.0f : none ? -INFINITY : __fmaf_rn(__fsub_rn(z_given, ref), scale, -logs);
+            out.logp[r] = !there ? 0.0f : none ? -INFINITY : __fmaf_rn(__fsub_rn(to_float(z_given), ref), scale, -logs);
     }
     if (TOP)
         for (int i = threadIdx.x; i < k; i += THREADS) {
@@ -302,9 +320,10 @@ __global__ __launch_bounds__(THREADS) void k_logprobs_grad(const T *logits, int 
     const T *row = logits + r * stride;
     T *drow = dlogits + r * out_stride;
     const Share sh = share_of(row, cols, piece, pieces);
-    const uint4 *body = reinterpret_cast<const uint4 *>(row + sh.head);
+    const uint4 *body = reinterpret_cast<const uint4 *>(row + sh.b0);
+    const int n_vec = sh.v1 - sh.v0;
     uint4 v[UNROLL];
-    load_vectors<T, THREADS>(v, body, sh.v0, sh.v1);      // on their way while the row's numbers arrive
+    load_vectors<T, THREADS>(v, body, 0, n_vec);          // on their way while the row's numbers arrive
 
     float g = dlogp ? dlogp[r] : 0.0f;
     const float h = dentropy ? dentropy[r] : 0.0f;
@@ -327,17 +346,17 @@ __global__ __launch_bounds__(THREADS) void k_logprobs_grad(const T *logits, int 
         const float x = max_nan(__fmul_rn(__fsub_rn(z, ref), c), -200.0f);
         return __fmul_rn(ex2(x), __fmaf_rn(B, x, A));
     };
-    const bool aligned = ((uintptr_t)(drow + sh.head) & 15) == 0;
-    for (int base = sh.v0; base < sh.v1; base += THREADS * UNROLL) {
+    const bool aligned = ((uintptr_t)(drow + sh.b0) & 15) == 0;
+    for (int base = 0; base < n_vec; base += THREADS * UNROLL) {
         uint4 next[UNROLL];
-        load_vectors<T, THREADS>(next, body, base + THREADS * UNROLL, sh.v1);
+        load_vectors<T, THREADS>(next, body, base + THREADS * UNROLL, n_vec);
 #pragma unroll
         for (int u = 0; u < UNROLL; ++u) {
-            const int i = base + (int)threadIdx.x + u * THREADS;
-            if (i < sh.v1) {
+            const int i = base + lane_start() + u * 32;
+            if (i < n_vec) {
                 float f[E];
                 Vec<T>::unpack(v[u], f);
-                const int j = sh.head + i * E;
+                const int j = sh.b0 + i * E;
 #pragma unroll
                 for (int e = 0; e < E; ++e) f[e] = zero ? 0.0f : slope(f[e]);
                 if ((unsigned)(t - j) < (unsigned)E && !zero)
@@ -383,13 +402,13 @@ int pdb_logprobs(pdb_tokens *t, const pdb_mat *logits, const pdb_ids *ids, float
     const LogprobsOut out{logp, lse, entropy, top_logp, top_ids};
     return with_type(logits->type, [&](auto *a) {
         using T = std::remove_pointer_t<decltype(a)>;
-        const Shape shape = row_shape(logits->rows, logits->cols, Vec<T>::E, t->sms);
+        const Shape shape = once_shape(logits->rows, logits->cols, Vec<T>::E, t->sms, 0, false);
         return with_threads(shape.threads, [&](auto n) {
             constexpr int N = decltype(n)::value;
             const auto kernel = entropy ? (top ? k_logprobs<T, true, true, N> : k_logprobs<T, true, false, N>)
                                         : (top ? k_logprobs<T, false, true, N> : k_logprobs<T, false, false, N>);
-            return launch_rows(kernel, logits->rows, shape, 0, s, (const T *)logits->data, (int)logits->cols,
-                               stride_of(logits), ids_of(ids, logp), scale, ignore, (int)k, out, t->status);
+            return launch_rows(kernel, shape, s, (const T *)logits->data, (int)logits->cols, stride_of(logits),
+                               ids_of(ids, logp), scale, ignore, (int)k, out, t->status);
         });
     });
 }
@@ -414,9 +433,12 @@ int pdb_logprobs_grad(pdb_tokens *t, const pdb_mat *logits, const pdb_ids *ids, 
     TokensUse use{t, s};
     return with_type(logits->type, [&](auto *a) {
         using T = std::remove_pointer_t<decltype(a)>;
-        Shape shape = row_shape(logits->rows, logits->cols, Vec<T>::E, t->sms);
-        const int pieces = shape.blocks;
-        return with_threads(shape.threads, [&](auto n) {
+        // pieces of about 4 vectors a thread and, for few rows, as many as there are SMs
+        const int64_t nv = logits->cols / Vec<T>::E + 1;
+        const int threads = nv < 1024 ? 128 : nv < 4096 ? 256 : 512;
+        int pieces = 1;
+        while (pieces < 64 && logits->rows * pieces < t->sms && nv / (2 * pieces) >= threads) pieces *= 2;
+        return with_threads(threads, [&](auto n) {
             constexpr int N = decltype(n)::value;
             k_logprobs_grad<T, N><<<(unsigned)(logits->rows * pieces), N, 0, s>>>(
                 (const T *)logits->data, (int)logits->cols, stride_of(logits), pieces, ids_of(ids, dlogp), scale, ignore,

@@ -1,5 +1,5 @@
-// One pass over a row of logits with the running maximum and sum of its softmax,
-// shared by logprobs.cu and distill.cu.
+// Rows of logits for logprobs.cu and distill.cu: shares of a row, running softmax
+// statistics, and the stream that brings the rows into shared memory.
 //
 // A row is worked on by a cluster of 1 to 8 blocks, one share each.  From the
 // row's first 16-byte boundary on it is a body of vectors of 16 bytes, split
@@ -7,18 +7,24 @@
 // and after the last vector (rows of odd lengths start anywhere) go to the
 // first and the last block, one element a thread.
 //
-// Thread t of a block holds the vectors t, t + THREADS, ... of its share, UNROLL
-// of them in registers at a time (64 bytes in flight per thread); what lies past
-// the share's end is filled with -inf, which adds nothing.
+// A share is worked on in chunks of THREADS * UNROLL vectors; warp w of the block has the chunk's vectors from 32 UNROLL w on,
+// UNROLL rows of 32.  Where a row is visited once they are loaded into registers, a chunk
+// ahead, and many small blocks share an SM: what one waits for at its row's end the others fill.
+// Where a row is visited twice (statistics, then gradient) clusters are persistent, cluster i taking the
+// rows i, i + clusters, ..., and the vectors travel by bulk copies through a ring in shared memory that keeps
+// as much of the row as fits for the second visit; the copies run over row ends, so that while a
+// row's statistics are joined the next row's first chunks arrive.
 #pragma once
 
 #include <cooperative_groups.h>
+
+#include <algorithm>
 
 #include "tokens.cuh"
 
 namespace pdb {
 
-constexpr int UNROLL = 4;
+constexpr int UNROLL = 4;               // vectors of a thread under way in registers
 constexpr int MAX_CLUSTER = 8;
 constexpr float LOG2E = 1.44269504088896340736f, LN2 = 0.69314718055994530942f;
 
@@ -36,8 +42,81 @@ __device__ __forceinline__ float max_nan(float a, float b)
     return y;
 }
 
-// logits are read through L2 only: the first pass leaves them there for the second,
-// the last pass marks them first to go
+// two fp32 operations in one instruction
+__device__ __forceinline__ uint64_t pair(float lo, float hi)
+{
+    uint64_t p;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(p) : "f"(lo), "f"(hi));
+    return p;
+}
+__device__ __forceinline__ void unpair(uint64_t p, float &lo, float &hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(p)); }
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b)
+{
+    uint64_t y;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(y) : "l"(a), "l"(b));
+    return y;
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b)
+{
+    uint64_t y;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(y) : "l"(a), "l"(b));
+    return y;
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c)
+{
+    uint64_t y;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(y) : "l"(a), "l"(b), "l"(c));
+    return y;
+}
+
+// ---- transaction barriers in shared memory, and bulk copies that complete on them
+__device__ __forceinline__ unsigned shared_addr(const void *p) { return (unsigned)__cvta_generic_to_shared(p); }
+__device__ __forceinline__ void bar_init(uint64_t *bar, unsigned count)
+{
+    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(shared_addr(bar)), "r"(count) : "memory");
+}
+__device__ __forceinline__ void bar_arrive(uint64_t *bar)
+{
+    asm volatile("{ .reg .b64 t; mbarrier.arrive.shared::cta.b64 t, [%0]; }" ::"r"(shared_addr(bar)) : "memory");
+}
+__device__ __forceinline__ void bar_expect(uint64_t *bar, unsigned bytes)
+{
+    asm volatile("{ .reg .b64 t; mbarrier.arrive.expect_tx.shared::cta.b64 t, [%0], %1; }" ::"r"(shared_addr(bar)), "r"(bytes)
+                 : "memory");
+}
+__device__ __forceinline__ bool bar_done(uint64_t *bar, unsigned parity)
+{
+    unsigned ok;
+    asm volatile("{ .reg .pred p; mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2; selp.u32 %0, 1, 0, p; }"
+                 : "=r"(ok) : "r"(shared_addr(bar)), "r"(parity) : "memory");
+    return ok != 0;
+}
+__device__ __forceinline__ uint4 ld_shared(unsigned at)
+{
+    uint4 v;
+    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
+    return v;
+}
+// four floats into shared memory of block `rank` of the cluster at the place that `to` has in this one, completing on that
+// block's barrier at `bar`'s place
+__device__ __forceinline__ void send_async(float *to, uint64_t *bar, int rank, float a, float b, float c, float d)
+{
+    unsigned dst, dbar;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(dst) : "r"(shared_addr(to)), "r"(rank));
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(dbar) : "r"(shared_addr(bar)), "r"(rank));
+    asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v4.f32 [%0], {%1, %2, %3, %4}, [%5];" ::"r"(dst), "f"(a),
+                 "f"(b), "f"(c), "f"(d), "r"(dbar)
+                 : "memory");
+}
+// `bytes` (a multiple of 16, both ends 16-byte aligned) from global to this block's shared memory
+__device__ __forceinline__ void bulk_copy(void *to, const void *from, unsigned bytes, uint64_t *bar)
+{
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(shared_addr(to)),
+                 "l"(from), "r"(bytes), "r"(shared_addr(bar))
+                 : "memory");
+}
+
+// logits that are read once, or again by few threads, come through L2 only
 __device__ __forceinline__ uint4 ld_keep(const uint4 *p)
 {
     uint4 v;
@@ -45,14 +124,6 @@ __device__ __forceinline__ uint4 ld_keep(const uint4 *p)
                  : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p) : "memory");
     return v;
 }
-__device__ __forceinline__ uint4 ld_last(const uint4 *p)
-{
-    uint4 v;
-    asm volatile("ld.global.cs.v4.u32 {%0, %1, %2, %3}, [%4];"
-                 : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p) : "memory");
-    return v;
-}
-
 // 16 bytes of elements: unpacking, packing, maximum
 template <typename T>
 struct Vec;
@@ -211,37 +282,48 @@ struct Stat {
     }
 };
 
-// adds a thread's UNROLL vectors.  Per element: unpacking, (z - m) c in two roundings,
-// the exponential, its sum and, with ENT, the sum of e x (x held above -200, where e = 0, so
-// that e x of a token masked by -inf is 0 and not a NaN).
-template <typename T, bool ENT>
-__device__ __forceinline__ void add_vectors(Stat<ENT> &a, const uint4 (&v)[UNROLL], float c, float &top)
+// Adds a thread's N vectors.  Per two elements: unpacking, (z - m) c in two roundings, two
+// exponentials, their sum and, with ENT, the sum of e x (x held above -200, where e = 0, so that e x
+// of a token masked by -inf is 0 and not a NaN).  The reference m moves only when the vectors'
+// maximum passes it by 2^8: e <= 2^8 until then costs no precision.
+template <typename T, bool ENT, int N>
+__device__ __forceinline__ void add_vectors(Stat<ENT> &a, const uint4 (&v)[N], float c, float &top)
 {
     constexpr int E = Vec<T>::E;
     typename Vec<T>::Max mx = Vec<T>::max_init();
 #pragma unroll
-    for (int u = 0; u < UNROLL; ++u) mx = Vec<T>::vmax(mx, v[u]);
+    for (int u = 0; u < N; ++u) mx = Vec<T>::vmax(mx, v[u]);
     const float cm = Vec<T>::max_float(mx);
     top = fmaxf(top, cm);
-    a.rebase(fmaxf(a.m, cm), c);
-    const float m = a.m;
-    float ps[UNROLL], pw[UNROLL];                 // UNROLL short chains of sums
+    if (__fmul_rn(__fsub_rn(cm, a.m), c) > 8.0f) a.rebase(cm, c);
+    const uint64_t m2 = pair(-a.m, -a.m), c2 = pair(c, c);
+    uint64_t ps[2] = {0, 0}, pw[2] = {0, 0};      // short chains of sums
 #pragma unroll
-    for (int u = 0; u < UNROLL; ++u) {
+    for (int u = 0; u < N; ++u) {
         float f[E];
         Vec<T>::unpack(v[u], f);
-        ps[u] = pw[u] = 0.0f;
 #pragma unroll
-        for (int i = 0; i < E; ++i) {
-            float x = __fmul_rn(__fsub_rn(f[i], m), c);
-            if (ENT) x = max_nan(x, -200.0f);
-            const float e = ex2(x);
-            ps[u] = __fadd_rn(ps[u], e);
-            if (ENT) pw[u] = __fmaf_rn(e, x, pw[u]);
+        for (int i = 0; i < E; i += 2) {
+            uint64_t x = mul2(add2(pair(f[i], f[i + 1]), m2), c2);
+            float x0, x1;
+            unpair(x, x0, x1);
+            if (ENT) {
+                x0 = max_nan(x0, -200.0f), x1 = max_nan(x1, -200.0f);
+                x = pair(x0, x1);
+            }
+            const uint64_t e = pair(ex2(x0), ex2(x1));
+            const int k = (i >> 1) & 1;
+            ps[k] = add2(ps[k], e);
+            if (ENT) pw[k] = fma2(e, x, pw[k]);
         }
     }
-    a.s = __fadd_rn(a.s, __fadd_rn(__fadd_rn(ps[0], ps[1]), __fadd_rn(ps[2], ps[3])));
-    if (ENT) a.w = __fadd_rn(a.w, __fadd_rn(__fadd_rn(pw[0], pw[1]), __fadd_rn(pw[2], pw[3])));
+    float lo, hi;
+    unpair(add2(ps[0], ps[1]), lo, hi);
+    a.s = __fadd_rn(a.s, __fadd_rn(lo, hi));
+    if (ENT) {
+        unpair(add2(pw[0], pw[1]), lo, hi);
+        a.w = __fadd_rn(a.w, __fadd_rn(lo, hi));
+    }
 }
 
 // one more element
@@ -255,19 +337,30 @@ __device__ __forceinline__ void add_element(Stat<ENT> &a, float z, float c)
     if (ENT) a.w = __fmaf_rn(e, x, a.w);
 }
 
-// the vectors base + threadIdx.x + u * THREADS below `end`
+// where a thread's vectors of a chunk start; they are 32 apart
+__device__ __forceinline__ int lane_start() { return (int)(threadIdx.x & ~31u) * UNROLL + (int)(threadIdx.x & 31); }
+
+// a thread's vectors of the chunk at `base` of a share of `end` vectors, -inf past it
 template <typename T, int THREADS>
-__device__ __forceinline__ void load_vectors(uint4 (&v)[UNROLL], const uint4 *__restrict__ body, int base, int end)
+__device__ __forceinline__ void load_vectors(uint4 (&v)[UNROLL], const uint4 *__restrict__ share, int base, int end)
 {
     constexpr uint32_t N = Vec<T>::NEG_INF;
+    const int first = base + lane_start();
+    const uint4 *from = share + first;
+    if (base + UNROLL * THREADS <= end) {
 #pragma unroll
-    for (int u = 0; u < UNROLL; ++u) {
-        const int i = base + (int)threadIdx.x + u * THREADS;
-        v[u] = i < end ? ld_keep(body + i) : uint4{N, N, N, N};
+        for (int u = 0; u < UNROLL; ++u) v[u] = ld_keep(from + u * 32);
+    } else {
+#pragma unroll
+        for (int u = 0; u < UNROLL; ++u) {
+            v[u] = uint4{N, N, N, N};
+            if (first + u * 32 < end) v[u] = ld_keep(from + u * 32);
+        }
     }
 }
 
-// joins the threads' statistics over the block, on every thread; `part` holds 3 * 32 floats
+// joins the threads' statistics over the block, on every thread, with one barrier; `part` holds 3 * 32 floats and is
+// not used again before another barrier
 template <int THREADS, bool ENT>
 __device__ __forceinline__ void block_join(Stat<ENT> &a, float c, float *part)
 {
@@ -283,20 +376,192 @@ __device__ __forceinline__ void block_join(Stat<ENT> &a, float c, float *part)
     a.template warp_join<W>(c);
 }
 
-// How many blocks share a row, and how many threads a block has.
-//   threads  one for every four vectors of a row, 128 to 512
-//   blocks   as long as the grid then still is at most two blocks per SM and each
-//            thread keeps a vector: a row alone on one SM is bound by that SM's loads
-struct Shape {
-    int blocks, threads;
+constexpr int MOST_SLOTS = 16;
+
+// One block's shares of its cluster's rows, chunk after chunk of SPAN = THREADS * UNROLL vectors, each row twice.
+// Thread 0 brings the chunks by bulk copies into `slots` places, in turn; a place is free again
+// when every warp has given it back.  A row's last `hold` chunks stay in their places after the first visit and
+// come again from there; the ones before are brought once more, after the held ones (L2 has seen them
+// a few microseconds ago).  Every wait has a limit, after which the status word holds PDB_ETIMEOUT and no
+// wait of the thread waits again.
+template <typename T, int THREADS>
+struct Stream {
+    static constexpr int SPAN = THREADS * UNROLL;
+    static constexpr unsigned LIMIT = 1u << 22;     // tries; one takes some 20 ns to a microsecond
+    uint4 *place;                       // slots * SPAN vectors
+    uint64_t *full, *empty;             // a barrier for each place
+    int *status;
+    int slots, hold;
+    int slot;                           // the next place to take
+    unsigned parity;                    // its full barrier's
+    bool gave_up;
+    // thread 0: what it brings next, and to where
+    const T *logits;
+    int64_t stride, rows, step, row;
+    int cols, rank, blocks;
+    int v, v_end, v_first, v_held;      // vectors: next, end of this sweep, the share's first, first held one
+    const uint4 *body;
+    int at, owed;                       // its place; places given back and not yet filled
+    unsigned free_parity;
+
+    __device__ __forceinline__ void wait(uint64_t *bar, unsigned par)
+    {
+        if (bar_done(bar, par) || gave_up) return;
+        for (unsigned i = 0; i < LIMIT; ++i)
+            if (bar_done(bar, par)) return;
+        set_status(status, PDB_ETIMEOUT);
+        gave_up = true;
+    }
+    // chunks of a share that pass through, before the held ones
+    __device__ __forceinline__ int passing(int n_vec) const { return max(0, (max(n_vec, 1) + SPAN - 1) / SPAN - hold); }
+    __device__ __forceinline__ void open()
+    {
+        if (row < rows) {
+            const T *r = logits + row * stride;
+            const Share s = share_of(r, cols, rank, blocks);
+            body = reinterpret_cast<const uint4 *>(r + s.head);
+            v = v_first = s.v0, v_end = s.v1;
+            v_held = s.v0 + passing(s.v1 - s.v0) * SPAN;
+        }
+    }
+    // `bars` holds 2 * MOST_SLOTS barriers; a barrier of the block follows before the first take
+    __device__ __forceinline__ void start(const T *logits_, int64_t stride_, int64_t rows_, int cols_, int64_t first,
+                                          int64_t step_, int rank_, int blocks_, uint4 *place_, uint64_t *bars, int slots_,
+                                          int hold_, int *status_)
+    {
+        place = place_, full = bars, empty = bars + MOST_SLOTS, status = status_, slots = slots_, hold = hold_;
+        slot = 0, parity = 0, gave_up = false;
+        if (threadIdx.x == 0) {
+            logits = logits_, stride = stride_, rows = rows_, cols = cols_, row = first, step = step_, rank = rank_;
+            blocks = blocks_, at = owed = 0, free_parity = 1;
+            for (int i = 0; i < slots; ++i) {
+                bar_init(full + i, 1);
+                bar_init(empty + i, THREADS / 32);
+            }
+            asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            open();
+            for (int i = 0; i < slots; ++i) bring();
+        }
+    }
+    // thread 0: brings the next chunk (a row without vectors has one empty chunk), if there is one
+    __device__ __forceinline__ void bring()
+    {
+        if (row >= rows) return;
+        wait(empty + at, free_parity);
+        const int n = min(SPAN, v_end - v);
+        bar_expect(full + at, n * 16);
+        if (n > 0) bulk_copy(place + at * SPAN, body + v, n * 16, full + at);
+        v += SPAN;
+        if (v >= v_end) {
+            if (v_end != v_held && v_held != v_first) {
+                v = v_first, v_end = v_held;        // the second sweep: the passing chunks once more
+            } else {
+                row += step;
+                open();
+            }
+        }
+        if (++at == slots) at = 0, free_parity ^= 1;
+    }
+    // the next chunk's place, once it is there
+    __device__ __forceinline__ int take()
+    {
+        wait(full + slot, parity);
+        const int p = slot;
+        if (++slot == slots) slot = 0, parity ^= 1;
+        return p;
+    }
+    // this thread's vectors in place p
+    __device__ __forceinline__ void read(uint4 (&x)[UNROLL], int p) const
+    {
+        const unsigned at = shared_addr(place) + (unsigned)(p * SPAN + lane_start()) * 16;
+#pragma unroll
+        for (int u = 0; u < UNROLL; ++u) x[u] = ld_shared(at + u * 512);
+    }
+    // the place of the chunk taken n takes ago
+    __device__ __forceinline__ int before(int n) const { return slot - n < 0 ? slot - n + slots : slot - n; }
+    // this warp has done with place p.  Thread 0 fills the place given back before that one, which the other warps are
+    // likely to have done with too.
+    __device__ __forceinline__ void give_back(int p)
+    {
+        __syncwarp();
+        if ((threadIdx.x & 31) == 0) {
+            bar_arrive(empty + p);
+            if (threadIdx.x == 0 && owed++) bring(), --owed;
+        }
+        __syncwarp();
+    }
+    // fills what is left, after a barrier of the block
+    __device__ __forceinline__ void settle()
+    {
+        if (threadIdx.x == 0 && owed) bring(), owed = 0;
+    }
 };
-inline Shape row_shape(int64_t rows, int64_t cols, int vec, int sms)
+
+// How a call is cut: blocks of a cluster, threads of a block, clusters, dynamic shared memory; for the stream also its
+// places, and how many chunks of a row are held.
+struct Shape {
+    int blocks, threads, map_bytes, bit_bytes;
+    int64_t clusters;
+    size_t smem;
+    int slots, hold;
+};
+constexpr size_t SMEM_PER_SM = 228 << 10, STATIC_SMEM = 3072;
+
+// blocks of a cluster: while they still find room on the SMs all at once and each thread has a vector.  A row alone on one
+// SM is bound by what that SM can have under way (4 x 128,000 bf16: 8 blocks 8.9 us, one 11.7)
+inline int cluster_of(int64_t rows, int64_t nv, int threads, int64_t resident)
 {
-    const int64_t nv = (cols + vec - 1) / vec;
-    Shape s;
-    s.threads = nv >= 2048 ? 512 : nv >= 1024 ? 256 : 128;
-    s.blocks = 1;
-    while (s.blocks < MAX_CLUSTER && rows * s.blocks * 2 <= (int64_t)sms * 2 && nv / (s.blocks * 2) >= s.threads) s.blocks *= 2;
+    int blocks = 1;
+    while (blocks < MAX_CLUSTER && rows * blocks * 2 <= resident && nv / (blocks * 2) >= threads) blocks *= 2;
+    return blocks;
+}
+
+// a share's marks: a bit per vector, in whole chunks, then a byte per vector
+inline void set_maps(Shape &s, int64_t vectors)
+{
+    const int64_t chunk = s.threads * UNROLL;
+    s.bit_bytes = (int)((vectors + chunk - 1) / chunk * chunk / 8);
+    s.map_bytes = s.bit_bytes + (int)((vectors + 15) / 16 * 16);
+}
+
+// One visit per row: a cluster per row.  Many rows: small blocks, whose waits at a row's ends overlap (1024 x 32,000 fp16:
+// 128 threads 16 us, 256 19, 512 27), 256 threads for rows of 128 KB and more (4096 x 128,000 bf16: 5 us of 157).
+// Few rows: as many threads as have two vectors each, up to 512.
+inline Shape once_shape(int64_t rows, int64_t cols, int vec, int sms, size_t extra, bool map)
+{
+    const int64_t nv = cols / vec + 1;
+    Shape s = {};
+    s.threads = rows < sms ? (nv < 1024 ? 128 : nv < 2048 ? 256 : 512) : nv < 8192 ? 128 : 256;
+    s.blocks = cluster_of(rows, nv, s.threads, sms);
+    while (map && nv / s.blocks > 65536 && s.blocks < MAX_CLUSTER) s.blocks *= 2;      // room for the marks
+    if (map) set_maps(s, nv / s.blocks + 1);
+    s.smem = extra + s.map_bytes;
+    s.clusters = rows;
+    return s;
+}
+
+// Two visits per row: persistent clusters, 512 threads of an SM in blocks of 128 (rows up to 96 KB) or 256, each with its part of
+// the SM's shared memory for the stream.  Measured with gradient, us: 8000 x 32,000 bf16 210 by 128 threads, 235 by 256, 335
+// by 512; 4096 x 128,000 bf16 417 by 256 threads and shares of half a row, 469 by 256 and whole rows (their second visit comes from
+// memory: more than L2 keeps is under way), 510 by 512 threads, whose waits nothing fills.
+inline Shape twice_shape(int64_t rows, int64_t cols, int vec, int sms, size_t extra)
+{
+    const int64_t nv = cols / vec + 1;
+    Shape s = {};
+    s.threads = nv < 6144 ? 128 : 256;
+    const int per = 512 / s.threads;
+    s.blocks = cluster_of(rows, nv, s.threads, (int64_t)sms * per);
+    while (nv / s.blocks > 13312 && s.blocks < MAX_CLUSTER) s.blocks *= 2;             // shares of up to 208 KB
+    set_maps(s, nv / s.blocks + 1);
+    const size_t chunk = (size_t)UNROLL * 16 * s.threads, fixed = extra + s.map_bytes;
+    const size_t most = SMEM_PER_SM / per - 1024 - STATIC_SMEM;    // an SM keeps 1 KB for each block
+    const int64_t chunks = std::max<int64_t>(1, (nv / s.blocks + UNROLL * s.threads) / (UNROLL * s.threads));
+    const int64_t fit = fixed < most ? (int64_t)((most - fixed) / chunk) : 0;
+    s.slots = (int)std::max<int64_t>(3, std::min({fit, 2 * chunks + 2, (int64_t)MOST_SLOTS}));
+    s.hold = (int)std::max<int64_t>(1, std::min<int64_t>(chunks, s.slots - 2));
+    s.smem = fixed + s.slots * chunk;
+    s.clusters = std::min(rows, std::max<int64_t>(1, (int64_t)sms * per / s.blocks));
     return s;
 }
 
@@ -309,14 +574,14 @@ inline auto with_threads(int threads, F f)
     return f(Num<128>());
 }
 
-// launch of `rows` clusters
 template <typename... P, typename... A>
-inline int launch_rows(void (*kernel)(P...), int64_t rows, Shape shape, size_t smem, cudaStream_t s, A... args)
+inline int launch_rows(void (*kernel)(P...), const Shape &shape, cudaStream_t s, A... args)
 {
+    if (!allow_smem((const void *)kernel)) return PDB_ECUDA;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(rows * shape.blocks));
+    cfg.gridDim = dim3((unsigned)(shape.clusters * shape.blocks));
     cfg.blockDim = dim3((unsigned)shape.threads);
-    cfg.dynamicSmemBytes = smem;
+    cfg.dynamicSmemBytes = shape.smem;
     cfg.stream = s;
     cudaLaunchAttribute at[1];
     at[0].id = cudaLaunchAttributeClusterDimension;

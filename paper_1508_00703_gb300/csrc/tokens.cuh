@@ -33,6 +33,9 @@ struct TokensUse {
     }
 };
 
+// lets a kernel have all of an SM's shared memory as dynamic one; once per kernel and device
+bool allow_smem(const void *kernel);
+
 inline int type_bytes(int type) { return type == PDB_TYPE_FLOAT ? 4 : 2; }
 
 // PDB_OK for a matrix that the calls accept
@@ -92,6 +95,20 @@ __device__ __forceinline__ int64_t load_id(Ids ids, int64_t i, int k = 0)
 {
     const int64_t at = i * ids.stride + k;
     return ids.wide ? (int64_t)__ldg((const long long *)ids.data + at) : (int64_t)__ldg((const int *)ids.data + at);
+}
+
+// the same in two steps, so that the warp does not wait for the load before it needs the id
+__device__ __forceinline__ int2 fetch_id(Ids ids, int64_t i, int k = 0)
+{
+    const int64_t at = i * ids.stride + k;
+    int2 raw = {0, 0};
+    if (ids.wide) raw = __ldg((const int2 *)ids.data + at);
+    else raw.x = __ldg((const int *)ids.data + at);
+    return raw;
+}
+__device__ __forceinline__ int64_t id_of(Ids ids, int2 raw)
+{
+    return ids.wide ? (int64_t)((uint64_t)(uint32_t)raw.y << 32 | (uint32_t)raw.x) : (int64_t)raw.x;
 }
 
 __device__ __forceinline__ float to_float(float v) { return v; }
