@@ -436,7 +436,8 @@ int pdb_sgd_epoch_ready_noalloc(const pdb_csr *X, const float *y, const uint32_t
  * result its declaration states.  Calls that share a handle must be ordered on
  * one stream.  Sums, softmax statistics and losses are held in fp32; a result
  * in 16 bits is rounded once.  No atomics add floating values: the same inputs
- * give the same bits.  No call allocates but pdb_tokens_create, and all but
+ * give the same bits.  No call allocates but pdb_tokens_create (and pdb_embed_grad above
+ * 65,536 ids: scratch of the radix sort, stream-ordered from the library's pool), and all but
  * pdb_tokens_create and pdb_tokens_status can be recorded into a CUDA graph (keep the
  * handle until the graph's last run has finished: pdb_tokens_free does not wait for it).
  * PDB_LOG prints nothing for these calls. */
@@ -487,8 +488,8 @@ int pdb_embed(pdb_tokens *t, const pdb_mat *table, const pdb_ids *ids, float sca
  * rows are not touched, so that dtable = the table and scale = -eta * scale of
  * pdb_embed make the SGD step in place.  Ids equal to `pad` are left out; so are
  * other ids outside [0, dtable->rows), which are recorded as PDB_ERANGE.
- * The ids are sorted with a stable sort; a run of equal ids is summed in fp32
- * in pieces of 32 sorted positions, the pieces then in order; rounded once to
+ * The ids are sorted with a stable sort; an id's rows are summed in fp32
+ * in pieces of 32, the pieces' sums in an order fixed by their number; rounded once to
  * dtable's type after the old value is added.  dout must not overlap dtable.
  * PDB_ETOOBIG beyond the handle's max_tokens or max_dim. */
 int pdb_embed_grad(pdb_tokens *t, const pdb_ids *ids, const pdb_mat *dout, float scale, int64_t pad, int accumulate,

@@ -6,9 +6,10 @@
 #include <set>
 #include <utility>
 
-#include "tokens.cuh"
+#include "rows.cuh"
 
 using namespace pdb;
+namespace cg = cooperative_groups;
 
 namespace {
 
@@ -23,33 +24,40 @@ template <>
 struct Raw<8> { using type = uint2; };
 template <>
 struct Raw<16> { using type = uint4; };
-template <>
-struct Raw<32> { struct type { uint4 a, b; }; };
 
 template <typename T, int E>
-struct alignas(E * sizeof(T) < 16 ? E * sizeof(T) : 16) Pack {
+struct alignas(E * sizeof(T)) Pack {
     T e[E];
 };
 
+// volatile: the loads of a batch are issued where they are written, all before the first is used
 template <typename T, int E>
 __device__ __forceinline__ Pack<T, E> load_pack(const T *p)
 {
+    constexpr int BYTES = E * sizeof(T);
     Pack<T, E> v;
-    if constexpr (E * sizeof(T) == 32) {
-        reinterpret_cast<uint4 *>(&v)[0] = reinterpret_cast<const uint4 *>(p)[0];
-        reinterpret_cast<uint4 *>(&v)[1] = reinterpret_cast<const uint4 *>(p)[1];
-    } else {
-        using R = typename Raw<E * sizeof(T)>::type;
-        *reinterpret_cast<R *>(&v) = *reinterpret_cast<const R *>(p);
-    }
+    uint32_t *w = reinterpret_cast<uint32_t *>(&v);
+    if constexpr (BYTES == 32)
+        asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                     : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7]) : "l"(p));
+    else if constexpr (BYTES == 16)
+        asm volatile("ld.global.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "l"(p));
+    else if constexpr (BYTES == 8)
+        asm volatile("ld.global.v2.b32 {%0, %1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "l"(p));
+    else if constexpr (BYTES == 4)
+        asm volatile("ld.global.b32 %0, [%1];" : "=r"(w[0]) : "l"(p));
+    else
+        asm volatile("ld.global.b16 %0, [%1];" : "=h"(*reinterpret_cast<uint16_t *>(&v)) : "l"(p));
     return v;
 }
 template <typename T, int E>
 __device__ __forceinline__ void store_pack(T *p, const Pack<T, E> &v)
 {
     if constexpr (E * sizeof(T) == 32) {
-        __stcs(reinterpret_cast<uint4 *>(p), reinterpret_cast<const uint4 *>(&v)[0]);
-        __stcs(reinterpret_cast<uint4 *>(p) + 1, reinterpret_cast<const uint4 *>(&v)[1]);
+        const uint32_t *w = reinterpret_cast<const uint32_t *>(&v);
+        asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]),
+                     "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
+                     : "memory");
     } else if constexpr (E * sizeof(T) == 16) {
         __stcs(reinterpret_cast<uint4 *>(p), *reinterpret_cast<const uint4 *>(&v));
     } else {
@@ -58,10 +66,10 @@ __device__ __forceinline__ void store_pack(T *p, const Pack<T, E> &v)
     }
 }
 
-// whether E elements of each row can be moved as one piece of up to 16 bytes
+// whether E elements of each row can be moved as one piece (up to 32 bytes: a lane's whole sector in one instruction)
 inline bool fits(const pdb_mat *m, int E)
 {
-    const int bytes = std::min(16, E * type_bytes(m->type));
+    const int bytes = E * type_bytes(m->type);
     return m->cols % E == 0 && (uintptr_t)m->data % bytes == 0 &&
            (m->rows < 2 || m->stride * type_bytes(m->type) % bytes == 0);
 }
@@ -113,23 +121,27 @@ __device__ __forceinline__ uint32_t embed_key(Ids ids, int64_t i, int64_t vocab,
     return there ? (uint32_t)v : (uint32_t)vocab;
 }
 
-__global__ void k_embed_keys(Ids ids, int64_t n, int64_t vocab, int64_t pad, uint32_t *__restrict__ key, int *status)
+// more than SORT_MAX ids: the keys for the library's radix sort
+__global__ void k_embed_keys(Ids ids, int64_t n, int64_t vocab, int64_t pad, uint32_t *__restrict__ key, int *long_runs,
+                             int *status)
 {
     const int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
+    if (i == 0) *long_runs = 0;          // for k_embed_sum
     if (i < n) key[i] = embed_key(ids, i, vocab, pad, status);
 }
 
 // Up to RANK_MAX ids: each id's place is the number of smaller ids and of equal ones before it,
-// counted against all of them in shared memory, in one launch.  A block places RANK_IDS ids, its
-// threads in RANK_SLICES slices of the others.
-constexpr int RANK_MAX = 8192, RANK_IDS = 64, RANK_SLICES = 8, RANK_THREADS = RANK_IDS * RANK_SLICES;
+// counted against all of them in shared memory.  A block places RANK_IDS ids, its
+// threads in RANK_SLICES slices of the others.  n^2 comparisons over the whole GPU: the least latency for few ids.
+constexpr int RANK_MAX = 2048, RANK_IDS = 64, RANK_SLICES = 8, RANK_THREADS = RANK_IDS * RANK_SLICES;
 
 __global__ __launch_bounds__(RANK_THREADS) void k_embed_rank(Ids ids, int n, int64_t vocab, int64_t pad,
                                                              uint32_t *__restrict__ skey, int32_t *__restrict__ spos,
-                                                             int *status)
+                                                             int *long_runs, int *status)
 {
     extern __shared__ __align__(16) uint32_t s_key[];       // n, rounded up to 4 * RANK_SLICES
     __shared__ int count[RANK_IDS];
+    if (blockIdx.x == 0 && threadIdx.x == 0) *long_runs = 0;      // for k_embed_sum
     const int padded = (n + 4 * RANK_SLICES - 1) / (4 * RANK_SLICES) * (4 * RANK_SLICES);
     for (int i = threadIdx.x; i < padded; i += RANK_THREADS)
         s_key[i] = i < n ? embed_key(ids, i, vocab, pad, status) : 0xffffffffu;   // the fill counts for nobody
@@ -160,15 +172,149 @@ __global__ __launch_bounds__(RANK_THREADS) void k_embed_rank(Ids ids, int n, int
     }
 }
 
+// Up to SORT_MAX ids: the whole stable sort in one launch, by a cluster of 1 to 8 blocks that keep the pairs (key, position)
+// in their shared memory.  Least significant digit first, one or two passes of up to 10 bits (three above 2^20
+// ids): a warp ranks its pairs by one ballot per digit bit and running counts per digit; the
+// counts are summed over the warps, then over the cluster; the pairs are put in order within the block
+// and then stored where they belong, in whichever block's shared memory that is, neighbours together (stored one by
+// one from their places, 65,536 pairs took 19 us a pass).
+constexpr int SORT_THREADS = 512, SORT_WARPS = SORT_THREADS / 32, SORT_CLUSTER = 8, SORT_MAX = 65536, SORT_BITS = 10;
+
+inline size_t sort_smem(int ipt)
+{
+    return sizeof(uint2) * 2 * SORT_THREADS * ipt + sizeof(uint32_t) * 3 * (1 << SORT_BITS) +
+           sizeof(uint16_t) * SORT_WARPS * (1 << SORT_BITS);
+}
+
+template <int IPT>
+__global__ __launch_bounds__(SORT_THREADS) void k_embed_sort(Ids ids, int n, int64_t vocab, int64_t pad, int passes, int bits,
+                                                             uint32_t *__restrict__ skey, int32_t *__restrict__ spos,
+                                                             int *long_runs, int *status)
+{
+    constexpr int SPAN = SORT_THREADS * IPT;
+    extern __shared__ __align__(16) uint2 s_pair[];         // [SPAN] this block's part of the order: key, position
+    uint2 *s_local = s_pair + SPAN;                         // [SPAN] its pairs by digit
+    uint32_t *s_hist = reinterpret_cast<uint32_t *>(s_local + SPAN);   // [1 << SORT_BITS] its count of each digit
+    uint32_t *s_first = s_hist + (1 << SORT_BITS);          // where each digit starts in s_local
+    uint32_t *s_move = s_first + (1 << SORT_BITS);          // from there to its place in the whole order
+    uint16_t *s_warp = reinterpret_cast<uint16_t *>(s_move + (1 << SORT_BITS));   // [warp][digit]
+    __shared__ uint32_t s_total[2][SORT_WARPS];
+    cg::cluster_group cluster = cg::this_cluster();
+    const int blocks = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const unsigned lt = lanemask_lt();
+    const int radix = 1 << bits;
+    if (rank == 0 && tid == 0) *long_runs = 0;              // for k_embed_sum
+    uint32_t key[IPT];
+    int32_t pos[IPT];
+#pragma unroll
+    for (int i = 0; i < IPT; ++i) {
+        pos[i] = rank * SPAN + warp * (32 * IPT) + i * 32 + lane;
+        key[i] = pos[i] < n ? embed_key(ids, pos[i], vocab, pad, status) : 0xffffffffu;      // the fill sorts behind all
+    }
+    for (int pass = 0; pass < passes; ++pass) {
+        const int shift = pass * bits;
+        uint16_t *count = s_warp + warp * radix;
+        for (int d = lane; d < radix; d += 32) count[d] = 0;
+        __syncwarp();
+        uint32_t place[IPT];
+#pragma unroll
+        for (int i = 0; i < IPT; ++i) {
+            const uint32_t d = key[i] >> shift & (radix - 1);
+            unsigned peers = FULL;
+            for (int b = 0; b < bits; ++b) {
+                const unsigned m = __ballot_sync(FULL, d >> b & 1);
+                peers &= d >> b & 1 ? m : ~m;
+            }
+            place[i] = __popc(peers & lt) | __popc(peers) << 16;
+        }
+#pragma unroll
+        for (int i = 0; i < IPT; ++i) {
+            const uint32_t d = key[i] >> shift & (radix - 1);
+            const uint32_t c = count[d];
+            __syncwarp();
+            if ((place[i] & 0xffff) == 0) count[d] = (uint16_t)(c + (place[i] >> 16));
+            place[i] = c + (place[i] & 0xffff);
+            __syncwarp();
+        }
+        __syncthreads();
+        // digits 2 tid, 2 tid + 1: counts by warp become places, their sums the block's counts
+        uint32_t own[2] = {0, 0};
+        if (2 * tid < radix) {
+#pragma unroll
+            for (int w = 0; w < SORT_WARPS; ++w) {
+                uint32_t *at = reinterpret_cast<uint32_t *>(s_warp + w * radix + 2 * tid);
+                const uint32_t c = *at;
+                *at = own[1] << 16 | own[0];
+                own[0] += c & 0xffff, own[1] += c >> 16;
+            }
+            s_hist[2 * tid] = own[0], s_hist[2 * tid + 1] = own[1];
+        }
+        cluster.sync();                  // every block has its pairs in registers and its counts in place
+        // pairs of the two digits in all blocks, and in those before this one
+        uint32_t all[2] = {0, 0}, before[2] = {0, 0};
+        if (2 * tid < radix)
+            for (int b = 0; b < blocks; ++b) {
+                const uint2 h = *reinterpret_cast<const uint2 *>(cluster.map_shared_rank(s_hist, b) + 2 * tid);
+                all[0] += h.x, all[1] += h.y;
+                if (b < rank) before[0] += h.x, before[1] += h.y;
+            }
+        uint32_t x = all[0] + all[1], y = own[0] + own[1];
+#pragma unroll
+        for (int off = 1; off < 32; off <<= 1) {
+            const uint32_t u = __shfl_up_sync(FULL, x, off), v = __shfl_up_sync(FULL, y, off);
+            if (lane >= off) x += u, y += v;
+        }
+        if (lane == 31) s_total[0][warp] = x, s_total[1][warp] = y;
+        __syncthreads();
+        x -= all[0] + all[1], y -= own[0] + own[1];
+#pragma unroll
+        for (int w = 0; w < SORT_WARPS; ++w)
+            if (w < warp) x += s_total[0][w], y += s_total[1][w];
+        if (2 * tid < radix) {
+            s_first[2 * tid] = y, s_move[2 * tid] = x + before[0] - y;
+            s_first[2 * tid + 1] = y + own[0], s_move[2 * tid + 1] = x + all[0] + before[1] - y - own[0];
+        }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < IPT; ++i) {
+            const uint32_t d = key[i] >> shift & (radix - 1);
+            s_local[s_first[d] + s_warp[warp * radix + d] + place[i]] = make_uint2(key[i], (uint32_t)pos[i]);
+        }
+        __syncthreads();
+        const bool last = pass == passes - 1;
+#pragma unroll
+        for (int i = 0; i < IPT; ++i) {
+            const uint32_t at = i * SORT_THREADS + tid;
+            const uint2 p = s_local[at];
+            const uint32_t to = at + s_move[p.x >> shift & (radix - 1)];
+            if (last) {
+                if (to < (uint32_t)n) skey[to] = p.x, spos[to] = (int32_t)p.y;
+            } else {
+                cluster.map_shared_rank(s_pair, to / SPAN)[to % SPAN] = p;
+            }
+        }
+        cluster.sync();                  // every pair has arrived, every count been read
+        if (!last)
+#pragma unroll
+            for (int i = 0; i < IPT; ++i) {
+                const uint2 p = s_pair[warp * (32 * IPT) + i * 32 + lane];
+                key[i] = p.x, pos[i] = (int32_t)p.y;
+            }
+    }
+}
+
 // ------------------------------------------------------------------ sums of runs
-// The sorted positions are cut into pieces of 32.  A warp sums one piece of 32 * E columns:
-// its rows are loaded SUM_UNROLL at a time, a run of equal ids that lies in the piece is written at once, and
-// what belongs to a run that crosses the piece's bounds is left in `part`: row 2b for the run that comes
-// into piece b from before, row 2b + 1 for one that starts in b and goes on.  k_embed_join
-// adds those in order.  So the work is even whatever the ids: a hot id of 6000 rows is 190 pieces.
-// Bound by memory: each row is read once, each result written once, and `part` is at most
-// 1/8 (fp32 rows) or 1/4 (16-bit rows) of the rows' bytes again, for runs that cross only.
-constexpr int PIECE = 32, SUM_UNROLL = 8, SUM_WARPS = 8;
+// A run of equal ids is cut into pieces of 32 positions from its start.  The sorted positions are cut into windows of 32, or of 8
+// where those would be too few to fill the SMs, and a warp sums the pieces that start in its window (31 positions more
+// than a window at most), 32 * E columns of them: rows are
+// loaded SUM_UNROLL at a time, a run that is one piece is written at once, and a piece of a longer run
+// is left in `part`: of the pieces that start at positions 32 w to 32 w + 31, row 2w + 1 for the first piece of a long run, row 2w
+// for a later piece (there cannot be two of one kind).  k_embed_join adds a long run's
+// pieces.  So the work is even whatever the ids: a hot id of 6000 rows is 188 pieces.
+// Bound by memory: each row is read once, each result written once, and `part` is written and read for runs
+// over 32 only, 1/8 (fp32 rows) or 1/4 (16-bit rows) of those runs' bytes in all.
+constexpr int PIECE = 32, SUM_WARPS = 8;
 
 template <typename O, int E, bool ACC>
 __device__ __forceinline__ void write_sum(O *at, const float (&sum)[E], const Pack<O, E> &old, float scale)
@@ -203,15 +349,17 @@ __device__ __forceinline__ void zero_rows(const uint32_t *__restrict__ key, int6
                                           O *__restrict__ dtable, int64_t stride, int dim)
 {
     const int lane = threadIdx.x & 31;
-    const int64_t v = v0 + lane;
-    int64_t lo = keys_below(key, n, (uint32_t)v0), hi = keys_below(key, n, (uint32_t)min64(vocab, v0 + 32));
-    const int64_t end = hi;
-    while (lo < hi) {                    // each lane its own id, between the two
-        const int64_t mid = (lo + hi) >> 1;
-        if (key[mid] < (uint32_t)v) lo = mid + 1;
-        else hi = mid;
+    const uint32_t first = (uint32_t)v0, end = (uint32_t)min64(vocab, v0 + 32);
+    unsigned present = 0;
+    for (int64_t at = keys_below(key, n, first); at < n;) {
+        const uint32_t k = at + lane < n ? key[at + lane] : 0xffffffffu;
+        present |= __reduce_or_sync(FULL, k < end ? 1u << (k - first) : 0u);
+        const uint32_t last = __shfl_sync(FULL, k, 31);
+        if (last >= end) break;
+        // a run that fills the lanes is passed over by a search
+        at = __shfl_sync(FULL, k, 0) == last ? keys_below(key, n, last + 1) : at + 32;
     }
-    unsigned absent = __ballot_sync(FULL, v < vocab && !(lo < end && key[lo] == (uint32_t)v));
+    unsigned absent = ~present & (end - first == 32 ? FULL : (1u << (end - first)) - 1);
     Pack<O, E> zero;
 #pragma unroll
     for (int e = 0; e < E; ++e) zero.e[e] = from_float<O>(0.0f);
@@ -226,103 +374,154 @@ template <typename T, typename O, int E, bool ACC>
 __global__ __launch_bounds__(SUM_WARPS * 32) void k_embed_sum(const uint32_t *__restrict__ key,
                                                               const int32_t *__restrict__ pos, int64_t n, int64_t vocab,
                                                               const T *__restrict__ dout, int64_t stride, int dim,
-                                                              int tiles, int64_t sum_blocks, float scale,
+                                                              int tiles, int log_window, int64_t sum_blocks,
+                                                              int64_t zero_groups, float scale,
                                                               O *__restrict__ dtable, int64_t out_stride,
-                                                              float *__restrict__ part)
+                                                              float *__restrict__ part, int *__restrict__ long_runs,
+                                                              int *__restrict__ run_list)
 {
-    const int lane = threadIdx.x & 31;
-    if (blockIdx.x >= sum_blocks) {      // without ACC: the rows of ids that do not occur
-        const int64_t group = (blockIdx.x - sum_blocks) * SUM_WARPS + (threadIdx.x >> 5);
-        if (group * 32 < vocab) zero_rows<O, E>(key, n, vocab, group * 32, dtable, out_stride, dim);
+    constexpr int SUM_UNROLL = ACC ? 4 : 8;          // rows under way, with the rows they are added to
+    const int lane = threadIdx.x & 31, size = 1 << log_window;
+    // without ACC some of the blocks, spread among the others, write zeros in the rows of ids that do not occur
+    const uint64_t zero_blocks = gridDim.x - sum_blocks, zeros_before = blockIdx.x * zero_blocks / gridDim.x;
+    if (!ACC && (blockIdx.x + 1) * zero_blocks / gridDim.x != zeros_before) {
+        const int64_t group = zeros_before * SUM_WARPS + (threadIdx.x >> 5);
+        if (group < zero_groups) zero_rows<O, E>(key, n, vocab, group * 32, dtable, out_stride, dim);
         return;
     }
-    const int64_t w = (int64_t)blockIdx.x * SUM_WARPS + (threadIdx.x >> 5);
-    const int64_t piece = w / tiles;
-    const int64_t p0 = piece * PIECE;
+    const int64_t w = (blockIdx.x - zeros_before) * SUM_WARPS + (threadIdx.x >> 5);
+    const int64_t window = w / tiles, p0 = window << log_window;
     if (p0 >= n) return;
-    const int col = (int)(w - piece * tiles) * 32 * E + lane * E;
+    const int tile = (int)(w - window * tiles), col = tile * 32 * E + lane * E;
     const bool on = col < dim;
-    const int count = (int)min64(PIECE, n - p0);
-    const uint32_t k = lane < count ? key[p0 + lane] : 0xffffffffu;
-    const int32_t p = lane < count ? pos[p0 + lane] : 0;
-    const uint32_t before = p0 > 0 ? key[p0 - 1] : 0xffffffffu, after = p0 + count < n ? key[p0 + count] : 0xffffffffu;
-    const uint32_t left = __shfl_up_sync(FULL, k, 1);
-    // positions that start a run; positions that end one within the piece or at its end
-    const unsigned heads = __ballot_sync(FULL, lane < count && k != (lane == 0 ? before : left));
-    const unsigned ends = (heads >> 1) | (1u << (count - 1));
-    const uint32_t last = __shfl_sync(FULL, k, count - 1);
-    const bool goes_on = last == after;
-    int seen = count;                    // positions in front of the ids left out
-    {
-        const unsigned out = __ballot_sync(FULL, lane < count && k >= (uint32_t)vocab);
-        if (out) seen = __ffs(out) - 1;
+    // keys and rows of the window and behind it, 64 positions in all
+    uint32_t k[2];
+    int32_t row[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const int64_t i = p0 + h * 32 + lane;
+        k[h] = i < n ? key[i] : 0xffffffffu;
+        row[h] = i < n ? pos[i] : 0;
     }
+    const uint32_t before = p0 > 0 ? key[p0 - 1] : 0xffffffffu;
+    const uint32_t left0 = __shfl_up_sync(FULL, k[0], 1), left1 = __shfl_up_sync(FULL, k[1], 1);
+    const uint32_t end0 = __shfl_sync(FULL, k[0], 31), first = __shfl_sync(FULL, k[0], 0);
+    // positions (of 64) where a run starts; those behind the last id that counts make one of their own
+    const uint64_t heads = (uint64_t)__ballot_sync(FULL, k[1] != (lane == 0 ? end0 : left1)) << 32 |
+                           __ballot_sync(FULL, k[0] != (lane == 0 ? before : left0));
+    const uint64_t counts = (uint64_t)__ballot_sync(FULL, k[1] < (uint32_t)vocab) << 32 | __ballot_sync(FULL, k[0] < (uint32_t)vocab);
+    const int limit = __popcll(counts);  // sorted: the ids that count come first
+    if (limit == 0) return;
+    // pieces that start in the window: at its heads, and one of the run that comes in
+    uint32_t starts = (uint32_t)heads & (uint32_t)counts & (0xffffffffu >> (32 - size));
+    int later = -1;                      // where a later piece of a run starts
+    if (!(heads & 1)) {
+        const int64_t origin = keys_below(key, n, first);
+        const int q = (int)(-(p0 - origin) & (PIECE - 1));
+        if (q < size && (heads & ((2ull << q) - 1)) == 0 && q < limit) later = q, starts |= 1u << q;
+    }
+    if (starts == 0) return;
+    const int s0 = __ffs(starts) - 1, last = 31 - __clz(starts);
+    const uint64_t behind = heads >> last >> 1;
+    const int run_end = behind ? last + __ffsll((long long)behind) : 64;
+    const int end = min(min(last + PIECE, run_end), limit);
     float sum[E];
 #pragma unroll
     for (int e = 0; e < E; ++e) sum[e] = 0.0f;
-    bool inside = heads & 1;             // the current run starts in this piece
-    for (int i0 = 0; i0 < seen; i0 += SUM_UNROLL) {
+    int from = s0;                       // start of the current piece
+    const int safe = on ? col : 0;       // lanes past the columns load what they do not use
+    auto id_at = [&](int i) {
+        const uint32_t a = __shfl_sync(FULL, k[0], i & 31), b = __shfl_sync(FULL, k[1], i & 31);
+        return i < 32 ? a : b;
+    };
+    for (int i0 = s0; i0 < end; i0 += SUM_UNROLL) {
         Pack<T, E> x[SUM_UNROLL];
         Pack<O, E> old[ACC ? SUM_UNROLL : 1];
-        uint32_t id[SUM_UNROLL];
 #pragma unroll
         for (int u = 0; u < SUM_UNROLL; ++u) {
-            const int i = i0 + u;
-            id[u] = __shfl_sync(FULL, k, i & 31);
-            const int32_t row = __shfl_sync(FULL, p, i & 31);
-            if (i < seen && on) {
-                x[u] = load_pack<T, E>(dout + row * stride + col);
-                if (ACC && (ends >> i & 1)) old[u] = load_pack<O, E>(dtable + (int64_t)id[u] * out_stride + col);
-            }
+            const int i = min(i0 + u, end - 1);
+            const int32_t ra = __shfl_sync(FULL, row[0], i & 31), rb = __shfl_sync(FULL, row[1], i & 31);
+            x[u] = load_pack<T, E>(dout + (i < 32 ? ra : rb) * stride + safe);
+            if (ACC) old[u] = load_pack<O, E>(dtable + (int64_t)id_at(i) * out_stride + safe);
         }
 #pragma unroll
         for (int u = 0; u < SUM_UNROLL; ++u) {
             const int i = i0 + u;
-            if (i >= seen) break;
-            if (i > 0 && (heads >> i & 1)) {
-#pragma unroll
-                for (int e = 0; e < E; ++e) sum[e] = 0.0f;
-                inside = true;
-            }
+            if (i >= end) break;
 #pragma unroll
             for (int e = 0; e < E; ++e) sum[e] = __fadd_rn(sum[e], to_float(x[u].e[e]));
-            if ((ends >> i & 1) && on) {
-                const bool crosses = !inside || (i == count - 1 && goes_on);
-                if (crosses) {
-                    Pack<float, E> y;
+            if (i + 1 == end || (heads >> (i + 1) & 1)) {
+                // longer than a piece: the same id stands 32 positions behind the start, or it is a later piece
+                const bool first_of_long = from != later && i + 1 == from + PIECE && p0 + from + PIECE < n &&
+                                           (i + 1 < 64 ? !(heads >> (i + 1) & 1) : false);
+                const uint32_t id = id_at(i);
+                if (from == later || first_of_long) {
+                    if (on) {
+                        float *at = part + (2 * ((p0 + from) / PIECE) + (first_of_long ? 1 : 0)) * dim + col;
 #pragma unroll
-                    for (int e = 0; e < E; ++e) y.e[e] = sum[e];
-                    float *at = part + (2 * piece + (inside ? 1 : 0)) * dim + col;
-#pragma unroll
-                    for (int e = 0; e < E; ++e) at[e] = y.e[e];
-                } else {
-                    write_sum<O, E, ACC>(dtable + (int64_t)id[u] * out_stride + col, sum, old[ACC ? u : 0], scale);
+                        for (int e = 0; e < E; ++e) at[e] = sum[e];
+                    }
+                    if (first_of_long && tile == 0 && lane == 0) run_list[atomicAdd(long_runs, 1)] = (int)(p0 + from);
+                } else if (on) {
+                    write_sum<O, E, ACC>(dtable + (int64_t)id * out_stride + col, sum, old[ACC ? u : 0], scale);
                 }
+#pragma unroll
+                for (int e = 0; e < E; ++e) sum[e] = 0.0f;
+                from = i + 1;
             }
         }
     }
 }
 
-// runs that cross pieces: the block of the piece in which one starts adds its parts, in order
+// Runs over 32 positions: blocks take (run, 128 columns) in turn; a warp holds four columns a lane of every
+// 8th piece, four loads under way; the warps' sums are added in order.  The order of a run's sum depends on its length alone.
+constexpr int JOIN_COLS = 128, JOIN_WARPS = 8;
+
 template <typename O, bool ACC>
-__global__ __launch_bounds__(256) void k_embed_join(const uint32_t *__restrict__ key, int64_t n, int64_t vocab, int dim,
-                                                    int tiles, float scale, O *__restrict__ dtable, int64_t out_stride,
-                                                    const float *__restrict__ part)
+__global__ __launch_bounds__(JOIN_WARPS * 32) void k_embed_join(const uint32_t *__restrict__ key, int64_t n, int dim, int tiles,
+                                                                float scale, O *__restrict__ dtable, int64_t out_stride,
+                                                                const float *__restrict__ part,
+                                                                const int *__restrict__ long_runs,
+                                                                const int *__restrict__ run_list)
 {
-    const int64_t piece = blockIdx.x / tiles;
-    const int col = (int)(blockIdx.x - piece * tiles) * 256 + threadIdx.x;
-    const int64_t next = (piece + 1) * PIECE;
-    const uint32_t v = key[next - 1];
-    // starts here and goes on
-    if (v >= (uint32_t)vocab || key[next] != v || (piece > 0 && key[piece * PIECE] == v && key[piece * PIECE - 1] == v)) return;
-    if (col >= dim) return;
-    float sum[1] = {part[(2 * piece + 1) * dim + col]};
-    for (int64_t b = piece + 1; b * PIECE < n && key[b * PIECE] == v; ++b)
-        sum[0] = __fadd_rn(sum[0], part[2 * b * dim + col]);
-    O *at = dtable + (int64_t)v * out_stride + col;
-    Pack<O, 1> old;
-    if (ACC) old.e[0] = *at;
-    write_sum<O, 1, ACC>(at, sum, old, scale);
+    __shared__ float s_sum[JOIN_WARPS][JOIN_COLS];
+    const int set = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int64_t items = (int64_t)*long_runs * tiles;
+    for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
+        const int64_t start = run_list[item / tiles], window = start / PIECE;
+        const int base = (int)(item % tiles) * JOIN_COLS, col0 = base + lane * 4;
+        const uint32_t v = key[start];
+        const int pieces = (int)((keys_below(key, n, v + 1) - start + PIECE - 1) / PIECE);
+        float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+        for (int b0 = set; b0 < pieces; b0 += 4 * JOIN_WARPS) {
+            float x[4][4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const int b = b0 + u * JOIN_WARPS;
+                const float *at = part + (2 * (window + b) + (b == 0 ? 1 : 0)) * dim + col0;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) x[u][e] = b < pieces && col0 + e < dim ? at[e] : 0.0f;
+            }
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+                if (b0 + u * JOIN_WARPS < pieces)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) sum[e] = __fadd_rn(sum[e], x[u][e]);
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s_sum[set][lane * 4 + e] = sum[e];
+        __syncthreads();
+        const int col = base + (int)threadIdx.x;
+        if (threadIdx.x < JOIN_COLS && col < dim) {
+            float total[1] = {0.0f};
+            for (int i = 0; i < min(JOIN_WARPS, pieces); ++i) total[0] = __fadd_rn(total[0], s_sum[i][threadIdx.x]);
+            O *at = dtable + (int64_t)v * out_stride + col;
+            Pack<O, 1> old;
+            if (ACC) old.e[0] = *at;
+            write_sum<O, 1, ACC>(at, total, old, scale);
+        }
+        __syncthreads();
+    }
 }
 
 }  // namespace
@@ -357,7 +556,7 @@ void pdb_tokens_free(pdb_tokens *t)
     if (t->ev_use) cudaEventSynchronize(t->ev_use);
     cudaStream_t s = own_stream();
     for (void *p : {(void *)t->status, (void *)t->key, (void *)t->skey, (void *)t->tkey, (void *)t->spos,
-                    (void *)t->tpos, (void *)t->part})
+                    (void *)t->tpos, (void *)t->part, (void *)t->run_list})
         release(p, s);
     if (t->ev_use) cudaEventDestroy(t->ev_use);
     delete t;
@@ -379,12 +578,13 @@ int pdb_tokens_create(int64_t max_tokens, int64_t max_dim, pdb_tokens **out, voi
     t->max_tokens = max_tokens;
     t->max_dim = max_dim;
     int rc = cudaEventCreateWithFlags(&t->ev_use, cudaEventDisableTiming) == cudaSuccess ? PDB_OK : PDB_ECUDA;
-    rc = rc ? rc : alloc((void **)&t->status, 2 * sizeof(int), s);
+    rc = rc ? rc : alloc((void **)&t->status, 3 * sizeof(int), s);
     for (uint32_t **p : {&t->key, &t->skey, &t->tkey, (uint32_t **)&t->spos, (uint32_t **)&t->tpos})
         rc = rc ? rc : alloc((void **)p, sizeof(uint32_t) * max_tokens, s);
-    // two rows of columns in fp32 for each piece of 32 ids
+    // two rows of columns in fp32 for each window of 32 ids
     rc = rc ? rc : alloc((void **)&t->part, sizeof(float) * 2 * ((max_tokens + PIECE - 1) / PIECE) * max_dim, s);
-    rc = rc ? rc : fill_words(t->status, 0u, 2 * sizeof(int), s);
+    rc = rc ? rc : alloc((void **)&t->run_list, sizeof(int) * (max_tokens / (PIECE + 1) + 1), s);
+    rc = rc ? rc : fill_words(t->status, 0u, 3 * sizeof(int), s);
     if (rc != PDB_OK) {
         cudaGetLastError();
         cudaStreamSynchronize(s);
@@ -459,11 +659,25 @@ int pdb_embed_grad(pdb_tokens *t, const pdb_ids *ids, const pdb_mat *dout, float
     const bool nothing = dim == 0 || vocab == 0;            // the ids are looked at all the same
     if (n > 0 && n <= RANK_MAX) {
         const size_t smem = sizeof(uint32_t) * ((n + 4 * RANK_SLICES - 1) / (4 * RANK_SLICES) * (4 * RANK_SLICES));
-        k_embed_rank<<<(unsigned)((n + RANK_IDS - 1) / RANK_IDS), RANK_THREADS, smem, s>>>(ids_of(ids), (int)n, vocab, pad,
-                                                                                          t->skey, t->spos, t->status);
+        k_embed_rank<<<(unsigned)((n + RANK_IDS - 1) / RANK_IDS), RANK_THREADS, smem, s>>>(
+            ids_of(ids), (int)n, vocab, pad, t->skey, t->spos, t->status + 2, t->status);
         note_launch();
+    } else if (n > 0 && n <= SORT_MAX) {
+        // blocks of 1024 to 8192 pairs, as many of a cluster as it takes
+        const int b = bits_for(vocab), passes = (b + SORT_BITS - 1) / SORT_BITS, bits = std::max(5, (b + passes - 1) / passes);
+        const auto sort = [&](auto i) {
+            constexpr int IPT = decltype(i)::value;
+            int blocks = 1;
+            while (blocks * SORT_THREADS * IPT < n) blocks *= 2;
+            Shape shape = {};
+            shape.blocks = blocks, shape.threads = SORT_THREADS, shape.clusters = 1, shape.smem = sort_smem(IPT);
+            return launch_rows(k_embed_sort<IPT>, shape, s, ids_of(ids), (int)n, vocab, pad, passes, bits, t->skey, t->spos,
+                               t->status + 2, t->status);
+        };
+        constexpr int UNIT = SORT_THREADS * SORT_CLUSTER;
+        rc = n <= 2 * UNIT ? sort(Num<2>()) : n <= 4 * UNIT ? sort(Num<4>()) : n <= 8 * UNIT ? sort(Num<8>()) : sort(Num<16>());
     } else if (n > 0) {
-        k_embed_keys<<<(unsigned)((n + 255) / 256), 256, 0, s>>>(ids_of(ids), n, vocab, pad, t->key, t->status);
+        k_embed_keys<<<(unsigned)((n + 255) / 256), 256, 0, s>>>(ids_of(ids), n, vocab, pad, t->key, t->status + 2, t->status);
         note_launch();
         if (!nothing)
             rc = radix_sort(t->key, nullptr, t->skey, t->spos, t->tkey, t->tpos, n, bits_for(vocab), t->status + 1, s);
@@ -474,22 +688,28 @@ int pdb_embed_grad(pdb_tokens *t, const pdb_ids *ids, const pdb_mat *dout, float
         using T = std::remove_pointer_t<decltype(a)>;
         using O = std::remove_pointer_t<decltype(b)>;
         constexpr int E = decltype(e)::value;
-        const int64_t pieces = (n + PIECE - 1) / PIECE;
+        // windows of 8 below 16 warps an SM (8191 x 320: 512 warps otherwise)
         const int tiles = (dim + 32 * E - 1) / (32 * E);
-        const int64_t sum_blocks = (pieces * tiles + SUM_WARPS - 1) / SUM_WARPS;
-        const int64_t zero_blocks = accumulate ? 0 : ((vocab + 31) / 32 + SUM_WARPS - 1) / SUM_WARPS;
-        if (sum_blocks + zero_blocks > 0) {
+        const int log_window = (n + PIECE - 1) / PIECE * tiles < (int64_t)t->sms * 16 ? 3 : 5;
+        const int64_t windows = (n + (1 << log_window) - 1) >> log_window;
+        const int64_t sum_blocks = (windows * tiles + SUM_WARPS - 1) / SUM_WARPS;
+        const int64_t zero_groups = accumulate ? 0 : (vocab + 31) / 32;
+        const int64_t blocks = sum_blocks + (zero_groups + SUM_WARPS - 1) / SUM_WARPS;
+        if (blocks > 0) {
             const auto kernel = accumulate ? k_embed_sum<T, O, E, true> : k_embed_sum<T, O, E, false>;
-            kernel<<<(unsigned)(sum_blocks + zero_blocks), SUM_WARPS * 32, 0, s>>>(
-                t->skey, t->spos, n, vocab, (const T *)dout->data, stride_of(dout), dim, tiles, sum_blocks, scale,
-                (O *)dtable->data, stride_of(dtable), t->part);
+            kernel<<<(unsigned)blocks, SUM_WARPS * 32, 0, s>>>(t->skey, t->spos, n, vocab, (const T *)dout->data,
+                                                               stride_of(dout), dim, tiles, log_window, sum_blocks, zero_groups,
+                                                               scale,
+                                                               (O *)dtable->data, stride_of(dtable), t->part, t->status + 2,
+                                                               t->run_list);
             note_launch();
         }
-        if (pieces > 1) {
+        if (n > PIECE) {                 // else no run is longer than a piece
             const auto kernel = accumulate ? k_embed_join<O, true> : k_embed_join<O, false>;
-            const int tiles = (dim + 255) / 256;
-            kernel<<<(unsigned)((pieces - 1) * tiles), 256, 0, s>>>(t->skey, n, vocab, dim, tiles, scale,
-                                                                    (O *)dtable->data, stride_of(dtable), t->part);
+            const int tiles = (dim + JOIN_COLS - 1) / JOIN_COLS;
+            const int64_t most = n / (PIECE + 1) * tiles;
+            kernel<<<(unsigned)std::max<int64_t>(1, std::min<int64_t>(most, t->sms * 8)), JOIN_WARPS * 32, 0, s>>>(
+                t->skey, n, dim, tiles, scale, (O *)dtable->data, stride_of(dtable), t->part, t->status + 2, t->run_list);
             note_launch();
         }
     };
@@ -497,7 +717,7 @@ int pdb_embed_grad(pdb_tokens *t, const pdb_ids *ids, const pdb_mat *dout, float
         with_type(dtable->type, [&](auto *b) {
             constexpr int E = 16 / sizeof(*a);
             if (fits(dout, E) && fits(dtable, E)) run(a, b, Num<E>());
-            else if (fits(dout, 2) && fits(dtable, 2)) run(a, b, Num<2>());
+            else if (fits(dout, E / 2) && fits(dtable, E / 2)) run(a, b, Num<E / 2>());
             else run(a, b, Num<1>());
         });
     });

@@ -10,11 +10,12 @@
 struct pdb_tokens {
     int device, sms;
     int64_t max_tokens, max_dim;
-    int *status;               // device: [0] first error recorded by a kernel; [1] always 0 (the sort's
-                               // kernels return at once when their status word is set)
+    int *status;               // device: [0] first error recorded by a kernel; [1] always 0 (the radix
+                               // sort's kernels return at once when their status word is set); [2] long runs (embed.cu)
     uint32_t *key, *skey, *tkey;   // [max_tokens] ids as sort keys, sorted, scratch
     int32_t *spos, *tpos;      // [max_tokens] positions in sorted order, scratch
-    float *part;               // pieces of runs that cross pieces (embed.cu)
+    float *part;               // pieces of long runs (embed.cu)
+    int *run_list;             // where they start
     cudaEvent_t ev_use;        // recorded after the last work any call enqueued on the handle
 };
 
