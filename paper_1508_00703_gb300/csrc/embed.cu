@@ -113,9 +113,9 @@ __global__ __launch_bounds__(256) void k_embed(const T *__restrict__ table, int6
 
 // ------------------------------------------------------------------ sorted ids
 // an id as a sort key; those left out (pad, out of range) sort last
-__device__ __forceinline__ uint32_t embed_key(Ids ids, int64_t i, int64_t vocab, int64_t pad, int *status)
+__device__ __forceinline__ uint32_t embed_key(Ids ids, int2 raw, int64_t vocab, int64_t pad, int *status)
 {
-    const int64_t v = load_id(ids, i);
+    const int64_t v = id_of(ids, raw);
     const bool there = v != pad && v >= 0 && v < vocab;
     if (!there && v != pad) set_status(status, PDB_ERANGE);
     return there ? (uint32_t)v : (uint32_t)vocab;
@@ -127,7 +127,7 @@ __global__ void k_embed_keys(Ids ids, int64_t n, int64_t vocab, int64_t pad, uin
 {
     const int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
     if (i == 0) *long_runs = 0;          // for k_embed_sum
-    if (i < n) key[i] = embed_key(ids, i, vocab, pad, status);
+    if (i < n) key[i] = embed_key(ids, fetch_id(ids, i), vocab, pad, status);
 }
 
 // Up to RANK_MAX ids: each id's place is the number of smaller ids and of equal ones before it,
@@ -143,8 +143,18 @@ __global__ __launch_bounds__(RANK_THREADS) void k_embed_rank(Ids ids, int n, int
     __shared__ int count[RANK_IDS];
     if (blockIdx.x == 0 && threadIdx.x == 0) *long_runs = 0;      // for k_embed_sum
     const int padded = (n + 4 * RANK_SLICES - 1) / (4 * RANK_SLICES) * (4 * RANK_SLICES);
-    for (int i = threadIdx.x; i < padded; i += RANK_THREADS)
-        s_key[i] = i < n ? embed_key(ids, i, vocab, pad, status) : 0xffffffffu;   // the fill counts for nobody
+    constexpr int EACH = RANK_MAX / RANK_THREADS;
+    int2 raw[EACH];
+#pragma unroll
+    for (int j = 0; j < EACH; ++j) {
+        const int i = j * RANK_THREADS + threadIdx.x;
+        raw[j] = i < n ? fetch_id(ids, i) : int2{0, 0};
+    }
+#pragma unroll
+    for (int j = 0; j < EACH; ++j) {
+        const int i = j * RANK_THREADS + threadIdx.x;
+        if (i < padded) s_key[i] = i < n ? embed_key(ids, raw[j], vocab, pad, status) : 0xffffffffu;   // the fill counts for nobody
+    }
     if (threadIdx.x < RANK_IDS) count[threadIdx.x] = 0;
     __syncthreads();
     const int mine = blockIdx.x * RANK_IDS + threadIdx.x % RANK_IDS, slice = threadIdx.x / RANK_IDS;
@@ -207,11 +217,15 @@ __global__ __launch_bounds__(SORT_THREADS) void k_embed_sort(Ids ids, int n, int
     if (rank == 0 && tid == 0) *long_runs = 0;              // for k_embed_sum
     uint32_t key[IPT];
     int32_t pos[IPT];
+    int2 raw[IPT];
 #pragma unroll
     for (int i = 0; i < IPT; ++i) {
         pos[i] = rank * SPAN + warp * (32 * IPT) + i * 32 + lane;
-        key[i] = pos[i] < n ? embed_key(ids, pos[i], vocab, pad, status) : 0xffffffffu;      // the fill sorts behind all
+        raw[i] = pos[i] < n ? fetch_id(ids, pos[i]) : int2{0, 0};
     }
+#pragma unroll
+    for (int i = 0; i < IPT; ++i)
+        key[i] = pos[i] < n ? embed_key(ids, raw[i], vocab, pad, status) : 0xffffffffu;      // the fill sorts behind all
     for (int pass = 0; pass < passes; ++pass) {
         const int shift = pass * bits;
         uint16_t *count = s_warp + warp * radix;
@@ -371,14 +385,14 @@ __device__ __forceinline__ void zero_rows(const uint32_t *__restrict__ key, int6
 }
 
 template <typename T, typename O, int E, bool ACC>
-__global__ __launch_bounds__(SUM_WARPS * 32) void k_embed_sum(const uint32_t *__restrict__ key,
+__global__ __launch_bounds__(SUM_WARPS * 32, ACC ? 2 : 4) void k_embed_sum(const uint32_t *__restrict__ key,
                                                               const int32_t *__restrict__ pos, int64_t n, int64_t vocab,
                                                               const T *__restrict__ dout, int64_t stride, int dim,
                                                               int tiles, int log_window, int64_t sum_blocks,
                                                               int64_t zero_groups, float scale,
                                                               O *__restrict__ dtable, int64_t out_stride,
                                                               float *__restrict__ part, int *__restrict__ long_runs,
-                                                              int *__restrict__ run_list)
+                                                              int4 *__restrict__ run_list)
 {
     constexpr int SUM_UNROLL = ACC ? 4 : 8;          // rows under way, with the rows they are added to
     const int lane = threadIdx.x & 31, size = 1 << log_window;
@@ -461,7 +475,12 @@ __global__ __launch_bounds__(SUM_WARPS * 32) void k_embed_sum(const uint32_t *__
 #pragma unroll
                         for (int e = 0; e < E; ++e) at[e] = sum[e];
                     }
-                    if (first_of_long && tile == 0 && lane == 0) run_list[atomicAdd(long_runs, 1)] = (int)(p0 + from);
+                    if (first_of_long && tile == 0) {
+                        const int64_t length = keys_below(key, n, id + 1) - (p0 + from);
+                        if (lane == 0)
+                            run_list[atomicAdd(long_runs, 1)] =
+                                make_int4((int)(p0 + from), (int)((length + PIECE - 1) / PIECE), (int)id, 0);
+                    }
                 } else if (on) {
                     write_sum<O, E, ACC>(dtable + (int64_t)id * out_stride + col, sum, old[ACC ? u : 0], scale);
                 }
@@ -477,36 +496,35 @@ __global__ __launch_bounds__(SUM_WARPS * 32) void k_embed_sum(const uint32_t *__
 // 8th piece, four loads under way; the warps' sums are added in order.  The order of a run's sum depends on its length alone.
 constexpr int JOIN_COLS = 128, JOIN_WARPS = 8;
 
-template <typename O, bool ACC>
-__global__ __launch_bounds__(JOIN_WARPS * 32) void k_embed_join(const uint32_t *__restrict__ key, int64_t n, int dim, int tiles,
-                                                                float scale, O *__restrict__ dtable, int64_t out_stride,
-                                                                const float *__restrict__ part,
+// JE: columns that one load brings (4, or 1 where the columns are no multiple of 4)
+template <typename O, int JE, bool ACC>
+__global__ __launch_bounds__(JOIN_WARPS * 32) void k_embed_join(int dim, int tiles, float scale, O *__restrict__ dtable,
+                                                                int64_t out_stride, const float *__restrict__ part,
                                                                 const int *__restrict__ long_runs,
-                                                                const int *__restrict__ run_list)
+                                                                const int4 *__restrict__ run_list)
 {
     __shared__ float s_sum[JOIN_WARPS][JOIN_COLS];
     const int set = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int64_t items = (int64_t)*long_runs * tiles;
     for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
-        const int64_t start = run_list[item / tiles], window = start / PIECE;
-        const int base = (int)(item % tiles) * JOIN_COLS, col0 = base + lane * 4;
-        const uint32_t v = key[start];
-        const int pieces = (int)((keys_below(key, n, v + 1) - start + PIECE - 1) / PIECE);
+        const int4 run = run_list[item / tiles];            // start, pieces, id
+        const int64_t window = run.x / PIECE;
+        const int pieces = run.y, base = (int)(item % tiles) * JOIN_COLS, col0 = base + lane * 4;
         float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
         for (int b0 = set; b0 < pieces; b0 += 4 * JOIN_WARPS) {
-            float x[4][4];
+            Pack<float, JE> x[4][4 / JE];
 #pragma unroll
             for (int u = 0; u < 4; ++u) {
-                const int b = b0 + u * JOIN_WARPS;
-                const float *at = part + (2 * (window + b) + (b == 0 ? 1 : 0)) * dim + col0;
+                const int b = min(b0 + u * JOIN_WARPS, pieces - 1);
+                const float *at = part + (2 * (window + b) + (b == 0 ? 1 : 0)) * dim;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) x[u][e] = b < pieces && col0 + e < dim ? at[e] : 0.0f;
+                for (int e = 0; e < 4; e += JE) x[u][e / JE] = load_pack<float, JE>(at + min(col0 + e, dim - JE));
             }
 #pragma unroll
             for (int u = 0; u < 4; ++u)
                 if (b0 + u * JOIN_WARPS < pieces)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) sum[e] = __fadd_rn(sum[e], x[u][e]);
+                    for (int e = 0; e < 4; ++e) sum[e] = __fadd_rn(sum[e], x[u][e / JE].e[e % JE]);
         }
 #pragma unroll
         for (int e = 0; e < 4; ++e) s_sum[set][lane * 4 + e] = sum[e];
@@ -515,7 +533,7 @@ __global__ __launch_bounds__(JOIN_WARPS * 32) void k_embed_join(const uint32_t *
         if (threadIdx.x < JOIN_COLS && col < dim) {
             float total[1] = {0.0f};
             for (int i = 0; i < min(JOIN_WARPS, pieces); ++i) total[0] = __fadd_rn(total[0], s_sum[i][threadIdx.x]);
-            O *at = dtable + (int64_t)v * out_stride + col;
+            O *at = dtable + (int64_t)run.z * out_stride + col;
             Pack<O, 1> old;
             if (ACC) old.e[0] = *at;
             write_sum<O, 1, ACC>(at, total, old, scale);
@@ -583,7 +601,7 @@ int pdb_tokens_create(int64_t max_tokens, int64_t max_dim, pdb_tokens **out, voi
         rc = rc ? rc : alloc((void **)p, sizeof(uint32_t) * max_tokens, s);
     // two rows of columns in fp32 for each window of 32 ids
     rc = rc ? rc : alloc((void **)&t->part, sizeof(float) * 2 * ((max_tokens + PIECE - 1) / PIECE) * max_dim, s);
-    rc = rc ? rc : alloc((void **)&t->run_list, sizeof(int) * (max_tokens / (PIECE + 1) + 1), s);
+    rc = rc ? rc : alloc((void **)&t->run_list, sizeof(int4) * (max_tokens / (PIECE + 1) + 1), s);
     rc = rc ? rc : fill_words(t->status, 0u, 3 * sizeof(int), s);
     if (rc != PDB_OK) {
         cudaGetLastError();
@@ -705,11 +723,13 @@ int pdb_embed_grad(pdb_tokens *t, const pdb_ids *ids, const pdb_mat *dout, float
             note_launch();
         }
         if (n > PIECE) {                 // else no run is longer than a piece
-            const auto kernel = accumulate ? k_embed_join<O, true> : k_embed_join<O, false>;
+            const bool four = dim % 4 == 0;
+            const auto kernel = accumulate ? (four ? k_embed_join<O, 4, true> : k_embed_join<O, 1, true>)
+                                           : (four ? k_embed_join<O, 4, false> : k_embed_join<O, 1, false>);
             const int tiles = (dim + JOIN_COLS - 1) / JOIN_COLS;
             const int64_t most = n / (PIECE + 1) * tiles;
             kernel<<<(unsigned)std::max<int64_t>(1, std::min<int64_t>(most, t->sms * 8)), JOIN_WARPS * 32, 0, s>>>(
-                t->skey, n, dim, tiles, scale, (O *)dtable->data, stride_of(dtable), t->part, t->status + 2, t->run_list);
+                dim, tiles, scale, (O *)dtable->data, stride_of(dtable), t->part, t->status + 2, t->run_list);
             note_launch();
         }
     };

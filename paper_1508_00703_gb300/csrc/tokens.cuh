@@ -15,7 +15,7 @@ struct pdb_tokens {
     uint32_t *key, *skey, *tkey;   // [max_tokens] ids as sort keys, sorted, scratch
     int32_t *spos, *tpos;      // [max_tokens] positions in sorted order, scratch
     float *part;               // pieces of long runs (embed.cu)
-    int *run_list;             // where they start
+    int4 *run_list;            // where they start, their pieces, their id
     cudaEvent_t ev_use;        // recorded after the last work any call enqueued on the handle
 };
 
@@ -102,9 +102,10 @@ __device__ __forceinline__ int64_t load_id(Ids ids, int64_t i, int k = 0)
 __device__ __forceinline__ int2 fetch_id(Ids ids, int64_t i, int k = 0)
 {
     const int64_t at = i * ids.stride + k;
+    // (volatile: several of them are issued before the first is used)
     int2 raw = {0, 0};
-    if (ids.wide) raw = __ldg((const int2 *)ids.data + at);
-    else raw.x = __ldg((const int *)ids.data + at);
+    if (ids.wide) asm volatile("ld.global.nc.v2.b32 {%0, %1}, [%2];" : "=r"(raw.x), "=r"(raw.y) : "l"((const int2 *)ids.data + at));
+    else asm volatile("ld.global.nc.b32 %0, [%1];" : "=r"(raw.x) : "l"((const int *)ids.data + at));
     return raw;
 }
 __device__ __forceinline__ int64_t id_of(Ids ids, int2 raw)
