@@ -501,16 +501,18 @@ class Tokens:
             self.handle = None
 
 
-_types = None
+class _Types(dict):
+    """Matrix types and id widths by torch dtype, filled when torch is first needed (this module does not import it)."""
+
+    def __missing__(self, dtype):
+        if not self:
+            import torch
+            self.update({torch.float32: PDB_TYPE_FLOAT, torch.bfloat16: PDB_TYPE_BFLOAT, torch.float16: PDB_TYPE_HALF,
+                         torch.int32: "int32", torch.int64: "int64"})
+        return self.get(dtype)
 
 
-def _type_of(dtype):
-    global _types
-    if _types is None:
-        import torch
-        _types = {torch.float32: PDB_TYPE_FLOAT, torch.bfloat16: PDB_TYPE_BFLOAT, torch.float16: PDB_TYPE_HALF,
-                  torch.int32: "int32", torch.int64: "int64"}
-    return _types.get(dtype)
+_types = _Types()
 
 
 def _refuse(what, why):
@@ -519,47 +521,47 @@ def _refuse(what, why):
 
 def _mat(t, tok, what):
     """A pdb_mat of a 2-D device tensor whose rows are contiguous."""
-    kind = _type_of(t.dtype)
+    kind = _types[t.dtype]
     if kind.__class__ is not int:
         _refuse(what, f"float32, bfloat16 or float16 wanted, got {t.dtype}")
-    if t.dim() != 2 or t.get_device() != tok.device:
+    stride = t.stride()
+    if len(stride) != 2 or t.get_device() != tok.device:
         _refuse(what, f"a matrix on cuda:{tok.device} wanted, got {tuple(t.shape)} on {t.device}")
     rows, cols = t.shape
-    stride, step = t.stride()
-    if (step != 1 and cols > 1) or (stride < cols and rows > 1):
-        _refuse(what, f"rows of neighbouring elements that do not overlap wanted, got strides {t.stride()}")
-    return pdb_mat(t.data_ptr(), rows, cols, stride, kind)
+    if (stride[1] != 1 and cols > 1) or (stride[0] < cols and rows > 1):
+        _refuse(what, f"rows of neighbouring elements that do not overlap wanted, got strides {stride}")
+    return pdb_mat(t.data_ptr(), rows, cols, stride[0], kind)
 
 
 def _ids(t, tok, what):
     """A pdb_ids of a vector of ids."""
-    kind = _type_of(t.dtype)
+    kind = _types[t.dtype]
     if kind.__class__ is not str:
         _refuse(what, f"int32 or int64 wanted, got {t.dtype}")
-    if t.dim() != 1 or t.get_device() != tok.device:
+    stride = t.stride()
+    if len(stride) != 1 or t.get_device() != tok.device:
         _refuse(what, f"a vector on cuda:{tok.device} wanted, got {tuple(t.shape)} on {t.device}")
-    return pdb_ids(t.data_ptr(), t.shape[0], t.stride(0), kind == "int64")
+    return pdb_ids(t.data_ptr(), t.numel(), stride[0], kind == "int64")
 
 
 def _rows_of_ids(t, tok, what):
     """A pdb_ids of a matrix of ids whose rows are contiguous."""
-    kind = _type_of(t.dtype)
+    kind = _types[t.dtype]
     if kind.__class__ is not str:
         _refuse(what, f"int32 or int64 wanted, got {t.dtype}")
-    if t.dim() != 2 or t.get_device() != tok.device:
+    stride = t.stride()
+    if len(stride) != 2 or t.get_device() != tok.device:
         _refuse(what, f"a matrix on cuda:{tok.device} wanted, got {tuple(t.shape)} on {t.device}")
-    rows, cols = t.shape
-    stride, step = t.stride()
-    if step != 1 and cols > 1:
-        _refuse(what, f"rows of neighbouring elements wanted, got strides {t.stride()}")
-    return pdb_ids(t.data_ptr(), rows * cols, stride, kind == "int64")
+    if stride[1] != 1 and t.shape[1] > 1:
+        _refuse(what, f"rows of neighbouring elements wanted, got strides {stride}")
+    return pdb_ids(t.data_ptr(), t.numel(), stride[0], kind == "int64")
 
 
 def _vec(t, n, tok, what, kind=PDB_TYPE_FLOAT):
     """The pointer of n contiguous device words (None stays None)."""
     if t is None:
         return None
-    if _type_of(t.dtype) != kind or t.get_device() != tok.device or t.numel() != n or not t.is_contiguous():
+    if _types[t.dtype] != kind or t.get_device() != tok.device or t.numel() != n or not t.is_contiguous():
         _refuse(what, f"{n} contiguous {'int32' if kind == 'int32' else 'float32'} on cuda:{tok.device} wanted, "
                       f"got {t.dtype} {tuple(t.shape)} on {t.device}")
     return t.data_ptr()

@@ -324,6 +324,7 @@ __global__ __launch_bounds__(THREADS, 1024 / THREADS) void k_distill_loss(const 
                                                                           int bit_bytes, int *status)
 {
     constexpr int E = Vec<T>::E;
+    after_previous();
     extern __shared__ __align__(16) unsigned char smem[];
     __shared__ float part[192], part2[64], own[4];
     __shared__ int twice;
@@ -412,6 +413,7 @@ __global__ __launch_bounds__(THREADS, 512 / THREADS) void k_distill_grad(const T
 {
     constexpr int E = Vec<T>::E;
     constexpr uint32_t NEG_INF = Vec<T>::NEG_INF;
+    after_previous();
     using In = Stream<T, THREADS>;
     extern __shared__ __align__(16) unsigned char smem[];
     __shared__ float part[2][192], part2[2][64];

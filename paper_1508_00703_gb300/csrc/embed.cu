@@ -84,6 +84,7 @@ __global__ __launch_bounds__(256) void k_embed(const T *__restrict__ table, int6
                                                int64_t n, int dim, int pieces, float scale, int64_t pad,
                                                O *__restrict__ out, int64_t out_stride, int *status)
 {
+    after_previous();
     const int lane = threadIdx.x & 31;
     const int64_t total = n * pieces, step = (int64_t)gridDim.x * 8;
     for (int64_t w = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); w < total; w += step) {
@@ -125,6 +126,7 @@ __device__ __forceinline__ uint32_t embed_key(Ids ids, int2 raw, int64_t vocab, 
 __global__ void k_embed_keys(Ids ids, int64_t n, int64_t vocab, int64_t pad, uint32_t *__restrict__ key, int *long_runs,
                              int *status)
 {
+    after_previous();
     const int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
     if (i == 0) *long_runs = 0;          // for k_embed_sum
     if (i < n) key[i] = embed_key(ids, fetch_id(ids, i), vocab, pad, status);
@@ -139,6 +141,8 @@ __global__ __launch_bounds__(RANK_THREADS) void k_embed_rank(Ids ids, int n, int
                                                              uint32_t *__restrict__ skey, int32_t *__restrict__ spos,
                                                              int *long_runs, int *status)
 {
+    after_previous();
+    let_next_start();
     extern __shared__ __align__(16) uint32_t s_key[];       // n, rounded up to 4 * RANK_SLICES
     __shared__ int count[RANK_IDS];
     if (blockIdx.x == 0 && threadIdx.x == 0) *long_runs = 0;      // for k_embed_sum
@@ -201,6 +205,8 @@ __global__ __launch_bounds__(SORT_THREADS) void k_embed_sort(Ids ids, int n, int
                                                              uint32_t *__restrict__ skey, int32_t *__restrict__ spos,
                                                              int *long_runs, int *status)
 {
+    after_previous();
+    let_next_start();
     constexpr int SPAN = SORT_THREADS * IPT;
     extern __shared__ __align__(16) uint2 s_pair[];         // [SPAN] this block's part of the order: key, position
     uint2 *s_local = s_pair + SPAN;                         // [SPAN] its pairs by digit
@@ -394,6 +400,7 @@ __global__ __launch_bounds__(SUM_WARPS * 32, ACC ? 2 : 4) void k_embed_sum(const
                                                               float *__restrict__ part, int *__restrict__ long_runs,
                                                               int4 *__restrict__ run_list)
 {
+    after_previous();
     constexpr int SUM_UNROLL = ACC ? 4 : 8;          // rows under way, with the rows they are added to
     const int lane = threadIdx.x & 31, size = 1 << log_window;
     // without ACC some of the blocks, spread among the others, write zeros in the rows of ids that do not occur
@@ -503,6 +510,7 @@ __global__ __launch_bounds__(JOIN_WARPS * 32) void k_embed_join(int dim, int til
                                                                 const int *__restrict__ long_runs,
                                                                 const int4 *__restrict__ run_list)
 {
+    after_previous();
     __shared__ float s_sum[JOIN_WARPS][JOIN_COLS];
     const int set = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int64_t items = (int64_t)*long_runs * tiles;
@@ -641,10 +649,8 @@ int pdb_embed(pdb_tokens *t, const pdb_mat *table, const pdb_ids *ids, float sca
         constexpr int E = decltype(e)::value;
         const int dim = (int)out->cols, pieces = (dim + LOOKUP_UNROLL * 32 * E - 1) / (LOOKUP_UNROLL * 32 * E);
         const int64_t blocks = std::min<int64_t>((out->rows * pieces + 7) / 8, (int64_t)1 << 24);
-        k_embed<T, O, E><<<(unsigned)blocks, 256, 0, s>>>((const T *)table->data, table->rows, stride_of(table),
-                                                          ids_of(ids), out->rows, dim, pieces, scale, pad,
-                                                          (O *)out->data, stride_of(out), t->status);
-        note_launch();
+        rc = launch(k_embed<T, O, E>, blocks, 256, 0, 1, s, (const T *)table->data, table->rows, stride_of(table),
+                    ids_of(ids), out->rows, dim, pieces, scale, pad, (O *)out->data, stride_of(out), t->status);
     };
     with_type(table->type, [&](auto *a) {
         with_type(out->type, [&](auto *b) {
@@ -655,7 +661,7 @@ int pdb_embed(pdb_tokens *t, const pdb_mat *table, const pdb_ids *ids, float sca
             else run(a, b, Num<1>());
         });
     });
-    return cudaPeekAtLastError() == cudaSuccess ? PDB_OK : PDB_ECUDA;
+    return rc;
 }
 
 int pdb_embed_grad(pdb_tokens *t, const pdb_ids *ids, const pdb_mat *dout, float scale, int64_t pad, int accumulate,
@@ -677,9 +683,8 @@ int pdb_embed_grad(pdb_tokens *t, const pdb_ids *ids, const pdb_mat *dout, float
     const bool nothing = dim == 0 || vocab == 0;            // the ids are looked at all the same
     if (n > 0 && n <= RANK_MAX) {
         const size_t smem = sizeof(uint32_t) * ((n + 4 * RANK_SLICES - 1) / (4 * RANK_SLICES) * (4 * RANK_SLICES));
-        k_embed_rank<<<(unsigned)((n + RANK_IDS - 1) / RANK_IDS), RANK_THREADS, smem, s>>>(
-            ids_of(ids), (int)n, vocab, pad, t->skey, t->spos, t->status + 2, t->status);
-        note_launch();
+        rc = launch(k_embed_rank, (n + RANK_IDS - 1) / RANK_IDS, RANK_THREADS, smem, 1, s, ids_of(ids), (int)n, vocab, pad,
+                    t->skey, t->spos, t->status + 2, t->status);
     } else if (n > 0 && n <= SORT_MAX) {
         // blocks of 1024 to 8192 pairs, as many of a cluster as it takes
         const int b = bits_for(vocab), passes = (b + SORT_BITS - 1) / SORT_BITS, bits = std::max(5, (b + passes - 1) / passes);
@@ -695,13 +700,11 @@ int pdb_embed_grad(pdb_tokens *t, const pdb_ids *ids, const pdb_mat *dout, float
         constexpr int UNIT = SORT_THREADS * SORT_CLUSTER;
         rc = n <= 2 * UNIT ? sort(Num<2>()) : n <= 4 * UNIT ? sort(Num<4>()) : n <= 8 * UNIT ? sort(Num<8>()) : sort(Num<16>());
     } else if (n > 0) {
-        k_embed_keys<<<(unsigned)((n + 255) / 256), 256, 0, s>>>(ids_of(ids), n, vocab, pad, t->key, t->status + 2, t->status);
-        note_launch();
-        if (!nothing)
+        rc = launch(k_embed_keys, (n + 255) / 256, 256, 0, 1, s, ids_of(ids), n, vocab, pad, t->key, t->status + 2, t->status);
+        if (!nothing && rc == PDB_OK)
             rc = radix_sort(t->key, nullptr, t->skey, t->spos, t->tkey, t->tpos, n, bits_for(vocab), t->status + 1, s);
     }
-    if (rc != PDB_OK) return rc;
-    if (nothing) return cudaPeekAtLastError() == cudaSuccess ? PDB_OK : PDB_ECUDA;
+    if (rc != PDB_OK || nothing) return rc;
     const auto run = [&](auto *a, auto *b, auto e) {
         using T = std::remove_pointer_t<decltype(a)>;
         using O = std::remove_pointer_t<decltype(b)>;
@@ -715,22 +718,18 @@ int pdb_embed_grad(pdb_tokens *t, const pdb_ids *ids, const pdb_mat *dout, float
         const int64_t blocks = sum_blocks + (zero_groups + SUM_WARPS - 1) / SUM_WARPS;
         if (blocks > 0) {
             const auto kernel = accumulate ? k_embed_sum<T, O, E, true> : k_embed_sum<T, O, E, false>;
-            kernel<<<(unsigned)blocks, SUM_WARPS * 32, 0, s>>>(t->skey, t->spos, n, vocab, (const T *)dout->data,
-                                                               stride_of(dout), dim, tiles, log_window, sum_blocks, zero_groups,
-                                                               scale,
-                                                               (O *)dtable->data, stride_of(dtable), t->part, t->status + 2,
-                                                               t->run_list);
-            note_launch();
+            rc = launch(kernel, blocks, SUM_WARPS * 32, 0, 1, s, t->skey, t->spos, n, vocab, (const T *)dout->data,
+                        stride_of(dout), dim, tiles, log_window, sum_blocks, zero_groups, scale, (O *)dtable->data,
+                        stride_of(dtable), t->part, t->status + 2, t->run_list);
         }
-        if (n > PIECE) {                 // else no run is longer than a piece
+        if (n > PIECE && rc == PDB_OK) {                 // else no run is longer than a piece
             const bool four = dim % 4 == 0;
             const auto kernel = accumulate ? (four ? k_embed_join<O, 4, true> : k_embed_join<O, 1, true>)
                                            : (four ? k_embed_join<O, 4, false> : k_embed_join<O, 1, false>);
             const int tiles = (dim + JOIN_COLS - 1) / JOIN_COLS;
             const int64_t most = n / (PIECE + 1) * tiles;
-            kernel<<<(unsigned)std::max<int64_t>(1, std::min<int64_t>(most, t->sms * 8)), JOIN_WARPS * 32, 0, s>>>(
-                dim, tiles, scale, (O *)dtable->data, stride_of(dtable), t->part, t->status + 2, t->run_list);
-            note_launch();
+            rc = launch(kernel, std::max<int64_t>(1, std::min<int64_t>(most, t->sms * 8)), JOIN_WARPS * 32, 0, 1, s, dim, tiles,
+                        scale, (O *)dtable->data, stride_of(dtable), t->part, t->status + 2, t->run_list);
         }
     };
     with_type(dout->type, [&](auto *a) {
@@ -741,7 +740,7 @@ int pdb_embed_grad(pdb_tokens *t, const pdb_ids *ids, const pdb_mat *dout, float
             else run(a, b, Num<1>());
         });
     });
-    return cudaPeekAtLastError() == cudaSuccess ? PDB_OK : PDB_ECUDA;
+    return rc;
 }
 
 }  // extern "C"

@@ -214,6 +214,7 @@ template <typename T, bool ENT, bool TOP, int THREADS>
 __global__ __launch_bounds__(THREADS, 1024 / THREADS) void k_logprobs(const T *__restrict__ logits, int cols, int64_t stride, Ids ids,
                                                       float scale, int64_t ignore, int k, LogprobsOut out, int *status)
 {
+    after_previous();
     __shared__ float part[96];
     __shared__ float own[4];            // this block's m, s, w, number of alternatives
     __shared__ __align__(16) unsigned char top_raw[TOP ? sizeof(TopShared) : 16];
@@ -314,6 +315,7 @@ __global__ __launch_bounds__(THREADS) void k_logprobs_grad(const T *logits, int 
                                                            const float *__restrict__ dentropy, T *dlogits,
                                                            int64_t out_stride, int *status)
 {
+    after_previous();
     constexpr int E = Vec<T>::E;
     const int64_t r = blockIdx.x / (unsigned)pieces;
     const int piece = (int)(blockIdx.x - r * pieces);
@@ -440,11 +442,9 @@ int pdb_logprobs_grad(pdb_tokens *t, const pdb_mat *logits, const pdb_ids *ids, 
         while (pieces < 64 && logits->rows * pieces < t->sms && nv / (2 * pieces) >= threads) pieces *= 2;
         return with_threads(threads, [&](auto n) {
             constexpr int N = decltype(n)::value;
-            k_logprobs_grad<T, N><<<(unsigned)(logits->rows * pieces), N, 0, s>>>(
-                (const T *)logits->data, (int)logits->cols, stride_of(logits), pieces, ids_of(ids, dlogp), scale, ignore,
-                lse, entropy, dlogp, dentropy, (T *)dlogits->data, stride_of(dlogits), t->status);
-            note_launch();
-            return cudaPeekAtLastError() == cudaSuccess ? PDB_OK : PDB_ECUDA;
+            return launch(k_logprobs_grad<T, N>, logits->rows * pieces, N, 0, 1, s, (const T *)logits->data,
+                          (int)logits->cols, stride_of(logits), pieces, ids_of(ids, dlogp), scale, ignore, lse, entropy,
+                          dlogp, dentropy, (T *)dlogits->data, stride_of(dlogits), t->status);
         });
     });
 }

@@ -578,20 +578,7 @@ template <typename... P, typename... A>
 inline int launch_rows(void (*kernel)(P...), const Shape &shape, cudaStream_t s, A... args)
 {
     if (!allow_smem((const void *)kernel)) return PDB_ECUDA;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(shape.clusters * shape.blocks));
-    cfg.blockDim = dim3((unsigned)shape.threads);
-    cfg.dynamicSmemBytes = shape.smem;
-    cfg.stream = s;
-    cudaLaunchAttribute at[1];
-    at[0].id = cudaLaunchAttributeClusterDimension;
-    at[0].val.clusterDim = {(unsigned)shape.blocks, 1, 1};
-    cfg.attrs = at;
-    cfg.numAttrs = 1;
-    const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, P(args)...);
-    note_launch();
-    if (e != cudaSuccess) cudaGetLastError();
-    return e == cudaSuccess ? PDB_OK : PDB_ECUDA;
+    return launch(kernel, shape.clusters * shape.blocks, shape.threads, shape.smem, shape.blocks, s, args...);
 }
 
 }  // namespace pdb

@@ -126,6 +126,36 @@ __device__ __forceinline__ __nv_bfloat16 from_float<__nv_bfloat16>(float v) { re
 template <>
 __device__ __forceinline__ __half from_float<__half>(float v) { return __float2half_rn(v); }
 
+// Every kernel of the token operators starts with this: it is launched while the kernel before it in the stream still
+// runs (launch below), and waits here until that one has ended and its writes are visible.  Takes the launch's latency out
+// of a sequence of calls (500 x 256 gradient, three kernels: 16.4 us a call -> 10.7).
+__device__ __forceinline__ void after_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+// lets the next kernel of the stream take its place on the SMs now (it waits for this one's end all the same)
+__device__ __forceinline__ void let_next_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+
+// `cluster` > 1: blocks of a cluster (grid is a multiple)
+template <typename... P, typename... A>
+inline int launch(void (*kernel)(P...), int64_t grid, int threads, size_t smem, int cluster, cudaStream_t s, A... args)
+{
+    cudaLaunchAttribute at[2];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    at[1].id = cudaLaunchAttributeClusterDimension;
+    at[1].val.clusterDim.x = (unsigned)cluster;
+    at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)grid);
+    cfg.blockDim = dim3((unsigned)threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = s;
+    cfg.attrs = at;
+    cfg.numAttrs = cluster > 1 ? 2 : 1;
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, P(args)...);
+    note_launch();
+    if (e != cudaSuccess) cudaGetLastError();
+    return e == cudaSuccess ? PDB_OK : PDB_ECUDA;
+}
+
 // a number as a type
 template <int N>
 struct Num {
