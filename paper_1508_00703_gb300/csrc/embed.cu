@@ -273,12 +273,18 @@ __global__ __launch_bounds__(SORT_THREADS) void k_embed_sort(Ids ids, int n, int
         cluster.sync();                  // every block has its pairs in registers and its counts in place
         // pairs of the two digits in all blocks, and in those before this one
         uint32_t all[2] = {0, 0}, before[2] = {0, 0};
-        if (2 * tid < radix)
-            for (int b = 0; b < blocks; ++b) {
-                const uint2 h = *reinterpret_cast<const uint2 *>(cluster.map_shared_rank(s_hist, b) + 2 * tid);
-                all[0] += h.x, all[1] += h.y;
-                if (b < rank) before[0] += h.x, before[1] += h.y;
-            }
+        if (2 * tid < radix) {
+            uint2 h[SORT_CLUSTER];
+#pragma unroll
+            for (int b = 0; b < SORT_CLUSTER; ++b)
+                h[b] = *reinterpret_cast<const uint2 *>(cluster.map_shared_rank(s_hist, min(b, blocks - 1)) + 2 * tid);
+#pragma unroll
+            for (int b = 0; b < SORT_CLUSTER; ++b)
+                if (b < blocks) {
+                    all[0] += h[b].x, all[1] += h[b].y;
+                    if (b < rank) before[0] += h[b].x, before[1] += h[b].y;
+                }
+        }
         uint32_t x = all[0] + all[1], y = own[0] + own[1];
 #pragma unroll
         for (int off = 1; off < 32; off <<= 1) {
@@ -401,7 +407,7 @@ __global__ __launch_bounds__(SUM_WARPS * 32, ACC ? 2 : 4) void k_embed_sum(const
                                                               int4 *__restrict__ run_list)
 {
     after_previous();
-    constexpr int SUM_UNROLL = ACC ? 4 : 8;          // rows under way, with the rows they are added to
+    constexpr int SUM_UNROLL = 8;        // rows under way, with those that finished sums are added to
     const int lane = threadIdx.x & 31, size = 1 << log_window;
     // without ACC some of the blocks, spread among the others, write zeros in the rows of ids that do not occur
     const uint64_t zero_blocks = gridDim.x - sum_blocks, zeros_before = blockIdx.x * zero_blocks / gridDim.x;
@@ -463,8 +469,14 @@ __global__ __launch_bounds__(SUM_WARPS * 32, ACC ? 2 : 4) void k_embed_sum(const
             const int i = min(i0 + u, end - 1);
             const int32_t ra = __shfl_sync(FULL, row[0], i & 31), rb = __shfl_sync(FULL, row[1], i & 31);
             x[u] = load_pack<T, E>(dout + (i < 32 ? ra : rb) * stride + safe);
-            if (ACC) old[u] = load_pack<O, E>(dtable + (int64_t)id_at(i) * out_stride + safe);
         }
+        if (ACC)
+#pragma unroll
+            for (int u = 0; u < SUM_UNROLL; ++u) {
+                const int i = i0 + u;
+                if (i + 1 == end || (i < end && (heads >> (i + 1) & 1)))
+                    old[u] = load_pack<O, E>(dtable + (int64_t)id_at(i) * out_stride + safe);
+            }
 #pragma unroll
         for (int u = 0; u < SUM_UNROLL; ++u) {
             const int i = i0 + u;
@@ -580,10 +592,7 @@ void pdb_tokens_free(pdb_tokens *t)
 {
     if (!t) return;
     if (t->ev_use) cudaEventSynchronize(t->ev_use);
-    cudaStream_t s = own_stream();
-    for (void *p : {(void *)t->status, (void *)t->key, (void *)t->skey, (void *)t->tkey, (void *)t->spos,
-                    (void *)t->tpos, (void *)t->part, (void *)t->run_list})
-        release(p, s);
+    release(t->arrays, own_stream());
     if (t->ev_use) cudaEventDestroy(t->ev_use);
     delete t;
 }
@@ -604,12 +613,16 @@ int pdb_tokens_create(int64_t max_tokens, int64_t max_dim, pdb_tokens **out, voi
     t->max_tokens = max_tokens;
     t->max_dim = max_dim;
     int rc = cudaEventCreateWithFlags(&t->ev_use, cudaEventDisableTiming) == cudaSuccess ? PDB_OK : PDB_ECUDA;
-    rc = rc ? rc : alloc((void **)&t->status, 3 * sizeof(int), s);
-    for (uint32_t **p : {&t->key, &t->skey, &t->tkey, (uint32_t **)&t->spos, (uint32_t **)&t->tpos})
-        rc = rc ? rc : alloc((void **)p, sizeof(uint32_t) * max_tokens, s);
-    // two rows of columns in fp32 for each window of 32 ids
-    rc = rc ? rc : alloc((void **)&t->part, sizeof(float) * 2 * ((max_tokens + PIECE - 1) / PIECE) * max_dim, s);
-    rc = rc ? rc : alloc((void **)&t->run_list, sizeof(int4) * (max_tokens / (PIECE + 1) + 1), s);
+    const size_t words = sizeof(uint32_t) * max_tokens, radix = max_tokens > SORT_MAX ? words : 0;   // of the radix sort only
+    rc = rc ? rc : alloc_block(t->arrays, {{(void **)&t->status, 3 * sizeof(int)},
+                                           {(void **)&t->key, radix},
+                                           {(void **)&t->tkey, radix},
+                                           {(void **)&t->tpos, radix},
+                                           {(void **)&t->skey, words},
+                                           {(void **)&t->spos, words},
+                                           // two rows of columns in fp32 for each 32 positions
+                                           {(void **)&t->part, sizeof(float) * 2 * ((max_tokens + PIECE - 1) / PIECE) * max_dim},
+                                           {(void **)&t->run_list, sizeof(int4) * (max_tokens / (PIECE + 1))}}, s);
     rc = rc ? rc : fill_words(t->status, 0u, 3 * sizeof(int), s);
     if (rc != PDB_OK) {
         cudaGetLastError();

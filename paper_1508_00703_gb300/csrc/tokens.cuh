@@ -12,10 +12,13 @@ struct pdb_tokens {
     int64_t max_tokens, max_dim;
     int *status;               // device: [0] first error recorded by a kernel; [1] always 0 (the radix
                                // sort's kernels return at once when their status word is set); [2] long runs (embed.cu)
-    uint32_t *key, *skey, *tkey;   // [max_tokens] ids as sort keys, sorted, scratch
-    int32_t *spos, *tpos;      // [max_tokens] positions in sorted order, scratch
+    uint32_t *skey;            // [max_tokens] ids as sort keys in sorted order
+    int32_t *spos;             // [max_tokens] their positions
+    uint32_t *key, *tkey;      // [max_tokens] beyond what a cluster sorts: keys, and the radix sort's scratch
+    int32_t *tpos;
     float *part;               // pieces of long runs (embed.cu)
     int4 *run_list;            // where they start, their pieces, their id
+    pdb::Block arrays;         // holds the device arrays
     cudaEvent_t ev_use;        // recorded after the last work any call enqueued on the handle
 };
 
