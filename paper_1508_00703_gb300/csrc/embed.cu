@@ -200,10 +200,18 @@ inline size_t sort_smem(int ipt)
            sizeof(uint16_t) * SORT_WARPS * (1 << SORT_BITS);
 }
 
+// Rows of the gradient that the SMs which have nothing to sort fill with zeros meanwhile (k_embed_sum then writes those that
+// do occur): `row` pieces of 16 bytes each, `stride` bytes apart.
+struct Fill {
+    char *to;
+    int64_t rows, stride;
+    int row;
+};
+
 template <int IPT>
 __global__ __launch_bounds__(SORT_THREADS) void k_embed_sort(Ids ids, int n, int64_t vocab, int64_t pad, int passes, int bits,
                                                              uint32_t *__restrict__ skey, int32_t *__restrict__ spos,
-                                                             int *long_runs, int *status)
+                                                             int *long_runs, Fill fill, int *status)
 {
     after_previous();
     let_next_start();
@@ -218,6 +226,13 @@ __global__ __launch_bounds__(SORT_THREADS) void k_embed_sort(Ids ids, int n, int
     cg::cluster_group cluster = cg::this_cluster();
     const int blocks = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    if (blockIdx.x >= blocks) {          // another cluster's block: a warp a row
+        for (int64_t r = (int64_t)(blockIdx.x - blocks) * SORT_WARPS + warp; r < fill.rows;
+             r += (int64_t)(gridDim.x - blocks) * SORT_WARPS)
+            for (int j = lane; j < fill.row; j += 32)
+                __stcs(reinterpret_cast<uint4 *>(fill.to + r * fill.stride) + j, uint4{0, 0, 0, 0});
+        return;
+    }
     const unsigned lt = lanemask_lt();
     const int radix = 1 << bits;
     if (rank == 0 && tid == 0) *long_runs = 0;              // for k_embed_sum
@@ -401,7 +416,7 @@ __global__ __launch_bounds__(SUM_WARPS * 32, ACC ? 2 : 4) void k_embed_sum(const
                                                               const int32_t *__restrict__ pos, int64_t n, int64_t vocab,
                                                               const T *__restrict__ dout, int64_t stride, int dim,
                                                               int tiles, int log_window, int64_t sum_blocks,
-                                                              int64_t zero_groups, float scale,
+                                                              int64_t zero_first, int64_t zero_groups, float scale,
                                                               O *__restrict__ dtable, int64_t out_stride,
                                                               float *__restrict__ part, int *__restrict__ long_runs,
                                                               int4 *__restrict__ run_list)
@@ -412,7 +427,7 @@ __global__ __launch_bounds__(SUM_WARPS * 32, ACC ? 2 : 4) void k_embed_sum(const
     // without ACC some of the blocks, spread among the others, write zeros in the rows of ids that do not occur
     const uint64_t zero_blocks = gridDim.x - sum_blocks, zeros_before = blockIdx.x * zero_blocks / gridDim.x;
     if (!ACC && (blockIdx.x + 1) * zero_blocks / gridDim.x != zeros_before) {
-        const int64_t group = zeros_before * SUM_WARPS + (threadIdx.x >> 5);
+        const int64_t group = zero_first + zeros_before * SUM_WARPS + (threadIdx.x >> 5);
         if (group < zero_groups) zero_rows<O, E>(key, n, vocab, group * 32, dtable, out_stride, dim);
         return;
     }
@@ -693,6 +708,15 @@ int pdb_embed_grad(pdb_tokens *t, const pdb_ids *ids, const pdb_mat *dout, float
     if (vocab == 0 && n == 0) return PDB_OK;
     cudaStream_t s = (cudaStream_t)stream;
     TokensUse use{t, s};
+    // What the sort leaves idle writes zeros: about as many bytes as go to memory in its time (the 20 us of 65,536 ids: 167 us
+    // -> 157 with 50,000 rows of 8 KB), none for the short sorts and rows that are not whole 16-byte pieces.
+    Fill fill = {};
+    const int64_t row_bytes = (int64_t)dim * type_bytes(dtable->type), step = stride_of(dtable) * type_bytes(dtable->type);
+    if (!accumulate && n > RANK_MAX && n <= SORT_MAX && row_bytes > 0 && row_bytes % 16 == 0 && step % 16 == 0 &&
+        (uintptr_t)dtable->data % 16 == 0) {
+        const int64_t rows = (n < 16384 ? 24 << 20 : 96 << 20) / row_bytes;
+        fill = Fill{(char *)dtable->data, std::min(rows, vocab) / 32 * 32, step, (int)(row_bytes / 16)};
+    }
     const bool nothing = dim == 0 || vocab == 0;            // the ids are looked at all the same
     if (n > 0 && n <= RANK_MAX) {
         const size_t smem = sizeof(uint32_t) * ((n + 4 * RANK_SLICES - 1) / (4 * RANK_SLICES) * (4 * RANK_SLICES));
@@ -706,9 +730,10 @@ int pdb_embed_grad(pdb_tokens *t, const pdb_ids *ids, const pdb_mat *dout, float
             int blocks = 1;
             while (blocks * SORT_THREADS * IPT < n) blocks *= 2;
             Shape shape = {};
-            shape.blocks = blocks, shape.threads = SORT_THREADS, shape.clusters = 1, shape.smem = sort_smem(IPT);
+            shape.blocks = blocks, shape.threads = SORT_THREADS, shape.smem = sort_smem(IPT);
+            shape.clusters = fill.rows > 0 ? t->sms / blocks : 1;
             return launch_rows(k_embed_sort<IPT>, shape, s, ids_of(ids), (int)n, vocab, pad, passes, bits, t->skey, t->spos,
-                               t->status + 2, t->status);
+                               t->status + 2, fill, t->status);
         };
         constexpr int UNIT = SORT_THREADS * SORT_CLUSTER;
         rc = n <= 2 * UNIT ? sort(Num<2>()) : n <= 4 * UNIT ? sort(Num<4>()) : n <= 8 * UNIT ? sort(Num<8>()) : sort(Num<16>());
@@ -727,13 +752,13 @@ int pdb_embed_grad(pdb_tokens *t, const pdb_ids *ids, const pdb_mat *dout, float
         const int log_window = (n + PIECE - 1) / PIECE * tiles < (int64_t)t->sms * 16 ? 3 : 5;
         const int64_t windows = (n + (1 << log_window) - 1) >> log_window;
         const int64_t sum_blocks = (windows * tiles + SUM_WARPS - 1) / SUM_WARPS;
-        const int64_t zero_groups = accumulate ? 0 : (vocab + 31) / 32;
-        const int64_t blocks = sum_blocks + (zero_groups + SUM_WARPS - 1) / SUM_WARPS;
+        const int64_t zero_first = fill.rows / 32, zero_groups = accumulate ? 0 : (vocab + 31) / 32;
+        const int64_t blocks = sum_blocks + (accumulate ? 0 : (zero_groups - zero_first + SUM_WARPS - 1) / SUM_WARPS);
         if (blocks > 0) {
             const auto kernel = accumulate ? k_embed_sum<T, O, E, true> : k_embed_sum<T, O, E, false>;
             rc = launch(kernel, blocks, SUM_WARPS * 32, 0, 1, s, t->skey, t->spos, n, vocab, (const T *)dout->data,
-                        stride_of(dout), dim, tiles, log_window, sum_blocks, zero_groups, scale, (O *)dtable->data,
-                        stride_of(dtable), t->part, t->status + 2, t->run_list);
+                        stride_of(dout), dim, tiles, log_window, sum_blocks, zero_first, zero_groups, scale,
+                        (O *)dtable->data, stride_of(dtable), t->part, t->status + 2, t->run_list);
         }
         if (n > PIECE && rc == PDB_OK) {                 // else no run is longer than a piece
             const bool four = dim % 4 == 0;
