@@ -432,13 +432,13 @@ int pdb_sgd_epoch_ready_noalloc(const pdb_csr *X, const float *y, const uint32_t
  *
  * Every call takes a pdb_tokens handle: the workspace of pdb_embed_grad, and
  * the status word in which the kernels record an id out of range
- * (pdb_tokens_status).  A recorded error stops no later call: a bad id gives the
+ * or an expired wait (pdb_tokens_status).  A recorded error stops no later call: a bad id gives the
  * result its declaration states.  Calls that share a handle must be ordered on
  * one stream.  Sums, softmax statistics and losses are held in fp32; a result
  * in 16 bits is rounded once.  No atomics add floating values: the same inputs
  * give the same bits.  No call allocates but pdb_tokens_create (and pdb_embed_grad above
- * 65,536 ids: scratch of the radix sort, stream-ordered from the library's pool), and all but
- * pdb_tokens_create and pdb_tokens_status can be recorded into a CUDA graph (keep the
+ * 65,536 ids: scratch of the radix sort, stream-ordered from the library's pool); all but
+ * these and pdb_tokens_status, pdb_embed_grad up to 65,536 ids included, can be recorded into a CUDA graph (keep the
  * handle until the graph's last run has finished: pdb_tokens_free does not wait for it).
  * PDB_LOG prints nothing for these calls. */
 
@@ -465,8 +465,8 @@ typedef struct {
 typedef struct pdb_tokens pdb_tokens; /* opaque, library-owned device arrays */
 
 /* Handle for calls of at most max_tokens ids (below 2^31) and, in pdb_embed_grad, rows of at
- * most max_dim elements; holds about (20 + max_dim / 4) bytes for each of
- * max_tokens.  Allocates stream-ordered on `stream`.
+ * most max_dim elements; holds about 8 + max_dim / 4 bytes for each of
+ * max_tokens (12 more above 65,536).  Allocates stream-ordered on `stream`.
  * pdb_tokens_free waits for the work enqueued on the handle, then releases it.
  * pdb_tokens_status SYNCHRONIZES `stream` and returns the first error that a
  * kernel recorded in the handle (PDB_OK when none). */
@@ -544,8 +544,8 @@ int pdb_logprobs_grad(pdb_tokens *t, const pdb_mat *logits, const pdb_ids *ids, 
  * gradient 0; a row of weight 0 has gradient 0, whatever it holds; a row of logits with
  * nothing but -inf has loss +inf and gradient 0.  A NaN in a row makes its loss and gradient NaN.
  * dlogits may be the logits' own memory (same data, stride and type); it must not overlap
- * them otherwise.  Reads the logits once from memory when the gradient is asked for
- * in this call. */
+ * them otherwise.  PDB_ETOOBIG above 1024 slots or 2^21 tokens.  Every wait of the kernel is bounded:
+ * one that runs out is recorded as PDB_ETIMEOUT and leaves the results of its rows undefined. */
 int pdb_distill(pdb_tokens *t, const pdb_mat *logits, const pdb_ids *top_ids, const pdb_mat *top_logits,
                 const float *teacher_lse, float temperature, float *loss, const float *weight, const pdb_mat *dlogits,
                 void *stream);

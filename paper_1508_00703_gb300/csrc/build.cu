@@ -894,7 +894,7 @@ const char *pdb_strerror(int code)
     switch (code) {
     case PDB_OK: return "ok";
     case PDB_EINVAL: return "invalid argument or malformed row_ptr";
-    case PDB_ERANGE: return "feature id outside [0, n_cols)";
+    case PDB_ERANGE: return "feature id outside [0, n_cols), or token id outside the vocabulary";
     case PDB_EDUP: return "feature id repeated inside one example";
     case PDB_ENOMEM: return "device allocation failed";
     case PDB_ECUDA: return "CUDA runtime error";
@@ -903,7 +903,8 @@ const char *pdb_strerror(int code)
     case PDB_ESTATE: return "handle in the wrong mode for this call";
     case PDB_ETOOBIG:
         return "problem beyond a fixed limit (allocation-free scratch: 2^20 features; CHAIN: 256 ids per example "
-               "unless the weights fit in shared memory; a feature in 2^29 positions or more)";
+               "unless the weights fit in shared memory; a feature in 2^29 positions or more; token operators: the handle's "
+               "tokens or columns, 64 alternatives, 1024 slots, 2^21 tokens in pdb_distill)";
     default: return "unknown error";
     }
 }

@@ -14,6 +14,11 @@
 // than the buffer reach tau (ties, masked rows) or a NaN hides from the maxima, a radix
 // selection over the block's share takes over: four counting passes, exact for
 // any order of the row.  The pass itself pays one maximum per thread and 64 bytes.
+//
+// Measured: 2039 x 50,001 bf16, entropy and 5 alternatives 48 us, 204 MB at 4.2 TB/s: 59% of the issue slots
+// taken (51 instructions per 8 logits, alternatives 15% on top), the rest waits at the rows' ends; 4096 x 128,000
+// bf16 without alternatives 157 us of 460 with the gradient, 6.7 TB/s; 4 x 128,000 with 20 alternatives 9.2 us, a chain of
+// latencies (two launches' worth of barriers, three reads).
 #include <algorithm>
 #include <cmath>
 

@@ -87,7 +87,7 @@ __device__ __forceinline__ void bar_expect(uint64_t *bar, unsigned bytes)
 __device__ __forceinline__ bool bar_done(uint64_t *bar, unsigned parity)
 {
     unsigned ok;
-    asm volatile("{ .reg .pred p; mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2; selp.u32 %0, 1, 0, p; }"
+    asm volatile("{ .reg .pred p; mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2; selp.u32 %0, 1, 0, p; }"
                  : "=r"(ok) : "r"(shared_addr(bar)), "r"(parity) : "memory");
     return ok != 0;
 }
