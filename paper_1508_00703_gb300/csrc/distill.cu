@@ -63,7 +63,7 @@ __device__ __forceinline__ void block_sums(float (&v)[N], float *part)
         for (int off = 16; off >= 1; off >>= 1) v[i] = __fadd_rn(v[i], __shfl_xor_sync(FULL, v[i], off));
         if ((threadIdx.x & 31) == 0) part[i * 32 + (threadIdx.x >> 5)] = v[i];
     }
-    __syncthreads();
+    team_sync<THREADS>();
 #pragma unroll
     for (int i = 0; i < N; ++i) {
         v[i] = part[i * 32 + (threadIdx.x & (W - 1))];
@@ -409,7 +409,7 @@ __global__ __launch_bounds__(THREADS, 1024 / THREADS) void k_distill_loss(const 
 // Shared memory: the slots of two rows in turn, the marks, the stream's places.
 
 template <typename T, bool BUCKET, int THREADS>
-__global__ __launch_bounds__(THREADS, 512 / THREADS) void k_distill_grad(const T *logits, int64_t rows, int cols, int64_t stride,
+__global__ __launch_bounds__(THREADS + 32, 512 / THREADS) void k_distill_grad(const T *logits, int64_t rows, int cols, int64_t stride,
                                                                          Teacher teach, float temperature, float *loss,
                                                                          const float *__restrict__ weight, T *dlogits,
                                                                          int64_t out_stride, int slots, int hold,
@@ -434,11 +434,18 @@ __global__ __launch_bounds__(THREADS, 512 / THREADS) void k_distill_grad(const T
 
     if (threadIdx.x == 0) bar_init(&joined[0], 1), bar_init(&joined[1], 1);
     In in;
-    in.start(logits, stride, rows, cols, first, step, rank, blocks,
-             reinterpret_cast<uint4 *>(reinterpret_cast<unsigned char *>(map) + map_bytes), bars, slots, hold, status);
-    for (int i = threadIdx.x; i < map_bytes / 16; i += THREADS) reinterpret_cast<uint4 *>(map)[i] = uint4{0, 0, 0, 0};
+    in.start(reinterpret_cast<uint4 *>(reinterpret_cast<unsigned char *>(map) + map_bytes), bars, slots, hold, status);
+    for (int i = threadIdx.x; i < map_bytes / 16; i += THREADS + 32) reinterpret_cast<uint4 *>(map)[i] = uint4{0, 0, 0, 0};
     if (threadIdx.x < 2) twice[threadIdx.x] = 0, edge_map[threadIdx.x] = 0;
 
+    if (blocks > 1) cluster.sync();     // every block's barriers are there
+    else __syncthreads();               // the map is clear
+    if (threadIdx.x >= THREADS) {
+        if (threadIdx.x == THREADS) in.bring_rows(logits, stride, rows, cols, first, step, rank, blocks);
+        __syncwarp();
+        if (blocks > 1) cluster.sync();
+        return;
+    }
     // a row's numbers, fetched a row ahead; its first THREADS slots two rows ahead
     RawSlot slot = {};
     auto fetch_slots = [&](int64_t r) {
@@ -489,15 +496,12 @@ __global__ __launch_bounds__(THREADS, 512 / THREADS) void k_distill_grad(const T
         }
     };
     fetch_slots(first);
-    if (blocks > 1) cluster.sync();     // every block's barriers are there
-    else __syncthreads();               // the map is clear
     if (first < rows) open_row(first, 0);
 
     int turn = 0;
     unsigned joins = 0;                 // rows joined so far
     for (int64_t r = first; r < rows; r += step, turn ^= 1) {
-        __syncthreads();                // the marks are set; the row before is written
-        in.settle();
+        team_sync<THREADS>();           // the marks are set; the row before is written
         if (threadIdx.x == 0) twice[turn ^ 1] = 0, edge_map[turn ^ 1] = 0;
         if (r != first) write_slots(r - step, turn ^ 1);
         const T *row = logits + r * stride;
@@ -607,7 +611,7 @@ __global__ __launch_bounds__(THREADS, 512 / THREADS) void k_distill_grad(const T
             in.give_back(p);
         }
     }
-    __syncthreads();
+    team_sync<THREADS>();
     if (first < rows) {
         const int64_t last = first + (rows - 1 - first) / step * step;
         write_slots(last, turn ^ 1);
@@ -653,9 +657,10 @@ extern "C" int pdb_distill(pdb_tokens *t, const pdb_mat *logits, const pdb_ids *
             });
         }
         const size_t slot_bytes = ((size_t)teach.K * SLOT_BYTES * 2 + 15) / 16 * 16;
-        const Shape shape = twice_shape(logits->rows, logits->cols, Vec<T>::E, t->sms, slot_bytes);
+        Shape shape = twice_shape(logits->rows, logits->cols, Vec<T>::E, t->sms, slot_bytes);
         return with_threads(shape.threads, [&](auto n) {
             constexpr int N = decltype(n)::value;
+            shape.threads = N + 32;     // and the warp that brings the rows
             return launch_rows(teacher_lse ? k_distill_grad<T, true, N> : k_distill_grad<T, false, N>, shape, s,
                                (const T *)logits->data, logits->rows, (int)logits->cols, stride_of(logits), teach,
                                temperature, loss, weight, (T *)dlogits->data, stride_of(dlogits), shape.slots, shape.hold,

@@ -359,6 +359,13 @@ __device__ __forceinline__ void load_vectors(uint4 (&v)[UNROLL], const uint4 *__
     }
 }
 
+// barrier of the block's first THREADS threads (a kernel may have a warp more, which brings its rows)
+template <int THREADS>
+__device__ __forceinline__ void team_sync()
+{
+    asm volatile("bar.sync 1, %0;" ::"n"(THREADS) : "memory");
+}
+
 // joins the threads' statistics over the block, on every thread, with one barrier; `part` holds 3 * 32 floats and is
 // not used again before another barrier
 template <int THREADS, bool ENT>
@@ -370,7 +377,7 @@ __device__ __forceinline__ void block_join(Stat<ENT> &a, float c, float *part)
         const int w = threadIdx.x >> 5;
         part[w] = a.m, part[32 + w] = a.s, part[64 + w] = a.w;
     }
-    __syncthreads();
+    team_sync<THREADS>();
     const int lane = threadIdx.x & (W - 1);
     a.m = part[lane], a.s = part[32 + lane], a.w = part[64 + lane];
     a.template warp_join<W>(c);
@@ -379,9 +386,9 @@ __device__ __forceinline__ void block_join(Stat<ENT> &a, float c, float *part)
 constexpr int MOST_SLOTS = 16;
 
 // One block's shares of its cluster's rows, chunk after chunk of SPAN = THREADS * UNROLL vectors, each row twice.
-// Thread 0 brings the chunks by bulk copies into `slots` places, in turn; a place is free again
-// when every warp has given it back.  A row's last `hold` chunks stay in their places after the first visit and
-// come again from there; the ones before are brought once more, after the held ones (L2 has seen them
+// A warp of its own brings the chunks by bulk copies into `slots` places, in turn; a place is free again
+// when each of the THREADS / 32 other warps has given it back.  A row's last `hold` chunks stay in their places after the first
+// visit and come again from there; the ones before are brought once more, after the held ones (L2 has seen them
 // a few microseconds ago).  Every wait has a limit, after which the status word holds PDB_ETIMEOUT and no
 // wait of the thread waits again.
 template <typename T, int THREADS>
@@ -392,17 +399,9 @@ struct Stream {
     uint64_t *full, *empty;             // a barrier for each place
     int *status;
     int slots, hold;
-    int slot;                           // the next place to take
+    int slot;                           // the next place to take or to fill
     unsigned parity;                    // its full barrier's
     bool gave_up;
-    // thread 0: what it brings next, and to where
-    const T *logits;
-    int64_t stride, rows, step, row;
-    int cols, rank, blocks;
-    int v, v_end, v_first, v_held;      // vectors: next, end of this sweep, the share's first, first held one
-    const uint4 *body;
-    int at, owed;                       // its place; places given back and not yet filled
-    unsigned free_parity;
 
     __device__ __forceinline__ void wait(uint64_t *bar, unsigned par)
     {
@@ -412,63 +411,62 @@ struct Stream {
         set_status(status, PDB_ETIMEOUT);
         gave_up = true;
     }
-    // chunks of a share that pass through, before the held ones
-    __device__ __forceinline__ int passing(int n_vec) const { return max(0, (max(n_vec, 1) + SPAN - 1) / SPAN - hold); }
-    __device__ __forceinline__ void open()
-    {
-        if (row < rows) {
-            const T *r = logits + row * stride;
-            const Share s = share_of(r, cols, rank, blocks);
-            body = reinterpret_cast<const uint4 *>(r + s.head);
-            v = v_first = s.v0, v_end = s.v1;
-            v_held = s.v0 + passing(s.v1 - s.v0) * SPAN;
-        }
-    }
-    // `bars` holds 2 * MOST_SLOTS barriers; a barrier of the block follows before the first take
-    __device__ __forceinline__ void start(const T *logits_, int64_t stride_, int64_t rows_, int cols_, int64_t first,
-                                          int64_t step_, int rank_, int blocks_, uint4 *place_, uint64_t *bars, int slots_,
-                                          int hold_, int *status_)
+    // `bars` holds 2 * MOST_SLOTS barriers; a barrier of the block follows before the first use
+    __device__ __forceinline__ void start(uint4 *place_, uint64_t *bars, int slots_, int hold_, int *status_)
     {
         place = place_, full = bars, empty = bars + MOST_SLOTS, status = status_, slots = slots_, hold = hold_;
         slot = 0, parity = 0, gave_up = false;
         if (threadIdx.x == 0) {
-            logits = logits_, stride = stride_, rows = rows_, cols = cols_, row = first, step = step_, rank = rank_;
-            blocks = blocks_, at = owed = 0, free_parity = 1;
             for (int i = 0; i < slots; ++i) {
                 bar_init(full + i, 1);
                 bar_init(empty + i, THREADS / 32);
             }
             asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-            open();
-            for (int i = 0; i < slots; ++i) bring();
         }
     }
-    // thread 0: brings the next chunk (a row without vectors has one empty chunk), if there is one
-    __device__ __forceinline__ void bring()
+    __device__ __forceinline__ void next()
     {
-        if (row >= rows) return;
-        wait(empty + at, free_parity);
-        const int n = min(SPAN, v_end - v);
-        bar_expect(full + at, n * 16);
-        if (n > 0) bulk_copy(place + at * SPAN, body + v, n * 16, full + at);
-        v += SPAN;
-        if (v >= v_end) {
-            if (v_end != v_held && v_held != v_first) {
-                v = v_first, v_end = v_held;        // the second sweep: the passing chunks once more
-            } else {
-                row += step;
-                open();
+        if (++slot == slots) slot = 0, parity ^= 1;
+    }
+    // chunks of a share that pass through, before the held ones (a row without vectors has one empty chunk)
+    __device__ __forceinline__ int passing(int n_vec) const { return max(0, (max(n_vec, 1) + SPAN - 1) / SPAN - hold); }
+    // the bringing thread, all of its work
+    __device__ __forceinline__ void bring_rows(const T *logits, int64_t stride, int64_t rows, int cols, int64_t first, int64_t step,
+                                               int rank, int blocks)
+    {
+        int brought = 0;
+        for (int64_t r = first; r < rows; r += step) {
+            const T *row = logits + r * stride;
+            const Share sh = share_of(row, cols, rank, blocks);
+            const uint4 *body = reinterpret_cast<const uint4 *>(row + sh.b0);
+            const int n_vec = sh.v1 - sh.v0;
+            int end = n_vec;
+            for (int sweep = 0; sweep < 2; ++sweep) {
+                for (int v = 0; v < end || (sweep == 0 && v == 0); v += SPAN) {
+                    wait(empty + slot, parity ^ 1);         // a place never used is free
+                    const int n = min(SPAN, end - v);
+                    bar_expect(full + slot, n * 16);
+                    if (n > 0) bulk_copy(place + slot * SPAN, body + v, n * 16, full + slot);
+                    next();
+                    ++brought;
+                }
+                end = passing(n_vec) * SPAN;                // the passing chunks once more
             }
         }
-        if (++at == slots) at = 0, free_parity ^= 1;
+        // nothing is under way when the block ends, whatever became of the other warps
+        for (int i = 0; i < min(slots, brought); ++i) {
+            if (slot == 0) slot = slots, parity ^= 1;
+            --slot;
+            wait(full + slot, parity);
+        }
     }
     // the next chunk's place, once it is there
     __device__ __forceinline__ int take()
     {
         wait(full + slot, parity);
         const int p = slot;
-        if (++slot == slots) slot = 0, parity ^= 1;
+        next();
         return p;
     }
     // this thread's vectors in place p
@@ -480,21 +478,11 @@ struct Stream {
     }
     // the place of the chunk taken n takes ago
     __device__ __forceinline__ int before(int n) const { return slot - n < 0 ? slot - n + slots : slot - n; }
-    // this warp has done with place p.  Thread 0 fills the place given back before that one, which the other warps are
-    // likely to have done with too.
+    // this warp has done with place p
     __device__ __forceinline__ void give_back(int p)
     {
         __syncwarp();
-        if ((threadIdx.x & 31) == 0) {
-            bar_arrive(empty + p);
-            if (threadIdx.x == 0 && owed++) bring(), --owed;
-        }
-        __syncwarp();
-    }
-    // fills what is left, after a barrier of the block
-    __device__ __forceinline__ void settle()
-    {
-        if (threadIdx.x == 0 && owed) bring(), owed = 0;
+        if ((threadIdx.x & 31) == 0) bar_arrive(empty + p);
     }
 };
 
