@@ -621,6 +621,33 @@ __global__ __launch_bounds__(THREADS + 32, 512 / THREADS) void k_distill_grad(co
 
 }  // namespace
 
+namespace pdb {
+
+// as the device says it: an SM more or less in one of its groups takes more than its share of the larger clusters
+int count_room(pdb_tokens *t)
+{
+    const auto kernel = k_distill_grad<__nv_bfloat16, true, 256>;
+    if (!allow_smem((const void *)kernel)) return PDB_ECUDA;
+    cudaLaunchAttribute at = {};
+    at.id = cudaLaunchAttributeClusterDimension;
+    cudaLaunchConfig_t cfg = {};
+    cfg.attrs = &at;
+    cfg.numAttrs = 1;
+    for (int i = 0; i < 3; ++i)
+        for (int log = 0; log < 4; ++log) {
+            at.val.clusterDim.x = 1u << log;
+            at.val.clusterDim.y = at.val.clusterDim.z = 1;
+            cfg.gridDim = dim3((unsigned)t->sms * 8);
+            cfg.blockDim = dim3(512 / (i == 2 ? 4 : 2) + 32);
+            cfg.dynamicSmemBytes = block_smem(1 << i);
+            if (cudaOccupancyMaxActiveClusters(&t->room[i][log], kernel, &cfg) != cudaSuccess) return PDB_ECUDA;
+            if (t->room[i][log] < 1) return PDB_ECUDA;
+        }
+    return PDB_OK;
+}
+
+}  // namespace pdb
+
 extern "C" int pdb_distill(pdb_tokens *t, const pdb_mat *logits, const pdb_ids *top_ids, const pdb_mat *top_logits,
                            const float *teacher_lse, float temperature, float *loss, const float *weight,
                            const pdb_mat *dlogits, void *stream)
@@ -657,7 +684,7 @@ extern "C" int pdb_distill(pdb_tokens *t, const pdb_mat *logits, const pdb_ids *
             });
         }
         const size_t slot_bytes = ((size_t)teach.K * SLOT_BYTES * 2 + 15) / 16 * 16;
-        Shape shape = twice_shape(logits->rows, logits->cols, Vec<T>::E, t->sms, slot_bytes);
+        Shape shape = twice_shape(logits->rows, logits->cols, Vec<T>::E, *t, slot_bytes);
         return with_threads(shape.threads, [&](auto n) {
             constexpr int N = decltype(n)::value;
             shape.threads = N + 32;     // and the warp that brings the rows

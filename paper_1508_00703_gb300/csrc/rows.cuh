@@ -496,12 +496,14 @@ struct Shape {
 };
 constexpr size_t SMEM_PER_SM = 228 << 10, STATIC_SMEM = 3072;
 
-// blocks of a cluster: while they still find room on the SMs all at once and each thread has a vector.  A row alone on one
-// SM is bound by what that SM can have under way (4 x 128,000 bf16: 8 blocks 8.9 us, one 11.7)
-inline int cluster_of(int64_t rows, int64_t nv, int threads, int64_t resident)
+// blocks of a cluster: while they still find room on the SMs all at once (`room`: clusters of so many blocks) and each
+// thread has a vector.  A row alone on one SM is bound by what that SM can have under way (4 x 128,000 bf16: 8 blocks
+// 8.9 us, one 11.7)
+template <typename F>
+inline int cluster_of(int64_t rows, int64_t nv, int threads, F room)
 {
     int blocks = 1;
-    while (blocks < MAX_CLUSTER && rows * blocks * 2 <= resident && nv / (blocks * 2) >= threads) blocks *= 2;
+    while (blocks < MAX_CLUSTER && rows <= room(blocks * 2) && nv / (blocks * 2) >= threads) blocks *= 2;
     return blocks;
 }
 
@@ -521,7 +523,7 @@ inline Shape once_shape(int64_t rows, int64_t cols, int vec, int sms, size_t ext
     const int64_t nv = cols / vec + 1;
     Shape s = {};
     s.threads = rows < sms ? (nv < 1024 ? 128 : nv < 2048 ? 256 : 512) : nv < 8192 ? 128 : 256;
-    s.blocks = cluster_of(rows, nv, s.threads, sms);
+    s.blocks = cluster_of(rows, nv, s.threads, [&](int blocks) { return sms / blocks; });
     while (map && nv / s.blocks > 65536 && s.blocks < MAX_CLUSTER) s.blocks *= 2;      // room for the marks
     if (map) set_maps(s, nv / s.blocks + 1);
     s.smem = extra + s.map_bytes;
@@ -529,27 +531,33 @@ inline Shape once_shape(int64_t rows, int64_t cols, int vec, int sms, size_t ext
     return s;
 }
 
-// Two visits per row: persistent clusters, 512 threads of an SM in blocks of 128 (rows up to 96 KB) or 256, each with its part of
-// the SM's shared memory for the stream.  Measured with gradient, us: 8000 x 32,000 bf16 210 by 128 threads, 235 by 256, 335
-// by 512; 4096 x 128,000 bf16 417 by 256 threads and shares of half a row, 469 by 256 and whole rows (their second visit comes from
-// memory: more than L2 keeps is under way), 510 by 512 threads, whose waits nothing fills.
-inline Shape twice_shape(int64_t rows, int64_t cols, int vec, int sms, size_t extra)
+// shared memory of a block where `per` of them share an SM, which keeps 1 KB for each
+constexpr size_t block_smem(int per) { return SMEM_PER_SM / per - 1024 - STATIC_SMEM; }
+
+// Two visits per row: persistent clusters, 512 threads of an SM in blocks of 128 or 256 and each block's warp that brings its
+// rows, each with its part of the SM's shared memory for the stream.  A row goes to one block of 128 up to 80 KB, to two up to 160 KB,
+// then to blocks of 256 whose shares end at 160 KB.  Measured with gradient, us, by 1 x 128, 2 x 128, 1 x 256, 2 x 256, 4 x 256:
+// 8000 x 32,000 bf16 219, 228, 226, 317, 527; 4000 x 64,000 bf16 227, 194, 199, 229, 330; 1501 x 50,001 fp32 144, 126, 124, 116, 149;
+// 4096 x 128,000 bf16 -, 452, -, 381, 464; 3000 x 90,000 fp32 -, 470, -, 397, 356.  Larger shares go to memory for their second
+// visit (more than L2 keeps is under way); smaller ones leave too little work between a row's waits.
+// No more clusters than run at once (t.room): one cluster more, and the others wait for its rows (76 clusters of 4 where 74
+// have room: 3000 x 128,000 fp32 733 us, 487 by 74).
+inline Shape twice_shape(int64_t rows, int64_t cols, int vec, const pdb_tokens &t, size_t extra)
 {
     const int64_t nv = cols / vec + 1;
     Shape s = {};
-    s.threads = nv < 6144 ? 128 : 256;
+    s.threads = nv <= 10240 ? 128 : 256;
     const int per = 512 / s.threads;
-    s.blocks = cluster_of(rows, nv, s.threads, (int64_t)sms * per);
-    while (nv / s.blocks > 13312 && s.blocks < MAX_CLUSTER) s.blocks *= 2;             // shares of up to 208 KB
+    s.blocks = cluster_of(rows, nv, s.threads, [&](int blocks) { return t.room[per / 2][__builtin_ctz(blocks)]; });
+    while (nv / s.blocks > s.threads * 40 && s.blocks < MAX_CLUSTER) s.blocks *= 2;
     set_maps(s, nv / s.blocks + 1);
-    const size_t chunk = (size_t)UNROLL * 16 * s.threads, fixed = extra + s.map_bytes;
-    const size_t most = SMEM_PER_SM / per - 1024 - STATIC_SMEM;    // an SM keeps 1 KB for each block
+    const size_t chunk = (size_t)UNROLL * 16 * s.threads, fixed = extra + s.map_bytes, most = block_smem(per);
     const int64_t chunks = std::max<int64_t>(1, (nv / s.blocks + UNROLL * s.threads) / (UNROLL * s.threads));
     const int64_t fit = fixed < most ? (int64_t)((most - fixed) / chunk) : 0;
     s.slots = (int)std::max<int64_t>(3, std::min({fit, 2 * chunks + 2, (int64_t)MOST_SLOTS}));
     s.hold = (int)std::max<int64_t>(1, std::min<int64_t>(chunks, s.slots - 2));
     s.smem = fixed + s.slots * chunk;
-    s.clusters = std::min(rows, std::max<int64_t>(1, (int64_t)sms * per / s.blocks));
+    s.clusters = std::min<int64_t>(rows, t.room[s.smem > most ? 0 : per / 2][__builtin_ctz(s.blocks)]);
     return s;
 }
 

@@ -9,6 +9,7 @@
 
 struct pdb_tokens {
     int device, sms;
+    int room[3][4];            // clusters of 1, 2, 4, 8 blocks that run at once, by 1, 2, 4 blocks an SM (distill.cu)
     int64_t max_tokens, max_dim;
     int *status;               // device: [0] first error recorded by a kernel; [1] always 0 (the radix
                                // sort's kernels return at once when their status word is set); [2] long runs (embed.cu)
@@ -39,6 +40,9 @@ struct TokensUse {
 
 // lets a kernel have all of an SM's shared memory as dynamic one; once per kernel and device
 bool allow_smem(const void *kernel);
+
+// fills t->room
+int count_room(pdb_tokens *t);
 
 inline int type_bytes(int type) { return type == PDB_TYPE_FLOAT ? 4 : 2; }
 
