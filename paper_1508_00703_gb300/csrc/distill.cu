@@ -196,6 +196,7 @@ struct Row {
     __device__ __forceinline__ bool first_of(const Slots &S, int k) const
     {
         bool is = true;
+#pragma unroll 1
         for (int i = 0; i < (repeated ? k : 0); ++i) is &= S.id[i] != S.id[k];
         return is;
     }
@@ -237,6 +238,7 @@ struct Row {
         }
         block_join<THREADS>(a, c, part);
         peak = -INFINITY, peak_z = -3.402823466e38f, odd = false;
+#pragma unroll 1
         for (int i = 0; i < THREADS / 32 && i * 32 < K; ++i) {
             peak = fmaxf(peak, part[96 + i]);
             peak_z = fmaxf(peak_z, part[128 + i]);
@@ -250,6 +252,7 @@ struct Row {
         if (threadIdx.x == 0) own[0] = a.m, own[1] = a.s, own[2] = repeated ? 1.0f : 0.0f;
         cluster.sync();
         a = Stat<false>();
+#pragma unroll 1
         for (int b = 0; b < (int)cluster.num_blocks(); ++b) {
             const float *o = cluster.map_shared_rank(own, b);
             a.join(o[0], o[1], 0.0f, c);
@@ -265,6 +268,7 @@ struct Row {
         if ((int)threadIdx.x < blocks) send_async(own + 4 * rank, bar, threadIdx.x, a.m, a.s, repeated ? 1.0f : 0.0f, 0.0f);
         in.wait(bar, parity);
         a = Stat<false>();
+#pragma unroll 1
         for (int b = 0; b < blocks; ++b) {
             a.join(own[4 * b], own[4 * b + 1], 0.0f, c);
             repeated |= own[4 * b + 2] != 0.0f;
@@ -279,6 +283,7 @@ struct Row {
         base = BUCKET ? teacher_lse : peak == -INFINITY ? 0.0f : peak;
         logt = 0.0f;
         float sums[BUCKET ? 2 : 1] = {};
+#pragma unroll 1
         for (int k = threadIdx.x; k < K; k += THREADS) {
             sums[0] = __fadd_rn(sums[0], q(S, k));
             if (BUCKET && S.id[k] >= 0 && first_of(S, k)) sums[1] = __fadd_rn(sums[1], ex2(__fmul_rn(__fsub_rn(S.z[k], m), c)));
@@ -301,6 +306,7 @@ struct Row {
         // slot by slot: the sums of q log q and q x alone are many times their difference
         const float logs = logf(s);
         float kl = 0.0f;
+#pragma unroll 1
         for (int k = threadIdx.x & 31; k < K; k += 32) {
             const float p = q(S, k), x = __fmaf_rn(__fsub_rn(S.z[k], m), inv, -logs);
             if (p != 0.0f) kl = __fmaf_rn(p, __fsub_rn(logq(S, k), x), kl);
@@ -356,12 +362,14 @@ __global__ __launch_bounds__(THREADS, 1024 / THREADS) void k_distill_loss(const 
     const float teacher_lse = BUCKET ? teach.lse[r] : 0.0f;
     if (threadIdx.x == 0) twice = 0, edge_map = 0;
     if (BUCKET) {
+#pragma unroll 1
         for (int i = threadIdx.x; i < map_bytes / 16; i += THREADS) reinterpret_cast<uint4 *>(map)[i] = uint4{0, 0, 0, 0};
         __syncthreads();
     }
     Row<BUCKET> R;
     R.peak = -INFINITY, R.peak_z = -3.402823466e38f, R.odd = false;
     uint4 around = {0, 0, 0, 0};        // of slot threadIdx.x: used when the pass is over
+#pragma unroll 1
     for (int k = threadIdx.x; k < K; k += THREADS) {
         if (k >= THREADS) slot.fetch(teach, r, k);
         const int j = slot.token(teach, cols, rank == 0, status);
@@ -384,6 +392,7 @@ __global__ __launch_bounds__(THREADS, 1024 / THREADS) void k_distill_loss(const 
     }
     if (has_edge && !(BUCKET && (edge_map >> threadIdx.x & 1))) add_element(R.a, to_float(z_edge), c);
     R.repeated = twice;
+#pragma unroll 1
     for (int k = threadIdx.x; k < K; k += THREADS) {
         const int j = S.id[k];
         if (k >= THREADS && j >= 0) around = fetch_around(row, sh, j);
@@ -407,6 +416,8 @@ __global__ __launch_bounds__(THREADS, 1024 / THREADS) void k_distill_loss(const 
 // the gradient, and after the barrier that opens the next row the slots' own elements.  The next row's slots
 // are read and marked, and its student logits fetched, before the second pass.
 // Shared memory: the slots of two rows in turn, the marks, the stream's places.
+// An SM's blocks are at different places of the kernel at any time, so its size counts: with the loops whose length is not known
+// left rolled it is 54 KB, and 8000 x 32,000 bf16 take 176 us; unrolled by the compiler's choice 97 KB and 219 us.
 
 template <typename T, bool BUCKET, int THREADS>
 __global__ __launch_bounds__(THREADS + 32, 512 / THREADS) void k_distill_grad(const T *logits, int64_t rows, int cols, int64_t stride,
@@ -435,6 +446,7 @@ __global__ __launch_bounds__(THREADS + 32, 512 / THREADS) void k_distill_grad(co
     if (threadIdx.x == 0) bar_init(&joined[0], 1), bar_init(&joined[1], 1);
     In in;
     in.start(reinterpret_cast<uint4 *>(reinterpret_cast<unsigned char *>(map) + map_bytes), bars, slots, hold, status);
+#pragma unroll 1
     for (int i = threadIdx.x; i < map_bytes / 16; i += THREADS + 32) reinterpret_cast<uint4 *>(map)[i] = uint4{0, 0, 0, 0};
     if (threadIdx.x < 2) twice[threadIdx.x] = 0, edge_map[threadIdx.x] = 0;
 
@@ -463,6 +475,7 @@ __global__ __launch_bounds__(THREADS + 32, 512 / THREADS) void k_distill_grad(co
         const Slots S(smem + turn * SLOT_BYTES * K, K);
         const Marks marks{map, map + bit_bytes / 4, &edge_map[turn]};
         peak = -INFINITY, odd = false;
+#pragma unroll 1
         for (int k = threadIdx.x; k < K; k += THREADS) {
             RawSlot here = slot;
             if (k >= THREADS) here.fetch(teach, r, k);
@@ -485,10 +498,12 @@ __global__ __launch_bounds__(THREADS + 32, 512 / THREADS) void k_distill_grad(co
     auto write_slots = [&](int64_t r, int turn) {
         const Share sh = share_of(logits + r * stride, cols, rank, blocks);
         const Slots S(smem + turn * SLOT_BYTES * K, K);
+#pragma unroll 1
         for (int k = threadIdx.x; k < (zero ? 0 : K); k += THREADS) {
             const int j = S.id[k];
             if (j < sh.j0 || j >= sh.j1 || !R.first_of(S, k)) continue;
             float q = 0.0f;
+#pragma unroll 1
             for (int i = k; i < (R.repeated ? K : k + 1); ++i)
                 if (S.id[i] == j) q = __fadd_rn(q, R.q(S, i));
             const float p = __fmul_rn(ex2(__fmul_rn(__fsub_rn(S.z[k], R.m), c)), one);
@@ -500,6 +515,7 @@ __global__ __launch_bounds__(THREADS + 32, 512 / THREADS) void k_distill_grad(co
 
     int turn = 0;
     unsigned joins = 0;                 // rows joined so far
+#pragma unroll 1
     for (int64_t r = first; r < rows; r += step, turn ^= 1) {
         team_sync<THREADS>();           // the marks are set; the row before is written
         if (threadIdx.x == 0) twice[turn ^ 1] = 0, edge_map[turn ^ 1] = 0;
@@ -515,6 +531,7 @@ __global__ __launch_bounds__(THREADS + 32, 512 / THREADS) void k_distill_grad(co
         const int n_vec = sh.v1 - sh.v0, passing = in.passing(n_vec);
         int chunks = 0;
         float unused = 0.0f;
+#pragma unroll 1
         for (int base = 0;; ) {
             const int p = in.take();
             uint4 x[UNROLL];
@@ -533,6 +550,7 @@ __global__ __launch_bounds__(THREADS + 32, 512 / THREADS) void k_distill_grad(co
         if (has_edge && !(BUCKET && (edge_map[turn] >> threadIdx.x & 1))) add_element(R.a, to_float(z_own_edge), c);
         R.repeated = twice[turn];
         R.peak = peak, R.peak_z = -3.402823466e38f, R.odd = odd;
+#pragma unroll 1
         for (int k = threadIdx.x; k < K; k += THREADS) {
             const int j = S.id[k];
             if (k >= THREADS && j >= 0) around = fetch_around(row, sh, j);
@@ -542,6 +560,7 @@ __global__ __launch_bounds__(THREADS + 32, 512 / THREADS) void k_distill_grad(co
             if (BUCKET) R.template add_around<T>(S, marks, sh, k, around, c);
         }
         R.template join<THREADS>(c, K, part[turn]);
+#pragma unroll 1
         for (int k = threadIdx.x; k < K; k += THREADS) marks.clear<E>(sh, S.id[k]);          // for the next row
         if (blocks > 1) R.exchange(in, blocks, rank, c, own[turn], &joined[turn], joins++ >> 1 & 1);
         R.template sum_slots<THREADS>(S, K, lse, c, part2[turn]);
@@ -565,13 +584,18 @@ __global__ __launch_bounds__(THREADS + 32, 512 / THREADS) void k_distill_grad(co
         if (r + step < rows) open_row(r + step, turn ^ 1);
         const uint64_t m2 = pair(-R.a.m, -R.a.m), c2 = pair(c, c), f2 = pair(factor, factor);
         // element by element where dlogits is not aligned as the logits are, and for rows of zeros whatever they hold
+        const bool aligned = ((uintptr_t)dbody & 15) == 0;
         auto write_any = [&](const uint4 &x, int i) {
             float f[E];
             Vec<T>::unpack(x, f);
 #pragma unroll
-            for (int e = 0; e < E; ++e)
-                dbody[i * E + e] =
-                    from_float<T>(zero ? 0.0f : __fmul_rn(ex2(__fmul_rn(__fsub_rn(f[e], R.a.m), c)), factor));
+            for (int e = 0; e < E; ++e) f[e] = zero ? 0.0f : __fmul_rn(ex2(__fmul_rn(__fsub_rn(f[e], R.a.m), c)), factor);
+            if (aligned) {
+                __stcs(reinterpret_cast<uint4 *>(dbody) + i, Vec<T>::pack(f));
+            } else {
+#pragma unroll
+                for (int e = 0; e < E; ++e) dbody[i * E + e] = from_float<T>(f[e]);
+            }
         };
         // 16-bit results: (z - m) c by one fused operation, whose m c is rounded to 2^-16 at most, against half a
         // unit of 2^-12 of the result; m is the row's, so that only rows of logits beyond 170 take the general form
@@ -589,24 +613,21 @@ __global__ __launch_bounds__(THREADS + 32, 512 / THREADS) void k_distill_grad(co
             }
             __stcs(reinterpret_cast<uint4 *>(dbody) + i, Vec<T>::pack(f));
         };
-        const bool plain = !zero && (fused || sizeof(T) == 4) && ((uintptr_t)dbody & 15) == 0;
+        const bool plain = !zero && (fused || sizeof(T) == 4) && aligned;
         // the held chunks first, while the others are brought again
         const int held = chunks - passing;
+#pragma unroll 1
         for (int n = 0; n < chunks; ++n) {
             const int p = n < held ? in.before(held - n) : in.take();
-            uint4 x[UNROLL];
-            in.read(x, p);
             const int base = (n < held ? passing + n : n - held) * In::SPAN, i = base + lane_start();
             if (plain && base + In::SPAN <= n_vec) {
+                uint4 x[UNROLL];
+                in.read(x, p);
 #pragma unroll
                 for (int u = 0; u < UNROLL; ++u) write(x[u], i + u * 32);
             } else {
-#pragma unroll
-                for (int u = 0; u < UNROLL; ++u)
-                    if (i + u * 32 < n_vec) {
-                        if (plain) write(x[u], i + u * 32);
-                        else write_any(x[u], i + u * 32);
-                    }
+#pragma unroll 1
+                for (int u = 0; u < UNROLL && i + u * 32 < n_vec; ++u) write_any(in.read_one(p, u), i + u * 32);
             }
             in.give_back(p);
         }

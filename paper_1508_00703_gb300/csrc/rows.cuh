@@ -406,6 +406,7 @@ struct Stream {
     __device__ __forceinline__ void wait(uint64_t *bar, unsigned par)
     {
         if (bar_done(bar, par) || gave_up) return;
+#pragma unroll 1
         for (unsigned i = 0; i < LIMIT; ++i)
             if (bar_done(bar, par)) return;
         set_status(status, PDB_ETIMEOUT);
@@ -417,6 +418,7 @@ struct Stream {
         place = place_, full = bars, empty = bars + MOST_SLOTS, status = status_, slots = slots_, hold = hold_;
         slot = 0, parity = 0, gave_up = false;
         if (threadIdx.x == 0) {
+#pragma unroll 1
             for (int i = 0; i < slots; ++i) {
                 bar_init(full + i, 1);
                 bar_init(empty + i, THREADS / 32);
@@ -436,13 +438,16 @@ struct Stream {
                                                int rank, int blocks)
     {
         int brought = 0;
+#pragma unroll 1
         for (int64_t r = first; r < rows; r += step) {
             const T *row = logits + r * stride;
             const Share sh = share_of(row, cols, rank, blocks);
             const uint4 *body = reinterpret_cast<const uint4 *>(row + sh.b0);
             const int n_vec = sh.v1 - sh.v0;
             int end = n_vec;
+#pragma unroll 1
             for (int sweep = 0; sweep < 2; ++sweep) {
+#pragma unroll 1
                 for (int v = 0; v < end || (sweep == 0 && v == 0); v += SPAN) {
                     wait(empty + slot, parity ^ 1);         // a place never used is free
                     const int n = min(SPAN, end - v);
@@ -455,6 +460,7 @@ struct Stream {
             }
         }
         // nothing is under way when the block ends, whatever became of the other warps
+#pragma unroll 1
         for (int i = 0; i < min(slots, brought); ++i) {
             if (slot == 0) slot = slots, parity ^= 1;
             --slot;
@@ -475,6 +481,10 @@ struct Stream {
         const unsigned at = shared_addr(place) + (unsigned)(p * SPAN + lane_start()) * 16;
 #pragma unroll
         for (int u = 0; u < UNROLL; ++u) x[u] = ld_shared(at + u * 512);
+    }
+    __device__ __forceinline__ uint4 read_one(int p, int u) const
+    {
+        return ld_shared(shared_addr(place) + (unsigned)(p * SPAN + lane_start() + u * 32) * 16);
     }
     // the place of the chunk taken n takes ago
     __device__ __forceinline__ int before(int n) const { return slot - n < 0 ? slot - n + slots : slot - n; }
