@@ -545,21 +545,21 @@ inline Shape once_shape(int64_t rows, int64_t cols, int vec, int sms, size_t ext
 constexpr size_t block_smem(int per) { return SMEM_PER_SM / per - 1024 - STATIC_SMEM; }
 
 // Two visits per row: persistent clusters, 512 threads of an SM in blocks of 128 or 256 and each block's warp that brings its
-// rows, each with its part of the SM's shared memory for the stream.  A row goes to one block of 128 up to 80 KB, to two up to 160 KB,
-// then to blocks of 256 whose shares end at 160 KB.  Measured with gradient, us, by 1 x 128, 2 x 128, 1 x 256, 2 x 256, 4 x 256:
-// 8000 x 32,000 bf16 219, 228, 226, 317, 527; 4000 x 64,000 bf16 227, 194, 199, 229, 330; 1501 x 50,001 fp32 144, 126, 124, 116, 149;
-// 4096 x 128,000 bf16 -, 452, -, 381, 464; 3000 x 90,000 fp32 -, 470, -, 397, 356.  Larger shares go to memory for their second
-// visit (more than L2 keeps is under way); smaller ones leave too little work between a row's waits.
+// rows, each with its part of the SM's shared memory for the stream.  A row goes to one block of 128 up to 72 KB, to two up to
+// 144 KB, then to two of 256, to four from 288 KB.  Measured with gradient, us, by 1 x 128, 2 x 128, 1 x 256, 2 x 256, 4 x 256:
+// 8000 x 32,000 bf16 176, 212, 203, 308, 521; 4000 x 64,000 bf16 222, 177, 174, 212, 320; 3000 x 40,000 fp32 212, 181, 181, 160, 232;
+// 4096 x 128,000 bf16 475, 450, 447, 356, 451; 3000 x 90,000 fp32 479, 470, 469, 398, 354.  Larger shares go to memory for
+// their second visit (more than L2 keeps is under way); smaller ones leave too little work between a row's waits.
 // No more clusters than run at once (t.room): one cluster more, and the others wait for its rows (76 clusters of 4 where 74
 // have room: 3000 x 128,000 fp32 733 us, 487 by 74).
 inline Shape twice_shape(int64_t rows, int64_t cols, int vec, const pdb_tokens &t, size_t extra)
 {
     const int64_t nv = cols / vec + 1;
     Shape s = {};
-    s.threads = nv <= 10240 ? 128 : 256;
+    s.threads = nv <= 9216 ? 128 : 256;
     const int per = 512 / s.threads;
     s.blocks = cluster_of(rows, nv, s.threads, [&](int blocks) { return t.room[per / 2][__builtin_ctz(blocks)]; });
-    while (nv / s.blocks > s.threads * 40 && s.blocks < MAX_CLUSTER) s.blocks *= 2;
+    while (nv / s.blocks > s.threads * 36 && s.blocks < MAX_CLUSTER) s.blocks *= 2;
     set_maps(s, nv / s.blocks + 1);
     const size_t chunk = (size_t)UNROLL * 16 * s.threads, fixed = extra + s.map_bytes, most = block_smem(per);
     const int64_t chunks = std::max<int64_t>(1, (nv / s.blocks + UNROLL * s.threads) / (UNROLL * s.threads));
