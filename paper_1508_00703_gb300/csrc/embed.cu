@@ -374,6 +374,7 @@ __device__ __forceinline__ int64_t keys_below(const uint32_t *__restrict__ key, 
 {
     const int lane = threadIdx.x & 31;
     int64_t lo = 0, hi = n;              // the answer lies in [lo, hi]
+#pragma unroll 1
     while (lo < hi) {
         const int64_t step = (hi - lo + 31) / 32, at = lo + lane * step;
         const int below = __popc(__ballot_sync(FULL, at < hi && key[at] < v));
@@ -392,6 +393,7 @@ __device__ __forceinline__ void zero_rows(const uint32_t *__restrict__ key, int6
     const int lane = threadIdx.x & 31;
     const uint32_t first = (uint32_t)v0, end = (uint32_t)min64(vocab, v0 + 32);
     unsigned present = 0;
+#pragma unroll 1
     for (int64_t at = keys_below(key, n, first); at < n;) {
         const uint32_t k = at + lane < n ? key[at + lane] : 0xffffffffu;
         present |= __reduce_or_sync(FULL, k < end ? 1u << (k - first) : 0u);
@@ -404,9 +406,11 @@ __device__ __forceinline__ void zero_rows(const uint32_t *__restrict__ key, int6
     Pack<O, E> zero;
 #pragma unroll
     for (int e = 0; e < E; ++e) zero.e[e] = from_float<O>(0.0f);
+#pragma unroll 1
     while (absent) {
         O *row = dtable + (v0 + __ffs(absent) - 1) * stride;
         absent &= absent - 1;
+#pragma unroll 1
         for (int j = lane * E; j < dim; j += 32 * E) store_pack<O, E>(row + j, zero);
     }
 }
@@ -476,6 +480,7 @@ __global__ __launch_bounds__(SUM_WARPS * 32, ACC ? 2 : 4) void k_embed_sum(const
         const uint32_t a = __shfl_sync(FULL, k[0], i & 31), b = __shfl_sync(FULL, k[1], i & 31);
         return i < 32 ? a : b;
     };
+#pragma unroll 1
     for (int i0 = s0; i0 < end; i0 += SUM_UNROLL) {
         Pack<T, E> x[SUM_UNROLL];
         Pack<O, E> old[ACC ? SUM_UNROLL : 1];
