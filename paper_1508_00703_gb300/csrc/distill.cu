@@ -355,7 +355,7 @@ __global__ __launch_bounds__(THREADS, 1024 / THREADS) void k_distill_loss(const 
     RawSlot slot = {};
     if ((int)threadIdx.x < K) slot.fetch(teach, r, threadIdx.x);
     uint4 x[UNROLL];
-    load_vectors<T, THREADS>(x, body, 0, n_vec);
+    load_vectors<T, THREADS, 32>(x, body, 0, lane_start(), n_vec);
     const bool has_edge = (int)threadIdx.x < sh.edges();
     T z_edge = from_float<T>(0.0f);
     if (has_edge) z_edge = row[sh.edge(threadIdx.x)];
@@ -384,7 +384,7 @@ __global__ __launch_bounds__(THREADS, 1024 / THREADS) void k_distill_loss(const 
     float unused = 0.0f;
     for (int base = 0; base < n_vec; base += THREADS * UNROLL) {
         uint4 next[UNROLL];
-        load_vectors<T, THREADS>(next, body, base + THREADS * UNROLL, n_vec);
+        load_vectors<T, THREADS, 32>(next, body, base + THREADS * UNROLL, lane_start(), n_vec);
         if (BUCKET) marks.leave_out<T>(x, base);
         add_vectors<T, false>(R.a, x, c, unused);
 #pragma unroll

@@ -9,15 +9,18 @@
 // Alternatives.  The pass keeps the maximum of each of 64 or 128 groups of
 // neighbouring threads.  A value tau that k of them reach is at most the k-th largest
 // logit, since k different logits reach it, and the groups that reach tau hold every logit that
-// does.  Only those groups' vectors are read again (from L2), their logits
-// >= tau collected (a few more than k as a rule) and ranked by counting.  Where more
+// does.  Only those groups' vectors are read again (from L2, dealt out over the block: a warp per group
+// waited for one group after the other, 3472 x 18,034 bf16 with 32 alternatives 54 us, 48 now), their logits
+// >= tau collected (a few more than k as a rule) and ranked by counting.  A thread's vectors are the block's
+// size apart, so that short shares have as many groups as long ones (8 x 4372 bf16, 32 alternatives: 17 us by
+// contiguous warps, whose few groups let too much through, 8 now).  Where more
 // than the buffer reach tau (ties, masked rows) or a NaN hides from the maxima, a radix
 // selection over the block's share takes over: four counting passes, exact for
 // any order of the row.  The pass itself pays one maximum per thread and 64 bytes.
 //
 // Measured: 2039 x 50,001 bf16, entropy and 5 alternatives 48 us, 204 MB at 4.2 TB/s: 59% of the issue slots
-// taken (51 instructions per 8 logits, alternatives 15% on top), the rest waits at the rows' ends; 4096 x 128,000
-// bf16 without alternatives 157 us of 460 with the gradient, 6.7 TB/s; 4 x 128,000 with 20 alternatives 9.2 us, a chain of
+// taken (51 instructions per 8 logits), the rest waits at the rows' ends; 4096 x 128,000
+// bf16 without alternatives 154 us of 460 with the gradient, 6.8 TB/s; 4 x 128,000 with 20 alternatives 8.4 us, a chain of
 // latencies (two launches' worth of barriers, three reads).
 #include <algorithm>
 #include <cmath>
@@ -151,13 +154,15 @@ __device__ __forceinline__ int top_of_share(TopShared &t, const T *row, const ui
         if (threadIdx.x < 32) {
             // tau by bisection over the orders of the groups' maxima: any value that k groups reach will do, the higher
             // the better; it stops when hardly more than k do
-            uint32_t o[GROUPS / 32], lo = 0, hi = 0;
+            uint32_t o[GROUPS / 32], lo = 0xffffffffu, hi = 0;
 #pragma unroll
             for (int i = 0; i < GROUPS / 32; ++i) {
                 o[i] = i * 32 < groups ? order_of(t.group[i * 32 + threadIdx.x]) : 0u;
                 hi = max(hi, o[i]);
+                if (i * 32 < groups) lo = min(lo, o[i]);
             }
             hi = __reduce_max_sync(FULL, hi) + 1;          // no group reaches hi; all reach lo
+            lo = __reduce_min_sync(FULL, lo);
             while (hi - lo > 1) {
                 const uint32_t mid = lo + (hi - lo) / 2;
                 int n = 0;
@@ -167,33 +172,39 @@ __device__ __forceinline__ int top_of_share(TopShared &t, const T *row, const ui
                 else hi = mid;
                 if (n >= k && n <= k + 1 + k / 8) break;
             }
-            if (threadIdx.x == 0) t.tau = order_value(lo == 0 ? order_of(-INFINITY) : lo);
+            if (threadIdx.x == 0) t.tau = order_value(lo);
         }
         __syncthreads();
         const float tau = t.tau;
         if ((int)threadIdx.x < groups && t.group[threadIdx.x] >= tau) t.list[atomicAdd(&t.n_list, 1)] = threadIdx.x;
         __syncthreads();
         const int n_list = t.n_list;    // k, or somewhat more
-        // a warp reads one group's vectors, `per` of them side by side
-        const int lane = threadIdx.x & 31, sub = lane % (unsigned)per, n_vec = sh.v1 - sh.v0;
+        const int n_vec = sh.v1 - sh.v0, turns = (n_vec + THREADS - 1) / THREADS;
         auto take = [&](float z, int j) {
             if (z >= tau) {
                 const int at = atomicAdd(&t.n, 1);
                 if (at < BUFFER) t.key[at] = key_of(order_of(z), j);
             }
         };
-        for (int g = threadIdx.x >> 5; g < n_list; g += THREADS / 32) {
-            const int member = t.list[g] * per + sub, start = (member & ~31) * UNROLL + (member & 31);
-            for (int i = lane / (unsigned)per;; i += 32 / (unsigned)per) {
-                const int v = start + i / UNROLL * (THREADS * UNROLL) + i % UNROLL * 32;
-                if (i / UNROLL * (THREADS * UNROLL) >= n_vec) break;
-                if (v >= n_vec) continue;
-                const uint4 x = ld_keep(share + v);
-                if (Vec<T>::max_float(Vec<T>::vmax(Vec<T>::max_init(), x)) < tau) continue;
-                float f[E];
-                Vec<T>::unpack(x, f);
+        // the groups' vectors, dealt out over the block, UNROLL of a thread under way; those side by side go together
+#pragma unroll 1
+        for (int i0 = threadIdx.x; i0 < n_list * turns * per; i0 += THREADS * UNROLL) {
+            uint4 x[UNROLL];
+            int at[UNROLL];
 #pragma unroll
-                for (int e = 0; e < E; ++e) take(f[e], sh.b0 + v * E + e);
+            for (int u = 0; u < UNROLL; ++u) {
+                const int i = i0 + u * THREADS, pair = i / (unsigned)per, g = pair / (unsigned)turns;
+                at[u] = n_vec;
+                if (g < n_list) at[u] = (pair - g * turns) * THREADS + t.list[g] * per + (i & (per - 1));
+                if (at[u] < n_vec) x[u] = ld_keep(share + at[u]);
+            }
+#pragma unroll
+            for (int u = 0; u < UNROLL; ++u) {
+                if (at[u] >= n_vec || Vec<T>::max_float(Vec<T>::vmax(Vec<T>::max_init(), x[u])) < tau) continue;
+                float f[E];
+                Vec<T>::unpack(x[u], f);
+#pragma unroll
+                for (int e = 0; e < E; ++e) take(f[e], sh.b0 + at[u] * E + e);
             }
         }
         if ((int)threadIdx.x < sh.edges()) take(to_float(row[sh.edge(threadIdx.x)]), sh.edge(threadIdx.x));
@@ -252,10 +263,10 @@ __global__ __launch_bounds__(THREADS, 1024 / THREADS) void k_logprobs(const T *_
     float top = -INFINITY;
     {
         uint4 v[UNROLL];
-        load_vectors<T, THREADS>(v, body, 0, n_vec);
+        load_vectors<T, THREADS, THREADS>(v, body, 0, threadIdx.x, n_vec);
         for (int base = 0; base < n_vec; base += THREADS * UNROLL) {
             uint4 next[UNROLL];
-            load_vectors<T, THREADS>(next, body, base + THREADS * UNROLL, n_vec);
+            load_vectors<T, THREADS, THREADS>(next, body, base + THREADS * UNROLL, threadIdx.x, n_vec);
             add_vectors<T, ENT>(a, v, c, top);
 #pragma unroll
             for (int u = 0; u < UNROLL; ++u) v[u] = next[u];
@@ -330,7 +341,7 @@ __global__ __launch_bounds__(THREADS) void k_logprobs_grad(const T *logits, int 
     const uint4 *body = reinterpret_cast<const uint4 *>(row + sh.b0);
     const int n_vec = sh.v1 - sh.v0;
     uint4 v[UNROLL];
-    load_vectors<T, THREADS>(v, body, 0, n_vec);          // on their way while the row's numbers arrive
+    load_vectors<T, THREADS, 32>(v, body, 0, lane_start(), n_vec);          // on their way while the row's numbers arrive
 
     float g = dlogp ? dlogp[r] : 0.0f;
     const float h = dentropy ? dentropy[r] : 0.0f;
@@ -356,7 +367,7 @@ __global__ __launch_bounds__(THREADS) void k_logprobs_grad(const T *logits, int 
     const bool aligned = ((uintptr_t)(drow + sh.b0) & 15) == 0;
     for (int base = 0; base < n_vec; base += THREADS * UNROLL) {
         uint4 next[UNROLL];
-        load_vectors<T, THREADS>(next, body, base + THREADS * UNROLL, n_vec);
+        load_vectors<T, THREADS, 32>(next, body, base + THREADS * UNROLL, lane_start(), n_vec);
 #pragma unroll
         for (int u = 0; u < UNROLL; ++u) {
             const int i = base + lane_start() + u * 32;

@@ -340,21 +340,20 @@ __device__ __forceinline__ void add_element(Stat<ENT> &a, float z, float c)
 // where a thread's vectors of a chunk start; they are 32 apart
 __device__ __forceinline__ int lane_start() { return (int)(threadIdx.x & ~31u) * UNROLL + (int)(threadIdx.x & 31); }
 
-// a thread's vectors of the chunk at `base` of a share of `end` vectors, -inf past it
-template <typename T, int THREADS>
-__device__ __forceinline__ void load_vectors(uint4 (&v)[UNROLL], const uint4 *__restrict__ share, int base, int end)
+// a thread's vectors of the chunk at `base` of a share of `end` vectors, -inf past it: `first`, and every STEP-th
+template <typename T, int THREADS, int STEP>
+__device__ __forceinline__ void load_vectors(uint4 (&v)[UNROLL], const uint4 *__restrict__ share, int base, int first, int end)
 {
     constexpr uint32_t N = Vec<T>::NEG_INF;
-    const int first = base + lane_start();
-    const uint4 *from = share + first;
+    const uint4 *from = share + base + first;
     if (base + UNROLL * THREADS <= end) {
 #pragma unroll
-        for (int u = 0; u < UNROLL; ++u) v[u] = ld_keep(from + u * 32);
+        for (int u = 0; u < UNROLL; ++u) v[u] = ld_keep(from + u * STEP);
     } else {
 #pragma unroll
         for (int u = 0; u < UNROLL; ++u) {
             v[u] = uint4{N, N, N, N};
-            if (first + u * 32 < end) v[u] = ld_keep(from + u * 32);
+            if (base + first + u * STEP < end) v[u] = ld_keep(from + u * STEP);
         }
     }
 }
