@@ -420,7 +420,7 @@ __global__ __launch_bounds__(THREADS, 1024 / THREADS) void k_distill_loss(const 
 // left rolled it is 54 KB, and 8000 x 32,000 bf16 take 176 us; unrolled by the compiler's choice 97 KB and 219 us.
 
 template <typename T, bool BUCKET, int THREADS>
-__global__ __launch_bounds__(THREADS + 32, 512 / THREADS) void k_distill_grad(const T *logits, int64_t rows, int cols, int64_t stride,
+__global__ __launch_bounds__(THREADS + 32, blocks_per_sm(THREADS)) void k_distill_grad(const T *logits, int64_t rows, int cols, int64_t stride,
                                                                          Teacher teach, float temperature, float *loss,
                                                                          const float *__restrict__ weight, T *dlogits,
                                                                          int64_t out_stride, int slots, int hold,
@@ -654,13 +654,14 @@ int count_room(pdb_tokens *t)
     cudaLaunchConfig_t cfg = {};
     cfg.attrs = &at;
     cfg.numAttrs = 1;
-    for (int i = 0; i < 3; ++i)
+    for (int i = 0; i <= ROOM_ALONE; ++i)
         for (int log = 0; log < 4; ++log) {
+            const int threads = i == ROOM_ALONE ? 256 : 256 >> i;
             at.val.clusterDim.x = 1u << log;
             at.val.clusterDim.y = at.val.clusterDim.z = 1;
             cfg.gridDim = dim3((unsigned)t->sms * 8);
-            cfg.blockDim = dim3(512 / (i == 2 ? 4 : 2) + 32);
-            cfg.dynamicSmemBytes = block_smem(1 << i);
+            cfg.blockDim = dim3(threads + 32);
+            cfg.dynamicSmemBytes = block_smem(i == ROOM_ALONE ? 1 : blocks_per_sm(threads));
             if (cudaOccupancyMaxActiveClusters(&t->room[i][log], kernel, &cfg) != cudaSuccess) return PDB_ECUDA;
             if (t->room[i][log] < 1) return PDB_ECUDA;
         }
@@ -705,14 +706,15 @@ extern "C" int pdb_distill(pdb_tokens *t, const pdb_mat *logits, const pdb_ids *
             });
         }
         const size_t slot_bytes = ((size_t)teach.K * SLOT_BYTES * 2 + 15) / 16 * 16;
-        Shape shape = twice_shape(logits->rows, logits->cols, Vec<T>::E, *t, slot_bytes);
-        return with_threads(shape.threads, [&](auto n) {
+        Shape shape = twice_shape(logits->rows, logits->cols, Vec<T>::E, *t, slot_bytes, teach.K);
+        const auto run = [&](auto n) {
             constexpr int N = decltype(n)::value;
             shape.threads = N + 32;     // and the warp that brings the rows
             return launch_rows(teacher_lse ? k_distill_grad<T, true, N> : k_distill_grad<T, false, N>, shape, s,
                                (const T *)logits->data, logits->rows, (int)logits->cols, stride_of(logits), teach,
                                temperature, loss, weight, (T *)dlogits->data, stride_of(dlogits), shape.slots, shape.hold,
                                shape.map_bytes, shape.bit_bytes, t->status);
-        });
+        };
+        return shape.threads == 64 ? run(Num<64>()) : shape.threads == 128 ? run(Num<128>()) : run(Num<256>());
     });
 }

@@ -9,7 +9,7 @@
 
 struct pdb_tokens {
     int device, sms;
-    int room[3][4];            // clusters of 1, 2, 4, 8 blocks that run at once, by 1, 2, 4 blocks an SM (distill.cu)
+    int room[4][4];            // clusters of 1, 2, 4, 8 blocks that run at once: blocks of 256, 128, 64, one an SM (distill.cu)
     int64_t max_tokens, max_dim;
     int *status;               // device: [0] first error recorded by a kernel; [1] always 0 (the radix
                                // sort's kernels return at once when their status word is set); [2] long runs (embed.cu)
@@ -24,6 +24,8 @@ struct pdb_tokens {
 };
 
 namespace pdb {
+
+constexpr int ROOM_ALONE = 3;
 
 // every call on a handle records ev_use when it returns; not while a graph is
 // recorded, whose event could not be waited for (the graph's owner keeps the handle)
