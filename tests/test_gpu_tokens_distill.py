@@ -294,3 +294,27 @@ def test_without_slots(tok):
     pdb.pdb_distill(tok, z, torch.zeros(3, 0, dtype=torch.int32, device="cuda"), torch.zeros(3, 0, device="cuda"), loss,
                     dlogits=d)
     assert loss.tolist() == [0.0] * 3 and torch.count_nonzero(d) == 0
+
+
+@pytest.mark.parametrize("n,cols,K,kind", [
+    (1000, 10_200, 64, "bf16"), (700, 10_200, 65, "f16"), (700, 10_260, 64, "bf16"), (1300, 5100, 3, "f32"),   # 64 or 128 threads
+    (300, 36_851, 9, "bf16"), (650, 36_871, 9, "f16"), (320, 73_702, 40, "bf16"),                              # one or two blocks
+    (200, 36_877, 40, "f32"), (160, 73_720, 12, "f32"), (170, 73_741, 12, "f32")])                             # two or four
+def test_rows_on_each_side_of_a_split(tok, n, cols, K, kind):
+    # more rows than clusters at once, so that every cluster takes several; in place the same bits as beside
+    g = _gen(cols + K)
+    z, ids, top, lse = _problem(n, cols, K, N.TYPES[kind], g, 2.0)
+    w = torch.rand(n, device="cuda", generator=g)
+    w[1::7] = 0.0                                       # rows of zeros among the others
+    ids[2::5, K // 2:] = -1                             # rows with empty slots
+    loss, d = torch.full((n,), 55.0, device="cuda"), torch.full_like(z, 9.0)
+    pdb.pdb_distill(tok, z, ids, top, loss, teacher_lse=lse, weight=w, dlogits=d, temperature=2.0)
+    for rows in (slice(0, 6), slice(n // 2, n // 2 + 6), slice(n - 6, n)):
+        (want, tol), (grad, tol_g) = N.distill(z[rows], ids[rows], top[rows], lse[rows], 2.0, w[rows], z.dtype)
+        N.assert_near(loss[rows], want, tol, "loss")
+        N.assert_near(d[rows], grad, tol_g, "dlogits")
+    assert torch.count_nonzero(d[1::7]) == 0
+    again = torch.full((n,), 55.0, device="cuda")
+    pdb.pdb_distill(tok, z, ids, top, again, teacher_lse=lse, weight=w, dlogits=z, temperature=2.0)
+    assert torch.equal(z, d) and torch.equal(again, loss)
+    pdb.check_tokens(tok)

@@ -349,3 +349,17 @@ def test_refusals():
     refused(pdb.PDB_EINVAL, pdb.pdb_tokens_create, -1, 4)
     refused(pdb.PDB_ETOOBIG, pdb.pdb_tokens_create, 1 << 31, 4)
     assert pdb.pdb_tokens_status(tok) == pdb.PDB_OK
+
+
+@pytest.mark.parametrize("n,vocab,dim,layout", [(1, 33, 4100, "whole"), (5, 9045, 880, "whole"), (40, 2100, 4096, "padded"),
+                                                (300, 1999, 1200, "shifted"), (2500, 5001, 700, "whole"),
+                                                (17_000, 9000, 516, "whole")])
+def test_zeroing_by_parts(n, vocab, dim, layout):
+    # rows long enough for several warps to share 32 of them, some written beside the sort, and a last group that is not whole
+    g = _gen(n)
+    tok = pdb.pdb_tokens_create(n, dim)
+    ids = _some_ids("zipf", n, vocab, g)
+    dout = _matrix(n, dim, torch.float32, g, layout)
+    _check_grad(ids, dout, vocab, 0.5, torch.float32, False, tok, layout)
+    _check_grad(ids % 32, dout, vocab, 0.5, torch.bfloat16, False, tok, layout)
+    pdb.check_tokens(tok)

@@ -341,3 +341,15 @@ def test_without_columns(tok):
     lse, H = torch.ones(3, device="cuda"), torch.ones(3, device="cuda")
     pdb.pdb_logprobs(tok, torch.empty(3, 0, device="cuda"), lse=lse, entropy=H)
     assert lse.tolist() == [-INF] * 3 and H.tolist() == [0.0] * 3
+
+
+@pytest.mark.parametrize("n,cols,k", [(1, 4470, 32), (8, 4372, 32), (3, 2051, 64), (20, 8200, 17), (245, 3728, 32), (2, 70_000, 64)])
+def test_alternatives_of_short_shares(tok, n, cols, k):
+    # few vectors for a block's threads, alone or split over a cluster; most of a row masked
+    g = _gen(cols + k)
+    ids = torch.randint(0, cols, (n,), device="cuda", generator=g)
+    z = _logits(n, cols, torch.float16, g)
+    _check(tok, z, ids, k=k)
+    drop = torch.rand(n, cols, device="cuda", generator=g) < 0.97
+    drop[:, -k:] = False
+    _check(tok, _lay(z.float().masked_fill(drop, -INF), "shifted"), ids, k=k)
