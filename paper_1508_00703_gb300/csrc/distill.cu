@@ -16,8 +16,8 @@
 // written over after that by the block that holds them.
 //
 // Measured: the loss alone, 1024 x 32,000 fp16, 64 slots, 15.6 us (66 MB, 4.2 TB/s: one round of blocks, of whose time
-// start, joins and end are 6 us); with gradient 4096 x 128,000 bf16 415 us (2.1 GB, 5.1 TB/s; DRAM moves little more
-// than that, the rest is time per row), 1501 x 50,001 fp32 123 us (4.9 TB/s).
+// start, joins and end are 6 us); with gradient 4096 x 128,000 bf16 356 us (2.1 GB, 5.9 TB/s; DRAM moves little more
+// than that, the rest is time per row), 1501 x 50,001 fp32 114 us (5.3 TB/s), 3000 x 128,000 fp32 487 us (6.3 TB/s).
 #include <algorithm>
 #include <cmath>
 

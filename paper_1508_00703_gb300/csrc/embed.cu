@@ -354,7 +354,7 @@ __global__ __launch_bounds__(SORT_THREADS) void k_embed_sort(Ids ids, int n, int
 // pieces.  So the work is even whatever the ids: a hot id of 6000 rows is 188 pieces.
 // Bound by memory: each row is read once, each result written once, and `part` is written and read for runs
 // over 32 only, 1/8 (fp32 rows) or 1/4 (16-bit rows) of those runs' bytes in all.  65,536 x 2048 bf16 into 50,000 rows of
-// fp32: 640 MB in 128 us, 5.0 TB/s (copies 6.7), whatever the occupancy (24 or 32 warps an SM).
+// fp32: 582 MB (and some of the zeros earlier, below) in 104 us, 5.6 TB/s (copies 6.7).
 constexpr int PIECE = 32, SUM_WARPS = 8;
 
 template <typename O, int E, bool ACC>
@@ -716,8 +716,8 @@ int pdb_embed_grad(pdb_tokens *t, const pdb_ids *ids, const pdb_mat *dout, float
     if (vocab == 0 && n == 0) return PDB_OK;
     cudaStream_t s = (cudaStream_t)stream;
     TokensUse use{t, s};
-    // What the sort leaves idle writes zeros: about as many bytes as go to memory in its time (the 20 us of 65,536 ids: 167 us
-    // -> 157 with 50,000 rows of 8 KB), none for the short sorts and rows that are not whole 16-byte pieces.
+    // What the sort leaves idle writes zeros: about as many bytes as go to memory in its time (the 25 us of 65,536 ids: 148 us
+    // -> 142 with 50,000 rows of 8 KB), none for the short sorts and rows that are not whole 16-byte pieces.
     Fill fill = {};
     const int64_t row_bytes = (int64_t)dim * type_bytes(dtable->type), step = stride_of(dtable) * type_bytes(dtable->type);
     if (!accumulate && n > RANK_MAX && n <= SORT_MAX && row_bytes > 0 && row_bytes % 16 == 0 && step % 16 == 0 &&
