@@ -420,11 +420,10 @@ __global__ __launch_bounds__(THREADS, 1024 / THREADS) void k_distill_loss(const 
 // left rolled it is 54 KB, and 8000 x 32,000 bf16 take 176 us; unrolled by the compiler's choice 97 KB and 219 us.
 
 template <typename T, bool BUCKET, int THREADS>
-__global__ __launch_bounds__(THREADS + 32, blocks_per_sm(THREADS)) void k_distill_grad(const T *logits, int64_t rows, int cols, int64_t stride,
-                                                                         Teacher teach, float temperature, float *loss,
-                                                                         const float *__restrict__ weight, T *dlogits,
-                                                                         int64_t out_stride, int slots, int hold,
-                                                                         int map_bytes, int bit_bytes, int *status)
+__global__ __launch_bounds__(THREADS + 32, blocks_per_sm(THREADS)) void k_distill_grad(
+    const T *logits, int64_t rows, int cols, int64_t stride, Teacher teach, float temperature, float *loss,
+    const float *__restrict__ weight, T *dlogits, int64_t out_stride, int slots, int hold, int map_bytes, int bit_bytes,
+    int *status)
 {
     constexpr int E = Vec<T>::E;
     constexpr uint32_t NEG_INF = Vec<T>::NEG_INF;
