@@ -474,6 +474,12 @@ int pdb_tokens_create(int64_t max_tokens, int64_t max_dim, pdb_tokens **out, voi
 void pdb_tokens_free(pdb_tokens *t);
 int pdb_tokens_status(const pdb_tokens *t, void *stream);
 
+/* Tries of a device-side wait in later calls on the handle (pdb_distill with gradient is the one
+ * that waits), each 20 ns to a microsecond, before PDB_ETIMEOUT; 2^22 unless set, at most 2^30.
+ * With 0 no try is made and such calls end with PDB_ETIMEOUT and undefined results: for tests of
+ * what a program does then. */
+int pdb_tokens_set_wait_limit(pdb_tokens *t, int64_t tries);
+
 /* out[i, :] = scale * table[ids[i], :]  (ids->n = out->rows, cols equal).
  * Reads of the chunks that the ids name (Definition 3).  An id equal to `pad`
  * gives a row of zeros, whatever its value; so does any other id outside [0, table->rows), which
@@ -544,8 +550,9 @@ int pdb_logprobs_grad(pdb_tokens *t, const pdb_mat *logits, const pdb_ids *ids, 
  * gradient 0; a row of weight 0 has gradient 0, whatever it holds; a row of logits with
  * nothing but -inf has loss +inf and gradient 0.  A NaN in a row makes its loss and gradient NaN.
  * dlogits may be the logits' own memory (same data, stride and type); it must not overlap
- * them otherwise.  PDB_ETOOBIG above 1024 slots or 2^21 tokens.  Every wait of the kernel is bounded:
- * one that runs out is recorded as PDB_ETIMEOUT and leaves the results of its rows undefined. */
+ * them otherwise.  PDB_ETOOBIG above 1024 slots or 2^21 tokens.  Every wait of the kernel is bounded
+ * (pdb_tokens_set_wait_limit): one that runs out is recorded as PDB_ETIMEOUT, ends the call's work on further rows of the
+ * same blocks, and leaves loss and dlogits undefined. */
 int pdb_distill(pdb_tokens *t, const pdb_mat *logits, const pdb_ids *top_ids, const pdb_mat *top_logits,
                 const float *teacher_lse, float temperature, float *loss, const float *weight, const pdb_mat *dlogits,
                 void *stream);

@@ -123,7 +123,8 @@ EXPORTS = ["pdb_build_conflicts", "pdb_conflicts_arrays", "pdb_schedule_build", 
            "pdb_schedule_free", "pdb_strerror", "pdb_memcpy", "pdb_eval_expf", "pdb_eval_grad", "pdb_launch_count",
            "pdb_sgd_epoch_ready_noalloc", "pdb_ssp_epoch", "pdb_bsp_plan_build", "pdb_bsp_plan_batches",
            "pdb_bsp_coef", "pdb_bsp_apply", "pdb_bsp_plan_free",
-           "pdb_tokens_create", "pdb_tokens_free", "pdb_tokens_status", "pdb_embed", "pdb_embed_grad", "pdb_logprobs",
+           "pdb_tokens_create", "pdb_tokens_free", "pdb_tokens_status",
+           "pdb_tokens_set_wait_limit", "pdb_embed", "pdb_embed_grad", "pdb_logprobs",
            "pdb_logprobs_grad", "pdb_distill"]
 
 
@@ -169,6 +170,7 @@ def load(path: str | None = None):
         lib.pdb_tokens_free.argtypes = [P]
         lib.pdb_tokens_free.restype = None
         lib.pdb_tokens_status.argtypes = [P, P]
+        lib.pdb_tokens_set_wait_limit.argtypes = [P, I64]
         lib.pdb_embed.argtypes = [P, M, J, F32, I64, M, P]
         lib.pdb_embed_grad.argtypes = [P, J, M, F32, I64, I32, M, P]
         lib.pdb_logprobs.argtypes = [P, M, J, F32, I64, P, P, P, I64, P, P, P]
@@ -581,6 +583,11 @@ def pdb_tokens_status(tok: Tokens, stream=None) -> int:
     """Synchronize the stream and return the first error a kernel recorded in tok
     (PDB_ERANGE: an id out of range; PDB_OK when none)."""
     return int(load().pdb_tokens_status(tok.handle, _stream(stream)))
+
+
+def pdb_tokens_set_wait_limit(tok: Tokens, tries: int):
+    """Tries of a device-side wait in later calls on tok (0: none, every such call ends with PDB_ETIMEOUT)."""
+    _check(load().pdb_tokens_set_wait_limit(tok.handle, tries), "pdb_tokens_set_wait_limit")
 
 
 def pdb_embed(tok: Tokens, table, ids, out, scale: float = 1.0, pad: int = -1, stream=None):

@@ -260,19 +260,26 @@ struct Row {
         }
     }
     // the same without a barrier of the cluster, which would wait for the stores of the row before: every block sends its
-    // numbers to every block, 16 bytes each, that complete on `bar`; `own` holds 4 * MAX_CLUSTER floats
+    // numbers to every block, 16 bytes each, that complete on `bar`; `own` holds 4 * MAX_CLUSTER floats.  With them goes
+    // whether a wait of the block has run out, so that all blocks stop after the same row, with no numbers on their way;
+    // true then
     template <typename In>
-    __device__ __forceinline__ void exchange(In &in, int blocks, int rank, float c, float *own, uint64_t *bar, unsigned parity)
+    __device__ __forceinline__ bool exchange(In &in, int blocks, int rank, float c, float *own, uint64_t *bar, unsigned parity,
+                                             bool stop)
     {
         if (threadIdx.x == 0) bar_expect(bar, 16 * blocks);
-        if ((int)threadIdx.x < blocks) send_async(own + 4 * rank, bar, threadIdx.x, a.m, a.s, repeated ? 1.0f : 0.0f, 0.0f);
-        in.wait(bar, parity);
+        if ((int)threadIdx.x < blocks)
+            send_async(own + 4 * rank, bar, threadIdx.x, a.m, a.s, repeated ? 1.0f : 0.0f, stop ? 1.0f : 0.0f);
+        in.wait_blocks(bar, parity);
+        stop = in.gave_up;
         a = Stat<false>();
 #pragma unroll 1
         for (int b = 0; b < blocks; ++b) {
             a.join(own[4 * b], own[4 * b + 1], 0.0f, c);
             repeated |= own[4 * b + 2] != 0.0f;
+            stop |= own[4 * b + 3] != 0.0f;
         }
+        return stop;
     }
     // sums over the slots: the teacher's weights and, with the bucket, the student's exponentials; `part` holds 64 floats;
     // one barrier
@@ -423,7 +430,7 @@ template <typename T, bool BUCKET, int THREADS>
 __global__ __launch_bounds__(THREADS + 32, blocks_per_sm(THREADS)) void k_distill_grad(
     const T *logits, int64_t rows, int cols, int64_t stride, Teacher teach, float temperature, float *loss,
     const float *__restrict__ weight, T *dlogits, int64_t out_stride, int slots, int hold, int map_bytes, int bit_bytes,
-    int *status)
+    unsigned tries, int *status)
 {
     constexpr int E = Vec<T>::E;
     constexpr uint32_t NEG_INF = Vec<T>::NEG_INF;
@@ -433,6 +440,7 @@ __global__ __launch_bounds__(THREADS + 32, blocks_per_sm(THREADS)) void k_distil
     __shared__ float part[2][192], part2[2][64];
     __shared__ __align__(16) float own[2][4 * MAX_CLUSTER];
     __shared__ int twice[2];
+    __shared__ int stopped;             // a wait has run out: the row under work is the last
     __shared__ unsigned edge_map[2];
     __shared__ uint64_t bars[2 * MOST_SLOTS], joined[2];
     const int K = teach.K;
@@ -444,10 +452,12 @@ __global__ __launch_bounds__(THREADS + 32, blocks_per_sm(THREADS)) void k_distil
 
     if (threadIdx.x == 0) bar_init(&joined[0], 1), bar_init(&joined[1], 1);
     In in;
-    in.start(reinterpret_cast<uint4 *>(reinterpret_cast<unsigned char *>(map) + map_bytes), bars, slots, hold, status);
+    in.start(reinterpret_cast<uint4 *>(reinterpret_cast<unsigned char *>(map) + map_bytes), bars, slots, hold, tries,
+             status);
 #pragma unroll 1
     for (int i = threadIdx.x; i < map_bytes / 16; i += THREADS + 32) reinterpret_cast<uint4 *>(map)[i] = uint4{0, 0, 0, 0};
     if (threadIdx.x < 2) twice[threadIdx.x] = 0, edge_map[threadIdx.x] = 0;
+    if (threadIdx.x == 0) stopped = 0;
 
     if (blocks > 1) cluster.sync();     // every block's barriers are there
     else __syncthreads();               // the map is clear
@@ -514,8 +524,9 @@ __global__ __launch_bounds__(THREADS + 32, blocks_per_sm(THREADS)) void k_distil
 
     int turn = 0;
     unsigned joins = 0;                 // rows joined so far
+    bool stop = false;                  // the same on all threads, and with the blocks' exchange on all blocks
 #pragma unroll 1
-    for (int64_t r = first; r < rows; r += step, turn ^= 1) {
+    for (int64_t r = first; r < rows && !stop; r += step, turn ^= 1) {
         team_sync<THREADS>();           // the marks are set; the row before is written
         if (threadIdx.x == 0) twice[turn ^ 1] = 0, edge_map[turn ^ 1] = 0;
         if (r != first) write_slots(r - step, turn ^ 1);
@@ -558,11 +569,15 @@ __global__ __launch_bounds__(THREADS + 32, blocks_per_sm(THREADS)) void k_distil
             R.peak_z = fmaxf(R.peak_z, z);
             if (BUCKET) R.template add_around<T>(S, marks, sh, k, around, c);
         }
+        if (in.gave_up) stopped = 1;
         R.template join<THREADS>(c, K, part[turn]);
 #pragma unroll 1
         for (int k = threadIdx.x; k < K; k += THREADS) marks.clear<E>(sh, S.id[k]);          // for the next row
-        if (blocks > 1) R.exchange(in, blocks, rank, c, own[turn], &joined[turn], joins++ >> 1 & 1);
+        if (blocks > 1 &&
+            R.exchange(in, blocks, rank, c, own[turn], &joined[turn], joins++ >> 1 & 1, *(volatile int *)&stopped != 0))
+            stopped = 1;
         R.template sum_slots<THREADS>(S, K, lse, c, part2[turn]);
+        stop = *(volatile int *)&stopped != 0;      // not written again before the next row's first barrier
         if (loss && rank == 0 && threadIdx.x >= THREADS - 32) {
             const float value = R.loss(S, K, temperature, inv);
             if (threadIdx.x == THREADS - 1) loss[r] = value;
@@ -632,7 +647,7 @@ __global__ __launch_bounds__(THREADS + 32, blocks_per_sm(THREADS)) void k_distil
         }
     }
     team_sync<THREADS>();
-    if (first < rows) {
+    if (first < rows && !stop) {
         const int64_t last = first + (rows - 1 - first) / step * step;
         write_slots(last, turn ^ 1);
     }
@@ -712,7 +727,7 @@ extern "C" int pdb_distill(pdb_tokens *t, const pdb_mat *logits, const pdb_ids *
             return launch_rows(teacher_lse ? k_distill_grad<T, true, N> : k_distill_grad<T, false, N>, shape, s,
                                (const T *)logits->data, logits->rows, (int)logits->cols, stride_of(logits), teach,
                                temperature, loss, weight, (T *)dlogits->data, stride_of(dlogits), shape.slots, shape.hold,
-                               shape.map_bytes, shape.bit_bytes, t->status);
+                               shape.map_bytes, shape.bit_bytes, t->tries, t->status);
         };
         return shape.threads == 64 ? run(Num<64>()) : shape.threads == 128 ? run(Num<128>()) : run(Num<256>());
     });

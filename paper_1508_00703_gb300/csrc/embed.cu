@@ -634,6 +634,7 @@ int pdb_tokens_create(int64_t max_tokens, int64_t max_dim, pdb_tokens **out, voi
     t->sms = l.sms;
     t->max_tokens = max_tokens;
     t->max_dim = max_dim;
+    t->tries = WAIT_TRIES;
     int rc = cudaEventCreateWithFlags(&t->ev_use, cudaEventDisableTiming) == cudaSuccess ? PDB_OK : PDB_ECUDA;
     const size_t words = sizeof(uint32_t) * max_tokens, radix = max_tokens > SORT_MAX ? words : 0;   // of the radix sort only
     rc = rc ? rc : alloc_block(t->arrays, {{(void **)&t->status, 3 * sizeof(int)},
@@ -664,6 +665,13 @@ int pdb_tokens_status(const pdb_tokens *t, void *stream)
     int st = 0;
     if (read_words(&st, t->status, sizeof(int), (cudaStream_t)stream) != PDB_OK) return PDB_ECUDA;
     return st;
+}
+
+int pdb_tokens_set_wait_limit(pdb_tokens *t, int64_t tries)
+{
+    if (!t || tries < 0 || tries > (int64_t)1 << 30) return PDB_EINVAL;
+    t->tries = (unsigned)tries;
+    return PDB_OK;
 }
 
 int pdb_embed(pdb_tokens *t, const pdb_mat *table, const pdb_ids *ids, float scale, int64_t pad, const pdb_mat *out,

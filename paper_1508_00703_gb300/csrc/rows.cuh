@@ -383,6 +383,7 @@ __device__ __forceinline__ void block_join(Stat<ENT> &a, float c, float *part)
 }
 
 constexpr int MOST_SLOTS = 16;
+constexpr unsigned WAIT_TRIES = 1u << 22;   // of a wait, unless the handle has another limit; one takes some 20 ns to a microsecond
 
 // One block's shares of its cluster's rows, chunk after chunk of SPAN = THREADS * UNROLL vectors, each row twice.
 // A warp of its own brings the chunks by bulk copies into `slots` places, in turn (issued by one of the reading threads
@@ -390,33 +391,49 @@ constexpr int MOST_SLOTS = 16;
 // when each of the THREADS / 32 other warps has given it back.  A row's last `hold` chunks stay in their places after the
 // first visit and come again from there; the ones before are brought once more, after the held ones (L2 has seen them
 // a few microseconds ago).  Every wait has a limit, after which the status word holds PDB_ETIMEOUT and no
-// wait of the thread waits again.
+// wait of the thread waits again.  A reader that has given up gives no place back; so the bringing thread runs out of
+// places and of its own tries, brings nothing more, and waits for what it has under way before it ends.
 template <typename T, int THREADS>
 struct Stream {
     static constexpr int SPAN = THREADS * UNROLL;
-    static constexpr unsigned LIMIT = 1u << 22;     // tries; one takes some 20 ns to a microsecond
+    static constexpr unsigned LIMIT = WAIT_TRIES;
     uint4 *place;                       // slots * SPAN vectors
     uint64_t *full, *empty;             // a barrier for each place
     int *status;
     int slots, hold;
     int slot;                           // the next place to take or to fill
     unsigned parity;                    // its full barrier's
+    unsigned tries;                     // of a wait
     bool gave_up;
 
+    // whether it is done after so many tries
+    __device__ __forceinline__ bool tried(uint64_t *bar, unsigned par, unsigned n)
+    {
+#pragma unroll 1
+        for (unsigned i = 0; i < n; ++i)
+            if (bar_done(bar, par)) return true;
+        set_status(status, PDB_ETIMEOUT);
+        return false;
+    }
     __device__ __forceinline__ void wait(uint64_t *bar, unsigned par)
     {
         if (bar_done(bar, par) || gave_up) return;
-#pragma unroll 1
-        for (unsigned i = 0; i < LIMIT; ++i)
-            if (bar_done(bar, par)) return;
-        set_status(status, PDB_ETIMEOUT);
-        gave_up = true;
+        gave_up = !tried(bar, par, tries);
     }
-    // `bars` holds 2 * MOST_SLOTS barriers; a barrier of the block follows before the first use
-    __device__ __forceinline__ void start(uint4 *place_, uint64_t *bars, int slots_, int hold_, int *status_)
+    // A wait for the cluster's other blocks, each of which sends its numbers once it has done with its own waits, given up
+    // or not: these must not be left out, so the limit is one that no run of another block's tries reaches
+    __device__ __forceinline__ void wait_blocks(uint64_t *bar, unsigned par)
+    {
+        if (bar_done(bar, par)) return;
+        gave_up |= !tried(bar, par, 4 * LIMIT);
+    }
+    // `bars` holds 2 * MOST_SLOTS barriers; a barrier of the block follows before the first use.  Without a try (tries_ == 0)
+    // the readers have given up before they start; the bringing thread has more tries than they have
+    __device__ __forceinline__ void start(uint4 *place_, uint64_t *bars, int slots_, int hold_, unsigned tries_, int *status_)
     {
         place = place_, full = bars, empty = bars + MOST_SLOTS, status = status_, slots = slots_, hold = hold_;
-        slot = 0, parity = 0, gave_up = false;
+        slot = 0, parity = 0, tries = threadIdx.x < THREADS ? tries_ : tries_ + 1024, gave_up = tries == 0;
+        if (gave_up) set_status(status, PDB_ETIMEOUT);
         if (threadIdx.x == 0) {
 #pragma unroll 1
             for (int i = 0; i < slots; ++i) {
@@ -439,17 +456,18 @@ struct Stream {
     {
         int brought = 0;
 #pragma unroll 1
-        for (int64_t r = first; r < rows; r += step) {
+        for (int64_t r = first; r < rows && !gave_up; r += step) {
             const T *row = logits + r * stride;
             const Share sh = share_of(row, cols, rank, blocks);
             const uint4 *body = reinterpret_cast<const uint4 *>(row + sh.b0);
             const int n_vec = sh.v1 - sh.v0;
             int end = n_vec;
 #pragma unroll 1
-            for (int sweep = 0; sweep < 2; ++sweep) {
+            for (int sweep = 0; sweep < 2 && !gave_up; ++sweep) {
 #pragma unroll 1
                 for (int v = 0; v < end || (sweep == 0 && v == 0); v += SPAN) {
                     wait(empty + slot, parity ^ 1);         // a place never used is free
+                    if (gave_up) break;                     // it may still be in use, its copy under way
                     const int n = min(SPAN, end - v);
                     bar_expect(full + slot, n * 16);
                     if (n > 0) bulk_copy(place + slot * SPAN, body + v, n * 16, full + slot);
@@ -459,12 +477,12 @@ struct Stream {
                 end = passing(n_vec) * SPAN;                // the passing chunks once more
             }
         }
-        // nothing is under way when the block ends, whatever became of the other warps
+        // nothing is under way when the block ends, whatever became of the other warps and of the waits above
 #pragma unroll 1
         for (int i = 0; i < min(slots, brought); ++i) {
             if (slot == 0) slot = slots, parity ^= 1;
             --slot;
-            wait(full + slot, parity);
+            tried(full + slot, parity, LIMIT);
         }
     }
     // the next chunk's place, once it is there
@@ -488,11 +506,11 @@ struct Stream {
     }
     // the place of the chunk taken n takes ago
     __device__ __forceinline__ int before(int n) const { return slot - n < 0 ? slot - n + slots : slot - n; }
-    // this warp has done with place p
+    // this warp has done with place p; not after a wait that ran out, behind which a copy may be under way to any place
     __device__ __forceinline__ void give_back(int p)
     {
         __syncwarp();
-        if ((threadIdx.x & 31) == 0) bar_arrive(empty + p);
+        if ((threadIdx.x & 31) == 0 && !gave_up) bar_arrive(empty + p);
     }
 };
 

@@ -11,6 +11,7 @@ struct pdb_tokens {
     int device, sms;
     int room[4][4];            // clusters of 1, 2, 4, 8 blocks that run at once: blocks of 256, 128, 64, one an SM (distill.cu)
     int64_t max_tokens, max_dim;
+    unsigned tries;            // of a wait of k_distill_grad
     int *status;               // device: [0] first error recorded by a kernel; [1] always 0 (the radix
                                // sort's kernels return at once when their status word is set); [2] long runs (embed.cu)
     uint32_t *skey;            // [max_tokens] ids as sort keys in sorted order
