@@ -548,7 +548,8 @@ int pdb_logprobs_grad(pdb_tokens *t, const pdb_mat *logits, const pdb_ids *ids, 
  * recorded as PDB_ERANGE.  Slots of one token add up in q (a teacher that lists a token
  * twice).  A row without slots, or whose slots all hold -inf, has loss 0 and
  * gradient 0; a row of weight 0 has gradient 0, whatever it holds; a row of logits with
- * nothing but -inf has loss +inf and gradient 0.  A NaN in a row makes its loss and gradient NaN.
+ * nothing but -inf has loss +inf and gradient 0 whatever its teacher logits hold.  Else a NaN in a row's logits or in its slots' teacher logits makes its
+ * loss and all of its gradient NaN.
  * dlogits may be the logits' own memory (same data, stride and type); it must not overlap
  * them otherwise.  PDB_ETOOBIG above 1024 slots or 2^21 tokens.  Every wait of the kernel is bounded
  * (pdb_tokens_set_wait_limit): one that runs out is recorded as PDB_ETIMEOUT, ends the call's work on further rows of the

@@ -586,9 +586,13 @@ __global__ __launch_bounds__(THREADS + 32, blocks_per_sm(THREADS)) void k_distil
         // own maximum, so that neither p_j nor p_t need be representable.
         zero = w_own == 0.0f || !R.live || R.s == 0.0f;
         wt = __fmul_rn(w_own, temperature);
-        one = __fdiv_rn(1.0f, R.s);
+        // A NaN among the student's logits or the teacher's is one in the whole row: the teacher's shows in the rest or in the
+        // slots' sum alone, and one in a slot not outside of the slots where nothing is left there
+        const float known = __fadd_rn(R.s, BUCKET ? R.rest : R.logt);
+        one = known != known ? known : __fdiv_rn(1.0f, R.s);
         const float factor =
-            BUCKET ? (R.a.s == 0.0f ? 0.0f : __fmul_rn(wt, __fsub_rn(__fmul_rn(R.lift, one), __fdiv_rn(R.rest, R.a.s))))
+            BUCKET ? (R.a.s == 0.0f ? __fmul_rn(0.0f, one)
+                                    : __fmul_rn(wt, __fsub_rn(__fmul_rn(R.lift, one), __fdiv_rn(R.rest, R.a.s))))
                    : __fmul_rn(wt, one);
         T *drow = dlogits + r * out_stride, *dbody = drow + sh.b0;
         if (has_edge) {
