@@ -320,9 +320,35 @@ __global__ __launch_bounds__(THREADS, 1024 / THREADS) void k_logprobs(const T *_
         }
 }
 
+// m and s (rows.cuh) of a whole row, on every thread of the block; `part` holds 96 floats
+template <typename T, int THREADS>
+__device__ __noinline__ float2 row_statistics(const T *row, int cols, float c, float *part)
+{
+    const Share sh = share_of(row, cols, 0, 1);
+    const uint4 *body = reinterpret_cast<const uint4 *>(row + sh.b0);
+    const int n_vec = sh.v1 - sh.v0;
+    Stat<false> a;
+    float unused = 0.0f;
+#pragma unroll 1
+    for (int base = 0; base < n_vec; base += THREADS * UNROLL) {
+        uint4 v[UNROLL];
+        load_vectors<T, THREADS, 32>(v, body, base, lane_start(), n_vec);
+        add_vectors<T, false>(a, v, c, unused);
+    }
+    if ((int)threadIdx.x < sh.edges()) add_element(a, to_float(row[sh.edge(threadIdx.x)]), c);
+    block_join<THREADS>(a, c, part);
+    return {a.m, a.s};
+}
+
 // dlogits = -p (A + B x) (+ scale g at the given token), x = (z - lse / scale) c, p = 2^x,
 // A = scale (g + h entropy), B = scale h ln2.  One pass, every element read and written once: bound by
 // memory.  A block takes one piece of a row; pieces of a row need nothing from one another.
+//
+// lse is rounded to 32 bits, which moves p by 2^-24 |lse|: a row masked by the type's lowest value from end to end would have
+// lse = that value, and p = 1 for all.  From |lse| = 256 on (p good to 2^-15 below), and where lse has left fp32's
+// range, the row's first block alone takes the whole row, with its maximum and sum formed again: x = (z - m) c - log2 s.
+constexpr float FAR_LSE = 256.0f;
+
 template <typename T, int THREADS>
 __global__ __launch_bounds__(THREADS) void k_logprobs_grad(const T *logits, int cols, int64_t stride, int pieces, Ids ids,
                                                            float scale, int64_t ignore, const float *__restrict__ lse,
@@ -333,13 +359,14 @@ __global__ __launch_bounds__(THREADS) void k_logprobs_grad(const T *logits, int 
 {
     after_previous();
     constexpr int E = Vec<T>::E;
+    __shared__ float part[96];
     const int64_t r = blockIdx.x / (unsigned)pieces;
     const int piece = (int)(blockIdx.x - r * pieces);
     const T *row = logits + r * stride;
     T *drow = dlogits + r * out_stride;
-    const Share sh = share_of(row, cols, piece, pieces);
+    Share sh = share_of(row, cols, piece, pieces);
     const uint4 *body = reinterpret_cast<const uint4 *>(row + sh.b0);
-    const int n_vec = sh.v1 - sh.v0;
+    int n_vec = sh.v1 - sh.v0;
     uint4 v[UNROLL];
     load_vectors<T, THREADS, 32>(v, body, 0, lane_start(), n_vec);          // on their way while the row's numbers arrive
 
@@ -354,14 +381,25 @@ __global__ __launch_bounds__(THREADS) void k_logprobs_grad(const T *logits, int 
         else g = 0.0f;
     }
     const float l = lse[r];
-    const bool zero = (g == 0.0f && h == 0.0f) || l == -INFINITY;
+    // up to a scale of 1 no finite logits have an lse of -inf
+    bool zero = (g == 0.0f && h == 0.0f) || (l == -INFINITY && scale <= 1.0f);
     const float H = h != 0.0f ? entropy[r] : 0.0f;
-    const float ref = __fdiv_rn(l, scale), c = __fmul_rn(scale, LOG2E);
+    const float c = __fmul_rn(scale, LOG2E);
+    float ref = __fdiv_rn(l, scale), log2s = 0.0f;
+    if (!zero && !(fabsf(l) < FAR_LSE && fabsf(ref) < INFINITY)) {
+        if (piece != 0) return;
+        const float2 ms = row_statistics<T, THREADS>(row, cols, c, part);
+        ref = ms.x, log2s = log2f(ms.y), zero = ms.y == 0.0f;
+        sh = share_of(row, cols, 0, 1);
+        body = reinterpret_cast<const uint4 *>(row + sh.b0);
+        n_vec = sh.v1 - sh.v0;
+        load_vectors<T, THREADS, 32>(v, body, 0, lane_start(), n_vec);
+    }
     const float A = -__fmul_rn(scale, __fmaf_rn(h, H, g)), B = -__fmul_rn(__fmul_rn(scale, h), LN2);
     const float at_t = __fmul_rn(scale, g);
     auto slope = [&](float z) {
         // x held above -200, where p = 0: B x p of a token masked by -inf is 0
-        const float x = max_nan(__fmul_rn(__fsub_rn(z, ref), c), -200.0f);
+        const float x = max_nan(__fmaf_rn(__fsub_rn(z, ref), c, -log2s), -200.0f);
         return __fmul_rn(ex2(x), __fmaf_rn(B, x, A));
     };
     const bool aligned = ((uintptr_t)(drow + sh.b0) & 15) == 0;
