@@ -35,7 +35,7 @@ constexpr int64_t MAX_COLS = 1 << 21;   // a block's marks then take 72 KB at mo
 // an element of a matrix of any type, fetched and converted in two steps (as fetch_id)
 __device__ __forceinline__ uint32_t fetch_element(const void *p, int type, int64_t i)
 {
-    return type == PDB_TYPE_FLOAT ? __ldg((const uint32_t *)p + i) : (uint32_t)__ldg((const uint16_t *)p + i);
+    return type == PDB_TYPE_FLOAT ? ((const uint32_t *)p)[i] : (uint32_t)((const uint16_t *)p)[i];
 }
 __device__ __forceinline__ float element_of(int type, uint32_t raw)
 {
@@ -335,7 +335,7 @@ struct Row {
 // ------------------------------------------------------------------ the loss alone: a cluster per row
 // Shared memory: the slots, then (bucket) the marks.
 template <typename T, bool BUCKET, int THREADS>
-__global__ __launch_bounds__(THREADS, 1024 / THREADS) void k_distill_loss(const T *__restrict__ logits, int cols,
+__global__ __launch_bounds__(THREADS, 1024 / THREADS) void k_distill_loss(const T *logits, int cols,
                                                                           int64_t stride, Teacher teach, float temperature,
                                                                           float *__restrict__ loss, int map_bytes,
                                                                           int bit_bytes, int *status)
@@ -429,7 +429,7 @@ __global__ __launch_bounds__(THREADS, 1024 / THREADS) void k_distill_loss(const 
 template <typename T, bool BUCKET, int THREADS>
 __global__ __launch_bounds__(THREADS + 32, blocks_per_sm(THREADS)) void k_distill_grad(
     const T *logits, int64_t rows, int cols, int64_t stride, Teacher teach, float temperature, float *loss,
-    const float *__restrict__ weight, T *dlogits, int64_t out_stride, int slots, int hold, int map_bytes, int bit_bytes,
+    const float *weight, T *dlogits, int64_t out_stride, int slots, int hold, int map_bytes, int bit_bytes,
     unsigned tries, int *status)
 {
     constexpr int E = Vec<T>::E;

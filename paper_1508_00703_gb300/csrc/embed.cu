@@ -79,7 +79,7 @@ inline bool fits(const pdb_mat *m, int E)
 constexpr int LOOKUP_UNROLL = 4;
 
 template <typename T, typename O, int E>
-__global__ __launch_bounds__(256) void k_embed(const T *__restrict__ table, int64_t vocab, int64_t stride, Ids ids,
+__global__ __launch_bounds__(256) void k_embed(const T *table, int64_t vocab, int64_t stride, Ids ids,
                                                int64_t n, int dim, int pieces, float scale, int64_t pad,
                                                O *__restrict__ out, int64_t out_stride, int *status)
 {
@@ -370,7 +370,7 @@ __device__ __forceinline__ void write_sum(O *at, const float (&sum)[E], const Pa
 }
 
 // number of sorted keys below v, by the whole warp: 32 probes at a time
-__device__ __forceinline__ int64_t keys_below(const uint32_t *__restrict__ key, int64_t n, uint32_t v)
+__device__ __forceinline__ int64_t keys_below(const uint32_t *key, int64_t n, uint32_t v)
 {
     const int lane = threadIdx.x & 31;
     int64_t lo = 0, hi = n;              // the answer lies in [lo, hi]
@@ -387,7 +387,7 @@ __device__ __forceinline__ int64_t keys_below(const uint32_t *__restrict__ key, 
 
 // zeros in the rows of 32 ids from v0 on that do not occur: every `parts`-th of them from the part-th on
 template <typename O, int E>
-__device__ __forceinline__ void zero_rows(const uint32_t *__restrict__ key, int64_t n, int64_t vocab, int64_t v0,
+__device__ __forceinline__ void zero_rows(const uint32_t *key, int64_t n, int64_t vocab, int64_t v0,
                                           int part, int parts, O *__restrict__ dtable, int64_t stride, int dim)
 {
     const int lane = threadIdx.x & 31;
@@ -417,9 +417,9 @@ __device__ __forceinline__ void zero_rows(const uint32_t *__restrict__ key, int6
 }
 
 template <typename T, typename O, int E, bool ACC>
-__global__ __launch_bounds__(SUM_WARPS * 32, ACC ? 2 : 4) void k_embed_sum(const uint32_t *__restrict__ key,
-                                                              const int32_t *__restrict__ pos, int64_t n, int64_t vocab,
-                                                              const T *__restrict__ dout, int64_t stride, int dim,
+__global__ __launch_bounds__(SUM_WARPS * 32, ACC ? 2 : 4) void k_embed_sum(const uint32_t *key,
+                                                              const int32_t *pos, int64_t n, int64_t vocab,
+                                                              const T *dout, int64_t stride, int dim,
                                                               int tiles, int log_window, int64_t sum_blocks,
                                                               int64_t zero_first, int64_t zero_groups, int log_parts, float scale,
                                                               O *__restrict__ dtable, int64_t out_stride,
@@ -535,9 +535,9 @@ constexpr int JOIN_COLS = 128, JOIN_WARPS = 8;
 // JE: columns that one load brings (4, or 1 where the columns are no multiple of 4)
 template <typename O, int JE, bool ACC>
 __global__ __launch_bounds__(JOIN_WARPS * 32) void k_embed_join(int dim, int tiles, float scale, O *__restrict__ dtable,
-                                                                int64_t out_stride, const float *__restrict__ part,
-                                                                const int *__restrict__ long_runs,
-                                                                const int4 *__restrict__ run_list)
+                                                                int64_t out_stride, const float *part,
+                                                                const int *long_runs,
+                                                                const int4 *run_list)
 {
     after_previous();
     __shared__ float s_sum[JOIN_WARPS][JOIN_COLS];

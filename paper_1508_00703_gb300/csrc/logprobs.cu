@@ -227,7 +227,7 @@ struct LogprobsOut {
 };
 
 template <typename T, bool ENT, bool TOP, int THREADS>
-__global__ __launch_bounds__(THREADS, 1024 / THREADS) void k_logprobs(const T *__restrict__ logits, int cols, int64_t stride, Ids ids,
+__global__ __launch_bounds__(THREADS, 1024 / THREADS) void k_logprobs(const T *logits, int cols, int64_t stride, Ids ids,
                                                       float scale, int64_t ignore, int k, LogprobsOut out, int *status)
 {
     after_previous();
@@ -351,10 +351,10 @@ constexpr float FAR_LSE = 256.0f;
 
 template <typename T, int THREADS>
 __global__ __launch_bounds__(THREADS) void k_logprobs_grad(const T *logits, int cols, int64_t stride, int pieces, Ids ids,
-                                                           float scale, int64_t ignore, const float *__restrict__ lse,
-                                                           const float *__restrict__ entropy,
-                                                           const float *__restrict__ dlogp,
-                                                           const float *__restrict__ dentropy, T *dlogits,
+                                                           float scale, int64_t ignore, const float *lse,
+                                                           const float *entropy,
+                                                           const float *dlogp,
+                                                           const float *dentropy, T *dlogits,
                                                            int64_t out_stride, int *status)
 {
     after_previous();

@@ -342,7 +342,7 @@ __device__ __forceinline__ int lane_start() { return (int)(threadIdx.x & ~31u) *
 
 // a thread's vectors of the chunk at `base` of a share of `end` vectors, -inf past it: `first`, and every STEP-th
 template <typename T, int THREADS, int STEP>
-__device__ __forceinline__ void load_vectors(uint4 (&v)[UNROLL], const uint4 *__restrict__ share, int base, int first, int end)
+__device__ __forceinline__ void load_vectors(uint4 (&v)[UNROLL], const uint4 *share, int base, int first, int end)
 {
     constexpr uint32_t N = Vec<T>::NEG_INF;
     const uint4 *from = share + base + first;

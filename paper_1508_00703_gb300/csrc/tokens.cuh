@@ -105,7 +105,7 @@ inline bool same_or_apart(const pdb_mat *a, const pdb_mat *b)
 __device__ __forceinline__ int64_t load_id(Ids ids, int64_t i, int k = 0)
 {
     const int64_t at = i * ids.stride + k;
-    return ids.wide ? (int64_t)__ldg((const long long *)ids.data + at) : (int64_t)__ldg((const int *)ids.data + at);
+    return ids.wide ? ((const int64_t *)ids.data)[at] : (int64_t)((const int *)ids.data)[at];
 }
 
 // the same in two steps, so that the warp does not wait for the load before it needs the id
@@ -114,8 +114,8 @@ __device__ __forceinline__ int2 fetch_id(Ids ids, int64_t i, int k = 0)
     const int64_t at = i * ids.stride + k;
     // (volatile: several of them are issued before the first is used)
     int2 raw = {0, 0};
-    if (ids.wide) asm volatile("ld.global.nc.v2.b32 {%0, %1}, [%2];" : "=r"(raw.x), "=r"(raw.y) : "l"((const int2 *)ids.data + at));
-    else asm volatile("ld.global.nc.b32 %0, [%1];" : "=r"(raw.x) : "l"((const int *)ids.data + at));
+    if (ids.wide) asm volatile("ld.global.v2.b32 {%0, %1}, [%2];" : "=r"(raw.x), "=r"(raw.y) : "l"((const int2 *)ids.data + at));
+    else asm volatile("ld.global.b32 %0, [%1];" : "=r"(raw.x) : "l"((const int *)ids.data + at));
     return raw;
 }
 __device__ __forceinline__ int64_t id_of(Ids ids, int2 raw)
@@ -139,6 +139,9 @@ __device__ __forceinline__ __half from_float<__half>(float v) { return __float2h
 // Every kernel of the token operators starts with this: it is launched while the kernel before it in the stream still
 // runs (launch below), and waits here until that one has ended and its writes are visible.  Takes the launch's latency out
 // of a sequence of calls (500 x 256 gradient, three kernels: 16.4 us a call -> 10.7).
+// What these kernels read is read by plain loads: the read-only ones (.nc, __ldg, what the compiler makes of a
+// const __restrict__ parameter) are for data that nobody writes while the kernel lives, and it lives while the kernel
+// before it still writes; the compiler may also move them over the wait.
 __device__ __forceinline__ void after_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 // lets the next kernel of the stream take its place on the SMs now (it waits for this one's end all the same)
 __device__ __forceinline__ void let_next_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
