@@ -5,6 +5,8 @@
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
+#include <algorithm>
+
 #include "common.cuh"
 
 struct pdb_tokens {
@@ -84,14 +86,35 @@ inline Ids ids_of(const pdb_ids *ids, bool given = true)
 // stride of a matrix whose stride may be unset (fewer than two rows)
 inline int64_t stride_of(const pdb_mat *m) { return m->rows > 1 ? m->stride : m->cols; }
 
-// whether two matrices share memory
+// whether `bytes` bytes at p share memory with rows of m
+inline bool meets_rows(const char *p, int64_t bytes, const pdb_mat *m)
+{
+    const int64_t width = m->cols * type_bytes(m->type), step = stride_of(m) * type_bytes(m->type);
+    // the first row that ends behind p is the one to look at
+    const int64_t from = p - (const char *)m->data - width;
+    const int64_t row = from < 0 ? 0 : from / step + 1;
+    return row < m->rows && (const char *)m->data + row * step < p + bytes;
+}
+
+// whether two matrices share memory; rows of the one may lie between rows of the other
 inline bool overlap(const pdb_mat *a, const pdb_mat *b)
 {
     if (a->rows == 0 || b->rows == 0 || a->cols == 0 || b->cols == 0) return false;
     const char *a0 = (const char *)a->data, *b0 = (const char *)b->data;
-    const char *a1 = a0 + ((a->rows - 1) * stride_of(a) + a->cols) * type_bytes(a->type);
-    const char *b1 = b0 + ((b->rows - 1) * stride_of(b) + b->cols) * type_bytes(b->type);
-    return a0 < b1 && b0 < a1;
+    const int64_t sa = stride_of(a) * type_bytes(a->type), sb = stride_of(b) * type_bytes(b->type);
+    const int64_t wa = a->cols * type_bytes(a->type), wb = b->cols * type_bytes(b->type);
+    if (a0 + (a->rows - 1) * sa + wa <= b0 || b0 + (b->rows - 1) * sb + wb <= a0) return false;
+    if (a->rows > 1 && b->rows > 1 && sa == sb) {
+        // row i of a against row j of b: k = i - j decides, and any k of the range that lies where they meet
+        const int64_t d = b0 - a0;
+        const auto down = [&](int64_t x) { return x >= 0 ? x / sa : -((-x + sa - 1) / sa); };
+        const int64_t first = std::max(down(d - wa) + 1, 1 - b->rows), last = std::min(-down(-(d + wb)) - 1, a->rows - 1);
+        return first <= last;
+    }
+    const pdb_mat *few = a->rows <= b->rows ? a : b, *other = few == a ? b : a;
+    for (int64_t i = 0; i < few->rows; ++i)
+        if (meets_rows((const char *)few->data + i * (few == a ? sa : sb), few == a ? wa : wb, other)) return true;
+    return false;
 }
 
 // a result that may be written over its input: the same matrix, or one apart
