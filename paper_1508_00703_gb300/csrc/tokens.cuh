@@ -51,6 +51,9 @@ int count_room(pdb_tokens *t);
 
 inline int type_bytes(int type) { return type == PDB_TYPE_FLOAT ? 4 : 2; }
 
+// elements from the first row's start to the last one's: what any memory holds, and far from the 64-bit range's end
+constexpr int64_t MOST_EXTENT = (int64_t)1 << 58;
+
 // PDB_OK for a matrix that the calls accept
 inline int check_mat(const pdb_mat *m)
 {
@@ -59,6 +62,7 @@ inline int check_mat(const pdb_mat *m)
     if (m->rows > 1 && m->stride < m->cols) return PDB_EINVAL;
     if (m->rows > 0 && m->cols > 0 && (!m->data || (uintptr_t)m->data % type_bytes(m->type) != 0)) return PDB_EINVAL;
     if (m->cols > INT32_MAX / 2 || m->rows > INT32_MAX) return PDB_ETOOBIG;
+    if (m->rows > 1 && m->stride > MOST_EXTENT / (m->rows - 1)) return PDB_EINVAL;
     return PDB_OK;
 }
 
@@ -68,6 +72,7 @@ inline int check_ids(const pdb_ids *ids, int64_t n, int64_t k = 1)
     if (!ids || ids->n != n * k) return PDB_EINVAL;
     if (n > 1 && ids->stride < k) return PDB_EINVAL;
     if (n * k > 0 && (!ids->data || (uintptr_t)ids->data % (ids->wide ? 8 : 4) != 0)) return PDB_EINVAL;
+    if (n > 1 && ids->stride > MOST_EXTENT / (n - 1)) return PDB_EINVAL;
     return PDB_OK;
 }
 

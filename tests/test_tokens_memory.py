@@ -1,5 +1,5 @@
 """Where matrices of the token operators lie, as far as refusals show it without a GPU: matrices that share
-memory are refused however their rows lie to one another."""
+memory are refused however their rows lie to one another, and so are extents that no memory holds."""
 import ctypes
 import random
 
@@ -52,3 +52,17 @@ def test_shared_memory_is_refused(lib, handle):
         ids = pdb.pdb_ids(4096, b.rows, 1, 0)
         assert lib.pdb_embed(handle, a, ids, 1.0, -1, b, None) == pdb.PDB_EINVAL
         assert lib.pdb_embed_grad(handle, ids, b, 1.0, -1, 0, a, None) == pdb.PDB_EINVAL
+
+
+@pytest.mark.parametrize("rows,stride", [(2, (1 << 63) - 1), (5, 1 << 61), (1 << 30, 1 << 33), ((1 << 31) - 1, 1 << 40)])
+def test_extents_past_any_memory(lib, handle, rows, stride):
+    i, f = pdb.pdb_ids(4096, rows, 1, 0), 4096
+    far, near = pdb.pdb_mat(BASE, rows, 4, stride, 0), pdb.pdb_mat(BASE, rows, 4, 4, 0)
+    for rc in [lib.pdb_embed(handle, far, i, 1.0, -1, near, None), lib.pdb_embed(handle, near, i, 1.0, -1, far, None),
+               lib.pdb_embed_grad(handle, i, far, 1.0, -1, 0, near, None),
+               lib.pdb_logprobs(handle, far, i, 1.0, -100, f, f, f, 0, None, None, None),
+               lib.pdb_logprobs_grad(handle, near, i, 1.0, -100, f, f, f, f, far, None),
+               lib.pdb_distill(handle, near, pdb.pdb_ids(4096, rows * 4, 4, 0), far, None, 1.0, f, None, None, None)]:
+        assert rc == pdb.PDB_EINVAL
+    ids = pdb.pdb_ids(4096, rows, stride, 0)
+    assert lib.pdb_logprobs(handle, near, ids, 1.0, -100, f, f, f, 0, None, None, None) == pdb.PDB_EINVAL
