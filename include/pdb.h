@@ -501,7 +501,7 @@ int pdb_embed(pdb_tokens *t, const pdb_mat *table, const pdb_ids *ids, float sca
 int pdb_embed_grad(pdb_tokens *t, const pdb_ids *ids, const pdb_mat *dout, float scale, int64_t pad, int accumulate,
                    const pdb_mat *dtable, void *stream);
 
-/* Per row of logits (z = scale * logits, scale > 0 the inverse temperature,
+/* Per row of logits (z = scale * logits, scale > 0 the inverse temperature, at most 2.3e38,
  * p = softmax of z):
  *   lse[r]      log sum_j exp z_j
  *   logp[r]     z_t - lse, t = ids[r]
@@ -532,7 +532,7 @@ int pdb_logprobs_grad(pdb_tokens *t, const pdb_mat *logits, const pdb_ids *ids, 
 /* Distillation from a teacher's top logits: row r of the student's logits
  * against K = top_logits->cols teacher logits (K <= 1024), slot k being token
  * top_ids->data[r * top_ids->stride + k]: here n = rows * K and stride, at least K,
- * is that of the rows.  With T = temperature > 0, p = softmax of logits[r] / T:
+ * is that of the rows.  With T = temperature > 0 (from 4.3e-39 to 1.8e19), p = softmax of logits[r] / T:
  *   teacher_lse == NULL   q_k = softmax of top_logits[r] / T over the row's slots
  *     loss[r] = T^2 * sum_k q_k (log q_k - log p_k)
  *   else   teacher_lse[r] = log sum exp of ALL the teacher's logits / T,

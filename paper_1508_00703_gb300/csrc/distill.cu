@@ -701,7 +701,7 @@ extern "C" int pdb_distill(pdb_tokens *t, const pdb_mat *logits, const pdb_ids *
     rc = rc ? rc : check_ids(top_ids, logits->rows, top_logits->cols);
     if (rc != PDB_OK) return rc;
     if (top_logits->rows != logits->rows || (!loss && !dlogits)) return PDB_EINVAL;
-    if (!(temperature > 0.0f) || std::isinf(temperature)) return PDB_EINVAL;
+    if (!(temperature > 0.0f) || !usable_scale(1.0f / temperature) || std::isinf(temperature * temperature)) return PDB_EINVAL;
     if (dlogits && (dlogits->rows != logits->rows || dlogits->cols != logits->cols || dlogits->type != logits->type ||
                     !same_or_apart(logits, dlogits)))
         return PDB_EINVAL;

@@ -449,7 +449,7 @@ int pdb_logprobs(pdb_tokens *t, const pdb_mat *logits, const pdb_ids *ids, float
     int rc = check_mat(logits);
     if (rc == PDB_OK && logp) rc = check_ids(ids, logits->rows);
     if (rc != PDB_OK) return rc;
-    if (!(scale > 0.0f) || std::isinf(scale) || k < 0 || k > logits->cols) return PDB_EINVAL;
+    if (!usable_scale(scale) || k < 0 || k > logits->cols) return PDB_EINVAL;
     if (k > MAX_TOP) return PDB_ETOOBIG;
     if (logits->rows == 0) return PDB_OK;
     cudaStream_t s = (cudaStream_t)stream;
@@ -479,7 +479,7 @@ int pdb_logprobs_grad(pdb_tokens *t, const pdb_mat *logits, const pdb_ids *ids, 
     rc = rc ? rc : check_mat(dlogits);
     if (rc == PDB_OK && dlogp) rc = check_ids(ids, logits->rows);
     if (rc != PDB_OK) return rc;
-    if (!(scale > 0.0f) || std::isinf(scale)) return PDB_EINVAL;
+    if (!usable_scale(scale)) return PDB_EINVAL;
     if (dlogits->rows != logits->rows || dlogits->cols != logits->cols || dlogits->type != logits->type ||
         !same_or_apart(logits, dlogits))
         return PDB_EINVAL;

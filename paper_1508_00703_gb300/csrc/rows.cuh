@@ -19,6 +19,7 @@
 #include <cooperative_groups.h>
 
 #include <algorithm>
+#include <cmath>
 
 #include "tokens.cuh"
 
@@ -27,6 +28,9 @@ namespace pdb {
 constexpr int UNROLL = 4;               // vectors of a thread under way in registers
 constexpr int MAX_CLUSTER = 8;
 constexpr float LOG2E = 1.44269504088896340736f, LN2 = 0.69314718055994530942f;
+
+// whether logits can be scaled by it: positive, and c = scale * log2(e) finite (0 * c is 0 then, for the row's maximum)
+inline bool usable_scale(float scale) { return scale > 0.0f && std::isfinite(scale * LOG2E); }
 
 __device__ __forceinline__ float ex2(float x)
 {
