@@ -434,7 +434,7 @@ int pdb_sgd_epoch_ready_noalloc(const pdb_csr *X, const float *y, const uint32_t
  * the status word in which the kernels record an id out of range
  * or an expired wait (pdb_tokens_status).  A recorded error stops no later call: a bad id gives the
  * result its declaration states.  Calls that share a handle must be ordered on
- * one stream.  Sums, softmax statistics and losses are held in fp32; a result
+ * one stream, and made while the device is current that was at pdb_tokens_create (PDB_EINVAL otherwise).  Sums, softmax statistics and losses are held in fp32; a result
  * in 16 bits is rounded once.  No atomics add floating values: the same inputs
  * give the same bits.  No call allocates but pdb_tokens_create (and pdb_embed_grad above
  * 65,536 ids: scratch of the radix sort, stream-ordered from the library's pool); all but

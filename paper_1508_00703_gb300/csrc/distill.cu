@@ -707,6 +707,7 @@ extern "C" int pdb_distill(pdb_tokens *t, const pdb_mat *logits, const pdb_ids *
         return PDB_EINVAL;
     if (logits->cols > MAX_COLS) return PDB_ETOOBIG;
     if (logits->rows == 0) return PDB_OK;
+    if ((rc = check_device(t)) != PDB_OK) return rc;
     cudaStream_t s = (cudaStream_t)stream;
     TokensUse use{t, s};
     const Teacher teach{ids_of(top_ids), top_logits->data, top_logits->type, (int)top_logits->cols, stride_of(top_logits),

@@ -662,6 +662,7 @@ int pdb_tokens_create(int64_t max_tokens, int64_t max_dim, pdb_tokens **out, voi
 int pdb_tokens_status(const pdb_tokens *t, void *stream)
 {
     if (!t) return PDB_EINVAL;
+    if (const int rc = check_device(t)) return rc;
     int st = 0;
     if (read_words(&st, t->status, sizeof(int), (cudaStream_t)stream) != PDB_OK) return PDB_ECUDA;
     return st;
@@ -685,6 +686,7 @@ int pdb_embed(pdb_tokens *t, const pdb_mat *table, const pdb_ids *ids, float sca
     if (rc != PDB_OK) return rc;
     if (table->cols != out->cols || overlap(table, out)) return PDB_EINVAL;
     if (out->rows == 0 || out->cols == 0) return PDB_OK;
+    if ((rc = check_device(t)) != PDB_OK) return rc;
     cudaStream_t s = (cudaStream_t)stream;
     TokensUse use{t, s};
     const auto run = [&](auto *a, auto *b, auto e) {
@@ -722,6 +724,7 @@ int pdb_embed_grad(pdb_tokens *t, const pdb_ids *ids, const pdb_mat *dout, float
     const int64_t n = dout->rows, vocab = dtable->rows;
     const int dim = (int)dout->cols;
     if (vocab == 0 && n == 0) return PDB_OK;
+    if ((rc = check_device(t)) != PDB_OK) return rc;
     cudaStream_t s = (cudaStream_t)stream;
     TokensUse use{t, s};
     // What the sort leaves idle writes zeros: about as many bytes as go to memory in its time (the 25 us of 65,536 ids: 148 us

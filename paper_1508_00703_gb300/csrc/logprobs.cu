@@ -452,6 +452,7 @@ int pdb_logprobs(pdb_tokens *t, const pdb_mat *logits, const pdb_ids *ids, float
     if (!usable_scale(scale) || k < 0 || k > logits->cols) return PDB_EINVAL;
     if (k > MAX_TOP) return PDB_ETOOBIG;
     if (logits->rows == 0) return PDB_OK;
+    if ((rc = check_device(t)) != PDB_OK) return rc;
     cudaStream_t s = (cudaStream_t)stream;
     TokensUse use{t, s};
     const bool top = k > 0 && (top_logp || top_ids);
@@ -485,6 +486,7 @@ int pdb_logprobs_grad(pdb_tokens *t, const pdb_mat *logits, const pdb_ids *ids, 
         return PDB_EINVAL;
     if (logits->rows == 0 || logits->cols == 0) return PDB_OK;
     if (!lse || (dentropy && !entropy)) return PDB_EINVAL;
+    if ((rc = check_device(t)) != PDB_OK) return rc;
     cudaStream_t s = (cudaStream_t)stream;
     TokensUse use{t, s};
     return with_type(logits->type, [&](auto *a) {

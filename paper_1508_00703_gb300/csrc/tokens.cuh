@@ -49,6 +49,14 @@ bool allow_smem(const void *kernel);
 // fills t->room
 int count_room(pdb_tokens *t);
 
+// PDB_OK where the current device is the handle's
+inline int check_device(const pdb_tokens *t)
+{
+    int device = -1;
+    if (cudaGetDevice(&device) != cudaSuccess) return PDB_ECUDA;
+    return device == t->device ? PDB_OK : PDB_EINVAL;
+}
+
 inline int type_bytes(int type) { return type == PDB_TYPE_FLOAT ? 4 : 2; }
 
 // elements from the first row's start to the last one's: what any memory holds, and far from the 64-bit range's end
