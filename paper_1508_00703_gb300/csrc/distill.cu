@@ -20,6 +20,7 @@
 // than that, the rest is time per row), 1501 x 50,001 fp32 114 us (5.3 TB/s), 3000 x 128,000 fp32 487 us (6.3 TB/s).
 #include <algorithm>
 #include <cmath>
+#include <mutex>
 
 #include "rows.cuh"
 
@@ -660,33 +661,42 @@ __global__ __launch_bounds__(THREADS + 32, blocks_per_sm(THREADS)) void k_distil
 
 }  // namespace
 
-namespace pdb {
+namespace {
 
-// as the device says it: an SM more or less in one of its groups takes more than its share of the larger clusters
-int count_room(pdb_tokens *t)
+// asked at a device's first call with gradient, then kept: 16 queries
+Room room_of(int device, int sms)
 {
+    static std::mutex lock;
+    static bool known[64];
+    static Room rooms[64];
+    std::lock_guard<std::mutex> guard(lock);
+    const bool kept = device >= 0 && device < 64;
+    if (kept && known[device]) return rooms[device];
+    Room room = {};
     const auto kernel = k_distill_grad<__nv_bfloat16, true, 256>;
-    if (!allow_smem((const void *)kernel)) return PDB_ECUDA;
+    if (!allow_smem((const void *)kernel)) return room;
     cudaLaunchAttribute at = {};
     at.id = cudaLaunchAttributeClusterDimension;
     cudaLaunchConfig_t cfg = {};
     cfg.attrs = &at;
     cfg.numAttrs = 1;
-    for (int i = 0; i <= ROOM_ALONE; ++i)
+    for (int i = 0; i <= Room::ALONE; ++i)
         for (int log = 0; log < 4; ++log) {
-            const int threads = i == ROOM_ALONE ? 256 : 256 >> i;
+            const int threads = i == Room::ALONE ? 256 : 256 >> i;
             at.val.clusterDim.x = 1u << log;
             at.val.clusterDim.y = at.val.clusterDim.z = 1;
-            cfg.gridDim = dim3((unsigned)t->sms * 8);
+            cfg.gridDim = dim3((unsigned)sms * 8);
             cfg.blockDim = dim3(threads + 32);
-            cfg.dynamicSmemBytes = block_smem(i == ROOM_ALONE ? 1 : blocks_per_sm(threads));
-            if (cudaOccupancyMaxActiveClusters(&t->room[i][log], kernel, &cfg) != cudaSuccess) return PDB_ECUDA;
-            if (t->room[i][log] < 1) return PDB_ECUDA;
+            cfg.dynamicSmemBytes = block_smem(i == Room::ALONE ? 1 : blocks_per_sm(threads));
+            int n = 0;
+            if (cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) == cudaSuccess) room.clusters[i][log] = n;
+            else cudaGetLastError();
         }
-    return PDB_OK;
+    if (kept && room.clusters[0][0] > 0) rooms[device] = room, known[device] = true;
+    return room;
 }
 
-}  // namespace pdb
+}  // namespace
 
 extern "C" int pdb_distill(pdb_tokens *t, const pdb_mat *logits, const pdb_ids *top_ids, const pdb_mat *top_logits,
                            const float *teacher_lse, float temperature, float *loss, const float *weight,
@@ -725,7 +735,8 @@ extern "C" int pdb_distill(pdb_tokens *t, const pdb_mat *logits, const pdb_ids *
             });
         }
         const size_t slot_bytes = ((size_t)teach.K * SLOT_BYTES * 2 + 15) / 16 * 16;
-        Shape shape = twice_shape(logits->rows, logits->cols, Vec<T>::E, *t, slot_bytes, teach.K);
+        Shape shape = twice_shape(logits->rows, logits->cols, Vec<T>::E, room_of(t->device, t->sms), slot_bytes, teach.K);
+        if (shape.clusters < 1) return PDB_ECUDA;
         const auto run = [&](auto n) {
             constexpr int N = decltype(n)::value;
             shape.threads = N + 32;     // and the warp that brings the rows

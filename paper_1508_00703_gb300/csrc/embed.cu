@@ -647,7 +647,6 @@ int pdb_tokens_create(int64_t max_tokens, int64_t max_dim, pdb_tokens **out, voi
                                            {(void **)&t->part, sizeof(float) * 2 * ((max_tokens + PIECE - 1) / PIECE) * max_dim},
                                            {(void **)&t->run_list, sizeof(int4) * (max_tokens / (PIECE + 1))}}, s);
     rc = rc ? rc : fill_words(t->status, 0u, 3 * sizeof(int), s);
-    rc = rc ? rc : count_room(t);
     if (rc != PDB_OK) {
         cudaGetLastError();
         cudaStreamSynchronize(s);

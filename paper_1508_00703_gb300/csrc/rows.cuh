@@ -569,6 +569,13 @@ constexpr int blocks_per_sm(int threads) { return threads == 64 ? 6 : 512 / thre
 // shared memory of a block where `per` of them share an SM, which keeps 1 KB for each
 constexpr size_t block_smem(int per) { return SMEM_PER_SM / per - 1024 - STATIC_SMEM; }
 
+// Clusters of 1, 2, 4 and 8 blocks of k_distill_grad that run at once on a device (0: none of that size), as the device says it: an SM
+// more or less in one of its groups takes more than its share of the larger clusters.
+struct Room {
+    static constexpr int ALONE = 3;
+    int clusters[4][4];                 // by blocks of 256, 128, 64 threads, and one block an SM
+};
+
 // Two visits per row: persistent clusters of blocks of 64, 128 or 256 threads, each block with its warp that brings its
 // rows and its part of the SM's shared memory for the stream.  A row goes to one block of 64 up to 20 KB (where `k` slots are one for
 // a thread), to one of 128 up to 72, to two up to 144, then to two of 256, to four from 288 KB.  Measured with gradient, us, by
@@ -577,16 +584,17 @@ constexpr size_t block_smem(int per) { return SMEM_PER_SM / per - 1024 - STATIC_
 // 4000 x 64,000 bf16 -, 222, 177, 174, 212, 320; 3000 x 40,000 fp32 -, 212, 181, 181, 160, 232;
 // 4096 x 128,000 bf16 -, 475, 450, 447, 356, 451; 3000 x 90,000 fp32 -, 479, 470, 469, 398, 354.  Larger shares go to memory for
 // their second visit (more than L2 keeps is under way); smaller ones leave too little work between a row's waits.
-// No more clusters than run at once (t.room): one cluster more, and the others wait for its rows (76 clusters of 4 where 74
+// No more clusters than run at once (room): one cluster more, and the others wait for its rows (76 clusters of 4 where 74
 // have room: 3000 x 128,000 fp32 733 us, 487 by 74).
-inline Shape twice_shape(int64_t rows, int64_t cols, int vec, const pdb_tokens &t, size_t extra, int k)
+inline Shape twice_shape(int64_t rows, int64_t cols, int vec, const Room &room, size_t extra, int k)
 {
     const int64_t nv = cols / vec + 1;
     Shape s = {};
     s.threads = nv <= 1280 && k <= 64 ? 64 : nv <= 9216 ? 128 : 256;
     const int per = blocks_per_sm(s.threads), kind = 8 - __builtin_ctz(s.threads);
-    s.blocks = cluster_of(rows, nv, s.threads, [&](int blocks) { return t.room[kind][__builtin_ctz(blocks)]; });
-    while (nv / s.blocks > s.threads * 36 && s.blocks < MAX_CLUSTER) s.blocks *= 2;
+    s.blocks = cluster_of(rows, nv, s.threads, [&](int blocks) { return room.clusters[kind][__builtin_ctz(blocks)]; });
+    while (nv / s.blocks > s.threads * 36 && s.blocks < MAX_CLUSTER && room.clusters[kind][__builtin_ctz(s.blocks * 2)] > 0)
+        s.blocks *= 2;
     set_maps(s, nv / s.blocks + 1);
     const size_t chunk = (size_t)UNROLL * 16 * s.threads, fixed = extra + s.map_bytes, most = block_smem(per);
     const int64_t chunks = std::max<int64_t>(1, (nv / s.blocks + UNROLL * s.threads) / (UNROLL * s.threads));
@@ -594,7 +602,7 @@ inline Shape twice_shape(int64_t rows, int64_t cols, int vec, const pdb_tokens &
     s.slots = (int)std::max<int64_t>(3, std::min({fit, 2 * chunks + 2, (int64_t)MOST_SLOTS}));
     s.hold = (int)std::max<int64_t>(1, std::min<int64_t>(chunks, s.slots - 2));
     s.smem = fixed + s.slots * chunk;
-    s.clusters = std::min<int64_t>(rows, t.room[s.smem > most ? ROOM_ALONE : kind][__builtin_ctz(s.blocks)]);
+    s.clusters = std::min<int64_t>(rows, room.clusters[s.smem > most ? Room::ALONE : kind][__builtin_ctz(s.blocks)]);
     return s;
 }
 

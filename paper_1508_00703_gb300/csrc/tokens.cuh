@@ -11,7 +11,6 @@
 
 struct pdb_tokens {
     int device, sms;
-    int room[4][4];            // clusters of 1, 2, 4, 8 blocks that run at once: blocks of 256, 128, 64, one an SM (distill.cu)
     int64_t max_tokens, max_dim;
     unsigned tries;            // of a wait of k_distill_grad
     int *status;               // device: [0] first error recorded by a kernel; [1] always 0 (the radix
@@ -28,8 +27,6 @@ struct pdb_tokens {
 
 namespace pdb {
 
-constexpr int ROOM_ALONE = 3;
-
 // every call on a handle records ev_use when it returns; not while a graph is
 // recorded, whose event could not be waited for (the graph's owner keeps the handle)
 struct TokensUse {
@@ -45,9 +42,6 @@ struct TokensUse {
 
 // lets a kernel have all of an SM's shared memory as dynamic one; once per kernel and device
 bool allow_smem(const void *kernel);
-
-// fills t->room
-int count_room(pdb_tokens *t);
 
 // PDB_OK where the current device is the handle's
 inline int check_device(const pdb_tokens *t)
