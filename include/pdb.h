@@ -494,8 +494,9 @@ int pdb_embed(pdb_tokens *t, const pdb_mat *table, const pdb_ids *ids, float sca
  * rows are not touched, so that dtable = the table and scale = -eta * scale of
  * pdb_embed make the SGD step in place.  Ids equal to `pad` are left out; so are
  * other ids outside [0, dtable->rows), which are recorded as PDB_ERANGE.
- * The ids are sorted with a stable sort; an id's rows are summed in fp32
- * in pieces of 32, the pieces' sums in an order fixed by their number; rounded once to
+ * The ids are sorted with a stable sort; an id's rows are summed in fp32 one after the other
+ * in pieces of 32, and of an id with more the sums of every 8th piece together, then these (up to) eight in turn: an
+ * order fixed by the id's number of rows.  The sum is multiplied by scale and rounded once to
  * dtable's type after the old value is added.  dout must not overlap dtable.
  * PDB_ETOOBIG beyond the handle's max_tokens or max_dim. */
 int pdb_embed_grad(pdb_tokens *t, const pdb_ids *ids, const pdb_mat *dout, float scale, int64_t pad, int accumulate,
