@@ -20,8 +20,6 @@ template <>
 struct Raw<4> { using type = uint32_t; };
 template <>
 struct Raw<8> { using type = uint2; };
-template <>
-struct Raw<16> { using type = uint4; };
 
 template <typename T, int E>
 struct alignas(E * sizeof(T)) Pack {
@@ -186,8 +184,8 @@ __global__ __launch_bounds__(RANK_THREADS) void k_embed_rank(Ids ids, int n, int
 }
 
 // Up to SORT_MAX ids: the whole stable sort in one launch, by a cluster of 1 to 8 blocks that keep the pairs (key, position)
-// in their shared memory.  Least significant digit first, one or two passes of up to 10 bits (three above 2^20
-// ids): a warp ranks its pairs by one ballot per digit bit and running counts per digit; the
+// in their shared memory.  Least significant digit first, passes of up to 10 bits: one for a table of fewer than 2^10 rows, two
+// below 2^20, three below 2^30, four above.  A warp ranks its pairs by one ballot per digit bit and running counts per digit; the
 // counts are summed over the warps, then over the cluster; the pairs are put in order within the block
 // and then stored where they belong, in whichever block's shared memory that is, neighbours together (stored one by
 // one from their places, 65,536 pairs took 19 us a pass).
