@@ -7,7 +7,7 @@ times an output matrix.  A step is what a program does that trains such a model:
   h @ W.T             logits
   pdb_distill         loss against the teacher's top logits, the gradient written over the logits
   d @ W, d.T @ h      gradients of h and W
-  pdb_embed_grad      the SGD step on the table, in place, each id's rows summed in data order
+  pdb_embed_grad      the SGD step on the table, in place, each id's rows summed in a fixed order
 
 and pdb_logprobs then scores held-out text: log probability of the tokens that followed,
 the model's entropy, and how often the token is among its five most probable.

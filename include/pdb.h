@@ -425,18 +425,21 @@ int pdb_sgd_epoch_ready_noalloc(const pdb_csr *X, const float *y, const uint32_t
  *
  * Operators of models over tokens: a chunk of the parameter database
  * (Definition 2) is a row of a table, a token's id names the row it reads and
- * updates (Definition 3), and an update sums an id's contributions in data
- * order as Algorithm 2a's write half does (pdb_bsp_apply), with vectors for
- * scalars.  The softmax losses take the place of pdb_loss.  The paper has no
- * formulas for them; each declaration gives its own.
+ * updates (Definition 3), and an update sums an id's contributions in a fixed
+ * order, as Algorithm 2a's write half does (pdb_bsp_apply: the data's; here the
+ * data's in pieces, pdb_embed_grad), with vectors for scalars.  The softmax losses
+ * take the place of pdb_loss.  The paper has no formulas for them; each declaration gives its own.
  *
  * Every call takes a pdb_tokens handle: the workspace of pdb_embed_grad, and
  * the status word in which the kernels record an id out of range
  * or an expired wait (pdb_tokens_status).  A recorded error stops no later call: a bad id gives the
  * result its declaration states.  Calls that share a handle must be ordered on
- * one stream, and made while the device is current that was at pdb_tokens_create (PDB_EINVAL otherwise).  Sums, softmax statistics and losses are held in fp32; a result
- * in 16 bits is rounded once.  No atomics add floating values: the same inputs
- * give the same bits.  No call allocates but pdb_tokens_create (and pdb_embed_grad above
+ * one stream, and made while the device is current that was at pdb_tokens_create
+ * (PDB_EINVAL otherwise).  Sums, softmax statistics and losses are held in fp32; a result
+ * in 16 bits is rounded once.  No atomics add floating values: the same call on the same
+ * inputs gives the same bits.  How a row of logits is split, and so the order of its sums, depends on
+ * its length, its alignment and the number of rows of the call: the same row alone and among others may
+ * differ in the last bits.  No call allocates but pdb_tokens_create (and pdb_embed_grad above
  * 65,536 ids: scratch of the radix sort, stream-ordered from the library's pool); all but
  * these and pdb_tokens_status, pdb_embed_grad up to 65,536 ids included, can be recorded into a CUDA graph (keep the
  * handle until the graph's last run has finished: pdb_tokens_free does not wait for it).
@@ -522,7 +525,8 @@ int pdb_logprobs(pdb_tokens *t, const pdb_mat *logits, const pdb_ids *ids, float
  * respect to the logits, lse and entropy as pdb_logprobs gave them:
  *   dlogits[r, j] = scale * (dlogp[r] * ([j = t] - p_j) - dentropy[r] * p_j * (log p_j + entropy[r]))
  * dlogp or dentropy may be NULL (zero); entropy is read with dentropy only,
- * ids with dlogp only.  A row whose two coefficients are 0 (dlogp counts as 0 where
+ * ids with dlogp only.  p is formed from lse where |lse| < 256; above, where its rounding would show in p, the
+ * row's maximum and sum are formed again.  A row whose two coefficients are 0 (dlogp counts as 0 where
  * pdb_logprobs leaves ids[r] out) or that has nothing left gets zeros, whatever it
  * holds.  dlogits may be the logits' own memory (same data, stride and type);
  * it must not overlap them otherwise. */

@@ -599,8 +599,8 @@ def pdb_embed(tok: Tokens, table, ids, out, scale: float = 1.0, pad: int = -1, s
 
 def pdb_embed_grad(tok: Tokens, ids, dout, dtable, scale: float = 1.0, pad: int = -1, accumulate: bool = False,
                    stream=None):
-    """dtable[v] = scale * sum of dout[i] over ids[i] = v, in data order (Algorithm 2a's ordered sums); every
-    row is written.  accumulate=True adds to the rows that occur and leaves the others: with the table for
+    """dtable[v] = scale * sum of dout[i] over ids[i] = v, in an order fixed by their number (pieces of 32 in data
+    order, the pieces as the header says); every row is written.  accumulate=True adds to the rows that occur and leaves the others: with the table for
     dtable and scale = -eta * scale, the SGD step in place."""
     _check(load().pdb_embed_grad(tok.handle, _ids(ids, tok, "pdb_embed_grad ids"),
                                  _mat(dout, tok, "pdb_embed_grad dout"), scale, pad, accumulate,

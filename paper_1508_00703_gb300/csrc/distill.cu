@@ -16,8 +16,9 @@
 // written over after that by the block that holds them.
 //
 // Measured: the loss alone, 1024 x 32,000 fp16, 64 slots, 15.6 us (66 MB, 4.2 TB/s: one round of blocks, of whose time
-// start, joins and end are 6 us); with gradient 4096 x 128,000 bf16 356 us (2.1 GB, 5.9 TB/s; DRAM moves little more
-// than that, the rest is time per row), 1501 x 50,001 fp32 114 us (5.3 TB/s), 3000 x 128,000 fp32 487 us (6.3 TB/s).
+// start, joins and end are 6 us); with gradient 4096 x 128,000 bf16 360 us (2.1 GB, 5.8 TB/s; DRAM moves little more
+// than that, the rest is time per row), 1501 x 50,001 fp32 114 us (5.3 TB/s), 3000 x 128,000 fp32 484 us (6.3 TB/s).  Many short
+// rows are bound by the chain of barriers and joins of each: 8000 x 2000 bf16 42 us, four times what their bytes take.
 #include <algorithm>
 #include <cmath>
 #include <mutex>
@@ -31,7 +32,7 @@ namespace {
 
 constexpr int MAX_SLOTS = 1024;
 constexpr float LEAST_REST = 1e-6f;     // a teacher's rest below this is the rounding of its lse
-constexpr int64_t MAX_COLS = 1 << 21;   // a block's marks then take 72 KB at most
+constexpr int64_t MAX_COLS = 1 << 21;   // a block's marks then take 73,872 bytes at most (fp32, clusters of 8)
 
 // an element of a matrix of any type, fetched and converted in two steps (as fetch_id)
 __device__ __forceinline__ uint32_t fetch_element(const void *p, int type, int64_t i)
