@@ -180,6 +180,29 @@ __device__ __forceinline__ float logit_in(const uint4 &x, const Share &sh, int j
     return z;
 }
 
+// The loss of a row whose sum came out infinite at a temperature below 1, with every term times T^2: (z - m) / T of a token masked
+// by the type's lowest value passes fp32's range, T (z - m) does not.  A call of its own, for the sake of the others.
+__device__ __noinline__ float loss_of_lowest(const float *t, const float *z, int K, float T, float base, float logt, float m,
+                                             float logs, float rest, float out_m, float out_logs)
+{
+    const float square = __fmul_rn(T, T);
+    float kl = 0.0f;
+#pragma unroll 1
+    for (int k = threadIdx.x & 31; k < K; k += 32) {
+        if (t[k] == -INFINITY) continue;
+        const float logq = __fsub_rn(__fsub_rn(t[k], base), logt), q = expf(logq);
+        const float x = __fmaf_rn(__fsub_rn(z[k], m), T, -__fmul_rn(logs, square));
+        if (q != 0.0f) kl = __fmaf_rn(q, __fsub_rn(__fmul_rn(logq, square), x), kl);
+    }
+#pragma unroll
+    for (int off = 16; off >= 1; off >>= 1) kl = __fadd_rn(kl, __shfl_xor_sync(FULL, kl, off));
+    if (rest > 0.0f) {
+        const float logp = __fmaf_rn(__fsub_rn(out_m, m), T, __fmul_rn(__fsub_rn(out_logs, logs), square));
+        kl = __fmaf_rn(rest, __fsub_rn(__fmul_rn(logf(rest), square), logp), kl);
+    }
+    return kl;
+}
+
 // What the slots and the pass over the row come to.
 template <bool BUCKET>
 struct Row {
@@ -330,6 +353,8 @@ struct Row {
                                                                               __fmul_rn(__fsub_rn(a.m, m), inv)));
             kl = __fmaf_rn(rest, ratio, kl);
         }
+        if (kl == INFINITY && temperature < 1.0f && live && s != 0.0f)
+            return loss_of_lowest(S.t, S.z, K, temperature, base, logt, m, logs, BUCKET ? rest : 0.0f, a.m, logf(a.s));
         return !live ? 0.0f : s == 0.0f ? INFINITY : __fmul_rn(__fmul_rn(temperature, temperature), kl);
     }
 };
