@@ -578,7 +578,7 @@ struct Room {
 
 // Two visits per row: persistent clusters of blocks of 64, 128 or 256 threads, each block with its warp that brings its
 // rows and its part of the SM's shared memory for the stream.  A row goes to one block of 64 up to 20 KB (where `k` slots are one for
-// a thread), to one of 128 up to 72, to two up to 144, then to two of 256, to four from 288 KB.  Measured with gradient, us, by
+// a thread), to one of 128 up to 72, to two up to 144, then to two of 256, to four from 288 KB.  Measured with gradient (all of them 1% faster than since a wait that runs out stops the cluster), us, by
 // 1 x 64, 1 x 128, 2 x 128, 1 x 256, 2 x 256, 4 x 256:
 // 8000 x 2000 bf16 42, 57; 4000 x 10,000 bf16 44, 48; 8000 x 16,000 bf16 123, 113; 8000 x 32,000 bf16 -, 176, 212, 203, 308, 521;
 // 4000 x 64,000 bf16 -, 222, 177, 174, 212, 320; 3000 x 40,000 fp32 -, 212, 181, 181, 160, 232;
