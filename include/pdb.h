@@ -478,7 +478,7 @@ void pdb_tokens_free(pdb_tokens *t);
 int pdb_tokens_status(const pdb_tokens *t, void *stream);
 
 /* Tries of a device-side wait in later calls on the handle (pdb_distill with gradient is the one
- * that waits), each 20 ns to a microsecond, before PDB_ETIMEOUT; 2^22 unless set, at most 2^30.
+ * that waits), each 20 ns to a microsecond, before PDB_ETIMEOUT: 2^22 unless set, and at most that.
  * With 0 no try is made and such calls end with PDB_ETIMEOUT and undefined results: for tests of
  * what a program does then. */
 int pdb_tokens_set_wait_limit(pdb_tokens *t, int64_t tries);

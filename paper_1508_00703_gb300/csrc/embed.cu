@@ -667,7 +667,7 @@ int pdb_tokens_status(const pdb_tokens *t, void *stream)
 
 int pdb_tokens_set_wait_limit(pdb_tokens *t, int64_t tries)
 {
-    if (!t || tries < 0 || tries > (int64_t)1 << 30) return PDB_EINVAL;
+    if (!t || tries < 0 || tries > (int64_t)WAIT_TRIES) return PDB_EINVAL;
     t->tries = (unsigned)tries;
     return PDB_OK;
 }

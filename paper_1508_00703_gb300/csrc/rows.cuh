@@ -387,7 +387,7 @@ __device__ __forceinline__ void block_join(Stat<ENT> &a, float c, float *part)
 }
 
 constexpr int MOST_SLOTS = 16;
-constexpr unsigned WAIT_TRIES = 1u << 22;   // of a wait, unless the handle has another limit; one takes some 20 ns to a microsecond
+constexpr unsigned WAIT_TRIES = 1u << 22;   // of a wait, unless the handle has a lower limit; one takes some 20 ns to a microsecond
 
 // One block's shares of its cluster's rows, chunk after chunk of SPAN = THREADS * UNROLL vectors, each row twice.
 // A warp of its own brings the chunks by bulk copies into `slots` places, in turn (issued by one of the reading threads

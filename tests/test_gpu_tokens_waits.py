@@ -59,7 +59,7 @@ def test_expired_waits_are_reported_not_hung(n, cols, K, kind, bucket):
 
 def test_limits_refused():
     tok = pdb.pdb_tokens_create()
-    for tries in (-1, (1 << 30) + 1):
+    for tries in (-1, (1 << 22) + 1, 1 << 31):
         with pytest.raises(pdb.PdbError) as e:
             pdb.pdb_tokens_set_wait_limit(tok, tries)
         assert e.value.code == pdb.PDB_EINVAL
