@@ -563,6 +563,86 @@ int pdb_distill(pdb_tokens *t, const pdb_mat *logits, const pdb_ids *top_ids, co
                 const float *teacher_lse, float temperature, float *loss, const float *weight, const pdb_mat *dlogits,
                 void *stream);
 
+/* Drafted tokens verified (speculative sampling: Leviathan, Kalman, Matias 2023; Chen et al. 2023): a draft model, as pdb_distill trains
+ * one, has proposed n_drafts tokens for each of n sequences; the tokens that come out are distributed as if drawn one by one from the
+ * target.  Sequence s has the target's logits in rows s * (n_drafts + 1) + d, d = 0 .. n_drafts (n = target->rows /
+ * (n_drafts + 1)), the draft's in rows s * n_drafts + d of `draft` (the target's type and columns), d < n_drafts, and the drafted
+ * tokens t_d = draft_ids->data[s * draft_ids->stride + d] (n * n_drafts ids; the stride is that of the rows).  With
+ * p_d = softmax(scale * target row), q_d = softmax(draft_scale * draft row), and u_d = accept_u[s * n_drafts + d], from d = 0 on:
+ *   u_d q_d(t_d) < p_d(t_d)   t_d is accepted
+ *   else                      a token is drawn from max(p_d - q_d, 0), and the sequence ends
+ * draft == NULL: q_d is 1 at t_d (drafts that come from no model; draft_scale is not read).  A negative id ends the
+ * sequence's drafts; so does an id >= cols, recorded as PDB_ERANGE, and a draft row that has nothing left or holds a NaN or +inf. Where
+ * they end, and behind the last, a token is drawn from p_d.  Drawn is the smallest j whose running sum of weights passes draw_u[s]
+ * times their sum.  n_drafts = 0: a token is drawn for each row (draft_ids and accept_u are not read).
+ *   accepted[s]             a, the number of accepted drafts (may be NULL)
+ *   tokens[s, 0..n_drafts]  row-major: the accepted drafts, the drawn token, then -1
+ *   logp[s, 0..n_drafts]    log p_d of these tokens, 0 behind them (may be NULL)
+ * A target row that has nothing left, or holds a NaN or +inf, accepts nothing, and -1 stands where the drawn token would.
+ * The random numbers are the caller's, in [0, 1); others count as their nearest end in the draw.  Sides that the 32-bit statistics cannot tell
+ * apart, and every draw, are decided on probabilities good to 2^-40 of themselves and sums without rounding: the tokens do not
+ * depend on how rows are split.  Rows behind the first refusal are not read.  PDB_ETOOBIG above 64 drafts or
+ * 2^21 tokens.  These are the draws a program makes with its models between the reads of Definition 3. */
+int pdb_verify(pdb_tokens *t, const pdb_mat *target, const pdb_ids *draft_ids, int64_t n_drafts, const pdb_mat *draft,
+               float scale, float draft_scale, const float *accept_u, const float *draw_u, int32_t *tokens, int32_t *accepted,
+               float *logp, void *stream);
+
+/* Tokens to experts and back: layers whose parameters are chunks (Definition 2) of which each token names a few.  Token i has k slots;
+ * slot j names expert ids->data[i * ids->stride + j] (ids->n = n * k; the stride is that of the rows).  The experts' rows stand
+ * one expert after the other, an expert's slots in ascending order of (i, j) (the data's order, as in Algorithm 2a's writes):
+ *   place[i, j]   the slot's row (row-major, n * k), -1 for none
+ *   source[r]     the slot i * k + j that has row r, -1 for none
+ *   ends[e]       the row behind expert e's last
+ * capacity == 0: the rows are packed, n * k of them; expert e starts at ends[e - 1].  Else expert e starts at row e * capacity
+ * and has that many at most (n_experts * capacity rows); its slots behind them have none.  A negative id is a slot without an
+ * expert; so is one >= n_experts, recorded as PDB_ERANGE.  PDB_ETOOBIG above 64 slots, 4096 experts, 2^31 - 1 rows, or n * k beyond
+ * the handle's max_tokens. */
+int pdb_route(pdb_tokens *t, const pdb_ids *ids, int64_t k, int64_t n_experts, int64_t capacity, int32_t *place,
+              int32_t *source, int32_t *ends, void *stream);
+
+/* rows[place[i, j], :] = x[i, :] (reads as in Definition 3), and zeros in rows with source[r] < 0; rows whose source is a slot that does not
+ * name them are left as they were.  Rounded once to the rows' type.  place (x->rows * k) and source (rows->rows) as pdb_route
+ * gives them; a place >= rows->rows counts as none and is recorded as PDB_ERANGE, here and below.  rows must not overlap x.
+ * Its gradient is pdb_route_join without weights, of the rows' gradient. */
+int pdb_route_rows(pdb_tokens *t, const pdb_mat *x, const int32_t *place, int64_t k, const int32_t *source,
+                   const pdb_mat *rows, void *stream);
+
+/* y[i, :] = sum over the slots j that have a row, ascending, of weight[i, j] * rows[place[i, j], :] (weight row-major, n * k;
+ * NULL: every weight 1).  Sums in fp32 in that order (each row's writes in the data's order, Algorithm 2a), rounded once to y's type; a
+ * token without rows gets zeros.  y must not overlap rows. */
+int pdb_route_join(pdb_tokens *t, const pdb_mat *rows, const int32_t *place, int64_t k, const float *weight,
+                   const pdb_mat *y, void *stream);
+
+/* Gradients of pdb_route_join (read and written as Definition 3's chunks): for dy = the gradient of y,
+ *   drows[place[i, j], :] = weight[i, j] * dy[i, :], zeros in rows with source[r] < 0
+ *   dweight[i, j]         = sum over c of dy[i, c] * rows[place[i, j], c], 0 for a slot without a row
+ * rows and dweight may be NULL together (drows alone).  Products and sums in fp32, in an order that depends on cols, types and
+ * alignment only; drows, of rows' type and size, is rounded once and may be the rows' own memory (same data, stride and type); it must
+ * not overlap them otherwise, nor dy. */
+int pdb_route_join_grad(pdb_tokens *t, const pdb_mat *rows, const int32_t *place, int64_t k, const int32_t *source,
+                        const float *weight, const pdb_mat *dy, const pdb_mat *drows, float *dweight, void *stream);
+
+/* The norm over many gradients, and a step clipped to it: with N = sqrt(sum over all n matrices of g^2) and
+ * f = max_norm / N where N > max_norm, else 1, for every matrix
+ *   out = scale * f * g, or with accumulate != 0   out = out + scale * f * g
+ * so that the gradients themselves as results and scale = 1 clip them in place, and the weights as results, accumulate and scale = -eta make
+ * the SGD step (Section 6.3's, over all of a model's chunks).  norm, one float, holds N (may be NULL); max_norm >= 0, infinity for no
+ * clipping; scale finite.  A gradient that holds a NaN or an infinity makes N one, and no result is written: the step is left
+ * out.  N is formed from 32-bit sums of squares of at most a piece of a matrix, added up in 64 bits in a fixed order; squares that
+ * leave fp32's range are formed in 64 bits.  The factor scale * f is rounded to fp32, as are its product with g and
+ * the sum with out; out is rounded once to its type.
+ *
+ * A plan holds where the matrices lie and the sums' workspace: pdb_clip_plan_build takes n gradients and their results, of the same rows and
+ * columns each, any types, and copies the descriptions (SYNCHRONIZES `stream`); the matrices must outlive the plan.  A result may be its
+ * gradient's own memory (same data, stride and type); results must not overlap otherwise, one another or any gradient
+ * (PDB_EINVAL).  PDB_ETOOBIG above 2^40 elements.  Calls on a plan must be ordered on one stream, and made while the device is current
+ * that was at its building (PDB_EINVAL otherwise); they can be recorded into a CUDA graph (keep the plan until its last run has
+ * finished).  pdb_clip_plan_free waits for the work enqueued on the plan. */
+typedef struct pdb_clip_plan pdb_clip_plan; /* opaque, library-owned device arrays */
+int pdb_clip_plan_build(const pdb_mat *grads, const pdb_mat *outs, int64_t n, pdb_clip_plan **out, void *stream);
+int pdb_clip(const pdb_clip_plan *p, float max_norm, float scale, int accumulate, float *norm, void *stream);
+void pdb_clip_plan_free(pdb_clip_plan *p);
+
 /* ---------------------------------------------------------------- utilities */
 
 /* cudaMemcpyAsync with the kind inferred from the pointers (for bindings that

@@ -125,7 +125,8 @@ EXPORTS = ["pdb_build_conflicts", "pdb_conflicts_arrays", "pdb_schedule_build", 
            "pdb_bsp_coef", "pdb_bsp_apply", "pdb_bsp_plan_free",
            "pdb_tokens_create", "pdb_tokens_free", "pdb_tokens_status",
            "pdb_tokens_set_wait_limit", "pdb_embed", "pdb_embed_grad", "pdb_logprobs",
-           "pdb_logprobs_grad", "pdb_distill"]
+           "pdb_logprobs_grad", "pdb_distill", "pdb_verify", "pdb_route", "pdb_route_rows", "pdb_route_join",
+           "pdb_route_join_grad", "pdb_clip_plan_build", "pdb_clip", "pdb_clip_plan_free"]
 
 
 def load(path: str | None = None):
@@ -176,6 +177,15 @@ def load(path: str | None = None):
         lib.pdb_logprobs.argtypes = [P, M, J, F32, I64, P, P, P, I64, P, P, P]
         lib.pdb_logprobs_grad.argtypes = [P, M, J, F32, I64, P, P, P, P, M, P]
         lib.pdb_distill.argtypes = [P, M, J, M, P, F32, P, P, M, P]
+        lib.pdb_verify.argtypes = [P, M, J, I64, M, F32, F32, P, P, P, P, P, P]
+        lib.pdb_route.argtypes = [P, J, I64, I64, I64, P, P, P, P]
+        lib.pdb_route_rows.argtypes = [P, M, P, I64, P, M, P]
+        lib.pdb_route_join.argtypes = [P, M, P, I64, P, M, P]
+        lib.pdb_route_join_grad.argtypes = [P, M, P, I64, P, P, M, M, P, P]
+        lib.pdb_clip_plan_build.argtypes = [M, M, I64, PP, P]
+        lib.pdb_clip.argtypes = [P, F32, F32, I32, P, P]
+        lib.pdb_clip_plan_free.argtypes = [P]
+        lib.pdb_clip_plan_free.restype = None
         lib.pdb_launch_count.argtypes = []
         lib.pdb_launch_count.restype = I64
         _lib = lib
@@ -656,6 +666,125 @@ def pdb_distill(tok: Tokens, logits, top_ids, top_logits, loss=None, teacher_lse
         _vec(teacher_lse, n, tok, "pdb_distill teacher_lse"), temperature, _vec(loss, n, tok, "pdb_distill loss"),
         _vec(weight, n, tok, "pdb_distill weight"),
         None if dlogits is None else _mat(dlogits, tok, "pdb_distill dlogits"), _stream(stream)), "pdb_distill")
+
+
+def pdb_verify(tok: Tokens, target, draft_ids, accept_u, draw_u, tokens, accepted=None, draft=None, logp=None,
+               scale: float = 1.0, draft_scale: float = 1.0, stream=None):
+    """Drafted tokens draft_ids (n, D) (a negative one ends its sequence's) verified against the target's logits, rows s * (D + 1) + d,
+    and the draft's, rows s * D + d (None: drafts from no model): tokens (n, D + 1) int32 gets the accepted drafts, the token
+    drawn after them, then -1; accepted (n) int32 their number; logp (n, D + 1) the tokens' log probabilities under the target.
+    accept_u (n, D) and draw_u (n) are the caller's random numbers in [0, 1).  D = 0 draws a token for each row of target."""
+    z = _mat(target, tok, "pdb_verify target")
+    if draft_ids.dim() != 2:
+        _refuse("pdb_verify draft_ids", f"(sequences, drafts) wanted, got {tuple(draft_ids.shape)}")
+    n, D = draft_ids.shape
+    if z.rows != n * (D + 1):
+        _refuse("pdb_verify target", f"{n * (D + 1)} rows wanted for {n} sequences of {D} drafts, got {z.rows}")
+    _check(load().pdb_verify(
+        tok.handle, z, _rows_of_ids(draft_ids, tok, "pdb_verify draft_ids"), D,
+        None if draft is None else _mat(draft, tok, "pdb_verify draft"), scale, draft_scale,
+        _vec(accept_u, n * D, tok, "pdb_verify accept_u"), _vec(draw_u, n, tok, "pdb_verify draw_u"),
+        _vec(tokens, n * (D + 1), tok, "pdb_verify tokens", "int32"), _vec(accepted, n, tok, "pdb_verify accepted", "int32"),
+        _vec(logp, n * (D + 1), tok, "pdb_verify logp"), _stream(stream)), "pdb_verify")
+
+
+def pdb_route(tok: Tokens, ids, n_experts: int, place, source, ends, capacity: int = 0, stream=None):
+    """Rows of the tokens' slots ids (n, k) (the slots' experts; a negative one: none), expert after expert, an expert's slots in
+    ascending order: place (n, k) int32 the slots' rows (-1: none), source int32 the rows' slots i * k + j (-1: none), ends
+    (n_experts) int32 the row behind each expert's last.  capacity 0: n * k packed rows; else n_experts * capacity, expert
+    e's from e * capacity on, slots behind its capacity without a row.  n * k is at most the handle's max_tokens."""
+    if ids.dim() != 2:
+        _refuse("pdb_route ids", f"(tokens, slots) wanted, got {tuple(ids.shape)}")
+    n, k = ids.shape
+    _check(load().pdb_route(
+        tok.handle, _rows_of_ids(ids, tok, "pdb_route ids"), k, n_experts, capacity,
+        _vec(place, n * k, tok, "pdb_route place", "int32"),
+        _vec(source, n_experts * capacity if capacity else n * k, tok, "pdb_route source", "int32"),
+        _vec(ends, n_experts, tok, "pdb_route ends", "int32"), _stream(stream)), "pdb_route")
+
+
+def _places(place, n, tok, what):
+    """(pointer, slots) of places (n, k)."""
+    if place.dim() != 2 or place.shape[0] != n:
+        _refuse(what, f"({n}, slots) wanted, got {tuple(place.shape)}")
+    return _vec(place, place.numel(), tok, what, "int32"), place.shape[1]
+
+
+def pdb_route_rows(tok: Tokens, x, place, source, rows, stream=None):
+    """rows[place[i, j]] = x[i], zeros in the rows without a source.  Its gradient: pdb_route_join of the rows' gradient, without weights."""
+    m, r = _mat(x, tok, "pdb_route_rows x"), _mat(rows, tok, "pdb_route_rows rows")
+    at, k = _places(place, m.rows, tok, "pdb_route_rows place")
+    _check(load().pdb_route_rows(tok.handle, m, at, k, _vec(source, r.rows, tok, "pdb_route_rows source", "int32"), r,
+                                 _stream(stream)), "pdb_route_rows")
+
+
+def pdb_route_join(tok: Tokens, rows, place, y, weight=None, stream=None):
+    """y[i] = the sum over its slots that have a row, ascending, of weight[i, j] * rows[place[i, j]] (weight None: 1)."""
+    r, m = _mat(rows, tok, "pdb_route_join rows"), _mat(y, tok, "pdb_route_join y")
+    at, k = _places(place, m.rows, tok, "pdb_route_join place")
+    _check(load().pdb_route_join(tok.handle, r, at, k, _vec(weight, m.rows * k, tok, "pdb_route_join weight"), m,
+                                 _stream(stream)), "pdb_route_join")
+
+
+def pdb_route_join_grad(tok: Tokens, rows, place, source, dy, drows, weight=None, dweight=None, stream=None):
+    """Gradients of pdb_route_join: drows[place[i, j]] = weight[i, j] * dy[i] (zeros in rows without a source; drows may be
+    rows itself) and, where dweight is given, dweight[i, j] = <dy[i], rows[place[i, j]]> (rows may be None otherwise)."""
+    d, m = _mat(drows, tok, "pdb_route_join_grad drows"), _mat(dy, tok, "pdb_route_join_grad dy")
+    at, k = _places(place, m.rows, tok, "pdb_route_join_grad place")
+    if dweight is not None and rows is None:
+        _refuse("pdb_route_join_grad", "dweight wants rows")
+    _check(load().pdb_route_join_grad(
+        tok.handle, None if dweight is None else _mat(rows, tok, "pdb_route_join_grad rows"), at, k,
+        _vec(source, d.rows, tok, "pdb_route_join_grad source", "int32"),
+        _vec(weight, m.rows * k, tok, "pdb_route_join_grad weight"), m, d,
+        _vec(dweight, m.rows * k, tok, "pdb_route_join_grad dweight"), _stream(stream)), "pdb_route_join_grad")
+
+
+class ClipPlan:
+    """Owns a pdb_clip_plan handle (keeps its gradients and results alive)."""
+
+    def __init__(self, handle, device, tensors):
+        self.handle, self.device, self.tensors = handle, device, tensors
+
+    def __del__(self):
+        if getattr(self, "handle", None) and _lib is not None:
+            _lib.pdb_clip_plan_free(self.handle)
+            self.handle = None
+
+
+def _flat_mat(t, plan, what):
+    """A pdb_mat of a contiguous tensor of any dimensions, or of a matrix whose rows are contiguous."""
+    if t.is_contiguous():
+        cols = t.shape[-1] if t.dim() else 1
+        t = t.view(-1, cols) if t.numel() else t.view(0, max(cols, 1))
+    return _mat(t, plan, what)
+
+
+def pdb_clip_plan_build(grads, outs=None, stream=None) -> ClipPlan:
+    """Where a model's gradients lie and the tensors that their steps go to (None: the gradients themselves), for pdb_clip:
+    float32, bfloat16 or float16 each, contiguous or matrices with contiguous rows (synchronizes)."""
+    import torch
+    grads = list(grads)
+    outs = grads if outs is None else list(outs)
+    if len(grads) != len(outs):
+        _refuse("pdb_clip_plan_build", f"{len(grads)} gradients and {len(outs)} results")
+    plan = ClipPlan(None, torch.cuda.current_device(), (grads, outs))
+    for g, o in zip(grads, outs):
+        if g.shape != o.shape:
+            _refuse("pdb_clip_plan_build", f"a gradient of shape {tuple(g.shape)} and a result of {tuple(o.shape)}")
+    g = (pdb_mat * len(grads))(*(_flat_mat(t, plan, "pdb_clip_plan_build grads") for t in grads))
+    o = (pdb_mat * len(outs))(*(_flat_mat(t, plan, "pdb_clip_plan_build outs") for t in outs))
+    h = ctypes.c_void_p()
+    _check(load().pdb_clip_plan_build(g, o, len(grads), ctypes.byref(h), _stream(stream)), "pdb_clip_plan_build")
+    plan.handle = h
+    return plan
+
+
+def pdb_clip(plan: ClipPlan, max_norm: float, norm=None, scale: float = 1.0, accumulate: bool = False, stream=None):
+    """Every result = scale * f * its gradient (accumulate: added to it), f = min(1, max_norm / N), N the norm over all of the
+    plan's gradients, written to norm (one float32 on the device).  Nothing is written where N is not finite."""
+    _check(load().pdb_clip(plan.handle, max_norm, scale, accumulate, _vec(norm, 1, plan, "pdb_clip norm"), _stream(stream)),
+           "pdb_clip")
 
 
 def check_tokens(tok: Tokens, stream=None):

@@ -1,0 +1,562 @@
+// Tokens to experts and back (pdb_route, pdb_route_rows, pdb_route_join,
+// pdb_route_join_grad).
+//
+// n tokens have k slots each; slot f = i k + j of token i names an expert e_f, or none.  The experts' rows lie one expert after the
+// other, an expert's slots in ascending order:
+//   place_f = first(e_f) + |{f' < f : e_f' = e_f}|,   first(e) = |{f : e_f < e}|, or e * capacity
+// a stable counting sort by expert.  With it rows go there, come back weighted and summed, and their gradients the other way.
+#include <algorithm>
+
+#include "pack.cuh"
+#include "rows.cuh"
+
+using namespace pdb;
+
+namespace {
+
+// ------------------------------------------------------------------ places
+constexpr int MAX_EXPERTS = 4096, MAX_ROUTE_SLOTS = 64, ROUTE_THREADS = 512, ROUTE_WARPS = ROUTE_THREADS / 32;
+
+struct Slots {
+    Ids ids;
+    uint32_t n, k;                      // slots in all, of a token
+    int experts;
+};
+
+// the expert of slot f, or `experts` for none
+__device__ __forceinline__ int expert_of(const Slots &s, int2 raw, int *status)
+{
+    const int64_t e = id_of(s.ids, raw);
+    if (e >= s.experts) set_status(status, PDB_ERANGE);
+    return e >= 0 && e < s.experts ? (int)e : s.experts;
+}
+__device__ __forceinline__ int2 fetch_slot(const Slots &s, uint32_t f)
+{
+    const uint32_t i = f / s.k;
+    return fetch_id(s.ids, i, (int)(f - i * s.k));
+}
+
+// how often each expert occurs among a block's slots
+template <int IPT>
+__global__ __launch_bounds__(ROUTE_THREADS) void k_route_count(Slots s, uint32_t *__restrict__ counts, int *status)
+{
+    after_previous();
+    let_next_start();
+    extern __shared__ uint32_t s_count[];
+    for (int e = threadIdx.x; e < s.experts; e += ROUTE_THREADS) s_count[e] = 0;
+    const uint32_t f0 = blockIdx.x * (uint32_t)(ROUTE_THREADS * IPT);
+    int2 raw[IPT];
+#pragma unroll
+    for (int i = 0; i < IPT; ++i) {
+        const uint32_t f = f0 + i * ROUTE_THREADS + threadIdx.x;
+        raw[i] = f < s.n ? fetch_slot(s, f) : int2{-1, -1};
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < IPT; ++i) {
+        const int e = expert_of(s, raw[i], status);
+        // one addition for the lanes of one expert
+        const unsigned peers = __match_any_sync(FULL, e);
+        if (e < s.experts && (peers & lanemask_lt()) == 0) atomicAdd(&s_count[e], __popc(peers));
+    }
+    __syncthreads();
+    for (int e = threadIdx.x; e < s.experts; e += ROUTE_THREADS) counts[(int64_t)blockIdx.x * s.experts + e] = s_count[e];
+}
+
+// A block's slots, warp after warp, 32 at a time: a lane's rank is the lower lanes of its expert, its warp's slots before
+// them, the lower warps', and the lower blocks'.
+template <int IPT>
+__global__ __launch_bounds__(ROUTE_THREADS) void k_route_place(Slots s, const uint32_t *counts, int64_t capacity,
+                                                               int32_t *__restrict__ place, int32_t *__restrict__ source,
+                                                               int32_t *__restrict__ ends, int *status)
+{
+    after_previous();
+    let_next_start();
+    extern __shared__ uint32_t s_first[];                                       // [experts] of all and of lower blocks, then
+    uint32_t *s_total = s_first + s.experts;                                    // [experts] slots of the expert in all
+    uint16_t *s_warp = reinterpret_cast<uint16_t *>(s_total + s.experts);       // [warp][experts] the expert's slots by warp
+    __shared__ uint32_t s_sum[ROUTE_WARPS];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, experts = s.experts;
+    const uint32_t f0 = blockIdx.x * (uint32_t)(ROUTE_THREADS * IPT) + warp * (32 * IPT) + lane;
+    int2 raw[IPT];
+#pragma unroll
+    for (int i = 0; i < IPT; ++i) raw[i] = f0 + i * 32 < s.n ? fetch_slot(s, f0 + i * 32) : int2{-1, -1};
+    for (int e = tid; e < experts; e += ROUTE_THREADS) s_first[e] = s_total[e] = 0;
+    for (int e = tid; e < ROUTE_WARPS * experts; e += ROUTE_THREADS) s_warp[e] = 0;
+    __syncthreads();
+    // the blocks' counts, every `sets`-th of them by one thread
+    if (gridDim.x > 1) {
+        const int sets = max(1, ROUTE_THREADS / experts);
+        for (int x = tid; x < sets * experts; x += ROUTE_THREADS) {
+            const int set = x / experts, e = x - set * experts;
+            uint32_t all = 0, before = 0;
+#pragma unroll 8
+            for (int b = set; b < (int)gridDim.x; b += sets) {
+                const uint32_t c = counts[(int64_t)b * experts + e];
+                all += c;
+                before += b < (int)blockIdx.x ? c : 0;
+            }
+            atomicAdd(&s_total[e], all);
+            atomicAdd(&s_first[e], before);
+        }
+    }
+    int expert[IPT], rank[IPT];
+    uint16_t *own = s_warp + warp * experts;
+#pragma unroll
+    for (int i = 0; i < IPT; ++i) {
+        expert[i] = expert_of(s, raw[i], status);
+        const unsigned peers = __match_any_sync(FULL, expert[i]);
+        const bool there = expert[i] < experts;
+        const int c = there ? own[expert[i]] : 0;
+        __syncwarp();
+        rank[i] = c + __popc(peers & lanemask_lt());
+        if (there && (peers & lanemask_lt()) == 0) own[expert[i]] = (uint16_t)(c + __popc(peers));
+        __syncwarp();
+    }
+    __syncthreads();
+    // experts tid * per ..: the warps' counts become places, the totals are summed up over the experts
+    const int per = (experts + ROUTE_THREADS - 1) / ROUTE_THREADS, e0 = min(experts, tid * per), e1 = min(experts, e0 + per);
+    uint32_t mine = 0;
+    for (int e = e0; e < e1; ++e) {
+        uint32_t sum = 0;
+#pragma unroll
+        for (int w = 0; w < ROUTE_WARPS; ++w) {
+            const uint32_t c = s_warp[w * experts + e];
+            s_warp[w * experts + e] = (uint16_t)sum;
+            sum += c;
+        }
+        if (gridDim.x == 1) s_total[e] = sum;
+        mine += s_total[e];
+    }
+    uint32_t up = mine;
+#pragma unroll
+    for (int off = 1; off < 32; off <<= 1) {
+        const uint32_t u = __shfl_up_sync(FULL, up, off);
+        if (lane >= off) up += u;
+    }
+    if (lane == 31) s_sum[warp] = up;
+    __syncthreads();
+    up -= mine;
+    for (int w = 0; w < warp; ++w) up += s_sum[w];
+    for (int e = e0; e < e1; ++e) {
+        const uint32_t total = s_total[e];
+        const uint32_t first = capacity ? (uint32_t)(e * capacity) : up;
+        const uint32_t end = first + (capacity ? (uint32_t)min64(total, capacity) : total);
+        if (blockIdx.x == 0) ends[e] = (int32_t)end;
+        s_total[e] = end;
+        s_first[e] += first;
+        up += total;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < IPT; ++i) {
+        const uint32_t f = f0 + i * 32;
+        if (f >= s.n) break;
+        int32_t at = -1;
+        if (expert[i] < experts) {
+            const uint32_t p = s_first[expert[i]] + own[expert[i]] + rank[i];
+            if (p < s_total[expert[i]]) at = (int32_t)p;          // with a capacity, slots behind it have no row
+        }
+        place[f] = at;
+        if (at >= 0) source[at] = (int32_t)f;
+    }
+    // rows that no slot takes
+    const int64_t rows = capacity ? experts * capacity : (int64_t)s.n;
+    for (int64_t r = (int64_t)blockIdx.x * ROUTE_THREADS + tid; r < rows; r += (int64_t)gridDim.x * ROUTE_THREADS)
+        if (r >= s_total[capacity ? (int)(r / capacity) : experts - 1]) source[r] = -1;
+}
+
+inline size_t place_smem(int experts) { return (size_t)experts * (8 + 2 * ROUTE_WARPS); }
+
+// ------------------------------------------------------------------ rows there
+// zeros in the rows of `rows` (8 of them from r0 on) that no slot takes, by a warp
+constexpr int ZERO_ROWS = 8;
+
+template <typename O, int E>
+__device__ __forceinline__ void zero_unused(const int32_t *source, int64_t r0, int64_t rows, int dim, O *out, int64_t stride)
+{
+    const int lane = threadIdx.x & 31;
+    unsigned unused = __ballot_sync(FULL, lane < ZERO_ROWS && r0 + lane < rows && source[r0 + lane] < 0);
+    Pack<O, E> zero;
+#pragma unroll
+    for (int e = 0; e < E; ++e) zero.e[e] = from_float<O>(0.0f);
+    for (; unused; unused &= unused - 1) {
+        O *row = out + (r0 + __ffs(unused) - 1) * stride;
+        for (int j = lane * E; j < dim; j += 32 * E) store_pack<O, E>(row + j, zero);
+    }
+}
+
+// A warp moves one piece of ROWS_UNROLL * 32 packs of a token's row, read once, to the rows of its slots; the warps behind
+// those write zeros where no slot is.  Bound by memory.
+constexpr int ROWS_UNROLL = 4;
+
+template <typename T, typename O, int E>
+__global__ __launch_bounds__(256) void k_route_rows(const T *x, int64_t stride, int64_t n, int k, int dim, int pieces,
+                                                    const int32_t *place, const int32_t *source, int64_t rows,
+                                                    O *__restrict__ out, int64_t out_stride, int *status)
+{
+    after_previous();
+    const int lane = threadIdx.x & 31;
+    const int64_t copies = n * pieces, w = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
+    if (w >= copies) {
+        zero_unused<O, E>(source, (w - copies) * ZERO_ROWS, rows, dim, out, out_stride);
+        return;
+    }
+    const int64_t i = w / pieces;
+    const int piece = (int)(w - i * pieces), j0 = (piece * ROWS_UNROLL * 32 + lane) * E;
+    const T *from = x + i * stride;
+    Pack<T, E> v[ROWS_UNROLL];
+#pragma unroll
+    for (int u = 0; u < ROWS_UNROLL; ++u)
+        if (j0 + u * 32 * E < dim) v[u] = load_pack<T, E>(from + j0 + u * 32 * E);
+    Pack<O, E> y[ROWS_UNROLL];
+#pragma unroll
+    for (int u = 0; u < ROWS_UNROLL; ++u)
+#pragma unroll
+        for (int e = 0; e < E; ++e) y[u].e[e] = from_float<O>(to_float(v[u].e[e]));
+    for (int s0 = 0; s0 < k; s0 += 32) {
+        const int32_t mine = s0 + lane < k ? place[i * k + s0 + lane] : -1;
+        if (mine >= rows) set_status(status, PDB_ERANGE);
+        unsigned there = __ballot_sync(FULL, mine >= 0 && mine < rows);
+        for (; there; there &= there - 1) {
+            O *to = out + (int64_t)__shfl_sync(FULL, mine, __ffs(there) - 1) * out_stride;
+#pragma unroll
+            for (int u = 0; u < ROWS_UNROLL; ++u)
+                if (j0 + u * 32 * E < dim) store_pack<O, E>(to + j0 + u * 32 * E, y[u]);
+        }
+    }
+}
+
+// ------------------------------------------------------------------ and back
+// A warp sums one piece of JOIN_UNROLL * 32 packs of a token's row over its slots in ascending order, JOIN_SLOTS rows under way
+// at once.  Bound by memory.
+constexpr int JOIN_UNROLL = 2, JOIN_SLOTS = 4;
+
+template <typename T, typename O, int E>
+__global__ __launch_bounds__(256) void k_route_join(const T *in, int64_t stride, int64_t rows, int k, const int32_t *place,
+                                                    const float *weight, int64_t n, int dim, int pieces, O *__restrict__ out,
+                                                    int64_t out_stride, int *status)
+{
+    after_previous();
+    const int lane = threadIdx.x & 31;
+    const int64_t w = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5), i = w / pieces;
+    if (i >= n) return;
+    const int piece = (int)(w - i * pieces), j0 = (piece * JOIN_UNROLL * 32 + lane) * E;
+    float sum[JOIN_UNROLL][E];
+#pragma unroll
+    for (int u = 0; u < JOIN_UNROLL; ++u)
+#pragma unroll
+        for (int e = 0; e < E; ++e) sum[u][e] = 0.0f;
+    for (int s0 = 0; s0 < k; s0 += 32) {
+        const int32_t mine = s0 + lane < k ? place[i * k + s0 + lane] : -1;
+        const float wt = weight && s0 + lane < k ? weight[i * k + s0 + lane] : 1.0f;
+        if (mine >= rows) set_status(status, PDB_ERANGE);
+        unsigned there = __ballot_sync(FULL, mine >= 0 && mine < rows);
+        while (there) {
+            Pack<T, E> v[JOIN_SLOTS][JOIN_UNROLL];
+            float ws[JOIN_SLOTS];
+            const int batch = min(JOIN_SLOTS, __popc(there));
+#pragma unroll
+            for (int s = 0; s < JOIN_SLOTS; ++s) {
+                const int at = there ? __ffs(there) - 1 : 0;
+                ws[s] = __shfl_sync(FULL, wt, at);
+                const T *from = in + (int64_t)__shfl_sync(FULL, mine, at) * stride;
+                if (s < batch)
+#pragma unroll
+                    for (int u = 0; u < JOIN_UNROLL; ++u)
+                        if (j0 + u * 32 * E < dim) v[s][u] = load_pack<T, E>(from + j0 + u * 32 * E);
+                there &= there - 1;
+            }
+#pragma unroll
+            for (int s = 0; s < JOIN_SLOTS; ++s)
+                if (s < batch)
+#pragma unroll
+                    for (int u = 0; u < JOIN_UNROLL; ++u)
+#pragma unroll
+                        for (int e = 0; e < E; ++e) sum[u][e] = __fmaf_rn(ws[s], to_float(v[s][u].e[e]), sum[u][e]);
+        }
+    }
+#pragma unroll
+    for (int u = 0; u < JOIN_UNROLL; ++u) {
+        const int j = j0 + u * 32 * E;
+        if (j >= dim) break;
+        Pack<O, E> y;
+#pragma unroll
+        for (int e = 0; e < E; ++e) y.e[e] = from_float<O>(sum[u][e]);
+        store_pack<O, E>(out + i * out_stride + j, y);
+    }
+}
+
+// Gradients of the join: drows[p_j] = w_j dy, dw_j = <dy, rows[p_j]>.  `team` warps of a block (a power of two) have a token:
+// each holds its packs of dy and goes over the slots; the dot products are summed over its lanes, then over the
+// team's warps in order.  Bound by memory.  The warps of the blocks behind write zeros in rows that no slot takes.
+constexpr int GRAD_WARPS = 8, GRAD_UNROLL = 2, GRAD_SLOTS = 2;
+
+template <typename T, typename D, int E>
+__global__ __launch_bounds__(GRAD_WARPS * 32) void k_route_join_grad(const T *in, int64_t stride, int64_t rows, int k,
+                                                                     const int32_t *place, const int32_t *source,
+                                                                     const float *weight, const D *dy, int64_t dy_stride,
+                                                                     int64_t n, int dim, int team, int64_t token_blocks,
+                                                                     T *drows, int64_t out_stride, float *__restrict__ dweight,
+                                                                     int *status)
+{
+    after_previous();
+    __shared__ float s_dot[GRAD_WARPS][MAX_ROUTE_SLOTS];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    if (blockIdx.x >= token_blocks) {
+        const int64_t r0 = ((blockIdx.x - token_blocks) * GRAD_WARPS + warp) * ZERO_ROWS;
+        zero_unused<T, E>(source, r0, rows, dim, drows, out_stride);
+        return;
+    }
+    const int64_t first = (int64_t)blockIdx.x * (GRAD_WARPS / team), i = first + warp / team;
+    const int part = warp & (team - 1);
+    for (int j = lane; j < k; j += 32) s_dot[warp][j] = 0.0f;
+    __syncwarp();
+    if (i < n) {
+        // the slots' rows and weights, two for a lane
+        int32_t at[2];
+        float wt[2];
+        uint64_t there = 0;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int j = h * 32 + lane;
+            at[h] = j < k ? place[i * k + j] : -1;
+            wt[h] = weight && j < k ? weight[i * k + j] : 1.0f;
+            if (at[h] >= rows) set_status(status, PDB_ERANGE);
+            there |= (uint64_t)__ballot_sync(FULL, at[h] >= 0 && at[h] < rows) << (h * 32);
+        }
+        for (int c0 = part * (GRAD_UNROLL * 32 * E); c0 < dim; c0 += team * (GRAD_UNROLL * 32 * E)) {
+            const int j0 = c0 + lane * E;
+            float d[GRAD_UNROLL][E];
+#pragma unroll
+            for (int u = 0; u < GRAD_UNROLL; ++u) {
+                Pack<D, E> v;
+                if (j0 + u * 32 * E < dim) v = load_pack<D, E>(dy + i * dy_stride + j0 + u * 32 * E);
+#pragma unroll
+                for (int e = 0; e < E; ++e) d[u][e] = j0 + u * 32 * E < dim ? to_float(v.e[e]) : 0.0f;
+            }
+            for (uint64_t left = there; left;) {
+                Pack<T, E> v[GRAD_SLOTS][GRAD_UNROLL];
+                int slot[GRAD_SLOTS];
+                int64_t row[GRAD_SLOTS];
+                const int batch = min(GRAD_SLOTS, __popcll(left));
+#pragma unroll
+                for (int s = 0; s < GRAD_SLOTS; ++s) {
+                    slot[s] = left ? __ffsll((long long)left) - 1 : 0;
+                    left &= left - 1;
+                    const int32_t a = __shfl_sync(FULL, at[0], slot[s] & 31), b = __shfl_sync(FULL, at[1], slot[s] & 31);
+                    row[s] = slot[s] < 32 ? a : b;
+                    if (dweight && s < batch)
+#pragma unroll
+                        for (int u = 0; u < GRAD_UNROLL; ++u)
+                            if (j0 + u * 32 * E < dim) v[s][u] = load_pack<T, E>(in + row[s] * stride + j0 + u * 32 * E);
+                }
+                // drows may be the rows' own memory: what is loaded is loaded before anything is stored there
+                asm volatile("" ::: "memory");
+#pragma unroll
+                for (int s = 0; s < GRAD_SLOTS; ++s) {
+                    if (s >= batch) break;
+                    const float wa = __shfl_sync(FULL, wt[0], slot[s] & 31), wb = __shfl_sync(FULL, wt[1], slot[s] & 31);
+                    const float ws = slot[s] < 32 ? wa : wb;
+                    float dot = 0.0f;
+#pragma unroll
+                    for (int u = 0; u < GRAD_UNROLL; ++u) {
+                        const int j = j0 + u * 32 * E;
+                        if (j >= dim) break;
+                        Pack<T, E> y;
+#pragma unroll
+                        for (int e = 0; e < E; ++e) {
+                            if (dweight) dot = __fmaf_rn(d[u][e], to_float(v[s][u].e[e]), dot);
+                            y.e[e] = from_float<T>(__fmul_rn(ws, d[u][e]));
+                        }
+                        store_pack<T, E>(drows + row[s] * out_stride + j, y);
+                    }
+                    if (dweight) {
+#pragma unroll
+                        for (int off = 16; off >= 1; off >>= 1) dot = __fadd_rn(dot, __shfl_xor_sync(FULL, dot, off));
+                        if (lane == 0) s_dot[warp][slot[s]] = __fadd_rn(s_dot[warp][slot[s]], dot);
+                    }
+                }
+            }
+        }
+    }
+    if (!dweight) return;
+    __syncthreads();
+    for (int x = threadIdx.x; x < GRAD_WARPS / team * k; x += GRAD_WARPS * 32) {
+        const int who = x / k, j = x - who * k;
+        if (first + who >= n) break;
+        float sum = s_dot[who * team][j];
+        for (int p = 1; p < team; ++p) sum = __fadd_rn(sum, s_dot[who * team + p][j]);
+        dweight[(first + who) * k + j] = sum;
+    }
+}
+
+// n tokens of k slots each and their places, or PDB_EINVAL
+int check_places(int64_t n, int64_t k, const int32_t *place)
+{
+    if (k < 1) return PDB_EINVAL;
+    if (k > MAX_ROUTE_SLOTS) return PDB_ETOOBIG;
+    if (n > 0 && (!place || (uintptr_t)place % 4 != 0)) return PDB_EINVAL;
+    return n * k > INT32_MAX ? PDB_ETOOBIG : PDB_OK;
+}
+int check_words(const void *p, int64_t n) { return n > 0 && (!p || (uintptr_t)p % 4 != 0) ? PDB_EINVAL : PDB_OK; }
+
+int64_t zero_warps(int64_t rows, int dim) { return dim > 0 ? (rows + ZERO_ROWS - 1) / ZERO_ROWS : 0; }
+
+}  // namespace
+
+extern "C" {
+
+int pdb_route(pdb_tokens *t, const pdb_ids *ids, int64_t k, int64_t n_experts, int64_t capacity, int32_t *place,
+              int32_t *source, int32_t *ends, void *stream)
+{
+    ApiScope scope("pdb_route", nullptr, nullptr, nullptr, nullptr, false);
+    if (!t || !ids || k < 1 || n_experts < 1 || capacity < 0 || ids->n < 0 || ids->n % k != 0) return PDB_EINVAL;
+    const int64_t n = ids->n / k;
+    if (k > MAX_ROUTE_SLOTS || n_experts > MAX_EXPERTS || ids->n > INT32_MAX || capacity > INT32_MAX / n_experts)
+        return PDB_ETOOBIG;
+    const int64_t rows = capacity ? capacity * n_experts : ids->n;
+    int rc = check_ids(ids, n, k);
+    rc = rc ? rc : check_words(place, ids->n);
+    rc = rc ? rc : check_words(source, rows);
+    rc = rc ? rc : check_words(ends, n_experts);
+    if (rc != PDB_OK) return rc;
+    if (ids->n > t->max_tokens) return PDB_ETOOBIG;
+    if ((rc = check_device(t)) != PDB_OK) return rc;
+    cudaStream_t s = (cudaStream_t)stream;
+    TokensUse use{t, s};
+    const Slots slots{{ids->data, n > 1 ? ids->stride : 0, ids->wide}, (uint32_t)ids->n, (uint32_t)k, (int)n_experts};
+    const auto run = [&](auto ipt) {
+        constexpr int IPT = decltype(ipt)::value;
+        const int64_t blocks = std::max<int64_t>(1, (ids->n + ROUTE_THREADS * IPT - 1) / (ROUTE_THREADS * IPT));
+        // the blocks' counts: no more words than slots, since blocks * experts <= slots where there are two blocks or more
+        int got = PDB_OK;
+        if (blocks > 1) got = launch(k_route_count<IPT>, blocks, ROUTE_THREADS, sizeof(uint32_t) * n_experts, 1, s, slots, t->skey, t->status);
+        if (got != PDB_OK) return got;
+        if (!allow_smem((const void *)k_route_place<IPT>)) return (int)PDB_ECUDA;
+        return launch(k_route_place<IPT>, blocks, ROUTE_THREADS, place_smem((int)n_experts), 1, s, slots, t->skey, capacity,
+                      place, source, ends, t->status);
+    };
+    // blocks of 2048 slots while there are few of them: each adds up the counts of all
+    return n_experts <= 1024 && ids->n <= 2048 * (int64_t)t->sms ? run(Num<4>()) : run(Num<16>());
+}
+
+int pdb_route_rows(pdb_tokens *t, const pdb_mat *x, const int32_t *place, int64_t k, const int32_t *source,
+                   const pdb_mat *rows, void *stream)
+{
+    ApiScope scope("pdb_route_rows", nullptr, nullptr, nullptr, nullptr, false);
+    if (!t) return PDB_EINVAL;
+    int rc = check_mat(x);
+    rc = rc ? rc : check_mat(rows);
+    rc = rc ? rc : check_places(x->rows, k, place);
+    rc = rc ? rc : check_words(source, rows->rows);
+    if (rc != PDB_OK) return rc;
+    if (x->cols != rows->cols || overlap(x, rows)) return PDB_EINVAL;
+    const int dim = (int)x->cols;
+    if (dim == 0 || rows->rows == 0) return PDB_OK;
+    if ((rc = check_device(t)) != PDB_OK) return rc;
+    cudaStream_t s = (cudaStream_t)stream;
+    TokensUse use{t, s};
+    const auto run = [&](auto *a, auto *b, auto e) {
+        using T = std::remove_pointer_t<decltype(a)>;
+        using O = std::remove_pointer_t<decltype(b)>;
+        constexpr int E = decltype(e)::value;
+        const int pieces = (dim + ROWS_UNROLL * 32 * E - 1) / (ROWS_UNROLL * 32 * E);
+        const int64_t blocks = (x->rows * pieces + zero_warps(rows->rows, dim) + 7) / 8;
+        if (blocks > INT32_MAX) return (int)PDB_ETOOBIG;
+        return launch(k_route_rows<T, O, E>, blocks, 256, 0, 1, s, (const T *)x->data, stride_of(x), x->rows, (int)k, dim, pieces,
+                      place, source, rows->rows, (O *)rows->data, stride_of(rows), t->status);
+    };
+    return with_type(x->type, [&](auto *a) {
+        return with_type(rows->type, [&](auto *b) {
+            // the widest moves that the columns' number and both matrices' alignment allow
+            if (fits(x, 8) && fits(rows, 8)) return run(a, b, Num<8>());
+            if (fits(x, 4) && fits(rows, 4)) return run(a, b, Num<4>());
+            return run(a, b, Num<1>());
+        });
+    });
+}
+
+int pdb_route_join(pdb_tokens *t, const pdb_mat *rows, const int32_t *place, int64_t k, const float *weight,
+                   const pdb_mat *y, void *stream)
+{
+    ApiScope scope("pdb_route_join", nullptr, nullptr, nullptr, nullptr, false);
+    if (!t) return PDB_EINVAL;
+    int rc = check_mat(rows);
+    rc = rc ? rc : check_mat(y);
+    rc = rc ? rc : check_places(y->rows, k, place);
+    if (rc == PDB_OK && weight) rc = check_words(weight, y->rows * k);
+    if (rc != PDB_OK) return rc;
+    if (y->cols != rows->cols || overlap(rows, y)) return PDB_EINVAL;
+    const int dim = (int)y->cols;
+    if (dim == 0 || y->rows == 0) return PDB_OK;
+    if ((rc = check_device(t)) != PDB_OK) return rc;
+    cudaStream_t s = (cudaStream_t)stream;
+    TokensUse use{t, s};
+    const auto run = [&](auto *a, auto *b, auto e) {
+        using T = std::remove_pointer_t<decltype(a)>;
+        using O = std::remove_pointer_t<decltype(b)>;
+        constexpr int E = decltype(e)::value;
+        const int pieces = (dim + JOIN_UNROLL * 32 * E - 1) / (JOIN_UNROLL * 32 * E);
+        const int64_t blocks = (y->rows * pieces + 7) / 8;
+        if (blocks > INT32_MAX) return (int)PDB_ETOOBIG;
+        return launch(k_route_join<T, O, E>, blocks, 256, 0, 1, s, (const T *)rows->data, stride_of(rows), rows->rows, (int)k,
+                      place, weight, y->rows, dim, pieces, (O *)y->data, stride_of(y), t->status);
+    };
+    return with_type(rows->type, [&](auto *a) {
+        return with_type(y->type, [&](auto *b) {
+            constexpr int E = 16 / sizeof(*a);
+            if (fits(rows, E) && fits(y, E)) return run(a, b, Num<E>());
+            if (fits(rows, E / 2) && fits(y, E / 2)) return run(a, b, Num<E / 2>());
+            return run(a, b, Num<1>());
+        });
+    });
+}
+
+int pdb_route_join_grad(pdb_tokens *t, const pdb_mat *rows, const int32_t *place, int64_t k, const int32_t *source,
+                        const float *weight, const pdb_mat *dy, const pdb_mat *drows, float *dweight, void *stream)
+{
+    ApiScope scope("pdb_route_join_grad", nullptr, nullptr, nullptr, nullptr, false);
+    if (!t || (dweight && !rows)) return PDB_EINVAL;
+    int rc = rows ? check_mat(rows) : PDB_OK;
+    rc = rc ? rc : check_mat(dy);
+    rc = rc ? rc : check_mat(drows);
+    rc = rc ? rc : check_places(dy->rows, k, place);
+    rc = rc ? rc : check_words(source, drows->rows);
+    if (rc == PDB_OK && weight) rc = check_words(weight, dy->rows * k);
+    if (rc == PDB_OK && rows) rc = check_words(dweight, dy->rows * k);
+    if (rc != PDB_OK) return rc;
+    if (dy->cols != drows->cols || overlap(dy, drows)) return PDB_EINVAL;
+    if (rows && (rows->rows != drows->rows || rows->cols != drows->cols || rows->type != drows->type ||
+                 !same_or_apart(rows, drows)))
+        return PDB_EINVAL;
+    const int dim = (int)dy->cols;
+    if (dy->rows == 0 && (drows->rows == 0 || dim == 0)) return PDB_OK;
+    if ((rc = check_device(t)) != PDB_OK) return rc;
+    cudaStream_t s = (cudaStream_t)stream;
+    TokensUse use{t, s};
+    const auto run = [&](auto *a, auto *b, auto e) {
+        using T = std::remove_pointer_t<decltype(a)>;
+        using D = std::remove_pointer_t<decltype(b)>;
+        constexpr int E = decltype(e)::value;
+        int team = 1;
+        while (team < GRAD_WARPS && team * GRAD_UNROLL * 32 * E < dim) team *= 2;
+        const int64_t token_blocks = (dy->rows + GRAD_WARPS / team - 1) / (GRAD_WARPS / team);
+        const int64_t blocks = token_blocks + (zero_warps(drows->rows, dim) + GRAD_WARPS - 1) / GRAD_WARPS;
+        if (blocks > INT32_MAX) return (int)PDB_ETOOBIG;
+        return launch(k_route_join_grad<T, D, E>, blocks, GRAD_WARPS * 32, 0, 1, s, rows ? (const T *)rows->data : (const T *)nullptr,
+                      rows ? stride_of(rows) : 0, drows->rows, (int)k, place, source, weight, (const D *)dy->data, stride_of(dy),
+                      dy->rows, dim, team, token_blocks, (T *)drows->data, stride_of(drows), dweight, t->status);
+    };
+    return with_type(drows->type, [&](auto *a) {
+        return with_type(dy->type, [&](auto *b) {
+            constexpr int E = 16 / sizeof(*a);
+            const auto all_fit = [&](int n) { return fits(dy, n) && fits(drows, n) && (!rows || fits(rows, n)); };
+            if (all_fit(E)) return run(a, b, Num<E>());
+            if (all_fit(E / 2)) return run(a, b, Num<E / 2>());
+            return run(a, b, Num<1>());
+        });
+    });
+}
+
+}  // extern "C"

@@ -27,17 +27,20 @@ struct pdb_tokens {
 
 namespace pdb {
 
-// every call on a handle records ev_use when it returns; not while a graph is
+// every call on a handle records its event when it returns; not while a graph is
 // recorded, whose event could not be waited for (the graph's owner keeps the handle)
-struct TokensUse {
-    const pdb_tokens *t;
+struct HandleUse {
+    cudaEvent_t ev_use;
     cudaStream_t s;
-    ~TokensUse()
+    ~HandleUse()
     {
         cudaStreamCaptureStatus capturing = cudaStreamCaptureStatusNone;
         if (cudaStreamIsCapturing(s, &capturing) != cudaSuccess || capturing != cudaStreamCaptureStatusNone) return;
-        if (t->ev_use) cudaEventRecord(t->ev_use, s);
+        if (ev_use) cudaEventRecord(ev_use, s);
     }
+};
+struct TokensUse : HandleUse {
+    TokensUse(const pdb_tokens *t, cudaStream_t stream) : HandleUse{t->ev_use, stream} {}
 };
 
 // lets a kernel have all of an SM's shared memory as dynamic one; once per kernel and device

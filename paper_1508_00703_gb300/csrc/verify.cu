@@ -1,0 +1,509 @@
+// Drafted tokens verified against the target's probabilities (pdb_verify).
+//
+// A sequence has D drafted tokens t_d, target logits z_0 .. z_D, draft logits y_0 .. y_{D-1}; p_d = softmax(scale z_d),
+// q_d = softmax(draft_scale y_d).  Position after position, while u_d q_d(t_d) < p_d(t_d), the draft is accepted; where it is not
+// (or the drafts end) the token is drawn from r = max(p - q, 0) (or r = p): the smallest j with r_0 + .. + r_j > v sum r.
+// The tokens are then distributed as if drawn from p one after the other (Leviathan, Kalman, Matias 2023; Chen et al. 2023).
+//
+// One cluster of blocks walks a sequence's positions, so no row behind the first refusal is read.  A position's rows take one pass of
+// running softmax statistics (rows.cuh).  Which token comes out must not hang on how a row is split or on 32-bit rounding: a
+// draft whose two sides lie closer than those statistics can tell, and every draw, are decided on numbers good to about 2^-42
+// (exp_two), summed as integers.
+#include <algorithm>
+#include <cmath>
+
+#include "rows.cuh"
+
+using namespace pdb;
+namespace cg = cooperative_groups;
+
+namespace {
+
+constexpr int MAX_DRAFTS = 64;
+constexpr int64_t MAX_VOCAB = 1 << 21;
+constexpr int PIECE = 256;              // tokens whose weights are summed together
+
+// ------------------------------------------------------------------ exp in two floats
+// e^x = 2^k 2^(i/256) e^r with 256 k + i = rint(256 x / ln 2) and |r| <= ln 2 / 512 (table-driven, after Tang 1989), x and the
+// result each the sum of two floats: the table holds 2^(i/256) to 2^-48, e^r = 1 + r + r^2/2 + r^3/6 + r^4/24 leaves 2^-52, and the
+// rounding of r^2/2 <= 2^-20.1 is 2^-44 of the result.
+constexpr double LN2_D = 0.693147180559945309417232121458;
+
+constexpr double exp_series(double x)
+{
+    double term = 1.0, sum = 1.0;
+    for (int i = 1; i < 30; ++i) term = term * x / i, sum += term;
+    return sum;
+}
+struct Exp2Table {
+    float hi[256], lo[256];
+    constexpr Exp2Table() : hi(), lo()
+    {
+        for (int i = 0; i < 256; ++i) {
+            const double v = exp_series(LN2_D * i / 256);
+            hi[i] = (float)v;
+            lo[i] = (float)(v - (double)(float)v);
+        }
+    }
+};
+__device__ const Exp2Table EXP2_TABLE;
+
+// ln 2 / 256 in four parts, the first three of 9 bits, so that their products with n of up to 15 bits are exact
+constexpr double LN2_STEP = LN2_D / 256;
+constexpr float STEP_1 = (float)((double)(int64_t)(LN2_STEP * 0x1p17) * 0x1p-17);
+constexpr float STEP_2 = (float)((double)(int64_t)((LN2_STEP - (double)STEP_1) * 0x1p26) * 0x1p-26);
+constexpr float STEP_3 = (float)((double)(int64_t)((LN2_STEP - (double)STEP_1 - (double)STEP_2) * 0x1p35) * 0x1p-35);
+constexpr float STEP_4 = (float)(LN2_STEP - (double)STEP_1 - (double)STEP_2 - (double)STEP_3);
+constexpr float PER_STEP = (float)(256 / LN2_D);
+
+struct Two {
+    float hi, lo;                       // hi + lo, |lo| <= ulp(hi)
+};
+
+// exp(scale * (z - m)), z <= m; 0 below e^-45 (a part of 2^-64 of the row's sum)
+__device__ __forceinline__ Two exp_two(float z, float m, float scale, const float2 *table)
+{
+    // z - m and its product with scale, exactly but for the last 2^-48
+    const float d = __fsub_rn(z, m), b = __fsub_rn(d, z);
+    const float dl = __fsub_rn(__fsub_rn(z, __fsub_rn(d, b)), __fadd_rn(m, b));
+    const float x = __fmul_rn(d, scale);
+    const float xl = __fmaf_rn(dl, scale, __fmaf_rn(d, scale, -x));
+    if (!(x >= -45.0f)) return {0.0f, 0.0f};
+    const float t = __fadd_rn(__fmul_rn(x, PER_STEP), 12582912.0f);       // 1.5 * 2^23: rounds to a whole number
+    const int n = __float_as_int(t) - 0x4b400000;
+    const float nf = __fsub_rn(t, 12582912.0f);
+    // r = x - n ln2/256: exact as far as 2^-35 goes, what that leaves out in rl
+    const float r2 = __fmaf_rn(-nf, STEP_2, __fmaf_rn(-nf, STEP_1, x));
+    const float r = __fmaf_rn(-nf, STEP_3, r2);
+    const float rl = __fadd_rn(__fmaf_rn(-nf, STEP_3, __fsub_rn(r2, r)), __fmaf_rn(-nf, STEP_4, xl));
+    // e^r - 1 = r + w
+    const float q = __fmaf_rn(r, __fmaf_rn(r, 1.0f / 24.0f, 1.0f / 6.0f), 0.5f);
+    const float w = __fmaf_rn(__fmul_rn(r, r), q, __fmaf_rn(rl, r, rl));
+    const float2 tab = table[n & 255];
+    const float ph = __fmul_rn(tab.x, r), pl = __fmaf_rn(tab.x, r, -ph);
+    const float low = __fadd_rn(pl, __fmaf_rn(tab.x, w, __fmaf_rn(tab.y, r, tab.y)));
+    const float h = __fadd_rn(tab.x, ph), hl = __fadd_rn(__fsub_rn(tab.x, h), ph);
+    const float power = __int_as_float(((n >> 8) + 127) << 23);
+    const float l = __fadd_rn(hl, low);
+    return {__fmul_rn(h, power), __fmul_rn(l, power)};
+}
+
+__device__ __forceinline__ Two times(Two a, Two b)
+{
+    const float h = __fmul_rn(a.hi, b.hi);
+    return {h, __fadd_rn(__fmaf_rn(a.hi, b.hi, -h), __fmaf_rn(a.hi, b.lo, __fmul_rn(a.lo, b.hi)))};
+}
+__device__ __forceinline__ Two two_of(double x)
+{
+    const float h = (float)x;
+    return {h, (float)(x - (double)h)};
+}
+// in units of 1 / unit, a power of two
+__device__ __forceinline__ int64_t whole_of(Two a, float unit)
+{
+    return __float2ll_rn(__fmul_rn(a.hi, unit)) + __float2ll_rn(__fmul_rn(a.lo, unit));
+}
+
+// ------------------------------------------------------------------ shared by the blocks of a sequence
+struct Shared {
+    float stat[2][4];                   // this block's m, s of the target's and the draft's row, for two positions in turn
+    float part[2][96];
+    int64_t warp_sum[2][16];
+    int64_t sum[2][2];                  // this block's exact sums of the two rows: 2^20 times the first, and the second
+    double row_sum[2];                  // the rows' exact sums
+    float2 row_inv[2];                  // their reciprocals
+    int64_t total;                      // this block's weights
+    int64_t at, before;                 // the drawn place among all weights, the weights of lower blocks
+    int64_t below;                      // weights before the piece that holds the drawn token
+    int none, piece, good;
+    float2 table[256];
+    int64_t weight[1];                  // of each of the block's pieces (as many as there are)
+};
+
+// one row of a position
+template <typename T>
+struct Row {
+    const T *z;
+    float scale, m, s;                  // its maximum, sum of exp(scale (z - m))
+    __device__ __forceinline__ bool valid() const { return s > 0.0f && s < INFINITY; }
+};
+
+template <typename T, int THREADS>
+__device__ __forceinline__ void share_stat(const Row<T> &row, int cols, int rank, int blocks, float *part, float *to)
+{
+    const float c = __fmul_rn(row.scale, LOG2E);
+    const Share sh = share_of(row.z, cols, rank, blocks);
+    const uint4 *body = reinterpret_cast<const uint4 *>(row.z + sh.b0);
+    const int n_vec = sh.v1 - sh.v0;
+    Stat<false> a;
+    float top = -INFINITY;
+    uint4 v[UNROLL];
+    load_vectors<T, THREADS, 32>(v, body, 0, lane_start(), n_vec);
+    const bool has_edge = (int)threadIdx.x < sh.edges();
+    T z_edge = from_float<T>(0.0f);
+    if (has_edge) z_edge = row.z[sh.edge(threadIdx.x)];
+    for (int base = 0; base < n_vec; base += THREADS * UNROLL) {
+        uint4 next[UNROLL];
+        load_vectors<T, THREADS, 32>(next, body, base + THREADS * UNROLL, lane_start(), n_vec);
+        add_vectors<T, false>(a, v, c, top);
+#pragma unroll
+        for (int u = 0; u < UNROLL; ++u) v[u] = next[u];
+    }
+    if (has_edge) add_element(a, to_float(z_edge), c);
+    a.rebase(fmaxf(a.m, top), c);        // to the maximum itself
+    block_join<THREADS>(a, c, part);
+    if (threadIdx.x == 0) to[0] = a.m, to[1] = a.s;
+}
+
+template <typename T, int THREADS>
+struct Walk {
+    Shared &sh;
+    cg::cluster_group cluster;
+    int rank, blocks, cols;
+    int first_piece, pieces;            // the block's
+
+    // m and s of the target's row, and of the draft's where it has one, over the cluster: the same on all its threads
+    __device__ __forceinline__ void stats(Row<T> &p, Row<T> &q, int turn)
+    {
+        share_stat<T, THREADS>(p, cols, rank, blocks, sh.part[0], sh.stat[turn]);
+        if (q.z) share_stat<T, THREADS>(q, cols, rank, blocks, sh.part[1], sh.stat[turn] + 2);
+        cluster.sync();
+        join(p, turn, 0);
+        if (q.z) join(q, turn, 2);
+    }
+    __device__ __forceinline__ void join(Row<T> &row, int turn, int at)
+    {
+        const float c = __fmul_rn(row.scale, LOG2E);
+        Stat<false> a;
+        for (int b = 0; b < blocks; ++b) {
+            const float *o = cluster.map_shared_rank(sh.stat[turn], b) + at;
+            a.join(o[0], o[1], 0.0f, c);
+        }
+        row.m = a.m, row.s = a.s;
+    }
+
+    // f(token, its place in the lane's order) of the lanes' tokens of a piece
+    template <typename F>
+    __device__ __forceinline__ void each_of(int piece, F f)
+    {
+        const int lane = threadIdx.x & 31;
+#pragma unroll
+        for (int u = 0; u < PIECE / 32; ++u) {
+            const int j = piece * PIECE + u * 32 + lane;
+            if (j < cols) f(j, u);
+        }
+    }
+
+    // sums of the warps' numbers, on thread 0
+    __device__ __forceinline__ int64_t block_sum(int64_t x, int64_t *part)
+    {
+#pragma unroll
+        for (int off = 16; off >= 1; off >>= 1) x += __shfl_xor_sync(FULL, x, off);
+        if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = x;
+        __syncthreads();
+        if (threadIdx.x == 0)
+            for (int w = 1; w < THREADS / 32; ++w) x += part[w];
+        return x;
+    }
+
+    // The rows' sums good to 2^-42, into sh.row_sum and sh.row_inv.  A thread's part is an integer in units that its number of
+    // tokens leaves room for; threads and blocks add up the two ends of theirs apart, so that nothing is lost and no order matters.
+    __device__ __forceinline__ void exact_sums(const Row<T> &p, const Row<T> &q, int all_pieces)
+    {
+        constexpr int W = THREADS / 32;
+        const int warp = threadIdx.x >> 5;
+        const int most = ((all_pieces + blocks - 1) / blocks + W - 1) / W * (PIECE / 32);    // tokens of a thread
+        const int bits = 62 - (32 - __clz(most));
+        const float unit = __int_as_float((bits + 127) << 23);
+#pragma unroll 1
+        for (int which = 0; which < (q.z ? 2 : 1); ++which) {
+            const T *z = which ? q.z : p.z;
+            const float m = which ? q.m : p.m, scale = which ? q.scale : p.scale;
+            int64_t sum = 0;
+#pragma unroll 1
+            for (int i = warp; i < pieces; i += W)
+                each_of(first_piece + i, [&](int j, int) { sum += whole_of(exp_two(to_float(z[j]), m, scale, sh.table), unit); });
+            const int64_t high = block_sum(sum >> 20, sh.warp_sum[0]), low = block_sum(sum & 0xfffff, sh.warp_sum[1]);
+            if (threadIdx.x == 0) sh.sum[which][0] = high, sh.sum[which][1] = low;
+            __syncthreads();
+        }
+        cluster.sync();
+        if (threadIdx.x == 0) {
+#pragma unroll 1
+            for (int which = 0; which < (q.z ? 2 : 1); ++which) {
+                int64_t high = 0, low = 0;
+                for (int b = 0; b < blocks; ++b) {
+                    const int64_t *o = cluster.map_shared_rank(&sh, b)->sum[which];
+                    high += o[0], low += o[1];
+                }
+                const double x = __fma_rn((double)high, 0x1p20, (double)low) * (double)__int_as_float((127 - bits) << 23);
+                const Two inv = two_of(1.0 / x);
+                sh.row_sum[which] = x;
+                sh.row_inv[which] = {inv.hi, inv.lo};
+            }
+        }
+        cluster.sync();                  // the others' sums have been read
+    }
+
+    // a token's weight in a draw, in units of 2^-60
+    struct Weights {
+        Row<T> p, q;
+        Two p_inv, q_inv;
+        int without;                     // a token left out
+        const float2 *table;
+        __device__ __forceinline__ int64_t operator()(int j) const
+        {
+            Two a = times(exp_two(to_float(p.z[j]), p.m, p.scale, table), p_inv);
+            if (q.z) {
+                const Two b = times(exp_two(to_float(q.z[j]), q.m, q.scale, table), q_inv);
+                const float d = __fsub_rn(a.hi, b.hi), e = __fsub_rn(d, a.hi);
+                const float dl = __fsub_rn(__fsub_rn(a.hi, __fsub_rn(d, e)), __fadd_rn(b.hi, e));
+                a = {d, __fadd_rn(dl, __fsub_rn(a.lo, b.lo))};
+            }
+            const int64_t w = whole_of(a, 0x1p60f);
+            return j == without || w < 0 ? 0 : w;
+        }
+    };
+
+    // floor(v * total), total - 1 at most (v from 1 on), 0 for a v below 0 or NaN
+    static __device__ __forceinline__ int64_t share_of_total(float v, int64_t total)
+    {
+        if (!(v > 0.0f)) return 0;
+        if (v >= 1.0f) return total - 1;
+        const uint32_t raw = __float_as_uint(v), e = raw >> 23;
+        const uint64_t digits = e ? (raw & 0x7fffff) | 0x800000 : raw & 0x7fffff;      // v = digits / 2^shift
+        const int shift = 150 - (int)max(e, 1u);
+        const uint64_t high = __umul64hi(digits, (uint64_t)total), low = digits * (uint64_t)total;
+        return (int64_t)(shift < 64 ? high << (64 - shift) | low >> shift : shift < 128 ? high >> (shift - 64) : 0);
+    }
+
+    // The smallest token whose running sum of weights passes v times all of them: on the thread that finds it, -1 on the others.
+    // Sets sh.none where no token has a weight.
+    __device__ __forceinline__ int draw(const Weights &weight, float v)
+    {
+        constexpr int W = THREADS / 32;
+        const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+        int64_t all = 0;                 // on lane 0
+#pragma unroll 1
+        for (int i = warp; i < pieces; i += W) {
+            int64_t sum = 0;
+            each_of(first_piece + i, [&](int j, int) { sum += weight(j); });
+#pragma unroll
+            for (int off = 16; off >= 1; off >>= 1) sum += __shfl_xor_sync(FULL, sum, off);
+            if (lane == 0) sh.weight[i] = sum, all += sum;
+        }
+        all = block_sum(all, sh.warp_sum[0]);
+        if (threadIdx.x == 0) sh.total = all;
+        cluster.sync();
+        if (threadIdx.x == 0) {
+            int64_t before = 0, total = 0;
+            for (int b = 0; b < blocks; ++b) {
+                const int64_t x = cluster.map_shared_rank(&sh, b)->total;
+                if (b < rank) before += x;
+                total += x;
+            }
+            sh.none = total <= 0;
+            sh.before = before;
+            sh.at = share_of_total(v, total);
+        }
+        cluster.sync();                  // the others' totals have been read
+        int found = -1;
+        const int64_t at = sh.at, before = sh.before;
+        if (warp == 0 && !sh.none && at >= before && at < before + sh.total) {
+            // a lane's run of pieces, then its pieces
+            const int each = (pieces + 31) / 32, i0 = min(pieces, lane * each), i1 = min(pieces, i0 + each);
+            int64_t mine = 0;
+            for (int i = i0; i < i1; ++i) mine += sh.weight[i];
+            int64_t up = mine;
+#pragma unroll
+            for (int off = 1; off < 32; off <<= 1) {
+                const int64_t x = __shfl_up_sync(FULL, up, off);
+                if (lane >= off) up += x;
+            }
+            int64_t below = before + up - mine;
+            if (at >= below && at < below + mine) {
+                int i = i0;
+                while (at >= below + sh.weight[i]) below += sh.weight[i++];
+                sh.piece = first_piece + i;
+                sh.below = below;
+            }
+            __syncwarp();
+            int64_t w[PIECE / 32];
+#pragma unroll
+            for (int u = 0; u < PIECE / 32; ++u) w[u] = 0;
+            each_of(sh.piece, [&](int j, int u) { w[u] = weight(j); });
+            int64_t sum = sh.below;
+#pragma unroll
+            for (int u = 0; u < PIECE / 32; ++u) {
+                int64_t upto = w[u];
+#pragma unroll
+                for (int off = 1; off < 32; off <<= 1) {
+                    const int64_t x = __shfl_up_sync(FULL, upto, off);
+                    if (lane >= off) upto += x;
+                }
+                if (at >= sum + upto - w[u] && at < sum + upto) found = sh.piece * PIECE + u * 32 + lane;
+                sum += __shfl_sync(FULL, upto, 31);
+            }
+        }
+        return found;
+    }
+};
+
+struct VerifyOut {
+    int32_t *tokens, *accepted;
+    float *logp;
+};
+
+// How far the two sides of an acceptance must lie apart for the statistics in 32 bits to decide it.  Their exponentials' arguments
+// x (in powers of two) are off by 2.1 |x| 2^-24 with |x| < 126 where they count, sums by the mean of that and their roundings: 2^-14.
+constexpr float SURE = 0x1p-12f;
+
+template <typename T, int THREADS>
+__global__ __launch_bounds__(THREADS) void k_verify(const T *target, int64_t t_stride, const T *draft, int64_t d_stride, int cols,
+                                                    Ids ids, int D, float scale, float draft_scale, const float *accept_u,
+                                                    const float *draw_u, VerifyOut out, int *status)
+{
+    after_previous();
+    extern __shared__ __align__(16) unsigned char s_raw[];
+    Shared &sh = *reinterpret_cast<Shared *>(s_raw);
+    cg::cluster_group cluster = cg::this_cluster();
+    const int blocks = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
+    const int64_t s = blockIdx.x / (unsigned)blocks;
+    const int all = (cols + PIECE - 1) / PIECE;
+    const int p0 = (int)((int64_t)all * rank / blocks), p1 = (int)((int64_t)all * (rank + 1) / blocks);
+    Walk<T, THREADS> walk{sh, cluster, rank, blocks, cols, p0, p1 - p0};
+    for (int i = threadIdx.x; i < 256; i += THREADS) sh.table[i] = {EXP2_TABLE.hi[i], EXP2_TABLE.lo[i]};
+    const bool writes = rank == 0 && threadIdx.x == 0;
+    const int64_t base = s * (D + 1);
+
+    Row<T> p{}, q{};
+    p.scale = scale, q.scale = draft_scale;
+    int a = 0;
+    bool refused = false;
+    int64_t t = -1;
+    float log_s = 0.0f;
+#pragma unroll 1
+    for (;; ++a) {
+        t = a < D ? load_id(ids, s, a) : -1;
+        if (t >= cols) {
+            if (writes) set_status(status, PDB_ERANGE);
+            t = -1;
+        }
+        p.z = target + (base + a) * t_stride;
+        q.z = t >= 0 && draft ? draft + (s * D + a) * d_stride : nullptr;
+        walk.stats(p, q, a & 1);
+        if (!p.valid()) break;
+        log_s = logf(p.s);
+        if (q.z && !q.valid()) t = -1;
+        if (t < 0) q.z = nullptr;        // the drafts end here
+        float z = 0.0f, u = 0.0f;
+        bool good = false, sure = true;
+        if (t >= 0) {
+            z = to_float(p.z[t]), u = accept_u[s * D + a];
+            const float right = __fdiv_rn(ex2(__fmul_rn(__fsub_rn(z, p.m), __fmul_rn(scale, LOG2E))), p.s);
+            float left = u;
+            if (q.z)
+                left = __fmul_rn(u, __fdiv_rn(ex2(__fmul_rn(__fsub_rn(to_float(q.z[t]), q.m), __fmul_rn(draft_scale, LOG2E))), q.s));
+            const float more = fmaxf(left, right);
+            good = left < right;
+            sure = fabsf(left - right) > SURE * more && more > 1e-30f;
+        }
+        if (!good || !sure) {
+            walk.exact_sums(p, q, all);
+            if (!sure) {
+                if (threadIdx.x == 0) {
+                    const double pe = exp((double)scale * ((double)z - (double)p.m)) / sh.row_sum[0];
+                    const double qe = q.z ? exp((double)draft_scale * ((double)to_float(q.z[t]) - (double)q.m)) / sh.row_sum[1] : 1.0;
+                    sh.good = (double)u * qe < pe;
+                }
+                __syncthreads();
+                good = sh.good;
+            }
+            if (!good) {
+                refused = t >= 0;
+                break;
+            }
+        }
+        if (writes) {
+            out.tokens[base + a] = (int32_t)t;
+            if (out.logp) out.logp[base + a] = __fmaf_rn(__fsub_rn(z, p.m), scale, -log_s);
+        }
+    }
+    int drawn = -1;
+    bool none = !p.valid();
+    if (!none) {
+        typename Walk<T, THREADS>::Weights weight{p, q, {sh.row_inv[0].x, sh.row_inv[0].y}, {sh.row_inv[1].x, sh.row_inv[1].y},
+                                                  refused && !q.z ? (int)t : -1, sh.table};
+#pragma unroll 1
+        for (;;) {
+            drawn = walk.draw(weight, draw_u[s]);
+            none = sh.none;
+            if (!none || !refused) break;
+            // nothing of p - q that 2^-60 could tell: from p
+            refused = false, weight.q.z = nullptr, weight.without = -1;
+            __syncthreads();
+        }
+    }
+    if (drawn >= 0) {
+        out.tokens[base + a] = drawn;
+        if (out.logp) out.logp[base + a] = __fmaf_rn(__fsub_rn(to_float(p.z[drawn]), p.m), scale, -log_s);
+    }
+    if (writes) {
+        if (out.accepted) out.accepted[s] = a;
+        for (int d = none ? a : a + 1; d <= D; ++d) {
+            out.tokens[base + d] = -1;
+            if (out.logp) out.logp[base + d] = 0.0f;
+        }
+    }
+    cluster.sync();                      // nobody reads this block's shared memory any more
+}
+
+size_t verify_smem(int64_t cols, int blocks)
+{
+    return sizeof(Shared) + sizeof(int64_t) * (((cols + PIECE - 1) / PIECE + blocks - 1) / blocks + 1);
+}
+
+}  // namespace
+
+extern "C" {
+
+int pdb_verify(pdb_tokens *t, const pdb_mat *target, const pdb_ids *draft_ids, int64_t n_drafts, const pdb_mat *draft,
+               float scale, float draft_scale, const float *accept_u, const float *draw_u, int32_t *tokens, int32_t *accepted,
+               float *logp, void *stream)
+{
+    ApiScope scope("pdb_verify", nullptr, nullptr, nullptr, nullptr, false);
+    if (!t || n_drafts < 0) return PDB_EINVAL;
+    int rc = check_mat(target);
+    if (rc == PDB_OK && draft) rc = check_mat(draft);
+    if (rc != PDB_OK) return rc;
+    if (n_drafts > MAX_DRAFTS || target->cols > MAX_VOCAB) return PDB_ETOOBIG;
+    if (target->rows % (n_drafts + 1) != 0 || target->cols < 1 || !usable_scale(scale)) return PDB_EINVAL;
+    const int64_t n = target->rows / (n_drafts + 1), drafts = n * n_drafts;
+    if (n_drafts > 0) rc = check_ids(draft_ids, n, n_drafts);
+    if (rc != PDB_OK) return rc;
+    if (draft && (draft->rows != drafts || draft->cols != target->cols || draft->type != target->type ||
+                  !usable_scale(draft_scale)))
+        return PDB_EINVAL;
+    const auto words = [](const void *p, int64_t k, bool optional) { return k == 0 || (p ? (uintptr_t)p % 4 == 0 : optional); };
+    if (!words(accept_u, drafts, false) || !words(draw_u, n, false) || !words(tokens, n, false) || !words(accepted, n, true) ||
+        !words(logp, n, true))
+        return PDB_EINVAL;
+    if (n == 0) return PDB_OK;
+    if ((rc = check_device(t)) != PDB_OK) return rc;
+    cudaStream_t s = (cudaStream_t)stream;
+    TokensUse use{t, s};
+    return with_type(target->type, [&](auto *a) {
+        using T = std::remove_pointer_t<decltype(a)>;
+        Shape shape = {};
+        shape.threads = 512;
+        shape.blocks = cluster_of(n, target->cols / Vec<T>::E + 1, shape.threads, [&](int blocks) { return t->sms * 4 / blocks; });
+        shape.clusters = n;
+        shape.smem = verify_smem(target->cols, shape.blocks);
+        return launch_rows(k_verify<T, 512>, shape, s, (const T *)target->data, stride_of(target),
+                           draft ? (const T *)draft->data : (const T *)nullptr, draft ? stride_of(draft) : 0, (int)target->cols,
+                           n_drafts > 0 ? ids_of(draft_ids) : Ids{}, (int)n_drafts, scale, draft_scale, accept_u, draw_u,
+                           VerifyOut{tokens, accepted, logp}, t->status);
+    });
+}
+
+}  // extern "C"
