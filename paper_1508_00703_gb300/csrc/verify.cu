@@ -93,15 +93,32 @@ __device__ __forceinline__ Two times(Two a, Two b)
     const float h = __fmul_rn(a.hi, b.hi);
     return {h, __fadd_rn(__fmaf_rn(a.hi, b.hi, -h), __fmaf_rn(a.hi, b.lo, __fmul_rn(a.lo, b.hi)))};
 }
-__device__ __forceinline__ Two two_of(double x)
+// 1 / a
+__device__ __forceinline__ Two inverse_of(Two a)
 {
-    const float h = (float)x;
-    return {h, (float)(x - (double)h)};
+    const float h = __fdiv_rn(1.0f, a.hi);
+    return {h, __fmul_rn(h, __fmaf_rn(-a.lo, h, __fmaf_rn(-a.hi, h, 1.0f)))};
 }
-// in units of 1 / unit, a power of two
-__device__ __forceinline__ int64_t whole_of(Two a, float unit)
+
+// A sum of numbers from 0 to 1 in units of 2^-46: the units of 2^-23, and what is left of them, each taken from the lowest bits of a
+// float that is large enough (a conversion to 64 bits takes 16 cycles an SM for each warp).
+struct Units {
+    int high = 0, low = 0;
+    __device__ __forceinline__ void add(Two a)
+    {
+        const float h = __fmaf_rn(a.hi, 0x1p23f, 8388608.0f);
+        const float rest = __fadd_rn(__fmaf_rn(__fsub_rn(h, 8388608.0f), -0x1p-23f, a.hi), a.lo);
+        const float l = __fmaf_rn(rest, 0x1p46f, 12582912.0f);
+        high += __float_as_int(h) - 0x4b000000, low += __float_as_int(l) - 0x4b400000;
+    }
+    __device__ __forceinline__ int64_t whole() const { return ((int64_t)high << 23) + low; }
+};
+__device__ __forceinline__ Two two_of(int64_t high, int64_t low)
 {
-    return __float2ll_rn(__fmul_rn(a.hi, unit)) + __float2ll_rn(__fmul_rn(a.lo, unit));
+    high += low >> 23, low &= 0x7fffff;
+    const float h = __ll2float_rn(high);
+    const int64_t rest = high - __float2ll_rn(h);
+    return {__fmul_rn(h, 0x1p-23f), __fmul_rn(__ll2float_rn(rest * 0x800000 + low), 0x1p-46f)};
 }
 
 // ------------------------------------------------------------------ shared by the blocks of a sequence
@@ -109,9 +126,8 @@ struct Shared {
     float stat[2][4];                   // this block's m, s of the target's and the draft's row, for two positions in turn
     float part[2][96];
     int64_t warp_sum[2][16];
-    int64_t sum[2][2];                  // this block's exact sums of the two rows: 2^20 times the first, and the second
-    double row_sum[2];                  // the rows' exact sums
-    float2 row_inv[2];                  // their reciprocals
+    int64_t sum[2][2];                  // this block's exact sums of the two rows, in units of 2^-23 and 2^-46
+    Two row_sum[2], row_inv[2];         // the rows' exact sums, and their reciprocals
     int64_t total;                      // this block's weights
     int64_t at, before;                 // the drawn place among all weights, the weights of lower blocks
     int64_t below;                      // weights before the piece that holds the drawn token
@@ -206,52 +222,45 @@ struct Walk {
         return x;
     }
 
-    // The rows' sums good to 2^-42, into sh.row_sum and sh.row_inv.  A thread's part is an integer in units that its number of
-    // tokens leaves room for; threads and blocks add up the two ends of theirs apart, so that nothing is lost and no order matters.
-    __device__ __forceinline__ void exact_sums(const Row<T> &p, const Row<T> &q, int all_pieces)
+    // The rows' sums good to 2^-42, into sh.row_sum and sh.row_inv.  Integers are added up: no order shows in them.
+    __device__ __forceinline__ void exact_sums(const Row<T> &p, const Row<T> &q)
     {
-        constexpr int W = THREADS / 32;
         const int warp = threadIdx.x >> 5;
-        const int most = ((all_pieces + blocks - 1) / blocks + W - 1) / W * (PIECE / 32);    // tokens of a thread
-        const int bits = 62 - (32 - __clz(most));
-        const float unit = __int_as_float((bits + 127) << 23);
 #pragma unroll 1
         for (int which = 0; which < (q.z ? 2 : 1); ++which) {
             const T *z = which ? q.z : p.z;
             const float m = which ? q.m : p.m, scale = which ? q.scale : p.scale;
-            int64_t sum = 0;
+            int64_t high = 0, low = 0;
 #pragma unroll 1
-            for (int i = warp; i < pieces; i += W)
-                each_of(first_piece + i, [&](int j, int) { sum += whole_of(exp_two(to_float(z[j]), m, scale, sh.table), unit); });
-            const int64_t high = block_sum(sum >> 20, sh.warp_sum[0]), low = block_sum(sum & 0xfffff, sh.warp_sum[1]);
+            for (int i = warp; i < pieces; i += THREADS / 32) {
+                Units sum;
+                each_of(first_piece + i, [&](int j, int) { sum.add(exp_two(to_float(z[j]), m, scale, sh.table)); });
+                high += sum.high, low += sum.low;
+            }
+            high = block_sum(high, sh.warp_sum[0]), low = block_sum(low, sh.warp_sum[1]);
             if (threadIdx.x == 0) sh.sum[which][0] = high, sh.sum[which][1] = low;
             __syncthreads();
         }
         cluster.sync();
-        if (threadIdx.x == 0) {
-#pragma unroll 1
-            for (int which = 0; which < (q.z ? 2 : 1); ++which) {
-                int64_t high = 0, low = 0;
-                for (int b = 0; b < blocks; ++b) {
-                    const int64_t *o = cluster.map_shared_rank(&sh, b)->sum[which];
-                    high += o[0], low += o[1];
-                }
-                const double x = __fma_rn((double)high, 0x1p20, (double)low) * (double)__int_as_float((127 - bits) << 23);
-                const Two inv = two_of(1.0 / x);
-                sh.row_sum[which] = x;
-                sh.row_inv[which] = {inv.hi, inv.lo};
+        if (threadIdx.x < (q.z ? 2 : 1)) {
+            int64_t high = 0, low = 0;
+            for (int b = 0; b < blocks; ++b) {
+                const int64_t *o = cluster.map_shared_rank(&sh, b)->sum[threadIdx.x];
+                high += o[0], low += o[1];
             }
+            sh.row_sum[threadIdx.x] = two_of(high, low);
+            sh.row_inv[threadIdx.x] = inverse_of(sh.row_sum[threadIdx.x]);
         }
         cluster.sync();                  // the others' sums have been read
     }
 
-    // a token's weight in a draw, in units of 2^-60
+    // a token's weight in a draw
     struct Weights {
         Row<T> p, q;
         Two p_inv, q_inv;
         int without;                     // a token left out
         const float2 *table;
-        __device__ __forceinline__ int64_t operator()(int j) const
+        __device__ __forceinline__ Two operator()(int j) const
         {
             Two a = times(exp_two(to_float(p.z[j]), p.m, p.scale, table), p_inv);
             if (q.z) {
@@ -260,8 +269,7 @@ struct Walk {
                 const float dl = __fsub_rn(__fsub_rn(a.hi, __fsub_rn(d, e)), __fadd_rn(b.hi, e));
                 a = {d, __fadd_rn(dl, __fsub_rn(a.lo, b.lo))};
             }
-            const int64_t w = whole_of(a, 0x1p60f);
-            return j == without || w < 0 ? 0 : w;
+            return j == without || a.hi < 0.0f ? Two{0.0f, 0.0f} : a;
         }
     };
 
@@ -286,8 +294,9 @@ struct Walk {
         int64_t all = 0;                 // on lane 0
 #pragma unroll 1
         for (int i = warp; i < pieces; i += W) {
-            int64_t sum = 0;
-            each_of(first_piece + i, [&](int j, int) { sum += weight(j); });
+            Units units;
+            each_of(first_piece + i, [&](int j, int) { units.add(weight(j)); });
+            int64_t sum = units.whole();
 #pragma unroll
             for (int off = 16; off >= 1; off >>= 1) sum += __shfl_xor_sync(FULL, sum, off);
             if (lane == 0) sh.weight[i] = sum, all += sum;
@@ -331,7 +340,11 @@ struct Walk {
             int64_t w[PIECE / 32];
 #pragma unroll
             for (int u = 0; u < PIECE / 32; ++u) w[u] = 0;
-            each_of(sh.piece, [&](int j, int u) { w[u] = weight(j); });
+            each_of(sh.piece, [&](int j, int u) {
+                Units one;
+                one.add(weight(j));
+                w[u] = one.whole();
+            });
             int64_t sum = sh.below;
 #pragma unroll
             for (int u = 0; u < PIECE / 32; ++u) {
@@ -359,7 +372,7 @@ struct VerifyOut {
 constexpr float SURE = 0x1p-12f;
 
 template <typename T, int THREADS>
-__global__ __launch_bounds__(THREADS) void k_verify(const T *target, int64_t t_stride, const T *draft, int64_t d_stride, int cols,
+__global__ __launch_bounds__(THREADS, 1024 / THREADS) void k_verify(const T *target, int64_t t_stride, const T *draft, int64_t d_stride, int cols,
                                                     Ids ids, int D, float scale, float draft_scale, const float *accept_u,
                                                     const float *draw_u, VerifyOut out, int *status)
 {
@@ -409,11 +422,12 @@ __global__ __launch_bounds__(THREADS) void k_verify(const T *target, int64_t t_s
             sure = fabsf(left - right) > SURE * more && more > 1e-30f;
         }
         if (!good || !sure) {
-            walk.exact_sums(p, q, all);
+            walk.exact_sums(p, q);
             if (!sure) {
                 if (threadIdx.x == 0) {
-                    const double pe = exp((double)scale * ((double)z - (double)p.m)) / sh.row_sum[0];
-                    const double qe = q.z ? exp((double)draft_scale * ((double)to_float(q.z[t]) - (double)q.m)) / sh.row_sum[1] : 1.0;
+                    const double pe = exp((double)scale * ((double)z - (double)p.m)) / ((double)sh.row_sum[0].hi + (double)sh.row_sum[0].lo);
+                    const double qe = q.z ? exp((double)draft_scale * ((double)to_float(q.z[t]) - (double)q.m)) /
+                                                 ((double)sh.row_sum[1].hi + (double)sh.row_sum[1].lo) : 1.0;
                     sh.good = (double)u * qe < pe;
                 }
                 __syncthreads();
@@ -432,14 +446,14 @@ __global__ __launch_bounds__(THREADS) void k_verify(const T *target, int64_t t_s
     int drawn = -1;
     bool none = !p.valid();
     if (!none) {
-        typename Walk<T, THREADS>::Weights weight{p, q, {sh.row_inv[0].x, sh.row_inv[0].y}, {sh.row_inv[1].x, sh.row_inv[1].y},
+        typename Walk<T, THREADS>::Weights weight{p, q, sh.row_inv[0], sh.row_inv[1],
                                                   refused && !q.z ? (int)t : -1, sh.table};
 #pragma unroll 1
         for (;;) {
             drawn = walk.draw(weight, draw_u[s]);
             none = sh.none;
             if (!none || !refused) break;
-            // nothing of p - q that 2^-60 could tell: from p
+            // nothing of p - q that 2^-46 could tell: from p
             refused = false, weight.q.z = nullptr, weight.without = -1;
             __syncthreads();
         }
@@ -495,14 +509,18 @@ int pdb_verify(pdb_tokens *t, const pdb_mat *target, const pdb_ids *draft_ids, i
     return with_type(target->type, [&](auto *a) {
         using T = std::remove_pointer_t<decltype(a)>;
         Shape shape = {};
-        shape.threads = 512;
-        shape.blocks = cluster_of(n, target->cols / Vec<T>::E + 1, shape.threads, [&](int blocks) { return t->sms * 4 / blocks; });
+        const int64_t nv = target->cols / Vec<T>::E + 1;
+        shape.threads = n * MAX_CLUSTER <= t->sms ? 512 : 256;
+        shape.blocks = cluster_of(n, nv, shape.threads, [&](int blocks) { return t->sms * (1024 / shape.threads) / blocks; });
         shape.clusters = n;
         shape.smem = verify_smem(target->cols, shape.blocks);
-        return launch_rows(k_verify<T, 512>, shape, s, (const T *)target->data, stride_of(target),
-                           draft ? (const T *)draft->data : (const T *)nullptr, draft ? stride_of(draft) : 0, (int)target->cols,
-                           n_drafts > 0 ? ids_of(draft_ids) : Ids{}, (int)n_drafts, scale, draft_scale, accept_u, draw_u,
-                           VerifyOut{tokens, accepted, logp}, t->status);
+        const auto run = [&](auto k) {
+            return launch_rows(k_verify<T, decltype(k)::value>, shape, s, (const T *)target->data, stride_of(target),
+                               draft ? (const T *)draft->data : (const T *)nullptr, draft ? stride_of(draft) : 0,
+                               (int)target->cols, n_drafts > 0 ? ids_of(draft_ids) : Ids{}, (int)n_drafts, scale, draft_scale,
+                               accept_u, draw_u, VerifyOut{tokens, accepted, logp}, t->status);
+        };
+        return shape.threads == 512 ? run(Num<512>()) : run(Num<256>());
     });
 }
 
