@@ -122,9 +122,15 @@ __device__ __forceinline__ Two two_of(int64_t high, int64_t low)
 }
 
 // ------------------------------------------------------------------ shared by the blocks of a sequence
+constexpr int MAX_GROUP = 8;            // positions whose rows are read before the first of them is decided
+
 struct Shared {
-    float stat[2][4];                   // this block's m, s of the target's and the draft's row, for two positions in turn
-    float part[2][96];
+    float part[2 * MAX_GROUP][2][16];   // the warps' m, s of each row of a group (target's, draft's, target's, ..)
+    float stat[2][2 * MAX_GROUP][2];    // this block's, for two groups in turn
+    float joined[2 * MAX_GROUP][2];     // all blocks'
+    float z[2 * MAX_GROUP];             // the rows' logits of the drafted tokens
+    int drafted[MAX_DRAFTS];
+    float u[MAX_DRAFTS];
     int64_t warp_sum[2][16];
     int64_t sum[2][2];                  // this block's exact sums of the two rows, in units of 2^-23 and 2^-46
     Two row_sum[2], row_inv[2];         // the rows' exact sums, and their reciprocals
@@ -145,68 +151,106 @@ struct Row {
 };
 
 template <typename T, int THREADS>
-__device__ __forceinline__ void share_stat(const Row<T> &row, int cols, int rank, int blocks, float *part, float *to)
-{
-    const float c = __fmul_rn(row.scale, LOG2E);
-    const Share sh = share_of(row.z, cols, rank, blocks);
-    const uint4 *body = reinterpret_cast<const uint4 *>(row.z + sh.b0);
-    const int n_vec = sh.v1 - sh.v0;
-    Stat<false> a;
-    float top = -INFINITY;
-    uint4 v[UNROLL];
-    load_vectors<T, THREADS, 32>(v, body, 0, lane_start(), n_vec);
-    const bool has_edge = (int)threadIdx.x < sh.edges();
-    T z_edge = from_float<T>(0.0f);
-    if (has_edge) z_edge = row.z[sh.edge(threadIdx.x)];
-    for (int base = 0; base < n_vec; base += THREADS * UNROLL) {
-        uint4 next[UNROLL];
-        load_vectors<T, THREADS, 32>(next, body, base + THREADS * UNROLL, lane_start(), n_vec);
-        add_vectors<T, false>(a, v, c, top);
-#pragma unroll
-        for (int u = 0; u < UNROLL; ++u) v[u] = next[u];
-    }
-    if (has_edge) add_element(a, to_float(z_edge), c);
-    a.rebase(fmaxf(a.m, top), c);        // to the maximum itself
-    block_join<THREADS>(a, c, part);
-    if (threadIdx.x == 0) to[0] = a.m, to[1] = a.s;
-}
-
-template <typename T, int THREADS>
 struct Walk {
     Shared &sh;
     cg::cluster_group cluster;
     int rank, blocks, cols;
     int first_piece, pieces;            // the block's
 
-    // m and s of the target's row, and of the draft's where it has one, over the cluster: the same on all its threads
-    __device__ __forceinline__ void stats(Row<T> &p, Row<T> &q, int turn)
+    // m and s of `rows` rows (row(i): where the i-th lies, c(i): its scale * log2(e)) over the cluster, into sh.joined.  The chunks
+    // of all rows follow one another, each loaded while the one before is added.
+    template <typename R, typename C>
+    __device__ __forceinline__ void stats(int rows, R row, C c_of, int turn)
     {
-        share_stat<T, THREADS>(p, cols, rank, blocks, sh.part[0], sh.stat[turn]);
-        if (q.z) share_stat<T, THREADS>(q, cols, rank, blocks, sh.part[1], sh.stat[turn] + 2);
-        cluster.sync();
-        join(p, turn, 0);
-        if (q.z) join(q, turn, 2);
-    }
-    __device__ __forceinline__ void join(Row<T> &row, int turn, int at)
-    {
-        const float c = __fmul_rn(row.scale, LOG2E);
+        constexpr int W = THREADS / 32, SPAN = THREADS * UNROLL;
+        const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+        uint4 v[UNROLL];
+        const T *z = row(0);
+        Share s = share_of(z, cols, rank, blocks);
+        bool has_edge = (int)threadIdx.x < s.edges();
+        T z_edge = from_float<T>(0.0f);
+        if (has_edge) z_edge = z[s.edge(threadIdx.x)];
+        load_vectors<T, THREADS, 32>(v, reinterpret_cast<const uint4 *>(z + s.b0), 0, lane_start(), s.v1 - s.v0);
         Stat<false> a;
-        for (int b = 0; b < blocks; ++b) {
-            const float *o = cluster.map_shared_rank(sh.stat[turn], b) + at;
-            a.join(o[0], o[1], 0.0f, c);
+        float top = -INFINITY;
+        int base = 0;
+#pragma unroll 1
+        for (int i = 0; i < rows;) {
+            const float c = c_of(i);
+            const bool ends = base + SPAN >= s.v1 - s.v0;
+            const bool edge = has_edge;
+            const T own_edge = z_edge;
+            base = ends ? 0 : base + SPAN;
+            if (ends && i + 1 < rows) {
+                z = row(i + 1);
+                s = share_of(z, cols, rank, blocks);
+                has_edge = (int)threadIdx.x < s.edges();
+                if (has_edge) z_edge = z[s.edge(threadIdx.x)];
+            }
+            uint4 next[UNROLL];
+            load_vectors<T, THREADS, 32>(next, reinterpret_cast<const uint4 *>(z + s.b0), base, lane_start(),
+                                         ends && i + 1 == rows ? 0 : s.v1 - s.v0);
+            add_vectors<T, false>(a, v, c, top);
+            if (ends) {
+                if (edge) add_element(a, to_float(own_edge), c);
+                a.rebase(fmaxf(a.m, top), c);             // to the maximum itself
+                a.template warp_join<32>(c);
+                if (lane == 0) sh.part[i][0][warp] = a.m, sh.part[i][1][warp] = a.s;
+                a = Stat<false>();
+                top = -INFINITY;
+                ++i;
+            }
+#pragma unroll
+            for (int u = 0; u < UNROLL; ++u) v[u] = next[u];
         }
-        row.m = a.m, row.s = a.s;
+        __syncthreads();
+        for (int i = warp; i < rows; i += W) {
+            a.m = sh.part[i][0][lane & (W - 1)], a.s = sh.part[i][1][lane & (W - 1)];
+            a.template warp_join<W>(c_of(i));
+            if (lane == 0) sh.stat[turn][i][0] = a.m, sh.stat[turn][i][1] = a.s;
+        }
+        cluster.sync();
+        for (int i = warp; i < rows; i += W) {
+            a = Stat<false>();
+            const int b = lane & (MAX_CLUSTER - 1);
+            if (b < blocks) {
+                const float *o = cluster.map_shared_rank(&sh, b)->stat[turn][i];
+                a.m = o[0], a.s = o[1];
+            }
+            a.template warp_join<MAX_CLUSTER>(c_of(i));
+            if (lane == 0) sh.joined[i][0] = a.m, sh.joined[i][1] = a.s;
+        }
+        __syncthreads();
     }
 
-    // f(token, its place in the lane's order) of the lanes' tokens of a piece
+    // f(the lane's tokens of a piece: z and, where there is one, y) of the warp's pieces; a piece's are loaded before the one before is
+    // worked on
     template <typename F>
-    __device__ __forceinline__ void each_of(int piece, F f)
+    __device__ __forceinline__ void each_piece(const T *z, const T *y, F f)
     {
+        constexpr int N = PIECE / 32, W = THREADS / 32;
         const int lane = threadIdx.x & 31;
+        const T none = from_float<T>(-INFINITY);
+        T a[N], b[N];
+        auto load = [&](int i) {
+            const int j = (first_piece + i) * PIECE + lane;
 #pragma unroll
-        for (int u = 0; u < PIECE / 32; ++u) {
-            const int j = piece * PIECE + u * 32 + lane;
-            if (j < cols) f(j, u);
+            for (int u = 0; u < N; ++u) {
+                const bool on = i < pieces && j + u * 32 < cols;
+                a[u] = none, b[u] = none;
+                if (on) a[u] = z[j + u * 32];
+                if (on && y) b[u] = y[j + u * 32];
+            }
+        };
+        int i = threadIdx.x >> 5;
+        load(i);
+#pragma unroll 1
+        for (; i < pieces; i += W) {
+            T x[N], w[N];
+#pragma unroll
+            for (int u = 0; u < N; ++u) x[u] = a[u], w[u] = b[u];
+            load(i + W);
+            f(i, x, w);
         }
     }
 
@@ -225,18 +269,17 @@ struct Walk {
     // The rows' sums good to 2^-42, into sh.row_sum and sh.row_inv.  Integers are added up: no order shows in them.
     __device__ __forceinline__ void exact_sums(const Row<T> &p, const Row<T> &q)
     {
-        const int warp = threadIdx.x >> 5;
 #pragma unroll 1
         for (int which = 0; which < (q.z ? 2 : 1); ++which) {
             const T *z = which ? q.z : p.z;
             const float m = which ? q.m : p.m, scale = which ? q.scale : p.scale;
             int64_t high = 0, low = 0;
-#pragma unroll 1
-            for (int i = warp; i < pieces; i += THREADS / 32) {
+            each_piece(z, nullptr, [&](int, const T (&x)[PIECE / 32], const T (&)[PIECE / 32]) {
                 Units sum;
-                each_of(first_piece + i, [&](int j, int) { sum.add(exp_two(to_float(z[j]), m, scale, sh.table)); });
+#pragma unroll
+                for (int u = 0; u < PIECE / 32; ++u) sum.add(exp_two(to_float(x[u]), m, scale, sh.table));
                 high += sum.high, low += sum.low;
-            }
+            });
             high = block_sum(high, sh.warp_sum[0]), low = block_sum(low, sh.warp_sum[1]);
             if (threadIdx.x == 0) sh.sum[which][0] = high, sh.sum[which][1] = low;
             __syncthreads();
@@ -260,11 +303,11 @@ struct Walk {
         Two p_inv, q_inv;
         int without;                     // a token left out
         const float2 *table;
-        __device__ __forceinline__ Two operator()(int j) const
+        __device__ __forceinline__ Two operator()(int j, T z, T y) const
         {
-            Two a = times(exp_two(to_float(p.z[j]), p.m, p.scale, table), p_inv);
+            Two a = times(exp_two(to_float(z), p.m, p.scale, table), p_inv);
             if (q.z) {
-                const Two b = times(exp_two(to_float(q.z[j]), q.m, q.scale, table), q_inv);
+                const Two b = times(exp_two(to_float(y), q.m, q.scale, table), q_inv);
                 const float d = __fsub_rn(a.hi, b.hi), e = __fsub_rn(d, a.hi);
                 const float dl = __fsub_rn(__fsub_rn(a.hi, __fsub_rn(d, e)), __fadd_rn(b.hi, e));
                 a = {d, __fadd_rn(dl, __fsub_rn(a.lo, b.lo))};
@@ -285,22 +328,22 @@ struct Walk {
         return (int64_t)(shift < 64 ? high << (64 - shift) | low >> shift : shift < 128 ? high >> (shift - 64) : 0);
     }
 
-    // The smallest token whose running sum of weights passes v times all of them: on the thread that finds it, -1 on the others.
-    // Sets sh.none where no token has a weight.
-    __device__ __forceinline__ int draw(const Weights &weight, float v)
+    // The smallest token whose running sum of weights passes v times all of them, and its logit: on the thread that finds it, -1 on
+    // the others.  Sets sh.none where no token has a weight.
+    __device__ __forceinline__ int draw(const Weights &weight, float v, float &logit)
     {
-        constexpr int W = THREADS / 32;
+        constexpr int N = PIECE / 32;
         const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
         int64_t all = 0;                 // on lane 0
-#pragma unroll 1
-        for (int i = warp; i < pieces; i += W) {
+        each_piece(weight.p.z, weight.q.z, [&](int i, const T (&z)[N], const T (&y)[N]) {
             Units units;
-            each_of(first_piece + i, [&](int j, int) { units.add(weight(j)); });
+#pragma unroll
+            for (int u = 0; u < N; ++u) units.add(weight((first_piece + i) * PIECE + u * 32 + lane, z[u], y[u]));
             int64_t sum = units.whole();
 #pragma unroll
             for (int off = 16; off >= 1; off >>= 1) sum += __shfl_xor_sync(FULL, sum, off);
             if (lane == 0) sh.weight[i] = sum, all += sum;
-        }
+        });
         all = block_sum(all, sh.warp_sum[0]);
         if (threadIdx.x == 0) sh.total = all;
         cluster.sync();
@@ -337,25 +380,33 @@ struct Walk {
                 sh.below = below;
             }
             __syncwarp();
-            int64_t w[PIECE / 32];
+            // a lane's neighbouring tokens of it
+            const int j0 = sh.piece * PIECE + lane * N;
+            T z[N], y[N];
 #pragma unroll
-            for (int u = 0; u < PIECE / 32; ++u) w[u] = 0;
-            each_of(sh.piece, [&](int j, int u) {
+            for (int u = 0; u < N; ++u) {
+                z[u] = y[u] = from_float<T>(-INFINITY);
+                if (j0 + u < cols) z[u] = weight.p.z[j0 + u];
+                if (j0 + u < cols && weight.q.z) y[u] = weight.q.z[j0 + u];
+            }
+            int64_t w[N], sum = 0;
+#pragma unroll
+            for (int u = 0; u < N; ++u) {
                 Units one;
-                one.add(weight(j));
-                w[u] = one.whole();
-            });
-            int64_t sum = sh.below;
+                one.add(weight(j0 + u, z[u], y[u]));
+                w[u] = one.whole(), sum += w[u];
+            }
+            up = sum;
 #pragma unroll
-            for (int u = 0; u < PIECE / 32; ++u) {
-                int64_t upto = w[u];
+            for (int off = 1; off < 32; off <<= 1) {
+                const int64_t x = __shfl_up_sync(FULL, up, off);
+                if (lane >= off) up += x;
+            }
+            below = sh.below + up - sum;
 #pragma unroll
-                for (int off = 1; off < 32; off <<= 1) {
-                    const int64_t x = __shfl_up_sync(FULL, upto, off);
-                    if (lane >= off) upto += x;
-                }
-                if (at >= sum + upto - w[u] && at < sum + upto) found = sh.piece * PIECE + u * 32 + lane;
-                sum += __shfl_sync(FULL, upto, 31);
+            for (int u = 0; u < N; ++u) {
+                if (at >= below && at < below + w[u]) found = j0 + u, logit = to_float(z[u]);
+                below += w[u];
             }
         }
         return found;
@@ -372,9 +423,10 @@ struct VerifyOut {
 constexpr float SURE = 0x1p-12f;
 
 template <typename T, int THREADS>
-__global__ __launch_bounds__(THREADS, 1024 / THREADS) void k_verify(const T *target, int64_t t_stride, const T *draft, int64_t d_stride, int cols,
-                                                    Ids ids, int D, float scale, float draft_scale, const float *accept_u,
-                                                    const float *draw_u, VerifyOut out, int *status)
+__global__ __launch_bounds__(THREADS, 1024 / THREADS) void k_verify(const T *target, int64_t t_stride, const T *draft,
+                                                                    int64_t d_stride, int cols, Ids ids, int D, int group,
+                                                                    float scale, float draft_scale, const float *accept_u,
+                                                                    const float *draw_u, VerifyOut out, int *status)
 {
     after_previous();
     extern __shared__ __align__(16) unsigned char s_raw[];
@@ -385,82 +437,120 @@ __global__ __launch_bounds__(THREADS, 1024 / THREADS) void k_verify(const T *tar
     const int all = (cols + PIECE - 1) / PIECE;
     const int p0 = (int)((int64_t)all * rank / blocks), p1 = (int)((int64_t)all * (rank + 1) / blocks);
     Walk<T, THREADS> walk{sh, cluster, rank, blocks, cols, p0, p1 - p0};
-    for (int i = threadIdx.x; i < 256; i += THREADS) sh.table[i] = {EXP2_TABLE.hi[i], EXP2_TABLE.lo[i]};
     const bool writes = rank == 0 && threadIdx.x == 0;
     const int64_t base = s * (D + 1);
+    for (int d = threadIdx.x; d < D; d += THREADS) {
+        const int64_t t = load_id(ids, s, d);
+        sh.drafted[d] = t >= 0 && t < cols ? (int)t : -1;
+        sh.u[d] = accept_u[s * D + d];
+        // recorded where no id before it ends the drafts
+        if (t >= cols && rank == 0) {
+            bool seen = true;
+            for (int e = 0; e < d; ++e) {
+                const int64_t before = load_id(ids, s, e);
+                seen &= before >= 0 && before < cols;
+            }
+            if (seen) set_status(status, PDB_ERANGE);
+        }
+    }
+    for (int i = threadIdx.x; i < 256; i += THREADS) sh.table[i] = {EXP2_TABLE.hi[i], EXP2_TABLE.lo[i]};
+    const float v = draw_u[s];
+    __syncthreads();
+    int length = 0;                      // drafts
+    while (length < D && sh.drafted[length] >= 0) ++length;
 
     Row<T> p{}, q{};
     p.scale = scale, q.scale = draft_scale;
-    int a = 0;
-    bool refused = false;
-    int64_t t = -1;
+    const float c = __fmul_rn(scale, LOG2E), cq = __fmul_rn(draft_scale, LOG2E);
+    const int each = draft ? 2 : 1;      // rows of a position
+    int a = 0;                           // the position
+    bool refused = false, stops = false;
+    int t = -1;
     float log_s = 0.0f;
 #pragma unroll 1
-    for (;; ++a) {
-        t = a < D ? load_id(ids, s, a) : -1;
-        if (t >= cols) {
-            if (writes) set_status(status, PDB_ERANGE);
-            t = -1;
-        }
-        p.z = target + (base + a) * t_stride;
-        q.z = t >= 0 && draft ? draft + (s * D + a) * d_stride : nullptr;
-        walk.stats(p, q, a & 1);
-        if (!p.valid()) break;
-        log_s = logf(p.s);
-        if (q.z && !q.valid()) t = -1;
-        if (t < 0) q.z = nullptr;        // the drafts end here
-        float z = 0.0f, u = 0.0f;
-        bool good = false, sure = true;
-        if (t >= 0) {
-            z = to_float(p.z[t]), u = accept_u[s * D + a];
-            const float right = __fdiv_rn(ex2(__fmul_rn(__fsub_rn(z, p.m), __fmul_rn(scale, LOG2E))), p.s);
-            float left = u;
-            if (q.z)
-                left = __fmul_rn(u, __fdiv_rn(ex2(__fmul_rn(__fsub_rn(to_float(q.z[t]), q.m), __fmul_rn(draft_scale, LOG2E))), q.s));
-            const float more = fmaxf(left, right);
-            good = left < right;
-            sure = fabsf(left - right) > SURE * more && more > 1e-30f;
-        }
-        if (!good || !sure) {
-            walk.exact_sums(p, q);
-            if (!sure) {
-                if (threadIdx.x == 0) {
-                    const double pe = exp((double)scale * ((double)z - (double)p.m)) / ((double)sh.row_sum[0].hi + (double)sh.row_sum[0].lo);
-                    const double qe = q.z ? exp((double)draft_scale * ((double)to_float(q.z[t]) - (double)q.m)) /
-                                                 ((double)sh.row_sum[1].hi + (double)sh.row_sum[1].lo) : 1.0;
-                    sh.good = (double)u * qe < pe;
-                }
-                __syncthreads();
-                good = sh.good;
+    for (int first = 0, turn = 0; !stops; first += group, turn ^= 1) {
+        // a group's rows; of the last position the target's alone
+        const int last = min(length, first + group - 1);
+        const int rows = (last - first + 1) * each - (draft && last == length ? 1 : 0);
+        const auto row = [&](int i) {
+            const int d = first + (each == 2 ? i >> 1 : i);
+            return each == 2 && (i & 1) ? draft + (s * D + d) * d_stride : target + (base + d) * t_stride;
+        };
+        __syncthreads();                 // the group before has been decided
+        if ((int)threadIdx.x < rows && first + (int)threadIdx.x / each < length)
+            sh.z[threadIdx.x] = to_float(row(threadIdx.x)[sh.drafted[first + (int)threadIdx.x / each]]);
+        walk.stats(rows, row, [&](int i) { return each == 2 && (i & 1) ? cq : c; }, turn);
+#pragma unroll 1
+        for (a = first;; ++a) {
+            const int i = (a - first) * each;
+            t = a < length ? sh.drafted[a] : -1;
+            p.z = row(i), p.m = sh.joined[i][0], p.s = sh.joined[i][1];
+            q.z = nullptr;
+            stops = true;
+            if (!p.valid()) break;
+            log_s = logf(p.s);
+            if (t >= 0 && draft) {
+                q.z = row(i + 1), q.m = sh.joined[i + 1][0], q.s = sh.joined[i + 1][1];
+                if (!q.valid()) t = -1, q.z = nullptr;    // the drafts end here
             }
-            if (!good) {
-                refused = t >= 0;
+            bool good = false, sure = true;
+            const float z = sh.z[i], u = sh.u[a < D ? a : 0];
+            if (t >= 0) {
+                const float right = __fdiv_rn(ex2(__fmul_rn(__fsub_rn(z, p.m), c)), p.s);
+                float left = u;
+                if (q.z) left = __fmul_rn(u, __fdiv_rn(ex2(__fmul_rn(__fsub_rn(sh.z[i + 1], q.m), cq)), q.s));
+                const float more = fmaxf(left, right);
+                good = left < right;
+                sure = fabsf(left - right) > SURE * more && more > 1e-30f;
+            }
+            if (!good || !sure) {
+                walk.exact_sums(p, q);
+                if (!sure) {
+                    if (threadIdx.x == 0) {
+                        const auto in_64 = [](float scale, float z, const Row<T> &r, Two sum) {
+                            return exp((double)scale * ((double)z - (double)r.m)) / ((double)sum.hi + (double)sum.lo);
+                        };
+                        const double pe = in_64(scale, z, p, sh.row_sum[0]);
+                        const double qe = q.z ? in_64(draft_scale, sh.z[i + 1], q, sh.row_sum[1]) : 1.0;
+                        sh.good = (double)u * qe < pe;
+                    }
+                    __syncthreads();
+                    good = sh.good;
+                }
+                if (!good) {
+                    refused = t >= 0;
+                    break;
+                }
+            }
+            if (writes) {
+                out.tokens[base + a] = t;
+                if (out.logp) out.logp[base + a] = __fmaf_rn(__fsub_rn(z, p.m), scale, -log_s);
+            }
+            if (a == last) {
+                stops = false;
                 break;
             }
         }
-        if (writes) {
-            out.tokens[base + a] = (int32_t)t;
-            if (out.logp) out.logp[base + a] = __fmaf_rn(__fsub_rn(z, p.m), scale, -log_s);
-        }
     }
-    int drawn = -1;
-    bool none = !p.valid();
-    if (!none) {
-        typename Walk<T, THREADS>::Weights weight{p, q, sh.row_inv[0], sh.row_inv[1],
-                                                  refused && !q.z ? (int)t : -1, sh.table};
+    bool none = true;
+    if (p.valid()) {
+        typename Walk<T, THREADS>::Weights weight{p, q, sh.row_inv[0], sh.row_inv[1], refused && !q.z ? t : -1, sh.table};
 #pragma unroll 1
         for (;;) {
-            drawn = walk.draw(weight, draw_u[s]);
+            float z = 0.0f;
+            const int drawn = walk.draw(weight, v, z);
             none = sh.none;
+            if (drawn >= 0) {
+                out.tokens[base + a] = drawn;
+                if (out.logp) out.logp[base + a] = __fmaf_rn(__fsub_rn(z, p.m), scale, -log_s);
+            }
             if (!none || !refused) break;
             // nothing of p - q that 2^-46 could tell: from p
             refused = false, weight.q.z = nullptr, weight.without = -1;
             __syncthreads();
         }
-    }
-    if (drawn >= 0) {
-        out.tokens[base + a] = drawn;
-        if (out.logp) out.logp[base + a] = __fmaf_rn(__fsub_rn(to_float(p.z[drawn]), p.m), scale, -log_s);
+    } else {
+        cluster.sync();                  // the others have read this block's statistics
     }
     if (writes) {
         if (out.accepted) out.accepted[s] = a;
@@ -469,7 +559,6 @@ __global__ __launch_bounds__(THREADS, 1024 / THREADS) void k_verify(const T *tar
             if (out.logp) out.logp[base + d] = 0.0f;
         }
     }
-    cluster.sync();                      // nobody reads this block's shared memory any more
 }
 
 size_t verify_smem(int64_t cols, int blocks)
@@ -513,11 +602,12 @@ int pdb_verify(pdb_tokens *t, const pdb_mat *target, const pdb_ids *draft_ids, i
         shape.threads = n * MAX_CLUSTER <= t->sms ? 512 : 256;
         shape.blocks = cluster_of(n, nv, shape.threads, [&](int blocks) { return t->sms * (1024 / shape.threads) / blocks; });
         shape.clusters = n;
+        const int group = n * MAX_CLUSTER <= t->sms ? MAX_GROUP : 1;
         shape.smem = verify_smem(target->cols, shape.blocks);
         const auto run = [&](auto k) {
             return launch_rows(k_verify<T, decltype(k)::value>, shape, s, (const T *)target->data, stride_of(target),
                                draft ? (const T *)draft->data : (const T *)nullptr, draft ? stride_of(draft) : 0,
-                               (int)target->cols, n_drafts > 0 ? ids_of(draft_ids) : Ids{}, (int)n_drafts, scale, draft_scale,
+                               (int)target->cols, n_drafts > 0 ? ids_of(draft_ids) : Ids{}, (int)n_drafts, group, scale, draft_scale,
                                accept_u, draw_u, VerifyOut{tokens, accepted, logp}, t->status);
         };
         return shape.threads == 512 ? run(Num<512>()) : run(Num<256>());
