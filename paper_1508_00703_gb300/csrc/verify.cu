@@ -21,7 +21,7 @@ namespace {
 
 constexpr int MAX_DRAFTS = 64;
 constexpr int64_t MAX_VOCAB = 1 << 21;
-constexpr int PIECE = 256;              // tokens whose weights are summed together
+constexpr int PIECE = 128;              // tokens whose weights are summed together
 
 // ------------------------------------------------------------------ exp in two floats
 // e^x = 2^k 2^(i/256) e^r with 256 k + i = rint(256 x / ln 2) and |r| <= ln 2 / 512 (table-driven, after Tang 1989), x and the
@@ -121,24 +121,83 @@ __device__ __forceinline__ Two two_of(int64_t high, int64_t low)
     return {__fmul_rn(h, 0x1p-23f), __fmul_rn(__ll2float_rn(rest * 0x800000 + low), 0x1p-46f)};
 }
 
-// ------------------------------------------------------------------ shared by the blocks of a sequence
-constexpr int MAX_GROUP = 8;            // positions whose rows are read before the first of them is decided
+// exp(scale (z - m)) of a row's tokens, z <= m
+template <bool EXACT>
+struct Term;
+template <>
+struct Term<true> {
+    float m, scale;
+    const float2 *table;
+    __device__ __forceinline__ Term(float m_, float scale_, const float2 *table_) : m(m_), scale(scale_), table(table_) {}
+    __device__ __forceinline__ Two operator()(float z) const { return exp_two(z, m, scale, table); }
+};
 
+// The same good to 2^-28.6, at half the price, where |m scale| log2(e) < 2^9: n + f = 256 (z c - m c), c = scale log2(e), n whole and |f| <= 1,
+// f formed by roundings of 2^-25; then 2^(i/256) 2^(f/256) as a whole number of 2^-29, and 2^-k, n = 256 (-k) + i.  An error that
+// all tokens of a row share falls out of its probabilities.
+constexpr float REACH = 512.0f;
+constexpr int64_t MOST_FAST = 1 << 17;  // tokens
+
+struct Digits {
+    uint32_t digits;                    // 2^29 to 2^30
+    int shift;                          // exp = digits * 2^-29 / 2^shift
+};
+template <>
+struct Term<false> {
+    float ch, cl, from, rest, low;
+    const float2 *table;                // 2^(i/256), and the same in units of 2^-29
+    Term() = default;
+    __device__ __forceinline__ Term(float m, float scale, const float2 *table_) : table(table_)
+    {
+        constexpr float log2e_rest = (float)(1.4426950408889634073599 - (double)LOG2E);
+        const float c = __fmul_rn(scale, LOG2E), c_rest = __fmaf_rn(scale, log2e_rest, __fmaf_rn(scale, LOG2E, -c));
+        ch = __fmul_rn(c, 256.0f), cl = __fmul_rn(c_rest, 256.0f);
+        const float mc = __fmul_rn(m, ch), whole = rintf(mc);
+        from = __fsub_rn(12582912.0f, whole);
+        rest = __fadd_rn(__fsub_rn(mc, whole), __fmaf_rn(m, cl, __fmaf_rn(m, ch, -mc)));
+        low = __fsub_rn(m, __fdiv_rn(60.0f, c));             // nothing below 2^-60
+    }
+    __device__ __forceinline__ Digits operator()(float z) const
+    {
+        constexpr float K1 = (float)(LN2_D / 256), K2 = (float)(LN2_D / 256 * LN2_D / 512),
+                        K3 = (float)(LN2_D / 256 * LN2_D / 512 * LN2_D / 768);
+        z = fmaxf(z, low);
+        const float t = __fmaf_rn(z, ch, from);              // n in its lowest bits
+        const float f = __fadd_rn(__fmaf_rn(z, ch, -__fsub_rn(t, from)), __fmaf_rn(z, cl, -rest));
+        const float s = __fmul_rn(f, __fmaf_rn(f, __fmaf_rn(f, K3, K2), K1));
+        const int n = __float_as_int(t);
+        const float2 tab = table[n & 255];
+        const float more = __fmaf_rn(__fmul_rn(tab.x, s), 0x1p29f, 12582912.0f);
+        return {(uint32_t)(__float_as_int(tab.y) + __float_as_int(more) - 0x4b400000), (0x4b400000 >> 8) - (n >> 8)};
+    }
+};
+// in units of 2^-45
+__device__ __forceinline__ int64_t whole_of(Digits d) { return (int64_t)((uint64_t)d.digits << 16 >> d.shift); }
+
+// How far from its token's borders a draw by Term<false> must lie to be taken, for weights that add up to 2^46: the running sum and v
+// times the whole one are moved by the terms of both rows and by their sums (4 * 2^-28.6 together), and by 2^17 tokens' cut off units in the sums
+// and the weights (2^-28 for either row): 2^-25.4 of them.
+constexpr int64_t MARGIN = (int64_t)1 << 21;
+
+// ------------------------------------------------------------------ shared by the blocks of a sequence
 struct Shared {
-    float part[2 * MAX_GROUP][2][16];   // the warps' m, s of each row of a group (target's, draft's, target's, ..)
-    float stat[2][2 * MAX_GROUP][2];    // this block's, for two groups in turn
-    float joined[2 * MAX_GROUP][2];     // all blocks'
-    float z[2 * MAX_GROUP];             // the rows' logits of the drafted tokens
+    float part[2][2][16];               // the warps' m, s of the target's and the draft's row
+    float stat[2][2][2];                // this block's, for two positions in turn
+    float joined[2][2];                 // all blocks'
+    float z[2];                         // the rows' logits of the drafted token
     int drafted[MAX_DRAFTS];
     float u[MAX_DRAFTS];
     int64_t warp_sum[2][16];
-    int64_t sum[2][2];                  // this block's exact sums of the two rows, in units of 2^-23 and 2^-46
-    Two row_sum[2], row_inv[2];         // the rows' exact sums, and their reciprocals
+    int64_t sum[2][2];                  // this block's sums of the two rows, in units of 2^-23 and 2^-46
+    Two row_sum[2], row_inv[2];         // the rows' sums, and their reciprocals
+    uint32_t inv_digits[2];             // the reciprocal as digits / 2^inv_shift, for weights in units of 2^-46
+    int inv_shift[2];
     int64_t total;                      // this block's weights
     int64_t at, before;                 // the drawn place among all weights, the weights of lower blocks
     int64_t below;                      // weights before the piece that holds the drawn token
-    int none, piece, good;
-    float2 table[256];
+    int64_t lane_weight[PIECE];         // of the tokens of that piece
+    int none, piece, good, unsure;
+    float2 table[256], fast_table[256]; // of Term<true>, of Term<false>
     int64_t weight[1];                  // of each of the block's pieces (as many as there are)
 };
 
@@ -157,8 +216,8 @@ struct Walk {
     int rank, blocks, cols;
     int first_piece, pieces;            // the block's
 
-    // m and s of `rows` rows (row(i): where the i-th lies, c(i): its scale * log2(e)) over the cluster, into sh.joined.  The chunks
-    // of all rows follow one another, each loaded while the one before is added.
+    // m and s of one or two rows (row(i): where the i-th lies, c(i): its scale * log2(e)) over the cluster, into sh.joined.  The chunks
+    // of both follow one another, each loaded while the one before is added.
     template <typename R, typename C>
     __device__ __forceinline__ void stats(int rows, R row, C c_of, int turn)
     {
@@ -234,12 +293,20 @@ struct Walk {
         T a[N], b[N];
         auto load = [&](int i) {
             const int j = (first_piece + i) * PIECE + lane;
+            if (i < pieces && (first_piece + i + 1) * PIECE <= cols) {
 #pragma unroll
-            for (int u = 0; u < N; ++u) {
-                const bool on = i < pieces && j + u * 32 < cols;
-                a[u] = none, b[u] = none;
-                if (on) a[u] = z[j + u * 32];
-                if (on && y) b[u] = y[j + u * 32];
+                for (int u = 0; u < N; ++u) a[u] = z[j + u * 32];
+                if (y)
+#pragma unroll
+                    for (int u = 0; u < N; ++u) b[u] = y[j + u * 32];
+            } else {
+#pragma unroll
+                for (int u = 0; u < N; ++u) {
+                    const bool on = i < pieces && j + u * 32 < cols;
+                    a[u] = b[u] = none;
+                    if (on) a[u] = z[j + u * 32];
+                    if (on && y) b[u] = y[j + u * 32];
+                }
             }
         };
         int i = threadIdx.x >> 5;
@@ -266,21 +333,29 @@ struct Walk {
         return x;
     }
 
-    // The rows' sums good to 2^-42, into sh.row_sum and sh.row_inv.  Integers are added up: no order shows in them.
-    __device__ __forceinline__ void exact_sums(const Row<T> &p, const Row<T> &q)
+    // The rows' sums, into sh.row_sum and sh.row_inv: good to 2^-42, or as good as Term<false> is.  Whole numbers are added up: no
+    // order of warps and blocks shows in them.
+    template <bool EXACT>
+    __device__ __forceinline__ void sums(const Row<T> &p, const Row<T> &q)
     {
+        constexpr int N = PIECE / 32;
 #pragma unroll 1
         for (int which = 0; which < (q.z ? 2 : 1); ++which) {
-            const T *z = which ? q.z : p.z;
-            const float m = which ? q.m : p.m, scale = which ? q.scale : p.scale;
+            const Term<EXACT> term(which ? q.m : p.m, which ? q.scale : p.scale, EXACT ? sh.table : sh.fast_table);
             int64_t high = 0, low = 0;
-            each_piece(z, nullptr, [&](int, const T (&x)[PIECE / 32], const T (&)[PIECE / 32]) {
-                Units sum;
+            each_piece(which ? q.z : p.z, nullptr, [&](int, const T (&x)[N], const T (&)[N]) {
+                if constexpr (EXACT) {
+                    Units sum;
 #pragma unroll
-                for (int u = 0; u < PIECE / 32; ++u) sum.add(exp_two(to_float(x[u]), m, scale, sh.table));
-                high += sum.high, low += sum.low;
+                    for (int u = 0; u < N; ++u) sum.add(term(to_float(x[u])));
+                    high += sum.high, low += sum.low;
+                } else {
+#pragma unroll
+                    for (int u = 0; u < N; ++u) low += whole_of(term(to_float(x[u])));
+                }
             });
-            high = block_sum(high, sh.warp_sum[0]), low = block_sum(low, sh.warp_sum[1]);
+            if (EXACT) high = block_sum(high, sh.warp_sum[0]);
+            low = block_sum(low, sh.warp_sum[1]);
             if (threadIdx.x == 0) sh.sum[which][0] = high, sh.sum[which][1] = low;
             __syncthreads();
         }
@@ -291,28 +366,70 @@ struct Walk {
                 const int64_t *o = cluster.map_shared_rank(&sh, b)->sum[threadIdx.x];
                 high += o[0], low += o[1];
             }
-            sh.row_sum[threadIdx.x] = two_of(high, low);
-            sh.row_inv[threadIdx.x] = inverse_of(sh.row_sum[threadIdx.x]);
+            const Two sum = EXACT ? two_of(high, low) : two_of(low >> 22, (low & 0x3fffff) << 1), inv = inverse_of(sum);
+            sh.row_sum[threadIdx.x] = sum, sh.row_inv[threadIdx.x] = inv;
+            if (!EXACT) {
+                // digits of 32 bits: weight = term's digits * digits / 2^(29 - 46 + shift)
+                const int e = (__float_as_int(inv.hi) >> 23) - 127;           // 2^e <= inv.hi < 2^(e + 1)
+                const int64_t units = __float2ll_rn(__fmul_rn(inv.hi, __int_as_float((30 - e + 127) << 23))) +
+                                      __float2ll_rn(__fmul_rn(inv.lo, __int_as_float((30 - e + 127) << 23)));
+                sh.inv_digits[threadIdx.x] = (uint32_t)units, sh.inv_shift[threadIdx.x] = 29 - 46 + 30 - e;
+            }
         }
         cluster.sync();                  // the others' sums have been read
     }
 
     // a token's weight in a draw
+    template <bool EXACT>
     struct Weights {
-        Row<T> p, q;
-        Two p_inv, q_inv;
+        Term<EXACT> p, q;
+        Two p_inv, q_inv;                // EXACT
+        uint32_t p_digits, q_digits;     // else
+        int p_shift, q_shift;
         int without;                     // a token left out
-        const float2 *table;
-        __device__ __forceinline__ Two operator()(int j, T z, T y) const
+        bool less;                       // the draft's probabilities are taken off
+        __device__ __forceinline__ Two exact(int j, T z, T y) const
         {
-            Two a = times(exp_two(to_float(z), p.m, p.scale, table), p_inv);
-            if (q.z) {
-                const Two b = times(exp_two(to_float(y), q.m, q.scale, table), q_inv);
+            Two a = times(p(to_float(z)), p_inv);
+            if (less) {
+                const Two b = times(q(to_float(y)), q_inv);
                 const float d = __fsub_rn(a.hi, b.hi), e = __fsub_rn(d, a.hi);
                 const float dl = __fsub_rn(__fsub_rn(a.hi, __fsub_rn(d, e)), __fadd_rn(b.hi, e));
                 a = {d, __fadd_rn(dl, __fsub_rn(a.lo, b.lo))};
             }
             return j == without || a.hi < 0.0f ? Two{0.0f, 0.0f} : a;
+        }
+        static __device__ __forceinline__ int64_t share(Digits d, uint32_t digits, int shift)
+        {
+            return (int64_t)((uint64_t)d.digits * digits >> min(d.shift + shift, 63));
+        }
+        // in units of 2^-46
+        __device__ __forceinline__ int64_t operator()(int j, T z, T y) const
+        {
+            if constexpr (EXACT) {
+                Units one;
+                one.add(exact(j, z, y));
+                return one.whole();
+            } else {
+                int64_t w = share(p(to_float(z)), p_digits, p_shift);
+                if (less) w -= share(q(to_float(y)), q_digits, q_shift);
+                return j == without || w < 0 ? 0 : w;
+            }
+        }
+        template <int N>
+        __device__ __forceinline__ int64_t sum(int j, const T (&z)[N], const T (&y)[N]) const
+        {
+            if constexpr (EXACT) {
+                Units all;
+#pragma unroll
+                for (int u = 0; u < N; ++u) all.add(exact(j + u * 32, z[u], y[u]));
+                return all.whole();
+            } else {
+                int64_t all = 0;
+#pragma unroll
+                for (int u = 0; u < N; ++u) all += (*this)(j + u * 32, z[u], y[u]);
+                return all;
+            }
         }
     };
 
@@ -329,17 +446,16 @@ struct Walk {
     }
 
     // The smallest token whose running sum of weights passes v times all of them, and its logit: on the thread that finds it, -1 on
-    // the others.  Sets sh.none where no token has a weight.
-    __device__ __forceinline__ int draw(const Weights &weight, float v, float &logit)
+    // the others.  Sets sh.none where no token has a weight; without EXACT sh.unsure where the place lies so near to a border between
+    // two tokens' weights that their errors may have moved it.
+    template <bool EXACT>
+    __device__ __forceinline__ int draw(const T *p, const T *q, const Weights<EXACT> &weight, float v, float &logit)
     {
         constexpr int N = PIECE / 32;
         const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
         int64_t all = 0;                 // on lane 0
-        each_piece(weight.p.z, weight.q.z, [&](int i, const T (&z)[N], const T (&y)[N]) {
-            Units units;
-#pragma unroll
-            for (int u = 0; u < N; ++u) units.add(weight((first_piece + i) * PIECE + u * 32 + lane, z[u], y[u]));
-            int64_t sum = units.whole();
+        each_piece(p, q, [&](int i, const T (&z)[N], const T (&y)[N]) {
+            int64_t sum = weight.sum((first_piece + i) * PIECE + lane, z, y);
 #pragma unroll
             for (int off = 16; off >= 1; off >>= 1) sum += __shfl_xor_sync(FULL, sum, off);
             if (lane == 0) sh.weight[i] = sum, all += sum;
@@ -355,6 +471,7 @@ struct Walk {
                 total += x;
             }
             sh.none = total <= 0;
+            sh.unsure = false;
             sh.before = before;
             sh.at = share_of_total(v, total);
         }
@@ -382,19 +499,12 @@ struct Walk {
             __syncwarp();
             // a lane's neighbouring tokens of it
             const int j0 = sh.piece * PIECE + lane * N;
-            T z[N], y[N];
-#pragma unroll
+            int64_t sum = 0;
+#pragma unroll 1
             for (int u = 0; u < N; ++u) {
-                z[u] = y[u] = from_float<T>(-INFINITY);
-                if (j0 + u < cols) z[u] = weight.p.z[j0 + u];
-                if (j0 + u < cols && weight.q.z) y[u] = weight.q.z[j0 + u];
-            }
-            int64_t w[N], sum = 0;
-#pragma unroll
-            for (int u = 0; u < N; ++u) {
-                Units one;
-                one.add(weight(j0 + u, z[u], y[u]));
-                w[u] = one.whole(), sum += w[u];
+                const int64_t w = j0 + u < cols ? weight(j0 + u, p[j0 + u], q ? q[j0 + u] : p[j0 + u]) : 0;
+                sh.lane_weight[lane * N + u] = w;
+                sum += w;
             }
             up = sum;
 #pragma unroll
@@ -403,12 +513,17 @@ struct Walk {
                 if (lane >= off) up += x;
             }
             below = sh.below + up - sum;
-#pragma unroll
+            const int64_t margin = EXACT ? 0 : MARGIN;
+            bool sure = false;
+#pragma unroll 1
             for (int u = 0; u < N; ++u) {
-                if (at >= below && at < below + w[u]) found = j0 + u, logit = to_float(z[u]);
-                below += w[u];
+                const int64_t w = sh.lane_weight[lane * N + u];
+                if (at >= below + margin && at < below + w - margin) found = j0 + u, logit = to_float(p[j0 + u]), sure = true;
+                below += w;
             }
+            if (!EXACT && !__any_sync(FULL, sure) && lane < blocks) cluster.map_shared_rank(&sh, lane)->unsure = true;
         }
+        if (!EXACT) cluster.sync();      // every block knows
         return found;
     }
 };
@@ -422,11 +537,45 @@ struct VerifyOut {
 // x (in powers of two) are off by 2.1 |x| 2^-24 with |x| < 126 where they count, sums by the mean of that and their roundings: 2^-14.
 constexpr float SURE = 0x1p-12f;
 
+// a row's m, s and its logit of the drafted token, from k_verify_rows
+struct Given {
+    float m, s, z, unused;
+};
+
+// Few sequences: the statistics of all their rows at once, a cluster for each.
+template <typename T, int THREADS>
+__global__ __launch_bounds__(THREADS, 1024 / THREADS) void k_verify_rows(const T *target, int64_t t_stride, const T *draft,
+                                                                         int64_t d_stride, int cols, Ids ids, int64_t targets, int D,
+                                                                         float scale, float draft_scale, Given *__restrict__ given)
+{
+    after_previous();
+    let_next_start();
+    __shared__ Shared sh;
+    cg::cluster_group cluster = cg::this_cluster();
+    const int blocks = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
+    const int64_t r = blockIdx.x / (unsigned)blocks;
+    const bool drafts = r >= targets;
+    const int64_t i = drafts ? r - targets : r, s = i / (drafts ? D : D + 1);
+    const int d = (int)(i - s * (drafts ? D : D + 1));
+    const T *row = drafts ? draft + i * d_stride : target + i * t_stride;
+    const bool writes = rank == 0 && threadIdx.x == 0;
+    float z = 0.0f;
+    if (writes && d < D) {
+        const int64_t t = load_id(ids, s, d);
+        if (t >= 0 && t < cols) z = to_float(row[t]);
+    }
+    Walk<T, THREADS> walk{sh, cluster, rank, blocks, cols, 0, 0};
+    walk.stats(1, [&](int) { return row; }, [&](int) { return __fmul_rn(drafts ? draft_scale : scale, LOG2E); }, 0);
+    cluster.sync();                      // the others have read this block's statistics
+    if (writes) given[r] = {sh.joined[0][0], sh.joined[0][1], z, 0.0f};
+}
+
 template <typename T, int THREADS>
 __global__ __launch_bounds__(THREADS, 1024 / THREADS) void k_verify(const T *target, int64_t t_stride, const T *draft,
-                                                                    int64_t d_stride, int cols, Ids ids, int D, int group,
+                                                                    int64_t d_stride, int cols, Ids ids, int64_t n, int D,
                                                                     float scale, float draft_scale, const float *accept_u,
-                                                                    const float *draw_u, VerifyOut out, int *status)
+                                                                    const float *draw_u, const Given *given, VerifyOut out,
+                                                                    int *status)
 {
     after_previous();
     extern __shared__ __align__(16) unsigned char s_raw[];
@@ -453,100 +602,113 @@ __global__ __launch_bounds__(THREADS, 1024 / THREADS) void k_verify(const T *tar
             if (seen) set_status(status, PDB_ERANGE);
         }
     }
-    for (int i = threadIdx.x; i < 256; i += THREADS) sh.table[i] = {EXP2_TABLE.hi[i], EXP2_TABLE.lo[i]};
+    for (int i = threadIdx.x; i < 256; i += THREADS) {
+        const float h = EXP2_TABLE.hi[i], l = EXP2_TABLE.lo[i];
+        sh.table[i] = {h, l};
+        sh.fast_table[i] = {h, __int_as_float(__float2int_rn(__fmul_rn(h, 0x1p29f)) + __float2int_rn(__fmul_rn(l, 0x1p29f)))};
+    }
     const float v = draw_u[s];
     __syncthreads();
-    int length = 0;                      // drafts
-    while (length < D && sh.drafted[length] >= 0) ++length;
 
     Row<T> p{}, q{};
     p.scale = scale, q.scale = draft_scale;
     const float c = __fmul_rn(scale, LOG2E), cq = __fmul_rn(draft_scale, LOG2E);
-    const int each = draft ? 2 : 1;      // rows of a position
     int a = 0;                           // the position
-    bool refused = false, stops = false;
+    bool refused = false, exact = false;
     int t = -1;
     float log_s = 0.0f;
 #pragma unroll 1
-    for (int first = 0, turn = 0; !stops; first += group, turn ^= 1) {
-        // a group's rows; of the last position the target's alone
-        const int last = min(length, first + group - 1);
-        const int rows = (last - first + 1) * each - (draft && last == length ? 1 : 0);
-        const auto row = [&](int i) {
-            const int d = first + (each == 2 ? i >> 1 : i);
-            return each == 2 && (i & 1) ? draft + (s * D + d) * d_stride : target + (base + d) * t_stride;
-        };
-        __syncthreads();                 // the group before has been decided
-        if ((int)threadIdx.x < rows && first + (int)threadIdx.x / each < length)
-            sh.z[threadIdx.x] = to_float(row(threadIdx.x)[sh.drafted[first + (int)threadIdx.x / each]]);
-        walk.stats(rows, row, [&](int i) { return each == 2 && (i & 1) ? cq : c; }, turn);
-#pragma unroll 1
-        for (a = first;; ++a) {
-            const int i = (a - first) * each;
-            t = a < length ? sh.drafted[a] : -1;
-            p.z = row(i), p.m = sh.joined[i][0], p.s = sh.joined[i][1];
-            q.z = nullptr;
-            stops = true;
-            if (!p.valid()) break;
-            log_s = logf(p.s);
-            if (t >= 0 && draft) {
-                q.z = row(i + 1), q.m = sh.joined[i + 1][0], q.s = sh.joined[i + 1][1];
-                if (!q.valid()) t = -1, q.z = nullptr;    // the drafts end here
+    for (;; ++a) {
+        t = a < D ? sh.drafted[a] : -1;
+        p.z = target + (base + a) * t_stride;
+        q.z = t >= 0 && draft ? draft + (s * D + a) * d_stride : nullptr;
+        float z = 0.0f, zq = 0.0f;
+        if (given) {
+            const Given g = given[base + a];
+            p.m = g.m, p.s = g.s, z = g.z;
+            if (q.z) {
+                const Given h = given[n * (D + 1) + s * D + a];
+                q.m = h.m, q.s = h.s, zq = h.z;
             }
-            bool good = false, sure = true;
-            const float z = sh.z[i], u = sh.u[a < D ? a : 0];
-            if (t >= 0) {
-                const float right = __fdiv_rn(ex2(__fmul_rn(__fsub_rn(z, p.m), c)), p.s);
-                float left = u;
-                if (q.z) left = __fmul_rn(u, __fdiv_rn(ex2(__fmul_rn(__fsub_rn(sh.z[i + 1], q.m), cq)), q.s));
-                const float more = fmaxf(left, right);
-                good = left < right;
-                sure = fabsf(left - right) > SURE * more && more > 1e-30f;
+        } else {
+            if (t >= 0 && threadIdx.x < (q.z ? 2 : 1)) sh.z[threadIdx.x] = to_float((threadIdx.x ? q.z : p.z)[t]);
+            walk.stats(q.z ? 2 : 1, [&](int i) { return i ? q.z : p.z; }, [&](int i) { return i ? cq : c; }, a & 1);
+            p.m = sh.joined[0][0], p.s = sh.joined[0][1], z = sh.z[0];
+            if (q.z) q.m = sh.joined[1][0], q.s = sh.joined[1][1], zq = sh.z[1];
+            __syncthreads();             // before the next position's
+        }
+        if (!p.valid()) break;
+        log_s = logf(p.s);
+        if (q.z && !q.valid()) t = -1, q.z = nullptr;     // the drafts end here
+        if (t < 0) break;
+        const float u = sh.u[a];
+        const float right = __fdiv_rn(ex2(__fmul_rn(__fsub_rn(z, p.m), c)), p.s);
+        float left = u;
+        if (q.z) left = __fmul_rn(u, __fdiv_rn(ex2(__fmul_rn(__fsub_rn(zq, q.m), cq)), q.s));
+        const float more = fmaxf(left, right);
+        bool good = left < right;
+        if (!(fabsf(left - right) > SURE * more && more > 1e-30f)) {
+            walk.template sums<true>(p, q);
+            exact = true;                // of this position
+            if (threadIdx.x == 0) {
+                const auto in_64 = [](float scale, float z, const Row<T> &r, Two sum) {
+                    return exp((double)scale * ((double)z - (double)r.m)) / ((double)sum.hi + (double)sum.lo);
+                };
+                const double pe = in_64(scale, z, p, sh.row_sum[0]);
+                const double qe = q.z ? in_64(draft_scale, zq, q, sh.row_sum[1]) : 1.0;
+                sh.good = (double)u * qe < pe;
             }
-            if (!good || !sure) {
-                walk.exact_sums(p, q);
-                if (!sure) {
-                    if (threadIdx.x == 0) {
-                        const auto in_64 = [](float scale, float z, const Row<T> &r, Two sum) {
-                            return exp((double)scale * ((double)z - (double)r.m)) / ((double)sum.hi + (double)sum.lo);
-                        };
-                        const double pe = in_64(scale, z, p, sh.row_sum[0]);
-                        const double qe = q.z ? in_64(draft_scale, sh.z[i + 1], q, sh.row_sum[1]) : 1.0;
-                        sh.good = (double)u * qe < pe;
-                    }
-                    __syncthreads();
-                    good = sh.good;
-                }
-                if (!good) {
-                    refused = t >= 0;
-                    break;
-                }
-            }
-            if (writes) {
-                out.tokens[base + a] = t;
-                if (out.logp) out.logp[base + a] = __fmaf_rn(__fsub_rn(z, p.m), scale, -log_s);
-            }
-            if (a == last) {
-                stops = false;
-                break;
-            }
+            __syncthreads();
+            good = sh.good;
+        } else {
+            exact = false;
+        }
+        if (!good) {
+            refused = true;
+            break;
+        }
+        if (writes) {
+            out.tokens[base + a] = t;
+            if (out.logp) out.logp[base + a] = __fmaf_rn(__fsub_rn(z, p.m), scale, -log_s);
         }
     }
     bool none = true;
     if (p.valid()) {
-        typename Walk<T, THREADS>::Weights weight{p, q, sh.row_inv[0], sh.row_inv[1], refused && !q.z ? t : -1, sh.table};
+        if (!refused) q.z = nullptr;
+        // one row's weights need no more than a common factor: the power of two that takes their sum to 1/2 to 1
+        const int half = (int)(__float_as_uint(__fmul_rn(p.s, 1.0f + 0x1p-10f)) >> 23) - 126;      // sum < 2^half
+        int without = refused && !q.z ? t : -1;
+        const auto reach = [](const Row<T> &r) { return r.scale > 1e-30f && fabsf(__fmul_rn(r.m, __fmul_rn(r.scale, LOG2E))) < REACH; };
+        bool fast = !exact && cols <= MOST_FAST && reach(p) && (!q.z || reach(q));
 #pragma unroll 1
         for (;;) {
             float z = 0.0f;
-            const int drawn = walk.draw(weight, v, z);
+            int drawn;
+            if (fast) {
+                typename Walk<T, THREADS>::template Weights<false> weight;
+                if (q.z) walk.template sums<false>(p, q);
+                weight.p = Term<false>(p.m, p.scale, sh.fast_table), weight.q = Term<false>(q.m, q.scale, sh.fast_table);
+                weight.p_digits = q.z ? sh.inv_digits[0] : 1u << 31, weight.p_shift = q.z ? sh.inv_shift[0] : 29 - 46 + 31 + half;
+                weight.q_digits = sh.inv_digits[1], weight.q_shift = sh.inv_shift[1];
+                weight.without = without, weight.less = q.z != nullptr;
+                drawn = walk.template draw<false>(p.z, q.z, weight, v, z);
+            } else {
+                if (q.z) walk.template sums<true>(p, q);
+                const Two unit = {__int_as_float((127 - half) << 23), 0.0f};
+                drawn = walk.template draw<true>(p.z, q.z,
+                                                 {{p.m, p.scale, sh.table}, {q.m, q.scale, sh.table}, q.z ? sh.row_inv[0] : unit,
+                                                  sh.row_inv[1], 0, 0, 0, 0, without, q.z != nullptr}, v, z);
+            }
             none = sh.none;
+            const bool unsure = fast && (none || sh.unsure);
             if (drawn >= 0) {
                 out.tokens[base + a] = drawn;
                 if (out.logp) out.logp[base + a] = __fmaf_rn(__fsub_rn(z, p.m), scale, -log_s);
             }
-            if (!none || !refused) break;
-            // nothing of p - q that 2^-46 could tell: from p
-            refused = false, weight.q.z = nullptr, weight.without = -1;
+            if (!unsure && (!none || !refused)) break;
+            // once more, exactly; or, with nothing of p - q that 2^-46 could tell, from p
+            if (!unsure) refused = false, q.z = nullptr, without = -1;
+            fast = false;
             __syncthreads();
         }
     } else {
@@ -597,20 +759,32 @@ int pdb_verify(pdb_tokens *t, const pdb_mat *target, const pdb_ids *draft_ids, i
     TokensUse use{t, s};
     return with_type(target->type, [&](auto *a) {
         using T = std::remove_pointer_t<decltype(a)>;
+        const int64_t nv = target->cols / Vec<T>::E + 1, rows = target->rows + (draft ? drafts : 0);
+        const bool few = n * MAX_CLUSTER <= t->sms && rows <= VERIFY_ROWS, ahead = few && n_drafts > 0;
         Shape shape = {};
-        const int64_t nv = target->cols / Vec<T>::E + 1;
-        shape.threads = n * MAX_CLUSTER <= t->sms ? 512 : 256;
+        shape.threads = few ? 512 : 256;
         shape.blocks = cluster_of(n, nv, shape.threads, [&](int blocks) { return t->sms * (1024 / shape.threads) / blocks; });
         shape.clusters = n;
-        const int group = n * MAX_CLUSTER <= t->sms ? MAX_GROUP : 1;
         shape.smem = verify_smem(target->cols, shape.blocks);
+        const Ids id = n_drafts > 0 ? ids_of(draft_ids) : Ids{};
+        const T *z = (const T *)target->data, *y = draft ? (const T *)draft->data : nullptr;
+        const int64_t z_step = stride_of(target), y_step = draft ? stride_of(draft) : 0;
+        Given *given = ahead ? (Given *)t->given : nullptr;
+        if (ahead) {
+            Shape each = shape;
+            each.blocks = cluster_of(rows, nv, 512, [&](int blocks) { return t->sms * 2 / blocks; });
+            each.clusters = rows;
+            each.smem = 0;
+            const int rc = launch_rows(k_verify_rows<T, 512>, each, s, z, z_step, y, y_step, (int)target->cols, id, target->rows,
+                                       (int)n_drafts, scale, draft_scale, given);
+            if (rc != PDB_OK) return rc;
+        }
         const auto run = [&](auto k) {
-            return launch_rows(k_verify<T, decltype(k)::value>, shape, s, (const T *)target->data, stride_of(target),
-                               draft ? (const T *)draft->data : (const T *)nullptr, draft ? stride_of(draft) : 0,
-                               (int)target->cols, n_drafts > 0 ? ids_of(draft_ids) : Ids{}, (int)n_drafts, group, scale, draft_scale,
-                               accept_u, draw_u, VerifyOut{tokens, accepted, logp}, t->status);
+            return launch_rows(k_verify<T, decltype(k)::value>, shape, s, z, z_step, y, y_step, (int)target->cols, id, n,
+                               (int)n_drafts, scale, draft_scale, accept_u, draw_u, (const Given *)given,
+                               VerifyOut{tokens, accepted, logp}, t->status);
         };
-        return shape.threads == 512 ? run(Num<512>()) : run(Num<256>());
+        return few ? run(Num<512>()) : run(Num<256>());
     });
 }
 
