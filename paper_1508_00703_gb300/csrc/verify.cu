@@ -139,40 +139,49 @@ constexpr float REACH = 512.0f;
 constexpr int64_t MOST_FAST = 1 << 17;  // tokens
 
 struct Digits {
-    uint32_t digits;                    // 2^29 to 2^30
-    int shift;                          // exp = digits * 2^-29 / 2^shift
+    uint32_t digits[2];                 // 2^29 to 2^30, of two tokens
+    int shift[2];                       // exp = digits * 2^-29 / 2^(shift - shift0)
 };
+// by any amount: nothing is left from 64 on
+__device__ __forceinline__ uint64_t shifted(uint64_t x, int by)
+{
+    asm("shr.u64 %0, %0, %1;" : "+l"(x) : "r"(by));
+    return x;
+}
 template <>
 struct Term<false> {
-    float ch, cl, from, rest, low;
+    uint64_t ch, cl, from, rest;        // two of each
+    float low;
+    int shift0;                         // added to the shifts
     const float2 *table;                // 2^(i/256), and the same in units of 2^-29
     Term() = default;
-    __device__ __forceinline__ Term(float m, float scale, const float2 *table_) : table(table_)
+    __device__ __forceinline__ Term(float m, float scale, const float2 *table_, int shift0_) : shift0(shift0_ + (0x4b400000 >> 8)), table(table_)
     {
         constexpr float log2e_rest = (float)(1.4426950408889634073599 - (double)LOG2E);
         const float c = __fmul_rn(scale, LOG2E), c_rest = __fmaf_rn(scale, log2e_rest, __fmaf_rn(scale, LOG2E, -c));
-        ch = __fmul_rn(c, 256.0f), cl = __fmul_rn(c_rest, 256.0f);
-        const float mc = __fmul_rn(m, ch), whole = rintf(mc);
-        from = __fsub_rn(12582912.0f, whole);
-        rest = __fadd_rn(__fsub_rn(mc, whole), __fmaf_rn(m, cl, __fmaf_rn(m, ch, -mc)));
+        const float c256 = __fmul_rn(c, 256.0f), l256 = __fmul_rn(c_rest, 256.0f);
+        const float mc = __fmul_rn(m, c256), whole = rintf(mc), fr = __fsub_rn(12582912.0f, whole);
+        const float r = __fadd_rn(__fsub_rn(mc, whole), __fmaf_rn(m, l256, __fmaf_rn(m, c256, -mc)));
+        ch = pair(c256, c256), cl = pair(l256, l256), from = pair(fr, fr), rest = pair(-r, -r);
         low = __fsub_rn(m, __fdiv_rn(60.0f, c));             // nothing below 2^-60
     }
-    __device__ __forceinline__ Digits operator()(float z) const
+    __device__ __forceinline__ Digits operator()(float z0, float z1) const
     {
         constexpr float K1 = (float)(LN2_D / 256), K2 = (float)(LN2_D / 256 * LN2_D / 512),
                         K3 = (float)(LN2_D / 256 * LN2_D / 512 * LN2_D / 768);
-        z = fmaxf(z, low);
-        const float t = __fmaf_rn(z, ch, from);              // n in its lowest bits
-        const float f = __fadd_rn(__fmaf_rn(z, ch, -__fsub_rn(t, from)), __fmaf_rn(z, cl, -rest));
-        const float s = __fmul_rn(f, __fmaf_rn(f, __fmaf_rn(f, K3, K2), K1));
-        const int n = __float_as_int(t);
-        const float2 tab = table[n & 255];
-        const float more = __fmaf_rn(__fmul_rn(tab.x, s), 0x1p29f, 12582912.0f);
-        return {(uint32_t)(__float_as_int(tab.y) + __float_as_int(more) - 0x4b400000), (0x4b400000 >> 8) - (n >> 8)};
+        const uint64_t z = pair(fmaxf(z0, low), fmaxf(z1, low));
+        const uint64_t t = fma2(z, ch, from);                // n in its lowest bits
+        const uint64_t f = add2(fma2(z, ch, fma2(t, pair(-1.0f, -1.0f), from)), fma2(z, cl, rest));
+        const uint64_t s = mul2(f, fma2(f, fma2(f, pair(K3, K3), pair(K2, K2)), pair(K1, K1)));
+        float t0, t1, x0, x1;
+        unpair(t, t0, t1);
+        const int n0 = __float_as_int(t0), n1 = __float_as_int(t1);
+        const float2 a = table[n0 & 255], b = table[n1 & 255];
+        unpair(fma2(mul2(pair(a.x, b.x), s), pair(0x1p29f, 0x1p29f), pair(12582912.0f, 12582912.0f)), x0, x1);
+        return {{(uint32_t)(__float_as_int(a.y) + __float_as_int(x0) - 0x4b400000), (uint32_t)(__float_as_int(b.y) + __float_as_int(x1) - 0x4b400000)},
+                {shift0 - (n0 >> 8), shift0 - (n1 >> 8)}};
     }
 };
-// in units of 2^-45
-__device__ __forceinline__ int64_t whole_of(Digits d) { return (int64_t)((uint64_t)d.digits << 16 >> d.shift); }
 
 // How far from its token's borders a draw by Term<false> must lie to be taken, for weights that add up to 2^46: the running sum and v
 // times the whole one are moved by the terms of both rows and by their sums (4 * 2^-28.6 together), and by 2^17 tokens' cut off units in the sums
@@ -195,7 +204,6 @@ struct Shared {
     int64_t total;                      // this block's weights
     int64_t at, before;                 // the drawn place among all weights, the weights of lower blocks
     int64_t below;                      // weights before the piece that holds the drawn token
-    int64_t lane_weight[PIECE];         // of the tokens of that piece
     int none, piece, good, unsure;
     float2 table[256], fast_table[256]; // of Term<true>, of Term<false>
     int64_t weight[1];                  // of each of the block's pieces (as many as there are)
@@ -333,6 +341,13 @@ struct Walk {
         return x;
     }
 
+    template <bool EXACT>
+    __device__ __forceinline__ Term<EXACT> term_of(const Row<T> &r, int shift0) const
+    {
+        if constexpr (EXACT) return {r.m, r.scale, sh.table};
+        else return {r.m, r.scale, sh.fast_table, shift0};
+    }
+
     // The rows' sums, into sh.row_sum and sh.row_inv: good to 2^-42, or as good as Term<false> is.  Whole numbers are added up: no
     // order of warps and blocks shows in them.
     template <bool EXACT>
@@ -341,7 +356,7 @@ struct Walk {
         constexpr int N = PIECE / 32;
 #pragma unroll 1
         for (int which = 0; which < (q.z ? 2 : 1); ++which) {
-            const Term<EXACT> term(which ? q.m : p.m, which ? q.scale : p.scale, EXACT ? sh.table : sh.fast_table);
+            const auto term = term_of<EXACT>(which ? q : p, 0);
             int64_t high = 0, low = 0;
             each_piece(which ? q.z : p.z, nullptr, [&](int, const T (&x)[N], const T (&)[N]) {
                 if constexpr (EXACT) {
@@ -351,7 +366,11 @@ struct Walk {
                     high += sum.high, low += sum.low;
                 } else {
 #pragma unroll
-                    for (int u = 0; u < N; ++u) low += whole_of(term(to_float(x[u])));
+                    for (int u = 0; u < N; u += 2) {
+                        const Digits d = term(to_float(x[u]), to_float(x[u + 1]));
+                        // in units of 2^-45
+                        low += (int64_t)(shifted((uint64_t)d.digits[0] << 16, d.shift[0]) + shifted((uint64_t)d.digits[1] << 16, d.shift[1]));
+                    }
                 }
             });
             if (EXACT) high = block_sum(high, sh.warp_sum[0]);
@@ -379,16 +398,15 @@ struct Walk {
         cluster.sync();                  // the others' sums have been read
     }
 
-    // a token's weight in a draw
+    // tokens' weights in a draw
     template <bool EXACT>
     struct Weights {
         Term<EXACT> p, q;
         Two p_inv, q_inv;                // EXACT
         uint32_t p_digits, q_digits;     // else
-        int p_shift, q_shift;
         int without;                     // a token left out
         bool less;                       // the draft's probabilities are taken off
-        __device__ __forceinline__ Two exact(int j, T z, T y) const
+        __device__ __forceinline__ Two exact(T z, T y) const
         {
             Two a = times(p(to_float(z)), p_inv);
             if (less) {
@@ -397,39 +415,44 @@ struct Walk {
                 const float dl = __fsub_rn(__fsub_rn(a.hi, __fsub_rn(d, e)), __fadd_rn(b.hi, e));
                 a = {d, __fadd_rn(dl, __fsub_rn(a.lo, b.lo))};
             }
-            return j == without || a.hi < 0.0f ? Two{0.0f, 0.0f} : a;
+            return __fadd_rn(a.hi, a.lo) < 0.0f ? Two{0.0f, 0.0f} : a;
         }
-        static __device__ __forceinline__ int64_t share(Digits d, uint32_t digits, int shift)
-        {
-            return (int64_t)((uint64_t)d.digits * digits >> min(d.shift + shift, 63));
-        }
-        // in units of 2^-46
-        __device__ __forceinline__ int64_t operator()(int j, T z, T y) const
+        // of two tokens, in units of 2^-46
+        __device__ __forceinline__ void two(T z0, T z1, T y0, T y1, int64_t (&w)[2]) const
         {
             if constexpr (EXACT) {
-                Units one;
-                one.add(exact(j, z, y));
-                return one.whole();
+                const Two a[2] = {exact(z0, y0), exact(z1, y1)};
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    Units one;
+                    one.add(a[i]);
+                    w[i] = one.whole();
+                }
             } else {
-                int64_t w = share(p(to_float(z)), p_digits, p_shift);
-                if (less) w -= share(q(to_float(y)), q_digits, q_shift);
-                return j == without || w < 0 ? 0 : w;
+                const Digits d = p(to_float(z0), to_float(z1));
+#pragma unroll
+                for (int i = 0; i < 2; ++i) w[i] = (int64_t)shifted((uint64_t)d.digits[i] * p_digits, d.shift[i]);
+                if (less) {
+                    const Digits e = q(to_float(y0), to_float(y1));
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) w[i] = max((long long)(w[i] - (int64_t)shifted((uint64_t)e.digits[i] * q_digits, e.shift[i])), 0ll);
+                }
             }
         }
+        // of a lane's tokens j, j + step, ..
         template <int N>
-        __device__ __forceinline__ int64_t sum(int j, const T (&z)[N], const T (&y)[N]) const
+        __device__ __forceinline__ void all(int j, int step, const T (&z)[N], const T (&y)[N], int64_t (&w)[N]) const
         {
-            if constexpr (EXACT) {
-                Units all;
 #pragma unroll
-                for (int u = 0; u < N; ++u) all.add(exact(j + u * 32, z[u], y[u]));
-                return all.whole();
-            } else {
-                int64_t all = 0;
-#pragma unroll
-                for (int u = 0; u < N; ++u) all += (*this)(j + u * 32, z[u], y[u]);
-                return all;
+            for (int u = 0; u < N; u += 2) {
+                int64_t x[2];
+                two(z[u], z[u + 1], y[u], y[u + 1], x);
+                w[u] = x[0], w[u + 1] = x[1];
             }
+            if (without >= 0)
+#pragma unroll
+                for (int u = 0; u < N; ++u)
+                    if (j + u * step == without) w[u] = 0;
         }
     };
 
@@ -455,9 +478,11 @@ struct Walk {
         const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
         int64_t all = 0;                 // on lane 0
         each_piece(p, q, [&](int i, const T (&z)[N], const T (&y)[N]) {
-            int64_t sum = weight.sum((first_piece + i) * PIECE + lane, z, y);
-#pragma unroll
-            for (int off = 16; off >= 1; off >>= 1) sum += __shfl_xor_sync(FULL, sum, off);
+            int64_t w[N];
+            weight.all((first_piece + i) * PIECE + lane, 32, z, y, w);
+            // the lanes' sums, below 2^48, added up in two halves
+            const uint64_t own = (uint64_t)(w[0] + w[1] + w[2] + w[3]);
+            const int64_t sum = ((int64_t)__reduce_add_sync(FULL, (unsigned)(own >> 24)) << 24) + __reduce_add_sync(FULL, (unsigned)own & 0xffffff);
             if (lane == 0) sh.weight[i] = sum, all += sum;
         });
         all = block_sum(all, sh.warp_sum[0]);
@@ -499,13 +524,17 @@ struct Walk {
             __syncwarp();
             // a lane's neighbouring tokens of it
             const int j0 = sh.piece * PIECE + lane * N;
-            int64_t sum = 0;
-#pragma unroll 1
+            T z[N], y[N];
+#pragma unroll
             for (int u = 0; u < N; ++u) {
-                const int64_t w = j0 + u < cols ? weight(j0 + u, p[j0 + u], q ? q[j0 + u] : p[j0 + u]) : 0;
-                sh.lane_weight[lane * N + u] = w;
-                sum += w;
+                z[u] = y[u] = from_float<T>(-INFINITY);
+                if (j0 + u < cols) z[u] = p[j0 + u];
+                if (j0 + u < cols && q) y[u] = q[j0 + u];
             }
+            int64_t w[N], sum = 0;
+            weight.all(j0, 1, z, y, w);
+#pragma unroll
+            for (int u = 0; u < N; ++u) sum += w[u];
             up = sum;
 #pragma unroll
             for (int off = 1; off < 32; off <<= 1) {
@@ -515,11 +544,10 @@ struct Walk {
             below = sh.below + up - sum;
             const int64_t margin = EXACT ? 0 : MARGIN;
             bool sure = false;
-#pragma unroll 1
+#pragma unroll
             for (int u = 0; u < N; ++u) {
-                const int64_t w = sh.lane_weight[lane * N + u];
-                if (at >= below + margin && at < below + w - margin) found = j0 + u, logit = to_float(p[j0 + u]), sure = true;
-                below += w;
+                if (at >= below + margin && at < below + w[u] - margin) found = j0 + u, logit = to_float(z[u]), sure = true;
+                below += w[u];
             }
             if (!EXACT && !__any_sync(FULL, sure) && lane < blocks) cluster.map_shared_rank(&sh, lane)->unsure = true;
         }
@@ -685,11 +713,11 @@ __global__ __launch_bounds__(THREADS, 1024 / THREADS) void k_verify(const T *tar
             float z = 0.0f;
             int drawn;
             if (fast) {
-                typename Walk<T, THREADS>::template Weights<false> weight;
                 if (q.z) walk.template sums<false>(p, q);
-                weight.p = Term<false>(p.m, p.scale, sh.fast_table), weight.q = Term<false>(q.m, q.scale, sh.fast_table);
-                weight.p_digits = q.z ? sh.inv_digits[0] : 1u << 31, weight.p_shift = q.z ? sh.inv_shift[0] : 29 - 46 + 31 + half;
-                weight.q_digits = sh.inv_digits[1], weight.q_shift = sh.inv_shift[1];
+                typename Walk<T, THREADS>::template Weights<false> weight;
+                weight.p = walk.template term_of<false>(p, q.z ? sh.inv_shift[0] : 29 - 46 + 31 + half);
+                weight.q = walk.template term_of<false>(q, sh.inv_shift[1]);
+                weight.p_digits = q.z ? sh.inv_digits[0] : 1u << 31, weight.q_digits = sh.inv_digits[1];
                 weight.without = without, weight.less = q.z != nullptr;
                 drawn = walk.template draw<false>(p.z, q.z, weight, v, z);
             } else {
@@ -697,7 +725,7 @@ __global__ __launch_bounds__(THREADS, 1024 / THREADS) void k_verify(const T *tar
                 const Two unit = {__int_as_float((127 - half) << 23), 0.0f};
                 drawn = walk.template draw<true>(p.z, q.z,
                                                  {{p.m, p.scale, sh.table}, {q.m, q.scale, sh.table}, q.z ? sh.row_inv[0] : unit,
-                                                  sh.row_inv[1], 0, 0, 0, 0, without, q.z != nullptr}, v, z);
+                                                  sh.row_inv[1], 0, 0, without, q.z != nullptr}, v, z);
             }
             none = sh.none;
             const bool unsure = fast && (none || sh.unsure);
