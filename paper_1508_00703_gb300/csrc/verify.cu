@@ -113,12 +113,13 @@ struct Units {
     }
     __device__ __forceinline__ int64_t whole() const { return ((int64_t)high << 23) + low; }
 };
-__device__ __forceinline__ Two two_of(int64_t high, int64_t low)
+// (high * 2^23 + low) * unit
+__device__ __forceinline__ Two two_of(int64_t high, int64_t low, float unit)
 {
     high += low >> 23, low &= 0x7fffff;
     const float h = __ll2float_rn(high);
     const int64_t rest = high - __float2ll_rn(h);
-    return {__fmul_rn(h, 0x1p-23f), __fmul_rn(__ll2float_rn(rest * 0x800000 + low), 0x1p-46f)};
+    return {__fmul_rn(h, __fmul_rn(unit, 0x1p23f)), __fmul_rn(__ll2float_rn(rest * 0x800000 + low), unit)};
 }
 
 // exp(scale (z - m)) of a row's tokens, z <= m
@@ -132,15 +133,29 @@ struct Term<true> {
     __device__ __forceinline__ Two operator()(float z) const { return exp_two(z, m, scale, table); }
 };
 
-// The same good to 2^-28.6, at half the price, where |m scale| log2(e) < 2^9: n + f = 256 (z c - m c), c = scale log2(e), n whole and |f| <= 1,
-// f formed by roundings of 2^-25; then 2^(i/256) 2^(f/256) as a whole number of 2^-29, and 2^-k, n = 256 (-k) + i.  An error that
+// The same good to 2^-29.7, at half the price, where |m scale| log2(e) < 2^9: n + f = 512 (z c - m c), c = scale log2(e), n whole and |f| <= 1,
+// f formed by roundings of 2^-25; then 2^(i/512) 2^(f/512) as a whole number of 2^-30, and 2^-k, n = 512 (-k) + i.  An error that
 // all tokens of a row share falls out of its probabilities.
 constexpr float REACH = 512.0f;
-constexpr int64_t MOST_FAST = 1 << 17;  // tokens
+constexpr int STEPS = 512, LOG_STEPS = 9;
+
+struct FastTable {
+    float value[STEPS];                 // 2^(i/512)
+    int digits[STEPS];                  // the same in units of 2^-30
+    constexpr FastTable() : value(), digits()
+    {
+        for (int i = 0; i < STEPS; ++i) {
+            const double v = exp_series(LN2_D * i / STEPS);
+            value[i] = (float)v;
+            digits[i] = (int)(v * 0x1p30 + 0.5);
+        }
+    }
+};
+__device__ const FastTable FAST_TABLE;
 
 struct Digits {
-    uint32_t digits[2];                 // 2^29 to 2^30, of two tokens
-    int shift[2];                       // exp = digits * 2^-29 / 2^(shift - shift0)
+    uint32_t digits[2];                 // 2^30 to 2^31, of two tokens
+    int shift[2];                       // exp = digits * 2^-30 / 2^(shift - shift0)
 };
 // by any amount: nothing is left from 64 on
 __device__ __forceinline__ uint64_t shifted(uint64_t x, int by)
@@ -153,22 +168,22 @@ struct Term<false> {
     uint64_t ch, cl, from, rest;        // two of each
     float low;
     int shift0;                         // added to the shifts
-    const float2 *table;                // 2^(i/256), and the same in units of 2^-29
+    const float2 *table;                // 2^(i/512), and the same in units of 2^-30
     Term() = default;
-    __device__ __forceinline__ Term(float m, float scale, const float2 *table_, int shift0_) : shift0(shift0_ + (0x4b400000 >> 8)), table(table_)
+    __device__ __forceinline__ Term(float m, float scale, const float2 *table_, int shift0_) : shift0(shift0_ + (0x4b400000 >> LOG_STEPS)), table(table_)
     {
         constexpr float log2e_rest = (float)(1.4426950408889634073599 - (double)LOG2E);
         const float c = __fmul_rn(scale, LOG2E), c_rest = __fmaf_rn(scale, log2e_rest, __fmaf_rn(scale, LOG2E, -c));
-        const float c256 = __fmul_rn(c, 256.0f), l256 = __fmul_rn(c_rest, 256.0f);
-        const float mc = __fmul_rn(m, c256), whole = rintf(mc), fr = __fsub_rn(12582912.0f, whole);
-        const float r = __fadd_rn(__fsub_rn(mc, whole), __fmaf_rn(m, l256, __fmaf_rn(m, c256, -mc)));
-        ch = pair(c256, c256), cl = pair(l256, l256), from = pair(fr, fr), rest = pair(-r, -r);
+        const float c1 = __fmul_rn(c, (float)STEPS), c2 = __fmul_rn(c_rest, (float)STEPS);
+        const float mc = __fmul_rn(m, c1), whole = rintf(mc), fr = __fsub_rn(12582912.0f, whole);
+        const float r = __fadd_rn(__fsub_rn(mc, whole), __fmaf_rn(m, c2, __fmaf_rn(m, c1, -mc)));
+        ch = pair(c1, c1), cl = pair(c2, c2), from = pair(fr, fr), rest = pair(-r, -r);
         low = __fsub_rn(m, __fdiv_rn(60.0f, c));             // nothing below 2^-60
     }
     __device__ __forceinline__ Digits operator()(float z0, float z1) const
     {
-        constexpr float K1 = (float)(LN2_D / 256), K2 = (float)(LN2_D / 256 * LN2_D / 512),
-                        K3 = (float)(LN2_D / 256 * LN2_D / 512 * LN2_D / 768);
+        constexpr double L = LN2_D / STEPS;
+        constexpr float K1 = (float)L, K2 = (float)(L * L / 2), K3 = (float)(L * L * L / 6);
         const uint64_t z = pair(fmaxf(z0, low), fmaxf(z1, low));
         const uint64_t t = fma2(z, ch, from);                // n in its lowest bits
         const uint64_t f = add2(fma2(z, ch, fma2(t, pair(-1.0f, -1.0f), from)), fma2(z, cl, rest));
@@ -176,17 +191,16 @@ struct Term<false> {
         float t0, t1, x0, x1;
         unpair(t, t0, t1);
         const int n0 = __float_as_int(t0), n1 = __float_as_int(t1);
-        const float2 a = table[n0 & 255], b = table[n1 & 255];
-        unpair(fma2(mul2(pair(a.x, b.x), s), pair(0x1p29f, 0x1p29f), pair(12582912.0f, 12582912.0f)), x0, x1);
+        const float2 a = table[n0 & (STEPS - 1)], b = table[n1 & (STEPS - 1)];
+        unpair(fma2(mul2(pair(a.x, b.x), s), pair(0x1p30f, 0x1p30f), pair(12582912.0f, 12582912.0f)), x0, x1);
         return {{(uint32_t)(__float_as_int(a.y) + __float_as_int(x0) - 0x4b400000), (uint32_t)(__float_as_int(b.y) + __float_as_int(x1) - 0x4b400000)},
-                {shift0 - (n0 >> 8), shift0 - (n1 >> 8)}};
+                {shift0 - (n0 >> LOG_STEPS), shift0 - (n1 >> LOG_STEPS)}};
     }
 };
 
-// How far from its token's borders a draw by Term<false> must lie to be taken, for weights that add up to 2^46: the running sum and v
-// times the whole one are moved by the terms of both rows and by their sums (4 * 2^-28.6 together), and by 2^17 tokens' cut off units in the sums
-// and the weights (2^-28 for either row): 2^-25.4 of them.
-constexpr int64_t MARGIN = (int64_t)1 << 21;
+// How far from its token's borders a draw by Term<false> must lie to be taken, for weights that add up to 2^53: the running sum and v
+// times the whole one are moved by the terms of both rows and by their sums, 4 * 2^-29.7 together; what shifts cut off is below 2^-31.
+constexpr int64_t MARGIN = (int64_t)1 << 26;
 
 // ------------------------------------------------------------------ shared by the blocks of a sequence
 struct Shared {
@@ -199,13 +213,13 @@ struct Shared {
     int64_t warp_sum[2][16];
     int64_t sum[2][2];                  // this block's sums of the two rows, in units of 2^-23 and 2^-46
     Two row_sum[2], row_inv[2];         // the rows' sums, and their reciprocals
-    uint32_t inv_digits[2];             // the reciprocal as digits / 2^inv_shift, for weights in units of 2^-46
+    uint32_t inv_digits[2];             // the reciprocal as digits / 2^(inv_shift + 53 - 30), for weights in units of 2^-53
     int inv_shift[2];
     int64_t total;                      // this block's weights
     int64_t at, before;                 // the drawn place among all weights, the weights of lower blocks
     int64_t below;                      // weights before the piece that holds the drawn token
     int none, piece, good, unsure;
-    float2 table[256], fast_table[256]; // of Term<true>, of Term<false>
+    float2 table[256], fast_table[STEPS];   // of Term<true>, of Term<false>
     int64_t weight[1];                  // of each of the block's pieces (as many as there are)
 };
 
@@ -290,6 +304,12 @@ struct Walk {
         __syncthreads();
     }
 
+    __device__ __forceinline__ void fill_table()
+    {
+        for (int i = threadIdx.x; i < 256; i += THREADS) sh.table[i] = {EXP2_TABLE.hi[i], EXP2_TABLE.lo[i]};
+        __syncthreads();
+    }
+
     // f(the lane's tokens of a piece: z and, where there is one, y) of the warp's pieces; a piece's are loaded before the one before is
     // worked on
     template <typename F>
@@ -341,6 +361,9 @@ struct Walk {
         return x;
     }
 
+    // a row's sum is below 2^above (and not below 2^(above - 2))
+    static __device__ __forceinline__ int above(const Row<T> &r) { return (int)(__float_as_uint(__fmul_rn(r.s, 1.0f + 0x1p-10f)) >> 23) - 126; }
+
     template <bool EXACT>
     __device__ __forceinline__ Term<EXACT> term_of(const Row<T> &r, int shift0) const
     {
@@ -357,6 +380,7 @@ struct Walk {
 #pragma unroll 1
         for (int which = 0; which < (q.z ? 2 : 1); ++which) {
             const auto term = term_of<EXACT>(which ? q : p, 0);
+            const uint32_t up = 1u << (32 - above(which ? q : p));       // the sum is below 2^62 units of 2^-30 / up
             int64_t high = 0, low = 0;
             each_piece(which ? q.z : p.z, nullptr, [&](int, const T (&x)[N], const T (&)[N]) {
                 if constexpr (EXACT) {
@@ -368,8 +392,7 @@ struct Walk {
 #pragma unroll
                     for (int u = 0; u < N; u += 2) {
                         const Digits d = term(to_float(x[u]), to_float(x[u + 1]));
-                        // in units of 2^-45
-                        low += (int64_t)(shifted((uint64_t)d.digits[0] << 16, d.shift[0]) + shifted((uint64_t)d.digits[1] << 16, d.shift[1]));
+                        low += (int64_t)(shifted((uint64_t)d.digits[0] * up, d.shift[0]) + shifted((uint64_t)d.digits[1] * up, d.shift[1]));
                     }
                 }
             });
@@ -385,14 +408,14 @@ struct Walk {
                 const int64_t *o = cluster.map_shared_rank(&sh, b)->sum[threadIdx.x];
                 high += o[0], low += o[1];
             }
-            const Two sum = EXACT ? two_of(high, low) : two_of(low >> 22, (low & 0x3fffff) << 1), inv = inverse_of(sum);
+            const float unit = EXACT ? 0x1p-46f : __int_as_float((127 - 62 + above(threadIdx.x ? q : p)) << 23);
+            const Two sum = EXACT ? two_of(high, low, unit) : two_of(low >> 23, low & 0x7fffff, unit), inv = inverse_of(sum);
             sh.row_sum[threadIdx.x] = sum, sh.row_inv[threadIdx.x] = inv;
             if (!EXACT) {
-                // digits of 32 bits: weight = term's digits * digits / 2^(29 - 46 + shift)
                 const int e = (__float_as_int(inv.hi) >> 23) - 127;           // 2^e <= inv.hi < 2^(e + 1)
-                const int64_t units = __float2ll_rn(__fmul_rn(inv.hi, __int_as_float((30 - e + 127) << 23))) +
-                                      __float2ll_rn(__fmul_rn(inv.lo, __int_as_float((30 - e + 127) << 23)));
-                sh.inv_digits[threadIdx.x] = (uint32_t)units, sh.inv_shift[threadIdx.x] = 29 - 46 + 30 - e;
+                const float scale = __int_as_float((30 - e + 127) << 23);
+                sh.inv_digits[threadIdx.x] = (uint32_t)(__float2ll_rn(__fmul_rn(inv.hi, scale)) + __float2ll_rn(__fmul_rn(inv.lo, scale)));
+                sh.inv_shift[threadIdx.x] = 30 - 53 + 30 - e;
             }
         }
         cluster.sync();                  // the others' sums have been read
@@ -417,7 +440,7 @@ struct Walk {
             }
             return __fadd_rn(a.hi, a.lo) < 0.0f ? Two{0.0f, 0.0f} : a;
         }
-        // of two tokens, in units of 2^-46
+        // of two tokens, in units of 2^-46 (EXACT) or 2^-53
         __device__ __forceinline__ void two(T z0, T z1, T y0, T y1, int64_t (&w)[2]) const
         {
             if constexpr (EXACT) {
@@ -480,9 +503,9 @@ struct Walk {
         each_piece(p, q, [&](int i, const T (&z)[N], const T (&y)[N]) {
             int64_t w[N];
             weight.all((first_piece + i) * PIECE + lane, 32, z, y, w);
-            // the lanes' sums, below 2^48, added up in two halves
+            // the lanes' sums, 2^53 at most, added up in two halves
             const uint64_t own = (uint64_t)(w[0] + w[1] + w[2] + w[3]);
-            const int64_t sum = ((int64_t)__reduce_add_sync(FULL, (unsigned)(own >> 24)) << 24) + __reduce_add_sync(FULL, (unsigned)own & 0xffffff);
+            const int64_t sum = ((int64_t)__reduce_add_sync(FULL, (unsigned)(own >> 27)) << 27) + __reduce_add_sync(FULL, (unsigned)own & 0x7ffffff);
             if (lane == 0) sh.weight[i] = sum, all += sum;
         });
         all = block_sum(all, sh.warp_sum[0]);
@@ -599,7 +622,7 @@ __global__ __launch_bounds__(THREADS, 1024 / THREADS) void k_verify_rows(const T
 }
 
 template <typename T, int THREADS>
-__global__ __launch_bounds__(THREADS, 1024 / THREADS) void k_verify(const T *target, int64_t t_stride, const T *draft,
+__global__ __launch_bounds__(THREADS, THREADS == 512 ? 1 : 4) void k_verify(const T *target, int64_t t_stride, const T *draft,
                                                                     int64_t d_stride, int cols, Ids ids, int64_t n, int D,
                                                                     float scale, float draft_scale, const float *accept_u,
                                                                     const float *draw_u, const Given *given, VerifyOut out,
@@ -630,11 +653,7 @@ __global__ __launch_bounds__(THREADS, 1024 / THREADS) void k_verify(const T *tar
             if (seen) set_status(status, PDB_ERANGE);
         }
     }
-    for (int i = threadIdx.x; i < 256; i += THREADS) {
-        const float h = EXP2_TABLE.hi[i], l = EXP2_TABLE.lo[i];
-        sh.table[i] = {h, l};
-        sh.fast_table[i] = {h, __int_as_float(__float2int_rn(__fmul_rn(h, 0x1p29f)) + __float2int_rn(__fmul_rn(l, 0x1p29f)))};
-    }
+    for (int i = threadIdx.x; i < STEPS; i += THREADS) sh.fast_table[i] = {FAST_TABLE.value[i], __int_as_float(FAST_TABLE.digits[i])};
     const float v = draw_u[s];
     __syncthreads();
 
@@ -676,8 +695,9 @@ __global__ __launch_bounds__(THREADS, 1024 / THREADS) void k_verify(const T *tar
         const float more = fmaxf(left, right);
         bool good = left < right;
         if (!(fabsf(left - right) > SURE * more && more > 1e-30f)) {
+            if (!exact) walk.fill_table();
+            exact = true;
             walk.template sums<true>(p, q);
-            exact = true;                // of this position
             if (threadIdx.x == 0) {
                 const auto in_64 = [](float scale, float z, const Row<T> &r, Two sum) {
                     return exp((double)scale * ((double)z - (double)r.m)) / ((double)sum.hi + (double)sum.lo);
@@ -688,8 +708,6 @@ __global__ __launch_bounds__(THREADS, 1024 / THREADS) void k_verify(const T *tar
             }
             __syncthreads();
             good = sh.good;
-        } else {
-            exact = false;
         }
         if (!good) {
             refused = true;
@@ -703,11 +721,9 @@ __global__ __launch_bounds__(THREADS, 1024 / THREADS) void k_verify(const T *tar
     bool none = true;
     if (p.valid()) {
         if (!refused) q.z = nullptr;
-        // one row's weights need no more than a common factor: the power of two that takes their sum to 1/2 to 1
-        const int half = (int)(__float_as_uint(__fmul_rn(p.s, 1.0f + 0x1p-10f)) >> 23) - 126;      // sum < 2^half
         int without = refused && !q.z ? t : -1;
         const auto reach = [](const Row<T> &r) { return r.scale > 1e-30f && fabsf(__fmul_rn(r.m, __fmul_rn(r.scale, LOG2E))) < REACH; };
-        bool fast = !exact && cols <= MOST_FAST && reach(p) && (!q.z || reach(q));
+        bool fast = !exact && reach(p) && (!q.z || reach(q)), filled = exact;
 #pragma unroll 1
         for (;;) {
             float z = 0.0f;
@@ -715,14 +731,17 @@ __global__ __launch_bounds__(THREADS, 1024 / THREADS) void k_verify(const T *tar
             if (fast) {
                 if (q.z) walk.template sums<false>(p, q);
                 typename Walk<T, THREADS>::template Weights<false> weight;
-                weight.p = walk.template term_of<false>(p, q.z ? sh.inv_shift[0] : 29 - 46 + 31 + half);
+                // one row's weights need no more than a common factor, a power of two
+                weight.p = walk.template term_of<false>(p, q.z ? sh.inv_shift[0] : 30 - 53 + 31 + walk.above(p));
                 weight.q = walk.template term_of<false>(q, sh.inv_shift[1]);
                 weight.p_digits = q.z ? sh.inv_digits[0] : 1u << 31, weight.q_digits = sh.inv_digits[1];
                 weight.without = without, weight.less = q.z != nullptr;
                 drawn = walk.template draw<false>(p.z, q.z, weight, v, z);
             } else {
+                if (!filled) walk.fill_table();
+                filled = true;
                 if (q.z) walk.template sums<true>(p, q);
-                const Two unit = {__int_as_float((127 - half) << 23), 0.0f};
+                const Two unit = {__int_as_float((127 - walk.above(p)) << 23), 0.0f};
                 drawn = walk.template draw<true>(p.z, q.z,
                                                  {{p.m, p.scale, sh.table}, {q.m, q.scale, sh.table}, q.z ? sh.row_inv[0] : unit,
                                                   sh.row_inv[1], 0, 0, without, q.z != nullptr}, v, z);
@@ -788,10 +807,10 @@ int pdb_verify(pdb_tokens *t, const pdb_mat *target, const pdb_ids *draft_ids, i
     return with_type(target->type, [&](auto *a) {
         using T = std::remove_pointer_t<decltype(a)>;
         const int64_t nv = target->cols / Vec<T>::E + 1, rows = target->rows + (draft ? drafts : 0);
-        const bool few = n * MAX_CLUSTER <= t->sms && rows <= VERIFY_ROWS, ahead = few && n_drafts > 0;
+        const bool few = n * MAX_CLUSTER <= t->sms, ahead = n * 2 <= t->sms && rows <= VERIFY_ROWS && n_drafts > 0;
         Shape shape = {};
         shape.threads = few ? 512 : 256;
-        shape.blocks = cluster_of(n, nv, shape.threads, [&](int blocks) { return t->sms * (1024 / shape.threads) / blocks; });
+        shape.blocks = cluster_of(n, nv, shape.threads, [&](int blocks) { return t->sms * (few ? 2 : 8) / blocks; });
         shape.clusters = n;
         shape.smem = verify_smem(target->cols, shape.blocks);
         const Ids id = n_drafts > 0 ? ids_of(draft_ids) : Ids{};
@@ -799,10 +818,10 @@ int pdb_verify(pdb_tokens *t, const pdb_mat *target, const pdb_ids *draft_ids, i
         const int64_t z_step = stride_of(target), y_step = draft ? stride_of(draft) : 0;
         Given *given = ahead ? (Given *)t->given : nullptr;
         if (ahead) {
-            Shape each = shape;
-            each.blocks = cluster_of(rows, nv, 512, [&](int blocks) { return t->sms * 2 / blocks; });
+            Shape each = {};
+            each.threads = 512;
+            each.blocks = cluster_of(rows, nv, each.threads, [&](int blocks) { return t->sms * 2 / blocks; });
             each.clusters = rows;
-            each.smem = 0;
             const int rc = launch_rows(k_verify_rows<T, 512>, each, s, z, z_step, y, y_step, (int)target->cols, id, target->rows,
                                        (int)n_drafts, scale, draft_scale, given);
             if (rc != PDB_OK) return rc;
