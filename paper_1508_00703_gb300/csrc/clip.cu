@@ -17,7 +17,7 @@ using namespace pdb;
 
 namespace {
 
-constexpr int CLIP_THREADS = 256, CLIP_BLOCKS_PER_SM = 4;
+constexpr int CLIP_THREADS = 256, NORM_BLOCKS_PER_SM = 4, STEP_BLOCKS_PER_SM = 8;
 constexpr int64_t MOST_ELEMENTS = (int64_t)1 << 40;           // more than the memory holds
 constexpr int WIDE = 8;                 // elements moved at a time, where the alignment allows it
 
@@ -33,7 +33,7 @@ struct ClipPiece {
 }  // namespace
 
 struct pdb_clip_plan {
-    int device, blocks;
+    int device, blocks, step_blocks;    // of the two launches
     int64_t n_pieces;
     ClipPiece *pieces;                  // device
     double *partial;                    // device: the blocks' sums
@@ -43,9 +43,9 @@ struct pdb_clip_plan {
 
 namespace {
 
-// f(element pointer of the row, column) for all single elements, g(...) for packs: one thread's of a piece
+// pack(row, column) for a thread's packs of a piece, one(row, column) for its single elements
 template <typename F, typename G>
-__device__ __forceinline__ void each_of_piece(const ClipPiece &p, F one, G pack)
+__device__ __forceinline__ void each_of_piece(const ClipPiece &p, G pack, F one)
 {
     const int packs = (p.cols - p.head) / WIDE, singles = p.cols - packs * WIDE;
     if (p.rows == 1) {
@@ -63,43 +63,76 @@ __device__ __forceinline__ void each_of_piece(const ClipPiece &p, F one, G pack)
     }
 }
 
+// vec(16 bytes of a thread's part of a gradient's piece), one(its single elements): the same part whatever they do with it
+template <typename T, int U, typename F, typename G>
+__device__ __forceinline__ void vectors_of_piece(const ClipPiece &p, F vec, G one)
+{
+    constexpr int E = Vec<T>::E;
+    const T *g = (const T *)p.g;
+    const int packs = (p.cols - p.head) / WIDE, singles = p.cols - packs * WIDE, row = packs * (WIDE / E);
+    if (p.rows == 1) {
+        const uint4 *body = reinterpret_cast<const uint4 *>(g + p.head);
+        int i = threadIdx.x;
+        if (U > 1)
+            for (; i + (U - 1) * CLIP_THREADS < row; i += U * CLIP_THREADS) {
+                uint4 v[U];
+#pragma unroll
+                for (int u = 0; u < U; ++u) v[u] = ld_keep(body + i + u * CLIP_THREADS);
+#pragma unroll
+                for (int u = 0; u < U; ++u) vec(v[u]);
+            }
+        for (; i < row; i += CLIP_THREADS) vec(ld_keep(body + i));
+    } else {
+        for (int i = threadIdx.x; i < p.rows * row; i += CLIP_THREADS) {
+            const int r = i / row;
+            vec(ld_keep(reinterpret_cast<const uint4 *>(g + r * p.g_stride + p.head) + (i - r * row)));
+        }
+    }
+    for (int i = threadIdx.x; i < p.rows * singles; i += CLIP_THREADS) {
+        const int r = i / singles, x = i - r * singles;
+        one(to_float(g[r * p.g_stride + (x < p.head ? x : x + packs * WIDE)]));
+    }
+}
+
 // A thread's sum of squares of a piece.  In 32 bits while that loses nothing: a sum that left fp32's range, or is so small that
 // squares may have been lost below it, is formed again in 64.
 template <typename T>
 __device__ __forceinline__ double piece_squares(const ClipPiece &p)
 {
-    const T *g = (const T *)p.g;
-    float sum = 0.0f, any = 0.0f;
-    each_of_piece(
+    constexpr int E = Vec<T>::E;
+    uint64_t pairs[2] = {0, 0};
+    float more = 0.0f, lo, hi;
+    uint32_t any = 0;                                 // bits of the magnitudes
+    vectors_of_piece<T, 4>(
         p,
-        [&](int r, int c) {
-            const float x = to_float(g[r * p.g_stride + c]);
-            sum = __fmaf_rn(x, x, sum);
-            any = fmaxf(any, fabsf(x));
-        },
-        [&](int r, int c) {
-            const Pack<T, WIDE> v = load_pack<T, WIDE>(g + r * p.g_stride + c);
+        [&](const uint4 &v) {
+            float f[E];
+            Vec<T>::unpack(v, f);
 #pragma unroll
-            for (int e = 0; e < WIDE; ++e) {
-                const float x = to_float(v.e[e]);
-                sum = __fmaf_rn(x, x, sum);
-                any = fmaxf(any, fabsf(x));
+            for (int e = 0; e < E; e += 2) {
+                const uint64_t x = pair(f[e], f[e + 1]);
+                pairs[e >> 1 & 1] = fma2(x, x, pairs[e >> 1 & 1]);
             }
-        });
-    if ((sum >= 0x1p-90f && sum < INFINITY) || (sum == 0.0f && any == 0.0f)) return sum;
-    double wide = 0.0;
-    each_of_piece(
-        p,
-        [&](int r, int c) {
-            const double x = to_float(g[r * p.g_stride + c]);
-            wide = __fma_rn(x, x, wide);
+            any |= (v.x | v.y | v.z | v.w) & (sizeof(T) == 2 ? 0x7fff7fffu : 0x7fffffffu);
         },
-        [&](int r, int c) {
-            for (int e = 0; e < WIDE; ++e) {
-                const double x = to_float(g[r * p.g_stride + c + e]);
-                wide = __fma_rn(x, x, wide);
-            }
+        [&](float f) {
+            more = __fmaf_rn(f, f, more);
+            any |= __float_as_uint(f) & 0x7fffffffu;
         });
+    unpair(add2(pairs[0], pairs[1]), lo, hi);
+    const float sum = __fadd_rn(__fadd_rn(lo, hi), more);
+    if ((sum >= 0x1p-90f && sum < INFINITY) || any == 0) return sum;
+    double wide = 0.0;
+    const auto square = [&](float f) { wide = __fma_rn((double)f, (double)f, wide); };
+    vectors_of_piece<T, 1>(
+        p,
+        [&](const uint4 &v) {
+            float f[E];
+            Vec<T>::unpack(v, f);
+#pragma unroll
+            for (int e = 0; e < E; ++e) square(f[e]);
+        },
+        square);
     return wide;
 }
 
@@ -121,8 +154,11 @@ __global__ __launch_bounds__(CLIP_THREADS) void k_clip_norm(const ClipPiece *pie
     after_previous();
     __shared__ double part[CLIP_THREADS / 32];
     double sum = 0.0;
+    ClipPiece next;
+    if (blockIdx.x < n) next = pieces[blockIdx.x];
     for (int64_t i = blockIdx.x; i < n; i += gridDim.x) {
-        const ClipPiece p = pieces[i];
+        const ClipPiece p = next;
+        if (i + gridDim.x < n) next = pieces[i + gridDim.x];
         const double x = p.g_type == PDB_TYPE_FLOAT    ? piece_squares<float>(p)
                          : p.g_type == PDB_TYPE_BFLOAT ? piece_squares<__nv_bfloat16>(p)
                                                        : piece_squares<__half>(p);
@@ -139,22 +175,23 @@ __device__ __forceinline__ void piece_step(const ClipPiece &p, float factor)
     O *out = (O *)p.out;
     const auto step = [&](float x, float old) {
         const float v = __fmul_rn(factor, x);
-        return from_float<O>(ACC ? __fadd_rn(old, v) : v);
+        return ACC ? __fadd_rn(old, v) : v;
     };
     each_of_piece(
         p,
         [&](int r, int c) {
             O *at = out + r * p.out_stride + c;
-            *at = step(to_float(g[r * p.g_stride + c]), ACC ? to_float(*at) : 0.0f);
+            const Pack<T, WIDE> v = load_pack<T, WIDE>(g + r * p.g_stride + c);
+            float f[WIDE], old[WIDE];
+            if (ACC) to_floats(load_pack<O, WIDE>(at), old);
+            to_floats(v, f);
+#pragma unroll
+            for (int e = 0; e < WIDE; ++e) f[e] = step(f[e], ACC ? old[e] : 0.0f);
+            store_pack<O, WIDE>(at, of_floats<O>(f));
         },
         [&](int r, int c) {
             O *at = out + r * p.out_stride + c;
-            const Pack<T, WIDE> v = load_pack<T, WIDE>(g + r * p.g_stride + c);
-            Pack<O, WIDE> y;
-            if (ACC) y = load_pack<O, WIDE>(at);
-#pragma unroll
-            for (int e = 0; e < WIDE; ++e) y.e[e] = step(to_float(v.e[e]), ACC ? to_float(y.e[e]) : 0.0f);
-            store_pack<O, WIDE>(at, y);
+            *at = from_float<O>(step(to_float(g[r * p.g_stride + c]), ACC ? to_float(*at) : 0.0f));
         });
 }
 
@@ -180,8 +217,13 @@ __global__ __launch_bounds__(CLIP_THREADS) void k_clip_step(const ClipPiece *pie
     if (!(all < INFINITY)) return;                        // a gradient that is not finite: no step
     const bool clips = all > (double)max_norm;
     const float factor = clips ? (float)((double)scale * ((double)max_norm / all)) : scale;
-    for (int64_t i = blockIdx.x; i < n; i += gridDim.x) {
-        const ClipPiece p = pieces[i];
+    // the last pieces first: L2 still holds what the norm's launch read last
+    int64_t i = (n - 1 - blockIdx.x) / gridDim.x * gridDim.x + blockIdx.x;
+    ClipPiece next;
+    if (i >= 0 && i < n) next = pieces[i];
+    for (; i >= 0 && i < n; i -= gridDim.x) {
+        const ClipPiece p = next;
+        if (i >= gridDim.x) next = pieces[i - gridDim.x];
         if (!ACC && factor == 1.0f && p.out == p.g) continue;
         if (p.g_type == PDB_TYPE_FLOAT) piece_step_to<float, ACC>(p, factor);
         else if (p.g_type == PDB_TYPE_BFLOAT) piece_step_to<__nv_bfloat16, ACC>(p, factor);
@@ -280,7 +322,7 @@ int pdb_clip_plan_build(const pdb_mat *grads, const pdb_mat *outs, int64_t n, pd
     const Launch l = launch_info();
     try {
         if (const int rc = check_apart(grads, outs, n)) return rc;
-        const int64_t shares = (int64_t)l.sms * CLIP_BLOCKS_PER_SM * 2;
+        const int64_t shares = (int64_t)l.sms * NORM_BLOCKS_PER_SM * 2;
         const int64_t most = std::min<int64_t>(16384, std::max<int64_t>(2048, (total / shares + WIDE - 1) / WIDE * WIDE));
         for (int64_t i = 0; i < n; ++i) cut(grads + i, outs + i, most, pieces);
         p = new pdb_clip_plan();
@@ -290,7 +332,8 @@ int pdb_clip_plan_build(const pdb_mat *grads, const pdb_mat *outs, int64_t n, pd
     cudaStream_t s = (cudaStream_t)stream;
     p->device = l.device;
     p->n_pieces = (int64_t)pieces.size();
-    p->blocks = (int)std::max<int64_t>(1, std::min<int64_t>(p->n_pieces, (int64_t)l.sms * CLIP_BLOCKS_PER_SM));
+    p->blocks = (int)std::max<int64_t>(1, std::min<int64_t>(p->n_pieces, (int64_t)l.sms * NORM_BLOCKS_PER_SM));
+    p->step_blocks = (int)std::max<int64_t>(1, std::min<int64_t>(p->n_pieces, (int64_t)l.sms * STEP_BLOCKS_PER_SM));
     int rc = cudaEventCreateWithFlags(&p->ev_use, cudaEventDisableTiming) == cudaSuccess ? PDB_OK : PDB_ECUDA;
     rc = rc ? rc : alloc_block(p->arrays, {{(void **)&p->partial, sizeof(double) * p->blocks},
                                            {(void **)&p->pieces, sizeof(ClipPiece) * p->n_pieces}}, s);
@@ -320,7 +363,7 @@ int pdb_clip(const pdb_clip_plan *p, float max_norm, float scale, int accumulate
     HandleUse use{p->ev_use, s};
     int rc = launch(k_clip_norm, p->blocks, CLIP_THREADS, 0, 1, s, p->pieces, p->n_pieces, p->partial);
     if (rc == PDB_OK)
-        rc = launch(accumulate ? k_clip_step<true> : k_clip_step<false>, p->blocks, CLIP_THREADS, 0, 1, s, p->pieces,
+        rc = launch(accumulate ? k_clip_step<true> : k_clip_step<false>, p->step_blocks, CLIP_THREADS, 0, 1, s, p->pieces,
                     p->n_pieces, p->partial, p->blocks, max_norm, scale, norm);
     return rc;
 }

@@ -1,6 +1,8 @@
 // Rows of a matrix moved E elements at a time (embed.cu, route.cu, clip.cu).
 #pragma once
 
+#include <type_traits>
+
 #include "tokens.cuh"
 
 namespace pdb {
@@ -53,6 +55,49 @@ __device__ __forceinline__ void store_pack(T *p, const Pack<T, E> &v)
         using R = typename Raw<E * sizeof(T)>::type;
         *reinterpret_cast<R *>(p) = *reinterpret_cast<const R *>(&v);
     }
+}
+
+// the elements in fp32 and back, 16-bit ones by the pair
+template <typename T, int E>
+__device__ __forceinline__ void to_floats(const Pack<T, E> &v, float (&f)[E])
+{
+    if constexpr (sizeof(T) == 2 && E % 2 == 0) {
+        const uint32_t *w = reinterpret_cast<const uint32_t *>(&v);
+#pragma unroll
+        for (int i = 0; i < E / 2; ++i) {
+            if constexpr (std::is_same_v<T, __half>) {
+                const float2 x = __half22float2(*reinterpret_cast<const __half2 *>(w + i));
+                f[2 * i] = x.x, f[2 * i + 1] = x.y;
+            } else {
+                f[2 * i] = __uint_as_float(w[i] << 16), f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+            }
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < E; ++i) f[i] = to_float(v.e[i]);
+    }
+}
+template <typename T, int E>
+__device__ __forceinline__ Pack<T, E> of_floats(const float (&f)[E])
+{
+    Pack<T, E> v;
+    if constexpr (sizeof(T) == 2 && E % 2 == 0) {
+        uint32_t *w = reinterpret_cast<uint32_t *>(&v);
+#pragma unroll
+        for (int i = 0; i < E / 2; ++i) {
+            if constexpr (std::is_same_v<T, __half>) {
+                const __half2 x = __floats2half2_rn(f[2 * i], f[2 * i + 1]);
+                w[i] = *reinterpret_cast<const uint32_t *>(&x);
+            } else {
+                const __nv_bfloat162 x = __floats2bfloat162_rn(f[2 * i], f[2 * i + 1]);
+                w[i] = *reinterpret_cast<const uint32_t *>(&x);
+            }
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < E; ++i) v.e[i] = from_float<T>(f[i]);
+    }
+    return v;
 }
 
 // whether E elements of each row can be moved as one piece (up to 32 bytes: a lane's whole sector in one instruction)

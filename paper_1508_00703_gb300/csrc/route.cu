@@ -168,6 +168,12 @@ __global__ __launch_bounds__(ROUTE_THREADS) void k_route_place(Slots s, const ui
 
 inline size_t place_smem(int experts) { return (size_t)experts * (8 + 2 * ROUTE_WARPS); }
 
+// w / pieces
+__device__ __forceinline__ int64_t row_of(int64_t w, int pieces)
+{
+    return w <= UINT32_MAX ? (int64_t)((uint32_t)w / (uint32_t)pieces) : w / pieces;
+}
+
 // ------------------------------------------------------------------ rows there
 // zeros in the rows of `rows` (8 of them from r0 on) that no slot takes, by a warp
 constexpr int ZERO_ROWS = 8;
@@ -188,7 +194,8 @@ __device__ __forceinline__ void zero_unused(const int32_t *source, int64_t r0, i
 
 // A warp moves one piece of ROWS_UNROLL * 32 packs of a token's row, read once, to the rows of its slots; the warps behind
 // those write zeros where no slot is.  Bound by memory.
-constexpr int ROWS_UNROLL = 4;
+template <int E>
+constexpr int ROWS_UNROLL = E > 1 ? 4 : 16;
 
 template <typename T, typename O, int E>
 __global__ __launch_bounds__(256) void k_route_rows(const T *x, int64_t stride, int64_t n, int k, int dim, int pieces,
@@ -202,18 +209,20 @@ __global__ __launch_bounds__(256) void k_route_rows(const T *x, int64_t stride, 
         zero_unused<O, E>(source, (w - copies) * ZERO_ROWS, rows, dim, out, out_stride);
         return;
     }
-    const int64_t i = w / pieces;
-    const int piece = (int)(w - i * pieces), j0 = (piece * ROWS_UNROLL * 32 + lane) * E;
+    const int64_t i = row_of(w, pieces);
+    const int piece = (int)(w - i * pieces), j0 = (piece * ROWS_UNROLL<E> * 32 + lane) * E;
     const T *from = x + i * stride;
-    Pack<T, E> v[ROWS_UNROLL];
+    Pack<T, E> v[ROWS_UNROLL<E>];
 #pragma unroll
-    for (int u = 0; u < ROWS_UNROLL; ++u)
+    for (int u = 0; u < ROWS_UNROLL<E>; ++u)
         if (j0 + u * 32 * E < dim) v[u] = load_pack<T, E>(from + j0 + u * 32 * E);
-    Pack<O, E> y[ROWS_UNROLL];
+    Pack<O, E> y[ROWS_UNROLL<E>];
 #pragma unroll
-    for (int u = 0; u < ROWS_UNROLL; ++u)
-#pragma unroll
-        for (int e = 0; e < E; ++e) y[u].e[e] = from_float<O>(to_float(v[u].e[e]));
+    for (int u = 0; u < ROWS_UNROLL<E>; ++u) {
+        float f[E];
+        to_floats(v[u], f);
+        y[u] = of_floats<O>(f);
+    }
     for (int s0 = 0; s0 < k; s0 += 32) {
         const int32_t mine = s0 + lane < k ? place[i * k + s0 + lane] : -1;
         if (mine >= rows) set_status(status, PDB_ERANGE);
@@ -221,174 +230,218 @@ __global__ __launch_bounds__(256) void k_route_rows(const T *x, int64_t stride, 
         for (; there; there &= there - 1) {
             O *to = out + (int64_t)__shfl_sync(FULL, mine, __ffs(there) - 1) * out_stride;
 #pragma unroll
-            for (int u = 0; u < ROWS_UNROLL; ++u)
+            for (int u = 0; u < ROWS_UNROLL<E>; ++u)
                 if (j0 + u * 32 * E < dim) store_pack<O, E>(to + j0 + u * 32 * E, y[u]);
         }
     }
 }
 
 // ------------------------------------------------------------------ and back
+// a lane's slot: its row (-1: none), its weight
+struct Slot {
+    int32_t at;
+    float weight;
+};
+__device__ __forceinline__ Slot load_slot(const int32_t *place, const float *weight, int64_t i, int k, int j, bool on)
+{
+    Slot s = {-1, 1.0f};
+    if (on && j < k) {
+        s.at = place[i * k + j];
+        if (weight) s.weight = weight[i * k + j];
+    }
+    return s;
+}
+// the lanes' slots that have a row
+__device__ __forceinline__ unsigned slots_there(const Slot &s, int64_t rows, int *status)
+{
+    if (s.at >= rows) set_status(status, PDB_ERANGE);
+    return __ballot_sync(FULL, s.at >= 0 && s.at < rows);
+}
+
 // A warp sums one piece of JOIN_UNROLL * 32 packs of a token's row over its slots in ascending order, JOIN_SLOTS rows under way
-// at once.  Bound by memory.
-constexpr int JOIN_UNROLL = 2, JOIN_SLOTS = 4;
+// at once, and takes the next piece; that one's first 32 places are on their way meanwhile.  Bound by memory.
+template <int E>
+constexpr int JOIN_UNROLL = E > 2 ? 2 : 4;
+constexpr int JOIN_SLOTS = 4, JOIN_BLOCKS = 3;
 
 template <typename T, typename O, int E>
-__global__ __launch_bounds__(256) void k_route_join(const T *in, int64_t stride, int64_t rows, int k, const int32_t *place,
-                                                    const float *weight, int64_t n, int dim, int pieces, O *__restrict__ out,
-                                                    int64_t out_stride, int *status)
+__global__ __launch_bounds__(256, JOIN_BLOCKS) void k_route_join(const T *in, int64_t stride, int64_t rows, int k,
+                                                                 const int32_t *place, const float *weight, int64_t n, int dim,
+                                                                 int pieces, O *__restrict__ out, int64_t out_stride, int *status)
 {
     after_previous();
+    constexpr int U = JOIN_UNROLL<E>;
     const int lane = threadIdx.x & 31;
-    const int64_t w = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5), i = w / pieces;
-    if (i >= n) return;
-    const int piece = (int)(w - i * pieces), j0 = (piece * JOIN_UNROLL * 32 + lane) * E;
-    float sum[JOIN_UNROLL][E];
+    const int64_t items = n * pieces, step = (int64_t)gridDim.x * 8;
+    int64_t w = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5), i = row_of(w, pieces);
+    Slot ahead = load_slot(place, weight, i, k, lane, w < items);
+    for (; w < items; w += step) {
+        const int64_t token = i;
+        const int j0 = ((int)(w - i * pieces) * U * 32 + lane) * E;
+        Slot slot = ahead;
+        i = row_of(w + step, pieces);
+        ahead = load_slot(place, weight, i, k, lane, w + step < items);
+        float sum[U][E];
 #pragma unroll
-    for (int u = 0; u < JOIN_UNROLL; ++u)
+        for (int u = 0; u < U; ++u)
 #pragma unroll
-        for (int e = 0; e < E; ++e) sum[u][e] = 0.0f;
-    for (int s0 = 0; s0 < k; s0 += 32) {
-        const int32_t mine = s0 + lane < k ? place[i * k + s0 + lane] : -1;
-        const float wt = weight && s0 + lane < k ? weight[i * k + s0 + lane] : 1.0f;
-        if (mine >= rows) set_status(status, PDB_ERANGE);
-        unsigned there = __ballot_sync(FULL, mine >= 0 && mine < rows);
-        while (there) {
-            Pack<T, E> v[JOIN_SLOTS][JOIN_UNROLL];
-            float ws[JOIN_SLOTS];
-            const int batch = min(JOIN_SLOTS, __popc(there));
+            for (int e = 0; e < E; ++e) sum[u][e] = 0.0f;
+        for (int s0 = 0; s0 < k; s0 += 32) {
+            if (s0) slot = load_slot(place, weight, token, k, s0 + lane, true);
+            unsigned there = slots_there(slot, rows, status);
+            while (there) {
+                Pack<T, E> v[JOIN_SLOTS][U];
+                float ws[JOIN_SLOTS];
+                const int batch = min(JOIN_SLOTS, __popc(there));
 #pragma unroll
-            for (int s = 0; s < JOIN_SLOTS; ++s) {
-                const int at = there ? __ffs(there) - 1 : 0;
-                ws[s] = __shfl_sync(FULL, wt, at);
-                const T *from = in + (int64_t)__shfl_sync(FULL, mine, at) * stride;
-                if (s < batch)
+                for (int s = 0; s < JOIN_SLOTS; ++s) {
+                    const int at = there ? __ffs(there) - 1 : 0;
+                    ws[s] = __shfl_sync(FULL, slot.weight, at);
+                    const T *from = in + (int64_t)__shfl_sync(FULL, slot.at, at) * stride;
+                    if (s < batch)
 #pragma unroll
-                    for (int u = 0; u < JOIN_UNROLL; ++u)
-                        if (j0 + u * 32 * E < dim) v[s][u] = load_pack<T, E>(from + j0 + u * 32 * E);
-                there &= there - 1;
+                        for (int u = 0; u < U; ++u)
+                            if (j0 + u * 32 * E < dim) v[s][u] = load_pack<T, E>(from + j0 + u * 32 * E);
+                    there &= there - 1;
+                }
+#pragma unroll
+                for (int s = 0; s < JOIN_SLOTS; ++s)
+                    if (s < batch)
+#pragma unroll
+                        for (int u = 0; u < U; ++u) {
+                            float f[E];
+                            to_floats(v[s][u], f);
+#pragma unroll
+                            for (int e = 0; e < E; ++e) sum[u][e] = __fmaf_rn(ws[s], f[e], sum[u][e]);
+                        }
             }
-#pragma unroll
-            for (int s = 0; s < JOIN_SLOTS; ++s)
-                if (s < batch)
-#pragma unroll
-                    for (int u = 0; u < JOIN_UNROLL; ++u)
-#pragma unroll
-                        for (int e = 0; e < E; ++e) sum[u][e] = __fmaf_rn(ws[s], to_float(v[s][u].e[e]), sum[u][e]);
         }
-    }
 #pragma unroll
-    for (int u = 0; u < JOIN_UNROLL; ++u) {
-        const int j = j0 + u * 32 * E;
-        if (j >= dim) break;
-        Pack<O, E> y;
-#pragma unroll
-        for (int e = 0; e < E; ++e) y.e[e] = from_float<O>(sum[u][e]);
-        store_pack<O, E>(out + i * out_stride + j, y);
+        for (int u = 0; u < U; ++u) {
+            const int j = j0 + u * 32 * E;
+            if (j >= dim) break;
+            store_pack<O, E>(out + token * out_stride + j, of_floats<O>(sum[u]));
+        }
     }
 }
 
-// Gradients of the join: drows[p_j] = w_j dy, dw_j = <dy, rows[p_j]>.  `team` warps of a block (a power of two) have a token:
-// each holds its packs of dy and goes over the slots; the dot products are summed over its lanes, then over the
-// team's warps in order.  Bound by memory.  The warps of the blocks behind write zeros in rows that no slot takes.
-constexpr int GRAD_WARPS = 8, GRAD_UNROLL = 2, GRAD_SLOTS = 2;
+// Gradients of the join: drows[p_j] = w_j dy, dw_j = <dy, rows[p_j]>.  `team` warps of a block (a power of two) have a token, whose columns
+// they take in turn: each holds its packs of dy and goes over the slots, GRAD_SLOTS rows under way at once; the dot products are summed over
+// the lanes, then over the team's warps in order.  The next token's places, weights and first packs of dy are on their way meanwhile.
+// At the end the warps write zeros in rows that no slot takes.  Bound by memory.
+constexpr int GRAD_UNROLL = 4, GRAD_WARPS = 8, GRAD_SLOTS = 4, GRAD_BLOCKS = 2;
 
 template <typename T, typename D, int E>
-__global__ __launch_bounds__(GRAD_WARPS * 32) void k_route_join_grad(const T *in, int64_t stride, int64_t rows, int k,
-                                                                     const int32_t *place, const int32_t *source,
-                                                                     const float *weight, const D *dy, int64_t dy_stride,
-                                                                     int64_t n, int dim, int team, int64_t token_blocks,
-                                                                     T *drows, int64_t out_stride, float *__restrict__ dweight,
-                                                                     int *status)
+__global__ __launch_bounds__(GRAD_WARPS * 32, GRAD_BLOCKS) void k_route_join_grad(const T *in, int64_t stride, int64_t rows, int k,
+                                                                                  const int32_t *place, const int32_t *source,
+                                                                                  const float *weight, const D *dy, int64_t dy_stride,
+                                                                                  int64_t n, int dim, int team, T *drows,
+                                                                                  int64_t out_stride, float *__restrict__ dweight,
+                                                                                  int *status)
 {
     after_previous();
-    __shared__ float s_dot[GRAD_WARPS][MAX_ROUTE_SLOTS];
+    constexpr int U = GRAD_UNROLL, SPAN = U * 32 * E;
+    __shared__ float s_dot[2][GRAD_WARPS][MAX_ROUTE_SLOTS];     // of two tokens in turn
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    if (blockIdx.x >= token_blocks) {
-        const int64_t r0 = ((blockIdx.x - token_blocks) * GRAD_WARPS + warp) * ZERO_ROWS;
-        zero_unused<T, E>(source, r0, rows, dim, drows, out_stride);
-        return;
-    }
-    const int64_t first = (int64_t)blockIdx.x * (GRAD_WARPS / team), i = first + warp / team;
-    const int part = warp & (team - 1);
-    for (int j = lane; j < k; j += 32) s_dot[warp][j] = 0.0f;
-    __syncwarp();
-    if (i < n) {
-        // the slots' rows and weights, two for a lane
-        int32_t at[2];
-        float wt[2];
-        uint64_t there = 0;
+    const int per = GRAD_WARPS / team, part = warp & (team - 1);
+    const int64_t step = (int64_t)gridDim.x * per;
+    int64_t first = (int64_t)blockIdx.x * per;
+    const auto load_dy = [&](int64_t i, int c0, Pack<D, E> (&d)[U]) {
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const int j = h * 32 + lane;
-            at[h] = j < k ? place[i * k + j] : -1;
-            wt[h] = weight && j < k ? weight[i * k + j] : 1.0f;
-            if (at[h] >= rows) set_status(status, PDB_ERANGE);
-            there |= (uint64_t)__ballot_sync(FULL, at[h] >= 0 && at[h] < rows) << (h * 32);
-        }
-        for (int c0 = part * (GRAD_UNROLL * 32 * E); c0 < dim; c0 += team * (GRAD_UNROLL * 32 * E)) {
-            const int j0 = c0 + lane * E;
-            float d[GRAD_UNROLL][E];
+        for (int u = 0; u < U; ++u)
+            if (i < n && c0 + u * 32 * E + lane * E < dim) d[u] = load_pack<D, E>(dy + i * dy_stride + c0 + u * 32 * E + lane * E);
+    };
+    Slot ahead = load_slot(place, weight, first + warp / team, k, lane, first + warp / team < n);
+    Pack<D, E> d_ahead[U];
+    load_dy(first + warp / team, part * SPAN, d_ahead);
+    for (int turn = 0; first < n; first += step, turn ^= 1) {
+        const int64_t i = first + warp / team;
+        const Slot slot0 = ahead;
+        Pack<D, E> d[U];
 #pragma unroll
-            for (int u = 0; u < GRAD_UNROLL; ++u) {
-                Pack<D, E> v;
-                if (j0 + u * 32 * E < dim) v = load_pack<D, E>(dy + i * dy_stride + j0 + u * 32 * E);
+        for (int u = 0; u < U; ++u) d[u] = d_ahead[u];
+        ahead = load_slot(place, weight, i + step, k, lane, i + step < n);
+        load_dy(i + step, part * SPAN, d_ahead);
+        float *dots = s_dot[turn][warp];
+        if (dweight)
+            for (int j = lane; j < k; j += 32) dots[j] = 0.0f;
+        __syncwarp();
+        if (i < n)
+            for (int c0 = part * SPAN; c0 < dim; c0 += team * SPAN) {
+                const int j0 = c0 + lane * E;
+                if (c0 != part * SPAN) load_dy(i, c0, d);
+                for (int s0 = 0; s0 < k; s0 += 32) {
+                    const Slot slot = s0 ? load_slot(place, weight, i, k, s0 + lane, true) : slot0;
+                    unsigned left = slots_there(slot, rows, status);
+                    while (left) {
+                        Pack<T, E> v[GRAD_SLOTS][U];
+                        int which[GRAD_SLOTS];
+                        int64_t row[GRAD_SLOTS];
+                        const int batch = min(GRAD_SLOTS, __popc(left));
 #pragma unroll
-                for (int e = 0; e < E; ++e) d[u][e] = j0 + u * 32 * E < dim ? to_float(v.e[e]) : 0.0f;
-            }
-            for (uint64_t left = there; left;) {
-                Pack<T, E> v[GRAD_SLOTS][GRAD_UNROLL];
-                int slot[GRAD_SLOTS];
-                int64_t row[GRAD_SLOTS];
-                const int batch = min(GRAD_SLOTS, __popcll(left));
+                        for (int s = 0; s < GRAD_SLOTS; ++s) {
+                            which[s] = left ? __ffs(left) - 1 : 0;
+                            left &= left - 1;
+                            row[s] = __shfl_sync(FULL, slot.at, which[s]);
+                            if (dweight && s < batch)
 #pragma unroll
-                for (int s = 0; s < GRAD_SLOTS; ++s) {
-                    slot[s] = left ? __ffsll((long long)left) - 1 : 0;
-                    left &= left - 1;
-                    const int32_t a = __shfl_sync(FULL, at[0], slot[s] & 31), b = __shfl_sync(FULL, at[1], slot[s] & 31);
-                    row[s] = slot[s] < 32 ? a : b;
-                    if (dweight && s < batch)
-#pragma unroll
-                        for (int u = 0; u < GRAD_UNROLL; ++u)
-                            if (j0 + u * 32 * E < dim) v[s][u] = load_pack<T, E>(in + row[s] * stride + j0 + u * 32 * E);
-                }
-                // drows may be the rows' own memory: what is loaded is loaded before anything is stored there
-                asm volatile("" ::: "memory");
-#pragma unroll
-                for (int s = 0; s < GRAD_SLOTS; ++s) {
-                    if (s >= batch) break;
-                    const float wa = __shfl_sync(FULL, wt[0], slot[s] & 31), wb = __shfl_sync(FULL, wt[1], slot[s] & 31);
-                    const float ws = slot[s] < 32 ? wa : wb;
-                    float dot = 0.0f;
-#pragma unroll
-                    for (int u = 0; u < GRAD_UNROLL; ++u) {
-                        const int j = j0 + u * 32 * E;
-                        if (j >= dim) break;
-                        Pack<T, E> y;
-#pragma unroll
-                        for (int e = 0; e < E; ++e) {
-                            if (dweight) dot = __fmaf_rn(d[u][e], to_float(v[s][u].e[e]), dot);
-                            y.e[e] = from_float<T>(__fmul_rn(ws, d[u][e]));
+                                for (int u = 0; u < U; ++u)
+                                    if (j0 + u * 32 * E < dim) v[s][u] = load_pack<T, E>(in + row[s] * stride + j0 + u * 32 * E);
                         }
-                        store_pack<T, E>(drows + row[s] * out_stride + j, y);
-                    }
-                    if (dweight) {
+                        // drows may be the rows' own memory: what is loaded is loaded before anything is stored there
+                        asm volatile("" ::: "memory");
+                        float dot[GRAD_SLOTS];
 #pragma unroll
-                        for (int off = 16; off >= 1; off >>= 1) dot = __fadd_rn(dot, __shfl_xor_sync(FULL, dot, off));
-                        if (lane == 0) s_dot[warp][slot[s]] = __fadd_rn(s_dot[warp][slot[s]], dot);
+                        for (int s = 0; s < GRAD_SLOTS; ++s) {
+                            dot[s] = 0.0f;
+                            const float ws = __shfl_sync(FULL, slot.weight, which[s]);
+                            if (s >= batch) continue;
+#pragma unroll
+                            for (int u = 0; u < U; ++u) {
+                                const int j = j0 + u * 32 * E;
+                                if (j >= dim) break;
+                                float g[E], f[E];
+                                to_floats(d[u], g);
+                                if (dweight) {
+                                    to_floats(v[s][u], f);
+#pragma unroll
+                                    for (int e = 0; e < E; ++e) dot[s] = __fmaf_rn(g[e], f[e], dot[s]);
+                                }
+#pragma unroll
+                                for (int e = 0; e < E; ++e) g[e] = __fmul_rn(ws, g[e]);
+                                store_pack<T, E>(drows + row[s] * out_stride + j, of_floats<T>(g));
+                            }
+                        }
+                        if (dweight) {
+                            // lanes of one half keep half of the slots' sums, then a quarter: lane 8 s has slot s
+                            static_assert(GRAD_SLOTS == 4, "two halvings");
+                            const bool high = lane & 16, odd = lane & 8;
+                            float a = high ? dot[2] : dot[0], b = high ? dot[3] : dot[1];
+                            a = __fadd_rn(a, __shfl_xor_sync(FULL, high ? dot[0] : dot[2], 16));
+                            b = __fadd_rn(b, __shfl_xor_sync(FULL, high ? dot[1] : dot[3], 16));
+                            float x = __fadd_rn(odd ? b : a, __shfl_xor_sync(FULL, odd ? a : b, 8));
+#pragma unroll
+                            for (int off = 4; off >= 1; off >>= 1) x = __fadd_rn(x, __shfl_xor_sync(FULL, x, off));
+                            const int s = lane >> 3, at = s0 + (s == 0 ? which[0] : s == 1 ? which[1] : s == 2 ? which[2] : which[3]);
+                            if ((lane & 7) == 0 && s < batch) dots[at] = __fadd_rn(dots[at], x);
+                            __syncwarp();
+                        }
                     }
                 }
             }
+        if (!dweight) continue;
+        __syncthreads();                 // (the next token's sums go to the other half)
+        for (int x = threadIdx.x; x < per * k; x += GRAD_WARPS * 32) {
+            const int who = x / k, j = x - who * k;
+            if (first + who >= n) break;
+            float sum = s_dot[turn][who * team][j];
+            for (int p = 1; p < team; ++p) sum = __fadd_rn(sum, s_dot[turn][who * team + p][j]);
+            dweight[(first + who) * k + j] = sum;
         }
     }
-    if (!dweight) return;
-    __syncthreads();
-    for (int x = threadIdx.x; x < GRAD_WARPS / team * k; x += GRAD_WARPS * 32) {
-        const int who = x / k, j = x - who * k;
-        if (first + who >= n) break;
-        float sum = s_dot[who * team][j];
-        for (int p = 1; p < team; ++p) sum = __fadd_rn(sum, s_dot[who * team + p][j]);
-        dweight[(first + who) * k + j] = sum;
-    }
+    if (dim > 0)
+        for (int64_t r0 = ((int64_t)blockIdx.x * GRAD_WARPS + warp) * ZERO_ROWS; r0 < rows; r0 += (int64_t)gridDim.x * GRAD_WARPS * ZERO_ROWS)
+            zero_unused<T, E>(source, r0, rows, dim, drows, out_stride);
 }
 
 // n tokens of k slots each and their places, or PDB_EINVAL
@@ -461,7 +514,7 @@ int pdb_route_rows(pdb_tokens *t, const pdb_mat *x, const int32_t *place, int64_
         using T = std::remove_pointer_t<decltype(a)>;
         using O = std::remove_pointer_t<decltype(b)>;
         constexpr int E = decltype(e)::value;
-        const int pieces = (dim + ROWS_UNROLL * 32 * E - 1) / (ROWS_UNROLL * 32 * E);
+        const int pieces = (dim + ROWS_UNROLL<E> * 32 * E - 1) / (ROWS_UNROLL<E> * 32 * E);
         const int64_t blocks = (x->rows * pieces + zero_warps(rows->rows, dim) + 7) / 8;
         if (blocks > INT32_MAX) return (int)PDB_ETOOBIG;
         return launch(k_route_rows<T, O, E>, blocks, 256, 0, 1, s, (const T *)x->data, stride_of(x), x->rows, (int)k, dim, pieces,
@@ -497,9 +550,8 @@ int pdb_route_join(pdb_tokens *t, const pdb_mat *rows, const int32_t *place, int
         using T = std::remove_pointer_t<decltype(a)>;
         using O = std::remove_pointer_t<decltype(b)>;
         constexpr int E = decltype(e)::value;
-        const int pieces = (dim + JOIN_UNROLL * 32 * E - 1) / (JOIN_UNROLL * 32 * E);
-        const int64_t blocks = (y->rows * pieces + 7) / 8;
-        if (blocks > INT32_MAX) return (int)PDB_ETOOBIG;
+        const int pieces = (dim + JOIN_UNROLL<E> * 32 * E - 1) / (JOIN_UNROLL<E> * 32 * E);
+        const int64_t blocks = std::min<int64_t>((y->rows * pieces + 7) / 8, (int64_t)t->sms * JOIN_BLOCKS);
         return launch(k_route_join<T, O, E>, blocks, 256, 0, 1, s, (const T *)rows->data, stride_of(rows), rows->rows, (int)k,
                       place, weight, y->rows, dim, pieces, (O *)y->data, stride_of(y), t->status);
     };
@@ -542,11 +594,11 @@ int pdb_route_join_grad(pdb_tokens *t, const pdb_mat *rows, const int32_t *place
         int team = 1;
         while (team < GRAD_WARPS && team * GRAD_UNROLL * 32 * E < dim) team *= 2;
         const int64_t token_blocks = (dy->rows + GRAD_WARPS / team - 1) / (GRAD_WARPS / team);
-        const int64_t blocks = token_blocks + (zero_warps(drows->rows, dim) + GRAD_WARPS - 1) / GRAD_WARPS;
-        if (blocks > INT32_MAX) return (int)PDB_ETOOBIG;
+        const int64_t zero_blocks = (zero_warps(drows->rows, dim) + GRAD_WARPS - 1) / GRAD_WARPS;
+        const int64_t blocks = std::min<int64_t>(std::max(token_blocks, zero_blocks), (int64_t)t->sms * GRAD_BLOCKS);
         return launch(k_route_join_grad<T, D, E>, blocks, GRAD_WARPS * 32, 0, 1, s, rows ? (const T *)rows->data : (const T *)nullptr,
                       rows ? stride_of(rows) : 0, drows->rows, (int)k, place, source, weight, (const D *)dy->data, stride_of(dy),
-                      dy->rows, dim, team, token_blocks, (T *)drows->data, stride_of(drows), dweight, t->status);
+                      dy->rows, dim, team, (T *)drows->data, stride_of(drows), dweight, t->status);
     };
     return with_type(drows->type, [&](auto *a) {
         return with_type(dy->type, [&](auto *b) {
