@@ -4,7 +4,7 @@ import math
 
 import pytest
 
-from _tokens import SLACK, TYPES, U, assert_near, rounding
+from tests._tokens import SLACK, TYPES, U, assert_near, rounding
 
 torch = pytest.importorskip("torch")
 pdb = pytest.importorskip("paper_1508_00703_gb300")

@@ -5,7 +5,7 @@ import math
 
 import pytest
 
-from _tokens import TYPES, U, Rows, assert_near
+from tests._tokens import TYPES, U, Rows, assert_near
 
 torch = pytest.importorskip("torch")
 pdb = pytest.importorskip("paper_1508_00703_gb300")
