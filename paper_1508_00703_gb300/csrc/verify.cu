@@ -35,18 +35,19 @@ constexpr double exp_series(double x)
     for (int i = 1; i < 30; ++i) term = term * x / i, sum += term;
     return sum;
 }
+template <int STEPS>
 struct Exp2Table {
-    float hi[256], lo[256];
+    float hi[STEPS], lo[STEPS];         // 2^(i/STEPS)
     constexpr Exp2Table() : hi(), lo()
     {
-        for (int i = 0; i < 256; ++i) {
-            const double v = exp_series(LN2_D * i / 256);
+        for (int i = 0; i < STEPS; ++i) {
+            const double v = exp_series(LN2_D * i / STEPS);
             hi[i] = (float)v;
             lo[i] = (float)(v - (double)(float)v);
         }
     }
 };
-__device__ const Exp2Table EXP2_TABLE;
+__device__ const Exp2Table<256> EXP2_TABLE;
 
 // ln 2 / 256 in four parts, the first three of 9 bits, so that their products with n of up to 15 bits are exact
 constexpr double LN2_STEP = LN2_D / 256;
@@ -113,94 +114,74 @@ struct Units {
     }
     __device__ __forceinline__ int64_t whole() const { return ((int64_t)high << 23) + low; }
 };
-// (high * 2^23 + low) * unit
-__device__ __forceinline__ Two two_of(int64_t high, int64_t low, float unit)
+// (high * 2^23 + low) * 2^-46
+__device__ __forceinline__ Two two_of(int64_t high, int64_t low)
 {
     high += low >> 23, low &= 0x7fffff;
     const float h = __ll2float_rn(high);
     const int64_t rest = high - __float2ll_rn(h);
-    return {__fmul_rn(h, __fmul_rn(unit, 0x1p23f)), __fmul_rn(__ll2float_rn(rest * 0x800000 + low), unit)};
+    return {__fmul_rn(h, 0x1p-23f), __fmul_rn(__ll2float_rn(rest * 0x800000 + low), 0x1p-46f)};
 }
 
-// exp(scale (z - m)) of a row's tokens, z <= m
-template <bool EXACT>
-struct Term;
-template <>
-struct Term<true> {
-    float m, scale;
-    const float2 *table;
-    __device__ __forceinline__ Term(float m_, float scale_, const float2 *table_) : m(m_), scale(scale_), table(table_) {}
-    __device__ __forceinline__ Two operator()(float z) const { return exp_two(z, m, scale, table); }
-};
-
-// The same good to 2^-29.7, at half the price, where |m scale| log2(e) < 2^9: n + f = 512 (z c - m c), c = scale log2(e), n whole and |f| <= 1,
-// f formed by roundings of 2^-25; then 2^(i/512) 2^(f/512) as a whole number of 2^-30, and 2^-k, n = 512 (-k) + i.  An error that
-// all tokens of a row share falls out of its probabilities.
+// exp(scale (z - m)) 2^-above of two tokens at once, z <= m, where |m scale| log2(e) < 2^9, to 2^-31.5: n + f = 512 (z c - m c),
+// c = scale log2(e), n whole and |f| <= 1, f formed by roundings of 2^-25; with n = 512 (-k) + i, 2^(i/512) + 2^(i/512) (2^(f/512) - 1) times a
+// power of two.  An error that all tokens of a row share falls out of its probabilities.  What the sums are made of are whole numbers of 2^-23 and of
+// 2^-45, both in the lowest bits of a float: additions and multiplications by the pair do nearly all of it (whole numbers
+// shifted into place took 2.5 times as long: half of the integer unit's instructions).
 constexpr float REACH = 512.0f;
 constexpr int STEPS = 512, LOG_STEPS = 9;
+__device__ const Exp2Table<STEPS> FAST_TABLE;
+constexpr int HIGH0 = 0x4b000000, LOW0 = 0x4b400000;       // the bits of 2^23 and 1.5 * 2^23
 
-struct FastTable {
-    float value[STEPS];                 // 2^(i/512)
-    int digits[STEPS];                  // the same in units of 2^-30
-    constexpr FastTable() : value(), digits()
-    {
-        for (int i = 0; i < STEPS; ++i) {
-            const double v = exp_series(LN2_D * i / STEPS);
-            value[i] = (float)v;
-            digits[i] = (int)(v * 0x1p30 + 0.5);
-        }
-    }
-};
-__device__ const FastTable FAST_TABLE;
+__device__ __forceinline__ uint64_t both(float x) { return pair(x, x); }
 
-struct Digits {
-    uint32_t digits[2];                 // 2^30 to 2^31, of two tokens
-    int shift[2];                       // exp = digits * 2^-30 / 2^(shift - shift0)
-};
-// by any amount: nothing is left from 64 on
-__device__ __forceinline__ uint64_t shifted(uint64_t x, int by)
-{
-    asm("shr.u64 %0, %0, %1;" : "+l"(x) : "r"(by));
-    return x;
-}
-template <>
-struct Term<false> {
+struct FastTerm {
     uint64_t ch, cl, from, rest;        // two of each
     float low;
-    int shift0;                         // added to the shifts
-    const float2 *table;                // 2^(i/512), and the same in units of 2^-30
-    Term() = default;
-    __device__ __forceinline__ Term(float m, float scale, const float2 *table_, int shift0_) : shift0(shift0_ + (0x4b400000 >> LOG_STEPS)), table(table_)
+    uint32_t bias;                      // of the power of two's bits
+    __device__ __forceinline__ FastTerm(float m, float scale, int above)
     {
         constexpr float log2e_rest = (float)(1.4426950408889634073599 - (double)LOG2E);
         const float c = __fmul_rn(scale, LOG2E), c_rest = __fmaf_rn(scale, log2e_rest, __fmaf_rn(scale, LOG2E, -c));
         const float c1 = __fmul_rn(c, (float)STEPS), c2 = __fmul_rn(c_rest, (float)STEPS);
-        const float mc = __fmul_rn(m, c1), whole = rintf(mc), fr = __fsub_rn(12582912.0f, whole);
-        const float r = __fadd_rn(__fsub_rn(mc, whole), __fmaf_rn(m, c2, __fmaf_rn(m, c1, -mc)));
-        ch = pair(c1, c1), cl = pair(c2, c2), from = pair(fr, fr), rest = pair(-r, -r);
+        const float mc = __fmul_rn(m, c1), whole = rintf(mc);
+        ch = both(c1), cl = both(c2), from = both(__fsub_rn(12582912.0f, whole));
+        rest = both(-__fadd_rn(__fsub_rn(mc, whole), __fmaf_rn(m, c2, __fmaf_rn(m, c1, -mc))));
         low = __fsub_rn(m, __fdiv_rn(60.0f, c));             // nothing below 2^-60
+        bias = ((uint32_t)(127 + 23 - above) << 23) - ((uint32_t)(LOW0 >> LOG_STEPS) << 23);
     }
-    __device__ __forceinline__ Digits operator()(float z0, float z1) const
+    // value: the terms times 2^23; high - HIGH0 units of 2^-23 and lowest - LOW0 of 2^-45 (what is left is 0.625 of 2^-23 at most)
+    __device__ __forceinline__ void operator()(float z0, float z1, const float2 *table, float (&value)[2], int (&high)[2],
+                                               int (&lowest)[2]) const
     {
         constexpr double L = LN2_D / STEPS;
-        constexpr float K1 = (float)L, K2 = (float)(L * L / 2), K3 = (float)(L * L * L / 6);
         const uint64_t z = pair(fmaxf(z0, low), fmaxf(z1, low));
         const uint64_t t = fma2(z, ch, from);                // n in its lowest bits
-        const uint64_t f = add2(fma2(z, ch, fma2(t, pair(-1.0f, -1.0f), from)), fma2(z, cl, rest));
-        const uint64_t s = mul2(f, fma2(f, fma2(f, pair(K3, K3), pair(K2, K2)), pair(K1, K1)));
+        const uint64_t f = add2(fma2(z, ch, fma2(t, both(-1.0f), from)), fma2(z, cl, rest));
+        const uint64_t s = mul2(f, fma2(f, fma2(f, both((float)(L * L * L / 6)), both((float)(L * L / 2))), both((float)L)));
         float t0, t1, x0, x1;
         unpair(t, t0, t1);
-        const int n0 = __float_as_int(t0), n1 = __float_as_int(t1);
+        const uint32_t n0 = __float_as_uint(t0), n1 = __float_as_uint(t1);
         const float2 a = table[n0 & (STEPS - 1)], b = table[n1 & (STEPS - 1)];
-        unpair(fma2(mul2(pair(a.x, b.x), s), pair(0x1p30f, 0x1p30f), pair(12582912.0f, 12582912.0f)), x0, x1);
-        return {{(uint32_t)(__float_as_int(a.y) + __float_as_int(x0) - 0x4b400000), (uint32_t)(__float_as_int(b.y) + __float_as_int(x1) - 0x4b400000)},
-                {shift0 - (n0 >> LOG_STEPS), shift0 - (n1 >> LOG_STEPS)}};
+        const uint64_t power = pair(__uint_as_float(((n0 >> LOG_STEPS) << 23) + bias), __uint_as_float(((n1 >> LOG_STEPS) << 23) + bias));
+        const uint64_t main = mul2(pair(a.x, b.x), power), more = mul2(fma2(pair(a.x, b.x), s, pair(a.y, b.y)), power);
+        const uint64_t sum = add2(main, more);
+        unpair(sum, value[0], value[1]);
+        const uint64_t h = add2(sum, both(8388608.0f));
+        unpair(h, x0, x1);
+        high[0] = __float_as_int(x0), high[1] = __float_as_int(x1);
+        // what is left of main + more, without rounding
+        const uint64_t left = add2(fma2(add2(h, both(-8388608.0f)), both(-1.0f), main), more);
+        unpair(fma2(left, both(4194304.0f), both(12582912.0f)), x0, x1);
+        lowest[0] = __float_as_int(x0), lowest[1] = __float_as_int(x1);
     }
 };
+__device__ __forceinline__ int64_t units(int high, int low) { return (int64_t)high * 0x400000 + low; }
 
-// How far from its token's borders a draw by Term<false> must lie to be taken, for weights that add up to 2^53: the running sum and v
-// times the whole one are moved by the terms of both rows and by their sums, 4 * 2^-29.7 together; what shifts cut off is below 2^-31.
-constexpr int64_t MARGIN = (int64_t)1 << 26;
+// How far from its token's borders a draw by FastTerm must lie to be taken, in units of 2^-45 of rows whose terms add up to 1/2 to 1: the terms
+// of both rows, and their sums, move the running sum and v times the whole one by 4 * 2^-31.5 together, their rounding to units by two
+// for each token.
+__device__ __forceinline__ int64_t fast_margin(int cols) { return (1 << 16) + 2 * (int64_t)cols; }
 
 // ------------------------------------------------------------------ shared by the blocks of a sequence
 struct Shared {
@@ -213,14 +194,17 @@ struct Shared {
     int64_t warp_sum[2][16];
     int64_t sum[2][2];                  // this block's sums of the two rows, in units of 2^-23 and 2^-46
     Two row_sum[2], row_inv[2];         // the rows' sums, and their reciprocals
-    uint32_t inv_digits[2];             // the reciprocal as digits / 2^(inv_shift + 53 - 30), for weights in units of 2^-53
-    int inv_shift[2];
     int64_t total;                      // this block's weights
     int64_t at, before;                 // the drawn place among all weights, the weights of lower blocks
     int64_t below;                      // weights before the piece that holds the drawn token
     int none, piece, good, unsure;
-    float2 table[256], fast_table[STEPS];   // of Term<true>, of Term<false>
-    int64_t weight[1];                  // of each of the block's pieces (as many as there are)
+    // a draw by FastTerm: sums of the rows' terms, and of those of the tokens that count, by warp and over the block; what lies near p = q
+    int64_t fast_warp[4][16], fast[4];
+    float near_warp[16], near;
+    int64_t low_p, low_q, margin;       // the sums of lower blocks
+    uint32_t ratio;                     // of the rows' sums, in units of 2^-30
+    float2 table[256], fast_table[STEPS];
+    int64_t weight[1];                  // of each of the block's pieces (as many as there are); with FastTerm p's, then q's
 };
 
 // one row of a position
@@ -361,43 +345,25 @@ struct Walk {
         return x;
     }
 
-    // a row's sum is below 2^above (and not below 2^(above - 2))
+    // a row's sum lies between 2^(above - 1) and 2^above, but for the statistics' error
     static __device__ __forceinline__ int above(const Row<T> &r) { return (int)(__float_as_uint(__fmul_rn(r.s, 1.0f + 0x1p-10f)) >> 23) - 126; }
 
-    template <bool EXACT>
-    __device__ __forceinline__ Term<EXACT> term_of(const Row<T> &r, int shift0) const
-    {
-        if constexpr (EXACT) return {r.m, r.scale, sh.table};
-        else return {r.m, r.scale, sh.fast_table, shift0};
-    }
-
-    // The rows' sums, into sh.row_sum and sh.row_inv: good to 2^-42, or as good as Term<false> is.  Whole numbers are added up: no
-    // order of warps and blocks shows in them.
-    template <bool EXACT>
+    // The rows' sums good to 2^-42, into sh.row_sum and sh.row_inv.  Whole numbers are added up: no order of warps and blocks shows in
+    // them.
     __device__ __forceinline__ void sums(const Row<T> &p, const Row<T> &q)
     {
         constexpr int N = PIECE / 32;
 #pragma unroll 1
         for (int which = 0; which < (q.z ? 2 : 1); ++which) {
-            const auto term = term_of<EXACT>(which ? q : p, 0);
-            const uint32_t up = 1u << (32 - above(which ? q : p));       // the sum is below 2^62 units of 2^-30 / up
+            const float m = which ? q.m : p.m, scale = which ? q.scale : p.scale;
             int64_t high = 0, low = 0;
             each_piece(which ? q.z : p.z, nullptr, [&](int, const T (&x)[N], const T (&)[N]) {
-                if constexpr (EXACT) {
-                    Units sum;
+                Units sum;
 #pragma unroll
-                    for (int u = 0; u < N; ++u) sum.add(term(to_float(x[u])));
-                    high += sum.high, low += sum.low;
-                } else {
-#pragma unroll
-                    for (int u = 0; u < N; u += 2) {
-                        const Digits d = term(to_float(x[u]), to_float(x[u + 1]));
-                        low += (int64_t)(shifted((uint64_t)d.digits[0] * up, d.shift[0]) + shifted((uint64_t)d.digits[1] * up, d.shift[1]));
-                    }
-                }
+                for (int u = 0; u < N; ++u) sum.add(exp_two(to_float(x[u]), m, scale, sh.table));
+                high += sum.high, low += sum.low;
             });
-            if (EXACT) high = block_sum(high, sh.warp_sum[0]);
-            low = block_sum(low, sh.warp_sum[1]);
+            high = block_sum(high, sh.warp_sum[0]), low = block_sum(low, sh.warp_sum[1]);
             if (threadIdx.x == 0) sh.sum[which][0] = high, sh.sum[which][1] = low;
             __syncthreads();
         }
@@ -408,74 +374,31 @@ struct Walk {
                 const int64_t *o = cluster.map_shared_rank(&sh, b)->sum[threadIdx.x];
                 high += o[0], low += o[1];
             }
-            const float unit = EXACT ? 0x1p-46f : __int_as_float((127 - 62 + above(threadIdx.x ? q : p)) << 23);
-            const Two sum = EXACT ? two_of(high, low, unit) : two_of(low >> 23, low & 0x7fffff, unit), inv = inverse_of(sum);
-            sh.row_sum[threadIdx.x] = sum, sh.row_inv[threadIdx.x] = inv;
-            if (!EXACT) {
-                const int e = (__float_as_int(inv.hi) >> 23) - 127;           // 2^e <= inv.hi < 2^(e + 1)
-                const float scale = __int_as_float((30 - e + 127) << 23);
-                sh.inv_digits[threadIdx.x] = (uint32_t)(__float2ll_rn(__fmul_rn(inv.hi, scale)) + __float2ll_rn(__fmul_rn(inv.lo, scale)));
-                sh.inv_shift[threadIdx.x] = 30 - 53 + 30 - e;
-            }
+            sh.row_sum[threadIdx.x] = two_of(high, low);
+            sh.row_inv[threadIdx.x] = inverse_of(sh.row_sum[threadIdx.x]);
         }
         cluster.sync();                  // the others' sums have been read
     }
 
-    // tokens' weights in a draw
-    template <bool EXACT>
+    // tokens' weights in a draw, in units of 2^-46
     struct Weights {
-        Term<EXACT> p, q;
-        Two p_inv, q_inv;                // EXACT
-        uint32_t p_digits, q_digits;     // else
+        Row<T> p, q;
+        Two p_inv, q_inv;
         int without;                     // a token left out
-        bool less;                       // the draft's probabilities are taken off
-        __device__ __forceinline__ Two exact(T z, T y) const
+        const float2 *table;
+        __device__ __forceinline__ int64_t operator()(int j, T z, T y) const
         {
-            Two a = times(p(to_float(z)), p_inv);
-            if (less) {
-                const Two b = times(q(to_float(y)), q_inv);
+            Two a = times(exp_two(to_float(z), p.m, p.scale, table), p_inv);
+            if (q.z) {
+                const Two b = times(exp_two(to_float(y), q.m, q.scale, table), q_inv);
                 const float d = __fsub_rn(a.hi, b.hi), e = __fsub_rn(d, a.hi);
                 const float dl = __fsub_rn(__fsub_rn(a.hi, __fsub_rn(d, e)), __fadd_rn(b.hi, e));
                 a = {d, __fadd_rn(dl, __fsub_rn(a.lo, b.lo))};
             }
-            return __fadd_rn(a.hi, a.lo) < 0.0f ? Two{0.0f, 0.0f} : a;
-        }
-        // of two tokens, in units of 2^-46 (EXACT) or 2^-53
-        __device__ __forceinline__ void two(T z0, T z1, T y0, T y1, int64_t (&w)[2]) const
-        {
-            if constexpr (EXACT) {
-                const Two a[2] = {exact(z0, y0), exact(z1, y1)};
-#pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    Units one;
-                    one.add(a[i]);
-                    w[i] = one.whole();
-                }
-            } else {
-                const Digits d = p(to_float(z0), to_float(z1));
-#pragma unroll
-                for (int i = 0; i < 2; ++i) w[i] = (int64_t)shifted((uint64_t)d.digits[i] * p_digits, d.shift[i]);
-                if (less) {
-                    const Digits e = q(to_float(y0), to_float(y1));
-#pragma unroll
-                    for (int i = 0; i < 2; ++i) w[i] = max((long long)(w[i] - (int64_t)shifted((uint64_t)e.digits[i] * q_digits, e.shift[i])), 0ll);
-                }
-            }
-        }
-        // of a lane's tokens j, j + step, ..
-        template <int N>
-        __device__ __forceinline__ void all(int j, int step, const T (&z)[N], const T (&y)[N], int64_t (&w)[N]) const
-        {
-#pragma unroll
-            for (int u = 0; u < N; u += 2) {
-                int64_t x[2];
-                two(z[u], z[u + 1], y[u], y[u + 1], x);
-                w[u] = x[0], w[u + 1] = x[1];
-            }
-            if (without >= 0)
-#pragma unroll
-                for (int u = 0; u < N; ++u)
-                    if (j + u * step == without) w[u] = 0;
+            if (j == without || __fadd_rn(a.hi, a.lo) < 0.0f) return 0;
+            Units one;
+            one.add(a);
+            return one.whole();
         }
     };
 
@@ -491,20 +414,39 @@ struct Walk {
         return (int64_t)(shift < 64 ? high << (64 - shift) | low >> shift : shift < 128 ? high >> (shift - 64) : 0);
     }
 
+    // inclusive sums over the lanes
+    static __device__ __forceinline__ int64_t scan(int64_t x)
+    {
+#pragma unroll
+        for (int off = 1; off < 32; off <<= 1) {
+            const int64_t y = __shfl_up_sync(FULL, x, off);
+            if ((int)(threadIdx.x & 31) >= off) x += y;
+        }
+        return x;
+    }
+    // a lane's neighbouring tokens of a piece
+    template <int N>
+    __device__ __forceinline__ void lane_tokens(const T *z, int j0, T (&x)[N]) const
+    {
+#pragma unroll
+        for (int u = 0; u < N; ++u) {
+            x[u] = from_float<T>(-INFINITY);
+            if (z && j0 + u < cols) x[u] = z[j0 + u];
+        }
+    }
+
     // The smallest token whose running sum of weights passes v times all of them, and its logit: on the thread that finds it, -1 on
-    // the others.  Sets sh.none where no token has a weight; without EXACT sh.unsure where the place lies so near to a border between
-    // two tokens' weights that their errors may have moved it.
-    template <bool EXACT>
-    __device__ __forceinline__ int draw(const T *p, const T *q, const Weights<EXACT> &weight, float v, float &logit)
+    // the others.  Sets sh.none where no token has a weight.
+    __device__ __forceinline__ int draw(const Weights &weight, float v, float &logit)
     {
         constexpr int N = PIECE / 32;
         const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
         int64_t all = 0;                 // on lane 0
-        each_piece(p, q, [&](int i, const T (&z)[N], const T (&y)[N]) {
-            int64_t w[N];
-            weight.all((first_piece + i) * PIECE + lane, 32, z, y, w);
-            // the lanes' sums, 2^53 at most, added up in two halves
-            const uint64_t own = (uint64_t)(w[0] + w[1] + w[2] + w[3]);
+        each_piece(weight.p.z, weight.q.z, [&](int i, const T (&z)[N], const T (&y)[N]) {
+            uint64_t own = 0;
+#pragma unroll
+            for (int u = 0; u < N; ++u) own += (uint64_t)weight((first_piece + i) * PIECE + u * 32 + lane, z[u], y[u]);
+            // the lanes' sums, 2^46 at most, added up in two halves
             const int64_t sum = ((int64_t)__reduce_add_sync(FULL, (unsigned)(own >> 27)) << 27) + __reduce_add_sync(FULL, (unsigned)own & 0x7ffffff);
             if (lane == 0) sh.weight[i] = sum, all += sum;
         });
@@ -519,7 +461,6 @@ struct Walk {
                 total += x;
             }
             sh.none = total <= 0;
-            sh.unsure = false;
             sh.before = before;
             sh.at = share_of_total(v, total);
         }
@@ -531,13 +472,7 @@ struct Walk {
             const int each = (pieces + 31) / 32, i0 = min(pieces, lane * each), i1 = min(pieces, i0 + each);
             int64_t mine = 0;
             for (int i = i0; i < i1; ++i) mine += sh.weight[i];
-            int64_t up = mine;
-#pragma unroll
-            for (int off = 1; off < 32; off <<= 1) {
-                const int64_t x = __shfl_up_sync(FULL, up, off);
-                if (lane >= off) up += x;
-            }
-            int64_t below = before + up - mine;
+            int64_t below = before + scan(mine) - mine;
             if (at >= below && at < below + mine) {
                 int i = i0;
                 while (at >= below + sh.weight[i]) below += sh.weight[i++];
@@ -545,37 +480,187 @@ struct Walk {
                 sh.below = below;
             }
             __syncwarp();
-            // a lane's neighbouring tokens of it
             const int j0 = sh.piece * PIECE + lane * N;
             T z[N], y[N];
-#pragma unroll
-            for (int u = 0; u < N; ++u) {
-                z[u] = y[u] = from_float<T>(-INFINITY);
-                if (j0 + u < cols) z[u] = p[j0 + u];
-                if (j0 + u < cols && q) y[u] = q[j0 + u];
-            }
+            lane_tokens(weight.p.z, j0, z);
+            lane_tokens(weight.q.z, j0, y);
             int64_t w[N], sum = 0;
-            weight.all(j0, 1, z, y, w);
 #pragma unroll
-            for (int u = 0; u < N; ++u) sum += w[u];
-            up = sum;
-#pragma unroll
-            for (int off = 1; off < 32; off <<= 1) {
-                const int64_t x = __shfl_up_sync(FULL, up, off);
-                if (lane >= off) up += x;
-            }
-            below = sh.below + up - sum;
-            const int64_t margin = EXACT ? 0 : MARGIN;
-            bool sure = false;
+            for (int u = 0; u < N; ++u) w[u] = weight(j0 + u, z[u], y[u]), sum += w[u];
+            below = sh.below + scan(sum) - sum;
 #pragma unroll
             for (int u = 0; u < N; ++u) {
-                if (at >= below + margin && at < below + w[u] - margin) found = j0 + u, logit = to_float(z[u]), sure = true;
+                if (at >= below && at < below + w[u]) found = j0 + u, logit = to_float(z[u]);
                 below += w[u];
             }
-            if (!EXACT && !__any_sync(FULL, sure) && lane < blocks) cluster.map_shared_rank(&sh, lane)->unsure = true;
         }
-        if (!EXACT) cluster.sync();      // every block knows
         return found;
+    }
+
+    // The same by FastTerm in one pass, with sh.unsure set where it may not be that token.  The weights are p - (SP / SQ) q of the tokens where that is
+    // positive, SP and SQ the rows' sums, which are known at the end of the pass only; so what is summed are the terms of p and those of q, over all
+    // tokens and over those where p / s > q / s', s and s' the sums as the 32-bit statistics have them.  A token is taken for the wrong side only
+    // where p and q differ by less than the statistics' error, and that error times the probability of the tokens near p = q (to 2^-12 of p) bounds
+    // what it adds.
+    template <bool LESS>
+    __device__ __forceinline__ int fast_draw(const Row<T> &p, const Row<T> &q, int without, float v, float &logit)
+    {
+        constexpr int N = PIECE / 32, W = THREADS / 32;
+        const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+        const int above_p = above(p), above_q = LESS ? above(q) : 0;
+        const FastTerm of_p(p.m, p.scale, above_p), of_q(LESS ? q.m : p.m, LESS ? q.scale : p.scale, above_q);
+        // the terms' probabilities, as the statistics have them
+        const float p_inv = __fdiv_rn(__int_as_float((127 + above_p - 23) << 23), p.s);
+        const float q_inv = LESS ? __fdiv_rn(__int_as_float((127 + above_q - 23) << 23), q.s) : 0.0f;
+        int64_t *const weight_q = sh.weight + pieces;
+        int64_t sum_p = 0, sum_q = 0, in_p = 0, in_q = 0;
+        float near = 0.0f;
+        each_piece(p.z, LESS ? q.z : nullptr, [&](int i, const T (&z)[N], const T (&y)[N]) {
+            int ph = 0, pl = 0, qh = 0, ql = 0;              // all tokens (LESS)
+            int aph = 0, apl = 0, aqh = 0, aql = 0;          // those that count
+            const int skip = !LESS && without >= 0 ? without - (first_piece + i) * PIECE - lane : -1;
+#pragma unroll
+            for (int u = 0; u < N; u += 2) {
+                float c[2], d[2];
+                int h[2], l[2], g[2], k[2];
+                of_p(to_float(z[u]), to_float(z[u + 1]), sh.fast_table, c, h, l);
+                if (LESS) of_q(to_float(y[u]), to_float(y[u + 1]), sh.fast_table, d, g, k);
+#pragma unroll
+                for (int x = 0; x < 2; ++x) {
+                    if (LESS) {
+                        const float a = __fmul_rn(c[x], p_inv), b = __fmul_rn(d[x], q_inv), over = __fsub_rn(a, b);
+                        ph += h[x] - HIGH0, pl += l[x] - LOW0, qh += g[x] - HIGH0, ql += k[x] - LOW0;
+                        if (fabsf(over) <= __fmul_rn(a, 0x1p-12f)) near = __fadd_rn(near, a);
+                        if (over > 0.0f) aph += h[x] - HIGH0, apl += l[x] - LOW0, aqh += g[x] - HIGH0, aql += k[x] - LOW0;
+                    } else if (skip != (u + x) * 32) {
+                        aph += h[x] - HIGH0, apl += l[x] - LOW0;
+                    }
+                }
+            }
+            if (LESS) sum_p += units(ph, pl), sum_q += units(qh, ql);
+            aph = __reduce_add_sync(FULL, aph), apl = __reduce_add_sync(FULL, apl);
+            if (LESS) aqh = __reduce_add_sync(FULL, aqh), aql = __reduce_add_sync(FULL, aql);
+            if (lane == 0) {
+                sh.weight[i] = units(aph, apl);
+                in_p += units(aph, apl);
+                if (LESS) weight_q[i] = units(aqh, aql), in_q += units(aqh, aql);
+            }
+        });
+        const int64_t own[4] = {in_p, in_q, sum_p, sum_q};
+#pragma unroll
+        for (int k = 0; k < (LESS ? 4 : 1); ++k) {
+            int64_t x = own[k];
+            if (k >= 2)
+#pragma unroll
+                for (int off = 16; off >= 1; off >>= 1) x += __shfl_xor_sync(FULL, x, off);
+            if (lane == 0) sh.fast_warp[k][warp] = x;
+        }
+        if (LESS) {
+#pragma unroll
+            for (int off = 16; off >= 1; off >>= 1) near = __fadd_rn(near, __shfl_xor_sync(FULL, near, off));
+            if (lane == 0) sh.near_warp[warp] = near;
+        }
+        __syncthreads();
+        if (threadIdx.x < 4) {
+            int64_t x = 0;
+            for (int w = 0; w < (LESS || threadIdx.x == 0 ? W : 0); ++w) x += sh.fast_warp[threadIdx.x][w];
+            sh.fast[threadIdx.x] = x;
+        } else if (threadIdx.x == 32) {
+            float x = 0.0f;
+            for (int w = 0; w < (LESS ? W : 0); ++w) x = __fadd_rn(x, sh.near_warp[w]);
+            sh.near = x;
+        }
+        cluster.sync();
+        if (threadIdx.x == 0) {
+            int64_t all[4] = {0, 0, 0, 0}, low_p = 0, low_q = 0;
+            float close = 0.0f;
+            for (int b = 0; b < blocks; ++b) {
+                const Shared *o = cluster.map_shared_rank(&sh, b);
+#pragma unroll
+                for (int k = 0; k < (LESS ? 4 : 1); ++k) all[k] += o->fast[k];
+                close = __fadd_rn(close, o->near);
+                if (b < rank) low_p += o->fast[0], low_q += o->fast[1];
+            }
+            sh.low_p = low_p, sh.low_q = low_q;
+            sh.ratio = 0, sh.margin = fast_margin(cols), sh.unsure = false;
+            if (LESS) {
+                sh.ratio = (uint32_t)(((uint64_t)all[2] << 17) / (uint64_t)max((long long)(all[3] >> 13), 1ll));
+                // the statistics' error, from what the sums have come to
+                const float x = __fmul_rn(__fdiv_rn(__ll2float_rn(all[2]), __ll2float_rn(all[3])), __fdiv_rn(p_inv, q_inv));
+                const float off = __fadd_rn(fabsf(__fsub_rn(x, 1.0f)), 0x1p-20f);
+                sh.unsure = !(off < 0x1p-13f);
+                sh.margin += __float2ll_rn(__fmul_rn(__fmul_rn(off, __fmul_rn(close, 1.01f)), 0x1p45f));
+            }
+            const int64_t total = all[0] - less(all[1], sh.ratio);
+            if (total <= 2 * sh.margin) sh.unsure = true;
+            sh.at = share_of_total(v, max((long long)total, 1ll));
+        }
+        cluster.sync();                  // the others' sums have been read
+        int found = -1;
+        const int64_t at = sh.at, margin = sh.margin;
+        const uint32_t ratio = sh.ratio;
+        int64_t P = sh.low_p, Q = sh.low_q;
+        if (warp == 0 && !sh.unsure && at >= P - less(Q, ratio) && at < P + sh.fast[0] - less(Q + sh.fast[1], ratio)) {
+            const int each = (pieces + 31) / 32, i0 = min(pieces, lane * each), i1 = min(pieces, i0 + each);
+            int64_t mine_p = 0, mine_q = 0;
+            for (int i = i0; i < i1; ++i) {
+                mine_p += sh.weight[i];
+                if (LESS) mine_q += weight_q[i];
+            }
+            int64_t to_p = P + scan(mine_p), to_q = LESS ? Q + scan(mine_q) : 0;
+            const bool here = i1 > i0 && at >= to_p - mine_p - less(to_q - mine_q, ratio) && at < to_p - less(to_q, ratio);
+            const unsigned lanes = __ballot_sync(FULL, here);
+            bool sure = false;
+            if (lanes) {
+                if (lane == __ffs(lanes) - 1) {
+                    P = to_p - mine_p, Q = to_q - mine_q;
+                    int i = i0;
+                    for (; i < i1 - 1; ++i) {
+                        const int64_t next_p = P + sh.weight[i], next_q = Q + (LESS ? weight_q[i] : 0);
+                        if (at < next_p - less(next_q, ratio)) break;
+                        P = next_p, Q = next_q;
+                    }
+                    sh.piece = first_piece + i;
+                    sh.low_p = P, sh.low_q = Q;
+                }
+                __syncwarp();
+                const int j0 = sh.piece * PIECE + lane * N;
+                T z[N], y[N];
+                lane_tokens(p.z, j0, z);
+                lane_tokens(LESS ? q.z : nullptr, j0, y);
+                int64_t wp[N], wq[N], sum_p = 0, sum_q = 0;
+#pragma unroll
+                for (int u = 0; u < N; u += 2) {
+                    float c[2], d[2];
+                    int h[2], l[2], g[2], k[2];
+                    of_p(to_float(z[u]), to_float(z[u + 1]), sh.fast_table, c, h, l);
+                    if (LESS) of_q(to_float(y[u]), to_float(y[u + 1]), sh.fast_table, d, g, k);
+#pragma unroll
+                    for (int x = 0; x < 2; ++x) {
+                        const bool counts = LESS ? __fsub_rn(__fmul_rn(c[x], p_inv), __fmul_rn(d[x], q_inv)) > 0.0f : j0 + u + x != without;
+                        wp[u + x] = counts ? units(h[x] - HIGH0, l[x] - LOW0) : 0;
+                        wq[u + x] = LESS && counts ? units(g[x] - HIGH0, k[x] - LOW0) : 0;
+                        sum_p += wp[u + x], sum_q += wq[u + x];
+                    }
+                }
+                P = sh.low_p + scan(sum_p) - sum_p, Q = LESS ? sh.low_q + scan(sum_q) - sum_q : 0;
+#pragma unroll
+                for (int u = 0; u < N; ++u) {
+                    const int64_t from = P - less(Q, ratio);
+                    P += wp[u], Q += wq[u];
+                    if (at >= from + margin && at < P - less(Q, ratio) - margin) found = j0 + u, logit = to_float(z[u]), sure = true;
+                }
+                sure = __any_sync(FULL, sure);
+            }
+            if (!sure && lane < blocks) cluster.map_shared_rank(&sh, lane)->unsure = true;
+        }
+        cluster.sync();                  // every block knows
+        return found;
+    }
+    // x * ratio / 2^30
+    static __device__ __forceinline__ int64_t less(int64_t x, uint32_t ratio)
+    {
+        return (int64_t)(__umul64hi((uint64_t)x, (uint64_t)ratio) << 34 | (uint64_t)x * ratio >> 30);
     }
 };
 
@@ -653,7 +738,7 @@ __global__ __launch_bounds__(THREADS, THREADS == 512 ? 1 : 4) void k_verify(cons
             if (seen) set_status(status, PDB_ERANGE);
         }
     }
-    for (int i = threadIdx.x; i < STEPS; i += THREADS) sh.fast_table[i] = {FAST_TABLE.value[i], __int_as_float(FAST_TABLE.digits[i])};
+    for (int i = threadIdx.x; i < STEPS; i += THREADS) sh.fast_table[i] = {FAST_TABLE.hi[i], FAST_TABLE.lo[i]};
     const float v = draw_u[s];
     __syncthreads();
 
@@ -697,7 +782,7 @@ __global__ __launch_bounds__(THREADS, THREADS == 512 ? 1 : 4) void k_verify(cons
         if (!(fabsf(left - right) > SURE * more && more > 1e-30f)) {
             if (!exact) walk.fill_table();
             exact = true;
-            walk.template sums<true>(p, q);
+            walk.sums(p, q);
             if (threadIdx.x == 0) {
                 const auto in_64 = [](float scale, float z, const Row<T> &r, Two sum) {
                     return exp((double)scale * ((double)z - (double)r.m)) / ((double)sum.hi + (double)sum.lo);
@@ -729,25 +814,17 @@ __global__ __launch_bounds__(THREADS, THREADS == 512 ? 1 : 4) void k_verify(cons
             float z = 0.0f;
             int drawn;
             if (fast) {
-                if (q.z) walk.template sums<false>(p, q);
-                typename Walk<T, THREADS>::template Weights<false> weight;
-                // one row's weights need no more than a common factor, a power of two
-                weight.p = walk.template term_of<false>(p, q.z ? sh.inv_shift[0] : 30 - 53 + 31 + walk.above(p));
-                weight.q = walk.template term_of<false>(q, sh.inv_shift[1]);
-                weight.p_digits = q.z ? sh.inv_digits[0] : 1u << 31, weight.q_digits = sh.inv_digits[1];
-                weight.without = without, weight.less = q.z != nullptr;
-                drawn = walk.template draw<false>(p.z, q.z, weight, v, z);
+                drawn = q.z ? walk.template fast_draw<true>(p, q, -1, v, z) : walk.template fast_draw<false>(p, q, without, v, z);
             } else {
                 if (!filled) walk.fill_table();
                 filled = true;
-                if (q.z) walk.template sums<true>(p, q);
+                if (q.z) walk.sums(p, q);
+                // one row's weights need no more than a common factor, a power of two
                 const Two unit = {__int_as_float((127 - walk.above(p)) << 23), 0.0f};
-                drawn = walk.template draw<true>(p.z, q.z,
-                                                 {{p.m, p.scale, sh.table}, {q.m, q.scale, sh.table}, q.z ? sh.row_inv[0] : unit,
-                                                  sh.row_inv[1], 0, 0, without, q.z != nullptr}, v, z);
+                drawn = walk.draw({p, q, q.z ? sh.row_inv[0] : unit, sh.row_inv[1], without, sh.table}, v, z);
             }
-            none = sh.none;
-            const bool unsure = fast && (none || sh.unsure);
+            const bool unsure = fast && sh.unsure;
+            none = !fast && sh.none;
             if (drawn >= 0) {
                 out.tokens[base + a] = drawn;
                 if (out.logp) out.logp[base + a] = __fmaf_rn(__fsub_rn(z, p.m), scale, -log_s);
@@ -772,7 +849,7 @@ __global__ __launch_bounds__(THREADS, THREADS == 512 ? 1 : 4) void k_verify(cons
 
 size_t verify_smem(int64_t cols, int blocks)
 {
-    return sizeof(Shared) + sizeof(int64_t) * (((cols + PIECE - 1) / PIECE + blocks - 1) / blocks + 1);
+    return sizeof(Shared) + 2 * sizeof(int64_t) * (((cols + PIECE - 1) / PIECE + blocks - 1) / blocks + 1);
 }
 
 }  // namespace
