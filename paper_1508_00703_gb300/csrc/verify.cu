@@ -123,10 +123,10 @@ __device__ __forceinline__ Two two_of(int64_t high, int64_t low)
     return {__fmul_rn(h, 0x1p-23f), __fmul_rn(__ll2float_rn(rest * 0x800000 + low), 0x1p-46f)};
 }
 
-// exp(scale (z - m)) 2^-above of two tokens at once, z <= m, where |m scale| log2(e) < 2^9, to 2^-31.5: n + f = 512 (z c - m c),
+// exp(scale (z - m)) 2^-down of two tokens at once, z <= m, where |m scale| log2(e) < 2^9, to 2^-31.5: n + f = 512 (z c - m c),
 // c = scale log2(e), n whole and |f| <= 1, f formed by roundings of 2^-25; with n = 512 (-k) + i, 2^(i/512) + 2^(i/512) (2^(f/512) - 1) times a
-// power of two.  An error that all tokens of a row share falls out of its probabilities.  What the sums are made of are whole numbers of 2^-23 and of
-// 2^-45, both in the lowest bits of a float: additions and multiplications by the pair do nearly all of it (whole numbers
+// power of two.  An error that all tokens of a row share falls out of its probabilities.  What the sums are made of are whole numbers of 2^-22 and of
+// 2^-44, both in the lowest bits of a float: additions and multiplications by the pair do nearly all of it (whole numbers
 // shifted into place took 2.5 times as long: half of the integer unit's instructions).
 constexpr float REACH = 512.0f;
 constexpr int STEPS = 512, LOG_STEPS = 9;
@@ -139,7 +139,7 @@ struct FastTerm {
     uint64_t ch, cl, from, rest;        // two of each
     float low;
     uint32_t bias;                      // of the power of two's bits
-    __device__ __forceinline__ FastTerm(float m, float scale, int above)
+    __device__ __forceinline__ FastTerm(float m, float scale, int down)
     {
         constexpr float log2e_rest = (float)(1.4426950408889634073599 - (double)LOG2E);
         const float c = __fmul_rn(scale, LOG2E), c_rest = __fmaf_rn(scale, log2e_rest, __fmaf_rn(scale, LOG2E, -c));
@@ -148,9 +148,9 @@ struct FastTerm {
         ch = both(c1), cl = both(c2), from = both(__fsub_rn(12582912.0f, whole));
         rest = both(-__fadd_rn(__fsub_rn(mc, whole), __fmaf_rn(m, c2, __fmaf_rn(m, c1, -mc))));
         low = __fsub_rn(m, __fdiv_rn(60.0f, c));             // nothing below 2^-60
-        bias = ((uint32_t)(127 + 23 - above) << 23) - ((uint32_t)(LOW0 >> LOG_STEPS) << 23);
+        bias = ((uint32_t)(127 + 22 - down) << 23) - ((uint32_t)(LOW0 >> LOG_STEPS) << 23);
     }
-    // value: the terms times 2^23; high - HIGH0 units of 2^-23 and lowest - LOW0 of 2^-45 (what is left is 0.625 of 2^-23 at most)
+    // value: the terms times 2^22; high - HIGH0 units of 2^-22 and lowest - LOW0 of 2^-44 (what is left is 0.625 of 2^-22 at most)
     __device__ __forceinline__ void operator()(float z0, float z1, const float2 *table, float (&value)[2], int (&high)[2],
                                                int (&lowest)[2]) const
     {
@@ -178,10 +178,10 @@ struct FastTerm {
 };
 __device__ __forceinline__ int64_t units(int high, int low) { return (int64_t)high * 0x400000 + low; }
 
-// How far from its token's borders a draw by FastTerm must lie to be taken, in units of 2^-45 of rows whose terms add up to 1/2 to 1: the terms
-// of both rows, and their sums, move the running sum and v times the whole one by 4 * 2^-31.5 together, their rounding to units by two
-// for each token.
-__device__ __forceinline__ int64_t fast_margin(int cols) { return (1 << 16) + 2 * (int64_t)cols; }
+// How far from its token's borders a draw by FastTerm must lie to be taken, in units of 2^-44 of rows whose terms add up to 2^(fine - 1) to
+// 2^fine: the terms of both rows, and their sums, move the running sum and v times the whole one by 4 * 2^-31.5 together, their
+// rounding to units by two for each token.
+__device__ __forceinline__ int64_t fast_margin(int cols, int fine) { return ((int64_t)1 << (15 + fine)) + 2 * (int64_t)cols; }
 
 // ------------------------------------------------------------------ shared by the blocks of a sequence
 struct Shared {
@@ -507,11 +507,12 @@ struct Walk {
     {
         constexpr int N = PIECE / 32, W = THREADS / 32;
         const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-        const int above_p = above(p), above_q = LESS ? above(q) : 0;
-        const FastTerm of_p(p.m, p.scale, above_p), of_q(LESS ? q.m : p.m, LESS ? q.scale : p.scale, above_q);
+        // the rows' sums are brought to the same size, as large as the largest term and 62 bits allow: fine units
+        const int above_p = above(p), above_q = LESS ? above(q) : above_p, fine = min(min(above_p, above_q), 17);
+        const FastTerm of_p(p.m, p.scale, above_p - fine), of_q(LESS ? q.m : p.m, LESS ? q.scale : p.scale, above_q - fine);
         // the terms' probabilities, as the statistics have them
-        const float p_inv = __fdiv_rn(__int_as_float((127 + above_p - 23) << 23), p.s);
-        const float q_inv = LESS ? __fdiv_rn(__int_as_float((127 + above_q - 23) << 23), q.s) : 0.0f;
+        const float p_inv = __fdiv_rn(__int_as_float((127 + above_p - fine - 22) << 23), p.s);
+        const float q_inv = LESS ? __fdiv_rn(__int_as_float((127 + above_q - fine - 22) << 23), q.s) : 0.0f;
         int64_t *const weight_q = sh.weight + pieces;
         int64_t sum_p = 0, sum_q = 0, in_p = 0, in_q = 0;
         float near = 0.0f;
@@ -582,14 +583,14 @@ struct Walk {
                 if (b < rank) low_p += o->fast[0], low_q += o->fast[1];
             }
             sh.low_p = low_p, sh.low_q = low_q;
-            sh.ratio = 0, sh.margin = fast_margin(cols), sh.unsure = false;
+            sh.ratio = 0, sh.margin = fast_margin(cols, fine), sh.unsure = false;
             if (LESS) {
-                sh.ratio = (uint32_t)(((uint64_t)all[2] << 17) / (uint64_t)max((long long)(all[3] >> 13), 1ll));
+                sh.ratio = (uint32_t)(((uint64_t)(all[2] >> fine) << 18) / (uint64_t)max((long long)(all[3] >> fine >> 12), 1ll));
                 // the statistics' error, from what the sums have come to
                 const float x = __fmul_rn(__fdiv_rn(__ll2float_rn(all[2]), __ll2float_rn(all[3])), __fdiv_rn(p_inv, q_inv));
                 const float off = __fadd_rn(fabsf(__fsub_rn(x, 1.0f)), 0x1p-20f);
                 sh.unsure = !(off < 0x1p-13f);
-                sh.margin += __float2ll_rn(__fmul_rn(__fmul_rn(off, __fmul_rn(close, 1.01f)), 0x1p45f));
+                sh.margin += __float2ll_rn(__fmul_rn(__fmul_rn(off, __fmul_rn(close, 1.01f)), __int_as_float((127 + 44 + fine) << 23)));
             }
             const int64_t total = all[0] - less(all[1], sh.ratio);
             if (total <= 2 * sh.margin) sh.unsure = true;
@@ -706,12 +707,79 @@ __global__ __launch_bounds__(THREADS, 1024 / THREADS) void k_verify_rows(const T
     if (writes) given[r] = {sh.joined[0][0], sh.joined[0][1], z, 0.0f};
 }
 
+// where a sequence's walk has come to: the first position that is not surely accepted, its rows' statistics and logits
+struct Start {
+    float m, s, z, qm, qs, qz;
+    int a, unused;
+};
+
+// whether u q < p, where the statistics can tell it (sure)
+template <typename T>
+__device__ __forceinline__ bool accepts(const Row<T> &p, const Row<T> &q, float z, float zq, float u, bool &sure)
+{
+    const float right = __fdiv_rn(ex2(__fmul_rn(__fsub_rn(z, p.m), __fmul_rn(p.scale, LOG2E))), p.s);
+    float left = u;
+    if (q.z) left = __fmul_rn(u, __fdiv_rn(ex2(__fmul_rn(__fsub_rn(zq, q.m), __fmul_rn(q.scale, LOG2E))), q.s));
+    const float more = fmaxf(left, right);
+    sure = fabsf(left - right) > SURE * more && more > 1e-30f;
+    return left < right;
+}
+
+// Many sequences: their walks, a cluster for each, up to the first position that k_verify has to look at.  Bound by memory, so with as many
+// threads as an SM holds; the draws' numbers want registers instead (both in one kernel: 256 x 5 drafts x 128,000 bf16 228 us).
 template <typename T, int THREADS>
-__global__ __launch_bounds__(THREADS, THREADS == 512 ? 1 : 4) void k_verify(const T *target, int64_t t_stride, const T *draft,
+__global__ __launch_bounds__(THREADS, 1024 / THREADS) void k_verify_walk(const T *target, int64_t t_stride, const T *draft,
+                                                                         int64_t d_stride, int cols, Ids ids, int D, float scale,
+                                                                         float draft_scale, const float *accept_u, VerifyOut out,
+                                                                         Start *__restrict__ start)
+{
+    after_previous();
+    let_next_start();
+    __shared__ Shared sh;
+    cg::cluster_group cluster = cg::this_cluster();
+    const int blocks = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
+    const int64_t s = blockIdx.x / (unsigned)blocks, base = s * (D + 1);
+    for (int d = threadIdx.x; d < D; d += THREADS) {
+        const int64_t t = load_id(ids, s, d);
+        sh.drafted[d] = t >= 0 && t < cols ? (int)t : -1;
+        sh.u[d] = accept_u[s * D + d];
+    }
+    __syncthreads();
+    Walk<T, THREADS> walk{sh, cluster, rank, blocks, cols, 0, 0};
+    const bool writes = rank == 0 && threadIdx.x == 0;
+    const float c = __fmul_rn(scale, LOG2E), cq = __fmul_rn(draft_scale, LOG2E);
+    Row<T> p{}, q{};
+    p.scale = scale, q.scale = draft_scale;
+    float z = 0.0f, zq = 0.0f;
+    int a = 0;
+#pragma unroll 1
+    for (;; ++a) {
+        const int t = a < D ? sh.drafted[a] : -1;
+        p.z = target + (base + a) * t_stride;
+        q.z = t >= 0 && draft ? draft + (s * D + a) * d_stride : nullptr;
+        if (t >= 0 && threadIdx.x < (q.z ? 2 : 1)) sh.z[threadIdx.x] = to_float((threadIdx.x ? q.z : p.z)[t]);
+        walk.stats(q.z ? 2 : 1, [&](int i) { return i ? q.z : p.z; }, [&](int i) { return i ? cq : c; }, a & 1);
+        p.m = sh.joined[0][0], p.s = sh.joined[0][1], z = sh.z[0];
+        if (q.z) q.m = sh.joined[1][0], q.s = sh.joined[1][1], zq = sh.z[1];
+        if (t < 0 || !p.valid() || (q.z && !q.valid())) break;
+        bool sure;
+        if (!accepts(p, q, z, zq, sh.u[a], sure) || !sure) break;
+        if (writes) {
+            out.tokens[base + a] = t;
+            if (out.logp) out.logp[base + a] = __fmaf_rn(__fsub_rn(z, p.m), scale, -logf(p.s));
+        }
+        __syncthreads();                 // before the next position's
+    }
+    if (writes) start[s] = {p.m, p.s, z, q.m, q.s, zq, a, 0};
+    cluster.sync();                      // the others have read this block's statistics
+}
+
+template <typename T, int THREADS>
+__global__ __launch_bounds__(THREADS, THREADS == 512 ? 1 : 2) void k_verify(const T *target, int64_t t_stride, const T *draft,
                                                                     int64_t d_stride, int cols, Ids ids, int64_t n, int D,
                                                                     float scale, float draft_scale, const float *accept_u,
-                                                                    const float *draw_u, const Given *given, VerifyOut out,
-                                                                    int *status)
+                                                                    const float *draw_u, const Given *given, const Start *start,
+                                                                    VerifyOut out, int *status)
 {
     after_previous();
     extern __shared__ __align__(16) unsigned char s_raw[];
@@ -745,7 +813,8 @@ __global__ __launch_bounds__(THREADS, THREADS == 512 ? 1 : 4) void k_verify(cons
     Row<T> p{}, q{};
     p.scale = scale, q.scale = draft_scale;
     const float c = __fmul_rn(scale, LOG2E), cq = __fmul_rn(draft_scale, LOG2E);
-    int a = 0;                           // the position
+    const int begin = start ? start[s].a : 0;
+    int a = begin;                       // the position
     bool refused = false, exact = false;
     int t = -1;
     float log_s = 0.0f;
@@ -762,6 +831,9 @@ __global__ __launch_bounds__(THREADS, THREADS == 512 ? 1 : 4) void k_verify(cons
                 const Given h = given[n * (D + 1) + s * D + a];
                 q.m = h.m, q.s = h.s, zq = h.z;
             }
+        } else if (start && a == begin) {
+            const Start g = start[s];
+            p.m = g.m, p.s = g.s, z = g.z, q.m = g.qm, q.s = g.qs, zq = g.qz;
         } else {
             if (t >= 0 && threadIdx.x < (q.z ? 2 : 1)) sh.z[threadIdx.x] = to_float((threadIdx.x ? q.z : p.z)[t]);
             walk.stats(q.z ? 2 : 1, [&](int i) { return i ? q.z : p.z; }, [&](int i) { return i ? cq : c; }, a & 1);
@@ -774,12 +846,8 @@ __global__ __launch_bounds__(THREADS, THREADS == 512 ? 1 : 4) void k_verify(cons
         if (q.z && !q.valid()) t = -1, q.z = nullptr;     // the drafts end here
         if (t < 0) break;
         const float u = sh.u[a];
-        const float right = __fdiv_rn(ex2(__fmul_rn(__fsub_rn(z, p.m), c)), p.s);
-        float left = u;
-        if (q.z) left = __fmul_rn(u, __fdiv_rn(ex2(__fmul_rn(__fsub_rn(zq, q.m), cq)), q.s));
-        const float more = fmaxf(left, right);
-        bool good = left < right;
-        if (!(fabsf(left - right) > SURE * more && more > 1e-30f)) {
+        bool sure, good = accepts(p, q, z, zq, u, sure);
+        if (!sure) {
             if (!exact) walk.fill_table();
             exact = true;
             walk.sums(p, q);
@@ -889,6 +957,7 @@ int pdb_verify(pdb_tokens *t, const pdb_mat *target, const pdb_ids *draft_ids, i
         shape.threads = few ? 512 : 256;
         shape.blocks = cluster_of(n, nv, shape.threads, [&](int blocks) { return t->sms * (few ? 2 : 8) / blocks; });
         shape.clusters = n;
+        const Shape walk = shape;
         shape.smem = verify_smem(target->cols, shape.blocks);
         const Ids id = n_drafts > 0 ? ids_of(draft_ids) : Ids{};
         const T *z = (const T *)target->data, *y = draft ? (const T *)draft->data : nullptr;
@@ -903,9 +972,16 @@ int pdb_verify(pdb_tokens *t, const pdb_mat *target, const pdb_ids *draft_ids, i
                                        (int)n_drafts, scale, draft_scale, given);
             if (rc != PDB_OK) return rc;
         }
+        Start *start = nullptr;
+        if (!few && !ahead && n_drafts > 0 && n <= VERIFY_ROWS / 2) {
+            start = (Start *)t->given;
+            const int rc = launch_rows(k_verify_walk<T, 256>, walk, s, z, z_step, y, y_step, (int)target->cols, id, (int)n_drafts, scale,
+                                       draft_scale, accept_u, VerifyOut{tokens, accepted, logp}, start);
+            if (rc != PDB_OK) return rc;
+        }
         const auto run = [&](auto k) {
             return launch_rows(k_verify<T, decltype(k)::value>, shape, s, z, z_step, y, y_step, (int)target->cols, id, n,
-                               (int)n_drafts, scale, draft_scale, accept_u, draw_u, (const Given *)given,
+                               (int)n_drafts, scale, draft_scale, accept_u, draw_u, (const Given *)given, (const Start *)start,
                                VerifyOut{tokens, accepted, logp}, t->status);
         };
         return few ? run(Num<512>()) : run(Num<256>());
