@@ -136,17 +136,25 @@ constexpr int HIGH0 = 0x4b000000, LOW0 = 0x4b400000;       // the bits of 2^23 a
 __device__ __forceinline__ uint64_t both(float x) { return pair(x, x); }
 
 struct FastTerm {
-    uint64_t ch, cl, from, rest;        // two of each
-    float low;
-    uint32_t bias;                      // of the power of two's bits
-    __device__ __forceinline__ FastTerm(float m, float scale, int down)
+    uint64_t ch, cl, from, rest;        // of the first token's row, of the second's
+    float low0, low1;
+    uint32_t bias0, bias1;              // of the powers of two's bits
+    __device__ __forceinline__ FastTerm(float m0, float scale0, int down0, float m1, float scale1, int down1)
+    {
+        float c[2], d[2], f[2], r[2];
+        of_row(m0, scale0, down0, c[0], d[0], f[0], r[0], low0, bias0);
+        of_row(m1, scale1, down1, c[1], d[1], f[1], r[1], low1, bias1);
+        ch = pair(c[0], c[1]), cl = pair(d[0], d[1]), from = pair(f[0], f[1]), rest = pair(r[0], r[1]);
+    }
+    static __device__ __forceinline__ void of_row(float m, float scale, int down, float &c1, float &c2, float &from, float &rest, float &low,
+                                                  uint32_t &bias)
     {
         constexpr float log2e_rest = (float)(1.4426950408889634073599 - (double)LOG2E);
         const float c = __fmul_rn(scale, LOG2E), c_rest = __fmaf_rn(scale, log2e_rest, __fmaf_rn(scale, LOG2E, -c));
-        const float c1 = __fmul_rn(c, (float)STEPS), c2 = __fmul_rn(c_rest, (float)STEPS);
+        c1 = __fmul_rn(c, (float)STEPS), c2 = __fmul_rn(c_rest, (float)STEPS);
         const float mc = __fmul_rn(m, c1), whole = rintf(mc);
-        ch = both(c1), cl = both(c2), from = both(__fsub_rn(12582912.0f, whole));
-        rest = both(-__fadd_rn(__fsub_rn(mc, whole), __fmaf_rn(m, c2, __fmaf_rn(m, c1, -mc))));
+        from = __fsub_rn(12582912.0f, whole);
+        rest = -__fadd_rn(__fsub_rn(mc, whole), __fmaf_rn(m, c2, __fmaf_rn(m, c1, -mc)));
         low = __fsub_rn(m, __fdiv_rn(60.0f, c));             // nothing below 2^-60
         bias = ((uint32_t)(127 + 22 - down) << 23) - ((uint32_t)(LOW0 >> LOG_STEPS) << 23);
     }
@@ -155,7 +163,7 @@ struct FastTerm {
                                                int (&lowest)[2]) const
     {
         constexpr double L = LN2_D / STEPS;
-        const uint64_t z = pair(fmaxf(z0, low), fmaxf(z1, low));
+        const uint64_t z = pair(fmaxf(z0, low0), fmaxf(z1, low1));
         const uint64_t t = fma2(z, ch, from);                // n in its lowest bits
         const uint64_t f = add2(fma2(z, ch, fma2(t, both(-1.0f), from)), fma2(z, cl, rest));
         const uint64_t s = mul2(f, fma2(f, fma2(f, both((float)(L * L * L / 6)), both((float)(L * L / 2))), both((float)L)));
@@ -163,7 +171,7 @@ struct FastTerm {
         unpair(t, t0, t1);
         const uint32_t n0 = __float_as_uint(t0), n1 = __float_as_uint(t1);
         const float2 a = table[n0 & (STEPS - 1)], b = table[n1 & (STEPS - 1)];
-        const uint64_t power = pair(__uint_as_float(((n0 >> LOG_STEPS) << 23) + bias), __uint_as_float(((n1 >> LOG_STEPS) << 23) + bias));
+        const uint64_t power = pair(__uint_as_float(((n0 >> LOG_STEPS) << 23) + bias0), __uint_as_float(((n1 >> LOG_STEPS) << 23) + bias1));
         const uint64_t main = mul2(pair(a.x, b.x), power), more = mul2(fma2(pair(a.x, b.x), s, pair(a.y, b.y)), power);
         const uint64_t sum = add2(main, more);
         unpair(sum, value[0], value[1]);
@@ -294,6 +302,15 @@ struct Walk {
         __syncthreads();
     }
 
+    // the block's part of a row into L2, all of it at once: a piece ahead, as each_piece loads, is too little for memory's latency
+    __device__ __forceinline__ void bring(const T *z) const
+    {
+        if (threadIdx.x != 0 || !z || pieces == 0) return;
+        const uintptr_t from = ((uintptr_t)(z + (int64_t)first_piece * PIECE) + 15) & ~(uintptr_t)15;
+        const uintptr_t to = (uintptr_t)(z + min((int64_t)(first_piece + pieces) * PIECE, (int64_t)cols)) & ~(uintptr_t)15;
+        if (from < to) asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(from), "r"((unsigned)(to - from)) : "memory");
+    }
+
     // f(the lane's tokens of a piece: z and, where there is one, y) of the warp's pieces; a piece's are loaded before the one before is
     // worked on
     template <typename F>
@@ -353,6 +370,7 @@ struct Walk {
     __device__ __forceinline__ void sums(const Row<T> &p, const Row<T> &q)
     {
         constexpr int N = PIECE / 32;
+        bring(p.z), bring(q.z);
 #pragma unroll 1
         for (int which = 0; which < (q.z ? 2 : 1); ++which) {
             const float m = which ? q.m : p.m, scale = which ? q.scale : p.scale;
@@ -442,6 +460,7 @@ struct Walk {
         constexpr int N = PIECE / 32;
         const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
         int64_t all = 0;                 // on lane 0
+        if (!weight.q.z) bring(weight.p.z);
         each_piece(weight.p.z, weight.q.z, [&](int i, const T (&z)[N], const T (&y)[N]) {
             uint64_t own = 0;
 #pragma unroll
@@ -507,35 +526,45 @@ struct Walk {
     {
         constexpr int N = PIECE / 32, W = THREADS / 32;
         const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+        bring(p.z);
+        if (LESS) bring(q.z);
         // the rows' sums are brought to the same size, as large as the largest term and 62 bits allow: fine units
         const int above_p = above(p), above_q = LESS ? above(q) : above_p, fine = min(min(above_p, above_q), 17);
-        const FastTerm of_p(p.m, p.scale, above_p - fine), of_q(LESS ? q.m : p.m, LESS ? q.scale : p.scale, above_q - fine);
+        // two tokens of p, or one of p and q each
+        const FastTerm term(p.m, p.scale, above_p - fine, LESS ? q.m : p.m, LESS ? q.scale : p.scale, above_q - fine);
         // the terms' probabilities, as the statistics have them
         const float p_inv = __fdiv_rn(__int_as_float((127 + above_p - fine - 22) << 23), p.s);
         const float q_inv = LESS ? __fdiv_rn(__int_as_float((127 + above_q - fine - 22) << 23), q.s) : 0.0f;
         int64_t *const weight_q = sh.weight + pieces;
         int64_t sum_p = 0, sum_q = 0, in_p = 0, in_q = 0;
         float near = 0.0f;
-        each_piece(p.z, LESS ? q.z : nullptr, [&](int i, const T (&z)[N], const T (&y)[N]) {
-            int ph = 0, pl = 0, qh = 0, ql = 0;              // all tokens (LESS)
-            int aph = 0, apl = 0, aqh = 0, aql = 0;          // those that count
-            const int skip = !LESS && without >= 0 ? without - (first_piece + i) * PIECE - lane : -1;
+        each_piece(p.z, LESS ? q.z : nullptr, [&](int i, const T (&raw_z)[N], const T (&raw_y)[N]) {
+            float z[N], y[N];
 #pragma unroll
-            for (int u = 0; u < N; u += 2) {
-                float c[2], d[2];
-                int h[2], l[2], g[2], k[2];
-                of_p(to_float(z[u]), to_float(z[u + 1]), sh.fast_table, c, h, l);
-                if (LESS) of_q(to_float(y[u]), to_float(y[u + 1]), sh.fast_table, d, g, k);
+            for (int u = 0; u < N; ++u) z[u] = to_float(raw_z[u]), y[u] = to_float(raw_y[u]);
+            int ph = -N * HIGH0, pl = -N * LOW0, qh = ph, ql = pl;     // all tokens (LESS)
+            int aph = 0, apl = 0, aqh = 0, aql = 0;                    // those that count
+            if constexpr (LESS) {
 #pragma unroll
-                for (int x = 0; x < 2; ++x) {
-                    if (LESS) {
-                        const float a = __fmul_rn(c[x], p_inv), b = __fmul_rn(d[x], q_inv), over = __fsub_rn(a, b);
-                        ph += h[x] - HIGH0, pl += l[x] - LOW0, qh += g[x] - HIGH0, ql += k[x] - LOW0;
-                        if (fabsf(over) <= __fmul_rn(a, 0x1p-12f)) near = __fadd_rn(near, a);
-                        if (over > 0.0f) aph += h[x] - HIGH0, apl += l[x] - LOW0, aqh += g[x] - HIGH0, aql += k[x] - LOW0;
-                    } else if (skip != (u + x) * 32) {
-                        aph += h[x] - HIGH0, apl += l[x] - LOW0;
-                    }
+                for (int u = 0; u < N; ++u) {
+                    float c[2];
+                    int h[2], l[2];
+                    term(z[u], y[u], sh.fast_table, c, h, l);
+                    ph += h[0], pl += l[0], qh += h[1], ql += l[1];
+                    const float a = __fmul_rn(c[0], p_inv), over = __fmaf_rn(-c[1], q_inv, a);
+                    if (fabsf(over) <= __fmul_rn(a, 0x1p-12f)) near = __fadd_rn(near, a);
+                    if (over > 0.0f) aph += h[0] - HIGH0, apl += l[0] - LOW0, aqh += h[1] - HIGH0, aql += l[1] - LOW0;
+                }
+            } else {
+                const int skip = without >= 0 ? without - (first_piece + i) * PIECE - lane : -1;
+#pragma unroll
+                for (int u = 0; u < N; u += 2) {
+                    float c[2];
+                    int h[2], l[2];
+                    term(z[u], z[u + 1], sh.fast_table, c, h, l);
+#pragma unroll
+                    for (int x = 0; x < 2; ++x)
+                        if (skip != (u + x) * 32) aph += h[x] - HIGH0, apl += l[x] - LOW0;
                 }
             }
             if (LESS) sum_p += units(ph, pl), sum_q += units(qh, ql);
@@ -631,18 +660,14 @@ struct Walk {
                 lane_tokens(LESS ? q.z : nullptr, j0, y);
                 int64_t wp[N], wq[N], sum_p = 0, sum_q = 0;
 #pragma unroll
-                for (int u = 0; u < N; u += 2) {
-                    float c[2], d[2];
-                    int h[2], l[2], g[2], k[2];
-                    of_p(to_float(z[u]), to_float(z[u + 1]), sh.fast_table, c, h, l);
-                    if (LESS) of_q(to_float(y[u]), to_float(y[u + 1]), sh.fast_table, d, g, k);
-#pragma unroll
-                    for (int x = 0; x < 2; ++x) {
-                        const bool counts = LESS ? __fsub_rn(__fmul_rn(c[x], p_inv), __fmul_rn(d[x], q_inv)) > 0.0f : j0 + u + x != without;
-                        wp[u + x] = counts ? units(h[x] - HIGH0, l[x] - LOW0) : 0;
-                        wq[u + x] = LESS && counts ? units(g[x] - HIGH0, k[x] - LOW0) : 0;
-                        sum_p += wp[u + x], sum_q += wq[u + x];
-                    }
+                for (int u = 0; u < N; ++u) {
+                    float c[2];
+                    int h[2], l[2];
+                    term(to_float(z[u]), to_float(LESS ? y[u] : z[u]), sh.fast_table, c, h, l);
+                    const bool counts = LESS ? __fmaf_rn(-c[1], q_inv, __fmul_rn(c[0], p_inv)) > 0.0f : j0 + u != without;
+                    wp[u] = counts ? units(h[0] - HIGH0, l[0] - LOW0) : 0;
+                    wq[u] = LESS && counts ? units(h[1] - HIGH0, l[1] - LOW0) : 0;
+                    sum_p += wp[u], sum_q += wq[u];
                 }
                 P = sh.low_p + scan(sum_p) - sum_p, Q = LESS ? sh.low_q + scan(sum_q) - sum_q : 0;
 #pragma unroll
@@ -679,39 +704,13 @@ struct Given {
     float m, s, z, unused;
 };
 
-// Few sequences: the statistics of all their rows at once, a cluster for each.
-template <typename T, int THREADS>
-__global__ __launch_bounds__(THREADS, 1024 / THREADS) void k_verify_rows(const T *target, int64_t t_stride, const T *draft,
-                                                                         int64_t d_stride, int cols, Ids ids, int64_t targets, int D,
-                                                                         float scale, float draft_scale, Given *__restrict__ given)
-{
-    after_previous();
-    let_next_start();
-    __shared__ Shared sh;
-    cg::cluster_group cluster = cg::this_cluster();
-    const int blocks = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
-    const int64_t r = blockIdx.x / (unsigned)blocks;
-    const bool drafts = r >= targets;
-    const int64_t i = drafts ? r - targets : r, s = i / (drafts ? D : D + 1);
-    const int d = (int)(i - s * (drafts ? D : D + 1));
-    const T *row = drafts ? draft + i * d_stride : target + i * t_stride;
-    const bool writes = rank == 0 && threadIdx.x == 0;
-    float z = 0.0f;
-    if (writes && d < D) {
-        const int64_t t = load_id(ids, s, d);
-        if (t >= 0 && t < cols) z = to_float(row[t]);
-    }
-    Walk<T, THREADS> walk{sh, cluster, rank, blocks, cols, 0, 0};
-    walk.stats(1, [&](int) { return row; }, [&](int) { return __fmul_rn(drafts ? draft_scale : scale, LOG2E); }, 0);
-    cluster.sync();                      // the others have read this block's statistics
-    if (writes) given[r] = {sh.joined[0][0], sh.joined[0][1], z, 0.0f};
-}
-
-// where a sequence's walk has come to: the first position that is not surely accepted, its rows' statistics and logits
+// Where a sequence's walk has come to: its position, what is to be done there, the rows' statistics and their logits of the drafted token.
+enum { DRAW_REST = 0, DRAW_TARGET = 1, NOTHING = 2, LATER = 3 };       // from p - q; from p; a target row without a distribution; exactly
 struct Start {
     float m, s, z, qm, qs, qz;
-    int a, unused;
+    int a, what;
 };
+static_assert(sizeof(Start) == 2 * sizeof(float4), "VERIFY_SEQUENCES of them in the handle");
 
 // whether u q < p, where the statistics can tell it (sure)
 template <typename T>
@@ -725,79 +724,26 @@ __device__ __forceinline__ bool accepts(const Row<T> &p, const Row<T> &q, float 
     return left < right;
 }
 
-// Many sequences: their walks, a cluster for each, up to the first position that k_verify has to look at.  Bound by memory, so with as many
-// threads as an SM holds; the draws' numbers want registers instead (both in one kernel: 256 x 5 drafts x 128,000 bf16 228 us).
-template <typename T, int THREADS>
-__global__ __launch_bounds__(THREADS, 1024 / THREADS) void k_verify_walk(const T *target, int64_t t_stride, const T *draft,
-                                                                         int64_t d_stride, int cols, Ids ids, int D, float scale,
-                                                                         float draft_scale, const float *accept_u, VerifyOut out,
-                                                                         Start *__restrict__ start)
+// what a position with its statistics comes to; -1 where its draft is surely accepted
+template <typename T>
+__device__ __forceinline__ int decide(const Row<T> &p, const Row<T> &q, int t, float z, float zq, float u)
 {
-    after_previous();
-    let_next_start();
-    __shared__ Shared sh;
-    cg::cluster_group cluster = cg::this_cluster();
-    const int blocks = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
-    const int64_t s = blockIdx.x / (unsigned)blocks, base = s * (D + 1);
-    for (int d = threadIdx.x; d < D; d += THREADS) {
-        const int64_t t = load_id(ids, s, d);
-        sh.drafted[d] = t >= 0 && t < cols ? (int)t : -1;
-        sh.u[d] = accept_u[s * D + d];
-    }
-    __syncthreads();
-    Walk<T, THREADS> walk{sh, cluster, rank, blocks, cols, 0, 0};
-    const bool writes = rank == 0 && threadIdx.x == 0;
-    const float c = __fmul_rn(scale, LOG2E), cq = __fmul_rn(draft_scale, LOG2E);
-    Row<T> p{}, q{};
-    p.scale = scale, q.scale = draft_scale;
-    float z = 0.0f, zq = 0.0f;
-    int a = 0;
-#pragma unroll 1
-    for (;; ++a) {
-        const int t = a < D ? sh.drafted[a] : -1;
-        p.z = target + (base + a) * t_stride;
-        q.z = t >= 0 && draft ? draft + (s * D + a) * d_stride : nullptr;
-        if (t >= 0 && threadIdx.x < (q.z ? 2 : 1)) sh.z[threadIdx.x] = to_float((threadIdx.x ? q.z : p.z)[t]);
-        walk.stats(q.z ? 2 : 1, [&](int i) { return i ? q.z : p.z; }, [&](int i) { return i ? cq : c; }, a & 1);
-        p.m = sh.joined[0][0], p.s = sh.joined[0][1], z = sh.z[0];
-        if (q.z) q.m = sh.joined[1][0], q.s = sh.joined[1][1], zq = sh.z[1];
-        if (t < 0 || !p.valid() || (q.z && !q.valid())) break;
-        bool sure;
-        if (!accepts(p, q, z, zq, sh.u[a], sure) || !sure) break;
-        if (writes) {
-            out.tokens[base + a] = t;
-            if (out.logp) out.logp[base + a] = __fmaf_rn(__fsub_rn(z, p.m), scale, -logf(p.s));
-        }
-        __syncthreads();                 // before the next position's
-    }
-    if (writes) start[s] = {p.m, p.s, z, q.m, q.s, zq, a, 0};
-    cluster.sync();                      // the others have read this block's statistics
+    if (!p.valid()) return NOTHING;
+    if (t < 0 || (q.z && !q.valid())) return DRAW_TARGET;            // the drafts end here
+    bool sure;
+    const bool good = accepts(p, q, z, zq, u, sure);
+    return !sure ? LATER : good ? -1 : DRAW_REST;
 }
 
-template <typename T, int THREADS>
-__global__ __launch_bounds__(THREADS, THREADS == 512 ? 1 : 2) void k_verify(const T *target, int64_t t_stride, const T *draft,
-                                                                    int64_t d_stride, int cols, Ids ids, int64_t n, int D,
-                                                                    float scale, float draft_scale, const float *accept_u,
-                                                                    const float *draw_u, const Given *given, const Start *start,
-                                                                    VerifyOut out, int *status)
+// a sequence's drafted tokens (-1 from the end on) and random numbers; an id out of range is recorded where no id before it ends the drafts
+template <int THREADS>
+__device__ __forceinline__ void load_drafts(Shared &sh, Ids ids, int64_t s, int D, int cols, const float *accept_u, bool records, int *status)
 {
-    after_previous();
-    extern __shared__ __align__(16) unsigned char s_raw[];
-    Shared &sh = *reinterpret_cast<Shared *>(s_raw);
-    cg::cluster_group cluster = cg::this_cluster();
-    const int blocks = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
-    const int64_t s = blockIdx.x / (unsigned)blocks;
-    const int all = (cols + PIECE - 1) / PIECE;
-    const int p0 = (int)((int64_t)all * rank / blocks), p1 = (int)((int64_t)all * (rank + 1) / blocks);
-    Walk<T, THREADS> walk{sh, cluster, rank, blocks, cols, p0, p1 - p0};
-    const bool writes = rank == 0 && threadIdx.x == 0;
-    const int64_t base = s * (D + 1);
     for (int d = threadIdx.x; d < D; d += THREADS) {
         const int64_t t = load_id(ids, s, d);
         sh.drafted[d] = t >= 0 && t < cols ? (int)t : -1;
         sh.u[d] = accept_u[s * D + d];
-        // recorded where no id before it ends the drafts
-        if (t >= cols && rank == 0) {
+        if (t >= cols && records) {
             bool seen = true;
             for (int e = 0; e < d; ++e) {
                 const int64_t before = load_id(ids, s, e);
@@ -806,112 +752,279 @@ __global__ __launch_bounds__(THREADS, THREADS == 512 ? 1 : 2) void k_verify(cons
             if (seen) set_status(status, PDB_ERANGE);
         }
     }
-    for (int i = threadIdx.x; i < STEPS; i += THREADS) sh.fast_table[i] = {FAST_TABLE.hi[i], FAST_TABLE.lo[i]};
-    const float v = draw_u[s];
-    __syncthreads();
+}
 
+// where a call's matrices and vectors lie
+template <typename T>
+struct Verify {
+    const T *target, *draft;
+    int64_t t_stride, d_stride;
+    int cols, D;
+    Ids ids;
+    int64_t n;
+    float scale, draft_scale;
+    const float *accept_u, *draw_u;
+    VerifyOut out;
+    const Given *given;                 // of all rows, or
+    Start *start;                       // of each sequence
+    int *status;
+    __device__ __forceinline__ const T *target_row(int64_t s, int a) const { return target + (s * (D + 1) + a) * t_stride; }
+    __device__ __forceinline__ const T *draft_row(int64_t s, int a) const { return draft + (s * D + a) * d_stride; }
+    __device__ __forceinline__ void accept(int64_t s, int a, int t, float z, const Row<T> &p) const
+    {
+        out.tokens[s * (D + 1) + a] = t;
+        if (out.logp) out.logp[s * (D + 1) + a] = __fmaf_rn(__fsub_rn(z, p.m), scale, -logf(p.s));
+    }
+    // a sequence's outputs behind its accepted drafts, but for the drawn token
+    __device__ __forceinline__ void finish(int64_t s, int a, bool drawn) const
+    {
+        if (out.accepted) out.accepted[s] = a;
+        for (int d = drawn ? a + 1 : a; d <= D; ++d) {
+            out.tokens[s * (D + 1) + d] = -1;
+            if (out.logp) out.logp[s * (D + 1) + d] = 0.0f;
+        }
+    }
+    // a position's statistics as k_verify_rows left them
+    __device__ __forceinline__ void look_up(int64_t s, int a, Row<T> &p, Row<T> &q, float &z, float &zq) const
+    {
+        const Given g = given[s * (D + 1) + a];
+        p.m = g.m, p.s = g.s, z = g.z;
+        if (q.z) {
+            const Given h = given[n * (D + 1) + s * D + a];
+            q.m = h.m, q.s = h.s, zq = h.z;
+        }
+    }
+};
+
+// Few sequences: the statistics of all their rows at once, a cluster for each.
+template <typename T, int THREADS>
+__global__ __launch_bounds__(THREADS, 1024 / THREADS) void k_verify_rows(Verify<T> v, Given *__restrict__ given)
+{
+    after_previous();
+    let_next_start();
+    __shared__ Shared sh;
+    cg::cluster_group cluster = cg::this_cluster();
+    const int blocks = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
+    const int64_t r = blockIdx.x / (unsigned)blocks, targets = v.n * (v.D + 1);
+    const bool drafts = r >= targets;
+    const int each = drafts ? v.D : v.D + 1;
+    const int64_t i = drafts ? r - targets : r, s = i / each;
+    const int d = (int)(i - s * each);
+    const T *row = drafts ? v.draft_row(s, d) : v.target_row(s, d);
+    const bool writes = rank == 0 && threadIdx.x == 0;
+    float z = 0.0f;
+    if (writes && d < v.D) {
+        const int64_t t = load_id(v.ids, s, d);
+        if (t >= 0 && t < v.cols) z = to_float(row[t]);
+    }
+    Walk<T, THREADS> walk{sh, cluster, rank, blocks, v.cols, 0, 0};
+    walk.stats(1, [&](int) { return row; }, [&](int) { return __fmul_rn(drafts ? v.draft_scale : v.scale, LOG2E); }, 0);
+    cluster.sync();                      // the others have read this block's statistics
+    if (writes) given[r] = {sh.joined[0][0], sh.joined[0][1], z, 0.0f};
+}
+
+// Many sequences: their walks, a cluster for each, up to the first position that is not surely accepted.  Bound by memory, so with as many
+// threads as an SM holds; the draws' numbers want registers instead (both in one kernel: 256 x 5 drafts x 128,000 bf16 228 us).
+template <typename T, int THREADS>
+__global__ __launch_bounds__(THREADS, 1024 / THREADS) void k_verify_walk(Verify<T> v)
+{
+    after_previous();
+    let_next_start();
+    __shared__ Shared sh;
+    cg::cluster_group cluster = cg::this_cluster();
+    const int blocks = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
+    const int64_t s = blockIdx.x / (unsigned)blocks;
+    load_drafts<THREADS>(sh, v.ids, s, v.D, v.cols, v.accept_u, rank == 0, v.status);
+    __syncthreads();
+    Walk<T, THREADS> walk{sh, cluster, rank, blocks, v.cols, 0, 0};
+    const bool writes = rank == 0 && threadIdx.x == 0;
+    const float c = __fmul_rn(v.scale, LOG2E), cq = __fmul_rn(v.draft_scale, LOG2E);
     Row<T> p{}, q{};
-    p.scale = scale, q.scale = draft_scale;
-    const float c = __fmul_rn(scale, LOG2E), cq = __fmul_rn(draft_scale, LOG2E);
-    const int begin = start ? start[s].a : 0;
-    int a = begin;                       // the position
-    bool refused = false, exact = false;
-    int t = -1;
-    float log_s = 0.0f;
+    p.scale = v.scale, q.scale = v.draft_scale;
+    float z = 0.0f, zq = 0.0f;
+    int a = 0, what;
 #pragma unroll 1
     for (;; ++a) {
-        t = a < D ? sh.drafted[a] : -1;
-        p.z = target + (base + a) * t_stride;
-        q.z = t >= 0 && draft ? draft + (s * D + a) * d_stride : nullptr;
-        float z = 0.0f, zq = 0.0f;
-        if (given) {
-            const Given g = given[base + a];
-            p.m = g.m, p.s = g.s, z = g.z;
-            if (q.z) {
-                const Given h = given[n * (D + 1) + s * D + a];
-                q.m = h.m, q.s = h.s, zq = h.z;
-            }
-        } else if (start && a == begin) {
-            const Start g = start[s];
-            p.m = g.m, p.s = g.s, z = g.z, q.m = g.qm, q.s = g.qs, zq = g.qz;
-        } else {
-            if (t >= 0 && threadIdx.x < (q.z ? 2 : 1)) sh.z[threadIdx.x] = to_float((threadIdx.x ? q.z : p.z)[t]);
-            walk.stats(q.z ? 2 : 1, [&](int i) { return i ? q.z : p.z; }, [&](int i) { return i ? cq : c; }, a & 1);
-            p.m = sh.joined[0][0], p.s = sh.joined[0][1], z = sh.z[0];
-            if (q.z) q.m = sh.joined[1][0], q.s = sh.joined[1][1], zq = sh.z[1];
-            __syncthreads();             // before the next position's
-        }
-        if (!p.valid()) break;
-        log_s = logf(p.s);
-        if (q.z && !q.valid()) t = -1, q.z = nullptr;     // the drafts end here
-        if (t < 0) break;
-        const float u = sh.u[a];
-        bool sure, good = accepts(p, q, z, zq, u, sure);
-        if (!sure) {
-            if (!exact) walk.fill_table();
-            exact = true;
-            walk.sums(p, q);
-            if (threadIdx.x == 0) {
-                const auto in_64 = [](float scale, float z, const Row<T> &r, Two sum) {
-                    return exp((double)scale * ((double)z - (double)r.m)) / ((double)sum.hi + (double)sum.lo);
-                };
-                const double pe = in_64(scale, z, p, sh.row_sum[0]);
-                const double qe = q.z ? in_64(draft_scale, zq, q, sh.row_sum[1]) : 1.0;
-                sh.good = (double)u * qe < pe;
-            }
-            __syncthreads();
-            good = sh.good;
-        }
-        if (!good) {
-            refused = true;
-            break;
-        }
-        if (writes) {
-            out.tokens[base + a] = t;
-            if (out.logp) out.logp[base + a] = __fmaf_rn(__fsub_rn(z, p.m), scale, -log_s);
-        }
+        const int t = a < v.D ? sh.drafted[a] : -1;
+        p.z = v.target_row(s, a);
+        q.z = t >= 0 && v.draft ? v.draft_row(s, a) : nullptr;
+        if (t >= 0 && threadIdx.x < (q.z ? 2 : 1)) sh.z[threadIdx.x] = to_float((threadIdx.x ? q.z : p.z)[t]);
+        walk.stats(q.z ? 2 : 1, [&](int i) { return i ? q.z : p.z; }, [&](int i) { return i ? cq : c; }, a & 1);
+        p.m = sh.joined[0][0], p.s = sh.joined[0][1], z = sh.z[0];
+        if (q.z) q.m = sh.joined[1][0], q.s = sh.joined[1][1], zq = sh.z[1];
+        what = decide(p, q, t, z, zq, t >= 0 ? sh.u[a] : 0.0f);
+        if (what >= 0) break;
+        if (writes) v.accept(s, a, t, z, p);
+        __syncthreads();                 // before the next position's
     }
-    bool none = true;
-    if (p.valid()) {
-        if (!refused) q.z = nullptr;
-        int without = refused && !q.z ? t : -1;
-        const auto reach = [](const Row<T> &r) { return r.scale > 1e-30f && fabsf(__fmul_rn(r.m, __fmul_rn(r.scale, LOG2E))) < REACH; };
-        bool fast = !exact && reach(p) && (!q.z || reach(q)), filled = exact;
+    if (writes) v.start[s] = {p.m, p.s, z, q.m, q.s, zq, a, what};
+    cluster.sync();                      // the others have read this block's statistics
+}
+
+// |m scale| log2(e) within what FastTerm takes
+template <typename T>
+__device__ __forceinline__ bool in_reach(const Row<T> &r)
+{
+    return r.scale > 1e-30f && fabsf(__fmul_rn(r.m, __fmul_rn(r.scale, LOG2E))) < REACH;
+}
+
+// Their draws; what FastTerm cannot tell is left to k_verify, whose larger clusters have it done sooner (here its few sequences, 2 of 256,
+// would be all that still runs at the end, 65 us of 228).
+template <typename T, int THREADS>
+__global__ __launch_bounds__(THREADS, 2) void k_verify_draw(Verify<T> v)
+{
+    after_previous();
+    let_next_start();
+    extern __shared__ __align__(16) unsigned char s_raw[];
+    Shared &sh = *reinterpret_cast<Shared *>(s_raw);
+    cg::cluster_group cluster = cg::this_cluster();
+    const int blocks = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
+    const int64_t s = blockIdx.x / (unsigned)blocks;
+    const int all = (v.cols + PIECE - 1) / PIECE;
+    const int p0 = (int)((int64_t)all * rank / blocks), p1 = (int)((int64_t)all * (rank + 1) / blocks);
+    Walk<T, THREADS> walk{sh, cluster, rank, blocks, v.cols, p0, p1 - p0};
+    const bool writes = rank == 0 && threadIdx.x == 0;
+    for (int i = threadIdx.x; i < STEPS; i += THREADS) sh.fast_table[i] = {FAST_TABLE.hi[i], FAST_TABLE.lo[i]};
+    const float draw_u = v.draw_u[s];
+    if (v.given) load_drafts<THREADS>(sh, v.ids, s, v.D, v.cols, v.accept_u, rank == 0, v.status);
+    __syncthreads();
+    Row<T> p{}, q{};
+    p.scale = v.scale, q.scale = v.draft_scale;
+    float z = 0.0f, zq = 0.0f;
+    int a = 0, what, t = -1;
+    if (v.given) {
 #pragma unroll 1
-        for (;;) {
-            float z = 0.0f;
-            int drawn;
-            if (fast) {
-                drawn = q.z ? walk.template fast_draw<true>(p, q, -1, v, z) : walk.template fast_draw<false>(p, q, without, v, z);
-            } else {
-                if (!filled) walk.fill_table();
-                filled = true;
-                if (q.z) walk.sums(p, q);
-                // one row's weights need no more than a common factor, a power of two
-                const Two unit = {__int_as_float((127 - walk.above(p)) << 23), 0.0f};
-                drawn = walk.draw({p, q, q.z ? sh.row_inv[0] : unit, sh.row_inv[1], without, sh.table}, v, z);
-            }
-            const bool unsure = fast && sh.unsure;
-            none = !fast && sh.none;
-            if (drawn >= 0) {
-                out.tokens[base + a] = drawn;
-                if (out.logp) out.logp[base + a] = __fmaf_rn(__fsub_rn(z, p.m), scale, -log_s);
-            }
-            if (!unsure && (!none || !refused)) break;
-            // once more, exactly; or, with nothing of p - q that 2^-46 could tell, from p
-            if (!unsure) refused = false, q.z = nullptr, without = -1;
-            fast = false;
-            __syncthreads();
+        for (;; ++a) {
+            t = a < v.D ? sh.drafted[a] : -1;
+            q.z = t >= 0 && v.draft ? v.draft_row(s, a) : nullptr;
+            v.look_up(s, a, p, q, z, zq);
+            what = decide(p, q, t, z, zq, t >= 0 ? sh.u[a] : 0.0f);
+            if (what >= 0) break;
+            if (writes) v.accept(s, a, t, z, p);
         }
     } else {
-        cluster.sync();                  // the others have read this block's statistics
+        const Start g = v.start[s];
+        p.m = g.m, p.s = g.s, z = g.z, q.m = g.qm, q.s = g.qs, zq = g.qz, a = g.a, what = g.what;
+        if (a < v.D && what == DRAW_REST) t = (int)load_id(v.ids, s, a);
     }
+    p.z = v.target_row(s, a);
+    q.z = what == DRAW_REST && v.draft ? v.draft_row(s, a) : nullptr;
+    int drawn = -1;
+    float logit = 0.0f;
+    if (what <= DRAW_TARGET && !(in_reach(p) && (!q.z || in_reach(q)))) what = LATER;
+    if (what <= DRAW_TARGET) {
+        drawn = q.z ? walk.template fast_draw<true>(p, q, -1, draw_u, logit)
+                    : walk.template fast_draw<false>(p, q, what == DRAW_REST ? t : -1, draw_u, logit);
+        if (sh.unsure) what = LATER;
+    }
+    if (drawn >= 0) v.accept(s, a, drawn, logit, p);
     if (writes) {
-        if (out.accepted) out.accepted[s] = a;
-        for (int d = none ? a : a + 1; d <= D; ++d) {
-            out.tokens[base + d] = -1;
-            if (out.logp) out.logp[base + d] = 0.0f;
+        if (what == LATER || v.given) v.start[s] = {p.m, p.s, z, q.m, q.s, zq, a, what};
+        if (what != LATER) v.finish(s, a, what != NOTHING);
+    }
+}
+
+// All of a sequence, exactly where that is needed: few sequences, a cluster for each, or with `later` those that the draws left, the clusters
+// taking them in turn.
+template <typename T, int THREADS>
+__global__ __launch_bounds__(THREADS, 1) void k_verify(Verify<T> v, bool later)
+{
+    after_previous();
+    extern __shared__ __align__(16) unsigned char s_raw[];
+    Shared &sh = *reinterpret_cast<Shared *>(s_raw);
+    cg::cluster_group cluster = cg::this_cluster();
+    const int blocks = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
+    const int all = (v.cols + PIECE - 1) / PIECE;
+    const int p0 = (int)((int64_t)all * rank / blocks), p1 = (int)((int64_t)all * (rank + 1) / blocks);
+    Walk<T, THREADS> walk{sh, cluster, rank, blocks, v.cols, p0, p1 - p0};
+    const bool writes = rank == 0 && threadIdx.x == 0;
+    const float c = __fmul_rn(v.scale, LOG2E), cq = __fmul_rn(v.draft_scale, LOG2E);
+    bool filled = false;                 // the exact terms' table
+#pragma unroll 1
+    for (int64_t s = blockIdx.x / (unsigned)blocks; s < v.n; s += gridDim.x / (unsigned)blocks) {
+        if (later && v.start[s].what != LATER) continue;
+        load_drafts<THREADS>(sh, v.ids, s, v.D, v.cols, v.accept_u, rank == 0 && !later, v.status);
+        if (!later)
+            for (int i = threadIdx.x; i < STEPS; i += THREADS) sh.fast_table[i] = {FAST_TABLE.hi[i], FAST_TABLE.lo[i]};
+        const float draw_u = v.draw_u[s];
+        __syncthreads();
+        Row<T> p{}, q{};
+        p.scale = v.scale, q.scale = v.draft_scale;
+        const int begin = later ? v.start[s].a : 0;
+        int a = begin, t = -1;           // the position, its drafted token
+        bool refused = false, exact = later;
+#pragma unroll 1
+        for (;; ++a) {
+            t = a < v.D ? sh.drafted[a] : -1;
+            p.z = v.target_row(s, a);
+            q.z = t >= 0 && v.draft ? v.draft_row(s, a) : nullptr;
+            float z = 0.0f, zq = 0.0f;
+            if (later && a == begin) {
+                const Start g = v.start[s];
+                p.m = g.m, p.s = g.s, z = g.z, q.m = g.qm, q.s = g.qs, zq = g.qz;
+            } else if (v.given) {
+                v.look_up(s, a, p, q, z, zq);
+            } else {
+                if (t >= 0 && threadIdx.x < (q.z ? 2 : 1)) sh.z[threadIdx.x] = to_float((threadIdx.x ? q.z : p.z)[t]);
+                walk.stats(q.z ? 2 : 1, [&](int i) { return i ? q.z : p.z; }, [&](int i) { return i ? cq : c; }, a & 1);
+                p.m = sh.joined[0][0], p.s = sh.joined[0][1], z = sh.z[0];
+                if (q.z) q.m = sh.joined[1][0], q.s = sh.joined[1][1], zq = sh.z[1];
+                __syncthreads();         // before the next position's
+            }
+            const float u = t >= 0 ? sh.u[a] : 0.0f;
+            int what = decide(p, q, t, z, zq, u);
+            if (what == LATER) {
+                if (!filled) walk.fill_table();
+                filled = exact = true;
+                walk.sums(p, q);
+                if (threadIdx.x == 0) {
+                    const auto in_64 = [](float scale, float z, const Row<T> &r, Two sum) {
+                        return exp((double)scale * ((double)z - (double)r.m)) / ((double)sum.hi + (double)sum.lo);
+                    };
+                    const double pe = in_64(v.scale, z, p, sh.row_sum[0]);
+                    const double qe = q.z ? in_64(v.draft_scale, zq, q, sh.row_sum[1]) : 1.0;
+                    sh.good = (double)u * qe < pe;
+                }
+                __syncthreads();
+                what = sh.good ? -1 : DRAW_REST;
+            }
+            if (what >= 0) {
+                refused = what == DRAW_REST;
+                break;
+            }
+            if (writes) v.accept(s, a, t, z, p);
         }
+        bool none = true;
+        if (p.valid()) {
+            if (!refused) q.z = nullptr;
+            int without = refused && !q.z ? t : -1;
+            bool fast = !exact && in_reach(p) && (!q.z || in_reach(q));
+#pragma unroll 1
+            for (;;) {
+                float z = 0.0f;
+                int drawn;
+                if (fast) {
+                    drawn = q.z ? walk.template fast_draw<true>(p, q, -1, draw_u, z) : walk.template fast_draw<false>(p, q, without, draw_u, z);
+                } else {
+                    if (!filled) walk.fill_table();
+                    filled = true;
+                    if (q.z) walk.sums(p, q);
+                    // one row's weights need no more than a common factor, a power of two
+                    const Two unit = {__int_as_float((127 - walk.above(p)) << 23), 0.0f};
+                    drawn = walk.draw({p, q, q.z ? sh.row_inv[0] : unit, sh.row_inv[1], without, sh.table}, draw_u, z);
+                }
+                const bool unsure = fast && sh.unsure;
+                none = !fast && sh.none;
+                if (drawn >= 0) v.accept(s, a, drawn, z, p);
+                if (!unsure && (!none || !refused)) break;
+                // once more, exactly; or, with nothing of p - q that 2^-46 could tell, from p
+                if (!unsure) refused = false, q.z = nullptr, without = -1;
+                fast = false;
+                __syncthreads();
+            }
+        }
+        if (writes) v.finish(s, a, !none);
+        cluster.sync();                  // before the next sequence, or the end: the others have read this block's numbers
     }
 }
 
@@ -951,40 +1064,46 @@ int pdb_verify(pdb_tokens *t, const pdb_mat *target, const pdb_ids *draft_ids, i
     TokensUse use{t, s};
     return with_type(target->type, [&](auto *a) {
         using T = std::remove_pointer_t<decltype(a)>;
-        const int64_t nv = target->cols / Vec<T>::E + 1, rows = target->rows + (draft ? drafts : 0);
-        const bool few = n * MAX_CLUSTER <= t->sms, ahead = n * 2 <= t->sms && rows <= VERIFY_ROWS && n_drafts > 0;
-        Shape shape = {};
-        shape.threads = few ? 512 : 256;
-        shape.blocks = cluster_of(n, nv, shape.threads, [&](int blocks) { return t->sms * (few ? 2 : 8) / blocks; });
-        shape.clusters = n;
-        const Shape walk = shape;
-        shape.smem = verify_smem(target->cols, shape.blocks);
-        const Ids id = n_drafts > 0 ? ids_of(draft_ids) : Ids{};
-        const T *z = (const T *)target->data, *y = draft ? (const T *)draft->data : nullptr;
-        const int64_t z_step = stride_of(target), y_step = draft ? stride_of(draft) : 0;
-        Given *given = ahead ? (Given *)t->given : nullptr;
-        if (ahead) {
-            Shape each = {};
-            each.threads = 512;
-            each.blocks = cluster_of(rows, nv, each.threads, [&](int blocks) { return t->sms * 2 / blocks; });
-            each.clusters = rows;
-            const int rc = launch_rows(k_verify_rows<T, 512>, each, s, z, z_step, y, y_step, (int)target->cols, id, target->rows,
-                                       (int)n_drafts, scale, draft_scale, given);
-            if (rc != PDB_OK) return rc;
-        }
-        Start *start = nullptr;
-        if (!few && !ahead && n_drafts > 0 && n <= VERIFY_ROWS / 2) {
-            start = (Start *)t->given;
-            const int rc = launch_rows(k_verify_walk<T, 256>, walk, s, z, z_step, y, y_step, (int)target->cols, id, (int)n_drafts, scale,
-                                       draft_scale, accept_u, VerifyOut{tokens, accepted, logp}, start);
-            if (rc != PDB_OK) return rc;
-        }
-        const auto run = [&](auto k) {
-            return launch_rows(k_verify<T, decltype(k)::value>, shape, s, z, z_step, y, y_step, (int)target->cols, id, n,
-                               (int)n_drafts, scale, draft_scale, accept_u, draw_u, (const Given *)given, (const Start *)start,
-                               VerifyOut{tokens, accepted, logp}, t->status);
+        const int64_t nv = target->cols / Vec<T>::E + 1;
+        const auto shaped = [&](int64_t rows, int threads, int per_sm, int64_t clusters, bool draws) {
+            Shape shape = {};
+            shape.threads = threads;
+            shape.blocks = cluster_of(rows, nv, threads, [&](int blocks) { return (int64_t)t->sms * per_sm / blocks; });
+            shape.clusters = clusters;
+            shape.smem = draws ? verify_smem(target->cols, shape.blocks) : 0;
+            return shape;
         };
-        return few ? run(Num<512>()) : run(Num<256>());
+        Verify<T> v = {};
+        v.target = (const T *)target->data, v.t_stride = stride_of(target);
+        if (draft) v.draft = (const T *)draft->data, v.d_stride = stride_of(draft);
+        v.cols = (int)target->cols, v.D = (int)n_drafts, v.n = n;
+        if (n_drafts > 0) v.ids = ids_of(draft_ids);
+        v.scale = scale, v.draft_scale = draft_scale, v.accept_u = accept_u, v.draw_u = draw_u;
+        v.out = {tokens, accepted, logp}, v.start = (Start *)(t->given + VERIFY_ROWS), v.status = t->status;
+        // the statistics of all rows at once where the SMs would not be busy with a position of each sequence: a launch more, fewer rounds
+        const int64_t rows = target->rows + (draft ? drafts : 0);
+        if (n_drafts > 0 && n * 2 <= t->sms && rows <= VERIFY_ROWS) {
+            v.given = (const Given *)t->given;
+            const int rc = launch_rows(k_verify_rows<T, 512>, shaped(rows, 512, 2, rows, false), s, v, (Given *)t->given);
+            if (rc != PDB_OK) return rc;
+        }
+        if (n * MAX_CLUSTER <= t->sms) return launch_rows(k_verify<T, 512>, shaped(n, 512, 2, n, true), s, v, false);
+        // sequences by as many as the handle has places for
+        for (int64_t first = 0; first < n; first += VERIFY_SEQUENCES) {
+            Verify<T> w = v;
+            w.n = std::min(VERIFY_SEQUENCES, n - first);
+            w.target += first * (n_drafts + 1) * v.t_stride;
+            if (draft) w.draft += first * n_drafts * v.d_stride;
+            w.ids.data = (const char *)v.ids.data + first * v.ids.stride * (v.ids.wide ? 8 : 4);
+            w.accept_u += first * n_drafts, w.draw_u += first, w.out.tokens += first * (n_drafts + 1);
+            if (accepted) w.out.accepted += first;
+            if (logp) w.out.logp += first * (n_drafts + 1);
+            int rc = v.given ? (int)PDB_OK : launch_rows(k_verify_walk<T, 256>, shaped(w.n, 256, 8, w.n, false), s, w);
+            rc = rc ? rc : launch_rows(k_verify_draw<T, 256>, shaped(w.n, 256, 8, w.n, true), s, w);
+            rc = rc ? rc : launch_rows(k_verify<T, 512>, shaped(1, 512, 2, std::min<int64_t>(w.n, std::max(1, t->sms / MAX_CLUSTER)), true), s, w, true);
+            if (rc != PDB_OK) return rc;
+        }
+        return (int)PDB_OK;
     });
 }
 
