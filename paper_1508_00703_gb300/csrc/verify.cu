@@ -868,10 +868,14 @@ __device__ __forceinline__ bool in_reach(const Row<T> &r)
     return r.scale > 1e-30f && fabsf(__fmul_rn(r.m, __fmul_rn(r.scale, LOG2E))) < REACH;
 }
 
-// Their draws; what FastTerm cannot tell is left to k_verify, whose larger clusters have it done sooner (here its few sequences, 2 of 256,
-// would be all that still runs at the end, 65 us of 228).
+// Many sequences, a cluster for each: its walk (bound by memory) up to the first position that is not surely accepted, and its draw (bound
+// by instructions); on an SM some sequences walk while others draw (in two kernels, 256 x 5 drafts x 128,000 bf16: 115 us and 100, together
+// WALKDRAW).  What FastTerm cannot tell is left to k_verify, whose larger clusters have it done sooner: two of 256 sequences, which
+// would be all that still runs at the end.
+constexpr int MANY_THREADS = 256, MANY_PER_SM = 3;
+
 template <typename T, int THREADS>
-__global__ __launch_bounds__(THREADS, 2) void k_verify_draw(Verify<T> v)
+__global__ __launch_bounds__(THREADS, MANY_PER_SM) void k_verify_many(Verify<T> v)
 {
     after_previous();
     let_next_start();
@@ -884,42 +888,47 @@ __global__ __launch_bounds__(THREADS, 2) void k_verify_draw(Verify<T> v)
     const int p0 = (int)((int64_t)all * rank / blocks), p1 = (int)((int64_t)all * (rank + 1) / blocks);
     Walk<T, THREADS> walk{sh, cluster, rank, blocks, v.cols, p0, p1 - p0};
     const bool writes = rank == 0 && threadIdx.x == 0;
+    load_drafts<THREADS>(sh, v.ids, s, v.D, v.cols, v.accept_u, rank == 0, v.status);
     for (int i = threadIdx.x; i < STEPS; i += THREADS) sh.fast_table[i] = {FAST_TABLE.hi[i], FAST_TABLE.lo[i]};
-    const float draw_u = v.draw_u[s];
-    if (v.given) load_drafts<THREADS>(sh, v.ids, s, v.D, v.cols, v.accept_u, rank == 0, v.status);
     __syncthreads();
+    const float c = __fmul_rn(v.scale, LOG2E), cq = __fmul_rn(v.draft_scale, LOG2E);
     Row<T> p{}, q{};
     p.scale = v.scale, q.scale = v.draft_scale;
     float z = 0.0f, zq = 0.0f;
-    int a = 0, what, t = -1;
-    if (v.given) {
+    int a = 0, what, t;
 #pragma unroll 1
-        for (;; ++a) {
-            t = a < v.D ? sh.drafted[a] : -1;
-            q.z = t >= 0 && v.draft ? v.draft_row(s, a) : nullptr;
+    for (;; ++a) {
+        t = a < v.D ? sh.drafted[a] : -1;
+        p.z = v.target_row(s, a);
+        q.z = t >= 0 && v.draft ? v.draft_row(s, a) : nullptr;
+        if (v.given) {
             v.look_up(s, a, p, q, z, zq);
-            what = decide(p, q, t, z, zq, t >= 0 ? sh.u[a] : 0.0f);
-            if (what >= 0) break;
-            if (writes) v.accept(s, a, t, z, p);
+        } else {
+            if (t >= 0 && threadIdx.x < (q.z ? 2 : 1)) sh.z[threadIdx.x] = to_float((threadIdx.x ? q.z : p.z)[t]);
+            walk.stats(q.z ? 2 : 1, [&](int i) { return i ? q.z : p.z; }, [&](int i) { return i ? cq : c; }, a & 1);
+            p.m = sh.joined[0][0], p.s = sh.joined[0][1], z = sh.z[0];
+            if (q.z) q.m = sh.joined[1][0], q.s = sh.joined[1][1], zq = sh.z[1];
         }
-    } else {
-        const Start g = v.start[s];
-        p.m = g.m, p.s = g.s, z = g.z, q.m = g.qm, q.s = g.qs, zq = g.qz, a = g.a, what = g.what;
-        if (a < v.D && what == DRAW_REST) t = (int)load_id(v.ids, s, a);
+        what = decide(p, q, t, z, zq, t >= 0 ? sh.u[a] : 0.0f);
+        if (what >= 0) break;
+        if (writes) v.accept(s, a, t, z, p);
+        __syncthreads();                 // before the next position's
     }
-    p.z = v.target_row(s, a);
-    q.z = what == DRAW_REST && v.draft ? v.draft_row(s, a) : nullptr;
+    if (what != DRAW_REST) q.z = nullptr;
+    if (what <= DRAW_TARGET && !(in_reach(p) && (!q.z || in_reach(q)))) what = LATER;
     int drawn = -1;
     float logit = 0.0f;
-    if (what <= DRAW_TARGET && !(in_reach(p) && (!q.z || in_reach(q)))) what = LATER;
     if (what <= DRAW_TARGET) {
+        const float draw_u = v.draw_u[s];
         drawn = q.z ? walk.template fast_draw<true>(p, q, -1, draw_u, logit)
                     : walk.template fast_draw<false>(p, q, what == DRAW_REST ? t : -1, draw_u, logit);
         if (sh.unsure) what = LATER;
+    } else {
+        cluster.sync();                  // the others have read this block's statistics
     }
     if (drawn >= 0) v.accept(s, a, drawn, logit, p);
     if (writes) {
-        if (what == LATER || v.given) v.start[s] = {p.m, p.s, z, q.m, q.s, zq, a, what};
+        v.start[s] = {p.m, p.s, z, q.m, q.s, zq, a, what};
         if (what != LATER) v.finish(s, a, what != NOTHING);
     }
 }
@@ -1098,8 +1107,7 @@ int pdb_verify(pdb_tokens *t, const pdb_mat *target, const pdb_ids *draft_ids, i
             w.accept_u += first * n_drafts, w.draw_u += first, w.out.tokens += first * (n_drafts + 1);
             if (accepted) w.out.accepted += first;
             if (logp) w.out.logp += first * (n_drafts + 1);
-            int rc = v.given ? (int)PDB_OK : launch_rows(k_verify_walk<T, 256>, shaped(w.n, 256, 8, w.n, false), s, w);
-            rc = rc ? rc : launch_rows(k_verify_draw<T, 256>, shaped(w.n, 256, 8, w.n, true), s, w);
+            int rc = launch_rows(k_verify_many<T, MANY_THREADS>, shaped(w.n, MANY_THREADS, 8, w.n, true), s, w);
             rc = rc ? rc : launch_rows(k_verify<T, 512>, shaped(1, 512, 2, std::min<int64_t>(w.n, std::max(1, t->sms / MAX_CLUSTER)), true), s, w, true);
             if (rc != PDB_OK) return rc;
         }
