@@ -577,7 +577,7 @@ int pdb_tokens_create(int64_t max_tokens, int64_t max_dim, pdb_tokens **out, voi
     t->tries = WAIT_TRIES;
     int rc = cudaEventCreateWithFlags(&t->ev_use, cudaEventDisableTiming) == cudaSuccess ? PDB_OK : PDB_ECUDA;
     const size_t words = sizeof(uint32_t) * max_tokens, radix = max_tokens > SORT_MAX ? words : 0;   // of the radix sort only
-    rc = rc ? rc : alloc_block(t->arrays, {{(void **)&t->given, sizeof(float4) * (VERIFY_ROWS + 2 * VERIFY_SEQUENCES) + 3 * sizeof(int)},
+    rc = rc ? rc : alloc_block(t->arrays, {{(void **)&t->given, sizeof(float4) * VERIFY_ROWS + 3 * sizeof(int)},
                                            {(void **)&t->key, radix},
                                            {(void **)&t->tkey, radix},
                                            {(void **)&t->tpos, radix},
@@ -586,7 +586,7 @@ int pdb_tokens_create(int64_t max_tokens, int64_t max_dim, pdb_tokens **out, voi
                                            // two rows of columns in fp32 for each 32 positions
                                            {(void **)&t->part, sizeof(float) * 2 * ((max_tokens + PIECE - 1) / PIECE) * max_dim},
                                            {(void **)&t->run_list, sizeof(int4) * (max_tokens / (PIECE + 1))}}, s);
-    if (rc == PDB_OK) t->status = (int *)(t->given + VERIFY_ROWS + 2 * VERIFY_SEQUENCES);
+    if (rc == PDB_OK) t->status = (int *)(t->given + VERIFY_ROWS);
     rc = rc ? rc : fill_words(t->status, 0u, 3 * sizeof(int), s);
     if (rc != PDB_OK) {
         cudaGetLastError();

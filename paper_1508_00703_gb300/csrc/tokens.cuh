@@ -21,15 +21,14 @@ struct pdb_tokens {
     int32_t *tpos;
     float *part;               // pieces of long runs (embed.cu)
     int4 *run_list;            // where they start, their pieces, their id
-    float4 *given;             // [VERIFY_ROWS] the statistics of few sequences' rows, then [2 * VERIFY_SEQUENCES] where walks have
-                               // come to (verify.cu)
+    float4 *given;             // [VERIFY_ROWS] the statistics of few sequences' rows (verify.cu)
     pdb::Block arrays;         // holds the device arrays
     cudaEvent_t ev_use;        // recorded after the last work any call enqueued on the handle
 };
 
 namespace pdb {
 
-constexpr int64_t VERIFY_ROWS = 4096, VERIFY_SEQUENCES = 2048;
+constexpr int64_t VERIFY_ROWS = 4096;
 
 // every call on a handle records its event when it returns; not while a graph is
 // recorded, whose event could not be waited for (the graph's owner keeps the handle)

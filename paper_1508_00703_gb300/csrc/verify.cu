@@ -542,7 +542,7 @@ struct Walk {
             float z[N], y[N];
 #pragma unroll
             for (int u = 0; u < N; ++u) z[u] = to_float(raw_z[u]), y[u] = to_float(raw_y[u]);
-            int ph = -N * HIGH0, pl = -N * LOW0, qh = ph, ql = pl;     // all tokens (LESS)
+            uint32_t ph = 0u - (uint32_t)N * HIGH0, pl = 0u - (uint32_t)N * LOW0, qh = ph, ql = pl;      // all tokens (LESS)
             int aph = 0, apl = 0, aqh = 0, aql = 0;                    // those that count
             if constexpr (LESS) {
 #pragma unroll
@@ -567,7 +567,7 @@ struct Walk {
                         if (skip != (u + x) * 32) aph += h[x] - HIGH0, apl += l[x] - LOW0;
                 }
             }
-            if (LESS) sum_p += units(ph, pl), sum_q += units(qh, ql);
+            if (LESS) sum_p += units((int)ph, (int)pl), sum_q += units((int)qh, (int)ql);
             aph = __reduce_add_sync(FULL, aph), apl = __reduce_add_sync(FULL, apl);
             if (LESS) aqh = __reduce_add_sync(FULL, aqh), aql = __reduce_add_sync(FULL, aql);
             if (lane == 0) {
@@ -704,13 +704,8 @@ struct Given {
     float m, s, z, unused;
 };
 
-// Where a sequence's walk has come to: its position, what is to be done there, the rows' statistics and their logits of the drafted token.
-enum { DRAW_REST = 0, DRAW_TARGET = 1, NOTHING = 2, LATER = 3 };       // from p - q; from p; a target row without a distribution; exactly
-struct Start {
-    float m, s, z, qm, qs, qz;
-    int a, what;
-};
-static_assert(sizeof(Start) == 2 * sizeof(float4), "VERIFY_SEQUENCES of them in the handle");
+// what is to be done at a position: a draw from p - q; from p; nothing (a target row without a distribution); what only exact numbers tell
+enum { DRAW_REST = 0, DRAW_TARGET = 1, NOTHING = 2, EXACTLY = 3 };
 
 // whether u q < p, where the statistics can tell it (sure)
 template <typename T>
@@ -732,7 +727,7 @@ __device__ __forceinline__ int decide(const Row<T> &p, const Row<T> &q, int t, f
     if (t < 0 || (q.z && !q.valid())) return DRAW_TARGET;            // the drafts end here
     bool sure;
     const bool good = accepts(p, q, z, zq, u, sure);
-    return !sure ? LATER : good ? -1 : DRAW_REST;
+    return !sure ? EXACTLY : good ? -1 : DRAW_REST;
 }
 
 // a sequence's drafted tokens (-1 from the end on) and random numbers; an id out of range is recorded where no id before it ends the drafts
@@ -765,8 +760,7 @@ struct Verify {
     float scale, draft_scale;
     const float *accept_u, *draw_u;
     VerifyOut out;
-    const Given *given;                 // of all rows, or
-    Start *start;                       // of each sequence
+    const Given *given;                 // of all rows, where k_verify_rows has been there
     int *status;
     __device__ __forceinline__ const T *target_row(int64_t s, int a) const { return target + (s * (D + 1) + a) * t_stride; }
     __device__ __forceinline__ const T *draft_row(int64_t s, int a) const { return draft + (s * D + a) * d_stride; }
@@ -868,17 +862,15 @@ __device__ __forceinline__ bool in_reach(const Row<T> &r)
     return r.scale > 1e-30f && fabsf(__fmul_rn(r.m, __fmul_rn(r.scale, LOG2E))) < REACH;
 }
 
-// Many sequences, a cluster for each: its walk (bound by memory) up to the first position that is not surely accepted, and its draw (bound
-// by instructions); on an SM some sequences walk while others draw (in two kernels, 256 x 5 drafts x 128,000 bf16: 115 us and 100, together
-// WALKDRAW).  What FastTerm cannot tell is left to k_verify, whose larger clusters have it done sooner: two of 256 sequences, which
-// would be all that still runs at the end.
-constexpr int MANY_THREADS = 256, MANY_PER_SM = 3;
+// A cluster for each sequence: its walk (bound by memory) up to the first position that is not accepted, and its draw (bound by instructions).
+// On an SM some sequences walk while others draw; in a kernel each they take as long, and the few whose draw has to be
+// exact (under 1 of 100, 50 us by eight blocks) are not hidden then (256 x 5 drafts x 128,000 bf16: 115 us, 100, 55).
+constexpr int MANY_THREADS = 256, FEW_THREADS = 512, MANY_PER_SM = 3;
 
 template <typename T, int THREADS>
-__global__ __launch_bounds__(THREADS, MANY_PER_SM) void k_verify_many(Verify<T> v)
+__global__ __launch_bounds__(THREADS, THREADS == FEW_THREADS ? 1 : MANY_PER_SM) void k_verify(Verify<T> v)
 {
     after_previous();
-    let_next_start();
     extern __shared__ __align__(16) unsigned char s_raw[];
     Shared &sh = *reinterpret_cast<Shared *>(s_raw);
     cg::cluster_group cluster = cg::this_cluster();
@@ -888,19 +880,21 @@ __global__ __launch_bounds__(THREADS, MANY_PER_SM) void k_verify_many(Verify<T> 
     const int p0 = (int)((int64_t)all * rank / blocks), p1 = (int)((int64_t)all * (rank + 1) / blocks);
     Walk<T, THREADS> walk{sh, cluster, rank, blocks, v.cols, p0, p1 - p0};
     const bool writes = rank == 0 && threadIdx.x == 0;
+    const float c = __fmul_rn(v.scale, LOG2E), cq = __fmul_rn(v.draft_scale, LOG2E);
     load_drafts<THREADS>(sh, v.ids, s, v.D, v.cols, v.accept_u, rank == 0, v.status);
     for (int i = threadIdx.x; i < STEPS; i += THREADS) sh.fast_table[i] = {FAST_TABLE.hi[i], FAST_TABLE.lo[i]};
+    const float draw_u = v.draw_u[s];
     __syncthreads();
-    const float c = __fmul_rn(v.scale, LOG2E), cq = __fmul_rn(v.draft_scale, LOG2E);
     Row<T> p{}, q{};
     p.scale = v.scale, q.scale = v.draft_scale;
-    float z = 0.0f, zq = 0.0f;
-    int a = 0, what, t;
+    int a = 0, t = -1;                   // the position, its drafted token
+    bool refused = false, exact = false; // exact: their table is there
 #pragma unroll 1
     for (;; ++a) {
         t = a < v.D ? sh.drafted[a] : -1;
         p.z = v.target_row(s, a);
         q.z = t >= 0 && v.draft ? v.draft_row(s, a) : nullptr;
+        float z = 0.0f, zq = 0.0f;
         if (v.given) {
             v.look_up(s, a, p, q, z, zq);
         } else {
@@ -908,133 +902,63 @@ __global__ __launch_bounds__(THREADS, MANY_PER_SM) void k_verify_many(Verify<T> 
             walk.stats(q.z ? 2 : 1, [&](int i) { return i ? q.z : p.z; }, [&](int i) { return i ? cq : c; }, a & 1);
             p.m = sh.joined[0][0], p.s = sh.joined[0][1], z = sh.z[0];
             if (q.z) q.m = sh.joined[1][0], q.s = sh.joined[1][1], zq = sh.z[1];
+            __syncthreads();             // before the next position's
         }
-        what = decide(p, q, t, z, zq, t >= 0 ? sh.u[a] : 0.0f);
-        if (what >= 0) break;
+        const float u = t >= 0 ? sh.u[a] : 0.0f;
+        int what = decide(p, q, t, z, zq, u);
+        if (what == EXACTLY) {
+            if (!exact) walk.fill_table();
+            exact = true;
+            walk.sums(p, q);
+            if (threadIdx.x == 0) {
+                const auto in_64 = [](float scale, float z, const Row<T> &r, Two sum) {
+                    return exp((double)scale * ((double)z - (double)r.m)) / ((double)sum.hi + (double)sum.lo);
+                };
+                const double pe = in_64(v.scale, z, p, sh.row_sum[0]);
+                const double qe = q.z ? in_64(v.draft_scale, zq, q, sh.row_sum[1]) : 1.0;
+                sh.good = (double)u * qe < pe;
+            }
+            __syncthreads();
+            what = sh.good ? -1 : DRAW_REST;
+        }
+        if (what >= 0) {
+            refused = what == DRAW_REST;
+            break;
+        }
         if (writes) v.accept(s, a, t, z, p);
-        __syncthreads();                 // before the next position's
     }
-    if (what != DRAW_REST) q.z = nullptr;
-    if (what <= DRAW_TARGET && !(in_reach(p) && (!q.z || in_reach(q)))) what = LATER;
-    int drawn = -1;
-    float logit = 0.0f;
-    if (what <= DRAW_TARGET) {
-        const float draw_u = v.draw_u[s];
-        drawn = q.z ? walk.template fast_draw<true>(p, q, -1, draw_u, logit)
-                    : walk.template fast_draw<false>(p, q, what == DRAW_REST ? t : -1, draw_u, logit);
-        if (sh.unsure) what = LATER;
+    bool none = true;
+    if (p.valid()) {
+        if (!refused) q.z = nullptr;
+        int without = refused && !q.z ? t : -1;
+        bool fast = in_reach(p) && (!q.z || in_reach(q));
+#pragma unroll 1
+        for (;;) {
+            float z = 0.0f;
+            int drawn;
+            if (fast) {
+                drawn = q.z ? walk.template fast_draw<true>(p, q, -1, draw_u, z) : walk.template fast_draw<false>(p, q, without, draw_u, z);
+            } else {
+                if (!exact) walk.fill_table();
+                exact = true;
+                if (q.z) walk.sums(p, q);
+                // one row's weights need no more than a common factor, a power of two
+                const Two unit = {__int_as_float((127 - walk.above(p)) << 23), 0.0f};
+                drawn = walk.draw({p, q, q.z ? sh.row_inv[0] : unit, sh.row_inv[1], without, sh.table}, draw_u, z);
+            }
+            const bool unsure = fast && sh.unsure;
+            none = !fast && sh.none;
+            if (drawn >= 0) v.accept(s, a, drawn, z, p);
+            if (!unsure && (!none || !refused)) break;
+            // once more, exactly; or, with nothing of p - q that 2^-46 could tell, from p
+            if (!unsure) refused = false, q.z = nullptr, without = -1;
+            fast = false;
+            __syncthreads();
+        }
     } else {
         cluster.sync();                  // the others have read this block's statistics
     }
-    if (drawn >= 0) v.accept(s, a, drawn, logit, p);
-    if (writes) {
-        v.start[s] = {p.m, p.s, z, q.m, q.s, zq, a, what};
-        if (what != LATER) v.finish(s, a, what != NOTHING);
-    }
-}
-
-// All of a sequence, exactly where that is needed: few sequences, a cluster for each, or with `later` those that the draws left, the clusters
-// taking them in turn.
-template <typename T, int THREADS>
-__global__ __launch_bounds__(THREADS, 1) void k_verify(Verify<T> v, bool later)
-{
-    after_previous();
-    extern __shared__ __align__(16) unsigned char s_raw[];
-    Shared &sh = *reinterpret_cast<Shared *>(s_raw);
-    cg::cluster_group cluster = cg::this_cluster();
-    const int blocks = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
-    const int all = (v.cols + PIECE - 1) / PIECE;
-    const int p0 = (int)((int64_t)all * rank / blocks), p1 = (int)((int64_t)all * (rank + 1) / blocks);
-    Walk<T, THREADS> walk{sh, cluster, rank, blocks, v.cols, p0, p1 - p0};
-    const bool writes = rank == 0 && threadIdx.x == 0;
-    const float c = __fmul_rn(v.scale, LOG2E), cq = __fmul_rn(v.draft_scale, LOG2E);
-    bool filled = false;                 // the exact terms' table
-#pragma unroll 1
-    for (int64_t s = blockIdx.x / (unsigned)blocks; s < v.n; s += gridDim.x / (unsigned)blocks) {
-        if (later && v.start[s].what != LATER) continue;
-        load_drafts<THREADS>(sh, v.ids, s, v.D, v.cols, v.accept_u, rank == 0 && !later, v.status);
-        if (!later)
-            for (int i = threadIdx.x; i < STEPS; i += THREADS) sh.fast_table[i] = {FAST_TABLE.hi[i], FAST_TABLE.lo[i]};
-        const float draw_u = v.draw_u[s];
-        __syncthreads();
-        Row<T> p{}, q{};
-        p.scale = v.scale, q.scale = v.draft_scale;
-        const int begin = later ? v.start[s].a : 0;
-        int a = begin, t = -1;           // the position, its drafted token
-        bool refused = false, exact = later;
-#pragma unroll 1
-        for (;; ++a) {
-            t = a < v.D ? sh.drafted[a] : -1;
-            p.z = v.target_row(s, a);
-            q.z = t >= 0 && v.draft ? v.draft_row(s, a) : nullptr;
-            float z = 0.0f, zq = 0.0f;
-            if (later && a == begin) {
-                const Start g = v.start[s];
-                p.m = g.m, p.s = g.s, z = g.z, q.m = g.qm, q.s = g.qs, zq = g.qz;
-            } else if (v.given) {
-                v.look_up(s, a, p, q, z, zq);
-            } else {
-                if (t >= 0 && threadIdx.x < (q.z ? 2 : 1)) sh.z[threadIdx.x] = to_float((threadIdx.x ? q.z : p.z)[t]);
-                walk.stats(q.z ? 2 : 1, [&](int i) { return i ? q.z : p.z; }, [&](int i) { return i ? cq : c; }, a & 1);
-                p.m = sh.joined[0][0], p.s = sh.joined[0][1], z = sh.z[0];
-                if (q.z) q.m = sh.joined[1][0], q.s = sh.joined[1][1], zq = sh.z[1];
-                __syncthreads();         // before the next position's
-            }
-            const float u = t >= 0 ? sh.u[a] : 0.0f;
-            int what = decide(p, q, t, z, zq, u);
-            if (what == LATER) {
-                if (!filled) walk.fill_table();
-                filled = exact = true;
-                walk.sums(p, q);
-                if (threadIdx.x == 0) {
-                    const auto in_64 = [](float scale, float z, const Row<T> &r, Two sum) {
-                        return exp((double)scale * ((double)z - (double)r.m)) / ((double)sum.hi + (double)sum.lo);
-                    };
-                    const double pe = in_64(v.scale, z, p, sh.row_sum[0]);
-                    const double qe = q.z ? in_64(v.draft_scale, zq, q, sh.row_sum[1]) : 1.0;
-                    sh.good = (double)u * qe < pe;
-                }
-                __syncthreads();
-                what = sh.good ? -1 : DRAW_REST;
-            }
-            if (what >= 0) {
-                refused = what == DRAW_REST;
-                break;
-            }
-            if (writes) v.accept(s, a, t, z, p);
-        }
-        bool none = true;
-        if (p.valid()) {
-            if (!refused) q.z = nullptr;
-            int without = refused && !q.z ? t : -1;
-            bool fast = !exact && in_reach(p) && (!q.z || in_reach(q));
-#pragma unroll 1
-            for (;;) {
-                float z = 0.0f;
-                int drawn;
-                if (fast) {
-                    drawn = q.z ? walk.template fast_draw<true>(p, q, -1, draw_u, z) : walk.template fast_draw<false>(p, q, without, draw_u, z);
-                } else {
-                    if (!filled) walk.fill_table();
-                    filled = true;
-                    if (q.z) walk.sums(p, q);
-                    // one row's weights need no more than a common factor, a power of two
-                    const Two unit = {__int_as_float((127 - walk.above(p)) << 23), 0.0f};
-                    drawn = walk.draw({p, q, q.z ? sh.row_inv[0] : unit, sh.row_inv[1], without, sh.table}, draw_u, z);
-                }
-                const bool unsure = fast && sh.unsure;
-                none = !fast && sh.none;
-                if (drawn >= 0) v.accept(s, a, drawn, z, p);
-                if (!unsure && (!none || !refused)) break;
-                // once more, exactly; or, with nothing of p - q that 2^-46 could tell, from p
-                if (!unsure) refused = false, q.z = nullptr, without = -1;
-                fast = false;
-                __syncthreads();
-            }
-        }
-        if (writes) v.finish(s, a, !none);
-        cluster.sync();                  // before the next sequence, or the end: the others have read this block's numbers
-    }
+    if (writes) v.finish(s, a, !none);
 }
 
 size_t verify_smem(int64_t cols, int blocks)
@@ -1074,10 +998,10 @@ int pdb_verify(pdb_tokens *t, const pdb_mat *target, const pdb_ids *draft_ids, i
     return with_type(target->type, [&](auto *a) {
         using T = std::remove_pointer_t<decltype(a)>;
         const int64_t nv = target->cols / Vec<T>::E + 1;
-        const auto shaped = [&](int64_t rows, int threads, int per_sm, int64_t clusters, bool draws) {
+        const auto shaped = [&](int64_t clusters, int threads, int per_sm, bool draws) {
             Shape shape = {};
             shape.threads = threads;
-            shape.blocks = cluster_of(rows, nv, threads, [&](int blocks) { return (int64_t)t->sms * per_sm / blocks; });
+            shape.blocks = cluster_of(clusters, nv, threads, [&](int blocks) { return (int64_t)t->sms * per_sm / blocks; });
             shape.clusters = clusters;
             shape.smem = draws ? verify_smem(target->cols, shape.blocks) : 0;
             return shape;
@@ -1088,30 +1012,16 @@ int pdb_verify(pdb_tokens *t, const pdb_mat *target, const pdb_ids *draft_ids, i
         v.cols = (int)target->cols, v.D = (int)n_drafts, v.n = n;
         if (n_drafts > 0) v.ids = ids_of(draft_ids);
         v.scale = scale, v.draft_scale = draft_scale, v.accept_u = accept_u, v.draw_u = draw_u;
-        v.out = {tokens, accepted, logp}, v.start = (Start *)(t->given + VERIFY_ROWS), v.status = t->status;
+        v.out = {tokens, accepted, logp}, v.status = t->status;
         // the statistics of all rows at once where the SMs would not be busy with a position of each sequence: a launch more, fewer rounds
         const int64_t rows = target->rows + (draft ? drafts : 0);
         if (n_drafts > 0 && n * 2 <= t->sms && rows <= VERIFY_ROWS) {
             v.given = (const Given *)t->given;
-            const int rc = launch_rows(k_verify_rows<T, 512>, shaped(rows, 512, 2, rows, false), s, v, (Given *)t->given);
+            const int rc = launch_rows(k_verify_rows<T, 512>, shaped(rows, 512, 2, false), s, v, (Given *)t->given);
             if (rc != PDB_OK) return rc;
         }
-        if (n * MAX_CLUSTER <= t->sms) return launch_rows(k_verify<T, 512>, shaped(n, 512, 2, n, true), s, v, false);
-        // sequences by as many as the handle has places for
-        for (int64_t first = 0; first < n; first += VERIFY_SEQUENCES) {
-            Verify<T> w = v;
-            w.n = std::min(VERIFY_SEQUENCES, n - first);
-            w.target += first * (n_drafts + 1) * v.t_stride;
-            if (draft) w.draft += first * n_drafts * v.d_stride;
-            w.ids.data = (const char *)v.ids.data + first * v.ids.stride * (v.ids.wide ? 8 : 4);
-            w.accept_u += first * n_drafts, w.draw_u += first, w.out.tokens += first * (n_drafts + 1);
-            if (accepted) w.out.accepted += first;
-            if (logp) w.out.logp += first * (n_drafts + 1);
-            int rc = launch_rows(k_verify_many<T, MANY_THREADS>, shaped(w.n, MANY_THREADS, 8, w.n, true), s, w);
-            rc = rc ? rc : launch_rows(k_verify<T, 512>, shaped(1, 512, 2, std::min<int64_t>(w.n, std::max(1, t->sms / MAX_CLUSTER)), true), s, w, true);
-            if (rc != PDB_OK) return rc;
-        }
-        return (int)PDB_OK;
+        if (n * MAX_CLUSTER <= t->sms) return launch_rows(k_verify<T, FEW_THREADS>, shaped(n, FEW_THREADS, 2, true), s, v);
+        return launch_rows(k_verify<T, MANY_THREADS>, shaped(n, MANY_THREADS, 8, true), s, v);
     });
 }
 
