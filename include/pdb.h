@@ -430,7 +430,7 @@ int pdb_sgd_epoch_ready_noalloc(const pdb_csr *X, const float *y, const uint32_t
  * data's in pieces, pdb_embed_grad), with vectors for scalars.  The softmax losses
  * take the place of pdb_loss.  The paper has no formulas for them; each declaration gives its own.
  *
- * Every call takes a pdb_tokens handle: the workspace of pdb_embed_grad, and
+ * Every call but pdb_clip's takes a pdb_tokens handle: the workspace of pdb_embed_grad, pdb_route and pdb_verify, and
  * the status word in which the kernels record an id out of range
  * or an expired wait (pdb_tokens_status).  A recorded error stops no later call: a bad id gives the
  * result its declaration states.  Calls that share a handle must be ordered on
@@ -467,8 +467,8 @@ typedef struct {
 
 typedef struct pdb_tokens pdb_tokens; /* opaque, library-owned device arrays */
 
-/* Handle for calls of at most max_tokens ids (below 2^31) and, in pdb_embed_grad, rows of at
- * most max_dim elements; holds about 8 + max_dim / 4 bytes for each of
+/* Handle for calls of at most max_tokens ids (below 2^31; in pdb_route, slots) and, in pdb_embed_grad, rows of at
+ * most max_dim elements; holds 64 KB, and about 8 + max_dim / 4 bytes for each of
  * max_tokens (12 more above 65,536).  Allocates stream-ordered on `stream`.
  * pdb_tokens_free waits for the work enqueued on the handle, then releases it.
  * pdb_tokens_status SYNCHRONIZES `stream` and returns the first error that a
@@ -579,9 +579,9 @@ int pdb_distill(pdb_tokens *t, const pdb_mat *logits, const pdb_ids *top_ids, co
  *   tokens[s, 0..n_drafts]  row-major: the accepted drafts, the drawn token, then -1
  *   logp[s, 0..n_drafts]    log p_d of these tokens, 0 behind them (may be NULL)
  * A target row that has nothing left, or holds a NaN or +inf, accepts nothing, and -1 stands where the drawn token would.
- * The random numbers are the caller's, in [0, 1); others count as their nearest end in the draw.  Sides that the 32-bit statistics cannot tell
- * apart, and every draw, are decided on probabilities good to 2^-40 of themselves and sums without rounding: the tokens do not
- * depend on how rows are split.  Rows behind the first refusal are not read.  PDB_ETOOBIG above 64 drafts or
+ * The random numbers are the caller's, in [0, 1); others count as their nearest end in the draw.  What 32-bit statistics (of which logp is formed, as in
+ * pdb_logprobs) or terms good to 2^-31 cannot tell apart is decided on terms good to 2^-40 and sums without rounding, so that the
+ * tokens do not depend on how rows are split.  Rows behind the first refusal are not read.  PDB_ETOOBIG above 64 drafts or
  * 2^21 tokens.  These are the draws a program makes with its models between the reads of Definition 3. */
 int pdb_verify(pdb_tokens *t, const pdb_mat *target, const pdb_ids *draft_ids, int64_t n_drafts, const pdb_mat *draft,
                float scale, float draft_scale, const float *accept_u, const float *draw_u, int32_t *tokens, int32_t *accepted,

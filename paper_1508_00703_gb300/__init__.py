@@ -581,7 +581,8 @@ def _vec(t, n, tok, what, kind=PDB_TYPE_FLOAT):
 
 def pdb_tokens_create(max_tokens: int = 0, max_dim: int = 0, stream=None) -> Tokens:
     """Workspace and status word of the token operators, for pdb_embed_grad
-    calls of at most max_tokens ids and max_dim columns (the other calls need neither)."""
+    calls of at most max_tokens ids and max_dim columns and pdb_route calls of at most max_tokens slots (the
+    other calls need neither)."""
     import torch
     h = ctypes.c_void_p()
     _check(load().pdb_tokens_create(int(max_tokens), int(max_dim), ctypes.byref(h), _stream(stream)),

@@ -3,7 +3,10 @@
 //   N = sqrt(sum over all gradients of g^2),  f = N > max_norm ? max_norm / N : 1,  out = [out +] scale f g
 //
 // Two launches: the sum, then the step.  A plan cuts the matrices into pieces, which the blocks take in turn, so that one launch
-// covers any number of gradients of any sizes, types and strides.
+// covers any number of gradients of any sizes, types and strides.  Bound by memory: 484 million bf16 gradients in 59 matrices, the step on fp32
+// weights, 138 us for the sum (967 MB at 7.0 TB/s) and 705 us for the step (4.8 GB at 6.9 TB/s).  The second read of the gradients cannot be
+// saved (none is scaled before all are summed) but for what L2 still holds, which the step therefore takes first: 102 million fp32 gradients
+// into bf16, 61 and 99 us, where 615 MB read and written take 91 and 410 MB more 61.
 #include <algorithm>
 #include <climits>
 #include <cmath>

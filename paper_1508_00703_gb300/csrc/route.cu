@@ -36,7 +36,9 @@ __device__ __forceinline__ int2 fetch_slot(const Slots &s, uint32_t f)
     return fetch_id(s.ids, i, (int)(f - i * s.k));
 }
 
-// how often each expert occurs among a block's slots
+// How often each expert occurs among a block's slots.  Two launches for more than one block's slots: the counts, then the places, whose
+// blocks each add up the counts of all.  131,072 slots, 64 experts: 5.3 and 8.4 us, chains of latencies (ids, counts, barriers); up to 2048
+// slots one block and one launch, 4.1 us for 16.
 template <int IPT>
 __global__ __launch_bounds__(ROUTE_THREADS) void k_route_count(Slots s, uint32_t *__restrict__ counts, int *status)
 {
@@ -193,7 +195,9 @@ __device__ __forceinline__ void zero_unused(const int32_t *source, int64_t r0, i
 }
 
 // A warp moves one piece of ROWS_UNROLL * 32 packs of a token's row, read once, to the rows of its slots; the warps behind
-// those write zeros where no slot is.  Bound by memory.
+// those write zeros where no slot is.  Bound by memory: 16,384 rows of 2048 bf16 to 8 places each 96 us, 605 MB at 6.3 TB/s (by
+// place, each token's row would be read 8 times).  Rows that start at any 4 bytes are moved element by element, 4099 x 1001 fp32 into 9600 rows 17 us, 55
+// MB at 3.2 TB/s.
 template <int E>
 constexpr int ROWS_UNROLL = E > 1 ? 4 : 16;
 
@@ -259,7 +263,8 @@ __device__ __forceinline__ unsigned slots_there(const Slot &s, int64_t rows, int
 }
 
 // A warp sums one piece of JOIN_UNROLL * 32 packs of a token's row over its slots in ascending order, JOIN_SLOTS rows under way
-// at once, and takes the next piece; that one's first 32 places are on their way meanwhile.  Bound by memory.
+// at once, and takes the next piece; that one's first 32 places are on their way meanwhile.  Bound by memory: 8192 tokens of 4 slots,
+// 4096 bf16, 48 us, 336 MB at 7.0 TB/s (a warp a piece, 106 registers a thread: 91 us; pieces of half the size: 65).
 template <int E>
 constexpr int JOIN_UNROLL = E > 2 ? 2 : 4;
 constexpr int JOIN_SLOTS = 4, JOIN_BLOCKS = 3;
@@ -328,7 +333,8 @@ __global__ __launch_bounds__(256, JOIN_BLOCKS) void k_route_join(const T *in, in
 // Gradients of the join: drows[p_j] = w_j dy, dw_j = <dy, rows[p_j]>.  `team` warps of a block (a power of two) have a token, whose columns
 // they take in turn: each holds its packs of dy and goes over the slots, GRAD_SLOTS rows under way at once; the dot products are summed over
 // the lanes, then over the team's warps in order.  The next token's places, weights and first packs of dy are on their way meanwhile.
-// At the end the warps write zeros in rows that no slot takes.  Bound by memory.
+// At the end the warps write zeros in rows that no slot takes.  Bound by memory: 8192 tokens of 4 slots, 4096 bf16, 107 us, 604 MB at 5.6 TB/s
+// (half of it written; a block a token: 186 us; packs of 1 instead of 4 of a lane: 150).
 constexpr int GRAD_UNROLL = 4, GRAD_WARPS = 8, GRAD_SLOTS = 4, GRAD_BLOCKS = 2;
 
 template <typename T, typename D, int E>

@@ -198,6 +198,20 @@ def test_ends_of_the_numbers(tok, u, v):
     _check(tok, z, ids, a, b, y)
 
 
+@pytest.mark.parametrize("size", [1e-35, 1e-31, 1e-25, 1e25, 1e31, 1e35])
+def test_far_scales(tok, size):
+    # logits of any size and the scale that makes them ordinary ones
+    z, ids, u, v, y = _inputs(30, 2, 2000, torch.float32, seed=17)
+    _check(tok, z / size, ids, u, v, y / size, size, size)
+
+
+@pytest.mark.parametrize("offset", [300.0, -3000.0, 1e6])
+def test_far_offsets(tok, offset):
+    # a distance that all logits share, which their type rounds
+    z, ids, u, v, y = _inputs(30, 2, 2000, torch.float32, seed=18)
+    _check(tok, z + offset, ids, u, v, y - offset)
+
+
 def test_rows_without_a_distribution(tok):
     for bad in (math.nan, math.inf, -math.inf):
         for where in range(3):
