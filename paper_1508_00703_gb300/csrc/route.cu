@@ -11,6 +11,7 @@
 #include "rows.cuh"
 
 using namespace pdb;
+namespace cg = cooperative_groups;
 
 namespace {
 
@@ -36,9 +37,8 @@ __device__ __forceinline__ int2 fetch_slot(const Slots &s, uint32_t f)
     return fetch_id(s.ids, i, (int)(f - i * s.k));
 }
 
-// How often each expert occurs among a block's slots.  Two launches for more than one block's slots: the counts, then the places, whose
-// blocks each add up the counts of all.  131,072 slots, 64 experts: 5.3 and 8.4 us, chains of latencies (ids, counts, barriers); up to 2048
-// slots one block and one launch, 4.1 us for 16.
+// More than a cluster's slots: how often each expert occurs among a block's slots, for the places' launch, whose blocks each add up the
+// counts of all.  131,072 slots, 64 experts: 5.3 and 8.4 us, chains of latencies (ids, counts, barriers).
 template <int IPT>
 __global__ __launch_bounds__(ROUTE_THREADS) void k_route_count(Slots s, uint32_t *__restrict__ counts, int *status)
 {
@@ -66,8 +66,11 @@ __global__ __launch_bounds__(ROUTE_THREADS) void k_route_count(Slots s, uint32_t
 }
 
 // A block's slots, warp after warp, 32 at a time: a lane's rank is the lower lanes of its expert, its warp's slots before
-// them, the lower warps', and the lower blocks'.
-template <int IPT>
+// them, the lower warps', and the lower blocks'.  Up to CLUSTER_SLOTS slots the blocks are a cluster and take one another's counts from
+// shared memory (ONE: a launch alone; 8198 slots, 32 experts: 9.7 us instead of 14.3 in two).
+constexpr int CLUSTER_SLOTS = 65536;
+
+template <int IPT, bool ONE>
 __global__ __launch_bounds__(ROUTE_THREADS) void k_route_place(Slots s, const uint32_t *counts, int64_t capacity,
                                                                int32_t *__restrict__ place, int32_t *__restrict__ source,
                                                                int32_t *__restrict__ ends, int *status)
@@ -76,7 +79,8 @@ __global__ __launch_bounds__(ROUTE_THREADS) void k_route_place(Slots s, const ui
     let_next_start();
     extern __shared__ uint32_t s_first[];                                       // [experts] of all and of lower blocks, then
     uint32_t *s_total = s_first + s.experts;                                    // [experts] slots of the expert in all
-    uint16_t *s_warp = reinterpret_cast<uint16_t *>(s_total + s.experts);       // [warp][experts] the expert's slots by warp
+    uint32_t *s_block = s_total + s.experts;                                    // [experts] the block's (ONE)
+    uint16_t *s_warp = reinterpret_cast<uint16_t *>(s_block + (ONE ? s.experts : 0));      // [warp][experts] the expert's slots by warp
     __shared__ uint32_t s_sum[ROUTE_WARPS];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, experts = s.experts;
     const uint32_t f0 = blockIdx.x * (uint32_t)(ROUTE_THREADS * IPT) + warp * (32 * IPT) + lane;
@@ -87,7 +91,7 @@ __global__ __launch_bounds__(ROUTE_THREADS) void k_route_place(Slots s, const ui
     for (int e = tid; e < ROUTE_WARPS * experts; e += ROUTE_THREADS) s_warp[e] = 0;
     __syncthreads();
     // the blocks' counts, every `sets`-th of them by one thread
-    if (gridDim.x > 1) {
+    if (!ONE) {
         const int sets = max(1, ROUTE_THREADS / experts);
         for (int x = tid; x < sets * experts; x += ROUTE_THREADS) {
             const int set = x / experts, e = x - set * experts;
@@ -118,7 +122,6 @@ __global__ __launch_bounds__(ROUTE_THREADS) void k_route_place(Slots s, const ui
     __syncthreads();
     // experts tid * per ..: the warps' counts become places, the totals are summed up over the experts
     const int per = (experts + ROUTE_THREADS - 1) / ROUTE_THREADS, e0 = min(experts, tid * per), e1 = min(experts, e0 + per);
-    uint32_t mine = 0;
     for (int e = e0; e < e1; ++e) {
         uint32_t sum = 0;
 #pragma unroll
@@ -127,9 +130,23 @@ __global__ __launch_bounds__(ROUTE_THREADS) void k_route_place(Slots s, const ui
             s_warp[w * experts + e] = (uint16_t)sum;
             sum += c;
         }
-        if (gridDim.x == 1) s_total[e] = sum;
-        mine += s_total[e];
+        if (ONE) s_block[e] = sum;
     }
+    uint32_t mine = 0;
+    if (ONE) {
+        cg::cluster_group cluster = cg::this_cluster();
+        cluster.sync();
+        for (int e = e0; e < e1; ++e) {
+            uint32_t all = 0, before = 0;
+            for (int b = 0; b < (int)gridDim.x; ++b) {
+                const uint32_t c = cluster.map_shared_rank(s_block, b)[e];
+                all += c;
+                before += b < (int)blockIdx.x ? c : 0;
+            }
+            s_total[e] = all, s_first[e] = before;
+        }
+    }
+    for (int e = e0; e < e1; ++e) mine += s_total[e];
     uint32_t up = mine;
 #pragma unroll
     for (int off = 1; off < 32; off <<= 1) {
@@ -166,9 +183,10 @@ __global__ __launch_bounds__(ROUTE_THREADS) void k_route_place(Slots s, const ui
     const int64_t rows = capacity ? experts * capacity : (int64_t)s.n;
     for (int64_t r = (int64_t)blockIdx.x * ROUTE_THREADS + tid; r < rows; r += (int64_t)gridDim.x * ROUTE_THREADS)
         if (r >= s_total[capacity ? (int)(r / capacity) : experts - 1]) source[r] = -1;
+    if (ONE) cg::this_cluster().sync();              // the others have read this block's counts
 }
 
-inline size_t place_smem(int experts) { return (size_t)experts * (8 + 2 * ROUTE_WARPS); }
+inline size_t place_smem(int experts, bool one) { return (size_t)experts * ((one ? 12 : 8) + 2 * ROUTE_WARPS); }
 
 // w / pieces
 __device__ __forceinline__ int64_t row_of(int64_t w, int pieces)
@@ -177,8 +195,9 @@ __device__ __forceinline__ int64_t row_of(int64_t w, int pieces)
 }
 
 // ------------------------------------------------------------------ rows there
-// zeros in the rows of `rows` (8 of them from r0 on) that no slot takes, by a warp
-constexpr int ZERO_ROWS = 8;
+// zeros in the rows of `rows` (ZERO_ROWS of them from r0 on) that no slot takes, by a warp: few, since a warp that finds all of its
+// rows unused is the launch's last (9600 rows of 1001 fp32 for 8198 slots: 12 us, with 8 to a warp 16)
+constexpr int ZERO_ROWS = 2;
 
 template <typename O, int E>
 __device__ __forceinline__ void zero_unused(const int32_t *source, int64_t r0, int64_t rows, int dim, O *out, int64_t stride)
@@ -196,8 +215,8 @@ __device__ __forceinline__ void zero_unused(const int32_t *source, int64_t r0, i
 
 // A warp moves one piece of ROWS_UNROLL * 32 packs of a token's row, read once, to the rows of its slots; the warps behind
 // those write zeros where no slot is.  Bound by memory: 16,384 rows of 2048 bf16 to 8 places each 96 us, 605 MB at 6.3 TB/s (by
-// place, each token's row would be read 8 times).  Rows that start at any 4 bytes are moved element by element, 4099 x 1001 fp32 into 9600 rows 17 us, 55
-// MB at 3.2 TB/s.
+// place, each token's row would be read 8 times).  Rows that start at any 4 bytes are moved element by element, 4099 x 1001 fp32 into 9600 rows 12 us, 55
+// MB at 4.6 TB/s.
 template <int E>
 constexpr int ROWS_UNROLL = E > 1 ? 4 : 16;
 
@@ -216,6 +235,7 @@ __global__ __launch_bounds__(256) void k_route_rows(const T *x, int64_t stride, 
     const int64_t i = row_of(w, pieces);
     const int piece = (int)(w - i * pieces), j0 = (piece * ROWS_UNROLL<E> * 32 + lane) * E;
     const T *from = x + i * stride;
+    int32_t mine = lane < k ? place[i * k + lane] : -1;          // on its way beside the row
     Pack<T, E> v[ROWS_UNROLL<E>];
 #pragma unroll
     for (int u = 0; u < ROWS_UNROLL<E>; ++u)
@@ -228,7 +248,7 @@ __global__ __launch_bounds__(256) void k_route_rows(const T *x, int64_t stride, 
         y[u] = of_floats<O>(f);
     }
     for (int s0 = 0; s0 < k; s0 += 32) {
-        const int32_t mine = s0 + lane < k ? place[i * k + s0 + lane] : -1;
+        if (s0) mine = s0 + lane < k ? place[i * k + s0 + lane] : -1;
         if (mine >= rows) set_status(status, PDB_ERANGE);
         unsigned there = __ballot_sync(FULL, mine >= 0 && mine < rows);
         for (; there; there &= there - 1) {
@@ -485,19 +505,30 @@ int pdb_route(pdb_tokens *t, const pdb_ids *ids, int64_t k, int64_t n_experts, i
     cudaStream_t s = (cudaStream_t)stream;
     TokensUse use{t, s};
     const Slots slots{{ids->data, n > 1 ? ids->stride : 0, ids->wide}, (uint32_t)ids->n, (uint32_t)k, (int)n_experts};
-    const auto run = [&](auto ipt) {
+    const auto run = [&](auto ipt, auto one) {
         constexpr int IPT = decltype(ipt)::value;
-        const int64_t blocks = std::max<int64_t>(1, (ids->n + ROUTE_THREADS * IPT - 1) / (ROUTE_THREADS * IPT));
-        // the blocks' counts: no more words than slots, since blocks * experts <= slots where there are two blocks or more
+        constexpr bool ONE = decltype(one)::value;
+        int64_t blocks = std::max<int64_t>(1, (ids->n + ROUTE_THREADS * IPT - 1) / (ROUTE_THREADS * IPT));
         int got = PDB_OK;
-        if (blocks > 1) got = launch(k_route_count<IPT>, blocks, ROUTE_THREADS, sizeof(uint32_t) * n_experts, 1, s, slots, t->skey, t->status);
-        if (got != PDB_OK) return got;
-        if (!allow_smem((const void *)k_route_place<IPT>)) return (int)PDB_ECUDA;
-        return launch(k_route_place<IPT>, blocks, ROUTE_THREADS, place_smem((int)n_experts), 1, s, slots, t->skey, capacity,
+        if (ONE) {
+            int cluster = 1;
+            while (cluster < blocks) cluster *= 2;
+            blocks = cluster;
+        } else {
+            // the blocks' counts: no more words than slots, since blocks * experts <= slots above CLUSTER_SLOTS
+            got = launch(k_route_count<IPT>, blocks, ROUTE_THREADS, sizeof(uint32_t) * n_experts, 1, s, slots, t->skey, t->status);
+            if (got != PDB_OK) return got;
+        }
+        const auto kernel = k_route_place<IPT, ONE>;
+        if (!allow_smem((const void *)kernel)) return (int)PDB_ECUDA;
+        return launch(kernel, blocks, ROUTE_THREADS, place_smem((int)n_experts, ONE), ONE ? (int)blocks : 1, s, slots, t->skey, capacity,
                       place, source, ends, t->status);
     };
+    static_assert(CLUSTER_SLOTS == ROUTE_THREADS * 16 * MAX_CLUSTER, "sixteen slots a thread");
     // blocks of 2048 slots while there are few of them: each adds up the counts of all
-    return n_experts <= 1024 && ids->n <= 2048 * (int64_t)t->sms ? run(Num<4>()) : run(Num<16>());
+    if (ids->n <= ROUTE_THREADS * 4 * MAX_CLUSTER) return run(Num<4>(), Num<1>());
+    if (ids->n <= CLUSTER_SLOTS) return run(Num<16>(), Num<1>());
+    return n_experts <= 1024 && ids->n <= 2048 * (int64_t)t->sms ? run(Num<4>(), Num<0>()) : run(Num<16>(), Num<0>());
 }
 
 int pdb_route_rows(pdb_tokens *t, const pdb_mat *x, const int32_t *place, int64_t k, const int32_t *source,

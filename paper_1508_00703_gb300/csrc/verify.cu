@@ -202,8 +202,7 @@ __device__ __forceinline__ int64_t fast_margin(int cols, int fine) { return ((in
 struct Shared {
     float part[2][2][16];               // the warps' m, s of the target's and the draft's row
     float stat[2][2][2];                // this block's, for two positions in turn
-    float joined[2][2];                 // all blocks'
-    float z[2];                         // the rows' logits of the drafted token
+    float z[2][2];                      // the rows' logits of the drafted token, for two positions in turn
     int drafted[MAX_DRAFTS];
     float u[MAX_DRAFTS];
     int64_t warp_sum[2][16];
@@ -237,10 +236,10 @@ struct Walk {
     int rank, blocks, cols;
     int first_piece, pieces;            // the block's
 
-    // m and s of one or two rows (row(i): where the i-th lies, c(i): its scale * log2(e)) over the cluster, into sh.joined.  The chunks
-    // of both follow one another, each loaded while the one before is added.
-    template <typename R, typename C>
-    __device__ __forceinline__ void stats(int rows, R row, C c_of, int turn)
+    // m and s of one or two rows (row(i): where the i-th lies, c(i): its scale * log2(e)) over the cluster, to out(i, m, s) on all threads.
+    // The chunks of both follow one another, each loaded while the one before is added.
+    template <typename R, typename C, typename F>
+    __device__ __forceinline__ void stats(int rows, R row, C c_of, int turn, F out)
     {
         constexpr int W = THREADS / 32, SPAN = THREADS * UNROLL;
         const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -290,7 +289,8 @@ struct Walk {
             if (lane == 0) sh.stat[turn][i][0] = a.m, sh.stat[turn][i][1] = a.s;
         }
         cluster.sync();
-        for (int i = warp; i < rows; i += W) {
+        // every warp for itself: barriers are what a position's end costs
+        for (int i = 0; i < rows; ++i) {
             a = Stat<false>();
             const int b = lane & (MAX_CLUSTER - 1);
             if (b < blocks) {
@@ -298,25 +298,14 @@ struct Walk {
                 a.m = o[0], a.s = o[1];
             }
             a.template warp_join<MAX_CLUSTER>(c_of(i));
-            if (lane == 0) sh.joined[i][0] = a.m, sh.joined[i][1] = a.s;
+            out(i, a.m, a.s);
         }
-        __syncthreads();
     }
 
     __device__ __forceinline__ void fill_table()
     {
         for (int i = threadIdx.x; i < 256; i += THREADS) sh.table[i] = {EXP2_TABLE.hi[i], EXP2_TABLE.lo[i]};
         __syncthreads();
-    }
-
-    // the block's part of a row into L2, all of it at once: a piece ahead, as each_piece loads, is too little for memory's latency (256 draws
-    // from 128,000 bf16: 112 us -> 106)
-    __device__ __forceinline__ void bring(const T *z) const
-    {
-        if (threadIdx.x != 0 || !z || pieces == 0) return;
-        const uintptr_t from = ((uintptr_t)(z + (int64_t)first_piece * PIECE) + 15) & ~(uintptr_t)15;
-        const uintptr_t to = (uintptr_t)(z + min((int64_t)(first_piece + pieces) * PIECE, (int64_t)cols)) & ~(uintptr_t)15;
-        if (from < to) asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(from), "r"((unsigned)(to - from)) : "memory");
     }
 
     // f(the lane's tokens of a piece: z and, where there is one, y) of the warp's pieces; a piece's are loaded before the one before is
@@ -378,7 +367,6 @@ struct Walk {
     __device__ __forceinline__ void sums(const Row<T> &p, const Row<T> &q)
     {
         constexpr int N = PIECE / 32;
-        bring(p.z), bring(q.z);
 #pragma unroll 1
         for (int which = 0; which < (q.z ? 2 : 1); ++which) {
             const float m = which ? q.m : p.m, scale = which ? q.scale : p.scale;
@@ -468,7 +456,6 @@ struct Walk {
         constexpr int N = PIECE / 32;
         const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
         int64_t all = 0;                 // on lane 0
-        if (!weight.q.z) bring(weight.p.z);
         each_piece(weight.p.z, weight.q.z, [&](int i, const T (&z)[N], const T (&y)[N]) {
             uint64_t own = 0;
 #pragma unroll
@@ -534,8 +521,6 @@ struct Walk {
     {
         constexpr int N = PIECE / 32, W = THREADS / 32;
         const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-        bring(p.z);
-        if (LESS) bring(q.z);
         // the rows' sums are brought to the same size, as large as the largest term and 62 bits allow: fine units
         const int above_p = above(p), above_q = LESS ? above(q) : above_p, fine = min(min(above_p, above_q), 17);
         // two tokens of p, or one of p and q each
@@ -820,47 +805,11 @@ __global__ __launch_bounds__(THREADS, 1024 / THREADS) void k_verify_rows(Verify<
         if (t >= 0 && t < v.cols) z = to_float(row[t]);
     }
     Walk<T, THREADS> walk{sh, cluster, rank, blocks, v.cols, 0, 0};
-    walk.stats(1, [&](int) { return row; }, [&](int) { return __fmul_rn(drafts ? v.draft_scale : v.scale, LOG2E); }, 0);
+    Row<T> of_row{};
+    walk.stats(1, [&](int) { return row; }, [&](int) { return __fmul_rn(drafts ? v.draft_scale : v.scale, LOG2E); }, 0,
+               [&](int, float m, float sum) { of_row.m = m, of_row.s = sum; });
     cluster.sync();                      // the others have read this block's statistics
-    if (writes) given[r] = {sh.joined[0][0], sh.joined[0][1], z, 0.0f};
-}
-
-// Many sequences: their walks, a cluster for each, up to the first position that is not surely accepted.  Bound by memory, so with as many
-// threads as an SM holds; the draws' numbers want registers instead (both in one kernel: 256 x 5 drafts x 128,000 bf16 228 us).
-template <typename T, int THREADS>
-__global__ __launch_bounds__(THREADS, 1024 / THREADS) void k_verify_walk(Verify<T> v)
-{
-    after_previous();
-    let_next_start();
-    __shared__ Shared sh;
-    cg::cluster_group cluster = cg::this_cluster();
-    const int blocks = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
-    const int64_t s = blockIdx.x / (unsigned)blocks;
-    load_drafts<THREADS>(sh, v.ids, s, v.D, v.cols, v.accept_u, rank == 0, v.status);
-    __syncthreads();
-    Walk<T, THREADS> walk{sh, cluster, rank, blocks, v.cols, 0, 0};
-    const bool writes = rank == 0 && threadIdx.x == 0;
-    const float c = __fmul_rn(v.scale, LOG2E), cq = __fmul_rn(v.draft_scale, LOG2E);
-    Row<T> p{}, q{};
-    p.scale = v.scale, q.scale = v.draft_scale;
-    float z = 0.0f, zq = 0.0f;
-    int a = 0, what;
-#pragma unroll 1
-    for (;; ++a) {
-        const int t = a < v.D ? sh.drafted[a] : -1;
-        p.z = v.target_row(s, a);
-        q.z = t >= 0 && v.draft ? v.draft_row(s, a) : nullptr;
-        if (t >= 0 && threadIdx.x < (q.z ? 2 : 1)) sh.z[threadIdx.x] = to_float((threadIdx.x ? q.z : p.z)[t]);
-        walk.stats(q.z ? 2 : 1, [&](int i) { return i ? q.z : p.z; }, [&](int i) { return i ? cq : c; }, a & 1);
-        p.m = sh.joined[0][0], p.s = sh.joined[0][1], z = sh.z[0];
-        if (q.z) q.m = sh.joined[1][0], q.s = sh.joined[1][1], zq = sh.z[1];
-        what = decide(p, q, t, z, zq, t >= 0 ? sh.u[a] : 0.0f);
-        if (what >= 0) break;
-        if (writes) v.accept(s, a, t, z, p);
-        __syncthreads();                 // before the next position's
-    }
-    if (writes) v.start[s] = {p.m, p.s, z, q.m, q.s, zq, a, what};
-    cluster.sync();                      // the others have read this block's statistics
+    if (writes) given[r] = {of_row.m, of_row.s, z, 0.0f};
 }
 
 // |m scale| log2(e) within what FastTerm takes
@@ -906,11 +855,12 @@ __global__ __launch_bounds__(THREADS, THREADS == FEW_THREADS ? 1 : MANY_PER_SM) 
         if (v.given) {
             v.look_up(s, a, p, q, z, zq);
         } else {
-            if (t >= 0 && threadIdx.x < (q.z ? 2 : 1)) sh.z[threadIdx.x] = to_float((threadIdx.x ? q.z : p.z)[t]);
-            walk.stats(q.z ? 2 : 1, [&](int i) { return i ? q.z : p.z; }, [&](int i) { return i ? cq : c; }, a & 1);
-            p.m = sh.joined[0][0], p.s = sh.joined[0][1], z = sh.z[0];
-            if (q.z) q.m = sh.joined[1][0], q.s = sh.joined[1][1], zq = sh.z[1];
-            __syncthreads();             // before the next position's
+            const int turn = a & 1;
+            if (t >= 0 && threadIdx.x < (q.z ? 2 : 1)) sh.z[turn][threadIdx.x] = to_float((threadIdx.x ? q.z : p.z)[t]);
+            walk.stats(q.z ? 2 : 1, [&](int i) { return i ? q.z : p.z; }, [&](int i) { return i ? cq : c; }, turn, [&](int i, float m, float sum) {
+                (i ? q.m : p.m) = m, (i ? q.s : p.s) = sum;
+            });
+            z = sh.z[turn][0], zq = sh.z[turn][1];
         }
         const float u = t >= 0 ? sh.u[a] : 0.0f;
         int what = decide(p, q, t, z, zq, u);

@@ -63,7 +63,7 @@ def _route(tok, ids, experts, capacity=0):
 
 
 @pytest.mark.parametrize("n,k,experts", [(0, 1, 3), (1, 1, 1), (1, 8, 4096), (31, 2, 5), (255, 4, 8), (1024, 2, 64), (1025, 2, 1),
-                                         (4096, 8, 60), (5000, 6, 256), (3000, 3, 1024), (2500, 7, 4000), (70_000, 8, 128),
+                                         (4096, 8, 60), (5000, 6, 256), (3000, 3, 1024), (2500, 7, 4000), (8192, 2, 60), (16_385, 1, 64), (65_536, 1, 4096), (65_537, 1, 128), (70_000, 8, 128),
                                          (9000, 64, 16)])
 @pytest.mark.parametrize("capacity", [0, 1, 100])
 @pytest.mark.parametrize("wide", [False, True])
