@@ -193,10 +193,26 @@ struct FastTerm {
 };
 __device__ __forceinline__ int64_t units(int high, int low) { return (int64_t)high * 0x400000 + low; }
 
-// How far from its token's borders a draw by FastTerm must lie to be taken, in units of 2^-44 of rows whose terms add up to 2^(fine - 1) to
-// 2^fine: the terms of both rows, and their sums, move the running sum and v times the whole one by 4 * 2^-31.5 together, their
-// rounding to units by two for each token.
-__device__ __forceinline__ int64_t fast_margin(int cols, int fine) { return ((int64_t)1 << (15 + fine)) + 2 * (int64_t)cols; }
+// How far from its token's borders a draw by FastTerm must lie to be taken, in units of 2^-44: the terms' rounding to units moves the running sum
+// and v times the whole one by two for each token, ratios and products round down; and their errors e = 2^-31.5 count with (1 - v) up
+// to the border and with v behind it, in all (1 - v) below + v behind: with P of p's terms below, `all` of them, half of e times all for most borders.
+// The ratio of the rows' sums, between 1/2 and 2, is off by 2 e of itself, by 2^-30 for its last digit and as much for its divisor's, which
+// moves both sides of q's: |Q - v all|.
+// P and Q are those before the token's piece, dP and dQ the piece's.
+__device__ __forceinline__ int64_t rounding_margin(int cols) { return 2 * (int64_t)cols + 8; }
+__device__ __forceinline__ int64_t term_margin(float v, int64_t P, int64_t dP, int64_t all_p, int64_t Q, int64_t dQ, int64_t all_q)
+{
+    constexpr float E = 0x1.7p-32f, RATIO = 4 * E + 0x1p-29f;        // (2^-31.5 = 0x1.6a1p-32)
+    v = fminf(fmaxf(v, 0.0f), 1.0f);
+    const float w = __fsub_rn(1.0f, v), p = __ll2float_rn(P + dP), q = __ll2float_rn(Q + dQ);
+    const float of_p = __fmaf_rn(w, p, __fmul_rn(v, __ll2float_rn(all_p - P)));
+    const float of_q = __fmaf_rn(w, q, __fmul_rn(v, __ll2float_rn(all_q - Q)));
+    const float shift = __fadd_rn(fabsf(__fmaf_rn(-v, __ll2float_rn(all_q), q)), __ll2float_rn(dQ));
+    const float margin = __fmaf_rn(E, __fadd_rn(of_p, __fmul_rn(2.0f, of_q)), __fmul_rn(RATIO, shift));
+    return __float2ll_ru(__fmul_rn(margin, 1.001f));
+}
+// what counts as near p = q, and how far off the statistics may be for it to hold all that they may have on the wrong side
+constexpr float NEAR = 0x1p-16f, NEAR_OFF = 0x1p-17f;
 
 // ------------------------------------------------------------------ shared by the blocks of a sequence
 struct Shared {
@@ -215,7 +231,8 @@ struct Shared {
     // a draw by FastTerm: sums of the rows' terms, and of those of the tokens that count, by warp and over the block; what lies near p = q
     int64_t fast_warp[4][16], fast[4];
     float near_warp[16], near;
-    int64_t low_p, low_q, margin;       // the sums of lower blocks
+    int64_t low_p, low_q, all_p, all_q; // the sums of lower blocks, of all
+    int64_t margin;
     uint32_t ratio;                     // of the rows' sums, in units of 2^-30
     float2 table[256], fast_table[STEPS];
     int64_t weight[1];                  // of each of the block's pieces (as many as there are); with FastTerm p's, then q's
@@ -514,7 +531,7 @@ struct Walk {
     // The same by FastTerm in one pass, with sh.unsure set where it may not be that token.  The weights are p - (SP / SQ) q of the tokens where that is
     // positive, SP and SQ the rows' sums, which are known at the end of the pass only; so what is summed are the terms of p and those of q, over all
     // tokens and over those where p / s > q / s', s and s' the sums as the 32-bit statistics have them.  A token is taken for the wrong side only
-    // where p and q differ by less than the statistics' error, and that error times the probability of the tokens near p = q (to 2^-12 of p) bounds
+    // where p and q differ by less than the statistics' error, and that error times the probability of the tokens near p = q (to NEAR of p) bounds
     // what it adds.
     template <bool LESS>
     __device__ __forceinline__ int fast_draw(const Row<T> &p, const Row<T> &q, int without, float v, float &logit)
@@ -545,7 +562,7 @@ struct Walk {
                     term(z[u], y[u], sh.fast_table, c, h, l);
                     ph += h[0], pl += l[0], qh += h[1], ql += l[1];
                     const float a = __fmul_rn(c[0], p_inv), over = __fmaf_rn(-c[1], q_inv, a);
-                    if (fabsf(over) <= __fmul_rn(a, 0x1p-12f)) near = __fadd_rn(near, a);
+                    if (fabsf(over) <= __fmul_rn(a, NEAR)) near = __fadd_rn(near, a);
                     if (over > 0.0f) aph += h[0] - HIGH0, apl += l[0] - LOW0, aqh += h[1] - HIGH0, aql += l[1] - LOW0;
                 }
             } else {
@@ -604,14 +621,14 @@ struct Walk {
                 close = __fadd_rn(close, o->near);
                 if (b < rank) low_p += o->fast[0], low_q += o->fast[1];
             }
-            sh.low_p = low_p, sh.low_q = low_q;
-            sh.ratio = 0, sh.margin = fast_margin(cols, fine), sh.unsure = false;
+            sh.low_p = low_p, sh.low_q = low_q, sh.all_p = all[0], sh.all_q = all[1];
+            sh.ratio = 0, sh.margin = rounding_margin(cols), sh.unsure = false;
             if (LESS) {
                 sh.ratio = (uint32_t)(((uint64_t)(all[2] >> fine) << 18) / (uint64_t)max((long long)(all[3] >> fine >> 12), 1ll));
                 // the statistics' error, from what the sums have come to
                 const float x = __fmul_rn(__fdiv_rn(__ll2float_rn(all[2]), __ll2float_rn(all[3])), __fdiv_rn(p_inv, q_inv));
                 const float off = __fadd_rn(fabsf(__fsub_rn(x, 1.0f)), 0x1p-20f);
-                sh.unsure = !(off < 0x1p-13f);
+                sh.unsure = !(off < NEAR_OFF);
                 sh.margin += __float2ll_rn(__fmul_rn(__fmul_rn(off, __fmul_rn(close, 1.01f)), __int_as_float((127 + 44 + fine) << 23)));
             }
             const int64_t total = all[0] - less(all[1], sh.ratio);
@@ -620,7 +637,7 @@ struct Walk {
         }
         cluster.sync();                  // the others' sums have been read
         int found = -1;
-        const int64_t at = sh.at, margin = sh.margin;
+        const int64_t at = sh.at;
         const uint32_t ratio = sh.ratio;
         int64_t P = sh.low_p, Q = sh.low_q;
         if (warp == 0 && !sh.unsure && at >= P - less(Q, ratio) && at < P + sh.fast[0] - less(Q + sh.fast[1], ratio)) {
@@ -662,7 +679,10 @@ struct Walk {
                     wq[u] = LESS && counts ? units(h[1] - HIGH0, l[1] - LOW0) : 0;
                     sum_p += wp[u], sum_q += wq[u];
                 }
-                P = sh.low_p + scan(sum_p) - sum_p, Q = LESS ? sh.low_q + scan(sum_q) - sum_q : 0;
+                const int64_t to_lane_p = scan(sum_p), to_lane_q = LESS ? scan(sum_q) : 0;
+                const int64_t margin = sh.margin + term_margin(v, sh.low_p, __shfl_sync(FULL, to_lane_p, 31), sh.all_p, LESS ? sh.low_q : 0,
+                                                               __shfl_sync(FULL, to_lane_q, 31), LESS ? sh.all_q : 0);
+                P = sh.low_p + to_lane_p - sum_p, Q = LESS ? sh.low_q + to_lane_q - sum_q : 0;
 #pragma unroll
                 for (int u = 0; u < N; ++u) {
                     const int64_t from = P - less(Q, ratio);

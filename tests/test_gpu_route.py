@@ -320,3 +320,28 @@ def test_refusals(tok):
                  lambda: pdb.pdb_route_join_grad(tok, rows, place, source, rows[:4], rows, dweight=w)):
         with pytest.raises(pdb.PdbError):
             call()
+
+
+@pytest.mark.parametrize("n,k,capacity", [(5000, 2, 0), (4000, 8, 900), (16_384, 4, 0), (16_384, 8, 2500)])
+def test_places_in_a_graph(tok, n, k, capacity):
+    # by one cluster of several blocks, and by two launches, beside calls of other sizes on the same handle
+    experts = 48
+    g = _gen(9)
+    ids = torch.randint(-1, experts, (n, k), device="cuda", generator=g)
+    place, source, ends = (torch.empty(s, device="cuda", dtype=torch.int32) for s in ((n, k), experts * capacity or n * k, experts))
+    other = torch.randint(0, experts, (17_000, 4), device="cuda", generator=g)
+    there = [torch.empty(s, device="cuda", dtype=torch.int32) for s in ((17_000, 4), 68_000, experts)]
+    graph, stream = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.graph(graph, stream=stream):
+        pdb.pdb_route(tok, other, experts, *there)
+        pdb.pdb_route(tok, ids, experts, place, source, ends, capacity=capacity)
+        pdb.pdb_route(tok, other, experts, *there)
+    torch.cuda.current_stream().wait_stream(stream)
+    for _ in range(3):
+        ids.copy_(torch.randint(-1, experts, (n, k), device="cuda", generator=g))
+        for t in (place, source, ends):
+            t.fill_(-7)
+        graph.replay()
+        assert all(torch.equal(a, b.cpu()) for a, b in zip(_want_places(ids, experts, capacity), (place, source, ends)))
+        assert torch.equal(there[2], torch.bincount(other.view(-1), minlength=experts).cumsum(0).int())
