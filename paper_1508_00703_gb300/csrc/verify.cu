@@ -10,7 +10,7 @@
 //
 // Which token comes out must not hang on how a row is split or on 32-bit rounding: of 128,000 tokens the running sums of p lie so close that
 // 32-bit ones would pick a neighbour in one draw of thirty.  So acceptances are taken from the statistics only where their error cannot
-// matter (2^-12 apart), and draws from terms good to 2^-31.5, summed as whole numbers (FastTerm), only where those cannot matter; the others, about 1 of
+// matter (2^-14.6 apart for most tokens), and draws from terms good to 2^-31.5, summed as whole numbers (FastTerm), only where those cannot matter; the others, about 1 of
 // 150 draws from 128,000 tokens, are decided on terms good to 2^-42 (exp_two).
 //
 // What bounds it.  256 sequences of 5 drafts, 128,000 bf16 tokens, four of five accepted: 205 us; 463 MB, 69 us at the copy rate, 115 by
@@ -708,9 +708,11 @@ struct VerifyOut {
     float *logp;
 };
 
-// How far the two sides of an acceptance must lie apart for the statistics in 32 bits to decide it.  Their exponentials' arguments
-// x (in powers of two) are off by 2.1 |x| 2^-24 with |x| < 126 where they count, sums by the mean of that and their roundings: 2^-14.
-constexpr float SURE = 0x1p-12f;
+// How far the two sides of an acceptance must lie apart for the statistics in 32 bits to decide it, in units of 2^-24 of the larger.
+// An exponential's argument x (in powers of two) is off by 3.2 |x| units (the difference, its product, scale log2(e)), the power by
+// 2.25 |x| + 4.  A row's sum has that by the mean over its mass, where |x| is at most log2(cols) (the entropy) and the references differ by 16, and
+// the roundings of five powers, of chains and joins: 2.25 * 37 + 25 + 91 for 2^21 fp32 tokens, 199 a row.  With divisions and u 411.
+constexpr float SURE_ROWS = 512.0f, SURE_X = 2.25f;
 
 // a row's m, s and its logit of the drafted token, from k_verify_rows
 struct Given {
@@ -724,11 +726,16 @@ enum { DRAW_REST = 0, DRAW_TARGET = 1, NOTHING = 2, EXACTLY = 3 };
 template <typename T>
 __device__ __forceinline__ bool accepts(const Row<T> &p, const Row<T> &q, float z, float zq, float u, bool &sure)
 {
-    const float right = __fdiv_rn(ex2(__fmul_rn(__fsub_rn(z, p.m), __fmul_rn(p.scale, LOG2E))), p.s);
-    float left = u;
-    if (q.z) left = __fmul_rn(u, __fdiv_rn(ex2(__fmul_rn(__fsub_rn(zq, q.m), __fmul_rn(q.scale, LOG2E))), q.s));
+    const float x = __fmul_rn(__fsub_rn(z, p.m), __fmul_rn(p.scale, LOG2E)), right = __fdiv_rn(ex2(x), p.s);
+    float left = u, y = 0.0f;
+    if (q.z) {
+        y = __fmul_rn(__fsub_rn(zq, q.m), __fmul_rn(q.scale, LOG2E));
+        left = __fmul_rn(u, __fdiv_rn(ex2(y), q.s));
+    }
+    // a power below the normal numbers is 0, however far
+    const float margin = __fmaf_rn(SURE_X, fminf(-x, 150.0f) + fminf(-y, 150.0f), SURE_ROWS);
     const float more = fmaxf(left, right);
-    sure = fabsf(left - right) > SURE * more && more > 1e-30f;
+    sure = fabsf(left - right) > 0x1p-24f * margin * more && more > 1e-30f;
     return left < right;
 }
 
