@@ -10,12 +10,12 @@
 //
 // Which token comes out must not hang on how a row is split or on 32-bit rounding: of 128,000 tokens the running sums of p lie so close that
 // 32-bit ones would pick a neighbour in one draw of thirty.  So acceptances are taken from the statistics only where their error cannot
-// matter (2^-14.6 apart for most tokens), and draws from terms good to 2^-31.5, summed as whole numbers (FastTerm), only where those cannot matter; the others, about 1 of
-// 150 draws from 128,000 tokens, are decided on terms good to 2^-42 (exp_two).
+// matter (2^-14.6 apart for most tokens), and draws from terms good to 2^-31.5, summed as whole numbers (FastTerm), only where those cannot matter; the others, one
+// of 2500 sequences with 5 drafts of 128,000 tokens, are decided on terms good to 2^-42 (exp_two).
 //
-// What bounds it.  256 sequences of 5 drafts, 128,000 bf16 tokens, four of five accepted: 205 us; 463 MB, 69 us at the copy rate, 115 by
+// What bounds it.  256 sequences of 5 drafts, 128,000 bf16 tokens, four of five accepted: 211 us; 463 MB, 69 us at the copy rate, 115 by
 // a kernel that walks only (cluster barriers between positions: 4.1 TB/s), and 100 by one that draws only (71 instructions for a token of both
-// rows, at 2.1 of 4 issued a cycle).  One sequence of 4 drafts: 17.5 us, two launches, seven cluster barriers and four passes of latency.
+// rows, at 2.1 of 4 issued a cycle).  One sequence of 4 drafts: 16.6 us, two launches, seven cluster barriers and four passes of latency.
 #include <algorithm>
 #include <cmath>
 
@@ -847,8 +847,8 @@ __device__ __forceinline__ bool in_reach(const Row<T> &r)
 }
 
 // A cluster for each sequence: its walk (bound by memory) up to the first position that is not accepted, and its draw (bound by instructions).
-// On an SM some sequences walk while others draw; in a kernel each they take as long, and the few whose draw has to be
-// exact (under 1 of 100, 50 us by eight blocks) are not hidden then (256 x 5 drafts x 128,000 bf16: 115 us, 100, 55).
+// On an SM some sequences walk while others draw; in a kernel each they take as long, and the few that have to be
+// exact (1 of 2500, 50 us by eight blocks) are not hidden then (256 x 5 drafts x 128,000 bf16: 115 us, 100, 50).
 constexpr int MANY_THREADS = 256, FEW_THREADS = 512, MANY_PER_SM = 3;
 
 template <typename T, int THREADS>
