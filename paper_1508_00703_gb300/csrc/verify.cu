@@ -90,10 +90,10 @@ __device__ __forceinline__ Two exp_two(float z, float m, float scale, const floa
     const float2 tab = table[n & 255];
     const float ph = __fmul_rn(tab.x, r), pl = __fmaf_rn(tab.x, r, -ph);
     const float low = __fadd_rn(pl, __fmaf_rn(tab.x, w, __fmaf_rn(tab.y, r, tab.y)));
-    const float h = __fadd_rn(tab.x, ph), hl = __fadd_rn(__fsub_rn(tab.x, h), ph);
+    const float h = __fadd_rn(tab.x, ph), l = __fadd_rn(__fadd_rn(__fsub_rn(tab.x, h), ph), low);
+    const float sum = __fadd_rn(h, l), rest = __fadd_rn(__fsub_rn(h, sum), l);
     const float power = __int_as_float(((n >> 8) + 127) << 23);
-    const float l = __fadd_rn(hl, low);
-    return {__fmul_rn(h, power), __fmul_rn(l, power)};
+    return {__fmul_rn(sum, power), __fmul_rn(rest, power)};
 }
 
 __device__ __forceinline__ Two times(Two a, Two b)
@@ -108,16 +108,16 @@ __device__ __forceinline__ Two inverse_of(Two a)
     return {h, __fmul_rn(h, __fmaf_rn(-a.lo, h, __fmaf_rn(-a.hi, h, 1.0f)))};
 }
 
-// A sum of numbers from 0 to 1 in units of 2^-46: the units of 2^-23, and what is left of them, each taken from the lowest bits of a
-// float that is large enough (a conversion to 64 bits takes 16 cycles an SM for each warp).
+// A sum of numbers from 0 to 1 in units of 2^-46: the units of 2^-23, taken from the lowest bits of a float that is large enough, and what is
+// left, which with the second float can be 1.5 * 2^-24 and so is more than such bits hold (a conversion to 64 bits for both takes 16 cycles an
+// SM for each warp).
 struct Units {
     int high = 0, low = 0;
     __device__ __forceinline__ void add(Two a)
     {
         const float h = __fmaf_rn(a.hi, 0x1p23f, 8388608.0f);
         const float rest = __fadd_rn(__fmaf_rn(__fsub_rn(h, 8388608.0f), -0x1p-23f, a.hi), a.lo);
-        const float l = __fmaf_rn(rest, 0x1p46f, 12582912.0f);
-        high += __float_as_int(h) - 0x4b000000, low += __float_as_int(l) - 0x4b400000;
+        high += __float_as_int(h) - 0x4b000000, low += __float2int_rn(__fmul_rn(rest, 0x1p46f));
     }
     __device__ __forceinline__ int64_t whole() const { return ((int64_t)high << 23) + low; }
 };

@@ -321,3 +321,60 @@ def test_refusals(tok):
         args.update(kw)
         with pytest.raises(pdb.PdbError):
             pdb.pdb_verify(tok, **args)
+
+
+def _wide_softmax(row, scale):
+    np = pytest.importorskip("numpy")
+    x = row.double().cpu().numpy().astype(np.longdouble) * np.longdouble(float(torch.tensor(scale, dtype=torch.float32)))
+    e = np.exp(x - x.max())
+    return e / e.sum()
+
+
+def _close_calls(weights, n, seed):
+    """n numbers in fp32 that lie 2^-36 to 2^-28 of the rows' sums from a border of the weights' running ones, and the tokens that they mean.  (The
+    kernel's last resort rounds each of V weights to 2^-46 of the rows' sums: V^0.5 2^-47.8 together, 8 times that for V = 128,000 is 2^-36.3;
+    of what p - q comes to it is more, by 1 / sum(p - q).)"""
+    import numpy as np
+    upto = np.cumsum(weights)
+    border = upto / upto[-1]
+    v = border.astype(np.float32)
+    off = np.abs(v.astype(np.longdouble) - border) * upto[-1]
+    where = np.nonzero((off > 2.0 ** -36) & (off < 2.0 ** -28) & (v > 0) & (v < 1) & (weights > 0))[0]
+    # as many of each size
+    size = np.floor(np.log2(off[where].astype(np.float64))).astype(int)
+    r = np.random.default_rng(seed)
+    chosen = np.concatenate([r.permutation(where[size == e])[:-(-n // 8)] for e in range(-36, -28)])[:n]
+    v = v[chosen]
+    return torch.from_numpy(v).cuda(), [int(np.sum(border <= np.longdouble(x))) for x in v]
+
+
+@pytest.mark.parametrize("vocab,kind,scale", [(128_000, "bf16", 1.0), (128_000, "f32", 0.7), (32_001, "f16", 1.0), (50_000, "f32", 2.0), (128_000, "bf16", 0.01)])
+@pytest.mark.parametrize("few", [False, True])
+def test_numbers_close_to_borders(tok, vocab, kind, scale, few):
+    # where the draw's margin decides: from p, from p - q, and from p without a token
+    dtype = TYPES[kind]
+    z = (torch.randn(1, vocab, device="cuda", generator=_gen(vocab)) * 2).to(dtype)
+    y = (z.float() + 0.3 * torch.randn(1, vocab, device="cuda", generator=_gen(vocab + 1))).to(dtype)
+    p, q = _wide_softmax(z[0], scale), _wide_softmax(y[0], scale)
+    n, few_rows = 140, 20
+    ran = 0
+    for form in ("p", "p - q", "without"):
+        t = int((q - p).argmax()) if form == "p - q" else int(p.argmin())
+        w = p.copy()
+        if form == "p - q":
+            w = (p - q).clip(min=0)
+        elif form == "without":
+            w[t] = 0
+        v, want = _close_calls(w, n, vocab)
+        ran += len(want)
+        D = 0 if form == "p" else 1
+        for s0 in range(0, len(want), few_rows if few else n):
+            part = v[s0:s0 + few_rows if few else None]
+            m = part.numel()
+            ids = torch.full((m, D), t, device="cuda", dtype=torch.int32)
+            u = torch.ones(m, D, device="cuda")
+            rows = z.expand(m * (D + 1), vocab).contiguous()
+            tokens, accepted, _ = _call(tok, rows, ids, u, part, y.expand(m, vocab).contiguous() if form == "p - q" else None, scale, scale)
+            assert (accepted == 0).all()
+            assert tokens[:, 0].tolist() == want[s0:s0 + m], form
+    assert ran >= 100

@@ -24,6 +24,7 @@ static float __fdiv_rn(float a, float b) { return a / b; }
 static float __fmaf_rn(float a, float b, float c) { return fmaf(a, b, c); }
 static float __ll2float_rn(int64_t x) { return (float)x; }
 static int64_t __float2ll_rn(float x) { return llrintf(x); }
+static int __float2int_rn(float x) { return (int)lrintf(x); }
 static int __float_as_int(float f) { int i; memcpy(&i, &f, 4); return i; }
 static uint32_t __float_as_uint(float f) { uint32_t i; memcpy(&i, &f, 4); return i; }
 static float __int_as_float(int i) { float f; memcpy(&f, &i, 4); return f; }
@@ -55,7 +56,7 @@ int main()
     for (int i = 0; i < STEPS; ++i) fast[i] = {FAST_TABLE.hi[i], FAST_TABLE.lo[i]};
     std::mt19937_64 g(1);
     std::uniform_real_distribution<double> U(0, 1);
-    double rel = 0, absolute = 0, fast_rel = 0, units_off = 0;
+    double rel = 0, absolute = 0, fast_rel = 0, units_off = 0, whole_off = 0;
     for (int k = 0; k < 400000; ++k) {
         const float m = (float)((U(g) - 0.5) * (k % 3 ? 40 : 400)), scale = k % 2 ? 1.0f : (float)(0.05 + U(g) * (k % 3 ? 3 : 1));
         float z = m - (float)(U(g) * (k % 7 ? 30 : 1e-3) / scale);
@@ -66,6 +67,10 @@ int main()
             const Two t = exp_two(z, m, scale, table);
             const double off = (double)fabsl((long double)t.hi + (long double)t.lo - e);
             if (x > -12) rel = fmax(rel, off / (double)e);
+            Units one;
+            one.add(t);
+            whole_off = fmax(whole_off, (double)fabsl(ldexpl((long double)one.whole(), -46) - (long double)t.hi - (long double)t.lo));
+            if (fabsf(t.lo) > t.hi * 0x1p-24f) units_off = 4;
             absolute = fmax(absolute, off);
         }
         if (fabsf(m * scale * LOG2E) >= REACH || x < -40) continue;
@@ -96,7 +101,24 @@ int main()
     const Two inv = inverse_of({3.0f, 1e-9f}), sum = two_of(((int64_t)5 << 23) + 7, -3);
     const double inv_off = fabs(((double)inv.hi + (double)inv.lo) * (3.0 + (double)1e-9f) - 1.0);
     const double sum_off = fabs((double)sum.hi + (double)sum.lo - (5.0 + 7 * 0x1p-23 - 3 * 0x1p-46));
-    printf("%.17g %.17g %.17g %.17g %.17g %.17g\n", rel, absolute, fast_rel, units_off, inv_off, sum_off);
+    // a row's sum as the kernel forms it
+    double row_off = 0;
+    for (int row = 0; row < 20; ++row) {
+        int64_t high = 0, low = 0;
+        long double all = 1;
+        Units one;
+        one.add(exp_two(3.0f, 3.0f, 1.0f, table));
+        high += one.high, low += one.low;
+        for (int k = 0; k < 30000; ++k) {
+            const float z = (float)(3.0 - U(g) * (row + 1));
+            Units more;
+            more.add(exp_two(z, 3.0f, 1.0f, table));
+            high += more.high, low += more.low, all += expl((long double)z - 3);
+        }
+        const Two of_row = two_of(high, low);
+        row_off = fmax(row_off, fabs((double)(((long double)of_row.hi + (long double)of_row.lo) / all - 1)));
+    }
+    printf("%.17g %.17g %.17g %.17g %.17g %.17g %.17g %.17g\n", rel, absolute, fast_rel, units_off, inv_off, sum_off, whole_off, row_off);
 }
 """
 
@@ -127,3 +149,9 @@ def test_fast_term(measured):
 
 def test_sums_and_reciprocals(measured):
     assert measured[4] <= 2.0 ** -45 and measured[5] <= 2.0 ** -46
+
+
+def test_units(measured):
+    # a rounding to units, and one of what is left (below 2^-23) as a float; so is a row's sum as good as its terms
+    assert measured[6] <= 2.0 ** -47 + 2.0 ** -48
+    assert measured[7] <= 2.0 ** -40.5
