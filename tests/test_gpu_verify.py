@@ -378,3 +378,36 @@ def test_numbers_close_to_borders(tok, vocab, kind, scale, few):
             assert (accepted == 0).all()
             assert tokens[:, 0].tolist() == want[s0:s0 + m], form
     assert ran >= 100
+
+
+@pytest.mark.parametrize("vocab,kind,scale", [(128_000, "bf16", 1.0), (128_000, "f32", 0.7), (32_001, "f16", 1.0), (50_000, "f32", 2.0), (128_000, "bf16", 0.01)])
+@pytest.mark.parametrize("few", [False, True])
+def test_acceptances_close_to_equal(tok, vocab, kind, scale, few):
+    # u q and p from 2^-12 to 2^-36 apart, by halves: from where the statistics decide to where the terms do, which are good to 2^-40.5 each
+    import numpy as np
+    dtype = TYPES[kind]
+    z = (torch.randn(1, vocab, device="cuda", generator=_gen(vocab + 2)) * 2).to(dtype)
+    y = (z.float() + 0.3 * torch.randn(1, vocab, device="cuda", generator=_gen(vocab + 3))).to(dtype)
+    p, q = _wide_softmax(z[0], scale), _wide_softmax(y[0], scale)
+    r = np.random.default_rng(vocab)
+    tokens, numbers = [], []
+    likely = np.nonzero(q > p)[0]
+    for size in range(-36, -12):
+        for sign in (-1, 1):
+            t = r.choice(likely, 4000)
+            u = (p[t] / q[t] * (1 + sign * 2.0 ** (size + 0.5))).astype(np.float32)
+            off = u.astype(np.longdouble) * q[t] / p[t] - 1
+            ok = np.nonzero((off * sign > 2.0 ** size) & (off * sign < 2.0 ** (size + 1)) & (u < 1))[0][:3]
+            tokens += t[ok].tolist()
+            numbers += u[ok].tolist()
+    assert len(tokens) >= 100
+    want = [float(np.longdouble(np.float32(u)) * q[t] - p[t]) < 0 for t, u in zip(tokens, numbers)]
+    step = 20 if few else len(tokens)
+    for s0 in range(0, len(tokens), step):
+        part = tokens[s0:s0 + step]
+        m = len(part)
+        ids = torch.tensor(part, device="cuda", dtype=torch.int32).view(m, 1)
+        u = torch.tensor(numbers[s0:s0 + step], device="cuda", dtype=torch.float32).view(m, 1)
+        _, accepted, _ = _call(tok, z.expand(2 * m, vocab).contiguous(), ids, u, torch.full((m,), 0.5, device="cuda"), y.expand(m, vocab).contiguous(),
+                               scale, scale)
+        assert accepted.tolist() == [int(x) for x in want[s0:s0 + step]]
