@@ -15,7 +15,7 @@
 //
 // What bounds it.  256 sequences of 5 drafts, 128,000 bf16 tokens, four of five accepted: 211 us; 463 MB, 69 us at the copy rate, 115 by
 // a kernel that walks only (cluster barriers between positions: 4.1 TB/s), and 100 by one that draws only (71 instructions for a token of both
-// rows, at 2.1 of 4 issued a cycle).  One sequence of 4 drafts: 16.6 us, two launches, seven cluster barriers and four passes of latency.
+// rows, at 2.1 of 4 issued a cycle).  One sequence of 4 drafts: 15.7 us, two launches, seven cluster barriers and four passes of latency.
 #include <algorithm>
 #include <cmath>
 
