@@ -11,7 +11,7 @@
 // Which token comes out must not hang on how a row is split or on 32-bit rounding: of 128,000 tokens the running sums of p lie so close that
 // 32-bit ones would pick a neighbour in one draw of thirty.  So acceptances are taken from the statistics only where their error cannot
 // matter (2^-14.6 apart for most tokens), and draws from terms good to 2^-31.5, summed as whole numbers (FastTerm), only where those cannot matter; the others, one
-// of 2500 sequences with 5 drafts of 128,000 tokens, are decided on terms good to 2^-42 (exp_two).
+// of 2500 sequences with 5 drafts of 128,000 tokens, are decided on terms good to 2^-40 (exp_two), summed as whole numbers of 2^-92 (Units).
 //
 // What bounds it.  256 sequences of 5 drafts, 128,000 bf16 tokens, four of five accepted: 211 us; 463 MB, 69 us at the copy rate, 115 by
 // a kernel that walks only (cluster barriers between positions: 4.1 TB/s), and 100 by one that draws only (71 instructions for a token of both
@@ -68,7 +68,7 @@ struct Two {
     float hi, lo;                       // hi + lo, |lo| <= ulp(hi)
 };
 
-// exp(scale * (z - m)), z <= m; 0 below e^-45 (a part of 2^-64 of the row's sum)
+// exp(scale * (z - m)), z <= m; 0 below e^-63 (2^-90.9)
 __device__ __forceinline__ Two exp_two(float z, float m, float scale, const float2 *table)
 {
     // z - m and its product with scale, exactly but for the last 2^-48
@@ -76,7 +76,7 @@ __device__ __forceinline__ Two exp_two(float z, float m, float scale, const floa
     const float dl = __fsub_rn(__fsub_rn(z, __fsub_rn(d, b)), __fadd_rn(m, b));
     const float x = __fmul_rn(d, scale);
     const float xl = __fmaf_rn(dl, scale, __fmaf_rn(d, scale, -x));
-    if (!(x >= -45.0f)) return {0.0f, 0.0f};
+    if (!(x >= -63.0f)) return {0.0f, 0.0f};
     const float t = __fadd_rn(__fmul_rn(x, PER_STEP), 12582912.0f);       // 1.5 * 2^23: rounds to a whole number
     const int n = __float_as_int(t) - 0x4b400000;
     const float nf = __fsub_rn(t, 12582912.0f);
@@ -108,26 +108,81 @@ __device__ __forceinline__ Two inverse_of(Two a)
     return {h, __fmul_rn(h, __fmaf_rn(-a.lo, h, __fmaf_rn(-a.hi, h, 1.0f)))};
 }
 
-// A sum of numbers from 0 to 1 in units of 2^-46: the units of 2^-23, taken from the lowest bits of a float that is large enough, and what is
-// left, which with the second float can be 1.5 * 2^-24 and so is more than such bits hold (a conversion to 64 bits for both takes 16 cycles an
-// SM for each warp).
+// a + b, exactly
+__device__ __forceinline__ Two sum_of(float a, float b)
+{
+    const float s = __fadd_rn(a, b), c = __fsub_rn(s, a);
+    return {s, __fadd_rn(__fsub_rn(a, __fsub_rn(s, c)), __fsub_rn(b, c))};
+}
+
+// A sum of numbers from 0 to 1 in units of 2^-92, so that a term of a long tail keeps its digits beside a row's largest (rounded to 2^-46 of
+// it, the 128,000 equal terms of a tail 2^-29 below it would be off by up to 2^-18 of themselves all in one direction, half a token's
+// weight in all).  The units of 2^-23 are taken from the lowest bits of a float that is large enough; what is left can with the second float be
+// 1.5 * 2^-24 and so is more than such bits hold; and what that leaves.
 struct Units {
-    int high = 0, low = 0;
+    int high = 0, low = 0, fine = 0, finest = 0;            // units of 2^-23, 2^-46, 2^-69, 2^-92
     __device__ __forceinline__ void add(Two a)
     {
         const float h = __fmaf_rn(a.hi, 0x1p23f, 8388608.0f);
-        const float rest = __fadd_rn(__fmaf_rn(__fsub_rn(h, 8388608.0f), -0x1p-23f, a.hi), a.lo);
-        high += __float_as_int(h) - 0x4b000000, low += __float2int_rn(__fmul_rn(rest, 0x1p46f));
+        const Two rest = sum_of(__fmaf_rn(__fsub_rn(h, 8388608.0f), -0x1p-23f, a.hi), a.lo);
+        const int l = __float2int_rn(__fmul_rn(rest.hi, 0x1p46f));
+        const Two more = sum_of(__fmaf_rn((float)l, -0x1p-46f, rest.hi), rest.lo);
+        const int f = __float2int_rn(__fmul_rn(more.hi, 0x1p69f));
+        const float last = __fadd_rn(__fmaf_rn((float)f, -0x1p-69f, more.hi), more.lo);
+        high += __float_as_int(h) - 0x4b000000, low += l, fine += f;
+        finest += __float2int_rn(__fmul_rn(__fmul_rn(last, 0x1p46f), 0x1p46f));
     }
-    __device__ __forceinline__ int64_t whole() const { return ((int64_t)high << 23) + low; }
+    __device__ __forceinline__ int64_t whole() const { return ((int64_t)high << 23) + low; }          // of 2^-46
+    __device__ __forceinline__ int64_t rest() const { return (int64_t)fine * 0x800000 + finest; }     // of 2^-92
 };
-// (high * 2^23 + low) * 2^-46
-__device__ __forceinline__ Two two_of(int64_t high, int64_t low)
+// (high * 2^23 + low) * 2^-46 + rest * 2^-92
+__device__ __forceinline__ Two two_of(int64_t high, int64_t low, int64_t rest = 0)
 {
     high += low >> 23, low &= 0x7fffff;
     const float h = __ll2float_rn(high);
-    const int64_t rest = high - __float2ll_rn(h);
-    return {__fmul_rn(h, 0x1p-23f), __fmul_rn(__ll2float_rn(rest * 0x800000 + low), 0x1p-46f)};
+    const int64_t left = high - __float2ll_rn(h);
+    const float l = __fmaf_rn(__ll2float_rn(rest), 0x1p-46f, __ll2float_rn(left * 0x800000 + low));
+    return {__fmul_rn(h, 0x1p-23f), __fmul_rn(l, 0x1p-46f)};
+}
+
+// whole numbers of 2^-92
+typedef __int128 Wide;
+constexpr int64_t REST = ((int64_t)1 << 46) - 1;
+__device__ __forceinline__ Wide wide(int64_t whole, int64_t rest) { return (Wide)whole * (REST + 1) + rest; }
+__device__ __forceinline__ Two two_of(Wide x)
+{
+    const int64_t whole = (int64_t)(x >> 46);
+    return two_of(whole >> 23, whole & 0x7fffff, (int64_t)x & REST);
+}
+
+// max(a, 0) in units of 2^-46, and the rest of 2^-92
+struct Weight {
+    int64_t whole, rest;
+};
+__device__ __forceinline__ Weight weight_of(Two a)
+{
+    if (!(a.hi > 0.0f)) return {0, 0};
+    Units one;
+    one.add(a);
+    const int64_t rest = one.rest();
+    return {one.whole() + (rest >> 46), rest & REST};
+}
+// a - b
+__device__ __forceinline__ Two less_by(Two a, Two b)
+{
+    const Two d = sum_of(a.hi, -b.hi);
+    return sum_of(d.hi, __fadd_rn(d.lo, __fsub_rn(a.lo, b.lo)));
+}
+
+// floor(v * total), total - 1 at most (v from 1 on), 0 for a v below 0 or NaN; total below 2^103
+__device__ __forceinline__ Wide share_of_total(float v, Wide total)
+{
+    if (!(v > 0.0f)) return 0;
+    if (v >= 1.0f) return total - 1;
+    const uint32_t raw = __float_as_uint(v), e = raw >> 23;
+    const uint32_t digits = e ? (raw & 0x7fffff) | 0x800000 : raw & 0x7fffff;          // v = digits / 2^shift
+    const int shift = 150 - (int)(e ? e : 1);
+    return shift < 127 ? total * digits >> shift : 0;
 }
 
 // exp(scale (z - m)) 2^-down of two tokens at once, z <= m, where |m scale| log2(e) < 2^9, to 2^-31.5: n + f = 512 (z c - m c),
@@ -221,21 +276,22 @@ struct Shared {
     float z[2][2];                      // the rows' logits of the drafted token, for two positions in turn
     int drafted[MAX_DRAFTS];
     float u[MAX_DRAFTS];
-    int64_t warp_sum[2][16];
-    int64_t sum[2][2];                  // this block's sums of the two rows, in units of 2^-23 and 2^-46
+    Wide warp_sum[16];
+    Wide sum[2];                        // this block's sums of the two rows
     Two row_sum[2], row_inv[2];         // the rows' sums, and their reciprocals
-    int64_t total;                      // this block's weights
-    int64_t at, before;                 // the drawn place among all weights, the weights of lower blocks
-    int64_t below;                      // weights before the piece that holds the drawn token
+    Wide total;                         // this block's weights
+    Wide at, before;                    // the drawn place among all weights, the weights of lower blocks
+    Wide below;                         // weights before the piece that holds the drawn token
     int none, piece, good, unsure;
     // a draw by FastTerm: sums of the rows' terms, and of those of the tokens that count, by warp and over the block; what lies near p = q
     int64_t fast_warp[4][16], fast[4];
     float near_warp[16], near;
     int64_t low_p, low_q, all_p, all_q; // the sums of lower blocks, of all
+    int64_t fast_at;                    // the drawn place
     int64_t margin;
     uint32_t ratio;                     // of the rows' sums, in units of 2^-30
     float2 table[256], fast_table[STEPS];
-    int64_t weight[1];                  // of each of the block's pieces (as many as there are); with FastTerm p's, then q's
+    int64_t weight[1];                  // of each of the block's pieces (as many as there are), then the rests; with FastTerm p's, then q's
 };
 
 // one row of a position
@@ -364,86 +420,71 @@ struct Walk {
         }
     }
 
-    // sums of the warps' numbers, on thread 0
-    __device__ __forceinline__ int64_t block_sum(int64_t x, int64_t *part)
+    // the number of the lane `off` below, or across
+    static __device__ __forceinline__ Wide of_lane(Wide x, int off, bool across)
+    {
+        const uint64_t low = (uint64_t)x, high = (uint64_t)(x >> 64);
+        const uint64_t l = across ? __shfl_xor_sync(FULL, low, off) : __shfl_up_sync(FULL, low, off);
+        const uint64_t h = across ? __shfl_xor_sync(FULL, high, off) : __shfl_up_sync(FULL, high, off);
+        return (Wide)((unsigned __int128)h << 64 | l);
+    }
+    // the sum of the threads' numbers, on thread 0
+    __device__ __forceinline__ Wide block_sum(Wide x)
     {
 #pragma unroll
-        for (int off = 16; off >= 1; off >>= 1) x += __shfl_xor_sync(FULL, x, off);
-        if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = x;
+        for (int off = 16; off >= 1; off >>= 1) x += of_lane(x, off, true);
+        __syncthreads();                 // (the last sum has been read)
+        if ((threadIdx.x & 31) == 0) sh.warp_sum[threadIdx.x >> 5] = x;
         __syncthreads();
         if (threadIdx.x == 0)
-            for (int w = 1; w < THREADS / 32; ++w) x += part[w];
+            for (int w = 1; w < THREADS / 32; ++w) x += sh.warp_sum[w];
         return x;
     }
 
     // a row's sum lies between 2^(above - 1) and 2^above, but for the statistics' error
     static __device__ __forceinline__ int above(const Row<T> &r) { return (int)(__float_as_uint(__fmul_rn(r.s, 1.0f + 0x1p-10f)) >> 23) - 126; }
 
-    // The rows' sums good to 2^-42, into sh.row_sum and sh.row_inv.  Whole numbers are added up: no order of warps and blocks shows in
-    // them.
+    // The rows' sums, of terms good to 2^-40, into sh.row_sum and sh.row_inv.  Whole numbers are added up: no order of warps and
+    // blocks shows in them.
     __device__ __forceinline__ void sums(const Row<T> &p, const Row<T> &q)
     {
         constexpr int N = PIECE / 32;
 #pragma unroll 1
         for (int which = 0; which < (q.z ? 2 : 1); ++which) {
             const float m = which ? q.m : p.m, scale = which ? q.scale : p.scale;
-            int64_t high = 0, low = 0;
+            int64_t whole = 0, rest = 0;
             each_piece(which ? q.z : p.z, nullptr, [&](int, const T (&x)[N], const T (&)[N]) {
                 Units sum;
 #pragma unroll
                 for (int u = 0; u < N; ++u) sum.add(exp_two(to_float(x[u]), m, scale, sh.table));
-                high += sum.high, low += sum.low;
+                whole += sum.whole(), rest += sum.rest();
             });
-            high = block_sum(high, sh.warp_sum[0]), low = block_sum(low, sh.warp_sum[1]);
-            if (threadIdx.x == 0) sh.sum[which][0] = high, sh.sum[which][1] = low;
-            __syncthreads();
+            const Wide all = block_sum(wide(whole, rest));
+            if (threadIdx.x == 0) sh.sum[which] = all;
         }
         cluster.sync();
         if (threadIdx.x < (q.z ? 2 : 1)) {
-            int64_t high = 0, low = 0;
-            for (int b = 0; b < blocks; ++b) {
-                const int64_t *o = cluster.map_shared_rank(&sh, b)->sum[threadIdx.x];
-                high += o[0], low += o[1];
-            }
-            sh.row_sum[threadIdx.x] = two_of(high, low);
+            Wide all = 0;
+            for (int b = 0; b < blocks; ++b) all += cluster.map_shared_rank(&sh, b)->sum[threadIdx.x];
+            sh.row_sum[threadIdx.x] = two_of(all);
             sh.row_inv[threadIdx.x] = inverse_of(sh.row_sum[threadIdx.x]);
         }
         cluster.sync();                  // the others' sums have been read
     }
 
-    // tokens' weights in a draw, in units of 2^-46
+    // tokens' weights in a draw
     struct Weights {
         Row<T> p, q;
         Two p_inv, q_inv;
         int without;                     // a token left out
         const float2 *table;
-        __device__ __forceinline__ int64_t operator()(int j, T z, T y) const
+        __device__ __forceinline__ Weight operator()(int j, T z, T y) const
         {
             Two a = times(exp_two(to_float(z), p.m, p.scale, table), p_inv);
-            if (q.z) {
-                const Two b = times(exp_two(to_float(y), q.m, q.scale, table), q_inv);
-                const float d = __fsub_rn(a.hi, b.hi), e = __fsub_rn(d, a.hi);
-                const float dl = __fsub_rn(__fsub_rn(a.hi, __fsub_rn(d, e)), __fadd_rn(b.hi, e));
-                a = {d, __fadd_rn(dl, __fsub_rn(a.lo, b.lo))};
-            }
-            if (j == without || __fadd_rn(a.hi, a.lo) < 0.0f) return 0;
-            Units one;
-            one.add(a);
-            return one.whole();
+            if (q.z) a = less_by(a, times(exp_two(to_float(y), q.m, q.scale, table), q_inv));
+            return j == without ? Weight{0, 0} : weight_of(a);
         }
     };
-
-    // floor(v * total), total - 1 at most (v from 1 on), 0 for a v below 0 or NaN
-    static __device__ __forceinline__ int64_t share_of_total(float v, int64_t total)
-    {
-        if (!(v > 0.0f)) return 0;
-        if (v >= 1.0f) return total - 1;
-        const uint32_t raw = __float_as_uint(v), e = raw >> 23;
-        const uint64_t digits = e ? (raw & 0x7fffff) | 0x800000 : raw & 0x7fffff;      // v = digits / 2^shift
-        const int shift = 150 - (int)max(e, 1u);
-        const uint64_t high = __umul64hi(digits, (uint64_t)total), low = digits * (uint64_t)total;
-        return (int64_t)(shift < 64 ? high << (64 - shift) | low >> shift : shift < 128 ? high >> (shift - 64) : 0);
-    }
 
     // inclusive sums over the lanes
     static __device__ __forceinline__ int64_t scan(int64_t x)
@@ -454,6 +495,20 @@ struct Walk {
             if ((int)(threadIdx.x & 31) >= off) x += y;
         }
         return x;
+    }
+    static __device__ __forceinline__ Wide scan(Wide x)
+    {
+#pragma unroll
+        for (int off = 1; off < 32; off <<= 1) {
+            const Wide y = of_lane(x, off, false);
+            if ((int)(threadIdx.x & 31) >= off) x += y;
+        }
+        return x;
+    }
+    // the sum of the lanes' numbers, from 0 to 2^53
+    static __device__ __forceinline__ int64_t lanes_sum(int64_t x)
+    {
+        return ((int64_t)__reduce_add_sync(FULL, (unsigned)(x >> 27)) << 27) + __reduce_add_sync(FULL, (unsigned)x & 0x7ffffff);
     }
     // a lane's neighbouring tokens of a piece
     template <int N>
@@ -472,22 +527,28 @@ struct Walk {
     {
         constexpr int N = PIECE / 32;
         const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-        int64_t all = 0;                 // on lane 0
+        Wide all = 0;                    // on lane 0
+        int64_t *const rest = sh.weight + pieces;
         each_piece(weight.p.z, weight.q.z, [&](int i, const T (&z)[N], const T (&y)[N]) {
-            uint64_t own = 0;
+            Weight own = {0, 0};
 #pragma unroll
-            for (int u = 0; u < N; ++u) own += (uint64_t)weight((first_piece + i) * PIECE + u * 32 + lane, z[u], y[u]);
-            // the lanes' sums, 2^46 at most, added up in two halves
-            const int64_t sum = ((int64_t)__reduce_add_sync(FULL, (unsigned)(own >> 27)) << 27) + __reduce_add_sync(FULL, (unsigned)own & 0x7ffffff);
-            if (lane == 0) sh.weight[i] = sum, all += sum;
+            for (int u = 0; u < N; ++u) {
+                const Weight w = weight((first_piece + i) * PIECE + u * 32 + lane, z[u], y[u]);
+                own.whole += w.whole, own.rest += w.rest;
+            }
+            const int64_t whole = lanes_sum(own.whole), more = lanes_sum(own.rest);
+            if (lane == 0) {
+                sh.weight[i] = whole, rest[i] = more;
+                all += wide(whole, more);
+            }
         });
-        all = block_sum(all, sh.warp_sum[0]);
+        all = block_sum(all);
         if (threadIdx.x == 0) sh.total = all;
         cluster.sync();
         if (threadIdx.x == 0) {
-            int64_t before = 0, total = 0;
+            Wide before = 0, total = 0;
             for (int b = 0; b < blocks; ++b) {
-                const int64_t x = cluster.map_shared_rank(&sh, b)->total;
+                const Wide x = cluster.map_shared_rank(&sh, b)->total;
                 if (b < rank) before += x;
                 total += x;
             }
@@ -497,16 +558,16 @@ struct Walk {
         }
         cluster.sync();                  // the others' totals have been read
         int found = -1;
-        const int64_t at = sh.at, before = sh.before;
+        const Wide at = sh.at, before = sh.before;
         if (warp == 0 && !sh.none && at >= before && at < before + sh.total) {
             // a lane's run of pieces, then its pieces
             const int each = (pieces + 31) / 32, i0 = min(pieces, lane * each), i1 = min(pieces, i0 + each);
-            int64_t mine = 0;
-            for (int i = i0; i < i1; ++i) mine += sh.weight[i];
-            int64_t below = before + scan(mine) - mine;
+            Wide mine = 0;
+            for (int i = i0; i < i1; ++i) mine += wide(sh.weight[i], rest[i]);
+            Wide below = before + scan(mine) - mine;
             if (at >= below && at < below + mine) {
                 int i = i0;
-                while (at >= below + sh.weight[i]) below += sh.weight[i++];
+                for (; at >= below + wide(sh.weight[i], rest[i]); ++i) below += wide(sh.weight[i], rest[i]);
                 sh.piece = first_piece + i;
                 sh.below = below;
             }
@@ -515,9 +576,12 @@ struct Walk {
             T z[N], y[N];
             lane_tokens(weight.p.z, j0, z);
             lane_tokens(weight.q.z, j0, y);
-            int64_t w[N], sum = 0;
+            Wide w[N], sum = 0;
 #pragma unroll
-            for (int u = 0; u < N; ++u) w[u] = weight(j0 + u, z[u], y[u]), sum += w[u];
+            for (int u = 0; u < N; ++u) {
+                const Weight one = weight(j0 + u, z[u], y[u]);
+                w[u] = wide(one.whole, one.rest), sum += w[u];
+            }
             below = sh.below + scan(sum) - sum;
 #pragma unroll
             for (int u = 0; u < N; ++u) {
@@ -633,11 +697,11 @@ struct Walk {
             }
             const int64_t total = all[0] - less(all[1], sh.ratio);
             if (total <= 2 * sh.margin) sh.unsure = true;
-            sh.at = share_of_total(v, max((long long)total, 1ll));
+            sh.fast_at = (int64_t)share_of_total(v, max((long long)total, 1ll));
         }
         cluster.sync();                  // the others' sums have been read
         int found = -1;
-        const int64_t at = sh.at;
+        const int64_t at = sh.fast_at;
         const uint32_t ratio = sh.ratio;
         int64_t P = sh.low_p, Q = sh.low_q;
         if (warp == 0 && !sh.unsure && at >= P - less(Q, ratio) && at < P + sh.fast[0] - less(Q + sh.fast[1], ratio)) {
@@ -935,7 +999,7 @@ __global__ __launch_bounds__(THREADS, THREADS == FEW_THREADS ? 1 : MANY_PER_SM) 
             none = !fast && sh.none;
             if (drawn >= 0) v.accept(s, a, drawn, z, p);
             if (!unsure && (!none || !refused)) break;
-            // once more, exactly; or, with nothing of p - q that 2^-46 could tell, from p
+            // once more, exactly; or, with nothing of p - q that 2^-92 could tell, from p
             if (!unsure) refused = false, q.z = nullptr, without = -1;
             fast = false;
             __syncthreads();
