@@ -1010,6 +1010,11 @@ __global__ __launch_bounds__(THREADS, THREADS == FEW_THREADS ? 1 : MANY_PER_SM) 
     if (writes) v.finish(s, a, !none);
 }
 
+// What a block's pieces may take: MANY_PER_SM blocks find room on an SM.  A cluster gets more blocks until they do, whatever its number of
+// sequences gives it.  bf16, draws alone, 1, 2, 4 and 8 blocks: 700 sequences of 500,000 tokens 710 us, 689, 673, 760, of 700,000 1586, 971, 906,
+// 1007, of 1,500,000 4919, 2724, 1953, 1986; of 2^21 one block has no room at all, 5871, 2544, 2702; 400 of 1,000,000 2754, 1310, 982, 923.
+constexpr size_t DRAW_SMEM = block_smem(MANY_PER_SM);
+
 size_t verify_smem(int64_t cols, int blocks)
 {
     return sizeof(Shared) + 2 * sizeof(int64_t) * (((cols + PIECE - 1) / PIECE + blocks - 1) / blocks + 1);
@@ -1051,6 +1056,7 @@ int pdb_verify(pdb_tokens *t, const pdb_mat *target, const pdb_ids *draft_ids, i
             Shape shape = {};
             shape.threads = threads;
             shape.blocks = cluster_of(clusters, nv, threads, [&](int blocks) { return (int64_t)t->sms * per_sm / blocks; });
+            while (draws && verify_smem(target->cols, shape.blocks) > DRAW_SMEM && shape.blocks < MAX_CLUSTER) shape.blocks *= 2;
             shape.clusters = clusters;
             shape.smem = draws ? verify_smem(target->cols, shape.blocks) : 0;
             return shape;
