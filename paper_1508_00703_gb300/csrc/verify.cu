@@ -10,7 +10,7 @@
 //
 // Which token comes out must not hang on how a row is split or on 32-bit rounding: of 128,000 tokens the running sums of p lie so close that
 // 32-bit ones would pick a neighbour in one draw of thirty.  So acceptances are taken from the statistics only where their error cannot
-// matter (2^-14.6 apart for most tokens), and draws from terms good to 2^-31.5, summed as whole numbers (FastTerm), only where those cannot matter; the others, one
+// matter (2^-15.6 apart for most tokens), and draws from terms good to 2^-31.5, summed as whole numbers (FastTerm), only where those cannot matter; the others, one
 // of 2500 sequences with 5 drafts of 128,000 tokens, are decided on terms good to 2^-40 (exp_two), summed as whole numbers of 2^-92 (Units).
 //
 // What bounds it.  256 sequences of 5 drafts, 128,000 bf16 tokens, four of five accepted: 211 us; 463 MB, 69 us at the copy rate, 115 by
@@ -774,9 +774,15 @@ struct VerifyOut {
 
 // How far the two sides of an acceptance must lie apart for the statistics in 32 bits to decide it, in units of 2^-24 of the larger.
 // An exponential's argument x (in powers of two) is off by 3.2 |x| units (the difference, its product, scale log2(e)), the power by
-// 2.25 |x| + 4.  A row's sum has that by the mean over its mass, where |x| is at most log2(cols) (the entropy) and the references differ by 16, and
-// the roundings of five powers, of chains and joins: 2.25 * 37 + 25 + 91 for 2^21 fp32 tokens, 199 a row.  With divisions and u 411.
-constexpr float SURE_ROWS = 512.0f, SURE_X = 2.25f;
+// 2.25 |x| + 4.  A row's sum has that by the mean over its mass, where |x| is at most log2(cols) (the entropy) and the references differ by 16: 2.25 * 37
+// for 2^21 tokens; five powers' roundings, 25; the additions within a chunk and of joins, 27; and one for each chunk that a thread adds (they can
+// all go one way: 2^21 fp32 tokens in one block of 512, 256 chunks, 520 units between two such rows).  Both rows 271, with divisions and u
+// 284, and twice the chunks.
+constexpr float SURE_X = 2.25f;
+inline float sure_rows(int64_t vectors, int blocks, int threads)
+{
+    return 304.0f + 2.0f * (float)(vectors / blocks / (threads * UNROLL) + 1);
+}
 
 // a row's m, s and its logit of the drafted token, from k_verify_rows
 struct Given {
@@ -788,7 +794,7 @@ enum { DRAW_REST = 0, DRAW_TARGET = 1, NOTHING = 2, EXACTLY = 3 };
 
 // whether u q < p, where the statistics can tell it (sure)
 template <typename T>
-__device__ __forceinline__ bool accepts(const Row<T> &p, const Row<T> &q, float z, float zq, float u, bool &sure)
+__device__ __forceinline__ bool accepts(const Row<T> &p, const Row<T> &q, float z, float zq, float u, float sure_rows, bool &sure)
 {
     const float x = __fmul_rn(__fsub_rn(z, p.m), __fmul_rn(p.scale, LOG2E)), right = __fdiv_rn(ex2(x), p.s);
     float left = u, y = 0.0f;
@@ -797,7 +803,7 @@ __device__ __forceinline__ bool accepts(const Row<T> &p, const Row<T> &q, float 
         left = __fmul_rn(u, __fdiv_rn(ex2(y), q.s));
     }
     // a power below the normal numbers is 0, however far
-    const float margin = __fmaf_rn(SURE_X, fminf(-x, 150.0f) + fminf(-y, 150.0f), SURE_ROWS);
+    const float margin = __fmaf_rn(SURE_X, fminf(-x, 150.0f) + fminf(-y, 150.0f), sure_rows);
     const float more = fmaxf(left, right);
     sure = fabsf(left - right) > 0x1p-24f * margin * more && more > 1e-30f;
     return left < right;
@@ -805,12 +811,12 @@ __device__ __forceinline__ bool accepts(const Row<T> &p, const Row<T> &q, float 
 
 // what a position with its statistics comes to; -1 where its draft is surely accepted
 template <typename T>
-__device__ __forceinline__ int decide(const Row<T> &p, const Row<T> &q, int t, float z, float zq, float u)
+__device__ __forceinline__ int decide(const Row<T> &p, const Row<T> &q, int t, float z, float zq, float u, float sure_rows)
 {
     if (!p.valid()) return NOTHING;
     if (t < 0 || (q.z && !q.valid())) return DRAW_TARGET;            // the drafts end here
     bool sure;
-    const bool good = accepts(p, q, z, zq, u, sure);
+    const bool good = accepts(p, q, z, zq, u, sure_rows, sure);
     return !sure ? EXACTLY : good ? -1 : DRAW_REST;
 }
 
@@ -841,7 +847,7 @@ struct Verify {
     int cols, D;
     Ids ids;
     int64_t n;
-    float scale, draft_scale;
+    float scale, draft_scale, sure_rows;
     const float *accept_u, *draw_u;
     VerifyOut out;
     const Given *given;                 // of all rows, where k_verify_rows has been there
@@ -954,7 +960,7 @@ __global__ __launch_bounds__(THREADS, THREADS == FEW_THREADS ? 1 : MANY_PER_SM) 
             z = sh.z[turn][0], zq = sh.z[turn][1];
         }
         const float u = t >= 0 ? sh.u[a] : 0.0f;
-        int what = decide(p, q, t, z, zq, u);
+        int what = decide(p, q, t, z, zq, u, v.sure_rows);
         if (what == EXACTLY) {
             if (!exact) walk.fill_table();
             exact = true;
@@ -1071,12 +1077,16 @@ int pdb_verify(pdb_tokens *t, const pdb_mat *target, const pdb_ids *draft_ids, i
         // the statistics of all rows at once where the SMs would not be busy with a position of each sequence: a launch more, fewer rounds
         const int64_t rows = target->rows + (draft ? drafts : 0);
         if (n_drafts > 0 && n * 2 <= t->sms && rows <= VERIFY_ROWS) {
+            const Shape shape = shaped(rows, 512, 2, false);
             v.given = (const Given *)t->given;
-            const int rc = launch_rows(k_verify_rows<T, 512>, shaped(rows, 512, 2, false), s, v, (Given *)t->given);
+            v.sure_rows = sure_rows(nv, shape.blocks, shape.threads);
+            const int rc = launch_rows(k_verify_rows<T, 512>, shape, s, v, (Given *)t->given);
             if (rc != PDB_OK) return rc;
         }
-        if (n * MAX_CLUSTER <= t->sms) return launch_rows(k_verify<T, FEW_THREADS>, shaped(n, FEW_THREADS, 2, true), s, v);
-        return launch_rows(k_verify<T, MANY_THREADS>, shaped(n, MANY_THREADS, 8, true), s, v);
+        const bool few = n * MAX_CLUSTER <= t->sms;
+        const Shape shape = few ? shaped(n, FEW_THREADS, 2, true) : shaped(n, MANY_THREADS, 8, true);
+        if (!v.given) v.sure_rows = sure_rows(nv, shape.blocks, shape.threads);
+        return few ? launch_rows(k_verify<T, FEW_THREADS>, shape, s, v) : launch_rows(k_verify<T, MANY_THREADS>, shape, s, v);
     });
 }
 
