@@ -582,7 +582,8 @@ int pdb_distill(pdb_tokens *t, const pdb_mat *logits, const pdb_ids *top_ids, co
  * The random numbers are the caller's, in [0, 1); others count as their nearest end in the draw.  What 32-bit statistics (of which logp is formed, as in
  * pdb_logprobs) or terms good to 2^-31 cannot tell apart is decided on terms good to 2^-40 of themselves, summed as whole numbers of 2^-92 of the rows'
  * sums (weights below 2^-90 of them may count as none), so that the tokens do not depend on how rows are split.
- * Rows behind the first refusal are not read.  PDB_ETOOBIG above 64 drafts or
+ * Rows behind the first refusal, and behind a sequence's last draft, change no result, but a call may read
+ * them (with few sequences, whose rows are all read at once).  PDB_ETOOBIG above 64 drafts or
  * 2^21 tokens.  These are the draws a program makes with its models between the reads of Definition 3. */
 int pdb_verify(pdb_tokens *t, const pdb_mat *target, const pdb_ids *draft_ids, int64_t n_drafts, const pdb_mat *draft,
                float scale, float draft_scale, const float *accept_u, const float *draw_u, int32_t *tokens, int32_t *accepted,

@@ -5,8 +5,9 @@
 // (or the drafts end) the token is drawn from r = max(p - q, 0) (or r = p): the smallest j with r_0 + .. + r_j > v sum r.
 // The tokens are then distributed as if drawn from p one after the other (Leviathan, Kalman, Matias 2023; Chen et al. 2023).
 //
-// One cluster of blocks walks a sequence's positions, so no row behind the first refusal is read.  A position's rows take one pass of
-// running softmax statistics (rows.cuh), the draw one more over the rows of its position, which L2 mostly still holds.
+// One cluster of blocks walks a sequence's positions up to the first refusal.  A position's rows take one pass of running softmax
+// statistics (rows.cuh), the draw one more over the rows of its position, which L2 mostly still holds.  Of few sequences the statistics of all
+// rows are formed at once before that (k_verify_rows), those behind a refusal or a sequence's last draft too.
 //
 // Which token comes out must not hang on how a row is split or on 32-bit rounding: of 128,000 tokens the running sums of p lie so close that
 // 32-bit ones would pick a neighbour in one draw of thirty.  So acceptances are taken from the statistics only where their error cannot
