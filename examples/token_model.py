@@ -43,7 +43,7 @@ class Model:
     def __init__(self, vocab, dim, context, tokens, seed, spread):
         g = torch.Generator(device="cuda")
         g.manual_seed(seed)
-        self.context, self.scale = context, math.sqrt(dim)
+        self.context, self.tokens, self.scale = context, tokens, math.sqrt(dim)
         self.table = torch.randn(vocab, dim, device="cuda", generator=g) * spread / math.sqrt(dim)
         self.out = torch.randn(vocab, dim, device="cuda", generator=g) * spread / math.sqrt(dim)
         self.tok = pdb.pdb_tokens_create(tokens * context, dim)
@@ -165,6 +165,12 @@ class Mixed(Model):
         return loss
 
 
+def _logits(model, ids):
+    """The logits behind any number of contexts, as many at a time as the model is made for."""
+    parts = [model.logits(part)[1] for part in ids.split(model.tokens)]
+    return parts[0] if len(parts) == 1 else torch.cat(parts)
+
+
 def speculate(target, draft, ids, rounds=8, drafts=4, seed=0):
     """Text behind the contexts ids (n, context), `rounds` rounds of up to drafts + 1 tokens, distributed as the target's: the
     tokens (n, rounds, drafts + 1), -1 behind a round's last, and the number of accepted drafts (n, rounds)."""
@@ -177,11 +183,11 @@ def speculate(target, draft, ids, rounds=8, drafts=4, seed=0):
         seq = torch.cat([ids, torch.zeros(n, drafts, device="cuda", dtype=ids.dtype)], 1)
         rows, drawn = [], torch.empty(n, 1, device="cuda", dtype=torch.int32)
         for d in range(drafts):
-            rows.append(draft.logits(seq[:, d:d + context].contiguous())[1])
+            rows.append(_logits(draft, seq[:, d:d + context].contiguous()))
             pdb.pdb_verify(tok, rows[-1], nothing.int(), nothing, torch.rand(n, device="cuda", generator=g), drawn)
             seq[:, context + d] = drawn[:, 0]
         every = seq.unfold(1, context, 1).reshape(-1, context)
-        z = target.logits(every)[1]
+        z = _logits(target, every)
         y = torch.stack(rows, 1).view(n * drafts, -1)
         tokens, accepted = torch.empty(n, drafts + 1, device="cuda", dtype=torch.int32), torch.empty(n, device="cuda", dtype=torch.int32)
         pdb.pdb_verify(tok, z, seq[:, context:], torch.rand(n, drafts, device="cuda", generator=g),
