@@ -186,7 +186,7 @@ def speculate(target, draft, ids, rounds=8, drafts=4, seed=0):
             rows.append(_logits(draft, seq[:, d:d + context].contiguous()))
             pdb.pdb_verify(tok, rows[-1], nothing.int(), nothing, torch.rand(n, device="cuda", generator=g), drawn)
             seq[:, context + d] = drawn[:, 0]
-        every = seq.unfold(1, context, 1).reshape(-1, context)
+        every = seq.unfold(1, context, 1).reshape(-1, context).contiguous()      # (of one sequence it is a view)
         z = _logits(target, every)
         y = torch.stack(rows, 1).view(n * drafts, -1)
         tokens, accepted = torch.empty(n, drafts + 1, device="cuda", dtype=torch.int32), torch.empty(n, device="cuda", dtype=torch.int32)
