@@ -313,8 +313,8 @@ int pdb_clip_plan_build(const pdb_mat *grads, const pdb_mat *outs, int64_t n, pd
     if (n < 0 || (n > 0 && (!grads || !outs))) return PDB_EINVAL;
     int64_t total = 0;
     for (int64_t i = 0; i < n; ++i) {
-        int rc = check_mat(grads + i);
-        rc = rc ? rc : check_mat(outs + i);
+        int rc = check_mat(grads + i, MOST_ELEMENTS, MOST_ELEMENTS);
+        rc = rc ? rc : check_mat(outs + i, MOST_ELEMENTS, MOST_ELEMENTS);
         if (rc != PDB_OK) return rc;
         if (grads[i].rows != outs[i].rows || grads[i].cols != outs[i].cols) return PDB_EINVAL;
         if (grads[i].rows > MOST_ELEMENTS / std::max<int64_t>(1, grads[i].cols)) return PDB_ETOOBIG;

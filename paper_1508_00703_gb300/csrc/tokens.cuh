@@ -62,14 +62,14 @@ inline int type_bytes(int type) { return type == PDB_TYPE_FLOAT ? 4 : 2; }
 // elements from the first row's start to the last one's: what any memory holds, and far from the 64-bit range's end
 constexpr int64_t MOST_EXTENT = (int64_t)1 << 58;
 
-// PDB_OK for a matrix that the calls accept
-inline int check_mat(const pdb_mat *m)
+// PDB_OK for a matrix that the calls accept (pdb_clip, which cuts matrices into pieces, more rows and columns than the others)
+inline int check_mat(const pdb_mat *m, int64_t most_rows = INT32_MAX, int64_t most_cols = INT32_MAX / 2)
 {
     if (!m || m->rows < 0 || m->cols < 0) return PDB_EINVAL;
     if (m->type != PDB_TYPE_FLOAT && m->type != PDB_TYPE_BFLOAT && m->type != PDB_TYPE_HALF) return PDB_EINVAL;
     if (m->rows > 1 && m->stride < m->cols) return PDB_EINVAL;
     if (m->rows > 0 && m->cols > 0 && (!m->data || (uintptr_t)m->data % type_bytes(m->type) != 0)) return PDB_EINVAL;
-    if (m->cols > INT32_MAX / 2 || m->rows > INT32_MAX) return PDB_ETOOBIG;
+    if (m->cols > most_cols || m->rows > most_rows) return PDB_ETOOBIG;
     if (m->rows > 1 && m->stride > MOST_EXTENT / (m->rows - 1)) return PDB_EINVAL;
     return PDB_OK;
 }
