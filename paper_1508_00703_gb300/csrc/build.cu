@@ -904,7 +904,8 @@ const char *pdb_strerror(int code)
     case PDB_ETOOBIG:
         return "problem beyond a fixed limit (allocation-free scratch: 2^20 features; CHAIN: 256 ids per example "
                "unless the weights fit in shared memory; a feature in 2^29 positions or more; token operators: the handle's "
-               "tokens or columns, 64 alternatives, 1024 slots, 2^21 tokens in pdb_distill)";
+               "tokens or columns, 64 alternatives, 1024 slots, 2^21 tokens in pdb_distill; 64 drafts, 2^21 tokens in pdb_verify; 64 slots, 4096 experts in "
+               "pdb_route; 2^40 elements in pdb_clip)";
     default: return "unknown error";
     }
 }

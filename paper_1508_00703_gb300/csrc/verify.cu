@@ -12,11 +12,11 @@
 // Which token comes out must not hang on how a row is split or on 32-bit rounding: of 128,000 tokens the running sums of p lie so close that
 // 32-bit ones would pick a neighbour in one draw of thirty.  So acceptances are taken from the statistics only where their error cannot
 // matter (2^-15.6 apart for most tokens), and draws from terms good to 2^-31.5, summed as whole numbers (FastTerm), only where those cannot matter; the others, one
-// of 2500 sequences with 5 drafts of 128,000 tokens, are decided on terms good to 2^-40 (exp_two), summed as whole numbers of 2^-92 (Units).
+// of 1300 sequences with 5 drafts of 128,000 tokens (12 of 15,360), are decided on terms good to 2^-40 (exp_two), summed as whole numbers of 2^-92 (Units).
 //
-// What bounds it.  256 sequences of 5 drafts, 128,000 bf16 tokens, four of five accepted: 211 us; 463 MB, 69 us at the copy rate, 115 by
+// What bounds it.  256 sequences of 5 drafts, 128,000 bf16 tokens, four of five accepted: 207 us; 463 MB, 69 us at the copy rate, 115 by
 // a kernel that walks only (cluster barriers between positions: 4.1 TB/s), and 100 by one that draws only (71 instructions for a token of both
-// rows, at 2.1 of 4 issued a cycle).  One sequence of 4 drafts: 15.7 us, two launches, seven cluster barriers and four passes of latency.
+// rows, at 2.1 of 4 issued a cycle).  One sequence of 4 drafts: 15 us, two launches, seven cluster barriers and four passes of latency.
 #include <algorithm>
 #include <cmath>
 
@@ -918,8 +918,10 @@ __device__ __forceinline__ bool in_reach(const Row<T> &r)
 }
 
 // A cluster for each sequence: its walk (bound by memory) up to the first position that is not accepted, and its draw (bound by instructions).
-// On an SM some sequences walk while others draw; in a kernel each they take as long, and the few that have to be
-// exact (1 of 2500, 50 us by eight blocks) are not hidden then (256 x 5 drafts x 128,000 bf16: 115 us, 100, 50).
+// On an SM some sequences walk while others draw; in a kernel each they take as long (256 x 5 drafts x 128,000 bf16: 115 us and 100), and the
+// few that have to be exact are not hidden then.  An exact draw takes three passes more by the cluster that has the sequence: 38 us by eight blocks
+// of 512; at the end of the launch up to 52 us of 159 (152 sequences, eight blocks of 256), 75 of 207 (256, four), 155 of 396 (608, two), 285 of
+// 559 (912, one), in its middle 4, 15, 31 and 194.
 constexpr int MANY_THREADS = 256, FEW_THREADS = 512, MANY_PER_SM = 3;
 
 template <typename T, int THREADS>
